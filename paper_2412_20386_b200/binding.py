@@ -137,6 +137,21 @@ def _load_native():
     return _native
 
 
+_native_block = None
+
+
+def _load_native_block():
+    """The same module with the entry points of ``include/ptq_block.h`` handed over too (``block.py``)."""
+    global _native_block
+    if _native_block is None:
+        L, native = load_library(), _load_native()
+        native.bind_block(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.ptq_scan_workspace_bytes, L.ptq_scan_forward, L.ptq_scan_backward, L.ptq_norm_forward, L.ptq_norm_workspace_bytes,
+            L.ptq_norm_backward, L.ptq_conv_forward, L.ptq_conv_workspace_bytes, L.ptq_conv_backward)))
+        _native_block = native
+    return _native_block
+
+
 def _check(status: int):
     if status != 0:
         raise PtqError(status, load_library().ptq_last_error().decode("utf-8", "replace"))

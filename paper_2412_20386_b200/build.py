@@ -20,10 +20,11 @@ from concurrent.futures import ThreadPoolExecutor
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _CSRC = os.path.join(_HERE, "csrc")
 _SO = os.path.join(_HERE, "libptq_linear.so")
-_SOURCES = ["ptq_api.cu"]
+_SOURCES = ["ptq_api.cu", "ptq_block.cu"]
 _DEPS = ["ptq_api.cu", "ptq_gemm.cuh", "ptq_fused.cuh", "ptq_small.cuh", "ptq_short_k.cuh", "ptq_quantize.cuh", "ptq_quantize_dynamic.cuh",
-         "ptq_calibrate.cuh", "ptq_probe.cuh", "ptx_sm100.cuh",
-         os.path.join("..", "..", "include", "ptq_linear.h")]
+         "ptq_calibrate.cuh", "ptq_probe.cuh", "ptx_sm100.cuh", "ptq_host.h",
+         "ptq_block.cu", "ptq_block.cuh", "ptq_scan.cuh", "ptq_norm.cuh", "ptq_conv.cuh",
+         os.path.join("..", "..", "include", "ptq_linear.h"), os.path.join("..", "..", "include", "ptq_block.h")]
 
 
 def nvcc_path() -> str:
@@ -35,7 +36,8 @@ def nvcc_path() -> str:
 
 _EXT = os.path.join(_HERE, "_ptq_torch.so")
 _EXT_STAMP = os.path.join(_HERE, "_build", "_ptq_torch.versions")     # what the extension was compiled against
-_EXT_DEPS = ["ptq_torch.cpp", os.path.join("..", "..", "include", "ptq_linear.h")]
+_EXT_SOURCES = ["ptq_torch.cpp", "ptq_torch_block.cpp"]
+_EXT_DEPS = _EXT_SOURCES + ["ptq_torch.h", os.path.join("..", "..", "include", "ptq_linear.h"), os.path.join("..", "..", "include", "ptq_block.h")]
 
 
 def up_to_date(target: str = _SO, deps=_DEPS) -> bool:
@@ -71,7 +73,7 @@ def _run(cmd, target: str, verbose: bool) -> None:
 
 def _build_library(verbose: bool) -> None:
     cmd = [nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-cudart", "static",
+           "-shared", "-Xcompiler", "-fPIC", "-cudart", "static", "--threads", "0",
            "-Xptxas", "-v" if verbose else "-warn-spills"]
     _run(cmd + [os.path.join(_CSRC, s) for s in _SOURCES], _SO, verbose)
 
@@ -85,7 +87,7 @@ def _build_extension(verbose: bool) -> None:
            "-isystem", os.path.join(root, "include"),
            "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
            "-isystem", os.path.join(cuda, "include"), "-isystem", sysconfig.get_paths()["include"],
-           os.path.join(_CSRC, "ptq_torch.cpp"), "-L" + os.path.join(root, "lib"),
+           *(os.path.join(_CSRC, f) for f in _EXT_SOURCES), "-L" + os.path.join(root, "lib"),
            "-Wl,-rpath," + os.path.join(root, "lib"),
            "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
     _run(cmd, _EXT, verbose)

@@ -8,7 +8,6 @@
 
 #include <atomic>
 #include <cmath>
-#include <cstdarg>
 #include <cstdio>
 #include <cstring>
 #include <memory>
@@ -21,6 +20,7 @@
 #include "ptq_calibrate.cuh"
 #include "ptq_fused.cuh"
 #include "ptq_gemm.cuh"
+#include "ptq_host.h"
 #include "ptq_probe.cuh"
 #include "ptq_quantize.cuh"
 #include "ptq_quantize_dynamic.cuh"
@@ -29,36 +29,7 @@
 
 namespace {
 
-thread_local char g_err[512] = "";
-std::atomic<unsigned long long> g_launches{0};
-
-ptq_status_t fail(ptq_status_t st, const char *fmt, ...)
-{
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_err, sizeof(g_err), fmt, ap);
-    va_end(ap);
-    return st;
-}
-
-#define PTQ_CUDA(...)                                                                          \
-    do {                                                                                       \
-        cudaError_t e_ = (__VA_ARGS__);                                                        \
-        if (e_ != cudaSuccess)                                                                 \
-            return fail(e_ == cudaErrorMemoryAllocation ? PTQ_ERR_NOMEM : PTQ_ERR_CUDA,        \
-                        "%s failed: %s", #__VA_ARGS__, cudaGetErrorString(e_));                \
-    } while (0)
-
-// The body of an entry point that allocates host memory: no exception may leave a C function.
-template <class Fn>
-ptq_status_t no_throw(Fn fn)
-{
-    try {
-        return fn();
-    } catch (const std::exception &) {      // std::bad_alloc is all that these bodies raise
-        return fail(PTQ_ERR_NOMEM, "host allocation failed");
-    }
-}
+using namespace ptq_host;
 
 // cuTensorMapEncodeTiled is reached through the runtime's driver entry point query, so the
 // library has no link-time dependency on libcuda and loads on machines without a driver.

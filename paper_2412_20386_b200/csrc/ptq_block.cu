@@ -1,0 +1,582 @@
+// Host side of the C ABI declared in include/ptq_block.h: argument checks, how the work is cut, kernel launches.
+#include "../../include/ptq_block.h"
+
+#include <algorithm>
+#include <cmath>
+
+#include "ptq_conv.cuh"
+#include "ptq_host.h"
+#include "ptq_norm.cuh"
+#include "ptq_scan.cuh"
+
+namespace {
+
+using namespace ptq_host;
+
+constexpr int kSms = 148;             // of the one GPU that the library is for; only cuts of the work go by it
+constexpr long long kMaxGrid = 0x7fffffffll;
+
+ptq_status_t check_arch()
+{
+    constexpr int kMaxDevices = 64;
+    static std::atomic<int> known[kMaxDevices] = {};      // 0: not asked yet, 1: sm_100, 2: another one
+    int dev = -1;
+    PTQ_CUDA(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= kMaxDevices) return fail(PTQ_ERR_CUDA, "device index %d out of range", dev);
+    int k = known[dev].load(std::memory_order_relaxed);
+    if (k == 0) {
+        int major = 0, minor = 0;
+        PTQ_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev));
+        PTQ_CUDA(cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev));
+        k = major == 10 && minor == 0 ? 1 : 2;
+        known[dev].store(k, std::memory_order_relaxed);
+    }
+    return k == 1 ? PTQ_OK : fail(PTQ_ERR_ARCH, "device %d is not compute capability 10.0", dev);
+}
+
+ptq_status_t launched()
+{
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    PTQ_CUDA(cudaGetLastError());
+    return PTQ_OK;
+}
+
+#define PTQ_TRY(...)                                  \
+    do {                                              \
+        const ptq_status_t st_ = (__VA_ARGS__);       \
+        if (st_ != PTQ_OK) return st_;                \
+    } while (0)
+
+int elem_bytes(int dtype) { return dtype == PTQ_F32 ? 4 : 2; }
+bool dtype_ok(int dtype) { return dtype == PTQ_F16 || dtype == PTQ_BF16 || dtype == PTQ_F32; }
+
+// Every pointer that is given on a multiple of `bytes`.
+bool aligned(std::initializer_list<const void *> ps, int bytes)
+{
+    for (const void *p : ps)
+        if (reinterpret_cast<uintptr_t>(p) % bytes) return false;
+    return true;
+}
+bool multiples(std::initializer_list<int64_t> pitches, int unit)
+{
+    for (int64_t v : pitches)
+        if (v % unit) return false;
+    return true;
+}
+bool not_negative(std::initializer_list<int64_t> pitches)
+{
+    for (int64_t v : pitches)
+        if (v < 0) return false;
+    return true;
+}
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+template <class Fn>
+ptq_status_t with_type(int dtype, Fn fn)
+{
+    if (dtype == PTQ_F16) return fn(__half());
+    if (dtype == PTQ_BF16) return fn(__nv_bfloat16());
+    return fn(0.0f);
+}
+
+// ---------------------------------------------------------------------------------------------------- scan
+// Lanes per channel and states per lane.
+struct ScanSplit {
+    int lanes, states;
+};
+ScanSplit scan_split(int states)
+{
+    if (states <= 4) return {1, states <= 1 ? 1 : states <= 2 ? 2 : 4};
+    return {states <= 8 ? 2 : states <= 16 ? 4 : 8, 4};
+}
+
+// How a call is cut: threads of a CTA, CTAs per group, chunks of the sequences.
+struct ScanPlan {
+    int threads, group_blocks, chunk_len, chunks;
+    long long ctas() const { return ctas_; }
+    long long ctas_;
+};
+ScanPlan scan_plan(const ptq_scan_t &s)
+{
+    const int lanes = scan_split(s.states).lanes, per_group = s.channels / s.groups;
+    ScanPlan p;
+    p.threads = lanes == 1 ? 128 : 256;
+    const auto blocks = [&](int threads) { return ceil_div(per_group, threads / lanes); };
+    if (lanes < 8 && static_cast<long long>(s.batch) * s.groups * blocks(p.threads) < kSms && s.length < 512) p.threads = 64;
+    p.group_blocks = static_cast<int>(blocks(p.threads));
+    const long long ctas = static_cast<long long>(s.batch) * s.groups * p.group_blocks;
+    long long chunks = ctas >= 2 * kSms ? 1 : std::min(ceil_div(4 * kSms, ctas), ceil_div(s.length, 256));
+    p.chunk_len = static_cast<int>(ceil_div(ceil_div(s.length, chunks), 64) * 64);
+    p.chunks = static_cast<int>(ceil_div(s.length, p.chunk_len));
+    p.ctas_ = ctas * p.chunks;
+    return p;
+}
+
+ptq_status_t scan_check(const ptq_scan_t *s)
+{
+    if (!s) return fail(PTQ_ERR_NULL, "the call's description is NULL");
+    if (!s->u || !s->delta || !s->B || !s->C || !s->A) return fail(PTQ_ERR_NULL, "u, delta, A, B or C is NULL");
+    if (!dtype_ok(s->dtype)) return fail(PTQ_ERR_VALUE, "unknown type %d", s->dtype);
+    if (s->batch < 1 || s->length < 1 || s->length > PTQ_MAX_LENGTH || s->channels < 1 || s->channels > PTQ_MAX_CHANNELS || s->states < 1 ||
+        s->states > PTQ_MAX_STATES || s->groups < 1)
+        return fail(PTQ_ERR_SHAPE, "batch %d, length %d, channels %d, states %d, groups %d out of range", s->batch, s->length, s->channels, s->states,
+                    s->groups);
+    if (s->channels % s->groups) return fail(PTQ_ERR_SHAPE, "%d channels do not make %d groups", s->channels, s->groups);
+    if (s->flags & ~(PTQ_SCAN_SOFTPLUS | PTQ_SEQ_REVERSE)) return fail(PTQ_ERR_VALUE, "unknown flags %u", s->flags);
+    if (!not_negative({s->u_pitch[0], s->u_pitch[1], s->delta_pitch[0], s->delta_pitch[1], s->z_pitch[0], s->z_pitch[1], s->B_pitch[0], s->B_pitch[1],
+                       s->B_pitch[2], s->C_pitch[0], s->C_pitch[1], s->C_pitch[2]}))
+        return fail(PTQ_ERR_SHAPE, "a pitch is negative");
+    if (!aligned({s->u, s->delta, s->z, s->B, s->C}, elem_bytes(s->dtype)) || !aligned({s->A, s->D, s->delta_bias, s->state, s->lengths}, 4))
+        return fail(PTQ_ERR_ALIGN, "an input is not aligned to its type");
+    if (scan_plan(*s).ctas() > kMaxGrid) return fail(PTQ_ERR_SHAPE, "the batch is too large for one launch");
+    return PTQ_OK;
+}
+
+ptq::ScanParams scan_params(const ptq_scan_t &s, const ScanPlan &plan)
+{
+    ptq::ScanParams p = {};
+    p.u = s.u;
+    p.delta = s.delta;
+    p.z = s.z;
+    p.B = s.B;
+    p.C = s.C;
+    p.u_b = s.u_pitch[0];
+    p.u_l = s.u_pitch[1];
+    p.delta_b = s.delta_pitch[0];
+    p.delta_l = s.delta_pitch[1];
+    p.z_b = s.z_pitch[0];
+    p.z_l = s.z_pitch[1];
+    p.B_b = s.B_pitch[0];
+    p.B_l = s.B_pitch[1];
+    p.B_g = s.B_pitch[2];
+    p.C_b = s.C_pitch[0];
+    p.C_l = s.C_pitch[1];
+    p.C_g = s.C_pitch[2];
+    p.A = s.A;
+    p.D = s.D;
+    p.delta_bias = s.delta_bias;
+    p.state = s.state;
+    p.lengths = s.lengths;
+    p.batch = s.batch;
+    p.length = s.length;
+    p.channels = s.channels;
+    p.states = s.states;
+    p.groups = s.groups;
+    p.group_channels = s.channels / s.groups;
+    p.group_blocks = plan.group_blocks;
+    p.chunk_len = plan.chunk_len;
+    p.chunks = plan.chunks;
+    p.flags = s.flags;
+    const int unit = 16 / elem_bytes(s.dtype);
+    p.whole = aligned({s.u, s.delta, s.z}, 16) && multiples({p.u_b, p.u_l, p.delta_b, p.delta_l, p.z ? p.z_b : 0, p.z ? p.z_l : 0}, unit) &&
+              s.channels % unit == 0 && p.group_channels % unit == 0;
+    p.whole_n = s.states % 4 == 0 && aligned({s.A, s.state}, 16);
+    return p;
+}
+
+// Workspace: slots and sums of the chunks, and for the backward pass the shares of the CTAs.
+struct ScanSpace {
+    size_t slots, sums, part_A, part_D, part_bias, part_BC, bytes;
+};
+ScanSpace scan_space(const ptq_scan_t &s, const ScanPlan &plan, bool backward)
+{
+    ScanSpace w = {};
+    size_t at = 0;
+    const auto take = [&](size_t floats) {
+        const size_t here = at;
+        at += padded(floats * 4);
+        return here;
+    };
+    const size_t rows = static_cast<size_t>(s.batch) * s.channels;
+    if (plan.chunks > 1) {
+        w.slots = take(rows * plan.chunks * s.states);
+        w.sums = take(rows * plan.chunks);
+    }
+    if (backward) {
+        w.part_A = take(rows * plan.chunks * s.states);
+        w.part_D = take(rows * plan.chunks);
+        w.part_bias = take(rows * plan.chunks);
+        if (plan.group_blocks > 1) w.part_BC = take(static_cast<size_t>(s.groups) * plan.group_blocks * s.batch * s.length * 2 * s.states);
+    }
+    w.bytes = at;
+    return w;
+}
+
+template <class Fn>
+ptq_status_t with_split(int states, Fn fn)
+{
+    const ScanSplit sp = scan_split(states);
+    using std::integral_constant;
+    if (sp.lanes == 1 && sp.states == 1) return fn(integral_constant<int, 1>(), integral_constant<int, 1>());
+    if (sp.lanes == 1 && sp.states == 2) return fn(integral_constant<int, 2>(), integral_constant<int, 1>());
+    if (sp.lanes == 1) return fn(integral_constant<int, 4>(), integral_constant<int, 1>());
+    if (sp.lanes == 2) return fn(integral_constant<int, 4>(), integral_constant<int, 2>());
+    if (sp.lanes == 4) return fn(integral_constant<int, 4>(), integral_constant<int, 4>());
+    return fn(integral_constant<int, 4>(), integral_constant<int, 8>());
+}
+
+size_t scan_forward_smem(int threads, int lanes, int states) { return static_cast<size_t>(8) * threads * 8 + static_cast<size_t>(8) * lanes * lanes * states * 2 * 4; }
+size_t scan_backward_smem(int threads, int lanes, int states)
+{
+    const size_t rows = ptq::kScanHistory, np = static_cast<size_t>(lanes) * states;
+    return rows * (threads / lanes) * 16 + rows * np * 8 + (threads / 32) * rows * 2 * np * 4;
+}
+
+template <int kMode>
+ptq_status_t launch_scan(const ptq_scan_t &s, const ScanPlan &plan, const ptq::ScanParams &p, cudaStream_t stream)
+{
+    const long long ctas = kMode == ptq::kScanForward ? plan.ctas() : plan.ctas() / plan.chunks * (plan.chunks - 1);
+    return with_type(s.dtype, [&](auto t) {
+        using T = decltype(t);
+        return with_split(s.states, [&](auto ns, auto lanes) {
+            constexpr int kNS = decltype(ns)::value, kS = decltype(lanes)::value;
+            ptq::ptq_scan_kernel<T, kNS, kS, kMode>
+                <<<static_cast<unsigned>(ctas), plan.threads, scan_forward_smem(plan.threads, kS, kNS), stream>>>(p);
+            return launched();
+        });
+    });
+}
+
+ptq_status_t check_space(const void *workspace, size_t have, size_t need)
+{
+    if (need == 0) return PTQ_OK;
+    if (!workspace) return fail(PTQ_ERR_NULL, "workspace is NULL");
+    if (!aligned({workspace}, 16)) return fail(PTQ_ERR_ALIGN, "workspace is not 16-byte aligned");
+    if (have < need) return fail(PTQ_ERR_SHAPE, "workspace has %zu bytes, %zu are needed", have, need);
+    return PTQ_OK;
+}
+
+// ---------------------------------------------------------------------------------------------------- norm
+ptq_status_t norm_check(const ptq_norm_t *n)
+{
+    if (!n) return fail(PTQ_ERR_NULL, "the call's description is NULL");
+    if (!n->x) return fail(PTQ_ERR_NULL, "x is NULL");
+    if (!dtype_ok(n->dtype) || !dtype_ok(n->residual_dtype)) return fail(PTQ_ERR_VALUE, "unknown type");
+    if (n->residual_dtype != n->dtype && n->residual_dtype != PTQ_F32) return fail(PTQ_ERR_VALUE, "the residual has x's type or binary32");
+    if (n->rows < 1 || n->cols < 1 || n->cols > PTQ_MAX_NORM_COLS || n->rows > (1ll << 40))
+        return fail(PTQ_ERR_SHAPE, "rows %lld, cols %d out of range", static_cast<long long>(n->rows), n->cols);
+    if (n->flags & ~(PTQ_NORM_LAYER | PTQ_NORM_GATE_OUT)) return fail(PTQ_ERR_VALUE, "unknown flags %u", n->flags);
+    if (!(n->eps >= 0.0f) || std::isinf(n->eps)) return fail(PTQ_ERR_VALUE, "eps must be finite and not negative");
+    if (!not_negative({n->x_pitch, n->residual_pitch, n->gate_pitch})) return fail(PTQ_ERR_SHAPE, "a pitch is negative");
+    if (!aligned({n->x, n->gate}, elem_bytes(n->dtype)) || !aligned({n->residual}, elem_bytes(n->residual_dtype)) ||
+        !aligned({n->weight, n->bias, n->scale}, 4))
+        return fail(PTQ_ERR_ALIGN, "an input is not aligned to its type");
+    return PTQ_OK;
+}
+ptq::NormParams norm_params(const ptq_norm_t &n)
+{
+    ptq::NormParams p = {};
+    p.x = n.x;
+    p.residual = n.residual;
+    p.gate = n.gate;
+    p.x_l = n.x_pitch;
+    p.residual_l = n.residual_pitch;
+    p.gate_l = n.gate_pitch;
+    p.weight = n.weight;
+    p.bias = n.bias;
+    p.scale = n.scale;
+    p.rows = n.rows;
+    p.cols = n.cols;
+    p.gate_at = !n.gate ? ptq::kGateNone : n.flags & PTQ_NORM_GATE_OUT ? ptq::kGateOut : ptq::kGateIn;
+    p.eps = n.eps;
+    p.inv_cols = static_cast<float>(1.0 / n.cols);
+    p.layer = n.flags & PTQ_NORM_LAYER;
+    const int unit = 16 / elem_bytes(n.dtype), runit = 16 / elem_bytes(n.residual_dtype);
+    p.whole = aligned({n.x, n.residual, n.gate}, 16) && n.x_pitch % unit == 0 && (!n.gate || n.gate_pitch % unit == 0) &&
+              (!n.residual || n.residual_pitch % runit == 0) && n.cols % unit == 0;
+    return p;
+}
+// Rows that a CTA takes at a time, and CTAs.
+struct NormPlan {
+    int threads, rows, ctas;
+};
+NormPlan norm_plan(const ptq_norm_t &n, bool backward)
+{
+    NormPlan p;
+    p.threads = static_cast<int>(ceil_div(n.cols, 256)) * 32;
+    const int batch = backward ? 2 : 4;
+    p.rows = p.threads > 256 || n.rows <= 8 * kSms ? 1 : batch;
+    const long long resident = std::max(1, std::min(32, (backward ? 512 : 768) / p.threads)) * static_cast<long long>(kSms);
+    p.ctas = static_cast<int>(std::min(ceil_div(n.rows, p.rows), resident));
+    return p;
+}
+template <bool kBackward>
+ptq_status_t launch_norm(const ptq_norm_t &n, const NormPlan &plan, const ptq::NormParams &p, cudaStream_t stream)
+{
+    return with_type(n.dtype, [&](auto t) {
+        using T = decltype(t);
+        const auto go = [&](auto r) {
+            using R = decltype(r);
+            constexpr int kRB = kBackward ? 2 : 4;
+            if (plan.rows > 1)
+                ptq::ptq_norm_kernel<T, R, kRB, kBackward><<<plan.ctas, plan.threads, 0, stream>>>(p);
+            else
+                ptq::ptq_norm_kernel<T, R, 1, kBackward><<<plan.ctas, plan.threads, 0, stream>>>(p);
+            return launched();
+        };
+        return n.residual_dtype == n.dtype ? go(T()) : go(0.0f);
+    });
+}
+
+// ---------------------------------------------------------------------------------------------------- conv
+ptq_status_t conv_check(const ptq_conv_t *c)
+{
+    if (!c) return fail(PTQ_ERR_NULL, "the call's description is NULL");
+    if (!c->x || !c->weight) return fail(PTQ_ERR_NULL, "x or weight is NULL");
+    if (!dtype_ok(c->dtype)) return fail(PTQ_ERR_VALUE, "unknown type %d", c->dtype);
+    if (c->batch < 1 || c->length < 1 || c->length > PTQ_MAX_LENGTH || c->channels < 1 || c->channels > PTQ_MAX_CHANNELS || c->taps < 2 || c->taps > 4)
+        return fail(PTQ_ERR_SHAPE, "batch %d, length %d, channels %d, taps %d out of range", c->batch, c->length, c->channels, c->taps);
+    if (c->flags & ~(PTQ_CONV_SILU | PTQ_SEQ_REVERSE)) return fail(PTQ_ERR_VALUE, "unknown flags %u", c->flags);
+    if (!not_negative({c->x_pitch[0], c->x_pitch[1]})) return fail(PTQ_ERR_SHAPE, "a pitch is negative");
+    if (!aligned({c->x, c->state}, elem_bytes(c->dtype)) || !aligned({c->weight, c->bias, c->lengths}, 4))
+        return fail(PTQ_ERR_ALIGN, "an input is not aligned to its type");
+    return PTQ_OK;
+}
+constexpr int kConvE = 8, kConvBackE = 4;      // channels of a thread, forward and backward
+ptq::ConvParams conv_params(const ptq_conv_t &c, int e, long long wanted_threads)
+{
+    ptq::ConvParams p = {};
+    p.x = c.x;
+    p.state = c.state;
+    p.x_b = c.x_pitch[0];
+    p.x_l = c.x_pitch[1];
+    p.weight = c.weight;
+    p.bias = c.bias;
+    p.lengths = c.lengths;
+    p.batch = c.batch;
+    p.length = c.length;
+    p.channels = c.channels;
+    p.flags = c.flags;
+    p.pieces = static_cast<int>(ceil_div(c.channels, e));
+    // segments of 8 to 64 steps: long ones read the rows in front of them seldom, short ones make enough threads
+    int seg = 64;
+    while (seg > 8 && static_cast<long long>(c.batch) * p.pieces * ceil_div(c.length, seg) < wanted_threads) seg /= 2;
+    p.segment = seg;
+    p.segments = static_cast<int>(ceil_div(c.length, seg));
+    const int unit = 16 / elem_bytes(c.dtype);
+    p.whole = aligned({c.x, c.state}, 16) && multiples({c.x_pitch[0], c.x_pitch[1], c.channels}, unit);
+    return p;
+}
+int conv_back_rows(const ptq_conv_t &c, const ptq::ConvParams &p)
+{
+    const long long blocks = ceil_div(p.pieces, 32), rows = ceil_div(static_cast<long long>(c.batch) * p.segments, 8);
+    return static_cast<int>(std::min(rows, std::max(1ll, ceil_div(2 * kSms, blocks))));
+}
+template <class Fn>
+ptq_status_t with_taps(int taps, Fn fn)
+{
+    if (taps == 2) return fn(std::integral_constant<int, 2>());
+    if (taps == 3) return fn(std::integral_constant<int, 3>());
+    return fn(std::integral_constant<int, 4>());
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ptq_scan_workspace_bytes(const ptq_scan_t *s, int backward)
+{
+    if (!s || s->batch < 1 || s->length < 1 || s->length > PTQ_MAX_LENGTH || s->channels < 1 || s->channels > PTQ_MAX_CHANNELS || s->states < 1 ||
+        s->states > PTQ_MAX_STATES || s->groups < 1 || s->channels % s->groups)
+        return 0;
+    return scan_space(*s, scan_plan(*s), backward != 0).bytes;
+}
+
+ptq_status_t ptq_scan_forward(const ptq_scan_t *s, void *y, float *final_state, float *history, void *workspace, size_t workspace_bytes, void *stream)
+{
+    PTQ_TRY(scan_check(s));
+    if (!y) return fail(PTQ_ERR_NULL, "y is NULL");
+    if (!aligned({y}, elem_bytes(s->dtype)) || !aligned({final_state, history}, 4)) return fail(PTQ_ERR_ALIGN, "an output is not aligned to its type");
+    const ScanPlan plan = scan_plan(*s);
+    const ScanSpace space = scan_space(*s, plan, false);
+    PTQ_TRY(check_space(workspace, workspace_bytes, space.bytes));
+    PTQ_TRY(check_arch());
+    ptq::ScanParams p = scan_params(*s, plan);
+    p.y = y;
+    p.final_state = final_state;
+    p.history = history;
+    p.whole = p.whole && aligned({y}, 16);
+    p.whole_n = p.whole_n && aligned({final_state, history}, 16);
+    unsigned char *w = static_cast<unsigned char *>(workspace);
+    p.slots = reinterpret_cast<float *>(w + space.slots);
+    p.sums = reinterpret_cast<float *>(w + space.sums);
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (s->length == 1 && !history)
+        return with_type(s->dtype, [&](auto t) {
+            using T = decltype(t);
+            return with_split(s->states, [&](auto ns, auto lanes) {
+                constexpr int kNS = decltype(ns)::value, kS = decltype(lanes)::value;
+                const long long blocks = ceil_div(s->channels, 256 / kS);
+                const long long rows = std::min<long long>(s->batch, std::max(1ll, ceil_div(16 * kSms, blocks)));
+                ptq::ptq_scan_step_kernel<T, kNS, kS><<<static_cast<unsigned>(blocks * rows), 256, 0, st>>>(p);
+                return launched();
+            });
+        });
+    if (plan.chunks > 1) PTQ_TRY(launch_scan<ptq::kScanSum>(*s, plan, p, st));
+    return launch_scan<ptq::kScanForward>(*s, plan, p, st);
+}
+
+ptq_status_t ptq_scan_backward(const ptq_scan_t *s, const float *history, const void *dy, const float *dfinal, const ptq_scan_grads_t *g, void *workspace,
+                               size_t workspace_bytes, void *stream)
+{
+    PTQ_TRY(scan_check(s));
+    if (!history || !dy || !g) return fail(PTQ_ERR_NULL, "history, dy or grads is NULL");
+    if (!g->du || !g->ddelta || !g->dB || !g->dC || !g->dA) return fail(PTQ_ERR_NULL, "du, ddelta, dA, dB or dC is NULL");
+    if ((s->z != nullptr) != (g->dz != nullptr)) return fail(PTQ_ERR_NULL, "z and dz are given together");
+    if (!aligned({dy, g->du, g->ddelta, g->dz, g->dB, g->dC}, elem_bytes(s->dtype)) ||
+        !aligned({history, dfinal, g->dA, g->dD, g->ddelta_bias, g->dstate}, 4))
+        return fail(PTQ_ERR_ALIGN, "an argument is not aligned to its type");
+    const ScanPlan plan = scan_plan(*s);
+    const ScanSpace space = scan_space(*s, plan, true);
+    PTQ_TRY(check_space(workspace, workspace_bytes, space.bytes));
+    PTQ_TRY(check_arch());
+    ptq::ScanParams p = scan_params(*s, plan);
+    unsigned char *w = static_cast<unsigned char *>(workspace);
+    const auto floats = [&](size_t at) { return reinterpret_cast<float *>(w + at); };
+    p.slots = floats(space.slots);
+    p.sums = floats(space.sums);
+    p.part_A = floats(space.part_A);
+    p.part_D = floats(space.part_D);
+    p.part_bias = floats(space.part_bias);
+    p.part_BC = plan.group_blocks > 1 ? floats(space.part_BC) : nullptr;
+    p.dy = dy;
+    p.dfinal = dfinal;
+    p.kept = history;
+    p.du = g->du;
+    p.ddelta = g->ddelta;
+    p.dz = g->dz;
+    p.dB = g->dB;
+    p.dC = g->dC;
+    p.dstate = g->dstate;
+    p.whole = p.whole && aligned({dy, g->du, g->ddelta, g->dz}, 16);
+    p.whole_n = p.whole_n && aligned({history, dfinal, g->dstate}, 16);
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (plan.chunks > 1) PTQ_TRY(launch_scan<ptq::kScanGradSum>(*s, plan, p, st));
+    return with_type(s->dtype, [&](auto t) {
+        using T = decltype(t);
+        PTQ_TRY(with_split(s->states, [&](auto ns, auto lanes) {
+            constexpr int kNS = decltype(ns)::value, kS = decltype(lanes)::value;
+            ptq::ptq_scan_backward_kernel<T, kNS, kS>
+                <<<static_cast<unsigned>(plan.ctas()), plan.threads, scan_backward_smem(plan.threads, kS, kNS), st>>>(p);
+            return launched();
+        }));
+        const int blocks_A = static_cast<int>(ceil_div(static_cast<long long>(s->channels) * s->states, 32));
+        const int blocks_D = static_cast<int>(ceil_div(s->channels, 32));
+        const long long outputs = p.part_BC ? static_cast<long long>(s->batch) * s->length * 2 * s->states * s->groups : 0;
+        const int blocks_BC = static_cast<int>(std::min<long long>(ceil_div(outputs, 256), 16 * kSms));
+        ptq::ptq_scan_finish_kernel<T><<<blocks_A + 2 * blocks_D + blocks_BC, 256, 0, st>>>(p, g->dA, g->dD, g->ddelta_bias, blocks_A, blocks_D);
+        return launched();
+    });
+}
+
+ptq_status_t ptq_norm_forward(const ptq_norm_t *n, void *y, void *residual_out, void *stream)
+{
+    PTQ_TRY(norm_check(n));
+    if (!y) return fail(PTQ_ERR_NULL, "y is NULL");
+    if (!aligned({y}, elem_bytes(n->dtype)) || !aligned({residual_out}, elem_bytes(n->residual_dtype)))
+        return fail(PTQ_ERR_ALIGN, "an output is not aligned to its type");
+    PTQ_TRY(check_arch());
+    ptq::NormParams p = norm_params(*n);
+    p.y = y;
+    p.residual_out = residual_out;
+    p.whole = p.whole && aligned({y, residual_out}, 16);
+    return launch_norm<false>(*n, norm_plan(*n, false), p, static_cast<cudaStream_t>(stream));
+}
+
+size_t ptq_norm_workspace_bytes(const ptq_norm_t *n)
+{
+    if (!n || n->rows < 1 || n->cols < 1 || n->cols > PTQ_MAX_NORM_COLS) return 0;
+    return padded(static_cast<size_t>(norm_plan(*n, true).ctas) * 3 * n->cols * 4);
+}
+
+ptq_status_t ptq_norm_backward(const ptq_norm_t *n, const void *dy, const void *dresidual_out, const ptq_norm_grads_t *g, void *workspace,
+                               size_t workspace_bytes, void *stream)
+{
+    PTQ_TRY(norm_check(n));
+    if (!dy || !g || !g->dx) return fail(PTQ_ERR_NULL, "dy, grads or dx is NULL");
+    if ((n->gate != nullptr) != (g->dgate != nullptr)) return fail(PTQ_ERR_NULL, "gate and dgate are given together");
+    if (!aligned({dy, g->dx, g->dgate}, elem_bytes(n->dtype)) || !aligned({dresidual_out, g->dresidual}, elem_bytes(n->residual_dtype)) ||
+        !aligned({g->dweight, g->dbias, g->dscale}, 4))
+        return fail(PTQ_ERR_ALIGN, "an argument is not aligned to its type");
+    PTQ_TRY(check_space(workspace, workspace_bytes, ptq_norm_workspace_bytes(n)));
+    PTQ_TRY(check_arch());
+    ptq::NormParams p = norm_params(*n);
+    p.dy = dy;
+    p.dresidual_out = dresidual_out;
+    p.dx = g->dx;
+    p.dresidual = g->dresidual;
+    p.dgate = g->dgate;
+    p.part = static_cast<float *>(workspace);
+    p.whole = p.whole && aligned({dy, dresidual_out, g->dx, g->dresidual, g->dgate}, 16);
+    const NormPlan plan = norm_plan(*n, true);
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    PTQ_TRY(launch_norm<true>(*n, plan, p, st));
+    if (!g->dweight && !g->dbias && !g->dscale) return PTQ_OK;
+    ptq::ptq_norm_finish_kernel<<<dim3(static_cast<unsigned>(ceil_div(n->cols, 32)), 3), 256, 0, st>>>(p.part, plan.ctas, n->cols, g->dweight, g->dbias,
+                                                                                                   g->dscale);
+    return launched();
+}
+
+ptq_status_t ptq_conv_forward(const ptq_conv_t *c, void *y, void *final_state, void *stream)
+{
+    PTQ_TRY(conv_check(c));
+    if (!y) return fail(PTQ_ERR_NULL, "y is NULL");
+    if (!aligned({y, final_state}, elem_bytes(c->dtype))) return fail(PTQ_ERR_ALIGN, "an output is not aligned to its type");
+    ptq::ConvParams p = conv_params(*c, kConvE, kSms * 512ll);
+    p.y = y;
+    p.final_state = final_state;
+    p.whole = p.whole && aligned({y, final_state}, 16);
+    const long long ctas = ceil_div(static_cast<long long>(c->batch) * p.segments * p.pieces, 256);
+    if (ctas > kMaxGrid) return fail(PTQ_ERR_SHAPE, "the batch is too large for one launch");
+    PTQ_TRY(check_arch());
+    return with_type(c->dtype, [&](auto t) {
+        using T = decltype(t);
+        return with_taps(c->taps, [&](auto w) {
+            ptq::ptq_conv_kernel<T, kConvE, decltype(w)::value><<<static_cast<unsigned>(ctas), 256, 0, static_cast<cudaStream_t>(stream)>>>(p);
+            return launched();
+        });
+    });
+}
+
+size_t ptq_conv_workspace_bytes(const ptq_conv_t *c)
+{
+    if (!c || c->batch < 1 || c->length < 1 || c->length > PTQ_MAX_LENGTH || c->channels < 1 || c->channels > PTQ_MAX_CHANNELS || c->taps < 2 ||
+        c->taps > 4)
+        return 0;
+    const ptq::ConvParams p = conv_params(*c, kConvBackE, kSms * 512ll);
+    return padded(static_cast<size_t>(conv_back_rows(*c, p)) * (c->taps + 1) * c->channels * 4);
+}
+
+ptq_status_t ptq_conv_backward(const ptq_conv_t *c, const void *dy, const void *dfinal, const ptq_conv_grads_t *g, void *workspace,
+                               size_t workspace_bytes, void *stream)
+{
+    PTQ_TRY(conv_check(c));
+    if (!dy || !g || !g->dx || !g->dweight) return fail(PTQ_ERR_NULL, "dy, grads, dx or dweight is NULL");
+    if (!aligned({dy, dfinal, g->dx, g->dstate}, elem_bytes(c->dtype)) || !aligned({g->dweight, g->dbias}, 4))
+        return fail(PTQ_ERR_ALIGN, "an argument is not aligned to its type");
+    PTQ_TRY(check_space(workspace, workspace_bytes, ptq_conv_workspace_bytes(c)));
+    PTQ_TRY(check_arch());
+    ptq::ConvParams p = conv_params(*c, kConvBackE, kSms * 512ll);
+    p.dy = dy;
+    p.dfinal = dfinal;
+    p.dx = g->dx;
+    p.dstate = g->dstate;
+    p.part = static_cast<float *>(workspace);
+    p.whole = p.whole && aligned({dy, dfinal, g->dx, g->dstate}, 16);
+    const int rows = conv_back_rows(*c, p);
+    const dim3 grid(static_cast<unsigned>(ceil_div(p.pieces, 32)), static_cast<unsigned>(rows));
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    PTQ_TRY(with_type(c->dtype, [&](auto t) {
+        using T = decltype(t);
+        return with_taps(c->taps, [&](auto w) {
+            ptq::ptq_conv_backward_kernel<T, kConvBackE, decltype(w)::value><<<grid, 256, 0, st>>>(p);
+            return launched();
+        });
+    }));
+    ptq::ptq_conv_finish_kernel<<<dim3(static_cast<unsigned>(ceil_div(c->channels, 32)), static_cast<unsigned>(c->taps + 1)), 256, 0, st>>>(
+        p.part, rows, c->channels, c->taps, g->dweight, g->dbias);
+    return launched();
+}
+
+}  // extern "C"

@@ -4,8 +4,7 @@
 // The offline steps (calibration, step search) go the same way, with host arrays through the buffer protocol: a calibration of
 // 8 x 197 x 384 with 192 outputs takes 60 us a call, 78 through ctypes, of which 36 are its copies, launches and the wait for them.
 // The C ABI's functions are handed over as addresses by the binding, so this module does not link the library.
-#define PY_SSIZE_T_CLEAN
-#include <Python.h>
+#include "ptq_torch.h"
 
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAStream.h>
@@ -267,7 +266,6 @@ PyObject *py_bind(PyObject *, PyObject *const *args, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
-#define PTQ_METHOD(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PTQ_METHOD("bind", py_bind), PTQ_METHOD("forward", py_forward),
                          PTQ_METHOD("forward_static", py_forward_static), PTQ_METHOD("forward_dynamic", py_forward_dynamic),
                          PTQ_METHOD("calibrate", py_calibrate), PTQ_METHOD("search", py_search),
@@ -276,4 +274,12 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ptq_torch", nullptr, -1, methods,
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__ptq_torch(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__ptq_torch(void)
+{
+    PyObject *m = PyModule_Create(&module);
+    if (m && ptq_add_block_methods(m) != 0) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}
