@@ -4,17 +4,14 @@
 #include <algorithm>
 #include <cmath>
 
+#include "ptq_block_host.h"
 #include "ptq_conv.cuh"
-#include "ptq_host.h"
 #include "ptq_norm.cuh"
-#include "ptq_scan.cuh"
+#include "ptq_scan_launch.cuh"
 
 namespace {
 
 using namespace ptq_host;
-
-constexpr int kSms = 148;             // of the one GPU that the library is for; only cuts of the work go by it
-constexpr long long kMaxGrid = 0x7fffffffll;
 
 ptq_status_t check_arch()
 {
@@ -33,19 +30,6 @@ ptq_status_t check_arch()
     }
     return k == 1 ? PTQ_OK : fail(PTQ_ERR_ARCH, "device %d is not compute capability 10.0", dev);
 }
-
-ptq_status_t launched()
-{
-    g_launches.fetch_add(1, std::memory_order_relaxed);
-    PTQ_CUDA(cudaGetLastError());
-    return PTQ_OK;
-}
-
-#define PTQ_TRY(...)                                  \
-    do {                                              \
-        const ptq_status_t st_ = (__VA_ARGS__);       \
-        if (st_ != PTQ_OK) return st_;                \
-    } while (0)
 
 int elem_bytes(int dtype) { return dtype == PTQ_F32 ? 4 : 2; }
 bool dtype_ok(int dtype) { return dtype == PTQ_F16 || dtype == PTQ_BF16 || dtype == PTQ_F32; }
@@ -69,7 +53,6 @@ bool not_negative(std::initializer_list<int64_t> pitches)
         if (v < 0) return false;
     return true;
 }
-long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 template <class Fn>
@@ -81,21 +64,11 @@ ptq_status_t with_type(int dtype, Fn fn)
 }
 
 // ---------------------------------------------------------------------------------------------------- scan
-// Lanes per channel and states per lane.
-struct ScanSplit {
-    int lanes, states;
-};
-ScanSplit scan_split(int states)
-{
-    if (states <= 4) return {1, states <= 1 ? 1 : states <= 2 ? 2 : 4};
-    return {states <= 8 ? 2 : states <= 16 ? 4 : 8, 4};
-}
-
 // How a call is cut: threads of a CTA, CTAs per group, chunks of the sequences.
 struct ScanPlan {
     int threads, group_blocks, chunk_len, chunks;
-    long long ctas() const { return ctas_; }
-    long long ctas_;
+    long long ctas;                   // of one chunk
+    ScanCut cut(int n, bool whole) const { return {threads, ctas * n, whole}; }
 };
 ScanPlan scan_plan(const ptq_scan_t &s)
 {
@@ -103,13 +76,13 @@ ScanPlan scan_plan(const ptq_scan_t &s)
     ScanPlan p;
     p.threads = lanes == 1 ? 128 : 256;
     const auto blocks = [&](int threads) { return ceil_div(per_group, threads / lanes); };
-    if (lanes < 8 && static_cast<long long>(s.batch) * s.groups * blocks(p.threads) < kSms && s.length < 512) p.threads = 64;
+    if (lanes < 8 && static_cast<long long>(s.batch) * s.groups * blocks(p.threads) < kSms && s.length < 512) p.threads = 128;
     p.group_blocks = static_cast<int>(blocks(p.threads));
     const long long ctas = static_cast<long long>(s.batch) * s.groups * p.group_blocks;
     long long chunks = ctas >= 2 * kSms ? 1 : std::min(ceil_div(4 * kSms, ctas), ceil_div(s.length, 256));
     p.chunk_len = static_cast<int>(ceil_div(ceil_div(s.length, chunks), 64) * 64);
     p.chunks = static_cast<int>(ceil_div(s.length, p.chunk_len));
-    p.ctas_ = ctas * p.chunks;
+    p.ctas = ctas;
     return p;
 }
 
@@ -129,7 +102,7 @@ ptq_status_t scan_check(const ptq_scan_t *s)
         return fail(PTQ_ERR_SHAPE, "a pitch is negative");
     if (!aligned({s->u, s->delta, s->z, s->B, s->C}, elem_bytes(s->dtype)) || !aligned({s->A, s->D, s->delta_bias, s->state, s->lengths}, 4))
         return fail(PTQ_ERR_ALIGN, "an input is not aligned to its type");
-    if (scan_plan(*s).ctas() > kMaxGrid) return fail(PTQ_ERR_SHAPE, "the batch is too large for one launch");
+    if (const ScanPlan plan = scan_plan(*s); plan.ctas * plan.chunks > kMaxGrid) return fail(PTQ_ERR_SHAPE, "the batch is too large for one launch");
     return PTQ_OK;
 }
 
@@ -168,11 +141,17 @@ ptq::ScanParams scan_params(const ptq_scan_t &s, const ScanPlan &plan)
     p.chunk_len = plan.chunk_len;
     p.chunks = plan.chunks;
     p.flags = s.flags;
-    const int unit = 16 / elem_bytes(s.dtype);
-    p.whole = aligned({s.u, s.delta, s.z}, 16) && multiples({p.u_b, p.u_l, p.delta_b, p.delta_l, p.z ? p.z_b : 0, p.z ? p.z_l : 0}, unit) &&
-              s.channels % unit == 0 && p.group_channels % unit == 0;
-    p.whole_n = s.states % 4 == 0 && aligned({s.A, s.state}, 16);
     return p;
+}
+
+// Whether a call's rows and states can be moved 16 bytes at a time, as far as its description goes.
+bool scan_whole(const ptq_scan_t &s)
+{
+    const int unit = 16 / elem_bytes(s.dtype);
+    return aligned({s.u, s.delta, s.z, s.A, s.D, s.delta_bias, s.state}, 16) &&
+           multiples({s.u_pitch[0], s.u_pitch[1], s.delta_pitch[0], s.delta_pitch[1], s.z ? s.z_pitch[0] : 0, s.z ? s.z_pitch[1] : 0,
+                      s.channels / s.groups}, unit) &&
+           (scan_split(s.states).states < 4 || s.states % 4 == 0);
 }
 
 // Workspace: slots and sums of the chunks, and for the backward pass the shares of the CTAs.
@@ -201,41 +180,6 @@ ScanSpace scan_space(const ptq_scan_t &s, const ScanPlan &plan, bool backward)
     }
     w.bytes = at;
     return w;
-}
-
-template <class Fn>
-ptq_status_t with_split(int states, Fn fn)
-{
-    const ScanSplit sp = scan_split(states);
-    using std::integral_constant;
-    if (sp.lanes == 1 && sp.states == 1) return fn(integral_constant<int, 1>(), integral_constant<int, 1>());
-    if (sp.lanes == 1 && sp.states == 2) return fn(integral_constant<int, 2>(), integral_constant<int, 1>());
-    if (sp.lanes == 1) return fn(integral_constant<int, 4>(), integral_constant<int, 1>());
-    if (sp.lanes == 2) return fn(integral_constant<int, 4>(), integral_constant<int, 2>());
-    if (sp.lanes == 4) return fn(integral_constant<int, 4>(), integral_constant<int, 4>());
-    return fn(integral_constant<int, 4>(), integral_constant<int, 8>());
-}
-
-size_t scan_forward_smem(int threads, int lanes, int states) { return static_cast<size_t>(8) * threads * 8 + static_cast<size_t>(8) * lanes * lanes * states * 2 * 4; }
-size_t scan_backward_smem(int threads, int lanes, int states)
-{
-    const size_t rows = ptq::kScanHistory, np = static_cast<size_t>(lanes) * states;
-    return rows * (threads / lanes) * 16 + rows * np * 8 + (threads / 32) * rows * 2 * np * 4;
-}
-
-template <int kMode>
-ptq_status_t launch_scan(const ptq_scan_t &s, const ScanPlan &plan, const ptq::ScanParams &p, cudaStream_t stream)
-{
-    const long long ctas = kMode == ptq::kScanForward ? plan.ctas() : plan.ctas() / plan.chunks * (plan.chunks - 1);
-    return with_type(s.dtype, [&](auto t) {
-        using T = decltype(t);
-        return with_split(s.states, [&](auto ns, auto lanes) {
-            constexpr int kNS = decltype(ns)::value, kS = decltype(lanes)::value;
-            ptq::ptq_scan_kernel<T, kNS, kS, kMode>
-                <<<static_cast<unsigned>(ctas), plan.threads, scan_forward_smem(plan.threads, kS, kNS), stream>>>(p);
-            return launched();
-        });
-    });
 }
 
 ptq_status_t check_space(const void *workspace, size_t have, size_t need)
@@ -282,10 +226,13 @@ ptq::NormParams norm_params(const ptq_norm_t &n)
     p.eps = n.eps;
     p.inv_cols = static_cast<float>(1.0 / n.cols);
     p.layer = n.flags & PTQ_NORM_LAYER;
-    const int unit = 16 / elem_bytes(n.dtype), runit = 16 / elem_bytes(n.residual_dtype);
-    p.whole = aligned({n.x, n.residual, n.gate}, 16) && n.x_pitch % unit == 0 && (!n.gate || n.gate_pitch % unit == 0) &&
-              (!n.residual || n.residual_pitch % runit == 0) && n.cols % unit == 0;
     return p;
+}
+bool norm_whole(const ptq_norm_t &n)
+{
+    const int unit = 16 / elem_bytes(n.dtype), residual_unit = 16 / elem_bytes(n.residual_dtype);
+    return aligned({n.x, n.residual, n.gate}, 16) && multiples({n.x_pitch, n.gate ? n.gate_pitch : 0, n.cols}, unit) &&
+           (!n.residual || n.residual_pitch % residual_unit == 0);
 }
 // Rows that a CTA takes at a time, and CTAs.
 struct NormPlan {
@@ -302,18 +249,21 @@ NormPlan norm_plan(const ptq_norm_t &n, bool backward)
     return p;
 }
 template <bool kBackward>
-ptq_status_t launch_norm(const ptq_norm_t &n, const NormPlan &plan, const ptq::NormParams &p, cudaStream_t stream)
+ptq_status_t launch_norm(const ptq_norm_t &n, const NormPlan &plan, const ptq::NormParams &p, bool whole_rows, cudaStream_t stream)
 {
     return with_type(n.dtype, [&](auto t) {
         using T = decltype(t);
         const auto go = [&](auto r) {
             using R = decltype(r);
-            constexpr int kRB = kBackward ? 2 : 4;
-            if (plan.rows > 1)
-                ptq::ptq_norm_kernel<T, R, kRB, kBackward><<<plan.ctas, plan.threads, 0, stream>>>(p);
-            else
-                ptq::ptq_norm_kernel<T, R, 1, kBackward><<<plan.ctas, plan.threads, 0, stream>>>(p);
-            return launched();
+            return with_flag(whole_rows, [&](auto whole) {
+                constexpr int kRB = kBackward ? 2 : 4;
+                constexpr bool kWhole = decltype(whole)::value;
+                if (plan.rows > 1)
+                    ptq::ptq_norm_kernel<T, R, kRB, kBackward, kWhole><<<plan.ctas, plan.threads, 0, stream>>>(p);
+                else
+                    ptq::ptq_norm_kernel<T, R, 1, kBackward, kWhole><<<plan.ctas, plan.threads, 0, stream>>>(p);
+                return launched();
+            });
         };
         return n.residual_dtype == n.dtype ? go(T()) : go(0.0f);
     });
@@ -354,9 +304,11 @@ ptq::ConvParams conv_params(const ptq_conv_t &c, int e, long long wanted_threads
     while (seg > 8 && static_cast<long long>(c.batch) * p.pieces * ceil_div(c.length, seg) < wanted_threads) seg /= 2;
     p.segment = seg;
     p.segments = static_cast<int>(ceil_div(c.length, seg));
-    const int unit = 16 / elem_bytes(c.dtype);
-    p.whole = aligned({c.x, c.state}, 16) && multiples({c.x_pitch[0], c.x_pitch[1], c.channels}, unit);
     return p;
+}
+bool conv_whole(const ptq_conv_t &c)
+{
+    return aligned({c.x, c.state}, 16) && multiples({c.x_pitch[0], c.x_pitch[1], c.channels}, 16 / elem_bytes(c.dtype));
 }
 int conv_back_rows(const ptq_conv_t &c, const ptq::ConvParams &p)
 {
@@ -396,25 +348,17 @@ ptq_status_t ptq_scan_forward(const ptq_scan_t *s, void *y, float *final_state, 
     p.y = y;
     p.final_state = final_state;
     p.history = history;
-    p.whole = p.whole && aligned({y}, 16);
-    p.whole_n = p.whole_n && aligned({final_state, history}, 16);
+    const bool whole = scan_whole(*s) && aligned({y, final_state, history}, 16);
     unsigned char *w = static_cast<unsigned char *>(workspace);
     p.slots = reinterpret_cast<float *>(w + space.slots);
     p.sums = reinterpret_cast<float *>(w + space.sums);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (s->length == 1 && !history)
-        return with_type(s->dtype, [&](auto t) {
-            using T = decltype(t);
-            return with_split(s->states, [&](auto ns, auto lanes) {
-                constexpr int kNS = decltype(ns)::value, kS = decltype(lanes)::value;
-                const long long blocks = ceil_div(s->channels, 256 / kS);
-                const long long rows = std::min<long long>(s->batch, std::max(1ll, ceil_div(16 * kSms, blocks)));
-                ptq::ptq_scan_step_kernel<T, kNS, kS><<<static_cast<unsigned>(blocks * rows), 256, 0, st>>>(p);
-                return launched();
-            });
-        });
-    if (plan.chunks > 1) PTQ_TRY(launch_scan<ptq::kScanSum>(*s, plan, p, st));
-    return launch_scan<ptq::kScanForward>(*s, plan, p, st);
+    return with_type(s->dtype, [&](auto t) {
+        using Launch = ScanLaunch<decltype(t)>;
+        if (s->length == 1 && !history) return Launch::step(p, whole, st);
+        if (plan.chunks > 1) PTQ_TRY(Launch::forward(ptq::kScanSum, p, plan.cut(plan.chunks - 1, whole), st));
+        return Launch::forward(ptq::kScanForward, p, plan.cut(plan.chunks, whole), st);
+    });
 }
 
 ptq_status_t ptq_scan_backward(const ptq_scan_t *s, const float *history, const void *dy, const float *dfinal, const ptq_scan_grads_t *g, void *workspace,
@@ -449,24 +393,13 @@ ptq_status_t ptq_scan_backward(const ptq_scan_t *s, const float *history, const 
     p.dB = g->dB;
     p.dC = g->dC;
     p.dstate = g->dstate;
-    p.whole = p.whole && aligned({dy, g->du, g->ddelta, g->dz}, 16);
-    p.whole_n = p.whole_n && aligned({history, dfinal, g->dstate}, 16);
+    const bool whole = scan_whole(*s) && aligned({dy, g->du, g->ddelta, g->dz, history, dfinal, g->dstate}, 16);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (plan.chunks > 1) PTQ_TRY(launch_scan<ptq::kScanGradSum>(*s, plan, p, st));
     return with_type(s->dtype, [&](auto t) {
-        using T = decltype(t);
-        PTQ_TRY(with_split(s->states, [&](auto ns, auto lanes) {
-            constexpr int kNS = decltype(ns)::value, kS = decltype(lanes)::value;
-            ptq::ptq_scan_backward_kernel<T, kNS, kS>
-                <<<static_cast<unsigned>(plan.ctas()), plan.threads, scan_backward_smem(plan.threads, kS, kNS), st>>>(p);
-            return launched();
-        }));
-        const int blocks_A = static_cast<int>(ceil_div(static_cast<long long>(s->channels) * s->states, 32));
-        const int blocks_D = static_cast<int>(ceil_div(s->channels, 32));
-        const long long outputs = p.part_BC ? static_cast<long long>(s->batch) * s->length * 2 * s->states * s->groups : 0;
-        const int blocks_BC = static_cast<int>(std::min<long long>(ceil_div(outputs, 256), 16 * kSms));
-        ptq::ptq_scan_finish_kernel<T><<<blocks_A + 2 * blocks_D + blocks_BC, 256, 0, st>>>(p, g->dA, g->dD, g->ddelta_bias, blocks_A, blocks_D);
-        return launched();
+        using Launch = ScanLaunch<decltype(t)>;
+        if (plan.chunks > 1) PTQ_TRY(Launch::forward(ptq::kScanGradSum, p, plan.cut(plan.chunks - 1, whole), st));
+        PTQ_TRY(Launch::backward(p, plan.cut(plan.chunks, whole), st));
+        return Launch::finish(p, g->dA, g->dD, g->ddelta_bias, st);
     });
 }
 
@@ -480,8 +413,7 @@ ptq_status_t ptq_norm_forward(const ptq_norm_t *n, void *y, void *residual_out, 
     ptq::NormParams p = norm_params(*n);
     p.y = y;
     p.residual_out = residual_out;
-    p.whole = p.whole && aligned({y, residual_out}, 16);
-    return launch_norm<false>(*n, norm_plan(*n, false), p, static_cast<cudaStream_t>(stream));
+    return launch_norm<false>(*n, norm_plan(*n, false), p, norm_whole(*n) && aligned({y, residual_out}, 16), static_cast<cudaStream_t>(stream));
 }
 
 size_t ptq_norm_workspace_bytes(const ptq_norm_t *n)
@@ -508,10 +440,9 @@ ptq_status_t ptq_norm_backward(const ptq_norm_t *n, const void *dy, const void *
     p.dresidual = g->dresidual;
     p.dgate = g->dgate;
     p.part = static_cast<float *>(workspace);
-    p.whole = p.whole && aligned({dy, dresidual_out, g->dx, g->dresidual, g->dgate}, 16);
     const NormPlan plan = norm_plan(*n, true);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    PTQ_TRY(launch_norm<true>(*n, plan, p, st));
+    PTQ_TRY(launch_norm<true>(*n, plan, p, norm_whole(*n) && aligned({dy, dresidual_out, g->dx, g->dresidual, g->dgate}, 16), st));
     if (!g->dweight && !g->dbias && !g->dscale) return PTQ_OK;
     ptq::ptq_norm_finish_kernel<<<dim3(static_cast<unsigned>(ceil_div(n->cols, 32)), 3), 256, 0, st>>>(p.part, plan.ctas, n->cols, g->dweight, g->dbias,
                                                                                                    g->dscale);
@@ -526,15 +457,17 @@ ptq_status_t ptq_conv_forward(const ptq_conv_t *c, void *y, void *final_state, v
     ptq::ConvParams p = conv_params(*c, kConvE, kSms * 512ll);
     p.y = y;
     p.final_state = final_state;
-    p.whole = p.whole && aligned({y, final_state}, 16);
     const long long ctas = ceil_div(static_cast<long long>(c->batch) * p.segments * p.pieces, 256);
     if (ctas > kMaxGrid) return fail(PTQ_ERR_SHAPE, "the batch is too large for one launch");
     PTQ_TRY(check_arch());
     return with_type(c->dtype, [&](auto t) {
         using T = decltype(t);
         return with_taps(c->taps, [&](auto w) {
-            ptq::ptq_conv_kernel<T, kConvE, decltype(w)::value><<<static_cast<unsigned>(ctas), 256, 0, static_cast<cudaStream_t>(stream)>>>(p);
-            return launched();
+            return with_flag(conv_whole(*c) && aligned({y, final_state}, 16), [&](auto whole) {
+                ptq::ptq_conv_kernel<T, kConvE, decltype(w)::value, decltype(whole)::value>
+                    <<<static_cast<unsigned>(ctas), 256, 0, static_cast<cudaStream_t>(stream)>>>(p);
+                return launched();
+            });
         });
     });
 }
@@ -563,15 +496,16 @@ ptq_status_t ptq_conv_backward(const ptq_conv_t *c, const void *dy, const void *
     p.dx = g->dx;
     p.dstate = g->dstate;
     p.part = static_cast<float *>(workspace);
-    p.whole = p.whole && aligned({dy, dfinal, g->dx, g->dstate}, 16);
     const int rows = conv_back_rows(*c, p);
     const dim3 grid(static_cast<unsigned>(ceil_div(p.pieces, 32)), static_cast<unsigned>(rows));
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     PTQ_TRY(with_type(c->dtype, [&](auto t) {
         using T = decltype(t);
         return with_taps(c->taps, [&](auto w) {
-            ptq::ptq_conv_backward_kernel<T, kConvBackE, decltype(w)::value><<<grid, 256, 0, st>>>(p);
-            return launched();
+            return with_flag(conv_whole(*c) && aligned({dy, dfinal, g->dx, g->dstate}, 16), [&](auto whole) {
+                ptq::ptq_conv_backward_kernel<T, kConvBackE, decltype(w)::value, decltype(whole)::value><<<grid, 256, 0, st>>>(p);
+                return launched();
+            });
         });
     }));
     ptq::ptq_conv_finish_kernel<<<dim3(static_cast<unsigned>(ceil_div(c->channels, 32)), static_cast<unsigned>(c->taps + 1)), 256, 0, st>>>(

@@ -34,78 +34,152 @@ __device__ __forceinline__ T from_f32(float v)
         return __float2bfloat16_rn(v);
 }
 
-// kE consecutive elements as they lie in memory.
+// kE consecutive elements as they lie in memory, in whole registers: held as 16-bit values, they would be taken apart, and
+// waited for, where they are loaded.
 template <typename T, int kE>
-struct alignas(kE * sizeof(T) >= 16 ? 16 : kE * sizeof(T)) Piece {
-    T v[kE];
-    __device__ __forceinline__ float operator[](int e) const { return to_f32<T>(v[e]); }
+struct Piece {
+    static constexpr int kWords = (kE * static_cast<int>(sizeof(T)) + 3) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ float operator[](int e) const
+    {
+        if constexpr (sizeof(T) == 4) {
+            return __uint_as_float(w[e]);
+        } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+            return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+        } else {
+            const __half2 h = *reinterpret_cast<const __half2 *>(&w[e / 2]);
+            return e & 1 ? __high2float(h) : __low2float(h);
+        }
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0u;
+    }
+    __device__ __forceinline__ void set(const float (&f)[kE])
+    {
+        zero();
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            if constexpr (sizeof(T) == 4) {
+                w[e] = __float_as_uint(f[e]);
+            } else if constexpr (kE % 2 == 0) {
+                if (e & 1) continue;
+                if constexpr (std::is_same_v<T, __half>) {
+                    const __half2 h = __floats2half2_rn(f[e], f[(e + 1) % kE]);
+                    w[e / 2] = *reinterpret_cast<const uint32_t *>(&h);
+                } else {
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(f[e], f[(e + 1) % kE]);
+                    w[e / 2] = *reinterpret_cast<const uint32_t *>(&h);
+                }
+            } else {
+                const T t = from_f32<T>(f[e]);
+                w[e / 2] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(&t)) << 16 * (e & 1);
+            }
+        }
+    }
 };
 
-// `n` of the kE elements exist.  `whole`: the address allows accesses of up to 16 bytes.  Plain loads: some kernels replace what they
-// have read (a state), which loads through the read-only path must not see.
+// Words of the accesses that move a piece, and how many elements one of them holds.
 template <typename T, int kE>
-__device__ __forceinline__ Piece<T, kE> load_piece(const T *p, int n, bool whole)
+constexpr int kAccessWords = kE * sizeof(T) >= 16 ? 4 : kE * sizeof(T) >= 8 ? 2 : 1;
+
+// `n` of the kE elements exist, the others are zeros.  kWhole: the pointer allows accesses of up to 16 bytes, and n ends between two of
+// them.  Plain loads: some kernels replace what they have read (a state), which loads through the read-only path must not see.
+template <bool kWhole, typename T, int kE>
+__device__ __forceinline__ Piece<T, kE> load_piece(const T *p, int n)
 {
     Piece<T, kE> r;
-    if (whole && n >= kE) {
-        constexpr int kWords = kE * static_cast<int>(sizeof(T)) / 4;
-        if constexpr (kWords >= 4) {
+    r.zero();
+    if constexpr (kWhole && kE * sizeof(T) >= 4) {
+        constexpr int kStep = kAccessWords<T, kE>, kElems = kStep * 4 / static_cast<int>(sizeof(T));
 #pragma unroll
-            for (int i = 0; i < kWords / 4; ++i) reinterpret_cast<uint4 *>(&r)[i] = reinterpret_cast<const uint4 *>(p)[i];
-        } else if constexpr (kWords == 2) {
-            *reinterpret_cast<uint2 *>(&r) = *reinterpret_cast<const uint2 *>(p);
-        } else {
-            *reinterpret_cast<uint32_t *>(&r) = *reinterpret_cast<const uint32_t *>(p);
+        for (int i = 0; i < Piece<T, kE>::kWords / kStep; ++i) {
+            if (n < (i + 1) * kElems) continue;
+            if constexpr (kStep == 4) {
+                const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
+                r.w[4 * i] = v.x;
+                r.w[4 * i + 1] = v.y;
+                r.w[4 * i + 2] = v.z;
+                r.w[4 * i + 3] = v.w;
+            } else if constexpr (kStep == 2) {
+                const uint2 v = reinterpret_cast<const uint2 *>(p)[i];
+                r.w[2 * i] = v.x;
+                r.w[2 * i + 1] = v.y;
+            } else {
+                r.w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+            }
         }
     } else {
 #pragma unroll
-        for (int e = 0; e < kE; ++e) r.v[e] = e < n ? p[e] : from_f32<T>(0.0f);
+        for (int e = 0; e < kE; ++e) {
+            if (e >= n) continue;
+            if constexpr (sizeof(T) == 4)
+                r.w[e] = reinterpret_cast<const uint32_t *>(p)[e];
+            else
+                r.w[e / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t *>(p)[e]) << 16 * (e & 1);
+        }
     }
     return r;
 }
-template <typename T, int kE>
-__device__ __forceinline__ void store_piece(T *p, const float (&f)[kE], int n, bool whole)
+template <bool kWhole, typename T, int kE>
+__device__ __forceinline__ void store_piece(T *p, const Piece<T, kE> &r, int n)
 {
-    Piece<T, kE> r;
+    if constexpr (kWhole && kE * sizeof(T) >= 4) {
+        constexpr int kStep = kAccessWords<T, kE>, kElems = kStep * 4 / static_cast<int>(sizeof(T));
 #pragma unroll
-    for (int e = 0; e < kE; ++e) r.v[e] = from_f32<T>(f[e]);
-    if (whole && n >= kE) {
-        constexpr int kWords = kE * static_cast<int>(sizeof(T)) / 4;
-        if constexpr (kWords >= 4) {
-#pragma unroll
-            for (int i = 0; i < kWords / 4; ++i) reinterpret_cast<uint4 *>(p)[i] = reinterpret_cast<const uint4 *>(&r)[i];
-        } else if constexpr (kWords == 2) {
-            *reinterpret_cast<uint2 *>(p) = *reinterpret_cast<const uint2 *>(&r);
-        } else {
-            *reinterpret_cast<uint32_t *>(p) = *reinterpret_cast<const uint32_t *>(&r);
+        for (int i = 0; i < Piece<T, kE>::kWords / kStep; ++i) {
+            if (n < (i + 1) * kElems) continue;
+            if constexpr (kStep == 4)
+                reinterpret_cast<uint4 *>(p)[i] = make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]);
+            else if constexpr (kStep == 2)
+                reinterpret_cast<uint2 *>(p)[i] = make_uint2(r.w[2 * i], r.w[2 * i + 1]);
+            else
+                reinterpret_cast<uint32_t *>(p)[i] = r.w[i];
         }
     } else {
 #pragma unroll
-        for (int e = 0; e < kE; ++e)
-            if (e < n) p[e] = r.v[e];
+        for (int e = 0; e < kE; ++e) {
+            if (e >= n) continue;
+            if constexpr (sizeof(T) == 4)
+                reinterpret_cast<uint32_t *>(p)[e] = r.w[e];
+            else
+                reinterpret_cast<uint16_t *>(p)[e] = static_cast<uint16_t>(r.w[e / 2] >> 16 * (e & 1));
+        }
     }
+}
+template <bool kWhole, typename T, int kE>
+__device__ __forceinline__ void store_piece(T *p, const float (&f)[kE], int n)
+{
+    Piece<T, kE> r;
+    r.set(f);
+    store_piece<kWhole, T, kE>(p, r, n);
 }
 
-// kN consecutive floats, of which n exist (16-byte accesses where `whole`).
-template <int kN>
-__device__ __forceinline__ void load_floats(float (&f)[kN], const float *p, int n, bool whole)
+// kN consecutive floats, of which n exist; kWhole: the address allows accesses of 16 bytes, and n is 0 or kN where kN is 4.
+template <bool kWhole, int kN>
+__device__ __forceinline__ void load_floats(float (&f)[kN], const float *p, int n)
 {
-    if (kN == 4 && whole && n >= 4) {
-        const float4 v = *reinterpret_cast<const float4 *>(p);
+    if constexpr (kN == 4 && kWhole) {
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (n >= 4) v = *reinterpret_cast<const float4 *>(p);
         f[0] = v.x;
-        f[1 % kN] = v.y;
-        f[2 % kN] = v.z;
-        f[3 % kN] = v.w;
+        f[1] = v.y;
+        f[2] = v.z;
+        f[3] = v.w;
     } else {
 #pragma unroll
-        for (int k = 0; k < kN; ++k) f[k] = k < n ? p[k] : 0.0f;
+        for (int k = 0; k < kN; ++k) {
+            f[k] = 0.0f;
+            if (k < n) f[k] = p[k];
+        }
     }
 }
-template <int kN>
-__device__ __forceinline__ void store_floats(float *p, const float (&f)[kN], int n, bool whole)
+template <bool kWhole, int kN>
+__device__ __forceinline__ void store_floats(float *p, const float (&f)[kN], int n)
 {
-    if (kN == 4 && whole && n >= 4) {
-        *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1 % kN], f[2 % kN], f[3 % kN]);
+    if constexpr (kN == 4 && kWhole) {
+        if (n >= 4) *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
     } else {
 #pragma unroll
         for (int k = 0; k < kN; ++k)
@@ -121,6 +195,62 @@ __device__ __forceinline__ float exp2_approx(float x)
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
+}
+
+// Two binary32 operations in one instruction (it occupies the pipe for two cycles and leaves the other issue slot free).
+__device__ __forceinline__ void fma_pair(float &d0, float &d1, float a0, float a1, float b0, float b1, float c0, float c1)
+{
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d0), "=f"(d1)
+        : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ void mul_pair(float &d0, float &d1, float a0, float a1, float b0, float b1)
+{
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d0), "=f"(d1)
+        : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+// d[k] = a[k] b[k] + c[k], and with one factor for all k; d may be any of the operands.
+template <int kN>
+__device__ __forceinline__ void fma_each(float (&d)[kN], const float (&a)[kN], const float (&b)[kN], const float (&c)[kN])
+{
+    if constexpr (kN == 1) d[0] = fmaf(a[0], b[0], c[0]);
+#pragma unroll
+    for (int k = 0; k + 1 < kN; k += 2) fma_pair(d[k], d[k + 1], a[k], a[k + 1], b[k], b[k + 1], c[k], c[k + 1]);
+}
+template <int kN>
+__device__ __forceinline__ void fma_each(float (&d)[kN], float a, const float (&b)[kN], const float (&c)[kN])
+{
+    if constexpr (kN == 1) d[0] = fmaf(a, b[0], c[0]);
+#pragma unroll
+    for (int k = 0; k + 1 < kN; k += 2) fma_pair(d[k], d[k + 1], a, a, b[k], b[k + 1], c[k], c[k + 1]);
+}
+template <int kN>
+__device__ __forceinline__ void mul_each(float (&d)[kN], const float (&a)[kN], const float (&b)[kN])
+{
+    if constexpr (kN == 1) d[0] = a[0] * b[0];
+#pragma unroll
+    for (int k = 0; k + 1 < kN; k += 2) mul_pair(d[k], d[k + 1], a[k], a[k + 1], b[k], b[k + 1]);
+}
+template <int kN>
+__device__ __forceinline__ void mul_each(float (&d)[kN], float a, const float (&b)[kN])
+{
+    if constexpr (kN == 1) d[0] = a * b[0];
+#pragma unroll
+    for (int k = 0; k + 1 < kN; k += 2) mul_pair(d[k], d[k + 1], a, a, b[k], b[k + 1]);
+}
+
+// sum_k a[k] b[k]
+template <int kN>
+__device__ __forceinline__ float dot_each(const float (&a)[kN], const float (&b)[kN])
+{
+    if constexpr (kN == 1) return a[0] * b[0];
+    float s[2];
+    mul_pair(s[0], s[1], a[0], a[1 % kN], b[0], b[1 % kN]);
+#pragma unroll
+    for (int k = 2; k + 1 < kN; k += 2) fma_pair(s[0], s[1], a[k], a[k + 1], b[k], b[k + 1], s[0], s[1]);
+    return s[0] + s[1];
 }
 
 // Sums over the lanes whose numbers differ in the bits kLow, 2 kLow, ..., kHigh of V values per lane: every level that

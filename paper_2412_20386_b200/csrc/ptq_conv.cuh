@@ -21,7 +21,6 @@ struct ConvParams {
     int segment, segments;            // steps of a segment (at least W-1), segments of a sequence
     int pieces;                       // pieces of a row
     unsigned flags;
-    bool whole;
     void *y, *final_state;            // dense; final_state may be null or the state itself
     // backward
     const void *dy, *dfinal;
@@ -29,7 +28,7 @@ struct ConvParams {
     float *part;                      // [gridDim.y][W + 1][channels]
 };
 
-template <typename T, int kE, int kW>
+template <typename T, int kE, int kW, bool kWhole>
 struct ConvRow {
     const ConvParams &p;
     int b, c, cn, len;
@@ -43,9 +42,9 @@ struct ConvRow {
     __device__ __forceinline__ Piece<T, kE> input(int i) const
     {
         if (i < 0)
-            return load_piece<T, kE>(static_cast<const T *>(p.state) + (static_cast<long long>(b) * (kW - 1) + (i + kW - 1)) * p.channels + c,
-                                     p.state ? cn : 0, p.whole);
-        return load_piece<T, kE>(static_cast<const T *>(p.x) + b * p.x_b + token(min(i, p.length - 1)) * p.x_l + c, i < len ? cn : 0, p.whole);
+            return load_piece<kWhole, T, kE>(static_cast<const T *>(p.state) + (static_cast<long long>(b) * (kW - 1) + (i + kW - 1)) * p.channels + c,
+                                     p.state ? cn : 0);
+        return load_piece<kWhole, T, kE>(static_cast<const T *>(p.x) + b * p.x_b + token(min(i, p.length - 1)) * p.x_l + c, i < len ? cn : 0);
     }
     __device__ __forceinline__ long long dense(int i) const { return (static_cast<long long>(b) * p.length + token(i)) * p.channels + c; }
 };
@@ -61,7 +60,7 @@ __device__ __forceinline__ void conv_weights(const ConvParams &p, int c, int cn,
     }
 }
 
-template <typename T, int kE, int kW>
+template <typename T, int kE, int kW, bool kWhole>
 __global__ void __launch_bounds__(256) ptq_conv_kernel(const ConvParams p)
 {
     constexpr int kAhead = 4;
@@ -69,7 +68,7 @@ __global__ void __launch_bounds__(256) ptq_conv_kernel(const ConvParams p)
     const long long row = idx / p.pieces;
     if (row >= static_cast<long long>(p.batch) * p.segments) return;
     const int seg = static_cast<int>(row % p.segments);
-    const ConvRow<T, kE, kW> in(p, static_cast<int>(row / p.segments), static_cast<int>(idx - row * p.pieces));
+    const ConvRow<T, kE, kW, kWhole> in(p, static_cast<int>(row / p.segments), static_cast<int>(idx - row * p.pieces));
     float w[kW][kE], bias[kE], x[kW][kE];
     conv_weights<T, kE, kW>(p, in.c, in.cn, w, bias);
     const int i0 = seg * p.segment, i1 = min(i0 + p.segment, in.len);
@@ -90,7 +89,7 @@ __global__ void __launch_bounds__(256) ptq_conv_kernel(const ConvParams p)
             float f[kE];
 #pragma unroll
             for (int e = 0; e < kE; ++e) f[e] = last[j][e];
-            store_piece<T, kE>(out + static_cast<long long>(j) * p.channels, f, in.cn, p.whole);
+            store_piece<kWhole, T, kE>(out + static_cast<long long>(j) * p.channels, f, in.cn);
         }
     }
     for (int i = i0; i < i1; i += kAhead) {
@@ -110,7 +109,7 @@ __global__ void __launch_bounds__(256) ptq_conv_kernel(const ConvParams p)
 #pragma unroll
                 for (int j = 0; j < kW - 1; ++j) x[j][e] = x[j + 1][e];
             }
-            if (i + a < i1) store_piece<T, kE>(static_cast<T *>(p.y) + in.dense(i + a), y, in.cn, p.whole);
+            if (i + a < i1) store_piece<kWhole, T, kE>(static_cast<T *>(p.y) + in.dense(i + a), y, in.cn);
         }
     }
 }
@@ -118,7 +117,7 @@ __global__ void __launch_bounds__(256) ptq_conv_kernel(const ConvParams p)
 // Gradients: dpre = dy silu'(pre) of the segment's outputs and of the W - 1 behind it gives dx of the segment,
 // dx[i] = sum_j weight[j] dpre[i + (W-1) - j], and x times dpre of the segment's own outputs dweight.  A warp takes 32 pieces of a
 // segment, goes on to others and keeps the sums of dweight and dbias in registers.
-template <typename T, int kE, int kW>
+template <typename T, int kE, int kW, bool kWhole>
 __global__ void __launch_bounds__(256) ptq_conv_backward_kernel(const ConvParams p)
 {
     __shared__ float s_sum[8][32 * kE];
@@ -136,7 +135,7 @@ __global__ void __launch_bounds__(256) ptq_conv_backward_kernel(const ConvParams
     const long long total = static_cast<long long>(p.batch) * p.segments;
     for (long long row = blockIdx.y * 8ll + warp; row < total && cn > 0; row += gridDim.y * 8ll) {
         const int seg = static_cast<int>(row % p.segments);
-        const ConvRow<T, kE, kW> in(p, static_cast<int>(row / p.segments), piece);
+        const ConvRow<T, kE, kW, kWhole> in(p, static_cast<int>(row / p.segments), piece);
         const int i0 = seg * p.segment, end = min(i0 + p.segment, p.length), i1 = min(end, in.len);
         const int first = seg == 0 ? -(kW - 1) : i0;      // the first segment makes the state's gradient too
         float x[kW][kE], d[kW][kE];                        // rows o-(W-1) .. o; dpre of the same rows
@@ -153,7 +152,7 @@ __global__ void __launch_bounds__(256) ptq_conv_backward_kernel(const ConvParams
         const int tail = in.len - (kW - 1);               // step of the final state's first row
         Piece<T, kE> nx = in.input(i0), nd;
         const auto dy_of = [&](int o) {
-            return load_piece<T, kE>(static_cast<const T *>(p.dy) + in.dense(min(o, p.length - 1)), o < in.len ? cn : 0, p.whole);
+            return load_piece<kWhole, T, kE>(static_cast<const T *>(p.dy) + in.dense(min(o, p.length - 1)), o < in.len ? cn : 0);
         };
         nd = dy_of(i0);
         for (int o = i0; o < end + kW - 1; ++o) {
@@ -193,16 +192,16 @@ __global__ void __launch_bounds__(256) ptq_conv_backward_kernel(const ConvParams
             const int i = o - (kW - 1);                    // the step whose gradient is complete now
             if (i >= first && i < end) {
                 if (p.dfinal && i >= tail && i < in.len) {
-                    const Piece<T, kE> f = load_piece<T, kE>(
-                        static_cast<const T *>(p.dfinal) + (static_cast<long long>(in.b) * (kW - 1) + (i - tail)) * p.channels + c, cn, p.whole);
+                    const Piece<T, kE> f = load_piece<kWhole, T, kE>(
+                        static_cast<const T *>(p.dfinal) + (static_cast<long long>(in.b) * (kW - 1) + (i - tail)) * p.channels + c, cn);
 #pragma unroll
                     for (int e = 0; e < kE; ++e) out[e] += f[e];
                 }
                 if (i >= 0)
-                    store_piece<T, kE>(static_cast<T *>(p.dx) + in.dense(i), out, cn, p.whole);
+                    store_piece<kWhole, T, kE>(static_cast<T *>(p.dx) + in.dense(i), out, cn);
                 else if (p.dstate)
-                    store_piece<T, kE>(static_cast<T *>(p.dstate) + (static_cast<long long>(in.b) * (kW - 1) + (i + kW - 1)) * p.channels + c, out,
-                                       cn, p.whole);
+                    store_piece<kWhole, T, kE>(static_cast<T *>(p.dstate) + (static_cast<long long>(in.b) * (kW - 1) + (i + kW - 1)) * p.channels + c, out,
+                                       cn);
             }
         }
     }

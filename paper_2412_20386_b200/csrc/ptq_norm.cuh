@@ -23,7 +23,7 @@ struct NormParams {
     long long rows;
     int cols, gate_at;
     float eps, inv_cols;
-    bool layer, whole;
+    bool layer;
     void *y, *residual_out;                     // dense
     // backward
     const void *dy, *dresidual_out;             // dense; dresidual_out may be null
@@ -54,7 +54,7 @@ __device__ __forceinline__ void row_sums(float (&v)[kV], float *buf, int warp, i
     }
 }
 
-template <typename T, typename R, int kRB, bool kBackward>
+template <typename T, typename R, int kRB, bool kBackward, bool kWhole>
 __global__ void __launch_bounds__(kRB > 1 ? 256 : 1024) ptq_norm_kernel(const NormParams p)
 {
     constexpr int kStages = 3;
@@ -78,12 +78,12 @@ __global__ void __launch_bounds__(kRB > 1 ? 256 : 1024) ptq_norm_kernel(const No
         for (int i = 0; i < kRB; ++i) {
             const long long m = m0 + i;
             const int n = m < p.rows ? cn : 0;
-            x[i] = load_piece<T, 8>(static_cast<const T *>(p.x) + m * p.x_l + c, n, p.whole);
-            if (p.residual) res[i] = load_piece<R, 8>(static_cast<const R *>(p.residual) + m * p.residual_l + c, n, p.whole);
-            if (p.gate) g[i] = load_piece<T, 8>(static_cast<const T *>(p.gate) + m * p.gate_l + c, n, p.whole);
+            x[i] = load_piece<kWhole, T, 8>(static_cast<const T *>(p.x) + m * p.x_l + c, n);
+            if (p.residual) res[i] = load_piece<kWhole, R, 8>(static_cast<const R *>(p.residual) + m * p.residual_l + c, n);
+            if (p.gate) g[i] = load_piece<kWhole, T, 8>(static_cast<const T *>(p.gate) + m * p.gate_l + c, n);
             if (kBackward) {
-                dy[i] = load_piece<T, 8>(static_cast<const T *>(p.dy) + m * p.cols + c, n, p.whole);
-                if (p.dresidual_out) dres[i] = load_piece<R, 8>(static_cast<const R *>(p.dresidual_out) + m * p.cols + c, n, p.whole);
+                dy[i] = load_piece<kWhole, T, 8>(static_cast<const T *>(p.dy) + m * p.cols + c, n);
+                if (p.dresidual_out) dres[i] = load_piece<kWhole, R, 8>(static_cast<const R *>(p.dresidual_out) + m * p.cols + c, n);
             }
         }
         float r[kRB][8], mean[kRB], rstd[kRB];
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kRB > 1 ? 256 : 1024) ptq_norm_kernel(const No
 #pragma unroll
         for (int i = 0; i < kRB; ++i) {
             if (!kBackward && p.residual_out && m0 + i < p.rows)
-                store_piece<R, 8>(static_cast<R *>(p.residual_out) + (m0 + i) * p.cols + c, r[i], cn, p.whole);
+                store_piece<kWhole, R, 8>(static_cast<R *>(p.residual_out) + (m0 + i) * p.cols + c, r[i], cn);
             rstd[i] = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(kRB > 1 ? 256 : 1024) ptq_norm_kernel(const No
                     y[e] = fmaf(r[i][e], weight[e], bias[e]);
                     if (p.gate_at == kGateOut) y[e] *= g[i][e] * sigmoid_f32(g[i][e]);
                 }
-                store_piece<T, 8>(static_cast<T *>(p.y) + (m0 + i) * p.cols + c, y, cn, p.whole);
+                store_piece<kWhole, T, 8>(static_cast<T *>(p.y) + (m0 + i) * p.cols + c, y, cn);
             }
         } else {
             float sums[2 * kRB], dn[kRB][8];
@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(kRB > 1 ? 256 : 1024) ptq_norm_kernel(const No
                     sums[2 * i] = fmaf(dn[i][e], r[i][e], sums[2 * i]);
                     sums[2 * i + 1] += dn[i][e];
                 }
-                if (p.gate_at == kGateOut && m0 + i < p.rows) store_piece<T, 8>(static_cast<T *>(p.dgate) + (m0 + i) * p.cols + c, dg, cn, p.whole);
+                if (p.gate_at == kGateOut && m0 + i < p.rows) store_piece<kWhole, T, 8>(static_cast<T *>(p.dgate) + (m0 + i) * p.cols + c, dg, cn);
             }
             row_sums<2 * kRB>(sums, s_sum[parity][2], warp, warps, lane);
 #pragma unroll
@@ -177,9 +177,9 @@ __global__ void __launch_bounds__(kRB > 1 ? 256 : 1024) ptq_norm_kernel(const No
                     sum_s[e] = fmaf(dr[e], v, sum_s[e]);
                 }
                 const long long at = (m0 + i) * p.cols + c;
-                store_piece<T, 8>(static_cast<T *>(p.dx) + at, dx, cn, p.whole);
-                if (p.dresidual) store_piece<R, 8>(static_cast<R *>(p.dresidual) + at, dr, cn, p.whole);
-                if (p.gate_at == kGateIn) store_piece<T, 8>(static_cast<T *>(p.dgate) + at, dg, cn, p.whole);
+                store_piece<kWhole, T, 8>(static_cast<T *>(p.dx) + at, dx, cn);
+                if (p.dresidual) store_piece<kWhole, R, 8>(static_cast<R *>(p.dresidual) + at, dr, cn);
+                if (p.gate_at == kGateIn) store_piece<kWhole, T, 8>(static_cast<T *>(p.dgate) + at, dg, cn);
             }
         }
     }

@@ -19,7 +19,7 @@
 namespace ptq {
 
 constexpr int kScanHistory = 16;      // steps between two states that are kept for the backward pass
-constexpr int kScanThreads = 256;
+constexpr int kScanThreads = 256, kScanLeast = 128;       // of a CTA: most, and fewest where a channel has fewer than eight lanes
 
 constexpr unsigned kScanSoftplus = 1u, kScanReverse = 2u;
 
@@ -33,8 +33,6 @@ struct ScanParams {
     int group_blocks;                           // CTAs that share the channels of a group
     int chunk_len, chunks;
     unsigned flags;
-    bool whole;                                 // u, delta, z, y, and dy, allow accesses of 16 bytes
-    bool whole_n;                               // states % 4 == 0 and the state pointers are 16-byte aligned
     float *slots;                               // [chunks][batch][channels][states]
     float *sums;                                // [chunks][batch][channels]: sum of dt of a chunk
     // forward
@@ -49,8 +47,47 @@ struct ScanParams {
     float *part_BC;                             // [groups * group_blocks][batch][length][2 states], null: straight to dB, dC
 };
 
-// log(1 + e^x)
-__device__ __forceinline__ float softplus_f32(float x) { return x > 20.0f ? x : log1pf(expf(x)); }
+// e^-|x|, the argument of the power of two to about 2^-46: its rounding alone would cost four units in the last place at |x| = 7.
+// |x| is cut at 126, where the result is zero.
+__device__ __forceinline__ float exp_minus_abs(float x)
+{
+    const float m = -fminf(fabsf(x), 126.0f), y = m * kLog2e;
+    const float rest = fmaf(m, 1.925963033e-8f, fmaf(m, kLog2e, -y));
+    const float t = exp2_approx(y);
+    return fmaf(t, rest * kLn2, t);
+}
+// log(1 + e^x) = max(x, 0) + log(1 + t), t = e^-|x|; log(1 + t) / t is a polynomial fitted to 5e-9 on [0, 1]: accurate relative to the
+// result, small ones too, with about 20 instructions (expf and log1pf take twice as many).
+__device__ __forceinline__ float softplus_of(float x, float t)
+{
+    float p = -0.0032440212f;
+    p = fmaf(p, t, 0.01985144429f);
+    p = fmaf(p, t, -0.05695949867f);
+    p = fmaf(p, t, 0.106036514f);
+    p = fmaf(p, t, -0.1530559063f);
+    p = fmaf(p, t, 0.1967593879f);
+    p = fmaf(p, t, -0.2495413423f);
+    p = fmaf(p, t, 0.3332996368f);
+    p = fmaf(p, t, -0.4999990165f);
+    p = fmaf(p, t, 1.0f);
+    return fmaf(p, t, x <= 0.0f ? 0.0f : x);              // NaN passes through
+}
+__device__ __forceinline__ float softplus_f32(float x) { return softplus_of(x, exp_minus_abs(x)); }
+
+// exp(dt A) as 2^(dt rate).  The hardware's power of two is low by 0.1 to 0.35 units of 2^-24 on average for the arguments of slow decays
+// (-0.1 .. 0), where a state multiplies hundreds of them: the argument is raised by a quarter of a unit, which the fused multiply-add
+// does at no cost and which rounds away where the memory is short.  2^kDecayShift is 1: a step with dt = 0 keeps the state.
+constexpr float kDecayShift = 2.15e-8f;
+template <int kNS>
+__device__ __forceinline__ void scan_decays(float (&a)[kNS], float dt, const float (&rate)[kNS])
+{
+    float shift[kNS];
+#pragma unroll
+    for (int k = 0; k < kNS; ++k) shift[k] = kDecayShift;
+    fma_each<kNS>(a, dt, rate, shift);
+#pragma unroll
+    for (int k = 0; k < kNS; ++k) a[k] = exp2_approx(a[k]);
+}
 
 // Decay rates times log2(e); finite, so that a step without a token (dt = 0) leaves the state as it is.
 __device__ __forceinline__ float scan_rate(float a) { return fminf(fmaxf(a * kLog2e, -3.0e38f), 3.0e38f); }
@@ -78,16 +115,16 @@ struct ScanBlock {
 
 // The state that enters a chunk, from what the chunks between it and `first` add: slot j holds the sum of chunk j alone (that of the
 // one next to the sequence's end holds the true state), sums[j] its dt.
-template <int kNS>
+template <bool kWhole, int kNS>
 __device__ __forceinline__ void scan_fold(float (&h)[kNS], const float (&rate)[kNS], const ScanParams &p, int b, int d, int n0, int nn, int from,
                                           int to, int by)
 {
     const long long row = static_cast<long long>(b) * p.channels + d, step = static_cast<long long>(p.batch) * p.channels;
-    load_floats<kNS>(h, p.slots + (from * step + row) * p.states + n0, nn, p.whole_n);
+    load_floats<kWhole, kNS>(h, p.slots + (from * step + row) * p.states + n0, nn);
 #pragma unroll 4
     for (int j = from + by; j != to; j += by) {
         float v[kNS];
-        load_floats<kNS>(v, p.slots + (j * step + row) * p.states + n0, nn, p.whole_n);
+        load_floats<kWhole, kNS>(v, p.slots + (j * step + row) * p.states + n0, nn);
         const float s = p.sums[j * step + row];
 #pragma unroll
         for (int k = 0; k < kNS; ++k) h[k] = fmaf(exp2_approx(rate[k] * s), h[k], v[k]);
@@ -98,28 +135,69 @@ __device__ __forceinline__ void scan_fold(float (&h)[kNS], const float (&rate)[k
 // state, from the last step to the first: e <- exp(dt A) (C dy silu(z) + e), for each chunk but the first one.
 enum { kScanForward = 0, kScanSum = 1, kScanGradSum = 2 };
 
-template <typename T, int kNS, int kS, int kMode>
-__global__ void __launch_bounds__(kScanThreads, 2) ptq_scan_kernel(const ScanParams p)
+template <typename T, int kNS, int kS, int kMode, bool kWhole>
+__global__ void __launch_bounds__(kScanThreads, 3) ptq_scan_kernel(const ScanParams p)
 {
     constexpr int kRows = 8 * kS, kNP = kNS * kS;         // steps of a tile, states padded
     constexpr int kGroup = kS < 4 ? 4 : kS;               // steps between two joint sums over the lanes of a channel
-    constexpr int kLeast = kS == 8 ? kScanThreads : 64;   // threads of the smallest CTA
-    constexpr int kBC = (kRows * kNP + kLeast - 1) / kLeast;              // values of B (and C) that a thread loads at most
     constexpr bool kBackward = kMode == kScanGradSum;
+    constexpr int kHalf = kRows * kS;                     // pieces of B (or of C) in a tile
+    constexpr int kLeast = kS == 8 ? kScanThreads : kScanLeast;
+    constexpr int kPieces = ((kMode == kScanForward ? 2 : 1) * kHalf + kLeast - 1) / kLeast;      // of a thread, at most
     extern __shared__ __align__(16) unsigned char scan_smem[];
     const int threads = blockDim.x, tid = threadIdx.x, lane = tid & 31;
     const int width = threads / kS;                       // channels of the CTA
     float2 *s_pair = reinterpret_cast<float2 *>(scan_smem);                       // [kRows][width]: (dt, dt u), later (o, -)
-    float *s_B = reinterpret_cast<float *>(s_pair + kRows * width);               // [kRows][kNP]
-    float *s_C = s_B + kRows * kNP;
+    float *s_B = reinterpret_cast<float *>(s_pair + kRows * width);               // [kRows][kNP], then C likewise
     const ScanBlock blk(p, blockIdx.x, kMode == kScanForward ? p.chunks : p.chunks - 1, kBackward ? 1 : 0, width);
     const bool softplus = p.flags & kScanSoftplus, reverse = p.flags & kScanReverse;
+    const int n_steps = max(blk.i1 - blk.i0, 0);
+    // step k of the chunk's loop is step i of the sequence, token first + k * way
+    const bool down = reverse != kBackward;
+    const int first_step = kBackward ? blk.i1 - 1 : blk.i0;
+    const long long first = reverse ? blk.len - 1 - first_step : first_step;
+    const int way = down ? -1 : 1;
+
+    // the thread's part of a row
+    const int row = tid / (width / 8), c = blk.c0 + (tid % (width / 8)) * 8;
+    const int cn = max(min(8, blk.c_end - c), 0);
+    const long long tok = first + way * row;
+    const T *at_u = kBackward ? static_cast<const T *>(p.dy) + (static_cast<long long>(blk.b) * p.length + tok) * p.channels + c
+                              : static_cast<const T *>(p.u) + blk.b * p.u_b + tok * p.u_l + c;
+    const T *at_delta = static_cast<const T *>(p.delta) + blk.b * p.delta_b + tok * p.delta_l + c;
+    const T *at_z = static_cast<const T *>(p.z) + blk.b * p.z_b + tok * p.z_l + c;
+    const long long next_u = way * kRows * (kBackward ? static_cast<long long>(p.channels) : p.u_l), next_delta = way * kRows * p.delta_l,
+                    next_z = way * kRows * p.z_l;
+    const bool gated = kMode != kScanSum && p.z;
+    Piece<T, 8> r_u, r_delta, r_z;
+    Piece<T, kNS> r_BC[kPieces];
+    const auto fetch = [&](int k0) {
+        const int n = k0 + row < n_steps ? cn : 0;
+        r_u = load_piece<kWhole, T, 8>(at_u, n);
+        r_delta = load_piece<kWhole, T, 8>(at_delta, n);
+        if (gated) r_z = load_piece<kWhole, T, 8>(at_z, n);
+        at_u += next_u;
+        at_delta += next_delta;
+        at_z += next_z;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int q = tid + i * threads, t = (q % kHalf) / kS, n0 = q % kS * kNS;
+            const bool is_C = kMode == kScanForward ? q >= kHalf : kBackward;
+            const bool on = q < (kMode == kScanForward ? 2 : 1) * kHalf && k0 + t < n_steps;
+            const long long token = first + way * (k0 + t);
+            const T *from = is_C ? static_cast<const T *>(p.C) + blk.b * p.C_b + token * p.C_l + blk.g * p.C_g + n0
+                                 : static_cast<const T *>(p.B) + blk.b * p.B_b + token * p.B_l + blk.g * p.B_g + n0;
+            r_BC[i] = load_piece<false, T, kNS>(from, on ? p.states - n0 : 0);
+        }
+    };
+    if (n_steps > 0) fetch(0);
+    const Piece<float, 8> bias = load_piece<kWhole, float, 8>(p.delta_bias + c, p.delta_bias ? cn : 0);
 
     // the lane's channel and states
     const int ch = tid / kS, n0 = (tid % kS) * kNS, d = blk.c0 + ch, col = scan_column(ch);
     const int nn = d < blk.c_end ? max(min(kNS, p.states - n0), 0) : 0;
     float rate[kNS], h[kNS];
-    load_floats<kNS>(rate, p.A + static_cast<long long>(d) * p.states + n0, nn, p.whole_n);
+    load_floats<kWhole, kNS>(rate, p.A + static_cast<long long>(d) * p.states + n0, nn);
 #pragma unroll
     for (int k = 0; k < kNS; ++k) {
         rate[k] = scan_rate(rate[k]);
@@ -129,113 +207,90 @@ __global__ void __launch_bounds__(kScanThreads, 2) ptq_scan_kernel(const ScanPar
     const long long slot_step = static_cast<long long>(p.batch) * p.channels * p.states;
     if constexpr (kMode == kScanForward) {
         if (blk.chunk > 0) {
-            if (nn > 0) scan_fold<kNS>(h, rate, p, blk.b, d, n0, nn, 1, blk.chunk + 1, 1);
+            if (nn > 0) scan_fold<kWhole, kNS>(h, rate, p, blk.b, d, n0, nn, 1, blk.chunk + 1, 1);
         } else if (p.state) {
-            load_floats<kNS>(h, (p.chunks > 1 ? p.slots : p.state) + state_at, nn, p.whole_n);
+            load_floats<kWhole, kNS>(h, (p.chunks > 1 ? p.slots : p.state) + state_at, nn);
         }
     } else if constexpr (kMode == kScanSum) {
         // chunk 0 starts from the true state; the second launch takes it from a copy, since the final state may replace it
         if (blk.chunk == 0 && p.state) {
-            load_floats<kNS>(h, p.state + state_at, nn, p.whole_n);
-            store_floats<kNS>(p.slots + state_at, h, nn, p.whole_n);
+            load_floats<kWhole, kNS>(h, p.state + state_at, nn);
+            store_floats<kWhole, kNS>(p.slots + state_at, h, nn);
         }
     } else if (blk.chunk == p.chunks - 1 && p.dfinal) {
-        load_floats<kNS>(h, p.dfinal + state_at, nn, p.whole_n);
+        load_floats<kWhole, kNS>(h, p.dfinal + state_at, nn);
     }
     float sum_dt = 0.0f;
+    T *at_y = static_cast<T *>(p.y) + (static_cast<long long>(blk.b) * p.length + tok) * p.channels + c;
+    float *at_kept = nullptr;
+    if (kMode == kScanForward && p.history)
+        at_kept = p.history +
+                  ((blk.b * static_cast<long long>((p.length + kScanHistory - 1) / kScanHistory) + blk.i0 / kScanHistory) * p.channels + d) * p.states + n0;
 
-    // the thread's part of a row
-    const int row = tid / (width / 8), c = blk.c0 + (tid % (width / 8)) * 8;
-    const int cn = max(min(8, blk.c_end - c), 0);
-    float bias[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) bias[e] = p.delta_bias && e < cn ? p.delta_bias[c + e] : 0.0f;
-    Piece<T, 8> r_u, r_delta, r_z;
-    T r_B[kBC], r_C[kBC];
-    const int n_steps = max(blk.i1 - blk.i0, 0);
-    // step k of the chunk's loop is step i of the sequence
-    const auto step_of = [&](int k) { return kBackward ? blk.i1 - 1 - k : blk.i0 + k; };
-    const auto token_of = [&](int i) { return static_cast<long long>(reverse ? blk.len - 1 - i : i); };
-    const auto fetch = [&](int k0) {
-        const bool on = k0 + row < n_steps;
-        const long long at = on ? token_of(step_of(k0 + row)) : 0;
-        const int n = on ? cn : 0;
-        const bool whole = p.whole;
-        if constexpr (kBackward)
-            r_u = load_piece<T, 8>(static_cast<const T *>(p.dy) + (static_cast<long long>(blk.b) * p.length + at) * p.channels + c, n, whole);
-        else
-            r_u = load_piece<T, 8>(static_cast<const T *>(p.u) + blk.b * p.u_b + at * p.u_l + c, n, whole);
-        r_delta = load_piece<T, 8>(static_cast<const T *>(p.delta) + blk.b * p.delta_b + at * p.delta_l + c, n, whole);
-        if (kMode != kScanSum && p.z) r_z = load_piece<T, 8>(static_cast<const T *>(p.z) + blk.b * p.z_b + at * p.z_l + c, n, whole);
-#pragma unroll
-        for (int i = 0; i < kBC; ++i) {
-            const int idx = tid + i * threads, t = idx / kNP, n1 = idx % kNP;
-            r_B[i] = r_C[i] = from_f32<T>(0.0f);
-            if (t < kRows && n1 < p.states && k0 + t < n_steps) {
-                const long long tok = token_of(step_of(k0 + t));
-                if (!kBackward) r_B[i] = __ldg(static_cast<const T *>(p.B) + blk.b * p.B_b + tok * p.B_l + blk.g * p.B_g + n1);
-                if (kMode != kScanSum) r_C[i] = __ldg(static_cast<const T *>(p.C) + blk.b * p.C_b + tok * p.C_l + blk.g * p.C_g + n1);
-            }
-        }
-    };
-    if (n_steps > 0) fetch(0);
+    float2 *const own = s_pair + row * width;             // the row that the thread fills and finishes
     for (int k0 = 0; k0 < n_steps; k0 += kRows) {
         const bool row_on = k0 + row < n_steps;
-        float u[8], gate[8];
+        const Piece<T, 8> u = r_u, z = r_z;
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
             float4 pair;
 #pragma unroll
             for (int o = 0; o < 2; ++o) {
                 const float x = r_delta[e + o] + bias[e + o];
-                float dt = softplus ? softplus_f32(x) : x;
-                if (!row_on) dt = 0.0f;
-                u[e + o] = r_u[e + o];
-                gate[e + o] = kMode != kScanSum && p.z ? r_z[e + o] * sigmoid_f32(r_z[e + o]) : 1.0f;
-                const float in = kBackward ? u[e + o] * gate[e + o] : dt * u[e + o];
+                const float dt = !row_on ? 0.0f : softplus ? softplus_f32(x) : x;
+                float in = r_u[e + o];
+                if constexpr (kBackward) {
+                    if (gated) in *= r_z[e + o] * sigmoid_f32(r_z[e + o]);
+                } else {
+                    in *= dt;
+                }
                 (o ? pair.z : pair.x) = dt;
                 (o ? pair.w : pair.y) = row_on ? in : 0.0f;
             }
-            *reinterpret_cast<float4 *>(s_pair + row * width + scan_column(c - blk.c0 + e)) = pair;
+            *reinterpret_cast<float4 *>(own + scan_column(c - blk.c0 + e)) = pair;
         }
 #pragma unroll
-        for (int i = 0; i < kBC; ++i) {
-            const int idx = tid + i * threads;
-            if (idx < kRows * kNP) {
-                if (!kBackward) s_B[idx] = to_f32<T>(r_B[i]);
-                if (kMode != kScanSum) s_C[idx] = to_f32<T>(r_C[i]);
+        for (int i = 0; i < kPieces; ++i) {
+            const int q = tid + i * threads;
+            if (q < (kMode == kScanForward ? 2 : 1) * kHalf) {
+                float f[kNS];
+#pragma unroll
+                for (int k = 0; k < kNS; ++k) f[k] = r_BC[i][k];
+                store_floats<true, kNS>(s_B + q * kNS, f, kNS);
             }
         }
         __syncthreads();
         if (k0 + kRows < n_steps) fetch(k0 + kRows);
         const int rows = min(kRows, n_steps - k0);
-        const float *s_in = kBackward ? s_C : s_B;
         for (int t = 0; t < rows; t += kGroup) {          // rows without a token have dt = 0: the state stays as it is
-            if (kMode == kScanForward && p.history && ((k0 + t) & (kScanHistory - 1)) == 0) {
-                const long long j = (blk.i0 + k0 + t) / kScanHistory, per = (p.length + kScanHistory - 1) / kScanHistory;
-                store_floats<kNS>(p.history + ((blk.b * per + j) * p.channels + d) * p.states + n0, h, nn, p.whole_n);
+            if (kMode == kScanForward && at_kept && ((k0 + t) & (kScanHistory - 1)) == 0) {
+                store_floats<kWhole, kNS>(at_kept, h, nn);
+                at_kept += static_cast<long long>(p.channels) * p.states;
             }
             float o[kGroup];
 #pragma unroll
             for (int s = 0; s < kGroup; ++s) {
                 const float2 x = s_pair[(t + s) * width + col];
-                float in[kNS], out[kNS];
-                load_floats<kNS>(in, s_in + (t + s) * kNP + n0, kNS, true);
-                if (kMode == kScanForward) load_floats<kNS>(out, s_C + (t + s) * kNP + n0, kNS, true);
-                if (kMode != kScanForward) sum_dt += x.x;
-                o[s] = 0.0f;
-#pragma unroll
-                for (int k = 0; k < kNS; ++k) {
-                    const float a = exp2_approx(x.x * rate[k]);
-                    if constexpr (kBackward)
-                        h[k] = a * fmaf(x.y, in[k], h[k]);
-                    else
-                        h[k] = fmaf(a, h[k], x.y * in[k]);
-                    if (kMode == kScanForward) o[s] = fmaf(h[k], out[k], o[s]);
+                float in[kNS], a[kNS];
+                load_floats<true, kNS>(in, s_B + (t + s) * kNP + n0, kNS);
+                scan_decays<kNS>(a, x.x, rate);
+                if constexpr (kBackward) {
+                    fma_each<kNS>(h, x.y, in, h);
+                    mul_each<kNS>(h, a, h);
+                } else {
+                    mul_each<kNS>(in, x.y, in);
+                    fma_each<kNS>(h, a, h, in);
+                }
+                if constexpr (kMode == kScanForward) {
+                    float out[kNS];
+                    load_floats<true, kNS>(out, s_B + kHalf * kNS + (t + s) * kNP + n0, kNS);
+                    o[s] = dot_each<kNS>(h, out);
+                } else {
+                    sum_dt += x.x;
                 }
             }
             if constexpr (kMode == kScanForward) {
-                // every lane of the channel ends up with the sum of one of kS steps (of each of kGroup, if it is alone)
+                // every lane of the channel ends up with the sum of one of kS steps
 #pragma unroll
                 for (int s = 0; s < kGroup; s += kS) {
                     float v[kS];
@@ -253,24 +308,29 @@ __global__ void __launch_bounds__(kScanThreads, 2) ptq_scan_kernel(const ScanPar
                 float y[8];
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
-                    const float4 pair = *reinterpret_cast<const float4 *>(s_pair + row * width + scan_column(c - blk.c0 + e));
-#pragma unroll
-                    for (int o = 0; o < 2; ++o) {
-                        float v = o ? pair.z : pair.x;
-                        if (p.D && e + o < cn) v = fmaf(__ldg(p.D + c + e + o), u[e + o], v);
-                        y[e + o] = v * gate[e + o];
-                    }
+                    const float4 pair = *reinterpret_cast<const float4 *>(own + scan_column(c - blk.c0 + e));
+                    y[e] = pair.x;
+                    y[e + 1] = pair.z;
                 }
-                store_piece<T, 8>(static_cast<T *>(p.y) + (static_cast<long long>(blk.b) * p.length + token_of(blk.i0 + k0 + row)) * p.channels + c,
-                                  y, cn, p.whole);
+                if (p.D) {
+                    const Piece<float, 8> skip = load_piece<kWhole, float, 8>(p.D + c, cn);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = fmaf(skip[e], u[e], y[e]);
+                }
+                if (gated) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] *= z[e] * sigmoid_f32(z[e]);
+                }
+                store_piece<kWhole, T, 8>(at_y, y, cn);
             }
+            at_y += static_cast<long long>(way * kRows) * p.channels;
         }
     }
     if constexpr (kMode == kScanForward) {
-        if (p.final_state && blk.chunk == p.chunks - 1) store_floats<kNS>(p.final_state + state_at, h, nn, p.whole_n);
+        if (p.final_state && blk.chunk == p.chunks - 1) store_floats<kWhole, kNS>(p.final_state + state_at, h, nn);
     } else {
         // forward: slot j + 1 is the state behind chunk j; backward: slot j the gradient in front of chunk j
-        store_floats<kNS>(p.slots + (blk.chunk + (kBackward ? 0 : 1)) * slot_step + state_at, h, nn, p.whole_n);
+        store_floats<kWhole, kNS>(p.slots + (blk.chunk + (kBackward ? 0 : 1)) * slot_step + state_at, h, nn);
         if (n0 == 0 && nn > 0)
             p.sums[(static_cast<long long>(blk.chunk + (kBackward ? 0 : 1)) * p.batch + blk.b) * p.channels + d] = sum_dt;
     }
@@ -284,22 +344,26 @@ __global__ void __launch_bounds__(kScanThreads, 2) ptq_scan_kernel(const ScanPar
 // of a warp, the warps' sums through shared memory, the CTAs' through global memory, each in a fixed order); over the
 // states of a channel o, s and r.  The rows' threads then make du = dt s + D dyo, ddelta = (u s + r ln 2) sigmoid and dz.
 // Bound: issue slots (about 24 per state and step, seven of them the sums of dB and dC).
-template <typename T, int kNS, int kS>
+template <typename T, int kNS, int kS, bool kWhole>
 __global__ void __launch_bounds__(kScanThreads, 2) ptq_scan_backward_kernel(const ScanParams p)
 {
     constexpr int kRows = kScanHistory, kNP = kNS * kS, kE = kRows / kS;     // channels of a row that a thread holds
-    constexpr int kLeast = kS == 8 ? kScanThreads : 64;
-    constexpr int kBC = (kRows * kNP + kLeast - 1) / kLeast;
+    constexpr bool kEarly = kE <= 4;                      // the next tile's rows are fetched into registers during this one's recurrence
+    constexpr int kHalf = kRows * kS;                     // pieces of B (or of C) in a tile
+    constexpr int kLeast = kS == 8 ? kScanThreads : kScanLeast;
+    constexpr int kPieces = (2 * kHalf + kLeast - 1) / kLeast;
     constexpr int kSteps = 8 / kNS;                       // steps whose dB (dC) values are summed together: eight values
+    constexpr int kLeft = kS >= 4 ? kS / 4 : 1;           // of them left in a lane
     constexpr int kGroup = kSteps > kS ? kSteps : kS;     // steps of an unrolled group
+    constexpr int kPairs = kS >= 4 ? kS / 2 : 1;          // steps whose (s, r) are summed together
     extern __shared__ __align__(16) unsigned char scan_smem[];
     const int threads = blockDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5;
     const int width = threads / kS;
     float2 *s_pair = reinterpret_cast<float2 *>(scan_smem);                       // [kRows][width]: (dt, dt u), later (s, r)
     float *s_do = reinterpret_cast<float *>(s_pair + kRows * width);              // [kRows][width]: dyo
     float *s_o = s_do + kRows * width;                                            // [kRows][width]: o without D u
-    float *s_B = s_o + kRows * width, *s_C = s_B + kRows * kNP;                   // [kRows][kNP]
-    float *s_sum = s_C + kRows * kNP;                                             // [warps][kRows][2][kNP]: dB, dC
+    float *s_BC = s_o + kRows * width;                                            // [2][kRows][kNP]
+    float *s_sum = s_BC + 2 * kRows * kNP;                                        // [warps][kRows][2][kNP]: dB, dC
     const ScanBlock blk(p, blockIdx.x, p.chunks, 0, width);
     const bool softplus = p.flags & kScanSoftplus, reverse = p.flags & kScanReverse;
 
@@ -307,16 +371,16 @@ __global__ void __launch_bounds__(kScanThreads, 2) ptq_scan_backward_kernel(cons
     const int nn = d < blk.c_end ? max(min(kNS, p.states - n0), 0) : 0;
     const long long state_at = (static_cast<long long>(blk.b) * p.channels + d) * p.states + n0;
     float rate[kNS], e[kNS], dA[kNS];
-    load_floats<kNS>(rate, p.A + static_cast<long long>(d) * p.states + n0, nn, p.whole_n);
+    load_floats<kWhole, kNS>(rate, p.A + static_cast<long long>(d) * p.states + n0, nn);
 #pragma unroll
     for (int k = 0; k < kNS; ++k) {
         rate[k] = scan_rate(rate[k]);
         e[k] = dA[k] = 0.0f;
     }
     if (blk.chunk < p.chunks - 1) {
-        if (nn > 0) scan_fold<kNS>(e, rate, p, blk.b, d, n0, nn, p.chunks - 1, blk.chunk, -1);
+        if (nn > 0) scan_fold<kWhole, kNS>(e, rate, p, blk.b, d, n0, nn, p.chunks - 1, blk.chunk, -1);
     } else if (p.dfinal) {
-        load_floats<kNS>(e, p.dfinal + state_at, nn, p.whole_n);
+        load_floats<kWhole, kNS>(e, p.dfinal + state_at, nn);
     }
 
     const int row = tid / (width / kE), c = blk.c0 + (tid % (width / kE)) * kE;
@@ -324,220 +388,255 @@ __global__ void __launch_bounds__(kScanThreads, 2) ptq_scan_backward_kernel(cons
     float sum_D[kE], sum_bias[kE];
 #pragma unroll
     for (int i = 0; i < kE; ++i) sum_D[i] = sum_bias[i] = 0.0f;
-    Piece<T, kE> r_u, r_delta, r_z, r_dy;
-    T r_B[kBC], r_C[kBC];
-    float r_h[kNS];
+    struct Rows {
+        Piece<T, kE> u, delta, z, dy;
+    };
+    const long long sequence = static_cast<long long>(blk.b) * p.length;
     const long long kept_rows = (p.length + kScanHistory - 1) / kScanHistory;
     const auto token_of = [&](int i) { return static_cast<long long>(reverse && i < blk.len ? blk.len - 1 - i : i); };
-    const auto fetch = [&](int i0) {
+    const auto rows_of = [&](int i0) {
+        Rows r;
         const bool on = i0 + row < blk.i1;
         const long long at = on ? token_of(i0 + row) : 0;
         const int n = on ? cn : 0;
-        r_u = load_piece<T, kE>(static_cast<const T *>(p.u) + blk.b * p.u_b + at * p.u_l + c, n, p.whole);
-        r_delta = load_piece<T, kE>(static_cast<const T *>(p.delta) + blk.b * p.delta_b + at * p.delta_l + c, n, p.whole);
-        r_dy = load_piece<T, kE>(static_cast<const T *>(p.dy) + (static_cast<long long>(blk.b) * p.length + at) * p.channels + c, n, p.whole);
-        if (p.z) r_z = load_piece<T, kE>(static_cast<const T *>(p.z) + blk.b * p.z_b + at * p.z_l + c, n, p.whole);
-#pragma unroll
-        for (int i = 0; i < kBC; ++i) {
-            const int idx = tid + i * threads, t = idx / kNP, n1 = idx % kNP;
-            r_B[i] = r_C[i] = from_f32<T>(0.0f);
-            if (t < kRows && n1 < p.states && i0 + t < blk.i1) {
-                const long long tok = token_of(i0 + t);
-                r_B[i] = __ldg(static_cast<const T *>(p.B) + blk.b * p.B_b + tok * p.B_l + blk.g * p.B_g + n1);
-                r_C[i] = __ldg(static_cast<const T *>(p.C) + blk.b * p.C_b + tok * p.C_l + blk.g * p.C_g + n1);
-            }
-        }
-        load_floats<kNS>(r_h, p.kept + ((blk.b * kept_rows + i0 / kScanHistory) * p.channels + d) * p.states + n0, nn, p.whole_n);
+        r.u = load_piece<kWhole, T, kE>(static_cast<const T *>(p.u) + blk.b * p.u_b + at * p.u_l + c, n);
+        r.delta = load_piece<kWhole, T, kE>(static_cast<const T *>(p.delta) + blk.b * p.delta_b + at * p.delta_l + c, n);
+        r.dy = load_piece<kWhole, T, kE>(static_cast<const T *>(p.dy) + (sequence + at) * p.channels + c, n);
+        if (p.z) r.z = load_piece<kWhole, T, kE>(static_cast<const T *>(p.z) + blk.b * p.z_b + at * p.z_l + c, n);
+        return r;
     };
-    // tiles without a token: their gradients are zeros
+    Piece<T, kNS> r_BC[kPieces];
+    float r_h[kNS];
+    const auto fetch = [&](int i0) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int q = tid + i * threads, t = (q % kHalf) / kS, n1 = q % kS * kNS;
+            const bool on = q < 2 * kHalf && i0 + t < blk.i1;
+            const long long tok = on ? token_of(i0 + t) : 0;
+            const T *from = q >= kHalf ? static_cast<const T *>(p.C) + blk.b * p.C_b + tok * p.C_l + blk.g * p.C_g + n1
+                                       : static_cast<const T *>(p.B) + blk.b * p.B_b + tok * p.B_l + blk.g * p.B_g + n1;
+            r_BC[i] = load_piece<false, T, kNS>(from, on ? p.states - n1 : 0);
+        }
+        load_floats<kWhole, kNS>(r_h, p.kept + ((blk.b * kept_rows + i0 / kScanHistory) * p.channels + d) * p.states + n0, nn);
+    };
+    const int slot_of_row = row * width;
+    const auto column = [&](int i) { return slot_of_row + scan_column(c - blk.c0 + i); };
+
     const int end = min(blk.i0 + p.chunk_len, p.length);
     int i0 = blk.i0 + (end - 1 - blk.i0) / kRows * kRows;
-    bool fetched = false;
+    // tiles without a token: their gradients are zeros
+    for (; i0 >= blk.i0 && i0 >= blk.i1; i0 -= kRows) {
+        if (i0 + row < end) {
+            float zero[kE];
+#pragma unroll
+            for (int i = 0; i < kE; ++i) zero[i] = 0.0f;
+            const long long at = (sequence + i0 + row) * p.channels + c;
+            store_piece<kWhole, T, kE>(static_cast<T *>(p.du) + at, zero, cn);
+            store_piece<kWhole, T, kE>(static_cast<T *>(p.ddelta) + at, zero, cn);
+            if (p.z) store_piece<kWhole, T, kE>(static_cast<T *>(p.dz) + at, zero, cn);
+        }
+    }
+    // where the thread's sums of dB and dC go: which of the two, which state
+    const int out_which = tid / kNP & 1, out_n = tid % kNP, share = blockIdx.x % (p.groups * p.group_blocks);
+    const auto put_BC = [&](int i, float v) {
+        const long long tok = sequence + token_of(i);
+        if (p.part_BC)
+            p.part_BC[((static_cast<long long>(share) * p.batch * p.length + tok) * 2 + out_which) * p.states + out_n] = v;
+        else
+            static_cast<T *>(out_which ? p.dC : p.dB)[(tok * p.groups + blk.g) * p.states + out_n] = from_f32<T>(v);
+    };
+    const int first_dead = max(i0 + kRows, blk.i0);
+    if (out_n < p.states)
+        for (int i = first_dead + tid / (2 * kNP); i < end; i += threads / (2 * kNP)) put_BC(i, 0.0f);
+
+    Rows ahead;
+    if (i0 >= blk.i0) {
+        fetch(i0);
+        if (kEarly) ahead = rows_of(i0);
+    }
     for (; i0 >= blk.i0; i0 -= kRows) {
-        const bool any = i0 < blk.i1;
-        float dt[kE], slope[kE], gate[kE];
-        if (any) {
-            if (!fetched) fetch(i0);
-            fetched = true;
-            const bool row_on = i0 + row < blk.i1;
+        const bool row_on = i0 + row < blk.i1;
+        {
+            const Rows r = kEarly ? ahead : rows_of(i0);
+            const Piece<float, kE> bias = load_piece<kWhole, float, kE>(p.delta_bias + c, p.delta_bias ? cn : 0);
 #pragma unroll
             for (int i = 0; i < kE; ++i) {
-                const float x = r_delta[i] + (p.delta_bias && i < cn ? __ldg(p.delta_bias + c + i) : 0.0f);
-                dt[i] = !row_on ? 0.0f : softplus ? softplus_f32(x) : x;
-                slope[i] = !row_on ? 0.0f : softplus ? sigmoid_f32(x) : 1.0f;
-                gate[i] = p.z ? sigmoid_f32(r_z[i]) : 1.0f;
-                const int at = row * width + scan_column(c - blk.c0 + i);
-                s_pair[at] = make_float2(dt[i], row_on ? dt[i] * r_u[i] : 0.0f);
-                s_do[at] = row_on ? (p.z ? r_dy[i] * r_z[i] * gate[i] : r_dy[i]) : 0.0f;
+                const float x = r.delta[i] + bias[i];
+                const float dt = !row_on ? 0.0f : softplus ? softplus_f32(x) : x;
+                float g = r.dy[i];
+                if (p.z) g *= r.z[i] * sigmoid_f32(r.z[i]);
+                s_pair[column(i)] = make_float2(dt, row_on ? dt * r.u[i] : 0.0f);
+                s_do[column(i)] = row_on ? g : 0.0f;
             }
 #pragma unroll
-            for (int i = 0; i < kBC; ++i) {
-                const int idx = tid + i * threads;
-                if (idx < kRows * kNP) {
-                    s_B[idx] = to_f32<T>(r_B[i]);
-                    s_C[idx] = to_f32<T>(r_C[i]);
+            for (int i = 0; i < kPieces; ++i) {
+                const int q = tid + i * threads;
+                if (q < 2 * kHalf) {
+                    float f[kNS];
+#pragma unroll
+                    for (int k = 0; k < kNS; ++k) f[k] = r_BC[i][k];
+                    store_floats<true, kNS>(s_BC + q * kNS, f, kNS);
                 }
             }
         }
-        const Piece<T, kE> u = r_u, z = r_z, dy = r_dy;
         float h[kNS];
 #pragma unroll
         for (int k = 0; k < kNS; ++k) h[k] = r_h[k];
         __syncthreads();
-        if (any) {
-            if (i0 > blk.i0) fetch(i0 - kRows);
-            float ah[kRows][kNS];
+        if (i0 > blk.i0) {
+            fetch(i0 - kRows);
+            if (kEarly) ahead = rows_of(i0 - kRows);
+        }
+        float ah[kRows][kNS];
 #pragma unroll
-            for (int t = 0; t < kRows; t += kGroup) {
-                float o[kGroup], dc[kGroup * kNS];
+        for (int t = 0; t < kRows; t += kGroup) {
+            float o[kGroup], dc[kGroup * kNS];
 #pragma unroll
-                for (int s = 0; s < kGroup; ++s) {
-                    const float2 x = s_pair[(t + s) * width + col];
-                    const float g = s_do[(t + s) * width + col];
-                    float in[kNS], out[kNS];
-                    load_floats<kNS>(in, s_B + (t + s) * kNP + n0, kNS, true);
-                    load_floats<kNS>(out, s_C + (t + s) * kNP + n0, kNS, true);
-                    o[s] = 0.0f;
+            for (int s = 0; s < kGroup; ++s) {
+                const float2 x = s_pair[(t + s) * width + col];
+                const float g = s_do[(t + s) * width + col];
+                float in[kNS], out[kNS], a[kNS], v[kNS];
+                load_floats<true, kNS>(in, s_BC + (t + s) * kNP + n0, kNS);
+                load_floats<true, kNS>(out, s_BC + (kRows + t + s) * kNP + n0, kNS);
+                scan_decays<kNS>(a, x.x, rate);
+                mul_each<kNS>(ah[t + s], a, h);
+                fma_each<kNS>(h, x.y, in, ah[t + s]);
+                o[s] = dot_each<kNS>(h, out);
+                mul_each<kNS>(v, g, h);
 #pragma unroll
-                    for (int k = 0; k < kNS; ++k) {
-                        ah[t + s][k] = exp2_approx(x.x * rate[k]) * h[k];
-                        h[k] = fmaf(x.y, in[k], ah[t + s][k]);
-                        o[s] = fmaf(h[k], out[k], o[s]);
-                        dc[s * kNS + k] = h[k] * g;
-                    }
+                for (int k = 0; k < kNS; ++k) dc[s * kNS + k] = v[k];
+            }
+            if (p.z) {
+#pragma unroll
+                for (int s = 0; s < kGroup; s += kS) {
+                    float v[kS];
+#pragma unroll
+                    for (int i = 0; i < kS; ++i) v[i] = o[s + i];
+                    lane_sums<kS, 1, kS / 2>(v, lane);
+                    s_o[(t + s + first_sum<kS, 1, kS / 2>(lane)) * width + col] = v[0];
                 }
-                if (p.z) {
+            }
 #pragma unroll
-                    for (int s = 0; s < kGroup; s += kS) {
-                        float v[kS];
+            for (int s = 0; s < kGroup; s += kSteps) {
+                float v[8];
 #pragma unroll
-                        for (int i = 0; i < kS; ++i) v[i] = o[s + i];
-                        lane_sums<kS, 1, kS / 2>(v, lane);
-                        s_o[(t + s + first_sum<kS, 1, kS / 2>(lane)) * width + col] = v[0];
-                    }
-                }
-                constexpr int kLeft = 8 * kS / 32 > 0 ? 8 * kS / 32 : 1;            // values left in a lane
+                for (int i = 0; i < 8; ++i) v[i] = dc[s * kNS + i];
+                lane_sums<8, kS, 16>(v, lane);
+                if (lane / kS < 8) {
 #pragma unroll
-                for (int s = 0; s < kGroup; s += kSteps) {
-                    float v[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = dc[s * kNS + i];
-                    lane_sums<8, kS, 16>(v, lane);
-                    if (lane / kS < 8) {
-#pragma unroll
-                        for (int i = 0; i < kLeft; ++i) {
-                            const int idx = first_sum<8, kS, 16>(lane) + i;
-                            s_sum[((warp * kRows + t + s + idx / kNS) * 2 + 1) * kNP + n0 + idx % kNS] = v[i];
-                        }
+                    for (int i = 0; i < kLeft; ++i) {
+                        const int idx = first_sum<8, kS, 16>(lane) + i;
+                        s_sum[((warp * kRows + t + s + idx / kNS) * 2 + 1) * kNP + n0 + idx % kNS] = v[i];
                     }
                 }
             }
-            constexpr int kPairs = kS >= 4 ? kS / 2 : kS == 2 ? 1 : 1;               // steps whose (s, r) are summed together
+        }
 #pragma unroll
-            for (int t = kRows - kGroup; t >= 0; t -= kGroup) {
-                float db[kGroup * kNS], sr[kGroup * 2];
+        for (int t = kRows - kGroup; t >= 0; t -= kGroup) {
+            float db[kGroup * kNS], sr[kGroup * 2];
 #pragma unroll
-                for (int s = kGroup - 1; s >= 0; --s) {
-                    const float2 x = s_pair[(t + s) * width + col];
-                    const float g = s_do[(t + s) * width + col];
-                    float in[kNS], out[kNS];
-                    load_floats<kNS>(in, s_B + (t + s) * kNP + n0, kNS, true);
-                    load_floats<kNS>(out, s_C + (t + s) * kNP + n0, kNS, true);
-                    float sum_s = 0.0f, sum_r = 0.0f;
+            for (int s = kGroup - 1; s >= 0; --s) {
+                const float2 x = s_pair[(t + s) * width + col];
+                const float g = s_do[(t + s) * width + col];
+                float in[kNS], out[kNS], a[kNS], v[kNS], G[kNS];
+                load_floats<true, kNS>(in, s_BC + (t + s) * kNP + n0, kNS);
+                load_floats<true, kNS>(out, s_BC + (kRows + t + s) * kNP + n0, kNS);
+                scan_decays<kNS>(a, x.x, rate);
+                fma_each<kNS>(G, g, out, e);
+                mul_each<kNS>(e, a, G);
+                mul_each<kNS>(v, x.y, G);
 #pragma unroll
-                    for (int k = 0; k < kNS; ++k) {
-                        const float G = fmaf(out[k], g, e[k]);
-                        db[s * kNS + k] = G * x.y;
-                        sum_s = fmaf(G, in[k], sum_s);
-                        const float q = G * ah[t + s][k];
-                        sum_r = fmaf(rate[k], q, sum_r);
-                        dA[k] = fmaf(x.x, q, dA[k]);
-                        e[k] = exp2_approx(x.x * rate[k]) * G;
-                    }
-                    sr[s * 2] = sum_s;
-                    sr[s * 2 + 1] = sum_r;
-                }
+                for (int k = 0; k < kNS; ++k) db[s * kNS + k] = v[k];
+                sr[s * 2] = dot_each<kNS>(G, in);
+                mul_each<kNS>(v, G, ah[t + s]);
+                sr[s * 2 + 1] = dot_each<kNS>(v, rate);
+                fma_each<kNS>(dA, x.x, v, dA);
+            }
 #pragma unroll
-                for (int s = 0; s < kGroup; s += kPairs) {
-                    float v[kPairs * 2];
+            for (int s = 0; s < kGroup; s += kPairs) {
+                float v[kPairs * 2];
 #pragma unroll
-                    for (int i = 0; i < kPairs * 2; ++i) v[i] = sr[s * 2 + i];
-                    lane_sums<kPairs * 2, 1, kS / 2>(v, lane);
-                    const int idx = first_sum<kPairs * 2, 1, kS / 2>(lane);
-                    float2 *at = s_pair + (t + s + idx / 2) * width + col;
-                    __syncwarp();                         // all lanes of the channel have read the step's pair
-                    if (kS == 1)
-                        *at = make_float2(v[0], v[1]);
-                    else
-                        (idx & 1 ? at->y : at->x) = v[0];
-                }
-                constexpr int kLeft = 8 * kS / 32 > 0 ? 8 * kS / 32 : 1;
+                for (int i = 0; i < kPairs * 2; ++i) v[i] = sr[s * 2 + i];
+                lane_sums<kPairs * 2, 1, kS / 2>(v, lane);
+                const int idx = first_sum<kPairs * 2, 1, kS / 2>(lane);
+                float2 *at = s_pair + (t + s + idx / 2) * width + col;
+                __syncwarp();                             // all lanes of the channel have read the step's pair
+                if (kS == 1)
+                    *at = make_float2(v[0], v[1]);
+                else
+                    (idx & 1 ? at->y : at->x) = v[0];
+            }
 #pragma unroll
-                for (int s = 0; s < kGroup; s += kSteps) {
-                    float v[8];
+            for (int s = 0; s < kGroup; s += kSteps) {
+                float v[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = db[s * kNS + i];
-                    lane_sums<8, kS, 16>(v, lane);
-                    if (lane / kS < 8) {
+                for (int i = 0; i < 8; ++i) v[i] = db[s * kNS + i];
+                lane_sums<8, kS, 16>(v, lane);
+                if (lane / kS < 8) {
 #pragma unroll
-                        for (int i = 0; i < kLeft; ++i) {
-                            const int idx = first_sum<8, kS, 16>(lane) + i;
-                            s_sum[(warp * kRows + t + s + idx / kNS) * 2 * kNP + n0 + idx % kNS] = v[i];
-                        }
+                    for (int i = 0; i < kLeft; ++i) {
+                        const int idx = first_sum<8, kS, 16>(lane) + i;
+                        s_sum[(warp * kRows + t + s + idx / kNS) * 2 * kNP + n0 + idx % kNS] = v[i];
                     }
                 }
             }
         }
         __syncthreads();
         if (i0 + row < end) {
-            const bool row_on = i0 + row < blk.i1;
+            const Rows r = rows_of(i0);                    // once more, from the cache: held in registers they would cost occupancy
+            const Piece<float, kE> bias = load_piece<kWhole, float, kE>(p.delta_bias + c, p.delta_bias ? cn : 0);
+            const Piece<float, kE> skip = load_piece<kWhole, float, kE>(p.D + c, p.D ? cn : 0);
             float du[kE], dd[kE], dz[kE];
 #pragma unroll
             for (int i = 0; i < kE; ++i) {
-                du[i] = dd[i] = dz[i] = 0.0f;
+                const float2 sr = s_pair[column(i)];
+                const float dyo = s_do[column(i)], D = skip[i], u = r.u[i], x = r.delta[i] + bias[i];
+                float dt = x, slope = 1.0f;
+                if (softplus) {
+                    const float t = exp_minus_abs(x);
+                    dt = softplus_of(x, t);
+                    slope = __fdividef(x < 0.0f ? t : 1.0f, 1.0f + t);
+                }
+                du[i] = p.D ? fmaf(dt, sr.x, D * dyo) : dt * sr.x;
+                dd[i] = fmaf(u, sr.x, sr.y * kLn2) * slope;
+                dz[i] = 0.0f;
+                if (p.z) {
+                    const float o = p.D ? fmaf(D, u, s_o[column(i)]) : s_o[column(i)], z = r.z[i], gate = sigmoid_f32(z);
+                    dz[i] = r.dy[i] * o * gate * fmaf(z, 1.0f - gate, 1.0f);
+                }
+                if (!row_on) du[i] = dd[i] = dz[i] = 0.0f;
                 if (row_on) {
-                    const int at = row * width + scan_column(c - blk.c0 + i);
-                    const float2 sr = s_pair[at];
-                    const float dyo = s_do[at], D = p.D && i < cn ? __ldg(p.D + c + i) : 0.0f;
-                    du[i] = p.D ? fmaf(dt[i], sr.x, D * dyo) : dt[i] * sr.x;
-                    dd[i] = fmaf(u[i], sr.x, sr.y * kLn2) * slope[i];
-                    if (p.z) {
-                        const float o = p.D ? fmaf(D, u[i], s_o[at]) : s_o[at];
-                        dz[i] = dy[i] * o * gate[i] * fmaf(z[i], 1.0f - gate[i], 1.0f);
-                    }
-                    sum_D[i] = fmaf(u[i], dyo, sum_D[i]);
+                    sum_D[i] = fmaf(u, dyo, sum_D[i]);
                     sum_bias[i] += dd[i];
                 }
             }
-            const long long at = (static_cast<long long>(blk.b) * p.length + token_of(i0 + row)) * p.channels + c;
-            store_piece<T, kE>(static_cast<T *>(p.du) + at, du, cn, p.whole);
-            store_piece<T, kE>(static_cast<T *>(p.ddelta) + at, dd, cn, p.whole);
-            if (p.z) store_piece<T, kE>(static_cast<T *>(p.dz) + at, dz, cn, p.whole);
+            const long long at = (sequence + token_of(i0 + row)) * p.channels + c;
+            store_piece<kWhole, T, kE>(static_cast<T *>(p.du) + at, du, cn);
+            store_piece<kWhole, T, kE>(static_cast<T *>(p.ddelta) + at, dd, cn);
+            if (p.z) store_piece<kWhole, T, kE>(static_cast<T *>(p.dz) + at, dz, cn);
         }
-        for (int idx = tid; idx < kRows * 2 * kNP; idx += threads) {
-            const int t = idx / (2 * kNP), which = idx / kNP & 1, n1 = idx % kNP;
-            if (i0 + t >= end || n1 >= p.states) continue;
+        for (int t = tid / (2 * kNP); t < kRows; t += threads / (2 * kNP)) {
+            const int i = i0 + t;
+            if (i >= end || out_n >= p.states) break;
             float v = 0.0f;
-            if (i0 + t < blk.i1)
-                for (int w = 0; w < warps; ++w) v += s_sum[w * kRows * 2 * kNP + idx];
-            const long long tok = static_cast<long long>(blk.b) * p.length + token_of(i0 + t);
-            if (p.part_BC) {
-                const int share = blockIdx.x % (p.groups * p.group_blocks);
-                p.part_BC[((static_cast<long long>(share) * p.batch * p.length + tok) * 2 + which) * p.states + n1] = v;
-            } else {
-                static_cast<T *>(which ? p.dC : p.dB)[(tok * p.groups + blk.g) * p.states + n1] = from_f32<T>(v);
+            if (i < blk.i1) {
+                const float *from = s_sum + (t * 2 + out_which) * kNP + out_n;
+#pragma unroll 8
+                for (int w = 0; w < warps; ++w) v += from[w * kRows * 2 * kNP];
             }
+            put_BC(i, v);
         }
         __syncthreads();                                   // s_sum and s_do are written anew
     }
     const long long part = static_cast<long long>(blk.b) * p.chunks + blk.chunk;
-    store_floats<kNS>(p.part_A + (part * p.channels + d) * p.states + n0, dA, nn, p.whole_n);
-    if (p.dstate && blk.chunk == 0) store_floats<kNS>(p.dstate + state_at, e, nn, p.whole_n);
+    store_floats<kWhole, kNS>(p.part_A + (part * p.channels + d) * p.states + n0, dA, nn);
+    if (p.dstate && blk.chunk == 0) store_floats<kWhole, kNS>(p.dstate + state_at, e, nn);
     // the rows' sums of a channel, in the order of the rows
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < kE; ++i) {
-        s_do[row * width + c - blk.c0 + i] = sum_D[i];
-        s_o[row * width + c - blk.c0 + i] = sum_bias[i];
+        s_do[slot_of_row + c - blk.c0 + i] = sum_D[i];
+        s_o[slot_of_row + c - blk.c0 + i] = sum_bias[i];
     }
     __syncthreads();
     for (int i = tid; i < width && blk.c0 + i < blk.c_end; i += threads) {
@@ -603,7 +702,7 @@ __global__ void __launch_bounds__(256) ptq_scan_finish_kernel(const ScanParams p
 
 // One token per sequence.  Bound: the state's bytes, read and written once.  A thread keeps its kNS rates and goes over
 // sequences; the lanes of a channel take its token's values alike.
-template <typename T, int kNS, int kS>
+template <typename T, int kNS, int kS, bool kWhole>
 __global__ void __launch_bounds__(256) ptq_scan_step_kernel(const ScanParams p)
 {
     const int per_cta = 256 / kS;
@@ -613,7 +712,7 @@ __global__ void __launch_bounds__(256) ptq_scan_step_kernel(const ScanParams p)
     const bool on = d < p.channels;
     const int g = on ? d / p.group_channels : 0;
     float rate[kNS];
-    load_floats<kNS>(rate, p.A + static_cast<long long>(d) * p.states + n0, nn, p.whole_n);
+    load_floats<kWhole, kNS>(rate, p.A + static_cast<long long>(d) * p.states + n0, nn);
 #pragma unroll
     for (int k = 0; k < kNS; ++k) rate[k] = scan_rate(rate[k]);
     const float bias = on && p.delta_bias ? p.delta_bias[d] : 0.0f, D = on && p.D ? p.D[d] : 0.0f;
@@ -624,23 +723,25 @@ __global__ void __launch_bounds__(256) ptq_scan_step_kernel(const ScanParams p)
         float h[kNS];
 #pragma unroll
         for (int k = 0; k < kNS; ++k) h[k] = 0.0f;
-        if (p.state) load_floats<kNS>(h, p.state + at, nn, p.whole_n);
+        if (p.state) load_floats<kWhole, kNS>(h, p.state + at, nn);
         float o = 0.0f, u = 0.0f;
         if (on && token) {
             u = to_f32<T>(static_cast<const T *>(p.u)[b * p.u_b + d]);
             const float x = to_f32<T>(static_cast<const T *>(p.delta)[b * p.delta_b + d]) + bias;
             const float dt = p.flags & kScanSoftplus ? softplus_f32(x) : x;
             const T *B = static_cast<const T *>(p.B) + b * p.B_b + g * p.B_g + n0, *C = static_cast<const T *>(p.C) + b * p.C_b + g * p.C_g + n0;
+            float a[kNS];
+            scan_decays<kNS>(a, dt, rate);
 #pragma unroll
             for (int k = 0; k < kNS; ++k) {
                 const float in = k < nn ? to_f32<T>(B[k]) : 0.0f, out = k < nn ? to_f32<T>(C[k]) : 0.0f;
-                h[k] = fmaf(exp2_approx(dt * rate[k]), h[k], dt * u * in);
+                h[k] = fmaf(a[k], h[k], dt * u * in);
                 o = fmaf(h[k], out, o);
             }
         }
 #pragma unroll
         for (int i = 1; i < kS; i *= 2) o += __shfl_xor_sync(0xffffffffu, o, i);
-        if (p.final_state) store_floats<kNS>(p.final_state + at, h, nn, p.whole_n);
+        if (p.final_state) store_floats<kWhole, kNS>(p.final_state + at, h, nn);
         if (on && token && n0 == 0) {
             if (p.D) o = fmaf(D, u, o);
             if (p.z) {
