@@ -64,25 +64,30 @@ ptq_status_t with_type(int dtype, Fn fn)
 }
 
 // ---------------------------------------------------------------------------------------------------- scan
-// How a call is cut: threads of a CTA, CTAs per group, chunks of the sequences.
+// How a call is cut.  Chunks: until the GPU has enough warps, but of 256 steps at least, since every further chunk has to be
+// gone over twice.  The forward pass and the backward pass cut a call alike, so that one rule sizes both workspaces.
 struct ScanPlan {
-    int threads, group_blocks, chunk_len, chunks;
-    long long ctas;                   // of one chunk
-    ScanCut cut(int n, bool whole) const { return {threads, ctas * n, whole}; }
+    ScanSplit split;                  // of the forward pass
+    int threads, group_warps, group_blocks, chunk_len, chunks;
+    long long warps, ctas;            // of one chunk
+    ScanCut cut(int n, bool whole) const { return {split, warps * n, threads, ctas * n, whole}; }
 };
 ScanPlan scan_plan(const ptq_scan_t &s)
 {
-    const int lanes = scan_split(s.states).lanes, per_group = s.channels / s.groups;
+    const int per_group = s.channels / s.groups, lanes = scan_split_backward(s.states).lanes;
+    const long long sequences = static_cast<long long>(s.batch) * s.groups;
     ScanPlan p;
-    p.threads = lanes == 1 ? 128 : 256;
-    const auto blocks = [&](int threads) { return ceil_div(per_group, threads / lanes); };
-    if (lanes < 8 && static_cast<long long>(s.batch) * s.groups * blocks(p.threads) < kSms && s.length < 512) p.threads = 128;
-    p.group_blocks = static_cast<int>(blocks(p.threads));
-    const long long ctas = static_cast<long long>(s.batch) * s.groups * p.group_blocks;
-    long long chunks = ctas >= 2 * kSms ? 1 : std::min(ceil_div(4 * kSms, ctas), ceil_div(s.length, 256));
+    p.split = scan_split_forward(s.states, false);
+    const auto warps = [&] { return sequences * ceil_div(per_group, p.split.width()); };
+    const long long chunks = std::max(1ll, std::min(ceil_div(16 * kSms, warps()), ceil_div(s.length, 256)));
+    if (warps() * chunks < 8 * kSms) p.split = scan_split_forward(s.states, true);
     p.chunk_len = static_cast<int>(ceil_div(ceil_div(s.length, chunks), 64) * 64);
     p.chunks = static_cast<int>(ceil_div(s.length, p.chunk_len));
-    p.ctas = ctas;
+    p.group_warps = static_cast<int>(ceil_div(per_group, p.split.width()));
+    p.warps = warps();
+    p.threads = lanes == 1 || (lanes < 8 && sequences * ceil_div(per_group, 256 / lanes) * p.chunks < kSms) ? 128 : 256;
+    p.group_blocks = static_cast<int>(ceil_div(per_group, p.threads / lanes));
+    p.ctas = sequences * p.group_blocks;
     return p;
 }
 
@@ -102,7 +107,7 @@ ptq_status_t scan_check(const ptq_scan_t *s)
         return fail(PTQ_ERR_SHAPE, "a pitch is negative");
     if (!aligned({s->u, s->delta, s->z, s->B, s->C}, elem_bytes(s->dtype)) || !aligned({s->A, s->D, s->delta_bias, s->state, s->lengths}, 4))
         return fail(PTQ_ERR_ALIGN, "an input is not aligned to its type");
-    if (const ScanPlan plan = scan_plan(*s); plan.ctas * plan.chunks > kMaxGrid) return fail(PTQ_ERR_SHAPE, "the batch is too large for one launch");
+    if (const ScanPlan plan = scan_plan(*s); std::max(plan.warps, plan.ctas) * plan.chunks > kMaxGrid) return fail(PTQ_ERR_SHAPE, "the batch is too large for one launch");
     return PTQ_OK;
 }
 
@@ -137,10 +142,12 @@ ptq::ScanParams scan_params(const ptq_scan_t &s, const ScanPlan &plan)
     p.states = s.states;
     p.groups = s.groups;
     p.group_channels = s.channels / s.groups;
+    p.group_warps = plan.group_warps;
     p.group_blocks = plan.group_blocks;
     p.chunk_len = plan.chunk_len;
     p.chunks = plan.chunks;
     p.flags = s.flags;
+    p.pairs = s.states % 2 == 0 && aligned({s.B, s.C}, 2 * elem_bytes(s.dtype)) && multiples({p.B_b, p.B_l, p.B_g, p.C_b, p.C_l, p.C_g}, 2);
     return p;
 }
 
@@ -151,7 +158,7 @@ bool scan_whole(const ptq_scan_t &s)
     return aligned({s.u, s.delta, s.z, s.A, s.D, s.delta_bias, s.state}, 16) &&
            multiples({s.u_pitch[0], s.u_pitch[1], s.delta_pitch[0], s.delta_pitch[1], s.z ? s.z_pitch[0] : 0, s.z ? s.z_pitch[1] : 0,
                       s.channels / s.groups}, unit) &&
-           (scan_split(s.states).states < 4 || s.states % 4 == 0);
+           (s.states <= 2 || s.states % 4 == 0);
 }
 
 // Workspace: slots and sums of the chunks, and for the backward pass the shares of the CTAs.

@@ -156,17 +156,20 @@ __device__ __forceinline__ void store_piece(T *p, const float (&f)[kE], int n)
     store_piece<kWhole, T, kE>(p, r, n);
 }
 
-// kN consecutive floats, of which n exist; kWhole: the address allows accesses of 16 bytes, and n is 0 or kN where kN is 4.
+// kN consecutive floats, of which n exist; kWhole: the address allows accesses of 16 bytes, and n is a multiple of four where kN is.
 template <bool kWhole, int kN>
 __device__ __forceinline__ void load_floats(float (&f)[kN], const float *p, int n)
 {
-    if constexpr (kN == 4 && kWhole) {
-        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (n >= 4) v = *reinterpret_cast<const float4 *>(p);
-        f[0] = v.x;
-        f[1] = v.y;
-        f[2] = v.z;
-        f[3] = v.w;
+    if constexpr (kN % 4 == 0 && kWhole) {
+#pragma unroll
+        for (int k = 0; k < kN; k += 4) {
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (n >= k + 4) v = *reinterpret_cast<const float4 *>(p + k);
+            f[k] = v.x;
+            f[k + 1] = v.y;
+            f[k + 2] = v.z;
+            f[k + 3] = v.w;
+        }
     } else {
 #pragma unroll
         for (int k = 0; k < kN; ++k) {
@@ -178,8 +181,10 @@ __device__ __forceinline__ void load_floats(float (&f)[kN], const float *p, int 
 template <bool kWhole, int kN>
 __device__ __forceinline__ void store_floats(float *p, const float (&f)[kN], int n)
 {
-    if constexpr (kN == 4 && kWhole) {
-        if (n >= 4) *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    if constexpr (kN % 4 == 0 && kWhole) {
+#pragma unroll
+        for (int k = 0; k < kN; k += 4)
+            if (n >= k + 4) *reinterpret_cast<float4 *>(p + k) = make_float4(f[k], f[k + 1], f[k + 2], f[k + 3]);
     } else {
 #pragma unroll
         for (int k = 0; k < kN; ++k)

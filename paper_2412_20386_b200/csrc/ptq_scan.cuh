@@ -19,7 +19,8 @@
 namespace ptq {
 
 constexpr int kScanHistory = 16;      // steps between two states that are kept for the backward pass
-constexpr int kScanThreads = 256, kScanLeast = 128;       // of a CTA: most, and fewest where a channel has fewer than eight lanes
+constexpr int kScanWarps = 4;         // of a CTA of the forward pass; they work alone
+constexpr int kScanThreads = 256, kScanLeast = 128;       // of a CTA of the backward pass: most, and fewest where a channel has fewer than eight lanes
 
 constexpr unsigned kScanSoftplus = 1u, kScanReverse = 2u;
 
@@ -30,9 +31,10 @@ struct ScanParams {
     const int *lengths;                         // may be null
     int batch, length, channels, states, groups;
     int group_channels;                         // channels / groups
-    int group_blocks;                           // CTAs that share the channels of a group
+    int group_warps, group_blocks;              // warps (CTAs of the backward pass) that share the channels of a group
     int chunk_len, chunks;
     unsigned flags;
+    bool pairs;                                 // B and C allow accesses of two states
     float *slots;                               // [chunks][batch][channels][states]
     float *sums;                                // [chunks][batch][channels]: sum of dt of a chunk
     // forward
@@ -47,36 +49,41 @@ struct ScanParams {
     float *part_BC;                             // [groups * group_blocks][batch][length][2 states], null: straight to dB, dC
 };
 
-// e^-|x|, the argument of the power of two to about 2^-46: its rounding alone would cost four units in the last place at |x| = 7.
-// |x| is cut at 126, where the result is zero.
-__device__ __forceinline__ float exp_minus_abs(float x)
+// The same of two values: t = e^-|x| and log(1 + e^x) = max(x, 0) + log(1 + t).  The argument of the power of two is carried to about 2^-46
+// (its rounding alone would cost four units in the last place at |x| = 7); |x| is cut at 126, where t is zero.  log(1 + t) / t is a
+// polynomial fitted to 5e-9 on [0, 1]: accurate relative to the result, small ones too, with half the instructions of expf and log1pf.
+__device__ __forceinline__ void exp_minus_abs_pair(float &t0, float &t1, float x0, float x1)
 {
-    const float m = -fminf(fabsf(x), 126.0f), y = m * kLog2e;
-    const float rest = fmaf(m, 1.925963033e-8f, fmaf(m, kLog2e, -y));
-    const float t = exp2_approx(y);
-    return fmaf(t, rest * kLn2, t);
+    const float m0 = -fminf(fabsf(x0), 126.0f), m1 = -fminf(fabsf(x1), 126.0f);
+    float y0, y1, r0, r1;
+    mul_pair(y0, y1, m0, m1, kLog2e, kLog2e);
+    fma_pair(r0, r1, m0, m1, kLog2e, kLog2e, -y0, -y1);
+    fma_pair(r0, r1, m0, m1, 1.925963033e-8f, 1.925963033e-8f, r0, r1);
+    y0 = exp2_approx(y0);
+    y1 = exp2_approx(y1);
+    mul_pair(r0, r1, r0, r1, kLn2, kLn2);
+    fma_pair(t0, t1, y0, y1, r0, r1, y0, y1);
 }
-// log(1 + e^x) = max(x, 0) + log(1 + t), t = e^-|x|; log(1 + t) / t is a polynomial fitted to 5e-9 on [0, 1]: accurate relative to the
-// result, small ones too, with about 20 instructions (expf and log1pf take twice as many).
-__device__ __forceinline__ float softplus_of(float x, float t)
+__device__ __forceinline__ void softplus_pair(float &s0, float &s1, float x0, float x1, float t0, float t1)
 {
-    float p = -0.0032440212f;
-    p = fmaf(p, t, 0.01985144429f);
-    p = fmaf(p, t, -0.05695949867f);
-    p = fmaf(p, t, 0.106036514f);
-    p = fmaf(p, t, -0.1530559063f);
-    p = fmaf(p, t, 0.1967593879f);
-    p = fmaf(p, t, -0.2495413423f);
-    p = fmaf(p, t, 0.3332996368f);
-    p = fmaf(p, t, -0.4999990165f);
-    p = fmaf(p, t, 1.0f);
-    return fmaf(p, t, x <= 0.0f ? 0.0f : x);              // NaN passes through
+    constexpr float kCoeff[] = {0.01985144429f, -0.05695949867f, 0.106036514f, -0.1530559063f, 0.1967593879f,
+                                -0.2495413423f, 0.3332996368f,   -0.4999990165f, 1.0f};
+    float p0 = -0.0032440212f, p1 = p0;
+#pragma unroll
+    for (float k : kCoeff) fma_pair(p0, p1, p0, p1, t0, t1, k, k);
+    fma_pair(s0, s1, p0, p1, t0, t1, x0 <= 0.0f ? 0.0f : x0, x1 <= 0.0f ? 0.0f : x1);      // NaN passes through
 }
-__device__ __forceinline__ float softplus_f32(float x) { return softplus_of(x, exp_minus_abs(x)); }
+__device__ __forceinline__ float softplus_f32(float x)
+{
+    float t, s, unused;
+    exp_minus_abs_pair(t, unused, x, 0.0f);
+    softplus_pair(s, unused, x, 0.0f, t, 1.0f);
+    return s;
+}
 
-// exp(dt A) as 2^(dt rate).  The hardware's power of two is low by 0.1 to 0.35 units of 2^-24 on average for the arguments of slow decays
-// (-0.1 .. 0), where a state multiplies hundreds of them: the argument is raised by a quarter of a unit, which the fused multiply-add
-// does at no cost and which rounds away where the memory is short.  2^kDecayShift is 1: a step with dt = 0 keeps the state.
+// exp(dt A) as 2^(dt rate).  The hardware's power of two is low by 0.1 to 0.35 units of 2^-24 on average for the arguments of slow
+// decays (-0.1 .. 0), where a state multiplies hundreds of them: the argument is raised by a quarter of a unit, which the fused
+// multiply-add does at no cost and which rounds away where the memory is short.  2^kDecayShift is 1: a step with dt = 0 keeps the state.
 constexpr float kDecayShift = 2.15e-8f;
 template <int kNS>
 __device__ __forceinline__ void scan_decays(float (&a)[kNS], float dt, const float (&rate)[kNS])
@@ -98,14 +105,15 @@ __device__ __forceinline__ int scan_column(int ch) { return (ch & ~7) | (((((ch 
 
 struct ScanBlock {
     int b, chunk, g, c0, c_end, len, i0, i1;
-    __device__ __forceinline__ ScanBlock(const ScanParams &p, int block, int chunks, int first_chunk, int width)
+    // block: which of the shares of `width` channels (group_blocks to a group) of which chunk of which sequence
+    __device__ __forceinline__ ScanBlock(const ScanParams &p, int block, int group_blocks, int chunks, int first_chunk, int width)
     {
-        const int per = p.groups * p.group_blocks;
+        const int per = p.groups * group_blocks;
         const int rest = block / per, blk = block - rest * per;
         b = rest / chunks;
         chunk = first_chunk + rest - b * chunks;
-        g = blk / p.group_blocks;
-        c0 = g * p.group_channels + (blk - g * p.group_blocks) * width;
+        g = blk / group_blocks;
+        c0 = g * p.group_channels + (blk - g * group_blocks) * width;
         c_end = min(c0 + width, (g + 1) * p.group_channels);
         len = p.lengths ? min(max(p.lengths[b], 0), p.length) : p.length;
         i0 = chunk * p.chunk_len;
@@ -135,31 +143,34 @@ __device__ __forceinline__ void scan_fold(float (&h)[kNS], const float (&rate)[k
 // state, from the last step to the first: e <- exp(dt A) (C dy silu(z) + e), for each chunk but the first one.
 enum { kScanForward = 0, kScanSum = 1, kScanGradSum = 2 };
 
-template <typename T, int kNS, int kS, int kMode, bool kWhole>
-__global__ void __launch_bounds__(kScanThreads, 3) ptq_scan_kernel(const ScanParams p)
+template <typename T, int kC, int kNS, int kS, int kMode, bool kWhole>
+__global__ void __launch_bounds__(kScanWarps * 32, 4) ptq_scan_kernel(const ScanParams p)
 {
-    constexpr int kRows = 8 * kS, kNP = kNS * kS;         // steps of a tile, states padded
-    constexpr int kGroup = kS < 4 ? 4 : kS;               // steps between two joint sums over the lanes of a channel
+    constexpr int kWidth = 32 / kS * kC, kPitch = kWidth + 2;      // channels of the warp; the pad keeps the rows' lanes off each other's banks
+    constexpr int kRows = 256 / kWidth, kNP = kNS * kS;            // steps of a tile, states padded
+    constexpr int kGroup = kS < 4 ? 4 : kS;               // steps of an unrolled group
     constexpr bool kBackward = kMode == kScanGradSum;
-    constexpr int kHalf = kRows * kS;                     // pieces of B (or of C) in a tile
-    constexpr int kLeast = kS == 8 ? kScanThreads : kScanLeast;
-    constexpr int kPieces = ((kMode == kScanForward ? 2 : 1) * kHalf + kLeast - 1) / kLeast;      // of a thread, at most
-    extern __shared__ __align__(16) unsigned char scan_smem[];
-    const int threads = blockDim.x, tid = threadIdx.x, lane = tid & 31;
-    const int width = threads / kS;                       // channels of the CTA
-    float2 *s_pair = reinterpret_cast<float2 *>(scan_smem);                       // [kRows][width]: (dt, dt u), later (o, -)
-    float *s_B = reinterpret_cast<float *>(s_pair + kRows * width);               // [kRows][kNP], then C likewise
-    const ScanBlock blk(p, blockIdx.x, kMode == kScanForward ? p.chunks : p.chunks - 1, kBackward ? 1 : 0, width);
+    constexpr int kKinds = kMode == kScanForward ? 2 : 1; // B and C, or one of them
+    constexpr int kPer = kNP >= 2 ? 2 : 1;                // their values in an access
+    constexpr int kBC = (kRows * kNP + 32 * kPer - 1) / (32 * kPer);       // accesses of a lane to each
+    __shared__ __align__(16) float2 s_pairs[kScanWarps][kRows * kPitch];                   // (dt, dt u), later (o, -)
+    __shared__ __align__(16) float s_states[kScanWarps][kKinds * kRows * kNP];           // [B, C][step][state]
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long unit = blockIdx.x * static_cast<long long>(kScanWarps) + warp;
+    const int chunks = kMode == kScanForward ? p.chunks : p.chunks - 1;
+    if (unit >= static_cast<long long>(p.batch) * p.groups * p.group_warps * chunks) return;
+    const ScanBlock blk(p, static_cast<int>(unit), p.group_warps, chunks, kBackward ? 1 : 0, kWidth);
+    float2 *const s_pair = s_pairs[warp];
+    float *const s_BC = s_states[warp];
     const bool softplus = p.flags & kScanSoftplus, reverse = p.flags & kScanReverse;
     const int n_steps = max(blk.i1 - blk.i0, 0);
     // step k of the chunk's loop is step i of the sequence, token first + k * way
-    const bool down = reverse != kBackward;
     const int first_step = kBackward ? blk.i1 - 1 : blk.i0;
     const long long first = reverse ? blk.len - 1 - first_step : first_step;
-    const int way = down ? -1 : 1;
+    const int way = reverse != kBackward ? -1 : 1;
 
-    // the thread's part of a row
-    const int row = tid / (width / 8), c = blk.c0 + (tid % (width / 8)) * 8;
+    // the lane's part of a row
+    const int row = lane / (kWidth / 8), c = blk.c0 + lane % (kWidth / 8) * 8;
     const int cn = max(min(8, blk.c_end - c), 0);
     const long long tok = first + way * row;
     const T *at_u = kBackward ? static_cast<const T *>(p.dy) + (static_cast<long long>(blk.b) * p.length + tok) * p.channels + c
@@ -170,7 +181,22 @@ __global__ void __launch_bounds__(kScanThreads, 3) ptq_scan_kernel(const ScanPar
                     next_z = way * kRows * p.z_l;
     const bool gated = kMode != kScanSum && p.z;
     Piece<T, 8> r_u, r_delta, r_z;
-    Piece<T, kNS> r_BC[kPieces];
+    Piece<T, kPer> r_BC[kKinds][kBC];
+    // the lane's first value of B and C in the tile: step t0, state n1; the others are kApart steps apart
+    constexpr int kApart = kBC > 1 ? 32 * kPer / kNP : kRows;
+    static_assert(kApart * kBC == kRows, "a fetch goes one tile on");
+    const int t0 = kPer * lane / kNP, n1 = kPer * lane % kNP;
+    const bool has = kPer * lane < kRows * kNP;
+    const T *at_BC[kKinds];
+    long long apart[kKinds];
+#pragma unroll
+    for (int j = 0; j < kKinds; ++j) {
+        const bool is_C = kMode == kScanForward ? j == 1 : kBackward;
+        const long long pitch = is_C ? p.C_l : p.B_l;
+        at_BC[j] = is_C ? static_cast<const T *>(p.C) + blk.b * p.C_b + blk.g * p.C_g : static_cast<const T *>(p.B) + blk.b * p.B_b + blk.g * p.B_g;
+        at_BC[j] += (first + way * t0) * pitch + n1;
+        apart[j] = way * kApart * pitch;
+    }
     const auto fetch = [&](int k0) {
         const int n = k0 + row < n_steps ? cn : 0;
         r_u = load_piece<kWhole, T, 8>(at_u, n);
@@ -180,142 +206,158 @@ __global__ void __launch_bounds__(kScanThreads, 3) ptq_scan_kernel(const ScanPar
         at_delta += next_delta;
         at_z += next_z;
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int q = tid + i * threads, t = (q % kHalf) / kS, n0 = q % kS * kNS;
-            const bool is_C = kMode == kScanForward ? q >= kHalf : kBackward;
-            const bool on = q < (kMode == kScanForward ? 2 : 1) * kHalf && k0 + t < n_steps;
-            const long long token = first + way * (k0 + t);
-            const T *from = is_C ? static_cast<const T *>(p.C) + blk.b * p.C_b + token * p.C_l + blk.g * p.C_g + n0
-                                 : static_cast<const T *>(p.B) + blk.b * p.B_b + token * p.B_l + blk.g * p.B_g + n0;
-            r_BC[i] = load_piece<false, T, kNS>(from, on ? p.states - n0 : 0);
+        for (int j = 0; j < kKinds; ++j) {
+#pragma unroll
+            for (int i = 0; i < kBC; ++i) {
+                const int states = has && k0 + t0 + i * kApart < n_steps ? p.states - n1 : 0;
+                r_BC[j][i] = p.pairs ? load_piece<true, T, kPer>(at_BC[j], states) : load_piece<false, T, kPer>(at_BC[j], states);
+                at_BC[j] += apart[j];
+            }
         }
     };
     if (n_steps > 0) fetch(0);
     const Piece<float, 8> bias = load_piece<kWhole, float, 8>(p.delta_bias + c, p.delta_bias ? cn : 0);
 
-    // the lane's channel and states
-    const int ch = tid / kS, n0 = (tid % kS) * kNS, d = blk.c0 + ch, col = scan_column(ch);
-    const int nn = d < blk.c_end ? max(min(kNS, p.states - n0), 0) : 0;
-    float rate[kNS], h[kNS];
-    load_floats<kWhole, kNS>(rate, p.A + static_cast<long long>(d) * p.states + n0, nn);
-#pragma unroll
-    for (int k = 0; k < kNS; ++k) {
-        rate[k] = scan_rate(rate[k]);
-        h[k] = 0.0f;
-    }
+    // the lane's channels and states
+    const int ch = lane / kS * kC, n0 = (lane % kS) * kNS, d = blk.c0 + ch;
+    int nn[kC];
+    float rate[kC][kNS], h[kC][kNS];
     const long long state_at = (static_cast<long long>(blk.b) * p.channels + d) * p.states + n0;
     const long long slot_step = static_cast<long long>(p.batch) * p.channels * p.states;
-    if constexpr (kMode == kScanForward) {
-        if (blk.chunk > 0) {
-            if (nn > 0) scan_fold<kWhole, kNS>(h, rate, p, blk.b, d, n0, nn, 1, blk.chunk + 1, 1);
-        } else if (p.state) {
-            load_floats<kWhole, kNS>(h, (p.chunks > 1 ? p.slots : p.state) + state_at, nn);
+    float sum_dt[kC];
+#pragma unroll
+    for (int j = 0; j < kC; ++j) {
+        nn[j] = d + j < blk.c_end ? max(min(kNS, p.states - n0), 0) : 0;
+        load_floats<kWhole, kNS>(rate[j], p.A + static_cast<long long>(d + j) * p.states + n0, nn[j]);
+#pragma unroll
+        for (int n = 0; n < kNS; ++n) {
+            rate[j][n] = scan_rate(rate[j][n]);
+            h[j][n] = 0.0f;
         }
-    } else if constexpr (kMode == kScanSum) {
-        // chunk 0 starts from the true state; the second launch takes it from a copy, since the final state may replace it
-        if (blk.chunk == 0 && p.state) {
-            load_floats<kWhole, kNS>(h, p.state + state_at, nn);
-            store_floats<kWhole, kNS>(p.slots + state_at, h, nn);
+        sum_dt[j] = 0.0f;
+        const long long at = state_at + j * p.states;
+        if constexpr (kMode == kScanForward) {
+            if (blk.chunk > 0) {
+                if (nn[j] > 0) scan_fold<kWhole, kNS>(h[j], rate[j], p, blk.b, d + j, n0, nn[j], 1, blk.chunk + 1, 1);
+            } else if (p.state) {
+                load_floats<kWhole, kNS>(h[j], (p.chunks > 1 ? p.slots : p.state) + at, nn[j]);
+            }
+        } else if constexpr (kMode == kScanSum) {
+            // chunk 0 starts from the true state; the second launch takes it from a copy, since the final state may replace it
+            if (blk.chunk == 0 && p.state) {
+                load_floats<kWhole, kNS>(h[j], p.state + at, nn[j]);
+                store_floats<kWhole, kNS>(p.slots + at, h[j], nn[j]);
+            }
+        } else if (blk.chunk == p.chunks - 1 && p.dfinal) {
+            load_floats<kWhole, kNS>(h[j], p.dfinal + at, nn[j]);
         }
-    } else if (blk.chunk == p.chunks - 1 && p.dfinal) {
-        load_floats<kWhole, kNS>(h, p.dfinal + state_at, nn);
     }
-    float sum_dt = 0.0f;
     T *at_y = static_cast<T *>(p.y) + (static_cast<long long>(blk.b) * p.length + tok) * p.channels + c;
     float *at_kept = nullptr;
     if (kMode == kScanForward && p.history)
         at_kept = p.history +
                   ((blk.b * static_cast<long long>((p.length + kScanHistory - 1) / kScanHistory) + blk.i0 / kScanHistory) * p.channels + d) * p.states + n0;
 
-    float2 *const own = s_pair + row * width;             // the row that the thread fills and finishes
+    float4 *const own = reinterpret_cast<float4 *>(s_pair + row * kPitch + lane % (kWidth / 8) * 8);      // what the lane fills and finishes
     for (int k0 = 0; k0 < n_steps; k0 += kRows) {
         const bool row_on = k0 + row < n_steps;
         const Piece<T, 8> u = r_u, z = r_z;
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-            float4 pair;
-#pragma unroll
-            for (int o = 0; o < 2; ++o) {
-                const float x = r_delta[e + o] + bias[e + o];
-                const float dt = !row_on ? 0.0f : softplus ? softplus_f32(x) : x;
-                float in = r_u[e + o];
-                if constexpr (kBackward) {
-                    if (gated) in *= r_z[e + o] * sigmoid_f32(r_z[e + o]);
-                } else {
-                    in *= dt;
+            float4 f;
+            f.x = r_delta[e] + bias[e];
+            f.z = r_delta[e + 1] + bias[e + 1];
+            if (softplus) {
+                float t0, t1;
+                exp_minus_abs_pair(t0, t1, f.x, f.z);
+                softplus_pair(f.x, f.z, f.x, f.z, t0, t1);
+            }
+            f.y = r_u[e];
+            f.w = r_u[e + 1];
+            if constexpr (kBackward) {
+                if (gated) {
+                    f.y *= r_z[e] * sigmoid_f32(r_z[e]);
+                    f.w *= r_z[e + 1] * sigmoid_f32(r_z[e + 1]);
                 }
-                (o ? pair.z : pair.x) = dt;
-                (o ? pair.w : pair.y) = row_on ? in : 0.0f;
+            } else {
+                mul_pair(f.y, f.w, f.y, f.w, f.x, f.z);
             }
-            *reinterpret_cast<float4 *>(own + scan_column(c - blk.c0 + e)) = pair;
+            if (!row_on) f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            own[e / 2] = f;
         }
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int q = tid + i * threads;
-            if (q < (kMode == kScanForward ? 2 : 1) * kHalf) {
-                float f[kNS];
+        for (int j = 0; j < kKinds; ++j) {
 #pragma unroll
-                for (int k = 0; k < kNS; ++k) f[k] = r_BC[i][k];
-                store_floats<true, kNS>(s_B + q * kNS, f, kNS);
+            for (int i = 0; i < kBC; ++i) {
+                float *at = s_BC + j * kRows * kNP + kPer * (lane + 32 * i);
+                if (!has) continue;
+                if constexpr (kPer == 2)
+                    *reinterpret_cast<float2 *>(at) = make_float2(r_BC[j][i][0], r_BC[j][i][1]);
+                else
+                    *at = r_BC[j][i][0];
             }
         }
-        __syncthreads();
+        __syncwarp();
         if (k0 + kRows < n_steps) fetch(k0 + kRows);
         const int rows = min(kRows, n_steps - k0);
         for (int t = 0; t < rows; t += kGroup) {          // rows without a token have dt = 0: the state stays as it is
             if (kMode == kScanForward && at_kept && ((k0 + t) & (kScanHistory - 1)) == 0) {
-                store_floats<kWhole, kNS>(at_kept, h, nn);
+#pragma unroll
+                for (int j = 0; j < kC; ++j) store_floats<kWhole, kNS>(at_kept + j * p.states, h[j], nn[j]);
                 at_kept += static_cast<long long>(p.channels) * p.states;
             }
-            float o[kGroup];
+            float o[kGroup * kC];
 #pragma unroll
             for (int s = 0; s < kGroup; ++s) {
-                const float2 x = s_pair[(t + s) * width + col];
-                float in[kNS], a[kNS];
-                load_floats<true, kNS>(in, s_B + (t + s) * kNP + n0, kNS);
-                scan_decays<kNS>(a, x.x, rate);
-                if constexpr (kBackward) {
-                    fma_each<kNS>(h, x.y, in, h);
-                    mul_each<kNS>(h, a, h);
-                } else {
-                    mul_each<kNS>(in, x.y, in);
-                    fma_each<kNS>(h, a, h, in);
-                }
-                if constexpr (kMode == kScanForward) {
-                    float out[kNS];
-                    load_floats<true, kNS>(out, s_B + kHalf * kNS + (t + s) * kNP + n0, kNS);
-                    o[s] = dot_each<kNS>(h, out);
-                } else {
-                    sum_dt += x.x;
+                float x[2 * kC], in[kNS], out[kNS];
+                load_floats<true, 2 * kC>(x, reinterpret_cast<const float *>(s_pair + (t + s) * kPitch + ch), 2 * kC);
+                load_floats<true, kNS>(in, s_BC + (t + s) * kNP + n0, kNS);
+                if (kMode == kScanForward) load_floats<true, kNS>(out, s_BC + kRows * kNP + (t + s) * kNP + n0, kNS);
+#pragma unroll
+                for (int j = 0; j < kC; ++j) {
+                    float a[kNS], v[kNS];
+                    scan_decays<kNS>(a, x[2 * j], rate[j]);
+                    if constexpr (kBackward) {
+                        fma_each<kNS>(v, x[2 * j + 1], in, h[j]);
+                        mul_each<kNS>(h[j], a, v);
+                    } else {
+                        mul_each<kNS>(v, x[2 * j + 1], in);
+                        fma_each<kNS>(h[j], a, h[j], v);
+                    }
+                    if constexpr (kMode == kScanForward)
+                        o[s * kC + j] = dot_each<kNS>(h[j], out);
+                    else
+                        sum_dt[j] += x[2 * j];
                 }
             }
             if constexpr (kMode == kScanForward) {
-                // every lane of the channel ends up with the sum of one of kS steps
+                // every lane of the channels ends up with the sum of one of kS values
 #pragma unroll
-                for (int s = 0; s < kGroup; s += kS) {
+                for (int s = 0; s < kGroup * kC; s += kS) {
                     float v[kS];
 #pragma unroll
                     for (int i = 0; i < kS; ++i) v[i] = o[s + i];
                     lane_sums<kS, 1, kS / 2>(v, lane);
-                    __syncwarp();                         // all lanes of the channel have read the steps' pairs
-                    s_pair[(t + s + first_sum<kS, 1, kS / 2>(lane)) * width + col].x = v[0];
+                    const int i = s + first_sum<kS, 1, kS / 2>(lane);
+                    __syncwarp();                         // all lanes of the channels have read the steps' pairs
+                    s_pair[(t + i / kC) * kPitch + ch + i % kC].x = v[0];
                 }
             }
         }
-        __syncthreads();
+        __syncwarp();
         if constexpr (kMode == kScanForward) {
             if (row_on) {
                 float y[8];
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
-                    const float4 pair = *reinterpret_cast<const float4 *>(own + scan_column(c - blk.c0 + e));
-                    y[e] = pair.x;
-                    y[e + 1] = pair.z;
+                    const float4 f = own[e / 2];
+                    y[e] = f.x;
+                    y[e + 1] = f.z;
                 }
                 if (p.D) {
                     const Piece<float, 8> skip = load_piece<kWhole, float, 8>(p.D + c, cn);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = fmaf(skip[e], u[e], y[e]);
+                    for (int e = 0; e < 8; e += 2) fma_pair(y[e], y[e + 1], skip[e], skip[e + 1], u[e], u[e + 1], y[e], y[e + 1]);
                 }
                 if (gated) {
 #pragma unroll
@@ -326,13 +368,17 @@ __global__ void __launch_bounds__(kScanThreads, 3) ptq_scan_kernel(const ScanPar
             at_y += static_cast<long long>(way * kRows) * p.channels;
         }
     }
-    if constexpr (kMode == kScanForward) {
-        if (p.final_state && blk.chunk == p.chunks - 1) store_floats<kWhole, kNS>(p.final_state + state_at, h, nn);
-    } else {
-        // forward: slot j + 1 is the state behind chunk j; backward: slot j the gradient in front of chunk j
-        store_floats<kWhole, kNS>(p.slots + (blk.chunk + (kBackward ? 0 : 1)) * slot_step + state_at, h, nn);
-        if (n0 == 0 && nn > 0)
-            p.sums[(static_cast<long long>(blk.chunk + (kBackward ? 0 : 1)) * p.batch + blk.b) * p.channels + d] = sum_dt;
+#pragma unroll
+    for (int j = 0; j < kC; ++j) {
+        const long long at = state_at + j * p.states;
+        if constexpr (kMode == kScanForward) {
+            if (p.final_state && blk.chunk == p.chunks - 1) store_floats<kWhole, kNS>(p.final_state + at, h[j], nn[j]);
+        } else {
+            // forward: slot j + 1 is the state behind chunk j; backward: slot j the gradient in front of chunk j
+            const long long slot = blk.chunk + (kBackward ? 0 : 1);
+            store_floats<kWhole, kNS>(p.slots + slot * slot_step + at, h[j], nn[j]);
+            if (n0 == 0 && nn[j] > 0) p.sums[(slot * p.batch + blk.b) * p.channels + d + j] = sum_dt[j];
+        }
     }
 }
 
@@ -364,7 +410,7 @@ __global__ void __launch_bounds__(kScanThreads, 2) ptq_scan_backward_kernel(cons
     float *s_o = s_do + kRows * width;                                            // [kRows][width]: o without D u
     float *s_BC = s_o + kRows * width;                                            // [2][kRows][kNP]
     float *s_sum = s_BC + 2 * kRows * kNP;                                        // [warps][kRows][2][kNP]: dB, dC
-    const ScanBlock blk(p, blockIdx.x, p.chunks, 0, width);
+    const ScanBlock blk(p, blockIdx.x, p.group_blocks, p.chunks, 0, width);
     const bool softplus = p.flags & kScanSoftplus, reverse = p.flags & kScanReverse;
 
     const int ch = tid / kS, n0 = (tid % kS) * kNS, d = blk.c0 + ch, col = scan_column(ch);
@@ -459,10 +505,20 @@ __global__ void __launch_bounds__(kScanThreads, 2) ptq_scan_backward_kernel(cons
         {
             const Rows r = kEarly ? ahead : rows_of(i0);
             const Piece<float, kE> bias = load_piece<kWhole, float, kE>(p.delta_bias + c, p.delta_bias ? cn : 0);
+            float dts[kE];
+#pragma unroll
+            for (int i = 0; i < kE; i += 2) {
+                dts[i] = r.delta[i] + bias[i];
+                dts[i + 1] = r.delta[i + 1] + bias[i + 1];
+                if (softplus) {
+                    float t0, t1;
+                    exp_minus_abs_pair(t0, t1, dts[i], dts[i + 1]);
+                    softplus_pair(dts[i], dts[i + 1], dts[i], dts[i + 1], t0, t1);
+                }
+            }
 #pragma unroll
             for (int i = 0; i < kE; ++i) {
-                const float x = r.delta[i] + bias[i];
-                const float dt = !row_on ? 0.0f : softplus ? softplus_f32(x) : x;
+                const float dt = row_on ? dts[i] : 0.0f;
                 float g = r.dy[i];
                 if (p.z) g *= r.z[i] * sigmoid_f32(r.z[i]);
                 s_pair[column(i)] = make_float2(dt, row_on ? dt * r.u[i] : 0.0f);
@@ -586,17 +642,25 @@ __global__ void __launch_bounds__(kScanThreads, 2) ptq_scan_backward_kernel(cons
             const Rows r = rows_of(i0);                    // once more, from the cache: held in registers they would cost occupancy
             const Piece<float, kE> bias = load_piece<kWhole, float, kE>(p.delta_bias + c, p.delta_bias ? cn : 0);
             const Piece<float, kE> skip = load_piece<kWhole, float, kE>(p.D + c, p.D ? cn : 0);
-            float du[kE], dd[kE], dz[kE];
+            float du[kE], dd[kE], dz[kE], dts[kE], slopes[kE];
+#pragma unroll
+            for (int i = 0; i < kE; i += 2) {
+                const float x0 = r.delta[i] + bias[i], x1 = r.delta[i + 1] + bias[i + 1];
+                dts[i] = x0;
+                dts[i + 1] = x1;
+                slopes[i] = slopes[i + 1] = 1.0f;
+                if (softplus) {
+                    float t0, t1;
+                    exp_minus_abs_pair(t0, t1, x0, x1);
+                    softplus_pair(dts[i], dts[i + 1], x0, x1, t0, t1);
+                    slopes[i] = __fdividef(x0 < 0.0f ? t0 : 1.0f, 1.0f + t0);
+                    slopes[i + 1] = __fdividef(x1 < 0.0f ? t1 : 1.0f, 1.0f + t1);
+                }
+            }
 #pragma unroll
             for (int i = 0; i < kE; ++i) {
                 const float2 sr = s_pair[column(i)];
-                const float dyo = s_do[column(i)], D = skip[i], u = r.u[i], x = r.delta[i] + bias[i];
-                float dt = x, slope = 1.0f;
-                if (softplus) {
-                    const float t = exp_minus_abs(x);
-                    dt = softplus_of(x, t);
-                    slope = __fdividef(x < 0.0f ? t : 1.0f, 1.0f + t);
-                }
+                const float dyo = s_do[column(i)], D = skip[i], u = r.u[i], dt = dts[i], slope = slopes[i];
                 du[i] = p.D ? fmaf(dt, sr.x, D * dyo) : dt * sr.x;
                 dd[i] = fmaf(u, sr.x, sr.y * kLn2) * slope;
                 dz[i] = 0.0f;

@@ -8,21 +8,47 @@
 
 namespace ptq_host {
 
-// Lanes per channel and states per lane.
+// Lanes per channel, channels of a lane and states of each.  Forward, a lane has two channels: the values of B and C that it reads from
+// shared memory serve both, and reading them for one channel each (18 cycles of the port per step and 256 decays, 72 for the four
+// schedulers, whose decays take 64) bound the kernel.  Where that leaves few warps, a channel has more lanes.
 struct ScanSplit {
-    int lanes, states;
+    int lanes, channels, states;
+    int width() const { return 32 / lanes * channels; }
 };
-inline ScanSplit scan_split(int states)
+inline ScanSplit scan_split_forward(int states, bool few)
 {
-    if (states <= 2) return {1, states};
-    if (states <= 4) return {2, 2};   // one lane of four would hold 64 products of the backward pass and 32 sums
-    return {states <= 8 ? 2 : states <= 16 ? 4 : 8, 4};
+    if (states <= 4) return {1, 1, states == 3 ? 4 : states};
+    if (states <= 8) return few ? ScanSplit{2, 1, 4} : ScanSplit{2, 2, 4};
+    if (states <= 16) return few ? ScanSplit{4, 1, 4} : ScanSplit{2, 2, 8};
+    return {4, 2, 8};
+}
+inline ScanSplit scan_split_backward(int states)
+{
+    if (states <= 2) return {1, 1, states};
+    if (states <= 4) return {2, 1, 2};
+    return {states <= 8 ? 2 : states <= 16 ? 4 : 8, 1, 4};
+}
+template <int kC, int kNS, int kS>
+struct ScanForm {
+    static constexpr int channels = kC, states = kNS, lanes = kS;
+};
+template <class Fn>
+ptq_status_t with_forward_split(ScanSplit sp, Fn fn)
+{
+    if (sp.lanes == 1 && sp.states == 1) return fn(ScanForm<1, 1, 1>());
+    if (sp.lanes == 1 && sp.states == 2) return fn(ScanForm<1, 2, 1>());
+    if (sp.lanes == 1) return fn(ScanForm<1, 4, 1>());
+    if (sp.lanes == 2 && sp.channels == 1) return fn(ScanForm<1, 4, 2>());
+    if (sp.lanes == 2 && sp.states == 4) return fn(ScanForm<2, 4, 2>());
+    if (sp.lanes == 2) return fn(ScanForm<2, 8, 2>());
+    if (sp.channels == 1) return fn(ScanForm<1, 4, 4>());
+    return fn(ScanForm<2, 8, 4>());
 }
 template <class Fn>
 ptq_status_t with_split(int states, Fn fn)
 {
     using std::integral_constant;
-    const ScanSplit sp = scan_split(states);
+    const ScanSplit sp = scan_split_backward(states);
     if (sp.lanes == 1 && sp.states == 1) return fn(integral_constant<int, 1>(), integral_constant<int, 1>());
     if (sp.lanes == 1) return fn(integral_constant<int, 2>(), integral_constant<int, 1>());
     if (sp.states == 2) return fn(integral_constant<int, 2>(), integral_constant<int, 2>());
@@ -31,8 +57,11 @@ ptq_status_t with_split(int states, Fn fn)
     return fn(integral_constant<int, 4>(), integral_constant<int, 8>());
 }
 
-// How a call is cut: threads of a CTA, CTAs, and whether rows are moved 16 bytes at a time.
+// How a launch is cut: warps and lanes of the forward pass, CTAs and threads of the backward pass, and whether rows are moved 16 bytes at a
+// time.
 struct ScanCut {
+    ScanSplit split;
+    long long warps;
     int threads;
     long long ctas;
     bool whole;
@@ -50,18 +79,18 @@ struct ScanLaunch {
 template <typename T>
 ptq_status_t ScanLaunch<T>::forward(int mode, const ptq::ScanParams &p, const ScanCut &cut, cudaStream_t stream)
 {
-    return with_split(p.states, [&](auto ns, auto lanes) {
+    return with_forward_split(cut.split, [&](auto form) {
         return with_flag(cut.whole, [&](auto whole) {
-            constexpr int kNS = decltype(ns)::value, kS = decltype(lanes)::value;
+            using F = decltype(form);
+            constexpr int kThreads = ptq::kScanWarps * 32;
             constexpr bool kWhole = decltype(whole)::value;
-            const size_t smem = static_cast<size_t>(64) * cut.threads + 64 * kS * kS * kNS;
-            const unsigned grid = static_cast<unsigned>(cut.ctas);
+            const unsigned grid = static_cast<unsigned>(ceil_div(cut.warps, ptq::kScanWarps));
             if (mode == ptq::kScanForward)
-                ptq::ptq_scan_kernel<T, kNS, kS, ptq::kScanForward, kWhole><<<grid, cut.threads, smem, stream>>>(p);
+                ptq::ptq_scan_kernel<T, F::channels, F::states, F::lanes, ptq::kScanForward, kWhole><<<grid, kThreads, 0, stream>>>(p);
             else if (mode == ptq::kScanSum)
-                ptq::ptq_scan_kernel<T, kNS, kS, ptq::kScanSum, kWhole><<<grid, cut.threads, smem, stream>>>(p);
+                ptq::ptq_scan_kernel<T, F::channels, F::states, F::lanes, ptq::kScanSum, kWhole><<<grid, kThreads, 0, stream>>>(p);
             else
-                ptq::ptq_scan_kernel<T, kNS, kS, ptq::kScanGradSum, kWhole><<<grid, cut.threads, smem, stream>>>(p);
+                ptq::ptq_scan_kernel<T, F::channels, F::states, F::lanes, ptq::kScanGradSum, kWhole><<<grid, kThreads, 0, stream>>>(p);
             return launched();
         });
     });
