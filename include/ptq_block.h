@@ -41,7 +41,7 @@ typedef enum { PTQ_F16 = 0, PTQ_BF16 = 1, PTQ_F32 = 2 } ptq_dtype_t;
 #define PTQ_MAX_CHANNELS    65536
 #define PTQ_MAX_STATES      32
 #define PTQ_MAX_NORM_COLS   8192
-#define PTQ_SCAN_HISTORY    16   /* steps between two states that the backward pass starts from */
+#define PTQ_SCAN_HISTORY    8    /* steps between two states that the backward pass starts from */
 
 /*
  * Gated linear recurrence.  For step i of a sequence (token p), channel d of group g = d / (channels / groups), state n:
@@ -70,7 +70,7 @@ typedef struct {
  *   y            device, [batch, length, channels]
  *   final_state  device, [batch, channels, states]: h behind the last step, or NULL; may be `state` itself
  *   history      device, [batch, ceil(length / PTQ_SCAN_HISTORY), channels, states], or NULL: the state in front of every
- *                16th step, for ptq_scan_backward; entries behind a sequence's end are left as they are
+ *                8th step, for ptq_scan_backward; entries behind a sequence's end are left as they are
  *   workspace    device, 16-byte aligned, at least ptq_scan_workspace_bytes(s, 0) bytes (may be 0: then it may be NULL)
  * Length 1 (a token of a generating model) takes a kernel of its own.
  */

@@ -24,7 +24,7 @@ import contextlib
 from . import binding
 
 FLAG_SEQ_REVERSE, FLAG_SCAN_SOFTPLUS, FLAG_CONV_SILU, FLAG_NORM_LAYER, FLAG_NORM_GATE_OUT = 2, 1, 1, 1, 2
-SCAN_HISTORY = 16                 # PTQ_SCAN_HISTORY: steps between two states that the backward pass starts from
+SCAN_HISTORY = 8                  # PTQ_SCAN_HISTORY: steps between two states that the backward pass starts from
 
 _on_device = contextlib.nullcontext()
 
@@ -51,7 +51,7 @@ def _status(r):
 
 
 def scan_history(u, states: int):
-    """The buffer ``[batch, ceil(length / 16), channels, states]`` that ``gated_scan`` fills for ``gated_scan_backward``."""
+    """The buffer ``[batch, ceil(length / 8), channels, states]`` that ``gated_scan`` fills for ``gated_scan_backward``."""
     import torch
     return torch.empty((u.shape[0], -(-u.shape[1] // SCAN_HISTORY), u.shape[2], states), dtype=torch.float32, device=u.device)
 

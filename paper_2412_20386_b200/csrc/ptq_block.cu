@@ -65,28 +65,27 @@ ptq_status_t with_type(int dtype, Fn fn)
 
 // ---------------------------------------------------------------------------------------------------- scan
 // How a call is cut.  Chunks: until the GPU has enough warps, but of 256 steps at least, since every further chunk has to be
-// gone over twice.  The forward pass and the backward pass cut a call alike, so that one rule sizes both workspaces.
+// gone over twice.  The forward pass and the backward pass cut the sequences alike, so that one rule sizes both workspaces.
 struct ScanPlan {
     ScanSplit split;                  // of the forward pass
-    int threads, group_warps, group_blocks, chunk_len, chunks;
+    int group_warps, group_blocks, chunk_len, chunks;
     long long warps, ctas;            // of one chunk
-    ScanCut cut(int n, bool whole) const { return {split, warps * n, threads, ctas * n, whole}; }
+    ScanCut cut(int n, bool whole) const { return {split, warps * n, ctas * n, whole}; }
 };
 ScanPlan scan_plan(const ptq_scan_t &s)
 {
-    const int per_group = s.channels / s.groups, lanes = scan_split_backward(s.states).lanes;
+    const int per_group = s.channels / s.groups;
     const long long sequences = static_cast<long long>(s.batch) * s.groups;
     ScanPlan p;
     p.split = scan_split_forward(s.states, false);
     const auto warps = [&] { return sequences * ceil_div(per_group, p.split.width()); };
-    const long long chunks = std::max(1ll, std::min(ceil_div(16 * kSms, warps()), ceil_div(s.length, 256)));
+    const long long chunks = std::max(1ll, std::min(ceil_div(12 * kSms, warps()), ceil_div(s.length, 256)));
     if (warps() * chunks < 8 * kSms) p.split = scan_split_forward(s.states, true);
     p.chunk_len = static_cast<int>(ceil_div(ceil_div(s.length, chunks), 64) * 64);
     p.chunks = static_cast<int>(ceil_div(s.length, p.chunk_len));
     p.group_warps = static_cast<int>(ceil_div(per_group, p.split.width()));
     p.warps = warps();
-    p.threads = lanes == 1 || (lanes < 8 && sequences * ceil_div(per_group, 256 / lanes) * p.chunks < kSms) ? 128 : 256;
-    p.group_blocks = static_cast<int>(ceil_div(per_group, p.threads / lanes));
+    p.group_blocks = static_cast<int>(ceil_div(per_group, scan_split_backward(s.states).width() * ptq::kScanWarps));
     p.ctas = sequences * p.group_blocks;
     return p;
 }

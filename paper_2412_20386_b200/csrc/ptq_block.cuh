@@ -156,7 +156,8 @@ __device__ __forceinline__ void store_piece(T *p, const float (&f)[kE], int n)
     store_piece<kWhole, T, kE>(p, r, n);
 }
 
-// kN consecutive floats, of which n exist; kWhole: the address allows accesses of 16 bytes, and n is a multiple of four where kN is.
+// kN consecutive floats, of which n exist; kWhole: the address allows accesses of 16 bytes (8, if kN is 2), and n ends between
+// two of them.
 template <bool kWhole, int kN>
 __device__ __forceinline__ void load_floats(float (&f)[kN], const float *p, int n)
 {
@@ -170,6 +171,11 @@ __device__ __forceinline__ void load_floats(float (&f)[kN], const float *p, int 
             f[k + 2] = v.z;
             f[k + 3] = v.w;
         }
+    } else if constexpr (kN == 2 && kWhole) {
+        float2 v = make_float2(0.0f, 0.0f);
+        if (n >= 2) v = *reinterpret_cast<const float2 *>(p);
+        f[0] = v.x;
+        f[1] = v.y;
     } else {
 #pragma unroll
         for (int k = 0; k < kN; ++k) {

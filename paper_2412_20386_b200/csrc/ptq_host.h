@@ -43,4 +43,28 @@ ptq_status_t no_throw(Fn fn)
     }
 }
 
+// Opt a kernel in to `bytes` of dynamic shared memory, once per kernel and device (the attribute belongs
+// to the function on the CURRENT device, which is `device`).  The kernel is
+// a template argument so that every kernel has its own flags.
+template <auto kKern>
+ptq_status_t ensure_smem(int device, int bytes)
+{
+    constexpr int kMaxDevices = 64;
+    static std::atomic<bool> done[kMaxDevices] = {};
+    if (device < 0 || device >= kMaxDevices) return fail(PTQ_ERR_CUDA, "device index %d out of range", device);
+    // lock-free once the attribute is set; two threads racing on the first call both set the same value
+    if (!done[device].load(std::memory_order_acquire)) {
+        PTQ_CUDA(cudaFuncSetAttribute(kKern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+        done[device].store(true, std::memory_order_release);
+    }
+    return PTQ_OK;
+}
+template <auto kKern>
+ptq_status_t ensure_smem(int bytes)
+{
+    int device = -1;
+    PTQ_CUDA(cudaGetDevice(&device));
+    return ensure_smem<kKern>(device, bytes);
+}
+
 }  // namespace ptq_host

@@ -18,9 +18,8 @@
 
 namespace ptq {
 
-constexpr int kScanHistory = 16;      // steps between two states that are kept for the backward pass
-constexpr int kScanWarps = 4;         // of a CTA of the forward pass; they work alone
-constexpr int kScanThreads = 256, kScanLeast = 128;       // of a CTA of the backward pass: most, and fewest where a channel has fewer than eight lanes
+constexpr int kScanHistory = 8;       // steps between two states that are kept for the backward pass
+constexpr int kScanWarps = 4;         // of a CTA; the forward pass's work alone
 
 constexpr unsigned kScanSoftplus = 1u, kScanReverse = 2u;
 
@@ -99,10 +98,6 @@ __device__ __forceinline__ void scan_decays(float (&a)[kNS], float dt, const flo
 // Decay rates times log2(e); finite, so that a step without a token (dt = 0) leaves the state as it is.
 __device__ __forceinline__ float scan_rate(float a) { return fminf(fmaxf(a * kLog2e, -3.0e38f), 3.0e38f); }
 
-// Where a channel's pair (dt, dt u) of a row lies: the four 16-byte pieces of eight channels are permuted by the number of
-// the eight, so that the rows' threads, which write eight channels each, meet no bank twice.
-__device__ __forceinline__ int scan_column(int ch) { return (ch & ~7) | (((((ch >> 1) & 3) ^ ((ch >> 4) & 3)) << 1) | (ch & 1)); }
-
 struct ScanBlock {
     int b, chunk, g, c0, c_end, len, i0, i1;
     // block: which of the shares of `width` channels (group_blocks to a group) of which chunk of which sequence
@@ -144,7 +139,7 @@ __device__ __forceinline__ void scan_fold(float (&h)[kNS], const float (&rate)[k
 enum { kScanForward = 0, kScanSum = 1, kScanGradSum = 2 };
 
 template <typename T, int kC, int kNS, int kS, int kMode, bool kWhole>
-__global__ void __launch_bounds__(kScanWarps * 32, 4) ptq_scan_kernel(const ScanParams p)
+__global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_kernel(const ScanParams p)
 {
     constexpr int kWidth = 32 / kS * kC, kPitch = kWidth + 2;      // channels of the warp; the pad keeps the rows' lanes off each other's banks
     constexpr int kRows = 256 / kWidth, kNP = kNS * kS;            // steps of a tile, states padded
@@ -382,108 +377,136 @@ __global__ void __launch_bounds__(kScanWarps * 32, 4) ptq_scan_kernel(const Scan
     }
 }
 
-// Backward pass of the tiles of kScanHistory steps of a chunk, from the last one to the first.  From the state that the
-// forward pass kept in front of the tile the lanes run the recurrence forward once more and hold a h of all its steps in registers; then
-// they run
-//   G = C dyo + e,   q = G a h,   s = sum_n G B,   r = sum_n rate q,   dA += dt q,   e <- a G         (dyo = dy silu(z))
-// backward, a taken again from dt.  Over the channels sum dC = h dyo and dB = G dt u (eight values at a time over the lanes
-// of a warp, the warps' sums through shared memory, the CTAs' through global memory, each in a fixed order); over the
-// states of a channel o, s and r.  The rows' threads then make du = dt s + D dyo, ddelta = (u s + r ln 2) sigmoid and dz.
-// Bound: issue slots (about 24 per state and step, seven of them the sums of dB and dC).
-template <typename T, int kNS, int kS, bool kWhole>
-__global__ void __launch_bounds__(kScanThreads, 2) ptq_scan_backward_kernel(const ScanParams p)
+// Shared memory of a CTA of the backward pass.
+__host__ __device__ constexpr size_t scan_backward_smem(int channels, int states, int lanes)
 {
-    constexpr int kRows = kScanHistory, kNP = kNS * kS, kE = kRows / kS;     // channels of a row that a thread holds
-    constexpr bool kEarly = kE <= 4;                      // the next tile's rows are fetched into registers during this one's recurrence
-    constexpr int kHalf = kRows * kS;                     // pieces of B (or of C) in a tile
-    constexpr int kLeast = kS == 8 ? kScanThreads : kScanLeast;
-    constexpr int kPieces = (2 * kHalf + kLeast - 1) / kLeast;
+    const size_t width = 32 / lanes * channels, rows = 256 / width, np = static_cast<size_t>(states) * lanes;
+    const size_t warp = rows * (width + 2) * 16 + 2 * rows * np * 4 + 2 * 32 * 8 * 4;
+    return kScanWarps * (warp + 2 * rows * 2 * np * 4);
+}
+
+// Backward pass of a chunk, tile by tile from the last one to the first, each in stretches of kScanHistory steps.  From the state that the
+// forward pass kept in front of the stretch the lanes run the recurrence forward once more and hold a h of its steps in registers;
+// then they run
+//   G = C dyo + e,   q = G a h,   s = sum_n G B,   r = sum_n rate q,   dA += dt q,   e <- a G         (dyo = dy silu(z))
+// backward, a taken again from dt.  Over the channels sum dC = h dyo and dB = G dt u: the two of a lane first, then eight values at a time
+// over the lanes of a warp, the four warps' sums through shared memory, the CTAs' through global memory, each in a fixed order.  Over the
+// states of a channel sum o, s and r.  The rows' lanes then make du = dt s + D dyo, ddelta = (u s + r ln 2) sigmoid and dz.
+// Bound: issue slots.
+template <typename T, int kC, int kNS, int kS, bool kWhole>
+__global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(const ScanParams p)
+{
+    constexpr int kWidth = 32 / kS * kC, kPitch = kWidth + 2;      // channels of a warp
+    constexpr int kRows = 256 / kWidth, kNP = kNS * kS;            // steps of a tile, states padded
+    constexpr int kStretch = kScanHistory;
     constexpr int kSteps = 8 / kNS;                       // steps whose dB (dC) values are summed together: eight values
     constexpr int kLeft = kS >= 4 ? kS / 4 : 1;           // of them left in a lane
-    constexpr int kGroup = kSteps > kS ? kSteps : kS;     // steps of an unrolled group
-    constexpr int kPairs = kS >= 4 ? kS / 2 : 1;          // steps whose (s, r) are summed together
+    constexpr int kSR = 2 * kC > kS ? 2 * kC : kS;        // values s and r that are summed together
+    constexpr int kO = kC > kS ? kC : kS;                 // values o that are summed together
+    constexpr int kPer = kNP >= 2 ? 2 : 1;
+    constexpr int kBC = (kRows * kNP + 32 * kPer - 1) / (32 * kPer);
+    constexpr int kApart = kBC > 1 ? 32 * kPer / kNP : kRows;
+    static_assert(kApart * kBC == kRows && kRows % kStretch == 0, "a fetch goes one tile on, in whole stretches");
+    constexpr bool kEarly = sizeof(T) == 2;               // the next tile's rows are fetched into registers during this one's recurrence
+    constexpr int kThreads = kScanWarps * 32;
+    struct Warp {
+        float2 pair[kRows * kPitch];                      // (dt, dt u), later (s, r)
+        float g[kRows * kPitch], o[kRows * kPitch];       // dyo; o without D u
+        float BC[2][kRows * kNP];
+        float sum_D[32][8], sum_bias[32][8];              // of the lane's channels, over its rows
+    };
     extern __shared__ __align__(16) unsigned char scan_smem[];
-    const int threads = blockDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5;
-    const int width = threads / kS;
-    float2 *s_pair = reinterpret_cast<float2 *>(scan_smem);                       // [kRows][width]: (dt, dt u), later (s, r)
-    float *s_do = reinterpret_cast<float *>(s_pair + kRows * width);              // [kRows][width]: dyo
-    float *s_o = s_do + kRows * width;                                            // [kRows][width]: o without D u
-    float *s_BC = s_o + kRows * width;                                            // [2][kRows][kNP]
-    float *s_sum = s_BC + 2 * kRows * kNP;                                        // [warps][kRows][2][kNP]: dB, dC
-    const ScanBlock blk(p, blockIdx.x, p.group_blocks, p.chunks, 0, width);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    Warp &w = reinterpret_cast<Warp *>(scan_smem)[warp];
+    float *const s_sum = reinterpret_cast<float *>(scan_smem + kScanWarps * sizeof(Warp));      // [2][kScanWarps][kRows][2][kNP]: dB, dC
+    constexpr int kSums = kRows * 2 * kNP;
+    static_assert(kScanWarps * (sizeof(Warp) + 2 * kSums * sizeof(float)) == scan_backward_smem(kC, kNS, kS), "as the launch sizes it");
+    const ScanBlock blk(p, blockIdx.x, p.group_blocks, p.chunks, 0, kWidth * kScanWarps);
     const bool softplus = p.flags & kScanSoftplus, reverse = p.flags & kScanReverse;
 
-    const int ch = tid / kS, n0 = (tid % kS) * kNS, d = blk.c0 + ch, col = scan_column(ch);
-    const int nn = d < blk.c_end ? max(min(kNS, p.states - n0), 0) : 0;
+    const int ch = lane / kS * kC, n0 = (lane % kS) * kNS, d = blk.c0 + warp * kWidth + ch;
     const long long state_at = (static_cast<long long>(blk.b) * p.channels + d) * p.states + n0;
-    float rate[kNS], e[kNS], dA[kNS];
-    load_floats<kWhole, kNS>(rate, p.A + static_cast<long long>(d) * p.states + n0, nn);
+    int nn[kC];
+    float rate[kC][kNS], e[kC][kNS], dA[kC][kNS];
 #pragma unroll
-    for (int k = 0; k < kNS; ++k) {
-        rate[k] = scan_rate(rate[k]);
-        e[k] = dA[k] = 0.0f;
-    }
-    if (blk.chunk < p.chunks - 1) {
-        if (nn > 0) scan_fold<kWhole, kNS>(e, rate, p, blk.b, d, n0, nn, p.chunks - 1, blk.chunk, -1);
-    } else if (p.dfinal) {
-        load_floats<kWhole, kNS>(e, p.dfinal + state_at, nn);
+    for (int j = 0; j < kC; ++j) {
+        nn[j] = d + j < blk.c_end ? max(min(kNS, p.states - n0), 0) : 0;
+        load_floats<kWhole, kNS>(rate[j], p.A + static_cast<long long>(d + j) * p.states + n0, nn[j]);
+#pragma unroll
+        for (int k = 0; k < kNS; ++k) {
+            rate[j][k] = scan_rate(rate[j][k]);
+            e[j][k] = dA[j][k] = 0.0f;
+        }
+        if (blk.chunk < p.chunks - 1) {
+            if (nn[j] > 0) scan_fold<kWhole, kNS>(e[j], rate[j], p, blk.b, d + j, n0, nn[j], p.chunks - 1, blk.chunk, -1);
+        } else if (p.dfinal) {
+            load_floats<kWhole, kNS>(e[j], p.dfinal + state_at + j * p.states, nn[j]);
+        }
     }
 
-    const int row = tid / (width / kE), c = blk.c0 + (tid % (width / kE)) * kE;
-    const int cn = max(min(kE, blk.c_end - c), 0);
-    float sum_D[kE], sum_bias[kE];
+    // the lane's part of a row
+    const int row = lane / (kWidth / 8), part8 = lane % (kWidth / 8) * 8, c = blk.c0 + warp * kWidth + part8;
+    const int cn = max(min(8, blk.c_end - c), 0);
 #pragma unroll
-    for (int i = 0; i < kE; ++i) sum_D[i] = sum_bias[i] = 0.0f;
+    for (int i = 0; i < 8; ++i) w.sum_D[lane][i] = w.sum_bias[lane][i] = 0.0f;
     struct Rows {
-        Piece<T, kE> u, delta, z, dy;
+        Piece<T, 8> u, delta, z, dy;
     };
     const long long sequence = static_cast<long long>(blk.b) * p.length;
-    const long long kept_rows = (p.length + kScanHistory - 1) / kScanHistory;
     const auto token_of = [&](int i) { return static_cast<long long>(reverse && i < blk.len ? blk.len - 1 - i : i); };
     const auto rows_of = [&](int i0) {
         Rows r;
         const bool on = i0 + row < blk.i1;
         const long long at = on ? token_of(i0 + row) : 0;
         const int n = on ? cn : 0;
-        r.u = load_piece<kWhole, T, kE>(static_cast<const T *>(p.u) + blk.b * p.u_b + at * p.u_l + c, n);
-        r.delta = load_piece<kWhole, T, kE>(static_cast<const T *>(p.delta) + blk.b * p.delta_b + at * p.delta_l + c, n);
-        r.dy = load_piece<kWhole, T, kE>(static_cast<const T *>(p.dy) + (sequence + at) * p.channels + c, n);
-        if (p.z) r.z = load_piece<kWhole, T, kE>(static_cast<const T *>(p.z) + blk.b * p.z_b + at * p.z_l + c, n);
+        r.u = load_piece<kWhole, T, 8>(static_cast<const T *>(p.u) + blk.b * p.u_b + at * p.u_l + c, n);
+        r.delta = load_piece<kWhole, T, 8>(static_cast<const T *>(p.delta) + blk.b * p.delta_b + at * p.delta_l + c, n);
+        r.dy = load_piece<kWhole, T, 8>(static_cast<const T *>(p.dy) + (sequence + at) * p.channels + c, n);
+        r.z.zero();
+        if (p.z) r.z = load_piece<kWhole, T, 8>(static_cast<const T *>(p.z) + blk.b * p.z_b + at * p.z_l + c, n);
         return r;
     };
-    Piece<T, kNS> r_BC[kPieces];
-    float r_h[kNS];
+    Piece<T, kPer> r_BC[2][kBC];
+    const int bc_t = kPer * lane / kNP, bc_n = kPer * lane % kNP;
+    const bool has = kPer * lane < kRows * kNP;
     const auto fetch = [&](int i0) {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int q = tid + i * threads, t = (q % kHalf) / kS, n1 = q % kS * kNS;
-            const bool on = q < 2 * kHalf && i0 + t < blk.i1;
-            const long long tok = on ? token_of(i0 + t) : 0;
-            const T *from = q >= kHalf ? static_cast<const T *>(p.C) + blk.b * p.C_b + tok * p.C_l + blk.g * p.C_g + n1
-                                       : static_cast<const T *>(p.B) + blk.b * p.B_b + tok * p.B_l + blk.g * p.B_g + n1;
-            r_BC[i] = load_piece<false, T, kNS>(from, on ? p.states - n1 : 0);
+        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+            for (int i = 0; i < kBC; ++i) {
+                const int step = i0 + bc_t + i * kApart;
+                const int states = has && step < blk.i1 ? p.states - bc_n : 0;
+                const long long tok = token_of(step);
+                const T *from = k ? static_cast<const T *>(p.C) + blk.b * p.C_b + tok * p.C_l + blk.g * p.C_g + bc_n
+                                  : static_cast<const T *>(p.B) + blk.b * p.B_b + tok * p.B_l + blk.g * p.B_g + bc_n;
+                r_BC[k][i] = p.pairs ? load_piece<true, T, kPer>(from, states) : load_piece<false, T, kPer>(from, states);
+            }
         }
-        load_floats<kWhole, kNS>(r_h, p.kept + ((blk.b * kept_rows + i0 / kScanHistory) * p.channels + d) * p.states + n0, nn);
     };
-    const int slot_of_row = row * width;
-    const auto column = [&](int i) { return slot_of_row + scan_column(c - blk.c0 + i); };
+    const long long kept_step = static_cast<long long>(p.channels) * p.states;
+    const float *const kept = p.kept + blk.b * ((p.length + kScanHistory - 1) / kScanHistory) * kept_step + static_cast<long long>(d) * p.states + n0;
+    float r_h[kC][kNS];
+    const auto fetch_state = [&](int i) {
+#pragma unroll
+        for (int j = 0; j < kC; ++j) load_floats<kWhole, kNS>(r_h[j], kept + i / kScanHistory * kept_step + j * p.states, nn[j]);
+    };
 
     const int end = min(blk.i0 + p.chunk_len, p.length);
     int i0 = blk.i0 + (end - 1 - blk.i0) / kRows * kRows;
     // tiles without a token: their gradients are zeros
     for (; i0 >= blk.i0 && i0 >= blk.i1; i0 -= kRows) {
         if (i0 + row < end) {
-            float zero[kE];
+            float zero[8];
 #pragma unroll
-            for (int i = 0; i < kE; ++i) zero[i] = 0.0f;
+            for (int i = 0; i < 8; ++i) zero[i] = 0.0f;
             const long long at = (sequence + i0 + row) * p.channels + c;
-            store_piece<kWhole, T, kE>(static_cast<T *>(p.du) + at, zero, cn);
-            store_piece<kWhole, T, kE>(static_cast<T *>(p.ddelta) + at, zero, cn);
-            if (p.z) store_piece<kWhole, T, kE>(static_cast<T *>(p.dz) + at, zero, cn);
+            store_piece<kWhole, T, 8>(static_cast<T *>(p.du) + at, zero, cn);
+            store_piece<kWhole, T, 8>(static_cast<T *>(p.ddelta) + at, zero, cn);
+            if (p.z) store_piece<kWhole, T, 8>(static_cast<T *>(p.dz) + at, zero, cn);
         }
     }
-    // where the thread's sums of dB and dC go: which of the two, which state
-    const int out_which = tid / kNP & 1, out_n = tid % kNP, share = blockIdx.x % (p.groups * p.group_blocks);
+    // the thread's sums of dB and dC: which of the two, which state, which step of the tile first
+    const int out_which = tid / kNP & 1, out_n = tid % kNP, out_t = tid / (2 * kNP), share = blockIdx.x % (p.groups * p.group_blocks);
     const auto put_BC = [&](int i, float v) {
         const long long tok = sequence + token_of(i);
         if (p.part_BC)
@@ -491,227 +514,249 @@ __global__ void __launch_bounds__(kScanThreads, 2) ptq_scan_backward_kernel(cons
         else
             static_cast<T *>(out_which ? p.dC : p.dB)[(tok * p.groups + blk.g) * p.states + out_n] = from_f32<T>(v);
     };
-    const int first_dead = max(i0 + kRows, blk.i0);
     if (out_n < p.states)
-        for (int i = first_dead + tid / (2 * kNP); i < end; i += threads / (2 * kNP)) put_BC(i, 0.0f);
+        for (int i = max(i0 + kRows, blk.i0) + out_t; i < end; i += kThreads / (2 * kNP)) put_BC(i, 0.0f);
 
     Rows ahead;
     if (i0 >= blk.i0) {
         fetch(i0);
         if (kEarly) ahead = rows_of(i0);
+        fetch_state(i0 + (min(kRows, blk.i1 - i0) - 1) / kStretch * kStretch);
     }
-    for (; i0 >= blk.i0; i0 -= kRows) {
+    const Piece<float, 8> bias = load_piece<kWhole, float, 8>(p.delta_bias + c, p.delta_bias ? cn : 0);
+    float4 *const own = reinterpret_cast<float4 *>(w.pair + row * kPitch + part8);
+    float *const own_g = w.g + row * kPitch + part8;
+    for (int parity = 0; i0 >= blk.i0; i0 -= kRows, parity ^= 1) {
         const bool row_on = i0 + row < blk.i1;
         {
             const Rows r = kEarly ? ahead : rows_of(i0);
-            const Piece<float, kE> bias = load_piece<kWhole, float, kE>(p.delta_bias + c, p.delta_bias ? cn : 0);
-            float dts[kE];
 #pragma unroll
-            for (int i = 0; i < kE; i += 2) {
-                dts[i] = r.delta[i] + bias[i];
-                dts[i + 1] = r.delta[i + 1] + bias[i + 1];
+            for (int i = 0; i < 8; i += 2) {
+                float4 f;
+                f.x = r.delta[i] + bias[i];
+                f.z = r.delta[i + 1] + bias[i + 1];
                 if (softplus) {
                     float t0, t1;
-                    exp_minus_abs_pair(t0, t1, dts[i], dts[i + 1]);
-                    softplus_pair(dts[i], dts[i + 1], dts[i], dts[i + 1], t0, t1);
+                    exp_minus_abs_pair(t0, t1, f.x, f.z);
+                    softplus_pair(f.x, f.z, f.x, f.z, t0, t1);
                 }
+                mul_pair(f.y, f.w, r.u[i], r.u[i + 1], f.x, f.z);
+                float2 g = make_float2(r.dy[i], r.dy[i + 1]);
+                if (p.z) {
+                    g.x *= r.z[i] * sigmoid_f32(r.z[i]);
+                    g.y *= r.z[i + 1] * sigmoid_f32(r.z[i + 1]);
+                }
+                if (!row_on) {
+                    f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    g = make_float2(0.0f, 0.0f);
+                }
+                own[i / 2] = f;
+                *reinterpret_cast<float2 *>(own_g + i) = g;
             }
 #pragma unroll
-            for (int i = 0; i < kE; ++i) {
-                const float dt = row_on ? dts[i] : 0.0f;
-                float g = r.dy[i];
-                if (p.z) g *= r.z[i] * sigmoid_f32(r.z[i]);
-                s_pair[column(i)] = make_float2(dt, row_on ? dt * r.u[i] : 0.0f);
-                s_do[column(i)] = row_on ? g : 0.0f;
-            }
+            for (int k = 0; k < 2; ++k) {
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                const int q = tid + i * threads;
-                if (q < 2 * kHalf) {
-                    float f[kNS];
-#pragma unroll
-                    for (int k = 0; k < kNS; ++k) f[k] = r_BC[i][k];
-                    store_floats<true, kNS>(s_BC + q * kNS, f, kNS);
+                for (int i = 0; i < kBC; ++i) {
+                    float *at = w.BC[k] + kPer * (lane + 32 * i);
+                    if (!has) continue;
+                    if constexpr (kPer == 2)
+                        *reinterpret_cast<float2 *>(at) = make_float2(r_BC[k][i][0], r_BC[k][i][1]);
+                    else
+                        *at = r_BC[k][i][0];
                 }
             }
         }
-        float h[kNS];
-#pragma unroll
-        for (int k = 0; k < kNS; ++k) h[k] = r_h[k];
-        __syncthreads();
+        __syncwarp();
         if (i0 > blk.i0) {
             fetch(i0 - kRows);
             if (kEarly) ahead = rows_of(i0 - kRows);
         }
-        float ah[kRows][kNS];
+        float *const sums = s_sum + (parity * kScanWarps + warp) * kSums;
+        for (int t0 = (min(kRows, blk.i1 - i0) - 1) / kStretch * kStretch; t0 >= 0; t0 -= kStretch) {
+            float h[kC][kNS], ah[kStretch][kC][kNS];
 #pragma unroll
-        for (int t = 0; t < kRows; t += kGroup) {
-            float o[kGroup], dc[kGroup * kNS];
+            for (int j = 0; j < kC; ++j)
 #pragma unroll
-            for (int s = 0; s < kGroup; ++s) {
-                const float2 x = s_pair[(t + s) * width + col];
-                const float g = s_do[(t + s) * width + col];
-                float in[kNS], out[kNS], a[kNS], v[kNS];
-                load_floats<true, kNS>(in, s_BC + (t + s) * kNP + n0, kNS);
-                load_floats<true, kNS>(out, s_BC + (kRows + t + s) * kNP + n0, kNS);
-                scan_decays<kNS>(a, x.x, rate);
-                mul_each<kNS>(ah[t + s], a, h);
-                fma_each<kNS>(h, x.y, in, ah[t + s]);
-                o[s] = dot_each<kNS>(h, out);
-                mul_each<kNS>(v, g, h);
+                for (int k = 0; k < kNS; ++k) h[j][k] = r_h[j][k];
+            if (i0 + t0 > blk.i0) fetch_state(i0 + t0 - kStretch);
+            float o[kStretch * kC], v8[kStretch * kNS];
 #pragma unroll
-                for (int k = 0; k < kNS; ++k) dc[s * kNS + k] = v[k];
+            for (int s = 0; s < kStretch; ++s) {
+                float x[2 * kC], g[kC], in[kNS], out[kNS];
+                load_floats<true, 2 * kC>(x, reinterpret_cast<const float *>(w.pair + (t0 + s) * kPitch + ch), 2 * kC);
+                load_floats<true, kC>(g, w.g + (t0 + s) * kPitch + ch, kC);
+                load_floats<true, kNS>(in, w.BC[0] + (t0 + s) * kNP + n0, kNS);
+                load_floats<true, kNS>(out, w.BC[1] + (t0 + s) * kNP + n0, kNS);
+                float dc[kNS];
+#pragma unroll
+                for (int j = 0; j < kC; ++j) {
+                    float a[kNS];
+                    scan_decays<kNS>(a, x[2 * j], rate[j]);
+                    mul_each<kNS>(ah[s][j], a, h[j]);
+                    fma_each<kNS>(h[j], x[2 * j + 1], in, ah[s][j]);
+                    o[s * kC + j] = dot_each<kNS>(h[j], out);
+                    if (j == 0)
+                        mul_each<kNS>(dc, g[j], h[j]);
+                    else
+                        fma_each<kNS>(dc, g[j], h[j], dc);
+                }
+#pragma unroll
+                for (int k = 0; k < kNS; ++k) v8[s * kNS + k] = dc[k];
+                if ((s + 1) % kSteps == 0) {
+                    float v[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = v8[(s + 1 - kSteps) * kNS + i];
+                    lane_sums<8, kS, 16>(v, lane);
+                    if (lane / kS < 8) {
+#pragma unroll
+                        for (int i = 0; i < kLeft; ++i) {
+                            const int idx = first_sum<8, kS, 16>(lane) + i;
+                            sums[((t0 + s + 1 - kSteps + idx / kNS) * 2 + 1) * kNP + n0 + idx % kNS] = v[i];
+                        }
+                    }
+                }
             }
             if (p.z) {
 #pragma unroll
-                for (int s = 0; s < kGroup; s += kS) {
-                    float v[kS];
+                for (int s = 0; s < kStretch * kC; s += kO) {
+                    float v[kO];
 #pragma unroll
-                    for (int i = 0; i < kS; ++i) v[i] = o[s + i];
-                    lane_sums<kS, 1, kS / 2>(v, lane);
-                    s_o[(t + s + first_sum<kS, 1, kS / 2>(lane)) * width + col] = v[0];
+                    for (int i = 0; i < kO; ++i) v[i] = o[s + i];
+                    lane_sums<kO, 1, kS / 2>(v, lane);
+#pragma unroll
+                    for (int i = 0; i < kO / kS; ++i) {
+                        const int idx = s + first_sum<kO, 1, kS / 2>(lane) + i;
+                        w.o[(t0 + idx / kC) * kPitch + ch + idx % kC] = v[i];
+                    }
                 }
             }
 #pragma unroll
-            for (int s = 0; s < kGroup; s += kSteps) {
-                float v[8];
+            for (int s = kStretch - 1; s >= 0; --s) {
+                float x[2 * kC], g[kC], in[kNS], out[kNS];
+                load_floats<true, 2 * kC>(x, reinterpret_cast<const float *>(w.pair + (t0 + s) * kPitch + ch), 2 * kC);
+                load_floats<true, kC>(g, w.g + (t0 + s) * kPitch + ch, kC);
+                load_floats<true, kNS>(in, w.BC[0] + (t0 + s) * kNP + n0, kNS);
+                load_floats<true, kNS>(out, w.BC[1] + (t0 + s) * kNP + n0, kNS);
+                float db[kNS];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = dc[s * kNS + i];
-                lane_sums<8, kS, 16>(v, lane);
-                if (lane / kS < 8) {
+                for (int j = 0; j < kC; ++j) {
+                    float a[kNS], G[kNS], q[kNS];
+                    scan_decays<kNS>(a, x[2 * j], rate[j]);
+                    fma_each<kNS>(G, g[j], out, e[j]);
+                    mul_each<kNS>(e[j], a, G);
+                    if (j == 0)
+                        mul_each<kNS>(db, x[2 * j + 1], G);
+                    else
+                        fma_each<kNS>(db, x[2 * j + 1], G, db);
+                    o[s * kC + j] = dot_each<kNS>(G, in);                            // s
+                    mul_each<kNS>(q, G, ah[s][j]);
+                    ah[s][j][0] = dot_each<kNS>(q, rate[j]);                         // r
+                    fma_each<kNS>(dA[j], x[2 * j], q, dA[j]);
+                }
 #pragma unroll
-                    for (int i = 0; i < kLeft; ++i) {
-                        const int idx = first_sum<8, kS, 16>(lane) + i;
-                        s_sum[((warp * kRows + t + s + idx / kNS) * 2 + 1) * kNP + n0 + idx % kNS] = v[i];
+                for (int k = 0; k < kNS; ++k) v8[s * kNS + k] = db[k];
+                if (s % kSteps == 0) {
+                    float v[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = v8[s * kNS + i];
+                    lane_sums<8, kS, 16>(v, lane);
+                    if (lane / kS < 8) {
+#pragma unroll
+                        for (int i = 0; i < kLeft; ++i) {
+                            const int idx = first_sum<8, kS, 16>(lane) + i;
+                            sums[(t0 + s + idx / kNS) * 2 * kNP + n0 + idx % kNS] = v[i];
+                        }
+                    }
+                }
+                if (s * 2 * kC % kSR == 0) {
+                    float v[kSR];
+#pragma unroll
+                    for (int i = 0; i < kSR; ++i) {
+                        const int at = s * kC + i / 2;
+                        v[i] = i & 1 ? ah[at / kC][at % kC][0] : o[at];
+                    }
+                    lane_sums<kSR, 1, kS / 2>(v, lane);
+                    __syncwarp();                         // all lanes of the channels have read the steps' pairs
+#pragma unroll
+                    for (int i = 0; i < kSR / kS; ++i) {
+                        const int idx = first_sum<kSR, 1, kS / 2>(lane) + i, at = s * kC + idx / 2;
+                        reinterpret_cast<float *>(w.pair + (t0 + at / kC) * kPitch + ch + at % kC)[idx & 1] = v[i];
                     }
                 }
             }
         }
-#pragma unroll
-        for (int t = kRows - kGroup; t >= 0; t -= kGroup) {
-            float db[kGroup * kNS], sr[kGroup * 2];
-#pragma unroll
-            for (int s = kGroup - 1; s >= 0; --s) {
-                const float2 x = s_pair[(t + s) * width + col];
-                const float g = s_do[(t + s) * width + col];
-                float in[kNS], out[kNS], a[kNS], v[kNS], G[kNS];
-                load_floats<true, kNS>(in, s_BC + (t + s) * kNP + n0, kNS);
-                load_floats<true, kNS>(out, s_BC + (kRows + t + s) * kNP + n0, kNS);
-                scan_decays<kNS>(a, x.x, rate);
-                fma_each<kNS>(G, g, out, e);
-                mul_each<kNS>(e, a, G);
-                mul_each<kNS>(v, x.y, G);
-#pragma unroll
-                for (int k = 0; k < kNS; ++k) db[s * kNS + k] = v[k];
-                sr[s * 2] = dot_each<kNS>(G, in);
-                mul_each<kNS>(v, G, ah[t + s]);
-                sr[s * 2 + 1] = dot_each<kNS>(v, rate);
-                fma_each<kNS>(dA, x.x, v, dA);
-            }
-#pragma unroll
-            for (int s = 0; s < kGroup; s += kPairs) {
-                float v[kPairs * 2];
-#pragma unroll
-                for (int i = 0; i < kPairs * 2; ++i) v[i] = sr[s * 2 + i];
-                lane_sums<kPairs * 2, 1, kS / 2>(v, lane);
-                const int idx = first_sum<kPairs * 2, 1, kS / 2>(lane);
-                float2 *at = s_pair + (t + s + idx / 2) * width + col;
-                __syncwarp();                             // all lanes of the channel have read the step's pair
-                if (kS == 1)
-                    *at = make_float2(v[0], v[1]);
-                else
-                    (idx & 1 ? at->y : at->x) = v[0];
-            }
-#pragma unroll
-            for (int s = 0; s < kGroup; s += kSteps) {
-                float v[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = db[s * kNS + i];
-                lane_sums<8, kS, 16>(v, lane);
-                if (lane / kS < 8) {
-#pragma unroll
-                    for (int i = 0; i < kLeft; ++i) {
-                        const int idx = first_sum<8, kS, 16>(lane) + i;
-                        s_sum[(warp * kRows + t + s + idx / kNS) * 2 * kNP + n0 + idx % kNS] = v[i];
-                    }
-                }
-            }
-        }
-        __syncthreads();
+        __syncthreads();                                   // the warps' sums of dB and dC; the next tile's go to the other half
         if (i0 + row < end) {
             const Rows r = rows_of(i0);                    // once more, from the cache: held in registers they would cost occupancy
-            const Piece<float, kE> bias = load_piece<kWhole, float, kE>(p.delta_bias + c, p.delta_bias ? cn : 0);
-            const Piece<float, kE> skip = load_piece<kWhole, float, kE>(p.D + c, p.D ? cn : 0);
-            float du[kE], dd[kE], dz[kE], dts[kE], slopes[kE];
+            const Piece<float, 8> skip = load_piece<kWhole, float, 8>(p.D + c, p.D ? cn : 0);
+            float du[8], dd[8], dz[8];
 #pragma unroll
-            for (int i = 0; i < kE; i += 2) {
+            for (int i = 0; i < 8; i += 2) {
                 const float x0 = r.delta[i] + bias[i], x1 = r.delta[i + 1] + bias[i + 1];
-                dts[i] = x0;
-                dts[i + 1] = x1;
-                slopes[i] = slopes[i + 1] = 1.0f;
+                float dt[2] = {x0, x1}, slope[2] = {1.0f, 1.0f};
                 if (softplus) {
                     float t0, t1;
                     exp_minus_abs_pair(t0, t1, x0, x1);
-                    softplus_pair(dts[i], dts[i + 1], x0, x1, t0, t1);
-                    slopes[i] = __fdividef(x0 < 0.0f ? t0 : 1.0f, 1.0f + t0);
-                    slopes[i + 1] = __fdividef(x1 < 0.0f ? t1 : 1.0f, 1.0f + t1);
+                    softplus_pair(dt[0], dt[1], x0, x1, t0, t1);
+                    slope[0] = __fdividef(x0 < 0.0f ? t0 : 1.0f, 1.0f + t0);
+                    slope[1] = __fdividef(x1 < 0.0f ? t1 : 1.0f, 1.0f + t1);
                 }
-            }
+                const float4 f = own[i / 2];
 #pragma unroll
-            for (int i = 0; i < kE; ++i) {
-                const float2 sr = s_pair[column(i)];
-                const float dyo = s_do[column(i)], D = skip[i], u = r.u[i], dt = dts[i], slope = slopes[i];
-                du[i] = p.D ? fmaf(dt, sr.x, D * dyo) : dt * sr.x;
-                dd[i] = fmaf(u, sr.x, sr.y * kLn2) * slope;
-                dz[i] = 0.0f;
-                if (p.z) {
-                    const float o = p.D ? fmaf(D, u, s_o[column(i)]) : s_o[column(i)], z = r.z[i], gate = sigmoid_f32(z);
-                    dz[i] = r.dy[i] * o * gate * fmaf(z, 1.0f - gate, 1.0f);
-                }
-                if (!row_on) du[i] = dd[i] = dz[i] = 0.0f;
-                if (row_on) {
-                    sum_D[i] = fmaf(u, dyo, sum_D[i]);
-                    sum_bias[i] += dd[i];
+                for (int k = 0; k < 2; ++k) {
+                    const float s = k ? f.z : f.x, q = k ? f.w : f.y, u = r.u[i + k], dyo = own_g[i + k];
+                    du[i + k] = dt[k] * s;
+                    if (p.D) du[i + k] = fmaf(skip[i + k], dyo, du[i + k]);
+                    dd[i + k] = fmaf(u, s, q * kLn2) * slope[k];
+                    dz[i + k] = 0.0f;
+                    if (p.z) {
+                        float o = w.o[row * kPitch + part8 + i + k];
+                        if (p.D) o = fmaf(skip[i + k], u, o);
+                        const float z = r.z[i + k], gate = sigmoid_f32(z);
+                        dz[i + k] = r.dy[i + k] * o * gate * fmaf(z, 1.0f - gate, 1.0f);
+                    }
+                    if (!row_on) du[i + k] = dd[i + k] = dz[i + k] = 0.0f;
+                    if (row_on) {
+                        w.sum_D[lane][i + k] = fmaf(u, dyo, w.sum_D[lane][i + k]);
+                        w.sum_bias[lane][i + k] += dd[i + k];
+                    }
                 }
             }
             const long long at = (sequence + token_of(i0 + row)) * p.channels + c;
-            store_piece<kWhole, T, kE>(static_cast<T *>(p.du) + at, du, cn);
-            store_piece<kWhole, T, kE>(static_cast<T *>(p.ddelta) + at, dd, cn);
-            if (p.z) store_piece<kWhole, T, kE>(static_cast<T *>(p.dz) + at, dz, cn);
+            store_piece<kWhole, T, 8>(static_cast<T *>(p.du) + at, du, cn);
+            store_piece<kWhole, T, 8>(static_cast<T *>(p.ddelta) + at, dd, cn);
+            if (p.z) store_piece<kWhole, T, 8>(static_cast<T *>(p.dz) + at, dz, cn);
         }
-        for (int t = tid / (2 * kNP); t < kRows; t += threads / (2 * kNP)) {
+        for (int t = out_t; t < kRows; t += kThreads / (2 * kNP)) {
             const int i = i0 + t;
             if (i >= end || out_n >= p.states) break;
             float v = 0.0f;
             if (i < blk.i1) {
-                const float *from = s_sum + (t * 2 + out_which) * kNP + out_n;
-#pragma unroll 8
-                for (int w = 0; w < warps; ++w) v += from[w * kRows * 2 * kNP];
+                const float *from = s_sum + parity * kScanWarps * kSums + (t * 2 + out_which) * kNP + out_n;
+#pragma unroll
+                for (int k = 0; k < kScanWarps; ++k) v += from[k * kSums];
             }
             put_BC(i, v);
         }
-        __syncthreads();                                   // s_sum and s_do are written anew
+        __syncwarp();
     }
     const long long part = static_cast<long long>(blk.b) * p.chunks + blk.chunk;
-    store_floats<kWhole, kNS>(p.part_A + (part * p.channels + d) * p.states + n0, dA, nn);
-    if (p.dstate && blk.chunk == 0) store_floats<kWhole, kNS>(p.dstate + state_at, e, nn);
-    // the rows' sums of a channel, in the order of the rows
-    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kE; ++i) {
-        s_do[slot_of_row + c - blk.c0 + i] = sum_D[i];
-        s_o[slot_of_row + c - blk.c0 + i] = sum_bias[i];
+    for (int j = 0; j < kC; ++j) {
+        store_floats<kWhole, kNS>(p.part_A + (part * p.channels + d + j) * p.states + n0, dA[j], nn[j]);
+        if (p.dstate && blk.chunk == 0) store_floats<kWhole, kNS>(p.dstate + state_at + j * p.states, e[j], nn[j]);
     }
-    __syncthreads();
-    for (int i = tid; i < width && blk.c0 + i < blk.c_end; i += threads) {
+    // the rows' sums of a channel, in the order of the rows
+    __syncwarp();
+    for (int i = lane; i < kWidth && blk.c0 + warp * kWidth + i < blk.c_end; i += 32) {
         float a = 0.0f, b = 0.0f;
-#pragma unroll
+#pragma unroll 8
         for (int r = 0; r < kRows; ++r) {
-            a += s_do[r * width + i];
-            b += s_o[r * width + i];
+            a += w.sum_D[r * (kWidth / 8) + i / 8][i % 8];
+            b += w.sum_bias[r * (kWidth / 8) + i / 8][i % 8];
         }
-        p.part_D[part * p.channels + blk.c0 + i] = a;
-        p.part_bias[part * p.channels + blk.c0 + i] = b;
+        p.part_D[part * p.channels + blk.c0 + warp * kWidth + i] = a;
+        p.part_bias[part * p.channels + blk.c0 + warp * kWidth + i] = b;
     }
 }
 

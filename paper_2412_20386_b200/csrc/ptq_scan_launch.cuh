@@ -24,9 +24,8 @@ inline ScanSplit scan_split_forward(int states, bool few)
 }
 inline ScanSplit scan_split_backward(int states)
 {
-    if (states <= 2) return {1, 1, states};
-    if (states <= 4) return {2, 1, 2};
-    return {states <= 8 ? 2 : states <= 16 ? 4 : 8, 1, 4};
+    if (states <= 4) return {1, 1, states == 3 ? 4 : states};
+    return {states <= 8 ? 2 : states <= 16 ? 4 : 8, 2, 4};        // a lane holds 64 products of the stretch
 }
 template <int kC, int kNS, int kS>
 struct ScanForm {
@@ -45,25 +44,32 @@ ptq_status_t with_forward_split(ScanSplit sp, Fn fn)
     return fn(ScanForm<2, 8, 4>());
 }
 template <class Fn>
-ptq_status_t with_split(int states, Fn fn)
+ptq_status_t with_backward_split(int states, Fn fn)
 {
-    using std::integral_constant;
     const ScanSplit sp = scan_split_backward(states);
-    if (sp.lanes == 1 && sp.states == 1) return fn(integral_constant<int, 1>(), integral_constant<int, 1>());
-    if (sp.lanes == 1) return fn(integral_constant<int, 2>(), integral_constant<int, 1>());
-    if (sp.states == 2) return fn(integral_constant<int, 2>(), integral_constant<int, 2>());
-    if (sp.lanes == 2) return fn(integral_constant<int, 4>(), integral_constant<int, 2>());
-    if (sp.lanes == 4) return fn(integral_constant<int, 4>(), integral_constant<int, 4>());
-    return fn(integral_constant<int, 4>(), integral_constant<int, 8>());
+    if (sp.lanes == 1 && sp.states == 1) return fn(ScanForm<1, 1, 1>());
+    if (sp.lanes == 1 && sp.states == 2) return fn(ScanForm<1, 2, 1>());
+    if (sp.lanes == 1) return fn(ScanForm<1, 4, 1>());
+    if (sp.lanes == 2) return fn(ScanForm<2, 4, 2>());
+    if (sp.lanes == 4) return fn(ScanForm<2, 4, 4>());
+    return fn(ScanForm<2, 4, 8>());
+}
+// One token per sequence: lanes of a channel, states of a lane.
+template <class Fn>
+ptq_status_t with_step_split(int states, Fn fn)
+{
+    if (states == 1) return fn(ScanForm<1, 1, 1>());
+    if (states == 2) return fn(ScanForm<1, 2, 1>());
+    if (states <= 4) return fn(ScanForm<1, 4, 1>());
+    if (states <= 8) return fn(ScanForm<1, 4, 2>());
+    if (states <= 16) return fn(ScanForm<1, 4, 4>());
+    return fn(ScanForm<1, 4, 8>());
 }
 
-// How a launch is cut: warps and lanes of the forward pass, CTAs and threads of the backward pass, and whether rows are moved 16 bytes at a
-// time.
+// How a launch is cut: the forward pass's split and its warps, CTAs of the backward pass, and whether rows are moved 16 bytes at a time.
 struct ScanCut {
     ScanSplit split;
-    long long warps;
-    int threads;
-    long long ctas;
+    long long warps, ctas;
     bool whole;
 };
 
@@ -98,12 +104,13 @@ ptq_status_t ScanLaunch<T>::forward(int mode, const ptq::ScanParams &p, const Sc
 template <typename T>
 ptq_status_t ScanLaunch<T>::backward(const ptq::ScanParams &p, const ScanCut &cut, cudaStream_t stream)
 {
-    return with_split(p.states, [&](auto ns, auto lanes) {
+    return with_backward_split(p.states, [&](auto form) {
         return with_flag(cut.whole, [&](auto whole) {
-            constexpr int kNS = decltype(ns)::value, kS = decltype(lanes)::value;
-            const size_t rows = ptq::kScanHistory, np = kNS * kS;
-            const size_t smem = rows * (cut.threads / kS) * 16 + rows * np * 8 + (cut.threads / 32) * rows * np * 8;
-            ptq::ptq_scan_backward_kernel<T, kNS, kS, decltype(whole)::value><<<static_cast<unsigned>(cut.ctas), cut.threads, smem, stream>>>(p);
+            using F = decltype(form);
+            constexpr auto kKern = ptq::ptq_scan_backward_kernel<T, F::channels, F::states, F::lanes, decltype(whole)::value>;
+            constexpr size_t kBytes = ptq::scan_backward_smem(F::channels, F::states, F::lanes);
+            PTQ_TRY(ensure_smem<kKern>(static_cast<int>(kBytes)));
+            kKern<<<static_cast<unsigned>(cut.ctas), ptq::kScanWarps * 32, kBytes, stream>>>(p);
             return launched();
         });
     });
@@ -121,12 +128,12 @@ ptq_status_t ScanLaunch<T>::finish(const ptq::ScanParams &p, float *dA, float *d
 template <typename T>
 ptq_status_t ScanLaunch<T>::step(const ptq::ScanParams &p, bool whole_rows, cudaStream_t stream)
 {
-    return with_split(p.states, [&](auto ns, auto lanes) {
+    return with_step_split(p.states, [&](auto form) {
         return with_flag(whole_rows, [&](auto whole) {
-            constexpr int kNS = decltype(ns)::value, kS = decltype(lanes)::value;
-            const long long blocks = ceil_div(p.channels, 256 / kS);
+            using F = decltype(form);
+            const long long blocks = ceil_div(p.channels, 256 / F::lanes);
             const long long rows = std::min<long long>(p.batch, std::max(1ll, ceil_div(16 * kSms, blocks)));
-            ptq::ptq_scan_step_kernel<T, kNS, kS, decltype(whole)::value><<<static_cast<unsigned>(blocks * rows), 256, 0, stream>>>(p);
+            ptq::ptq_scan_step_kernel<T, F::states, F::lanes, decltype(whole)::value><<<static_cast<unsigned>(blocks * rows), 256, 0, stream>>>(p);
             return launched();
         });
     });
