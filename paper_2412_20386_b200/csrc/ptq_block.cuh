@@ -156,6 +156,45 @@ __device__ __forceinline__ void store_piece(T *p, const float (&f)[kE], int n)
     store_piece<kWhole, T, kE>(p, r, n);
 }
 
+// A piece on its way to shared memory, its 16-byte parts at to[0], to[32], ... (a lane's part of rows of 32, so that no two lanes meet a bank):
+// asynchronous where accesses of 16 bytes are allowed.  The lane that asked for it may read it after staged().
+template <bool kWhole, typename T, int kE>
+__device__ __forceinline__ void stage_piece(uint4 *to, const T *p, int n)
+{
+    static_assert(kE * sizeof(T) % 16 == 0, "whole parts");
+    constexpr int kParts = kE * static_cast<int>(sizeof(T)) / 16, kElems = 16 / static_cast<int>(sizeof(T));
+    if constexpr (kWhole) {
+        const uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(to));
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) {
+            const int bytes = n >= (i + 1) * kElems ? 16 : 0;      // the rest of the 16 is filled with zeros, nothing is read for none
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + 512 * i), "l"(p + i * kElems), "r"(bytes) : "memory");
+        }
+    } else {
+        const Piece<T, kE> r = load_piece<false, T, kE>(p, n);
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) to[32 * i] = make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]);
+    }
+}
+template <typename T, int kE>
+__device__ __forceinline__ Piece<T, kE> staged_piece(const uint4 *from)
+{
+    Piece<T, kE> r;
+#pragma unroll
+    for (int i = 0; i < Piece<T, kE>::kWords / 4; ++i) {
+        const uint4 v = from[32 * i];
+        r.w[4 * i] = v.x;
+        r.w[4 * i + 1] = v.y;
+        r.w[4 * i + 2] = v.z;
+        r.w[4 * i + 3] = v.w;
+    }
+    return r;
+}
+__device__ __forceinline__ void staged()
+{
+    asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
 // kN consecutive floats, of which n exist; kWhole: the address allows accesses of 16 bytes (8, if kN is 2), and n ends between
 // two of them.
 template <bool kWhole, int kN>

@@ -378,10 +378,10 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_kernel(const Scan
 }
 
 // Shared memory of a CTA of the backward pass.
-__host__ __device__ constexpr size_t scan_backward_smem(int channels, int states, int lanes)
+__host__ __device__ constexpr size_t scan_backward_smem(int channels, int states, int lanes, int bytes)
 {
     const size_t width = 32 / lanes * channels, rows = 256 / width, np = static_cast<size_t>(states) * lanes;
-    const size_t warp = rows * (width + 2) * 16 + 2 * rows * np * 4 + 2 * 32 * 8 * 4;
+    const size_t warp = 2 * 4 * 32 * 8 * bytes + rows * (width + 2) * 16 + 2 * rows * np * 4 + 2 * 32 * 8 * 4;
     return kScanWarps * (warp + 2 * rows * 2 * np * 4);
 }
 
@@ -407,20 +407,22 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
     constexpr int kBC = (kRows * kNP + 32 * kPer - 1) / (32 * kPer);
     constexpr int kApart = kBC > 1 ? 32 * kPer / kNP : kRows;
     static_assert(kApart * kBC == kRows && kRows % kStretch == 0, "a fetch goes one tile on, in whole stretches");
-    constexpr bool kEarly = sizeof(T) == 2;               // the next tile's rows are fetched into registers during this one's recurrence
     constexpr int kThreads = kScanWarps * 32;
+    enum { kU, kDelta, kDy, kZ, kTensors };               // what a lane reads of a row
+    constexpr int kParts = sizeof(T) / 2;
     struct Warp {
+        uint4 rows[2][kTensors][kParts][32];              // of this tile and, on their way, of the next one
         float2 pair[kRows * kPitch];                      // (dt, dt u), later (s, r)
         float g[kRows * kPitch], o[kRows * kPitch];       // dyo; o without D u
         float BC[2][kRows * kNP];
-        float sum_D[32][8], sum_bias[32][8];              // of the lane's channels, over its rows
+        float sum_D[8][32], sum_bias[8][32];              // of the lane's channels, over its rows
     };
     extern __shared__ __align__(16) unsigned char scan_smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     Warp &w = reinterpret_cast<Warp *>(scan_smem)[warp];
     float *const s_sum = reinterpret_cast<float *>(scan_smem + kScanWarps * sizeof(Warp));      // [2][kScanWarps][kRows][2][kNP]: dB, dC
     constexpr int kSums = kRows * 2 * kNP;
-    static_assert(kScanWarps * (sizeof(Warp) + 2 * kSums * sizeof(float)) == scan_backward_smem(kC, kNS, kS), "as the launch sizes it");
+    static_assert(kScanWarps * (sizeof(Warp) + 2 * kSums * sizeof(float)) == scan_backward_smem(kC, kNS, kS, sizeof(T)), "as the launch sizes it");
     const ScanBlock blk(p, blockIdx.x, p.group_blocks, p.chunks, 0, kWidth * kScanWarps);
     const bool softplus = p.flags & kScanSoftplus, reverse = p.flags & kScanReverse;
 
@@ -448,23 +450,17 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
     const int row = lane / (kWidth / 8), part8 = lane % (kWidth / 8) * 8, c = blk.c0 + warp * kWidth + part8;
     const int cn = max(min(8, blk.c_end - c), 0);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w.sum_D[lane][i] = w.sum_bias[lane][i] = 0.0f;
-    struct Rows {
-        Piece<T, 8> u, delta, z, dy;
-    };
+    for (int i = 0; i < 8; ++i) w.sum_D[i][lane] = w.sum_bias[i][lane] = 0.0f;
     const long long sequence = static_cast<long long>(blk.b) * p.length;
     const auto token_of = [&](int i) { return static_cast<long long>(reverse && i < blk.len ? blk.len - 1 - i : i); };
-    const auto rows_of = [&](int i0) {
-        Rows r;
+    const auto fetch_rows = [&](int i0, int to) {
         const bool on = i0 + row < blk.i1;
         const long long at = on ? token_of(i0 + row) : 0;
         const int n = on ? cn : 0;
-        r.u = load_piece<kWhole, T, 8>(static_cast<const T *>(p.u) + blk.b * p.u_b + at * p.u_l + c, n);
-        r.delta = load_piece<kWhole, T, 8>(static_cast<const T *>(p.delta) + blk.b * p.delta_b + at * p.delta_l + c, n);
-        r.dy = load_piece<kWhole, T, 8>(static_cast<const T *>(p.dy) + (sequence + at) * p.channels + c, n);
-        r.z.zero();
-        if (p.z) r.z = load_piece<kWhole, T, 8>(static_cast<const T *>(p.z) + blk.b * p.z_b + at * p.z_l + c, n);
-        return r;
+        stage_piece<kWhole, T, 8>(&w.rows[to][kU][0][lane], static_cast<const T *>(p.u) + blk.b * p.u_b + at * p.u_l + c, n);
+        stage_piece<kWhole, T, 8>(&w.rows[to][kDelta][0][lane], static_cast<const T *>(p.delta) + blk.b * p.delta_b + at * p.delta_l + c, n);
+        stage_piece<kWhole, T, 8>(&w.rows[to][kDy][0][lane], static_cast<const T *>(p.dy) + (sequence + at) * p.channels + c, n);
+        if (p.z) stage_piece<kWhole, T, 8>(&w.rows[to][kZ][0][lane], static_cast<const T *>(p.z) + blk.b * p.z_b + at * p.z_l + c, n);
     };
     Piece<T, kPer> r_BC[2][kBC];
     const int bc_t = kPer * lane / kNP, bc_n = kPer * lane % kNP;
@@ -517,10 +513,9 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
     if (out_n < p.states)
         for (int i = max(i0 + kRows, blk.i0) + out_t; i < end; i += kThreads / (2 * kNP)) put_BC(i, 0.0f);
 
-    Rows ahead;
     if (i0 >= blk.i0) {
         fetch(i0);
-        if (kEarly) ahead = rows_of(i0);
+        fetch_rows(i0, 0);
         fetch_state(i0 + (min(kRows, blk.i1 - i0) - 1) / kStretch * kStretch);
     }
     const Piece<float, 8> bias = load_piece<kWhole, float, 8>(p.delta_bias + c, p.delta_bias ? cn : 0);
@@ -528,23 +523,27 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
     float *const own_g = w.g + row * kPitch + part8;
     for (int parity = 0; i0 >= blk.i0; i0 -= kRows, parity ^= 1) {
         const bool row_on = i0 + row < blk.i1;
+        staged();
         {
-            const Rows r = kEarly ? ahead : rows_of(i0);
+            const Piece<T, 8> u = staged_piece<T, 8>(&w.rows[parity][kU][0][lane]), delta = staged_piece<T, 8>(&w.rows[parity][kDelta][0][lane]),
+                              dy = staged_piece<T, 8>(&w.rows[parity][kDy][0][lane]);
+            Piece<T, 8> z;
+            if (p.z) z = staged_piece<T, 8>(&w.rows[parity][kZ][0][lane]);
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
                 float4 f;
-                f.x = r.delta[i] + bias[i];
-                f.z = r.delta[i + 1] + bias[i + 1];
+                f.x = delta[i] + bias[i];
+                f.z = delta[i + 1] + bias[i + 1];
                 if (softplus) {
                     float t0, t1;
                     exp_minus_abs_pair(t0, t1, f.x, f.z);
                     softplus_pair(f.x, f.z, f.x, f.z, t0, t1);
                 }
-                mul_pair(f.y, f.w, r.u[i], r.u[i + 1], f.x, f.z);
-                float2 g = make_float2(r.dy[i], r.dy[i + 1]);
+                mul_pair(f.y, f.w, u[i], u[i + 1], f.x, f.z);
+                float2 g = make_float2(dy[i], dy[i + 1]);
                 if (p.z) {
-                    g.x *= r.z[i] * sigmoid_f32(r.z[i]);
-                    g.y *= r.z[i + 1] * sigmoid_f32(r.z[i + 1]);
+                    g.x *= z[i] * sigmoid_f32(z[i]);
+                    g.y *= z[i + 1] * sigmoid_f32(z[i + 1]);
                 }
                 if (!row_on) {
                     f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -569,7 +568,7 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
         __syncwarp();
         if (i0 > blk.i0) {
             fetch(i0 - kRows);
-            if (kEarly) ahead = rows_of(i0 - kRows);
+            fetch_rows(i0 - kRows, parity ^ 1);
         }
         float *const sums = s_sum + (parity * kScanWarps + warp) * kSums;
         for (int t0 = (min(kRows, blk.i1 - i0) - 1) / kStretch * kStretch; t0 >= 0; t0 -= kStretch) {
@@ -687,12 +686,17 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
         }
         __syncthreads();                                   // the warps' sums of dB and dC; the next tile's go to the other half
         if (i0 + row < end) {
-            const Rows r = rows_of(i0);                    // once more, from the cache: held in registers they would cost occupancy
+            const Piece<T, 8> u = staged_piece<T, 8>(&w.rows[parity][kU][0][lane]), delta = staged_piece<T, 8>(&w.rows[parity][kDelta][0][lane]);
+            Piece<T, 8> z, dy;
+            if (p.z) {
+                z = staged_piece<T, 8>(&w.rows[parity][kZ][0][lane]);
+                dy = staged_piece<T, 8>(&w.rows[parity][kDy][0][lane]);
+            }
             const Piece<float, 8> skip = load_piece<kWhole, float, 8>(p.D + c, p.D ? cn : 0);
             float du[8], dd[8], dz[8];
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
-                const float x0 = r.delta[i] + bias[i], x1 = r.delta[i + 1] + bias[i + 1];
+                const float x0 = delta[i] + bias[i], x1 = delta[i + 1] + bias[i + 1];
                 float dt[2] = {x0, x1}, slope[2] = {1.0f, 1.0f};
                 if (softplus) {
                     float t0, t1;
@@ -702,23 +706,24 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
                     slope[1] = __fdividef(x1 < 0.0f ? t1 : 1.0f, 1.0f + t1);
                 }
                 const float4 f = own[i / 2];
+                const float2 gs = *reinterpret_cast<const float2 *>(own_g + i), os = *reinterpret_cast<const float2 *>(w.o + row * kPitch + part8 + i);
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const float s = k ? f.z : f.x, q = k ? f.w : f.y, u = r.u[i + k], dyo = own_g[i + k];
+                    const float s = k ? f.z : f.x, q = k ? f.w : f.y, uu = u[i + k], dyo = k ? gs.y : gs.x;
                     du[i + k] = dt[k] * s;
                     if (p.D) du[i + k] = fmaf(skip[i + k], dyo, du[i + k]);
-                    dd[i + k] = fmaf(u, s, q * kLn2) * slope[k];
+                    dd[i + k] = fmaf(uu, s, q * kLn2) * slope[k];
                     dz[i + k] = 0.0f;
                     if (p.z) {
-                        float o = w.o[row * kPitch + part8 + i + k];
-                        if (p.D) o = fmaf(skip[i + k], u, o);
-                        const float z = r.z[i + k], gate = sigmoid_f32(z);
-                        dz[i + k] = r.dy[i + k] * o * gate * fmaf(z, 1.0f - gate, 1.0f);
+                        float o = k ? os.y : os.x;
+                        if (p.D) o = fmaf(skip[i + k], uu, o);
+                        const float zz = z[i + k], gate = sigmoid_f32(zz);
+                        dz[i + k] = dy[i + k] * o * gate * fmaf(zz, 1.0f - gate, 1.0f);
                     }
                     if (!row_on) du[i + k] = dd[i + k] = dz[i + k] = 0.0f;
                     if (row_on) {
-                        w.sum_D[lane][i + k] = fmaf(u, dyo, w.sum_D[lane][i + k]);
-                        w.sum_bias[lane][i + k] += dd[i + k];
+                        w.sum_D[i + k][lane] = fmaf(uu, dyo, w.sum_D[i + k][lane]);
+                        w.sum_bias[i + k][lane] += dd[i + k];
                     }
                 }
             }
@@ -752,8 +757,8 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
         float a = 0.0f, b = 0.0f;
 #pragma unroll 8
         for (int r = 0; r < kRows; ++r) {
-            a += w.sum_D[r * (kWidth / 8) + i / 8][i % 8];
-            b += w.sum_bias[r * (kWidth / 8) + i / 8][i % 8];
+            a += w.sum_D[i % 8][r * (kWidth / 8) + i / 8];
+            b += w.sum_bias[i % 8][r * (kWidth / 8) + i / 8];
         }
         p.part_D[part * p.channels + blk.c0 + warp * kWidth + i] = a;
         p.part_bias[part * p.channels + blk.c0 + warp * kWidth + i] = b;

@@ -108,7 +108,7 @@ ptq_status_t ScanLaunch<T>::backward(const ptq::ScanParams &p, const ScanCut &cu
         return with_flag(cut.whole, [&](auto whole) {
             using F = decltype(form);
             constexpr auto kKern = ptq::ptq_scan_backward_kernel<T, F::channels, F::states, F::lanes, decltype(whole)::value>;
-            constexpr size_t kBytes = ptq::scan_backward_smem(F::channels, F::states, F::lanes);
+            constexpr size_t kBytes = ptq::scan_backward_smem(F::channels, F::states, F::lanes, sizeof(T));
             PTQ_TRY(ensure_smem<kKern>(static_cast<int>(kBytes)));
             kKern<<<static_cast<unsigned>(cut.ctas), ptq::kScanWarps * 32, kBytes, stream>>>(p);
             return launched();
