@@ -237,21 +237,24 @@ ptq::NormParams norm_params(const ptq_norm_t &n)
 bool norm_whole(const ptq_norm_t &n)
 {
     const int unit = 16 / elem_bytes(n.dtype), residual_unit = 16 / elem_bytes(n.residual_dtype);
-    return aligned({n.x, n.residual, n.gate}, 16) && multiples({n.x_pitch, n.gate ? n.gate_pitch : 0, n.cols}, unit) &&
+    return aligned({n.x, n.residual, n.gate, n.weight, n.bias, n.scale}, 16) && multiples({n.x_pitch, n.gate ? n.gate_pitch : 0, n.cols}, unit) &&
            (!n.residual || n.residual_pitch % residual_unit == 0);
 }
-// Rows that a CTA takes at a time, and CTAs.
+// Threads of a CTA, rows that it takes at a time, sets of rows and bytes of shared memory, CTAs.
 struct NormPlan {
-    int threads, rows, ctas;
+    int threads, rows, stages, bytes, ctas;
 };
 NormPlan norm_plan(const ptq_norm_t &n, bool backward)
 {
     NormPlan p;
     p.threads = static_cast<int>(ceil_div(n.cols, 256)) * 32;
-    const int batch = backward ? 2 : 4;
-    p.rows = p.threads > 256 || n.rows <= 8 * kSms ? 1 : batch;
-    const long long resident = std::max(1, std::min(32, (backward ? 512 : 768) / p.threads)) * static_cast<long long>(kSms);
-    p.ctas = static_cast<int>(std::min(ceil_div(n.rows, p.rows), resident));
+    p.rows = p.threads > 256 || n.rows <= 8 * kSms ? 1 : backward ? 2 : 4;
+    const ptq::NormStage stage(n.residual, n.gate, backward, backward && n.residual, elem_bytes(n.dtype) / 2, elem_bytes(n.residual_dtype) / 2, p.rows,
+                               p.threads);
+    p.stages = 2 * 16 * stage.size <= 200 * 1024 ? 2 : 1;
+    p.bytes = p.stages * 16 * stage.size;
+    const int resident = std::max(1, std::min((backward ? 640 : 1024) / p.threads, 220 * 1024 / (p.bytes + 8 * 1024)));
+    p.ctas = static_cast<int>(std::min<long long>(ceil_div(n.rows, p.rows), std::min(resident, 24) * kSms));
     return p;
 }
 template <bool kBackward>
@@ -264,11 +267,16 @@ ptq_status_t launch_norm(const ptq_norm_t &n, const NormPlan &plan, const ptq::N
             return with_flag(whole_rows, [&](auto whole) {
                 constexpr int kRB = kBackward ? 2 : 4;
                 constexpr bool kWhole = decltype(whole)::value;
-                if (plan.rows > 1)
-                    ptq::ptq_norm_kernel<T, R, kRB, kBackward, kWhole><<<plan.ctas, plan.threads, 0, stream>>>(p);
-                else
-                    ptq::ptq_norm_kernel<T, R, 1, kBackward, kWhole><<<plan.ctas, plan.threads, 0, stream>>>(p);
-                return launched();
+                const auto launch = [&](auto kern) {
+                    constexpr auto kKern = decltype(kern)::value;
+                    PTQ_TRY(ensure_smem<kKern>(200 * 1024));
+                    kKern<<<plan.ctas, plan.threads, plan.bytes, stream>>>(p);
+                    return launched();
+                };
+                using Kern = void (*)(const ptq::NormParams);
+                if (plan.threads > 256) return launch(std::integral_constant<Kern, ptq::ptq_norm_kernel<T, R, 1, true, kBackward, kWhole>>());
+                if (plan.rows > 1) return launch(std::integral_constant<Kern, ptq::ptq_norm_kernel<T, R, kRB, false, kBackward, kWhole>>());
+                return launch(std::integral_constant<Kern, ptq::ptq_norm_kernel<T, R, 1, false, kBackward, kWhole>>());
             });
         };
         return n.residual_dtype == n.dtype ? go(T()) : go(0.0f);
@@ -419,7 +427,9 @@ ptq_status_t ptq_norm_forward(const ptq_norm_t *n, void *y, void *residual_out, 
     ptq::NormParams p = norm_params(*n);
     p.y = y;
     p.residual_out = residual_out;
-    return launch_norm<false>(*n, norm_plan(*n, false), p, norm_whole(*n) && aligned({y, residual_out}, 16), static_cast<cudaStream_t>(stream));
+    const NormPlan plan = norm_plan(*n, false);
+    p.stages = plan.stages;
+    return launch_norm<false>(*n, plan, p, norm_whole(*n) && aligned({y, residual_out}, 16), static_cast<cudaStream_t>(stream));
 }
 
 size_t ptq_norm_workspace_bytes(const ptq_norm_t *n)
@@ -448,9 +458,10 @@ ptq_status_t ptq_norm_backward(const ptq_norm_t *n, const void *dy, const void *
     p.part = static_cast<float *>(workspace);
     const NormPlan plan = norm_plan(*n, true);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    p.stages = plan.stages;
     PTQ_TRY(launch_norm<true>(*n, plan, p, norm_whole(*n) && aligned({dy, dresidual_out, g->dx, g->dresidual, g->dgate}, 16), st));
     if (!g->dweight && !g->dbias && !g->dscale) return PTQ_OK;
-    ptq::ptq_norm_finish_kernel<<<dim3(static_cast<unsigned>(ceil_div(n->cols, 32)), 3), 256, 0, st>>>(p.part, plan.ctas, n->cols, g->dweight, g->dbias,
+    ptq::ptq_norm_finish_kernel<<<dim3(static_cast<unsigned>(ceil_div(n->cols, 32)), 3), 1024, 0, st>>>(p.part, plan.ctas, n->cols, g->dweight, g->dbias,
                                                                                                    g->dscale);
     return launched();
 }
@@ -514,7 +525,7 @@ ptq_status_t ptq_conv_backward(const ptq_conv_t *c, const void *dy, const void *
             });
         });
     }));
-    ptq::ptq_conv_finish_kernel<<<dim3(static_cast<unsigned>(ceil_div(c->channels, 32)), static_cast<unsigned>(c->taps + 1)), 256, 0, st>>>(
+    ptq::ptq_conv_finish_kernel<<<dim3(static_cast<unsigned>(ceil_div(c->channels, 32)), static_cast<unsigned>(c->taps + 1)), 1024, 0, st>>>(
         p.part, rows, c->channels, c->taps, g->dweight, g->dbias);
     return launched();
 }

@@ -156,10 +156,10 @@ __device__ __forceinline__ void store_piece(T *p, const float (&f)[kE], int n)
     store_piece<kWhole, T, kE>(p, r, n);
 }
 
-// A piece on its way to shared memory, its 16-byte parts at to[0], to[32], ... (a lane's part of rows of 32, so that no two lanes meet a bank):
-// asynchronous where accesses of 16 bytes are allowed.  The lane that asked for it may read it after staged().
+// A piece on its way to shared memory, its 16-byte parts at to[0], to[apart], ... (one thread's of a row of threads, so that no two of them
+// meet a bank): asynchronous where accesses of 16 bytes are allowed.  The thread that asked for it may read it after staged().
 template <bool kWhole, typename T, int kE>
-__device__ __forceinline__ void stage_piece(uint4 *to, const T *p, int n)
+__device__ __forceinline__ void stage_piece(uint4 *to, const T *p, int n, int apart = 32)
 {
     static_assert(kE * sizeof(T) % 16 == 0, "whole parts");
     constexpr int kParts = kE * static_cast<int>(sizeof(T)) / 16, kElems = 16 / static_cast<int>(sizeof(T));
@@ -168,21 +168,21 @@ __device__ __forceinline__ void stage_piece(uint4 *to, const T *p, int n)
 #pragma unroll
         for (int i = 0; i < kParts; ++i) {
             const int bytes = n >= (i + 1) * kElems ? 16 : 0;      // the rest of the 16 is filled with zeros, nothing is read for none
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + 512 * i), "l"(p + i * kElems), "r"(bytes) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + 16 * apart * i), "l"(p + i * kElems), "r"(bytes) : "memory");
         }
     } else {
         const Piece<T, kE> r = load_piece<false, T, kE>(p, n);
 #pragma unroll
-        for (int i = 0; i < kParts; ++i) to[32 * i] = make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]);
+        for (int i = 0; i < kParts; ++i) to[apart * i] = make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]);
     }
 }
 template <typename T, int kE>
-__device__ __forceinline__ Piece<T, kE> staged_piece(const uint4 *from)
+__device__ __forceinline__ Piece<T, kE> staged_piece(const uint4 *from, int apart = 32)
 {
     Piece<T, kE> r;
 #pragma unroll
     for (int i = 0; i < Piece<T, kE>::kWords / 4; ++i) {
-        const uint4 v = from[32 * i];
+        const uint4 v = from[apart * i];
         r.w[4 * i] = v.x;
         r.w[4 * i + 1] = v.y;
         r.w[4 * i + 2] = v.z;
@@ -190,9 +190,13 @@ __device__ __forceinline__ Piece<T, kE> staged_piece(const uint4 *from)
     }
     return r;
 }
-__device__ __forceinline__ void staged()
+__device__ __forceinline__ void staged() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// Copies in groups: staged_but<n>() waits for all groups but the last n.
+__device__ __forceinline__ void stage_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kGroups>
+__device__ __forceinline__ void staged_but()
 {
-    asm volatile("cp.async.wait_all;" ::: "memory");
+    asm volatile("cp.async.wait_group %0;" ::"n"(kGroups) : "memory");
 }
 
 // kN consecutive floats, of which n exist; kWhole: the address allows accesses of 16 bytes (8, if kN is 2), and n ends between
@@ -336,6 +340,26 @@ __device__ __forceinline__ int first_sum(int lane)
         return ((lane & kLow) ? kV / 2 : 0) + first_sum<kV / 2, kLow * 2, kHigh>(lane);
     else
         return 0;
+}
+
+// Column sums of the partial results of other CTAs, in the order of the rows: the sum of part[r * pitch] for r < rows.  Called by all of
+// a CTA of 32 x 32 threads, one column per lane (`on`: it has one), every 32nd row per warp; the result is the first warp's.
+__device__ __forceinline__ float sum_rows(const float *part, long long rows, long long pitch, bool on, float (&s)[32][33])
+{
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    float v = 0.0f;
+    if (on) {
+#pragma unroll 8
+        for (long long r = y; r < rows; r += 32) v += part[r * pitch];
+    }
+    s[y][x] = v;
+    __syncthreads();
+    v = 0.0f;
+    if (y == 0) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v += s[i][x];
+    }
+    return v;
 }
 
 }  // namespace ptq

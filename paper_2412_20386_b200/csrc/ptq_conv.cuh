@@ -222,27 +222,18 @@ __global__ void __launch_bounds__(256) ptq_conv_backward_kernel(const ConvParams
     }
 }
 
-// Sums of the CTAs' shares, in their order: part[rows][W + 1][cols] -> dweight [cols][W], dbias [cols].
-__global__ void __launch_bounds__(256) ptq_conv_finish_kernel(const float *part, int rows, int cols, int taps, float *dweight, float *dbias)
+// Sums of the CTAs' shares: part[rows][W + 1][cols] -> dweight [cols][W], dbias [cols].
+__global__ void __launch_bounds__(1024) ptq_conv_finish_kernel(const float *part, int rows, int cols, int taps, float *dweight, float *dbias)
 {
-    __shared__ float s[8][33];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, col = blockIdx.x * 32 + x, j = blockIdx.y;
+    __shared__ float s[32][33];
+    const int col = blockIdx.x * 32 + (threadIdx.x & 31), j = blockIdx.y;
     if (j == taps && !dbias) return;
-    float v = 0.0f;
-    if (col < cols) {
-#pragma unroll 8
-        for (int r = y; r < rows; r += 8) v += part[(static_cast<long long>(r) * (taps + 1) + j) * cols + col];
-    }
-    s[y][x] = v;
-    __syncthreads();
-    if (y == 0 && col < cols) {
-#pragma unroll
-        for (int i = 1; i < 8; ++i) v += s[i][x];
-        if (j < taps)
-            dweight[static_cast<long long>(col) * taps + j] = v;
-        else
-            dbias[col] = v;
-    }
+    const float v = sum_rows(part + static_cast<long long>(j) * cols + col, rows, static_cast<long long>(taps + 1) * cols, col < cols, s);
+    if (threadIdx.x >= 32 || col >= cols) return;
+    if (j < taps)
+        dweight[static_cast<long long>(col) * taps + j] = v;
+    else
+        dbias[col] = v;
 }
 
 }  // namespace ptq

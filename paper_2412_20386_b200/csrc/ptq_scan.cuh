@@ -765,49 +765,32 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
     }
 }
 
-// Column sums of the partial results, one output after another: part[rows][cols] -> out[cols].  A CTA takes 32 columns, its
-// eight warps every eighth row each.
-__device__ __forceinline__ void sum_rows(const float *part, float *out, long long rows, long long cols, long long first, float (&s)[8][33])
-{
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const long long col = first + x;
-    float v = 0.0f;
-    if (col < cols) {
-#pragma unroll 8
-        for (long long r = y; r < rows; r += 8) v += part[r * cols + col];
-    }
-    s[y][x] = v;
-    __syncthreads();
-    if (y == 0 && col < cols) {
-#pragma unroll
-        for (int i = 1; i < 8; ++i) v += s[i][x];
-        out[col] = v;
-    }
-}
-
+// The shares of the CTAs of the backward pass: dA, dD and ddelta_bias over the sequences and chunks, dB and dC over the CTAs of a group.
+constexpr int kScanFinishThreads = 1024;
 template <typename T>
-__global__ void __launch_bounds__(256) ptq_scan_finish_kernel(const ScanParams p, float *dA, float *dD, float *dbias, int blocks_A, int blocks_D)
+__global__ void __launch_bounds__(kScanFinishThreads) ptq_scan_finish_kernel(const ScanParams p, float *dA, float *dD, float *dbias, int blocks_A, int blocks_D)
 {
-    __shared__ float s[8][33];
+    __shared__ float s[32][33];
     const long long rows = static_cast<long long>(p.batch) * p.chunks;
     int block = blockIdx.x;
-    if (block < blocks_A) {
-        sum_rows(p.part_A, dA, rows, static_cast<long long>(p.channels) * p.states, block * 32ll, s);
+    if (block < blocks_A + 2 * blocks_D) {
+        const bool is_A = block < blocks_A, is_D = block < blocks_A + blocks_D;
+        float *out = is_A ? dA : is_D ? dD : dbias;
+        if (!out) return;
+        const long long cols = is_A ? static_cast<long long>(p.channels) * p.states : p.channels;
+        const long long col = (is_A ? block : (block - blocks_A) % blocks_D) * 32ll + (threadIdx.x & 31);
+        const float v = sum_rows((is_A ? p.part_A : is_D ? p.part_D : p.part_bias) + col, rows, cols, col < cols, s);
+        if (threadIdx.x < 32 && col < cols) out[col] = v;
         return;
     }
-    block -= blocks_A;
-    if (block < 2 * blocks_D) {
-        float *out = block < blocks_D ? dD : dbias;
-        if (out) sum_rows(block < blocks_D ? p.part_D : p.part_bias, out, rows, p.channels, block % blocks_D * 32ll, s);
-        return;
-    }
-    // dB and dC: the shares of the CTAs of a group
+    block -= blocks_A + 2 * blocks_D;
     const long long per = static_cast<long long>(p.batch) * p.length * 2 * p.states;
-    const long long total = per * p.groups, stride = static_cast<long long>(gridDim.x - blocks_A - 2 * blocks_D) * 256;
-    for (long long idx = (block - 2 * blocks_D) * 256ll + threadIdx.x; idx < total; idx += stride) {
+    const long long total = per * p.groups, stride = static_cast<long long>(gridDim.x - blocks_A - 2 * blocks_D) * kScanFinishThreads;
+    for (long long idx = block * static_cast<long long>(kScanFinishThreads) + threadIdx.x; idx < total; idx += stride) {
         const long long g = idx / per, rest = idx - g * per, tok = rest / (2 * p.states);
         const int q = static_cast<int>(rest - tok * (2 * p.states));
         float v = 0.0f;
+#pragma unroll 4
         for (int j = 0; j < p.group_blocks; ++j) v += p.part_BC[(g * p.group_blocks + j) * per + rest];
         const long long at = (tok * p.groups + g) * p.states + (q >= p.states ? q - p.states : q);
         static_cast<T *>(q >= p.states ? p.dC : p.dB)[at] = from_f32<T>(v);
