@@ -297,8 +297,7 @@ ptq_status_t conv_check(const ptq_conv_t *c)
         return fail(PTQ_ERR_ALIGN, "an input is not aligned to its type");
     return PTQ_OK;
 }
-constexpr int kConvE = 8, kConvBackE = 4;      // channels of a thread, forward and backward
-ptq::ConvParams conv_params(const ptq_conv_t &c, int e, long long wanted_threads)
+ptq::ConvParams conv_params(const ptq_conv_t &c, long long segments)
 {
     ptq::ConvParams p = {};
     p.x = c.x;
@@ -312,22 +311,45 @@ ptq::ConvParams conv_params(const ptq_conv_t &c, int e, long long wanted_threads
     p.length = c.length;
     p.channels = c.channels;
     p.flags = c.flags;
-    p.pieces = static_cast<int>(ceil_div(c.channels, e));
-    // segments of 8 to 64 steps: long ones read the rows in front of them seldom, short ones make enough threads
-    int seg = 64;
-    while (seg > 8 && static_cast<long long>(c.batch) * p.pieces * ceil_div(c.length, seg) < wanted_threads) seg /= 2;
-    p.segment = seg;
-    p.segments = static_cast<int>(ceil_div(c.length, seg));
+    p.pieces = static_cast<int>(ceil_div(c.channels, ptq::kConvE));
+    p.segment = static_cast<int>(std::max<long long>(ceil_div(c.length, segments), 4));      // no shorter than the taps
+    p.segments = static_cast<int>(ceil_div(c.length, p.segment));
     return p;
+}
+// Forward: segments until the GPU has about 96 thousand threads, but of 8 steps at least (each reads taps - 1 rows again).
+ptq::ConvParams conv_forward_params(const ptq_conv_t &c)
+{
+    const long long threads = static_cast<long long>(c.batch) * ceil_div(c.channels, ptq::kConvE);
+    return conv_params(c, std::max(1ll, std::min(ceil_div(kSms * 640, threads), ceil_div(c.length, 8))));
+}
+// Backward: one wave of CTAs of eight warps, two to an SM, that go over the segments; as many segments as make the longest walk of a warp
+// shortest (a segment costs its steps and about 10 more for its start).
+struct ConvBackPlan {
+    ptq::ConvParams p;
+    int blocks, rows;
+};
+ConvBackPlan conv_back_plan(const ptq_conv_t &c)
+{
+    ConvBackPlan plan;
+    plan.blocks = static_cast<int>(ceil_div(ceil_div(c.channels, ptq::kConvE), 32));
+    const long long rows = std::max(1, 2 * kSms / plan.blocks), warps = rows * 8;
+    long long best = 1, least = -1;
+    for (long long n = 1; n <= 256 && (n == 1 || c.length / n >= 8); ++n) {
+        const long long cost = ceil_div(c.batch * n, warps) * (ceil_div(c.length, n) + 10);
+        if (least < 0 || cost < least) {
+            least = cost;
+            best = n;
+        }
+    }
+    plan.p = conv_params(c, best);
+    plan.rows = static_cast<int>(std::min(rows, ceil_div(static_cast<long long>(c.batch) * plan.p.segments, 8)));
+    return plan;
 }
 bool conv_whole(const ptq_conv_t &c)
 {
-    return aligned({c.x, c.state}, 16) && multiples({c.x_pitch[0], c.x_pitch[1], c.channels}, 16 / elem_bytes(c.dtype));
-}
-int conv_back_rows(const ptq_conv_t &c, const ptq::ConvParams &p)
-{
-    const long long blocks = ceil_div(p.pieces, 32), rows = ceil_div(static_cast<long long>(c.batch) * p.segments, 8);
-    return static_cast<int>(std::min(rows, std::max(1ll, ceil_div(2 * kSms, blocks))));
+    // a piece has kConvE channels: 8 bytes of 16-bit values, 16 of binary32 ones
+    return aligned({c.x, c.state}, ptq::kConvE * elem_bytes(c.dtype)) && aligned({c.weight, c.bias}, 16) &&
+           multiples({c.x_pitch[0], c.x_pitch[1], c.channels}, ptq::kConvE);
 }
 template <class Fn>
 ptq_status_t with_taps(int taps, Fn fn)
@@ -471,7 +493,7 @@ ptq_status_t ptq_conv_forward(const ptq_conv_t *c, void *y, void *final_state, v
     PTQ_TRY(conv_check(c));
     if (!y) return fail(PTQ_ERR_NULL, "y is NULL");
     if (!aligned({y, final_state}, elem_bytes(c->dtype))) return fail(PTQ_ERR_ALIGN, "an output is not aligned to its type");
-    ptq::ConvParams p = conv_params(*c, kConvE, kSms * 512ll);
+    ptq::ConvParams p = conv_forward_params(*c);
     p.y = y;
     p.final_state = final_state;
     const long long ctas = ceil_div(static_cast<long long>(c->batch) * p.segments * p.pieces, 256);
@@ -480,8 +502,8 @@ ptq_status_t ptq_conv_forward(const ptq_conv_t *c, void *y, void *final_state, v
     return with_type(c->dtype, [&](auto t) {
         using T = decltype(t);
         return with_taps(c->taps, [&](auto w) {
-            return with_flag(conv_whole(*c) && aligned({y, final_state}, 16), [&](auto whole) {
-                ptq::ptq_conv_kernel<T, kConvE, decltype(w)::value, decltype(whole)::value>
+            return with_flag(conv_whole(*c) && aligned({y, final_state}, ptq::kConvE * elem_bytes(c->dtype)), [&](auto whole) {
+                ptq::ptq_conv_kernel<T, decltype(w)::value, decltype(whole)::value>
                     <<<static_cast<unsigned>(ctas), 256, 0, static_cast<cudaStream_t>(stream)>>>(p);
                 return launched();
             });
@@ -494,8 +516,7 @@ size_t ptq_conv_workspace_bytes(const ptq_conv_t *c)
     if (!c || c->batch < 1 || c->length < 1 || c->length > PTQ_MAX_LENGTH || c->channels < 1 || c->channels > PTQ_MAX_CHANNELS || c->taps < 2 ||
         c->taps > 4)
         return 0;
-    const ptq::ConvParams p = conv_params(*c, kConvBackE, kSms * 512ll);
-    return padded(static_cast<size_t>(conv_back_rows(*c, p)) * (c->taps + 1) * c->channels * 4);
+    return padded(static_cast<size_t>(conv_back_plan(*c).rows) * (c->taps + 1) * c->channels * 4);
 }
 
 ptq_status_t ptq_conv_backward(const ptq_conv_t *c, const void *dy, const void *dfinal, const ptq_conv_grads_t *g, void *workspace,
@@ -507,20 +528,21 @@ ptq_status_t ptq_conv_backward(const ptq_conv_t *c, const void *dy, const void *
         return fail(PTQ_ERR_ALIGN, "an argument is not aligned to its type");
     PTQ_TRY(check_space(workspace, workspace_bytes, ptq_conv_workspace_bytes(c)));
     PTQ_TRY(check_arch());
-    ptq::ConvParams p = conv_params(*c, kConvBackE, kSms * 512ll);
+    const ConvBackPlan plan = conv_back_plan(*c);
+    ptq::ConvParams p = plan.p;
     p.dy = dy;
     p.dfinal = dfinal;
     p.dx = g->dx;
     p.dstate = g->dstate;
     p.part = static_cast<float *>(workspace);
-    const int rows = conv_back_rows(*c, p);
-    const dim3 grid(static_cast<unsigned>(ceil_div(p.pieces, 32)), static_cast<unsigned>(rows));
+    const int rows = plan.rows;
+    const dim3 grid(static_cast<unsigned>(plan.blocks), static_cast<unsigned>(rows));
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     PTQ_TRY(with_type(c->dtype, [&](auto t) {
         using T = decltype(t);
         return with_taps(c->taps, [&](auto w) {
-            return with_flag(conv_whole(*c) && aligned({dy, dfinal, g->dx, g->dstate}, 16), [&](auto whole) {
-                ptq::ptq_conv_backward_kernel<T, kConvBackE, decltype(w)::value, decltype(whole)::value><<<grid, 256, 0, st>>>(p);
+            return with_flag(conv_whole(*c) && aligned({dy, dfinal, g->dx, g->dstate}, ptq::kConvE * elem_bytes(c->dtype)), [&](auto whole) {
+                ptq::ptq_conv_backward_kernel<T, decltype(w)::value, decltype(whole)::value><<<grid, 256, 0, st>>>(p);
                 return launched();
             });
         });

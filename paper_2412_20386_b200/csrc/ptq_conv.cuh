@@ -32,52 +32,88 @@ template <typename T, int kE, int kW, bool kWhole>
 struct ConvRow {
     const ConvParams &p;
     int b, c, cn, len;
+    long long way;                    // tokens between two steps of the sequence
+    const T *first;                   // the token of step 0
     __device__ __forceinline__ ConvRow(const ConvParams &q, int b_, int piece) : p(q), b(b_), c(piece * kE)
     {
         cn = max(min(kE, p.channels - c), 0);
         len = p.lengths ? min(max(p.lengths[b], 0), p.length) : p.length;
+        const bool reverse = p.flags & kConvReverse;
+        way = reverse ? -1 : 1;
+        first = static_cast<const T *>(p.x) + b * p.x_b + (reverse ? len - 1ll : 0ll) * p.x_l + c;
     }
     __device__ __forceinline__ long long token(int i) const { return (p.flags & kConvReverse) && i < len ? len - 1 - i : i; }
-    // row i of the sequence with its state in front: i from -(W-1) on; zeros behind the end
+    // step i of the sequence with its state in front: i from -(W-1) on; zeros behind the end
     __device__ __forceinline__ Piece<T, kE> input(int i) const
     {
         if (i < 0)
             return load_piece<kWhole, T, kE>(static_cast<const T *>(p.state) + (static_cast<long long>(b) * (kW - 1) + (i + kW - 1)) * p.channels + c,
-                                     p.state ? cn : 0);
-        return load_piece<kWhole, T, kE>(static_cast<const T *>(p.x) + b * p.x_b + token(min(i, p.length - 1)) * p.x_l + c, i < len ? cn : 0);
+                                             p.state ? cn : 0);
+        return step(i);
     }
+    __device__ __forceinline__ Piece<T, kE> step(int i) const { return load_piece<kWhole, T, kE>(first + way * i * p.x_l, i < len ? cn : 0); }
     __device__ __forceinline__ long long dense(int i) const { return (static_cast<long long>(b) * p.length + token(i)) * p.channels + c; }
 };
 
-template <typename T, int kE, int kW>
+// Weights and bias of a thread's channels.
+template <int kE, int kW, bool kWhole>
 __device__ __forceinline__ void conv_weights(const ConvParams &p, int c, int cn, float (&w)[kW][kE], float (&bias)[kE])
 {
+    float f[kE * kW];                 // the channels' weights lie one behind the other
+    const Piece<float, kE> b = load_piece<kWhole, float, kE>(p.bias + c, p.bias ? cn : 0);
+    const Piece<float, kE * kW> all = load_piece<kWhole, float, kE * kW>(p.weight + static_cast<long long>(c) * kW, cn * kW);
+#pragma unroll
+    for (int i = 0; i < kE * kW; ++i) f[i] = all[i];
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
 #pragma unroll
-        for (int j = 0; j < kW; ++j) w[j][e] = e < cn ? __ldg(p.weight + static_cast<long long>(c + e) * kW + j) : 0.0f;
-        bias[e] = p.bias && e < cn ? __ldg(p.bias + c + e) : 0.0f;
+        for (int j = 0; j < kW; ++j) w[j][e] = f[e * kW + j];
+        bias[e] = b[e];
     }
 }
 
-template <typename T, int kE, int kW, bool kWhole>
+// pre of the newest row of the window
+template <int kE, int kW>
+__device__ __forceinline__ void conv_row(float (&v)[kE], const float (&w)[kW][kE], const float (&x)[kW][kE], const float (&bias)[kE])
+{
+#pragma unroll
+    for (int e = 0; e < kE; ++e) v[e] = bias[e];
+#pragma unroll
+    for (int j = 0; j < kW; ++j) fma_each<kE>(v, w[j], x[j], v);
+}
+template <int kE, int kW>
+__device__ __forceinline__ void conv_shift(float (&x)[kW][kE])
+{
+#pragma unroll
+    for (int j = 0; j < kW - 1; ++j)
+#pragma unroll
+        for (int e = 0; e < kE; ++e) x[j][e] = x[j + 1][e];
+}
+
+constexpr int kConvE = 4;             // channels of a thread: with eight, weights and window leave too few warps
+constexpr int kConvAhead = 4;         // rows that are loaded together, one set under way while the other is worked on
+
+template <typename T, int kW, bool kWhole>
 __global__ void __launch_bounds__(256) ptq_conv_kernel(const ConvParams p)
 {
-    constexpr int kAhead = 4;
+    constexpr int kE = kConvE;
     const long long idx = blockIdx.x * 256ll + threadIdx.x;
     const long long row = idx / p.pieces;
     if (row >= static_cast<long long>(p.batch) * p.segments) return;
     const int seg = static_cast<int>(row % p.segments);
     const ConvRow<T, kE, kW, kWhole> in(p, static_cast<int>(row / p.segments), static_cast<int>(idx - row * p.pieces));
-    float w[kW][kE], bias[kE], x[kW][kE];
-    conv_weights<T, kE, kW>(p, in.c, in.cn, w, bias);
     const int i0 = seg * p.segment, i1 = min(i0 + p.segment, in.len);
+    Piece<T, kE> before[kW - 1], next[kConvAhead];
 #pragma unroll
-    for (int j = 0; j < kW - 1; ++j) {
-        const Piece<T, kE> v = in.input(i0 - (kW - 1) + j);
+    for (int j = 0; j < kW - 1; ++j) before[j] = in.input(i0 - (kW - 1) + j);
 #pragma unroll
-        for (int e = 0; e < kE; ++e) x[j][e] = v[e];
-    }
+    for (int a = 0; a < kConvAhead; ++a) next[a] = in.step(i0 + a);
+    float w[kW][kE], bias[kE], x[kW][kE];
+    conv_weights<kE, kW, kWhole>(p, in.c, in.cn, w, bias);
+#pragma unroll
+    for (int j = 0; j < kW - 1; ++j)
+#pragma unroll
+        for (int e = 0; e < kE; ++e) x[j][e] = before[j][e];
     // the thread that reads the state replaces it: the two may be one buffer
     if (seg == 0 && p.final_state) {
         T *out = static_cast<T *>(p.final_state) + static_cast<long long>(in.b) * (kW - 1) * p.channels + in.c;
@@ -85,31 +121,30 @@ __global__ void __launch_bounds__(256) ptq_conv_kernel(const ConvParams p)
 #pragma unroll
         for (int j = 0; j < kW - 1; ++j) last[j] = in.input(in.len - (kW - 1) + j);
 #pragma unroll
-        for (int j = 0; j < kW - 1; ++j) {
-            float f[kE];
-#pragma unroll
-            for (int e = 0; e < kE; ++e) f[e] = last[j][e];
-            store_piece<kWhole, T, kE>(out + static_cast<long long>(j) * p.channels, f, in.cn);
-        }
+        for (int j = 0; j < kW - 1; ++j) store_piece<kWhole, T, kE>(out + static_cast<long long>(j) * p.channels, last[j], in.cn);
     }
-    for (int i = i0; i < i1; i += kAhead) {
-        Piece<T, kE> next[kAhead];
+    T *y = static_cast<T *>(p.y) + in.dense(i0);
+    const long long y_step = in.way * p.channels;
+    for (int i = i0; i < i1; i += kConvAhead) {
+        Piece<T, kE> now[kConvAhead];
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) next[a] = in.input(min(i + a, i1 - 1));
+        for (int a = 0; a < kConvAhead; ++a) {
+            now[a] = next[a];
+            next[a] = in.step(i + kConvAhead + a);
+        }
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            float y[kE];
+        for (int a = 0; a < kConvAhead; ++a) {
+            float v[kE];
 #pragma unroll
-            for (int e = 0; e < kE; ++e) {
-                x[kW - 1][e] = next[a][e];
-                float v = bias[e];
+            for (int e = 0; e < kE; ++e) x[kW - 1][e] = now[a][e];
+            conv_row<kE, kW>(v, w, x, bias);
+            if (p.flags & kConvSilu) {
 #pragma unroll
-                for (int j = 0; j < kW; ++j) v = fmaf(w[j][e], x[j][e], v);
-                y[e] = p.flags & kConvSilu ? v * sigmoid_f32(v) : v;
-#pragma unroll
-                for (int j = 0; j < kW - 1; ++j) x[j][e] = x[j + 1][e];
+                for (int e = 0; e < kE; ++e) v[e] *= sigmoid_f32(v[e]);
             }
-            if (i + a < i1) store_piece<kWhole, T, kE>(static_cast<T *>(p.y) + in.dense(i + a), y, in.cn);
+            conv_shift<kE, kW>(x);
+            if (i + a < i1) store_piece<kWhole, T, kE>(y, v, in.cn);
+            y += y_step;
         }
     }
 }
@@ -117,15 +152,16 @@ __global__ void __launch_bounds__(256) ptq_conv_kernel(const ConvParams p)
 // Gradients: dpre = dy silu'(pre) of the segment's outputs and of the W - 1 behind it gives dx of the segment,
 // dx[i] = sum_j weight[j] dpre[i + (W-1) - j], and x times dpre of the segment's own outputs dweight.  A warp takes 32 pieces of a
 // segment, goes on to others and keeps the sums of dweight and dbias in registers.
-template <typename T, int kE, int kW, bool kWhole>
-__global__ void __launch_bounds__(256) ptq_conv_backward_kernel(const ConvParams p)
+template <typename T, int kW, bool kWhole>
+__global__ void __launch_bounds__(256, 2) ptq_conv_backward_kernel(const ConvParams p)
 {
+    constexpr int kE = kConvE;
     __shared__ float s_sum[8][32 * kE];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int piece = blockIdx.x * 32 + lane;
     const int c = piece * kE, cn = max(min(kE, p.channels - c), 0);
     float w[kW][kE], bias[kE], dw[kW][kE], db[kE];
-    conv_weights<T, kE, kW>(p, c, cn, w, bias);
+    conv_weights<kE, kW, kWhole>(p, c, cn, w, bias);
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
         db[e] = 0.0f;
@@ -138,70 +174,83 @@ __global__ void __launch_bounds__(256) ptq_conv_backward_kernel(const ConvParams
         const ConvRow<T, kE, kW, kWhole> in(p, static_cast<int>(row / p.segments), piece);
         const int i0 = seg * p.segment, end = min(i0 + p.segment, p.length), i1 = min(end, in.len);
         const int first = seg == 0 ? -(kW - 1) : i0;      // the first segment makes the state's gradient too
+        const int tail = in.len - (kW - 1);               // step of the final state's first row
+        const int last = end + kW - 1;                    // behind the last output whose dpre is needed
+        const T *dy0 = static_cast<const T *>(p.dy) + (static_cast<long long>(in.b) * p.length + (in.way < 0 ? in.len - 1 : 0)) * p.channels + c;
+        const auto dy_of = [&](int o) { return load_piece<kWhole, T, kE>(dy0 + in.way * o * p.channels, o < in.len && o < last ? cn : 0); };
+        Piece<T, kE> before[kW - 1], next_x[kConvAhead], next_dy[kConvAhead];
+#pragma unroll
+        for (int j = 0; j < kW - 1; ++j) before[j] = in.input(i0 - (kW - 1) + j);
+#pragma unroll
+        for (int a = 0; a < kConvAhead; ++a) {
+            next_x[a] = in.step(i0 + a);
+            next_dy[a] = dy_of(i0 + a);
+        }
         float x[kW][kE], d[kW][kE];                        // rows o-(W-1) .. o; dpre of the same rows
 #pragma unroll
-        for (int j = 0; j < kW - 1; ++j) {
-            const Piece<T, kE> v = in.input(i0 - (kW - 1) + j);
+        for (int j = 0; j < kW - 1; ++j)
 #pragma unroll
             for (int e = 0; e < kE; ++e) {
-                x[j][e] = v[e];
-                d[j][e] = 0.0f;
+                x[j][e] = before[j][e];
+                d[j][e] = 0.0f;                            // outputs in front of the segment: no dx of it needs them
             }
-        }
-        // outputs o = i0 .. ; d of outputs in front of the segment is of no use to it, in front of the sequence it is zero
-        const int tail = in.len - (kW - 1);               // step of the final state's first row
-        Piece<T, kE> nx = in.input(i0), nd;
-        const auto dy_of = [&](int o) {
-            return load_piece<kWhole, T, kE>(static_cast<const T *>(p.dy) + in.dense(min(o, p.length - 1)), o < in.len ? cn : 0);
-        };
-        nd = dy_of(i0);
-        for (int o = i0; o < end + kW - 1; ++o) {
-            const Piece<T, kE> vx = nx, vd = nd;
-            if (o + 1 < end + kW - 1) {
-                nx = in.input(o + 1);
-                nd = dy_of(o + 1);
+        for (int o0 = i0; o0 < last; o0 += kConvAhead) {
+            Piece<T, kE> now_x[kConvAhead], now_dy[kConvAhead];
+#pragma unroll
+            for (int a = 0; a < kConvAhead; ++a) {
+                now_x[a] = next_x[a];
+                now_dy[a] = next_dy[a];
+                if (o0 + kConvAhead < last) {
+                    next_x[a] = in.step(o0 + kConvAhead + a);
+                    next_dy[a] = dy_of(o0 + kConvAhead + a);
+                }
             }
-            const bool on = o < in.len, own = o < i1;
-            float out[kE];
 #pragma unroll
-            for (int e = 0; e < kE; ++e) {
-                x[kW - 1][e] = vx[e];
-                float v = bias[e];
+            for (int a = 0; a < kConvAhead; ++a) {
+                const int o = o0 + a;
+                float v[kE], g[kE], out[kE];
 #pragma unroll
-                for (int j = 0; j < kW; ++j) v = fmaf(w[j][e], x[j][e], v);
-                float g = vd[e];
+                for (int e = 0; e < kE; ++e) {
+                    x[kW - 1][e] = now_x[a][e];
+                    g[e] = now_dy[a][e];
+                }
                 if (p.flags & kConvSilu) {
-                    const float s = sigmoid_f32(v);
-                    g *= s * fmaf(v, 1.0f - s, 1.0f);
-                }
-                d[kW - 1][e] = on ? g : 0.0f;
-                if (own) {
-                    db[e] += g;
+                    conv_row<kE, kW>(v, w, x, bias);
 #pragma unroll
-                    for (int j = 0; j < kW; ++j) dw[j][e] = fmaf(g, x[j][e], dw[j][e]);
+                    for (int e = 0; e < kE; ++e) {
+                        const float s = sigmoid_f32(v[e]);
+                        g[e] *= s * fmaf(v[e], 1.0f - s, 1.0f);
+                    }
                 }
-                out[e] = 0.0f;
 #pragma unroll
-                for (int j = 0; j < kW; ++j) out[e] = fmaf(w[j][e], d[kW - 1 - j][e], out[e]);
-#pragma unroll
-                for (int j = 0; j < kW - 1; ++j) {
-                    x[j][e] = x[j + 1][e];
-                    d[j][e] = d[j + 1][e];
+                for (int e = 0; e < kE; ++e) {
+                    if (o >= in.len || o >= last) g[e] = 0.0f;
+                    d[kW - 1][e] = g[e];
+                    if (o >= i1) g[e] = 0.0f;              // the next segment's own
+                    db[e] += g[e];
+                    out[e] = 0.0f;
                 }
-            }
-            const int i = o - (kW - 1);                    // the step whose gradient is complete now
-            if (i >= first && i < end) {
-                if (p.dfinal && i >= tail && i < in.len) {
-                    const Piece<T, kE> f = load_piece<kWhole, T, kE>(
-                        static_cast<const T *>(p.dfinal) + (static_cast<long long>(in.b) * (kW - 1) + (i - tail)) * p.channels + c, cn);
 #pragma unroll
-                    for (int e = 0; e < kE; ++e) out[e] += f[e];
+                for (int j = 0; j < kW; ++j) {
+                    fma_each<kE>(dw[j], g, x[j], dw[j]);
+                    fma_each<kE>(out, w[j], d[kW - 1 - j], out);
                 }
-                if (i >= 0)
-                    store_piece<kWhole, T, kE>(static_cast<T *>(p.dx) + in.dense(i), out, cn);
-                else if (p.dstate)
-                    store_piece<kWhole, T, kE>(static_cast<T *>(p.dstate) + (static_cast<long long>(in.b) * (kW - 1) + (i + kW - 1)) * p.channels + c, out,
-                                       cn);
+                conv_shift<kE, kW>(x);
+                conv_shift<kE, kW>(d);
+                const int i = o - (kW - 1);                // the step whose gradient is complete now
+                if (i >= first && i < end) {
+                    if (p.dfinal && i >= tail && i < in.len) {
+                        const Piece<T, kE> f = load_piece<kWhole, T, kE>(
+                            static_cast<const T *>(p.dfinal) + (static_cast<long long>(in.b) * (kW - 1) + (i - tail)) * p.channels + c, cn);
+#pragma unroll
+                        for (int e = 0; e < kE; ++e) out[e] += f[e];
+                    }
+                    if (i >= 0)
+                        store_piece<kWhole, T, kE>(static_cast<T *>(p.dx) + in.dense(i), out, cn);
+                    else if (p.dstate)
+                        store_piece<kWhole, T, kE>(static_cast<T *>(p.dstate) + (static_cast<long long>(in.b) * (kW - 1) + (i + kW - 1)) * p.channels + c,
+                                                   out, cn);
+                }
             }
         }
     }
