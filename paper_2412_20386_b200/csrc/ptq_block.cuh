@@ -80,6 +80,13 @@ struct Piece {
     }
 };
 
+template <typename T, int kE>
+__device__ __forceinline__ void floats_of(float (&f)[kE], const Piece<T, kE> &r)
+{
+#pragma unroll
+    for (int e = 0; e < kE; ++e) f[e] = r[e];
+}
+
 // Words of the accesses that move a piece, and how many elements one of them holds.
 template <typename T, int kE>
 constexpr int kAccessWords = kE * sizeof(T) >= 16 ? 4 : kE * sizeof(T) >= 8 ? 2 : 1;
@@ -264,6 +271,19 @@ __device__ __forceinline__ void mul_pair(float &d0, float &d1, float a0, float a
     asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
         : "=f"(d0), "=f"(d1)
         : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+__device__ __forceinline__ void add_pair(float &d0, float &d1, float a0, float a1, float b0, float b1)
+{
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d0), "=f"(d1)
+        : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+template <int kN>
+__device__ __forceinline__ void add_each(float (&d)[kN], const float (&a)[kN], const float (&b)[kN])
+{
+    static_assert(kN % 2 == 0, "pairs");
+#pragma unroll
+    for (int k = 0; k < kN; k += 2) add_pair(d[k], d[k + 1], a[k], a[k + 1], b[k], b[k + 1]);
 }
 // d[k] = a[k] b[k] + c[k], and with one factor for all k; d may be any of the operands.
 template <int kN>

@@ -32,26 +32,23 @@ struct NormParams {
     float *part;                                // [gridDim.x][3][cols]: dweight, dbias, dscale
 };
 
-// Sums over the CTA of kV values per thread, the same in every thread.  `buf` [kV][warps]; a barrier lies between the writes and
+// Sums over the CTA of kV values per thread, the same in every thread.  `buf` [warps][kV]; a barrier lies between the writes and
 // the reads, and the caller gives another buffer the next time.
 template <int kV>
 __device__ __forceinline__ void row_sums(float (&v)[kV], float *buf, int warp, int warps, int lane)
 {
+    lane_sums<kV, 1, 16>(v, lane);
+    if (lane < kV) buf[warp * kV + first_sum<kV, 1, 16>(lane)] = v[0];
+    if (warps == 1)
+        __syncwarp();
+    else
+        __syncthreads();
+    load_floats<true, kV>(v, buf, kV);
+    for (int w = 1; w < warps; ++w) {
+        float more[kV];
+        load_floats<true, kV>(more, buf + w * kV, kV);
 #pragma unroll
-    for (int i = 0; i < kV; ++i) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-    }
-    if (warps == 1) return;
-    if (lane == 0) {
-#pragma unroll
-        for (int i = 0; i < kV; ++i) buf[i * kNormMaxWarps + warp] = v[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kV; ++i) {
-        v[i] = 0.0f;
-        for (int w = 0; w < warps; ++w) v[i] += buf[i * kNormMaxWarps + w];
+        for (int i = 0; i < kV; ++i) v[i] += more[i];
     }
 }
 
@@ -78,24 +75,21 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) ptq_norm_kernel(const Norm
 {
     constexpr int kStages = 3;
     constexpr int kParts = sizeof(T) / 2, kResidualParts = sizeof(R) / 2;
-    __shared__ float s_sum[2][kStages][2 * kRB * kNormMaxWarps];
+    __shared__ __align__(16) float s_sum[2][kStages][2 * kRB * (kWide ? kNormMaxWarps : 8)];
     extern __shared__ __align__(16) uint4 norm_rows[];
     const int threads = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = threads >> 5;
     const int c = threadIdx.x * 8, cn = max(min(8, p.cols - c), 0);
     const bool has_dr = kBackward && p.dresidual_out;
     const NormStage at(p.residual, p.gate, kBackward, has_dr, kParts, kResidualParts, kRB, threads);
-    Piece<float, 8> weight, bias, scale;
+    float weight[8], bias[8], scale[8];
     const auto parameters = [&] {
-        weight = load_piece<kWhole, float, 8>(p.weight + c, p.weight ? cn : 0);
-        bias = load_piece<kWhole, float, 8>(p.bias + c, p.bias ? cn : 0);
-        scale = load_piece<kWhole, float, 8>(p.scale + c, p.scale ? cn : 0);
-        if (!p.weight) {
+        floats_of(weight, load_piece<kWhole, float, 8>(p.weight + c, p.weight ? cn : 0));
+        floats_of(bias, load_piece<kWhole, float, 8>(p.bias + c, p.bias ? cn : 0));
+        floats_of(scale, load_piece<kWhole, float, 8>(p.scale + c, p.scale ? cn : 0));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) weight.w[e] = __float_as_uint(1.0f);
-        }
-        if (!p.scale) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) scale.w[e] = __float_as_uint(1.0f);
+        for (int e = 0; e < 8; ++e) {
+            if (!p.weight) weight[e] = 1.0f;
+            if (!p.scale) scale[e] = 1.0f;
         }
     };
     if (!kWide) parameters();
@@ -103,26 +97,33 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) ptq_norm_kernel(const Norm
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         if (kBackward) sum_w[e] = sum_b[e] = sum_s[e] = 0.0f;
-    const auto fetch = [&](long long m0, int stage) {
+    const long long step = static_cast<long long>(gridDim.x) * kRB;
+    long long m0 = static_cast<long long>(blockIdx.x) * kRB;
+    // the thread's part of the next set's first row
+    const T *at_x = static_cast<const T *>(p.x) + m0 * p.x_l + c, *at_gate = static_cast<const T *>(p.gate) + m0 * p.gate_l + c,
+            *at_dy = static_cast<const T *>(p.dy) + m0 * p.cols + c;
+    const R *at_residual = static_cast<const R *>(p.residual) + m0 * p.residual_l + c, *at_dr = static_cast<const R *>(p.dresidual_out) + m0 * p.cols + c;
+    const auto fetch = [&](long long m, int stage) {
         uint4 *to = norm_rows + stage * at.size + threadIdx.x;
 #pragma unroll
         for (int i = 0; i < kRB; ++i) {
-            const long long m = m0 + i;
-            const int n = m < p.rows ? cn : 0;
-            stage_piece<kWhole, T, 8>(to + at.x + i * kParts * threads, static_cast<const T *>(p.x) + m * p.x_l + c, n, threads);
-            if (p.residual)
-                stage_piece<kWhole, R, 8>(to + at.residual + i * kResidualParts * threads, static_cast<const R *>(p.residual) + m * p.residual_l + c, n, threads);
-            if (p.gate) stage_piece<kWhole, T, 8>(to + at.gate + i * kParts * threads, static_cast<const T *>(p.gate) + m * p.gate_l + c, n, threads);
-            if (kBackward) stage_piece<kWhole, T, 8>(to + at.dy + i * kParts * threads, static_cast<const T *>(p.dy) + m * p.cols + c, n, threads);
-            if (has_dr)
-                stage_piece<kWhole, R, 8>(to + at.dresidual + i * kResidualParts * threads, static_cast<const R *>(p.dresidual_out) + m * p.cols + c, n, threads);
+            const int n = m + i < p.rows ? cn : 0;
+            stage_piece<kWhole, T, 8>(to + at.x + i * kParts * threads, at_x + i * p.x_l, n, threads);
+            if (p.residual) stage_piece<kWhole, R, 8>(to + at.residual + i * kResidualParts * threads, at_residual + i * p.residual_l, n, threads);
+            if (p.gate) stage_piece<kWhole, T, 8>(to + at.gate + i * kParts * threads, at_gate + i * p.gate_l, n, threads);
+            if (kBackward) stage_piece<kWhole, T, 8>(to + at.dy + i * kParts * threads, at_dy + static_cast<long long>(i) * p.cols, n, threads);
+            if (has_dr) stage_piece<kWhole, R, 8>(to + at.dresidual + i * kResidualParts * threads, at_dr + static_cast<long long>(i) * p.cols, n, threads);
         }
         stage_group();
+        at_x += step * p.x_l;
+        at_residual += step * p.residual_l;
+        at_gate += step * p.gate_l;
+        at_dy += step * p.cols;
+        at_dr += step * p.cols;
     };
-    const long long step = static_cast<long long>(gridDim.x) * kRB;
-    long long m0 = static_cast<long long>(blockIdx.x) * kRB;
     if (p.stages == 2 && m0 < p.rows) fetch(m0, 0);
-    for (int parity = 0; m0 < p.rows; m0 += step, parity ^= 1) {
+    long long out = m0 * p.cols + c;                      // where the thread's part of the set's first row goes
+    for (int parity = 0; m0 < p.rows; m0 += step, out += step * p.cols, parity ^= 1) {
         if (p.stages == 2) {
             if (m0 + step < p.rows)
                 fetch(m0 + step, parity ^ 1);
@@ -140,72 +141,69 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) ptq_norm_kernel(const Norm
         float r[kRB][8], mean[kRB], rstd[kRB];
 #pragma unroll
         for (int i = 0; i < kRB; ++i) {
-            mean[i] = 0.0f;
-            const Piece<T, 8> x = x_of(i);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) r[i][e] = x[e];
+            floats_of(r[i], x_of(i));
             if (p.gate_at == kGateIn) {
                 const Piece<T, 8> g = gate_of(i);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) r[i][e] *= g[e] * sigmoid_f32(g[e]);
             }
-            if (p.scale) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) r[i][e] *= scale[e];
-            }
             if (p.residual) {
-                const Piece<R, 8> res = staged_piece<R, 8>(from + at.residual + i * kResidualParts * threads, threads);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) r[i][e] += res[e];
+                float res[8];
+                floats_of(res, staged_piece<R, 8>(from + at.residual + i * kResidualParts * threads, threads));
+                fma_each<8>(r[i], scale, r[i], res);
+            } else if (p.scale) {
+                mul_each<8>(r[i], scale, r[i]);
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) mean[i] += r[i][e];
+            if (!kBackward && p.residual_out && m0 + i < p.rows)
+                store_piece<kWhole, R, 8>(static_cast<R *>(p.residual_out) + out + static_cast<long long>(i) * p.cols, r[i], cn);
         }
         if (p.layer) {
+#pragma unroll
+            for (int i = 0; i < kRB; ++i) {
+                float s[4];
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) add_pair(s[e], s[e + 1], r[i][e], r[i][e + 1], r[i][e + 4], r[i][e + 5]);
+                add_pair(s[0], s[1], s[0], s[1], s[2], s[3]);
+                mean[i] = s[0] + s[1];
+            }
             row_sums<kRB>(mean, s_sum[parity][0], warp, warps, lane);
 #pragma unroll
-            for (int i = 0; i < kRB; ++i) mean[i] *= p.inv_cols;
-        }
+            for (int i = 0; i < kRB; ++i) {
+                const float m = -mean[i] * p.inv_cols;
 #pragma unroll
-        for (int i = 0; i < kRB; ++i) {
-            if (!kBackward && p.residual_out && m0 + i < p.rows)
-                store_piece<kWhole, R, 8>(static_cast<R *>(p.residual_out) + (m0 + i) * p.cols + c, r[i], cn);
-            rstd[i] = 0.0f;
+                for (int e = 0; e < 8; e += 2) add_pair(r[i][e], r[i][e + 1], r[i][e], r[i][e + 1], m, m);
+                if (cn < 8) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (p.layer) r[i][e] = e < cn ? r[i][e] - mean[i] : 0.0f;
-                rstd[i] = fmaf(r[i][e], r[i][e], rstd[i]);
+                    for (int e = 0; e < 8; ++e)
+                        if (e >= cn) r[i][e] = 0.0f;
+                }
             }
         }
+#pragma unroll
+        for (int i = 0; i < kRB; ++i) rstd[i] = dot_each<8>(r[i], r[i]);
         row_sums<kRB>(rstd, s_sum[parity][1], warp, warps, lane);
 #pragma unroll
         for (int i = 0; i < kRB; ++i) {
             rstd[i] = rsqrtf(fmaf(rstd[i], p.inv_cols, p.eps));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) r[i][e] *= rstd[i];                          // n from here on
+            mul_each<8>(r[i], rstd[i], r[i]);                                        // n from here on
         }
         if constexpr (!kBackward) {
 #pragma unroll
             for (int i = 0; i < kRB; ++i) {
                 if (m0 + i >= p.rows) break;
-                float y[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = fmaf(r[i][e], weight[e], bias[e]);
+                fma_each<8>(r[i], r[i], weight, bias);
                 if (p.gate_at == kGateOut) {
                     const Piece<T, 8> g = gate_of(i);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] *= g[e] * sigmoid_f32(g[e]);
+                    for (int e = 0; e < 8; ++e) r[i][e] *= g[e] * sigmoid_f32(g[e]);
                 }
-                store_piece<kWhole, T, 8>(static_cast<T *>(p.y) + (m0 + i) * p.cols + c, y, cn);
+                store_piece<kWhole, T, 8>(static_cast<T *>(p.y) + out + static_cast<long long>(i) * p.cols, r[i], cn);
             }
         } else {
             float sums[2 * kRB], dn[kRB][8];
 #pragma unroll
             for (int i = 0; i < kRB; ++i) {
-                const Piece<T, 8> dy = staged_piece<T, 8>(from + at.dy + i * kParts * threads, threads);
-                sums[2 * i] = sums[2 * i + 1] = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) dn[i][e] = dy[e];
+                floats_of(dn[i], staged_piece<T, 8>(from + at.dy + i * kParts * threads, threads));
                 if (p.gate_at == kGateOut) {
                     const Piece<T, 8> g = gate_of(i);
                     float dg[8];
@@ -215,53 +213,51 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) ptq_norm_kernel(const Norm
                         dg[e] = dn[i][e] * fmaf(r[i][e], weight[e], bias[e]) * s * fmaf(z, 1.0f - s, 1.0f);
                         dn[i][e] *= z * s;
                     }
-                    if (m0 + i < p.rows) store_piece<kWhole, T, 8>(static_cast<T *>(p.dgate) + (m0 + i) * p.cols + c, dg, cn);
+                    if (m0 + i < p.rows) store_piece<kWhole, T, 8>(static_cast<T *>(p.dgate) + out + static_cast<long long>(i) * p.cols, dg, cn);
                 }
+                fma_each<8>(sum_w, dn[i], r[i], sum_w);
+                add_each<8>(sum_b, dn[i], sum_b);
+                mul_each<8>(dn[i], dn[i], weight);
+                sums[2 * i] = dot_each<8>(dn[i], r[i]);
+                float s[4];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    sum_w[e] = fmaf(dn[i][e], r[i][e], sum_w[e]);
-                    sum_b[e] += dn[i][e];
-                    dn[i][e] *= weight[e];
-                    sums[2 * i] = fmaf(dn[i][e], r[i][e], sums[2 * i]);
-                    sums[2 * i + 1] += dn[i][e];
-                }
+                for (int e = 0; e < 4; e += 2) add_pair(s[e], s[e + 1], dn[i][e], dn[i][e + 1], dn[i][e + 4], dn[i][e + 5]);
+                add_pair(s[0], s[1], s[0], s[1], s[2], s[3]);
+                sums[2 * i + 1] = s[0] + s[1];
             }
             row_sums<2 * kRB>(sums, s_sum[parity][2], warp, warps, lane);
 #pragma unroll
             for (int i = 0; i < kRB; ++i) {
                 if (m0 + i >= p.rows) break;
-                const float along = sums[2 * i] * p.inv_cols, flat = p.layer ? sums[2 * i + 1] * p.inv_cols : 0.0f;
-                const long long out = (m0 + i) * p.cols + c;
-                float dx[8];
+                const float along = -sums[2 * i] * p.inv_cols, flat = p.layer ? -sums[2 * i + 1] * p.inv_cols : 0.0f;
+                const long long row = out + static_cast<long long>(i) * p.cols;
+                fma_each<8>(dn[i], along, r[i], dn[i]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dn[i][e] = (fmaf(-r[i][e], along, dn[i][e]) - flat) * rstd[i];       // dr from here on
+                for (int e = 0; e < 8; e += 2) add_pair(dn[i][e], dn[i][e + 1], dn[i][e], dn[i][e + 1], flat, flat);
+                float dr[8], v[8], dx[8];
                 if (has_dr) {
-                    const Piece<R, 8> dres = staged_piece<R, 8>(from + at.dresidual + i * kResidualParts * threads, threads);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) dn[i][e] += dres[e];
+                    floats_of(dr, staged_piece<R, 8>(from + at.dresidual + i * kResidualParts * threads, threads));
+                    fma_each<8>(dr, rstd[i], dn[i], dr);
+                } else {
+                    mul_each<8>(dr, rstd[i], dn[i]);
                 }
-                if (p.dresidual) store_piece<kWhole, R, 8>(static_cast<R *>(p.dresidual) + out, dn[i], cn);
-                const Piece<T, 8> x = x_of(i);
+                if (p.dresidual) store_piece<kWhole, R, 8>(static_cast<R *>(p.dresidual) + row, dr, cn);
+                floats_of(v, x_of(i));
+                mul_each<8>(dx, dr, scale);
                 if (p.gate_at == kGateIn) {
                     const Piece<T, 8> g = gate_of(i);
                     float dg[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float z = g[e], s = sigmoid_f32(z);
-                        dx[e] = dn[i][e] * scale[e];
-                        dg[e] = dx[e] * x[e] * s * fmaf(z, 1.0f - s, 1.0f);
-                        dx[e] *= z * s;
-                        sum_s[e] = fmaf(dn[i][e], x[e] * z * s, sum_s[e]);
+                        const float z = g[e], s = sigmoid_f32(z), silu = z * s;
+                        dg[e] = dx[e] * v[e] * s * fmaf(z, 1.0f - s, 1.0f);
+                        dx[e] *= silu;
+                        v[e] *= silu;
                     }
-                    store_piece<kWhole, T, 8>(static_cast<T *>(p.dgate) + out, dg, cn);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        dx[e] = dn[i][e] * scale[e];
-                        sum_s[e] = fmaf(dn[i][e], x[e], sum_s[e]);
-                    }
+                    store_piece<kWhole, T, 8>(static_cast<T *>(p.dgate) + row, dg, cn);
                 }
-                store_piece<kWhole, T, 8>(static_cast<T *>(p.dx) + out, dx, cn);
+                if (p.scale) fma_each<8>(sum_s, dr, v, sum_s);
+                store_piece<kWhole, T, 8>(static_cast<T *>(p.dx) + row, dx, cn);
             }
         }
     }
