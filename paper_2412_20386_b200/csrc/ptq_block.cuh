@@ -175,7 +175,10 @@ __device__ __forceinline__ void stage_piece(uint4 *to, const T *p, int n, int ap
 #pragma unroll
         for (int i = 0; i < kParts; ++i) {
             const int bytes = n >= (i + 1) * kElems ? 16 : 0;      // the rest of the 16 is filled with zeros, nothing is read for none
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + 16 * apart * i), "l"(p + i * kElems), "r"(bytes) : "memory");
+            if constexpr (kParts == 1)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + 16 * apart * i), "l"(p + i * kElems), "r"(bytes) : "memory");
+            else                                           // half a sector: the other part finds it in the first-level cache
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(at + 16 * apart * i), "l"(p + i * kElems), "r"(bytes) : "memory");
         }
     } else {
         const Piece<T, kE> r = load_piece<false, T, kE>(p, n);

@@ -52,6 +52,30 @@ __device__ __forceinline__ void row_sums(float (&v)[kV], float *buf, int warp, i
     }
 }
 
+// Stores eight columns of a row per lane.  Two parts of 16 bytes (binary32) would each fill half a sector: they change hands within pairs of
+// lanes through `slot` (two 16-byte places of each thread, `apart` from each other), so that an instruction fills whole ones.
+// Called by whole warps; `left`: columns from the lane's first one to the end of the row.
+template <bool kWhole, typename V>
+__device__ __forceinline__ void store_columns(V *at, const float (&f)[8], int left, uint4 *slot, int apart, int lane)
+{
+    if constexpr (kWhole && sizeof(V) == 4) {
+        Piece<float, 8> r;
+        r.set(f);
+        slot[0] = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+        slot[apart] = make_uint4(r.w[4], r.w[5], r.w[6], r.w[7]);
+        __syncwarp();
+        const int part = lane & 1;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int owner = i - part;                    // relative to the lane
+            if (left - 8 * owner >= 4 * part + 4) *reinterpret_cast<uint4 *>(at + 8 * owner + 4 * part) = slot[owner + part * apart];
+        }
+        __syncwarp();
+    } else {
+        store_piece<kWhole, V, 8>(at, f, max(min(8, left), 0));
+    }
+}
+
 // Where a thread's pieces of the rows lie in shared memory, in units of 16 bytes: kRB rows of each tensor that the call has.
 struct NormStage {
     int x, residual, gate, dy, dresidual, size;
@@ -78,7 +102,7 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) ptq_norm_kernel(const Norm
     __shared__ __align__(16) float s_sum[2][kStages][2 * kRB * (kWide ? kNormMaxWarps : 8)];
     extern __shared__ __align__(16) uint4 norm_rows[];
     const int threads = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = threads >> 5;
-    const int c = threadIdx.x * 8, cn = max(min(8, p.cols - c), 0);
+    const int c = threadIdx.x * 8, left = p.cols - c, cn = max(min(8, left), 0);
     const bool has_dr = kBackward && p.dresidual_out;
     const NormStage at(p.residual, p.gate, kBackward, has_dr, kParts, kResidualParts, kRB, threads);
     float weight[8], bias[8], scale[8];
@@ -134,7 +158,7 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) ptq_norm_kernel(const Norm
             fetch(m0, 0);
             staged();
         }
-        const uint4 *from = norm_rows + (p.stages == 2 ? parity * at.size : 0) + threadIdx.x;
+        uint4 *from = norm_rows + (p.stages == 2 ? parity * at.size : 0) + threadIdx.x;
         const auto x_of = [&](int i) { return staged_piece<T, 8>(from + at.x + i * kParts * threads, threads); };
         const auto gate_of = [&](int i) { return staged_piece<T, 8>(from + at.gate + i * kParts * threads, threads); };
         if (kWide) parameters();
@@ -154,8 +178,13 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) ptq_norm_kernel(const Norm
             } else if (p.scale) {
                 mul_each<8>(r[i], scale, r[i]);
             }
-            if (!kBackward && p.residual_out && m0 + i < p.rows)
-                store_piece<kWhole, R, 8>(static_cast<R *>(p.residual_out) + out + static_cast<long long>(i) * p.cols, r[i], cn);
+            if (!kBackward && p.residual_out && m0 + i < p.rows) {
+                R *to = static_cast<R *>(p.residual_out) + out + static_cast<long long>(i) * p.cols;
+                if (p.residual)
+                    store_columns<kWhole, R>(to, r[i], left, from + at.residual + i * kResidualParts * threads, threads, lane);
+                else
+                    store_piece<kWhole, R, 8>(to, r[i], cn);
+            }
         }
         if (p.layer) {
 #pragma unroll
@@ -197,7 +226,8 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) ptq_norm_kernel(const Norm
 #pragma unroll
                     for (int e = 0; e < 8; ++e) r[i][e] *= g[e] * sigmoid_f32(g[e]);
                 }
-                store_piece<kWhole, T, 8>(static_cast<T *>(p.y) + out + static_cast<long long>(i) * p.cols, r[i], cn);
+                store_columns<kWhole, T>(static_cast<T *>(p.y) + out + static_cast<long long>(i) * p.cols, r[i], left, from + at.x + i * kParts * threads, threads,
+                                         lane);
             }
         } else {
             float sums[2 * kRB], dn[kRB][8];
@@ -241,7 +271,12 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) ptq_norm_kernel(const Norm
                 } else {
                     mul_each<8>(dr, rstd[i], dn[i]);
                 }
-                if (p.dresidual) store_piece<kWhole, R, 8>(static_cast<R *>(p.dresidual) + row, dr, cn);
+                if (p.dresidual) {
+                    if (p.residual)
+                        store_columns<kWhole, R>(static_cast<R *>(p.dresidual) + row, dr, left, from + at.residual + i * kResidualParts * threads, threads, lane);
+                    else
+                        store_piece<kWhole, R, 8>(static_cast<R *>(p.dresidual) + row, dr, cn);
+                }
                 floats_of(v, x_of(i));
                 mul_each<8>(dx, dr, scale);
                 if (p.gate_at == kGateIn) {
@@ -257,7 +292,7 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) ptq_norm_kernel(const Norm
                     store_piece<kWhole, T, 8>(static_cast<T *>(p.dgate) + row, dg, cn);
                 }
                 if (p.scale) fma_each<8>(sum_s, dr, v, sum_s);
-                store_piece<kWhole, T, 8>(static_cast<T *>(p.dx) + row, dx, cn);
+                store_columns<kWhole, T>(static_cast<T *>(p.dx) + row, dx, left, from + at.x + i * kParts * threads, threads, lane);
             }
         }
     }
