@@ -64,27 +64,39 @@ ptq_status_t with_type(int dtype, Fn fn)
 }
 
 // ---------------------------------------------------------------------------------------------------- scan
-// How a call is cut.  Chunks: until the GPU has enough warps, but of 256 steps at least, since every further chunk has to be
-// gone over twice.  The forward pass and the backward pass cut the sequences alike, so that one rule sizes both workspaces.
+// How a call is cut.  The forward pass and the backward pass cut the sequences alike, so that one rule sizes both workspaces.
 struct ScanPlan {
     ScanSplit split;                  // of the forward pass
     int group_warps, group_blocks, chunk_len, chunks;
     long long warps, ctas;            // of one chunk
     ScanCut cut(int n, bool whole) const { return {split, warps * n, ctas * n, whole}; }
 };
+// Chunks of a multiple of 32 steps.  The time goes as the steps of a chunk and as the sets of warps that the GPU holds at once (12 to
+// an SM).  More than one chunk: everything but the output is gone over twice, there is another launch
+// (about 60 steps), and the last chunk folds the others' sums.
 ScanPlan scan_plan(const ptq_scan_t &s)
 {
     const int per_group = s.channels / s.groups;
     const long long sequences = static_cast<long long>(s.batch) * s.groups;
     ScanPlan p;
     p.split = scan_split_forward(s.states, false);
-    const auto warps = [&] { return sequences * ceil_div(per_group, p.split.width()); };
-    const long long chunks = std::max(1ll, std::min(ceil_div(12 * kSms, warps()), ceil_div(s.length, 256)));
-    if (warps() * chunks < 8 * kSms) p.split = scan_split_forward(s.states, true);
-    p.chunk_len = static_cast<int>(ceil_div(ceil_div(s.length, chunks), 64) * 64);
+    long long warps = sequences * ceil_div(per_group, p.split.width());
+    long long chunks = 1;
+    double least = -1.0;
+    for (long long n = 1; n <= ceil_div(s.length, 32) && n <= 512; n = n < 16 ? n + 1 : n + n / 8) {
+        const double len = 32.0 * static_cast<double>(ceil_div(ceil_div(s.length, n), 32));
+        const double load = std::max(1.0, std::ceil(static_cast<double>(warps) * n / (12.0 * kSms) - 0.02));
+        const double cost = n == 1 ? s.length * load : 1.8 * len * load + 60.0 + 2.0 * n;
+        if (least < 0.0 || cost < least) {
+            least = cost;
+            chunks = n;
+        }
+    }
+    if (warps * chunks < 8 * kSms) p.split = scan_split_forward(s.states, true);
+    p.chunk_len = static_cast<int>(ceil_div(ceil_div(s.length, chunks), 32) * 32);
     p.chunks = static_cast<int>(ceil_div(s.length, p.chunk_len));
     p.group_warps = static_cast<int>(ceil_div(per_group, p.split.width()));
-    p.warps = warps();
+    p.warps = sequences * p.group_warps;
     p.group_blocks = static_cast<int>(ceil_div(per_group, scan_split_backward(s.states).width() * ptq::kScanWarps));
     p.ctas = sequences * p.group_blocks;
     return p;
@@ -146,7 +158,16 @@ ptq::ScanParams scan_params(const ptq_scan_t &s, const ScanPlan &plan)
     p.chunk_len = plan.chunk_len;
     p.chunks = plan.chunks;
     p.flags = s.flags;
-    p.pairs = s.states % 2 == 0 && aligned({s.B, s.C}, 2 * elem_bytes(s.dtype)) && multiples({p.B_b, p.B_l, p.B_g, p.C_b, p.C_l, p.C_g}, 2);
+    p.unit = 1;
+    for (int unit : {4, 2})
+        if (p.unit == 1 && aligned({s.u, s.delta, s.z}, unit * elem_bytes(s.dtype)) &&
+            multiples({p.u_b, p.u_l, p.delta_b, p.delta_l, p.z_b, p.z_l, p.group_channels}, unit))
+            p.unit = unit;
+    p.bc_unit = 1;
+    for (int unit : {4, 2})
+        if (p.bc_unit == 1 && s.states % unit == 0 && aligned({s.B, s.C}, unit * elem_bytes(s.dtype)) &&
+            multiples({p.B_b, p.B_l, p.B_g, p.C_b, p.C_l, p.C_g}, unit))
+            p.bc_unit = unit;
     return p;
 }
 
@@ -385,13 +406,15 @@ ptq_status_t ptq_scan_forward(const ptq_scan_t *s, void *y, float *final_state, 
     p.final_state = final_state;
     p.history = history;
     const bool whole = scan_whole(*s) && aligned({y, final_state, history}, 16);
+    if (!aligned({y}, 4 * elem_bytes(s->dtype))) p.unit = 1;
     unsigned char *w = static_cast<unsigned char *>(workspace);
     p.slots = reinterpret_cast<float *>(w + space.slots);
     p.sums = reinterpret_cast<float *>(w + space.sums);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return with_type(s->dtype, [&](auto t) {
         using Launch = ScanLaunch<decltype(t)>;
-        if (s->length == 1 && !history) return Launch::step(p, whole, st);
+        if (s->length == 1 && !history)        // here only the states and B and C have to be whole
+            return Launch::step(p, (s->states <= 2 || s->states % 4 == 0) && aligned({s->A, s->state, final_state}, 16) && p.bc_unit >= std::min(s->states, 4), st);
         if (plan.chunks > 1) PTQ_TRY(Launch::forward(ptq::kScanSum, p, plan.cut(plan.chunks - 1, whole), st));
         return Launch::forward(ptq::kScanForward, p, plan.cut(plan.chunks, whole), st);
     });
@@ -430,6 +453,7 @@ ptq_status_t ptq_scan_backward(const ptq_scan_t *s, const float *history, const 
     p.dC = g->dC;
     p.dstate = g->dstate;
     const bool whole = scan_whole(*s) && aligned({dy, g->du, g->ddelta, g->dz, history, dfinal, g->dstate}, 16);
+    if (!aligned({dy, g->du, g->ddelta, g->dz}, 4 * elem_bytes(s->dtype))) p.unit = 1;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return with_type(s->dtype, [&](auto t) {
         using Launch = ScanLaunch<decltype(t)>;

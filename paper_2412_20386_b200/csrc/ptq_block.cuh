@@ -92,9 +92,9 @@ template <typename T, int kE>
 constexpr int kAccessWords = kE * sizeof(T) >= 16 ? 4 : kE * sizeof(T) >= 8 ? 2 : 1;
 
 // `n` of the kE elements exist, the others are zeros.  kWhole: the pointer allows accesses of up to 16 bytes, and n ends between two of
-// them.  Plain loads: some kernels replace what they have read (a state), which loads through the read-only path must not see.
+// them; otherwise of `unit` elements (4, 2 or 1), of which 16-bit types make use.  Plain loads: some kernels replace what they have read (a state), which loads through the read-only path must not see.
 template <bool kWhole, typename T, int kE>
-__device__ __forceinline__ Piece<T, kE> load_piece(const T *p, int n)
+__device__ __forceinline__ Piece<T, kE> load_piece(const T *p, int n, int unit = 1)
 {
     Piece<T, kE> r;
     r.zero();
@@ -118,6 +118,26 @@ __device__ __forceinline__ Piece<T, kE> load_piece(const T *p, int n)
             }
         }
     } else {
+        if constexpr (sizeof(T) == 2 && kE % 4 == 0) {
+            if (unit >= 4) {
+#pragma unroll
+                for (int i = 0; i < kE / 4; ++i) {
+                    if (n < 4 * i + 4) continue;
+                    const uint2 v = reinterpret_cast<const uint2 *>(p)[i];
+                    r.w[2 * i] = v.x;
+                    r.w[2 * i + 1] = v.y;
+                }
+                return r;
+            }
+        }
+        if constexpr (sizeof(T) == 2 && kE % 2 == 0) {
+            if (unit >= 2) {
+#pragma unroll
+                for (int i = 0; i < kE / 2; ++i)
+                    if (n >= 2 * i + 2) r.w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+                return r;
+            }
+        }
 #pragma unroll
         for (int e = 0; e < kE; ++e) {
             if (e >= n) continue;
@@ -130,7 +150,7 @@ __device__ __forceinline__ Piece<T, kE> load_piece(const T *p, int n)
     return r;
 }
 template <bool kWhole, typename T, int kE>
-__device__ __forceinline__ void store_piece(T *p, const Piece<T, kE> &r, int n)
+__device__ __forceinline__ void store_piece(T *p, const Piece<T, kE> &r, int n, int unit = 1)
 {
     if constexpr (kWhole && kE * sizeof(T) >= 4) {
         constexpr int kStep = kAccessWords<T, kE>, kElems = kStep * 4 / static_cast<int>(sizeof(T));
@@ -145,6 +165,22 @@ __device__ __forceinline__ void store_piece(T *p, const Piece<T, kE> &r, int n)
                 reinterpret_cast<uint32_t *>(p)[i] = r.w[i];
         }
     } else {
+        if constexpr (sizeof(T) == 2 && kE % 4 == 0) {
+            if (unit >= 4) {
+#pragma unroll
+                for (int i = 0; i < kE / 4; ++i)
+                    if (n >= 4 * i + 4) reinterpret_cast<uint2 *>(p)[i] = make_uint2(r.w[2 * i], r.w[2 * i + 1]);
+                return;
+            }
+        }
+        if constexpr (sizeof(T) == 2 && kE % 2 == 0) {
+            if (unit >= 2) {
+#pragma unroll
+                for (int i = 0; i < kE / 2; ++i)
+                    if (n >= 2 * i + 2) reinterpret_cast<uint32_t *>(p)[i] = r.w[i];
+                return;
+            }
+        }
 #pragma unroll
         for (int e = 0; e < kE; ++e) {
             if (e >= n) continue;
@@ -156,17 +192,17 @@ __device__ __forceinline__ void store_piece(T *p, const Piece<T, kE> &r, int n)
     }
 }
 template <bool kWhole, typename T, int kE>
-__device__ __forceinline__ void store_piece(T *p, const float (&f)[kE], int n)
+__device__ __forceinline__ void store_piece(T *p, const float (&f)[kE], int n, int unit = 1)
 {
     Piece<T, kE> r;
     r.set(f);
-    store_piece<kWhole, T, kE>(p, r, n);
+    store_piece<kWhole, T, kE>(p, r, n, unit);
 }
 
 // A piece on its way to shared memory, its 16-byte parts at to[0], to[apart], ... (one thread's of a row of threads, so that no two of them
 // meet a bank): asynchronous where accesses of 16 bytes are allowed.  The thread that asked for it may read it after staged().
 template <bool kWhole, typename T, int kE>
-__device__ __forceinline__ void stage_piece(uint4 *to, const T *p, int n, int apart = 32)
+__device__ __forceinline__ void stage_piece(uint4 *to, const T *p, int n, int apart = 32, int unit = 1)
 {
     static_assert(kE * sizeof(T) % 16 == 0, "whole parts");
     constexpr int kParts = kE * static_cast<int>(sizeof(T)) / 16, kElems = 16 / static_cast<int>(sizeof(T));
@@ -181,7 +217,7 @@ __device__ __forceinline__ void stage_piece(uint4 *to, const T *p, int n, int ap
                 asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(at + 16 * apart * i), "l"(p + i * kElems), "r"(bytes) : "memory");
         }
     } else {
-        const Piece<T, kE> r = load_piece<false, T, kE>(p, n);
+        const Piece<T, kE> r = load_piece<false, T, kE>(p, n, unit);
 #pragma unroll
         for (int i = 0; i < kParts; ++i) to[apart * i] = make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]);
     }

@@ -33,7 +33,8 @@ struct ScanParams {
     int group_warps, group_blocks;              // warps (CTAs of the backward pass) that share the channels of a group
     int chunk_len, chunks;
     unsigned flags;
-    bool pairs;                                 // B and C allow accesses of two states
+    int unit;                                   // channels that an access of general rows may take: 4, 2 or 1
+    int bc_unit;                                // the same of the states of B and C
     float *slots;                               // [chunks][batch][channels][states]
     float *sums;                                // [chunks][batch][channels]: sum of dt of a chunk
     // forward
@@ -194,9 +195,9 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_kernel(const Scan
     }
     const auto fetch = [&](int k0) {
         const int n = k0 + row < n_steps ? cn : 0;
-        r_u = load_piece<kWhole, T, 8>(at_u, n);
-        r_delta = load_piece<kWhole, T, 8>(at_delta, n);
-        if (gated) r_z = load_piece<kWhole, T, 8>(at_z, n);
+        r_u = load_piece<kWhole, T, 8>(at_u, n, p.unit);
+        r_delta = load_piece<kWhole, T, 8>(at_delta, n, p.unit);
+        if (gated) r_z = load_piece<kWhole, T, 8>(at_z, n, p.unit);
         at_u += next_u;
         at_delta += next_delta;
         at_z += next_z;
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_kernel(const Scan
 #pragma unroll
             for (int i = 0; i < kBC; ++i) {
                 const int states = has && k0 + t0 + i * kApart < n_steps ? p.states - n1 : 0;
-                r_BC[j][i] = p.pairs ? load_piece<true, T, kPer>(at_BC[j], states) : load_piece<false, T, kPer>(at_BC[j], states);
+                r_BC[j][i] = p.bc_unit >= 2 ? load_piece<true, T, kPer>(at_BC[j], states) : load_piece<false, T, kPer>(at_BC[j], states);
                 at_BC[j] += apart[j];
             }
         }
@@ -358,7 +359,7 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_kernel(const Scan
 #pragma unroll
                     for (int e = 0; e < 8; ++e) y[e] *= z[e] * sigmoid_f32(z[e]);
                 }
-                store_piece<kWhole, T, 8>(at_y, y, cn);
+                store_piece<kWhole, T, 8>(at_y, y, cn, p.unit);
             }
             at_y += static_cast<long long>(way * kRows) * p.channels;
         }
@@ -457,10 +458,10 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
         const bool on = i0 + row < blk.i1;
         const long long at = on ? token_of(i0 + row) : 0;
         const int n = on ? cn : 0;
-        stage_piece<kWhole, T, 8>(&w.rows[to][kU][0][lane], static_cast<const T *>(p.u) + blk.b * p.u_b + at * p.u_l + c, n);
-        stage_piece<kWhole, T, 8>(&w.rows[to][kDelta][0][lane], static_cast<const T *>(p.delta) + blk.b * p.delta_b + at * p.delta_l + c, n);
-        stage_piece<kWhole, T, 8>(&w.rows[to][kDy][0][lane], static_cast<const T *>(p.dy) + (sequence + at) * p.channels + c, n);
-        if (p.z) stage_piece<kWhole, T, 8>(&w.rows[to][kZ][0][lane], static_cast<const T *>(p.z) + blk.b * p.z_b + at * p.z_l + c, n);
+        stage_piece<kWhole, T, 8>(&w.rows[to][kU][0][lane], static_cast<const T *>(p.u) + blk.b * p.u_b + at * p.u_l + c, n, 32, p.unit);
+        stage_piece<kWhole, T, 8>(&w.rows[to][kDelta][0][lane], static_cast<const T *>(p.delta) + blk.b * p.delta_b + at * p.delta_l + c, n, 32, p.unit);
+        stage_piece<kWhole, T, 8>(&w.rows[to][kDy][0][lane], static_cast<const T *>(p.dy) + (sequence + at) * p.channels + c, n, 32, p.unit);
+        if (p.z) stage_piece<kWhole, T, 8>(&w.rows[to][kZ][0][lane], static_cast<const T *>(p.z) + blk.b * p.z_b + at * p.z_l + c, n, 32, p.unit);
     };
     Piece<T, kPer> r_BC[2][kBC];
     const int bc_t = kPer * lane / kNP, bc_n = kPer * lane % kNP;
@@ -475,7 +476,7 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
                 const long long tok = token_of(step);
                 const T *from = k ? static_cast<const T *>(p.C) + blk.b * p.C_b + tok * p.C_l + blk.g * p.C_g + bc_n
                                   : static_cast<const T *>(p.B) + blk.b * p.B_b + tok * p.B_l + blk.g * p.B_g + bc_n;
-                r_BC[k][i] = p.pairs ? load_piece<true, T, kPer>(from, states) : load_piece<false, T, kPer>(from, states);
+                r_BC[k][i] = p.bc_unit >= 2 ? load_piece<true, T, kPer>(from, states) : load_piece<false, T, kPer>(from, states);
             }
         }
     };
@@ -496,9 +497,9 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
 #pragma unroll
             for (int i = 0; i < 8; ++i) zero[i] = 0.0f;
             const long long at = (sequence + i0 + row) * p.channels + c;
-            store_piece<kWhole, T, 8>(static_cast<T *>(p.du) + at, zero, cn);
-            store_piece<kWhole, T, 8>(static_cast<T *>(p.ddelta) + at, zero, cn);
-            if (p.z) store_piece<kWhole, T, 8>(static_cast<T *>(p.dz) + at, zero, cn);
+            store_piece<kWhole, T, 8>(static_cast<T *>(p.du) + at, zero, cn, p.unit);
+            store_piece<kWhole, T, 8>(static_cast<T *>(p.ddelta) + at, zero, cn, p.unit);
+            if (p.z) store_piece<kWhole, T, 8>(static_cast<T *>(p.dz) + at, zero, cn, p.unit);
         }
     }
     // the thread's sums of dB and dC: which of the two, which state, which step of the tile first
@@ -728,9 +729,9 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
                 }
             }
             const long long at = (sequence + token_of(i0 + row)) * p.channels + c;
-            store_piece<kWhole, T, 8>(static_cast<T *>(p.du) + at, du, cn);
-            store_piece<kWhole, T, 8>(static_cast<T *>(p.ddelta) + at, dd, cn);
-            if (p.z) store_piece<kWhole, T, 8>(static_cast<T *>(p.dz) + at, dz, cn);
+            store_piece<kWhole, T, 8>(static_cast<T *>(p.du) + at, du, cn, p.unit);
+            store_piece<kWhole, T, 8>(static_cast<T *>(p.ddelta) + at, dd, cn, p.unit);
+            if (p.z) store_piece<kWhole, T, 8>(static_cast<T *>(p.dz) + at, dz, cn, p.unit);
         }
         for (int t = out_t; t < kRows; t += kThreads / (2 * kNP)) {
             const int i = i0 + t;
@@ -797,56 +798,78 @@ __global__ void __launch_bounds__(kScanFinishThreads) ptq_scan_finish_kernel(con
     }
 }
 
-// One token per sequence.  Bound: the state's bytes, read and written once.  A thread keeps its kNS rates and goes over
-// sequences; the lanes of a channel take its token's values alike.
+// One token per sequence.  Bound: the state's bytes, read and written once, and close behind it the issue slots.  The kS lanes of a channel
+// hold kNS states each and take kS sequences at a time: every lane makes dt, dt u and in the end y of one of them and hands the former
+// round; all loads of the set go out before its first store.
 template <typename T, int kNS, int kS, bool kWhole>
-__global__ void __launch_bounds__(256) ptq_scan_step_kernel(const ScanParams p)
+__global__ void __launch_bounds__(256, 4) ptq_scan_step_kernel(const ScanParams p)
 {
+    const int lane = threadIdx.x & 31, own = lane % kS, base = lane - own;
     const int per_cta = 256 / kS;
-    const int blocks = (p.channels + per_cta - 1) / per_cta;
-    const int d = (blockIdx.x % blocks) * per_cta + threadIdx.x / kS, n0 = (threadIdx.x % kS) * kNS;
-    const int nn = d < p.channels ? max(min(kNS, p.states - n0), 0) : 0;
+    const int blocks = (p.channels + per_cta - 1) / per_cta, rows = gridDim.x / blocks;
+    const int d = (blockIdx.x % blocks) * per_cta + threadIdx.x / kS, n0 = own * kNS;
     const bool on = d < p.channels;
+    const int nn = on ? max(min(kNS, p.states - n0), 0) : 0;
     const int g = on ? d / p.group_channels : 0;
     float rate[kNS];
     load_floats<kWhole, kNS>(rate, p.A + static_cast<long long>(d) * p.states + n0, nn);
 #pragma unroll
     for (int k = 0; k < kNS; ++k) rate[k] = scan_rate(rate[k]);
     const float bias = on && p.delta_bias ? p.delta_bias[d] : 0.0f, D = on && p.D ? p.D[d] : 0.0f;
-#pragma unroll 2
-    for (int b = blockIdx.x / blocks; b < p.batch; b += gridDim.x / blocks) {
-        const bool token = !p.lengths || p.lengths[b] > 0;
-        const long long at = (static_cast<long long>(b) * p.channels + d) * p.states + n0;
-        float h[kNS];
+    const long long state_step = static_cast<long long>(p.channels) * p.states, jump = static_cast<long long>(rows) * kS;
+    long long b0 = static_cast<long long>(blockIdx.x / blocks) * kS;
+    const T *at_u = static_cast<const T *>(p.u) + (b0 + own) * p.u_b + d, *at_delta = static_cast<const T *>(p.delta) + (b0 + own) * p.delta_b + d,
+            *at_z = static_cast<const T *>(p.z) + (b0 + own) * p.z_b + d, *at_B = static_cast<const T *>(p.B) + b0 * p.B_b + g * p.B_g + n0,
+            *at_C = static_cast<const T *>(p.C) + b0 * p.C_b + g * p.C_g + n0;
+    long long at_state = b0 * state_step + static_cast<long long>(d) * p.states + n0;
+    T *at_y = static_cast<T *>(p.y) + (b0 + own) * p.channels + d;
+    for (; b0 < p.batch; b0 += jump) {
+        const bool token = on && b0 + own < p.batch && (!p.lengths || p.lengths[b0 + own] > 0);
+        float h[kS][kNS];
+        Piece<T, kNS> B[kS], C[kS];
 #pragma unroll
-        for (int k = 0; k < kNS; ++k) h[k] = 0.0f;
-        if (p.state) load_floats<kWhole, kNS>(h, p.state + at, nn);
-        float o = 0.0f, u = 0.0f;
-        if (on && token) {
-            u = to_f32<T>(static_cast<const T *>(p.u)[b * p.u_b + d]);
-            const float x = to_f32<T>(static_cast<const T *>(p.delta)[b * p.delta_b + d]) + bias;
-            const float dt = p.flags & kScanSoftplus ? softplus_f32(x) : x;
-            const T *B = static_cast<const T *>(p.B) + b * p.B_b + g * p.B_g + n0, *C = static_cast<const T *>(p.C) + b * p.C_b + g * p.C_g + n0;
-            float a[kNS];
-            scan_decays<kNS>(a, dt, rate);
-#pragma unroll
-            for (int k = 0; k < kNS; ++k) {
-                const float in = k < nn ? to_f32<T>(B[k]) : 0.0f, out = k < nn ? to_f32<T>(C[k]) : 0.0f;
-                h[k] = fmaf(a[k], h[k], dt * u * in);
-                o = fmaf(h[k], out, o);
-            }
+        for (int i = 0; i < kS; ++i) {
+            const int n = b0 + i < p.batch ? nn : 0;
+            load_floats<kWhole, kNS>(h[i], p.state + at_state + i * state_step, p.state ? n : 0);
+            B[i] = load_piece<kWhole, T, kNS>(at_B + i * p.B_b, n);
+            C[i] = load_piece<kWhole, T, kNS>(at_C + i * p.C_b, n);
         }
+        const Piece<T, 1> ru = load_piece<false, T, 1>(at_u, token), rdelta = load_piece<false, T, 1>(at_delta, token),
+                          rz = load_piece<false, T, 1>(at_z, token && p.z);
+        const float x = rdelta[0] + bias, u = ru[0];
+        const float dt = !token ? 0.0f : p.flags & kScanSoftplus ? softplus_f32(x) : x;
+        float o[kS];
 #pragma unroll
-        for (int i = 1; i < kS; i *= 2) o += __shfl_xor_sync(0xffffffffu, o, i);
-        if (p.final_state) store_floats<kWhole, kNS>(p.final_state + at, h, nn);
-        if (on && token && n0 == 0) {
-            if (p.D) o = fmaf(D, u, o);
-            if (p.z) {
-                const float z = to_f32<T>(static_cast<const T *>(p.z)[b * p.z_b + d]);
-                o *= z * sigmoid_f32(z);
-            }
-            static_cast<T *>(p.y)[static_cast<long long>(b) * p.channels + d] = from_f32<T>(o);
+        for (int i = 0; i < kS; ++i) {
+            const float dt_i = __shfl_sync(0xffffffffu, dt, base + i), in = __shfl_sync(0xffffffffu, dt * u, base + i);
+            const bool token_i = __shfl_sync(0xffffffffu, token, base + i);
+            float a[kNS], f[kNS];
+            scan_decays<kNS>(a, dt_i, rate);
+            floats_of(f, B[i]);
+            mul_each<kNS>(f, in, f);
+            fma_each<kNS>(a, a, h[i], f);
+#pragma unroll
+            for (int k = 0; k < kNS; ++k) h[i][k] = token_i ? a[k] : h[i][k];       // what is read for no token may be anything
+            floats_of(f, C[i]);
+            o[i] = dot_each<kNS>(h[i], f);
+            if (p.final_state) store_floats<kWhole, kNS>(p.final_state + at_state + i * state_step, h[i], b0 + i < p.batch ? nn : 0);
         }
+        lane_sums<kS, 1, kS / 2>(o, lane);
+        // the lane holds the sum of sequence first_sum: its own bits in reverse
+        float y = o[0];
+        if (kS > 2) y = __shfl_sync(0xffffffffu, y, base + first_sum<kS, 1, kS / 2>(own));
+        if (token) {
+            if (p.D) y = fmaf(D, u, y);
+            if (p.z) y *= rz[0] * sigmoid_f32(rz[0]);
+            *at_y = from_f32<T>(y);
+        }
+        at_u += jump * p.u_b;
+        at_delta += jump * p.delta_b;
+        at_z += jump * p.z_b;
+        at_B += jump * p.B_b;
+        at_C += jump * p.C_b;
+        at_state += jump * state_step;
+        at_y += jump * p.channels;
     }
 }
 

@@ -132,7 +132,7 @@ ptq_status_t ScanLaunch<T>::step(const ptq::ScanParams &p, bool whole_rows, cuda
         return with_flag(whole_rows, [&](auto whole) {
             using F = decltype(form);
             const long long blocks = ceil_div(p.channels, 256 / F::lanes);
-            const long long rows = std::min<long long>(p.batch, std::max(1ll, ceil_div(16 * kSms, blocks)));
+            const long long rows = std::max(1ll, std::min<long long>(ceil_div(p.batch, F::lanes), 4 * kSms / blocks));
             ptq::ptq_scan_step_kernel<T, F::states, F::lanes, decltype(whole)::value><<<static_cast<unsigned>(blocks * rows), 256, 0, stream>>>(p);
             return launched();
         });
