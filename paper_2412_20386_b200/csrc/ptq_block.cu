@@ -81,11 +81,12 @@ ScanPlan scan_plan(const ptq_scan_t &s)
     ScanPlan p;
     p.split = scan_split_forward(s.states, false);
     long long warps = sequences * ceil_div(per_group, p.split.width());
+    const double filled = s.lengths ? 0.5 : 1.0;          // a padded batch holds about half the tokens
     long long chunks = 1;
     double least = -1.0;
     for (long long n = 1; n <= ceil_div(s.length, 32) && n <= 512; n = n < 16 ? n + 1 : n + n / 8) {
         const double len = 32.0 * static_cast<double>(ceil_div(ceil_div(s.length, n), 32));
-        const double load = std::max(1.0, std::ceil(static_cast<double>(warps) * n / (12.0 * kSms) - 0.02));
+        const double load = std::max(1.0, std::ceil(filled * static_cast<double>(warps) * n / (12.0 * kSms) - 0.02));
         const double cost = n == 1 ? s.length * load : 1.8 * len * load + 60.0 + 2.0 * n;
         if (least < 0.0 || cost < least) {
             least = cost;
