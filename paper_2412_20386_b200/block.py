@@ -19,32 +19,25 @@ output is left as it is there, a new one holds zeros, and gradients are zeros.
 """
 from __future__ import annotations
 
-import contextlib
-
 from . import binding
 
 FLAG_SEQ_REVERSE, FLAG_SCAN_SOFTPLUS, FLAG_CONV_SILU, FLAG_NORM_LAYER, FLAG_NORM_GATE_OUT = 2, 1, 1, 1, 2
 SCAN_HISTORY = 8                  # PTQ_SCAN_HISTORY: steps between two states that the backward pass starts from
 
-_on_device = contextlib.nullcontext()
-
-
 def _native():
     return binding._native_block or binding._load_native_block()
 
 
-def _on(stream, tensor):
-    """The context in which `stream` (None: the current one) is the current stream of the tensor's device."""
+def _call(f, stream, tensor, *args):
+    """An extension call on `stream` (None: the current one of the tensors' device); a status code becomes an exception."""
     if stream is None:
-        return _on_device
-    import torch
-    if torch.is_tensor(tensor) and tensor.device != stream.device:
-        raise ValueError("the stream belongs to another device than the tensors")
-    return torch.cuda.stream(stream)
-
-
-def _status(r):
-    """The answer of an extension call: a status code becomes an exception."""
+        r = f(*args)
+    else:
+        import torch
+        if torch.is_tensor(tensor) and tensor.device != stream.device:
+            raise ValueError("the stream belongs to another device than the tensors")
+        with torch.cuda.stream(stream):
+            r = f(*args)
     if r.__class__ is int:
         binding._check(r)
     return r
@@ -67,16 +60,14 @@ def gated_scan(u, delta, A, B, C, D=None, z=None, delta_bias=None, state=None, l
     ``[batch, channels, states]`` is h in front of the first step; ``final_state`` receives h behind the last one and may be ``state``
     itself.  ``reverse`` goes from the last token to the first.  ``history`` (``scan_history``) is kept for the backward pass."""
     flags = (FLAG_SCAN_SOFTPLUS if softplus else 0) | (FLAG_SEQ_REVERSE if reverse else 0)
-    with _on(stream, u):
-        return _status(_native().scan(0, u, delta, A, B, C, D, z, delta_bias, state, lengths, flags, y, final_state, history))
+    return _call(_native().scan, stream, u, 0, u, delta, A, B, C, D, z, delta_bias, state, lengths, flags, y, final_state, history)
 
 
 def gated_scan_step(state, u, delta, A, B, C, D=None, z=None, delta_bias=None, softplus: bool = True, new_state=None, y=None, stream=None):
     """``gated_scan`` of one token per sequence: u, delta, z ``[batch, channels]``, B, C ``[batch, states]`` or ``[batch, groups, states]``.
     ``state`` is replaced unless ``new_state`` is given.  Returns y ``[batch, channels]``."""
-    with _on(stream, u):
-        return _status(_native().scan(1, u, delta, A, B, C, D, z, delta_bias, state, None, FLAG_SCAN_SOFTPLUS if softplus else 0, y,
-                                      state if new_state is None else new_state, None))
+    return _call(_native().scan, stream, u, 1, u, delta, A, B, C, D, z, delta_bias, state, None, FLAG_SCAN_SOFTPLUS if softplus else 0, y,
+                 state if new_state is None else new_state, None)
 
 
 def gated_scan_backward(dy, u, delta, A, B, C, history, D=None, z=None, delta_bias=None, state=None, lengths=None, softplus: bool = True,
@@ -84,8 +75,7 @@ def gated_scan_backward(dy, u, delta, A, B, C, history, D=None, z=None, delta_bi
     """``ptq_scan_backward``: gradients of ``gated_scan`` for dy and dfinal (the gradient of ``final_state``), from the ``history`` that the
     forward call filled.  ``state`` is the one that the forward call started from."""
     flags = (FLAG_SCAN_SOFTPLUS if softplus else 0) | (FLAG_SEQ_REVERSE if reverse else 0)
-    with _on(stream, u):
-        g = _status(_native().scan_backward(u, delta, A, B, C, D, z, delta_bias, state, lengths, flags, dy, history, dfinal))
+    g = _call(_native().scan_backward, stream, u, u, delta, A, B, C, D, z, delta_bias, state, lengths, flags, dy, history, dfinal)
     return dict(zip(("u", "delta", "A", "B", "C", "D", "z", "delta_bias", "state"), g))
 
 
@@ -103,16 +93,14 @@ def block_norm(x, weight=None, bias=None, residual=None, scale=None, gate=None, 
 
     with the root-mean-square norm or (``kind="layer"``) the layer norm.  The residual may be float32 beside any x.  Returns y, or (y, r)
     where ``residual`` or ``residual_out`` is given; ``residual_out`` may be ``residual`` itself."""
-    with _on(stream, x):
-        out, r = _status(_native().norm(x, weight, bias, residual, scale, gate, _norm_flags(kind, gate_at), eps, y, residual_out))
+    out, r = _call(_native().norm, stream, x, x, weight, bias, residual, scale, gate, _norm_flags(kind, gate_at), eps, y, residual_out)
     return out if r is None else (out, r)
 
 
 def block_norm_backward(dy, x, weight=None, bias=None, residual=None, scale=None, gate=None, kind: str = "rms", gate_at: str = "in", eps: float = 1e-5,
                         dresidual_out=None, stream=None):
     """``ptq_norm_backward``: gradients of ``block_norm`` for dy and dresidual_out (the gradient of r)."""
-    with _on(stream, x):
-        g = _status(_native().norm_backward(x, weight, bias, residual, scale, gate, _norm_flags(kind, gate_at), eps, dy, dresidual_out))
+    g = _call(_native().norm_backward, stream, x, x, weight, bias, residual, scale, gate, _norm_flags(kind, gate_at), eps, dy, dresidual_out)
     return dict(zip(("x", "weight", "bias", "residual", "scale", "gate"), g))
 
 
@@ -122,13 +110,11 @@ def short_conv(x, weight, bias=None, state=None, lengths=None, silu: bool = True
     the first step; ``final_state`` receives the last rows and may be ``state`` itself: one token of a generating model is a call of
     length 1."""
     flags = (FLAG_CONV_SILU if silu else 0) | (FLAG_SEQ_REVERSE if reverse else 0)
-    with _on(stream, x):
-        return _status(_native().conv(x, weight, bias, state, lengths, flags, y, final_state))
+    return _call(_native().conv, stream, x, x, weight, bias, state, lengths, flags, y, final_state)
 
 
 def short_conv_backward(dy, x, weight, bias=None, state=None, lengths=None, silu: bool = True, reverse: bool = False, dfinal=None, stream=None):
     """``ptq_conv_backward``: gradients of ``short_conv`` for dy and dfinal (the gradient of ``final_state``)."""
     flags = (FLAG_CONV_SILU if silu else 0) | (FLAG_SEQ_REVERSE if reverse else 0)
-    with _on(stream, x):
-        g = _status(_native().conv_backward(x, weight, bias, state, lengths, flags, dy, dfinal))
+    g = _call(_native().conv_backward, stream, x, x, weight, bias, state, lengths, flags, dy, dfinal)
     return dict(zip(("x", "weight", "bias", "state"), g))

@@ -79,7 +79,7 @@ ScanPlan scan_plan(const ptq_scan_t &s)
     const int per_group = s.channels / s.groups;
     const long long sequences = static_cast<long long>(s.batch) * s.groups;
     ScanPlan p;
-    p.split = scan_split_forward(s.states, false);
+    p.split = scan_split_forward(s.states, 0);
     long long warps = sequences * ceil_div(per_group, p.split.width());
     const double filled = s.lengths ? 0.5 : 1.0;          // a padded batch holds about half the tokens
     long long chunks = 1;
@@ -93,7 +93,7 @@ ScanPlan scan_plan(const ptq_scan_t &s)
             chunks = n;
         }
     }
-    if (warps * chunks < 8 * kSms) p.split = scan_split_forward(s.states, true);
+    if (warps * chunks < 9 * kSms) p.split = scan_split_forward(s.states, warps * chunks < 4 * kSms ? 2 : 1);
     p.chunk_len = static_cast<int>(ceil_div(ceil_div(s.length, chunks), 32) * 32);
     p.chunks = static_cast<int>(ceil_div(s.length, p.chunk_len));
     p.group_warps = static_cast<int>(ceil_div(per_group, p.split.width()));

@@ -15,11 +15,11 @@ struct ScanSplit {
     int lanes, channels, states;
     int width() const { return 32 / lanes * channels; }
 };
-inline ScanSplit scan_split_forward(int states, bool few)
+inline ScanSplit scan_split_forward(int states, int level)      // 0: many warps, 1, 2: few
 {
     if (states <= 4) return {1, 1, states == 3 ? 4 : states};
-    if (states <= 8) return few ? ScanSplit{2, 1, 4} : ScanSplit{2, 2, 4};
-    if (states <= 16) return few ? ScanSplit{4, 1, 4} : ScanSplit{2, 2, 8};
+    if (states <= 8) return level == 2 ? ScanSplit{2, 1, 4} : ScanSplit{2, 2, 4};
+    if (states <= 16) return level == 2 ? ScanSplit{4, 1, 4} : level == 1 ? ScanSplit{4, 2, 4} : ScanSplit{2, 2, 8};
     return {4, 2, 8};
 }
 inline ScanSplit scan_split_backward(int states)
@@ -41,6 +41,7 @@ ptq_status_t with_forward_split(ScanSplit sp, Fn fn)
     if (sp.lanes == 2 && sp.states == 4) return fn(ScanForm<2, 4, 2>());
     if (sp.lanes == 2) return fn(ScanForm<2, 8, 2>());
     if (sp.channels == 1) return fn(ScanForm<1, 4, 4>());
+    if (sp.states == 4) return fn(ScanForm<2, 4, 4>());
     return fn(ScanForm<2, 8, 4>());
 }
 template <class Fn>

@@ -76,7 +76,7 @@ def check(ptq, t, kind, gate_at, eps=1e-5, cotangent=True, seed=3):
         ref.close(got[k], g64[k], bound[k], 2 * f, "gradient of " + k)
 
 
-@pytest.mark.parametrize("kind,gate_at", itertools.product(["rms", "layer"], ["in", "out"]))
+@pytest.mark.parametrize("kind,gate_at", list(itertools.product(["rms", "layer"], ["in", "out"])))
 @pytest.mark.parametrize("dtype,residual", [(ref.F32, ref.F32), (ref.BF16, ref.F32), (ref.BF16, ref.BF16), (ref.F16, ref.F16), (ref.F16, ref.F32), (ref.F16, None)])
 def test_forms_and_types(ptq, kind, gate_at, dtype, residual):
     for i, (scale, gate, weight, bias) in enumerate(itertools.product([False, True], repeat=4)):
