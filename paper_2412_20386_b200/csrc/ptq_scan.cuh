@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_kernel(const Scan
 __host__ __device__ constexpr size_t scan_backward_smem(int channels, int states, int lanes, int bytes)
 {
     const size_t width = 32 / lanes * channels, rows = 256 / width, np = static_cast<size_t>(states) * lanes;
-    const size_t warp = 2 * 4 * 32 * 8 * bytes + rows * (width + 2) * 16 + 2 * rows * np * 4 + 2 * 32 * 8 * 4;
+    const size_t warp = 2 * 4 * 32 * 8 * bytes + rows * (width + 2) * 20 + 2 * rows * np * 4 + 2 * 32 * 8 * 4;
     return kScanWarps * (warp + 2 * rows * 2 * np * 4);
 }
 
@@ -415,8 +415,9 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
         uint4 rows[2][kTensors][kParts][32];              // of this tile and, on their way, of the next one
         float2 pair[kRows * kPitch];                      // (dt, dt u), later (s, r)
         float g[kRows * kPitch], o[kRows * kPitch];       // dyo; o without D u
+        float dt[kRows * kPitch];
         float BC[2][kRows * kNP];
-        float sum_D[8][32], sum_bias[8][32];              // of the lane's channels, over its rows
+        float2 sum_D[4][32], sum_bias[4][32];             // of the lane's channels, over its rows
     };
     extern __shared__ __align__(16) unsigned char scan_smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -451,7 +452,7 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
     const int row = lane / (kWidth / 8), part8 = lane % (kWidth / 8) * 8, c = blk.c0 + warp * kWidth + part8;
     const int cn = max(min(8, blk.c_end - c), 0);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w.sum_D[i][lane] = w.sum_bias[i][lane] = 0.0f;
+    for (int i = 0; i < 4; ++i) w.sum_D[i][lane] = w.sum_bias[i][lane] = make_float2(0.0f, 0.0f);
     const long long sequence = static_cast<long long>(blk.b) * p.length;
     const auto token_of = [&](int i) { return static_cast<long long>(reverse && i < blk.len ? blk.len - 1 - i : i); };
     const auto fetch_rows = [&](int i0, int to) {
@@ -466,17 +467,19 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
     Piece<T, kPer> r_BC[2][kBC];
     const int bc_t = kPer * lane / kNP, bc_n = kPer * lane % kNP;
     const bool has = kPer * lane < kRows * kNP;
+    const long long way = reverse ? -1 : 1, first = reverse ? blk.len - 1ll : 0ll;         // step i is token first + way i
+    const T *const B0 = static_cast<const T *>(p.B) + blk.b * p.B_b + blk.g * p.B_g + bc_n + first * p.B_l,
+            *const C0 = static_cast<const T *>(p.C) + blk.b * p.C_b + blk.g * p.C_g + bc_n + first * p.C_l;
     const auto fetch = [&](int i0) {
+        const T *at[2] = {B0 + way * (i0 + bc_t) * p.B_l, C0 + way * (i0 + bc_t) * p.C_l};
+        const long long apart[2] = {way * kApart * p.B_l, way * kApart * p.C_l};
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
 #pragma unroll
             for (int i = 0; i < kBC; ++i) {
-                const int step = i0 + bc_t + i * kApart;
-                const int states = has && step < blk.i1 ? p.states - bc_n : 0;
-                const long long tok = token_of(step);
-                const T *from = k ? static_cast<const T *>(p.C) + blk.b * p.C_b + tok * p.C_l + blk.g * p.C_g + bc_n
-                                  : static_cast<const T *>(p.B) + blk.b * p.B_b + tok * p.B_l + blk.g * p.B_g + bc_n;
-                r_BC[k][i] = p.bc_unit >= 2 ? load_piece<true, T, kPer>(from, states) : load_piece<false, T, kPer>(from, states);
+                const int states = has && i0 + bc_t + i * kApart < blk.i1 ? p.states - bc_n : 0;
+                r_BC[k][i] = p.bc_unit >= 2 ? load_piece<true, T, kPer>(at[k], states) : load_piece<false, T, kPer>(at[k], states);
+                at[k] += apart[k];
             }
         }
     };
@@ -521,7 +524,7 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
     }
     const Piece<float, 8> bias = load_piece<kWhole, float, 8>(p.delta_bias + c, p.delta_bias ? cn : 0);
     float4 *const own = reinterpret_cast<float4 *>(w.pair + row * kPitch + part8);
-    float *const own_g = w.g + row * kPitch + part8;
+    float *const own_g = w.g + row * kPitch + part8, *const own_dt = w.dt + row * kPitch + part8;
     for (int parity = 0; i0 >= blk.i0; i0 -= kRows, parity ^= 1) {
         const bool row_on = i0 + row < blk.i1;
         staged();
@@ -552,6 +555,7 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
                 }
                 own[i / 2] = f;
                 *reinterpret_cast<float2 *>(own_g + i) = g;
+                *reinterpret_cast<float2 *>(own_dt + i) = make_float2(f.x, f.z);
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -697,12 +701,13 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
             float du[8], dd[8], dz[8];
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
-                const float x0 = delta[i] + bias[i], x1 = delta[i + 1] + bias[i + 1];
-                float dt[2] = {x0, x1}, slope[2] = {1.0f, 1.0f};
+                const float2 dts = *reinterpret_cast<const float2 *>(own_dt + i);
+                const float dt[2] = {dts.x, dts.y};
+                float slope[2] = {1.0f, 1.0f};
                 if (softplus) {
+                    const float x0 = delta[i] + bias[i], x1 = delta[i + 1] + bias[i + 1];
                     float t0, t1;
                     exp_minus_abs_pair(t0, t1, x0, x1);
-                    softplus_pair(dt[0], dt[1], x0, x1, t0, t1);
                     slope[0] = __fdividef(x0 < 0.0f ? t0 : 1.0f, 1.0f + t0);
                     slope[1] = __fdividef(x1 < 0.0f ? t1 : 1.0f, 1.0f + t1);
                 }
@@ -722,10 +727,14 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
                         dz[i + k] = dy[i + k] * o * gate * fmaf(zz, 1.0f - gate, 1.0f);
                     }
                     if (!row_on) du[i + k] = dd[i + k] = dz[i + k] = 0.0f;
-                    if (row_on) {
-                        w.sum_D[i + k][lane] = fmaf(uu, dyo, w.sum_D[i + k][lane]);
-                        w.sum_bias[i + k][lane] += dd[i + k];
-                    }
+                }
+                if (row_on) {
+                    float2 sum = w.sum_D[i / 2][lane];
+                    fma_pair(sum.x, sum.y, u[i], u[i + 1], gs.x, gs.y, sum.x, sum.y);
+                    w.sum_D[i / 2][lane] = sum;
+                    sum = w.sum_bias[i / 2][lane];
+                    add_pair(sum.x, sum.y, sum.x, sum.y, dd[i], dd[i + 1]);
+                    w.sum_bias[i / 2][lane] = sum;
                 }
             }
             const long long at = (sequence + token_of(i0 + row)) * p.channels + c;
@@ -733,16 +742,24 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
             store_piece<kWhole, T, 8>(static_cast<T *>(p.ddelta) + at, dd, cn, p.unit);
             if (p.z) store_piece<kWhole, T, 8>(static_cast<T *>(p.dz) + at, dz, cn, p.unit);
         }
-        for (int t = out_t; t < kRows; t += kThreads / (2 * kNP)) {
-            const int i = i0 + t;
-            if (i >= end || out_n >= p.states) break;
-            float v = 0.0f;
-            if (i < blk.i1) {
-                const float *from = s_sum + parity * kScanWarps * kSums + (t * 2 + out_which) * kNP + out_n;
+        if (out_n < p.states) {
+            constexpr int kApartOut = kThreads / (2 * kNP) < kRows ? kThreads / (2 * kNP) : kRows;
+            const float *from = s_sum + parity * kScanWarps * kSums + (out_t * 2 + out_which) * kNP + out_n;
+            const bool inside = i0 + kRows <= blk.i1;       // the whole tile has tokens: they follow one another
+            const long long tok = sequence + first + way * (i0 + out_t), tok_step = way * kApartOut;
+            float *share_at = p.part_BC + ((static_cast<long long>(share) * p.batch * p.length + tok) * 2 + out_which) * p.states + out_n;
 #pragma unroll
-                for (int k = 0; k < kScanWarps; ++k) v += from[k * kSums];
+            for (int j = 0; j < kRows / kApartOut; ++j) {
+                const int i = i0 + out_t + j * kApartOut;
+                if (out_t >= kRows) continue;
+                float v = 0.0f;
+#pragma unroll
+                for (int k = 0; k < kScanWarps; ++k) v += from[k * kSums + j * kApartOut * 2 * kNP];
+                if (inside && p.part_BC)
+                    share_at[j * tok_step * 2 * p.states] = v;
+                else if (i < end)
+                    put_BC(i, i < blk.i1 ? v : 0.0f);
             }
-            put_BC(i, v);
         }
         __syncwarp();
     }
@@ -758,8 +775,9 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
         float a = 0.0f, b = 0.0f;
 #pragma unroll 8
         for (int r = 0; r < kRows; ++r) {
-            a += w.sum_D[i % 8][r * (kWidth / 8) + i / 8];
-            b += w.sum_bias[i % 8][r * (kWidth / 8) + i / 8];
+            const float2 D2 = w.sum_D[i % 8 / 2][r * (kWidth / 8) + i / 8], b2 = w.sum_bias[i % 8 / 2][r * (kWidth / 8) + i / 8];
+            a += i & 1 ? D2.y : D2.x;
+            b += i & 1 ? b2.y : b2.x;
         }
         p.part_D[part * p.channels + blk.c0 + warp * kWidth + i] = a;
         p.part_bias[part * p.channels + blk.c0 + warp * kWidth + i] = b;
