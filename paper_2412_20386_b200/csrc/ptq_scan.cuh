@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_kernel(const Scan
 __host__ __device__ constexpr size_t scan_backward_smem(int channels, int states, int lanes, int bytes)
 {
     const size_t width = 32 / lanes * channels, rows = 256 / width, np = static_cast<size_t>(states) * lanes;
-    const size_t warp = 2 * 4 * 32 * 8 * bytes + rows * (width + 2) * 20 + 2 * rows * np * 4 + 2 * 32 * 8 * 4;
+    const size_t warp = 2 * 4 * 32 * 8 * bytes + rows * (width + 2) * 20 + 2 * rows * np * 4 + 2 * width * 4 + 2 * 32 * 8 * 4;
     return kScanWarps * (warp + 2 * rows * 2 * np * 4);
 }
 
@@ -417,6 +417,7 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
         float g[kRows * kPitch], o[kRows * kPitch];       // dyo; o without D u
         float dt[kRows * kPitch];
         float BC[2][kRows * kNP];
+        float bias[kWidth], skip[kWidth];                 // delta_bias and D of the warp's channels, zeros for none
         float2 sum_D[4][32], sum_bias[4][32];             // of the lane's channels, over its rows
     };
     extern __shared__ __align__(16) unsigned char scan_smem[];
@@ -522,7 +523,12 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
         fetch_rows(i0, 0);
         fetch_state(i0 + (min(kRows, blk.i1 - i0) - 1) / kStretch * kStretch);
     }
-    const Piece<float, 8> bias = load_piece<kWhole, float, 8>(p.delta_bias + c, p.delta_bias ? cn : 0);
+    for (int i = lane; i < kWidth; i += 32) {
+        const int channel = blk.c0 + warp * kWidth + i;
+        w.bias[i] = p.delta_bias && channel < blk.c_end ? p.delta_bias[channel] : 0.0f;
+        w.skip[i] = p.D && channel < blk.c_end ? p.D[channel] : 0.0f;
+    }
+    __syncwarp();
     float4 *const own = reinterpret_cast<float4 *>(w.pair + row * kPitch + part8);
     float *const own_g = w.g + row * kPitch + part8, *const own_dt = w.dt + row * kPitch + part8;
     for (int parity = 0; i0 >= blk.i0; i0 -= kRows, parity ^= 1) {
@@ -535,9 +541,10 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
             if (p.z) z = staged_piece<T, 8>(&w.rows[parity][kZ][0][lane]);
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
+                const float2 bias = *reinterpret_cast<const float2 *>(w.bias + part8 + i);
                 float4 f;
-                f.x = delta[i] + bias[i];
-                f.z = delta[i + 1] + bias[i + 1];
+                f.x = delta[i] + bias.x;
+                f.z = delta[i + 1] + bias.y;
                 if (softplus) {
                     float t0, t1;
                     exp_minus_abs_pair(t0, t1, f.x, f.z);
@@ -606,6 +613,18 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
                 }
 #pragma unroll
                 for (int k = 0; k < kNS; ++k) v8[s * kNS + k] = dc[k];
+                if ((s + 1) * kC % kO == 0 && p.z) {
+                    constexpr int kOSteps = kO / kC;
+                    float v[kO];
+#pragma unroll
+                    for (int i = 0; i < kO; ++i) v[i] = o[(s + 1 - kOSteps) * kC + i];
+                    lane_sums<kO, 1, kS / 2>(v, lane);
+#pragma unroll
+                    for (int i = 0; i < kO / kS; ++i) {
+                        const int idx = first_sum<kO, 1, kS / 2>(lane) + i;
+                        w.o[(t0 + s + 1 - kOSteps + idx / kC) * kPitch + ch + idx % kC] = v[i];
+                    }
+                }
                 if ((s + 1) % kSteps == 0) {
                     float v[8];
 #pragma unroll
@@ -617,20 +636,6 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
                             const int idx = first_sum<8, kS, 16>(lane) + i;
                             sums[((t0 + s + 1 - kSteps + idx / kNS) * 2 + 1) * kNP + n0 + idx % kNS] = v[i];
                         }
-                    }
-                }
-            }
-            if (p.z) {
-#pragma unroll
-                for (int s = 0; s < kStretch * kC; s += kO) {
-                    float v[kO];
-#pragma unroll
-                    for (int i = 0; i < kO; ++i) v[i] = o[s + i];
-                    lane_sums<kO, 1, kS / 2>(v, lane);
-#pragma unroll
-                    for (int i = 0; i < kO / kS; ++i) {
-                        const int idx = s + first_sum<kO, 1, kS / 2>(lane) + i;
-                        w.o[(t0 + idx / kC) * kPitch + ch + idx % kC] = v[i];
                     }
                 }
             }
@@ -697,7 +702,6 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
                 z = staged_piece<T, 8>(&w.rows[parity][kZ][0][lane]);
                 dy = staged_piece<T, 8>(&w.rows[parity][kDy][0][lane]);
             }
-            const Piece<float, 8> skip = load_piece<kWhole, float, 8>(p.D + c, p.D ? cn : 0);
             float du[8], dd[8], dz[8];
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
@@ -705,24 +709,26 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
                 const float dt[2] = {dts.x, dts.y};
                 float slope[2] = {1.0f, 1.0f};
                 if (softplus) {
-                    const float x0 = delta[i] + bias[i], x1 = delta[i + 1] + bias[i + 1];
+                    const float2 bias = *reinterpret_cast<const float2 *>(w.bias + part8 + i);
+                    const float x0 = delta[i] + bias.x, x1 = delta[i + 1] + bias.y;
                     float t0, t1;
                     exp_minus_abs_pair(t0, t1, x0, x1);
                     slope[0] = __fdividef(x0 < 0.0f ? t0 : 1.0f, 1.0f + t0);
                     slope[1] = __fdividef(x1 < 0.0f ? t1 : 1.0f, 1.0f + t1);
                 }
                 const float4 f = own[i / 2];
+                const float2 skip = *reinterpret_cast<const float2 *>(w.skip + part8 + i);
                 const float2 gs = *reinterpret_cast<const float2 *>(own_g + i), os = *reinterpret_cast<const float2 *>(w.o + row * kPitch + part8 + i);
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const float s = k ? f.z : f.x, q = k ? f.w : f.y, uu = u[i + k], dyo = k ? gs.y : gs.x;
                     du[i + k] = dt[k] * s;
-                    if (p.D) du[i + k] = fmaf(skip[i + k], dyo, du[i + k]);
+                    if (p.D) du[i + k] = fmaf(k ? skip.y : skip.x, dyo, du[i + k]);
                     dd[i + k] = fmaf(uu, s, q * kLn2) * slope[k];
                     dz[i + k] = 0.0f;
                     if (p.z) {
                         float o = k ? os.y : os.x;
-                        if (p.D) o = fmaf(skip[i + k], uu, o);
+                        if (p.D) o = fmaf(k ? skip.y : skip.x, uu, o);
                         const float zz = z[i + k], gate = sigmoid_f32(zz);
                         dz[i + k] = dy[i + k] * o * gate * fmaf(zz, 1.0f - gate, 1.0f);
                     }
