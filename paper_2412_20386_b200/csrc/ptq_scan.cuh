@@ -791,7 +791,7 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
 }
 
 // The shares of the CTAs of the backward pass: dA, dD and ddelta_bias over the sequences and chunks, dB and dC over the CTAs of a group.
-constexpr int kScanFinishThreads = 1024;
+constexpr int kScanFinishThreads = 1024;    // the threads behind the last whole token have nothing to do
 template <typename T>
 __global__ void __launch_bounds__(kScanFinishThreads) ptq_scan_finish_kernel(const ScanParams p, float *dA, float *dD, float *dbias, int blocks_A, int blocks_D)
 {
@@ -808,17 +808,21 @@ __global__ void __launch_bounds__(kScanFinishThreads) ptq_scan_finish_kernel(con
         if (threadIdx.x < 32 && col < cols) out[col] = v;
         return;
     }
+    // dB and dC: a CTA takes whole tokens; one 64-bit division per CTA, the threads' own are of 32 bits
     block -= blocks_A + 2 * blocks_D;
-    const long long per = static_cast<long long>(p.batch) * p.length * 2 * p.states;
-    const long long total = per * p.groups, stride = static_cast<long long>(gridDim.x - blocks_A - 2 * blocks_D) * kScanFinishThreads;
-    for (long long idx = block * static_cast<long long>(kScanFinishThreads) + threadIdx.x; idx < total; idx += stride) {
-        const long long g = idx / per, rest = idx - g * per, tok = rest / (2 * p.states);
-        const int q = static_cast<int>(rest - tok * (2 * p.states));
+    const int pair = 2 * p.states, tokens = kScanFinishThreads / pair, t = threadIdx.x / pair, q = threadIdx.x - t * pair;
+    const long long all = static_cast<long long>(p.batch) * p.length, per = all * pair;
+    const long long sets = (all + tokens - 1) / tokens, stride = gridDim.x - blocks_A - 2 * blocks_D;
+    if (t >= tokens) return;
+    T *const out = static_cast<T *>(q >= p.states ? p.dC : p.dB) + (q >= p.states ? q - p.states : q);
+    for (long long set = block; set < sets * p.groups; set += stride) {
+        const long long g = set / sets, tok = (set - g * sets) * tokens + t;
+        if (tok >= all) continue;
+        const float *from = p.part_BC + g * p.group_blocks * per + tok * pair + q;
         float v = 0.0f;
-#pragma unroll 4
-        for (int j = 0; j < p.group_blocks; ++j) v += p.part_BC[(g * p.group_blocks + j) * per + rest];
-        const long long at = (tok * p.groups + g) * p.states + (q >= p.states ? q - p.states : q);
-        static_cast<T *>(q >= p.states ? p.dC : p.dB)[at] = from_f32<T>(v);
+#pragma unroll 8
+        for (int j = 0; j < p.group_blocks; ++j, from += per) v += *from;
+        out[(tok * p.groups + g) * p.states] = from_f32<T>(v);
     }
 }
 
