@@ -338,11 +338,11 @@ ptq::ConvParams conv_params(const ptq_conv_t &c, long long segments)
     p.segments = static_cast<int>(ceil_div(c.length, p.segment));
     return p;
 }
-// Forward: segments until the GPU has about 96 thousand threads, but of 8 steps at least (each reads taps - 1 rows again).
+// Forward: segments until the GPU has about 120 thousand threads, but of 8 steps at least (each reads taps - 1 rows again).
 ptq::ConvParams conv_forward_params(const ptq_conv_t &c)
 {
     const long long threads = static_cast<long long>(c.batch) * ceil_div(c.channels, ptq::kConvE);
-    return conv_params(c, std::max(1ll, std::min(ceil_div(kSms * 640, threads), ceil_div(c.length, 8))));
+    return conv_params(c, std::max(1ll, std::min(ceil_div(kSms * 800, threads), ceil_div(c.length, 8))));
 }
 // Backward: one wave of CTAs of eight warps, two to an SM, that go over the segments; as many segments as make the longest walk of a warp
 // shortest (a segment costs its steps and about 10 more for its start).

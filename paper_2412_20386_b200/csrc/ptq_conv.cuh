@@ -91,7 +91,7 @@ __device__ __forceinline__ void conv_shift(float (&x)[kW][kE])
 }
 
 constexpr int kConvE = 4;             // channels of a thread: with eight, weights and window leave too few warps
-constexpr int kConvAhead = 4;         // rows that are loaded together, one set under way while the other is worked on
+constexpr int kConvAhead = 2;         // rows that are loaded together, one set under way while the other is worked on
 
 template <typename T, int kW, bool kWhole>
 __global__ void __launch_bounds__(256) ptq_conv_kernel(const ConvParams p)
