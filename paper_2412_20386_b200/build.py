@@ -22,7 +22,7 @@ _CSRC = os.path.join(_HERE, "csrc")
 _SO = os.path.join(_HERE, "libptq_linear.so")
 _SOURCES = ["ptq_api.cu", "ptq_block.cu", "ptq_scan_f16.cu", "ptq_scan_bf16.cu", "ptq_scan_f32.cu"]
 _DEPS = ["ptq_api.cu", "ptq_gemm.cuh", "ptq_fused.cuh", "ptq_small.cuh", "ptq_short_k.cuh", "ptq_quantize.cuh", "ptq_quantize_dynamic.cuh",
-         "ptq_calibrate.cuh", "ptq_probe.cuh", "ptx_sm100.cuh", "ptq_host.h",
+         "ptq_calibrate.cuh", "ptq_probe.cuh", "ptx_sm100.cuh", "ptx_griddep.cuh", "ptq_host.h",
          "ptq_block.cu", "ptq_scan_f16.cu", "ptq_scan_bf16.cu", "ptq_scan_f32.cu", "ptq_block_host.h", "ptq_scan_launch.cuh",
          "ptq_block.cuh", "ptq_scan.cuh", "ptq_norm.cuh", "ptq_conv.cuh",
          os.path.join("..", "..", "include", "ptq_linear.h"), os.path.join("..", "..", "include", "ptq_block.h")]

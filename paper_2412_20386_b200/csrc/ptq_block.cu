@@ -508,9 +508,8 @@ ptq_status_t ptq_norm_backward(const ptq_norm_t *n, const void *dy, const void *
     p.stages = plan.stages;
     PTQ_TRY(launch_norm<true>(*n, plan, p, norm_whole(*n) && aligned({dy, dresidual_out, g->dx, g->dresidual, g->dgate}, 16), st));
     if (!g->dweight && !g->dbias && !g->dscale) return PTQ_OK;
-    ptq::ptq_norm_finish_kernel<<<dim3(static_cast<unsigned>(ceil_div(n->cols, 32)), 3), 1024, 0, st>>>(p.part, plan.ctas, n->cols, g->dweight, g->dbias,
-                                                                                                   g->dscale);
-    return launched();
+    return launch_next(ptq::ptq_norm_finish_kernel, dim3(static_cast<unsigned>(ceil_div(n->cols, 32)), 3), 1024, 0, st, p.part, plan.ctas, n->cols, g->dweight,
+                       g->dbias, g->dscale);
 }
 
 ptq_status_t ptq_conv_forward(const ptq_conv_t *c, void *y, void *final_state, void *stream)
@@ -572,9 +571,8 @@ ptq_status_t ptq_conv_backward(const ptq_conv_t *c, const void *dy, const void *
             });
         });
     }));
-    ptq::ptq_conv_finish_kernel<<<dim3(static_cast<unsigned>(ceil_div(c->channels, 32)), static_cast<unsigned>(c->taps + 1)), 1024, 0, st>>>(
-        p.part, rows, c->channels, c->taps, g->dweight, g->dbias);
-    return launched();
+    return launch_next(ptq::ptq_conv_finish_kernel, dim3(static_cast<unsigned>(ceil_div(c->channels, 32)), static_cast<unsigned>(c->taps + 1)), 1024, 0, st,
+                       p.part, rows, c->channels, c->taps, g->dweight, g->dbias);
 }
 
 }  // extern "C"

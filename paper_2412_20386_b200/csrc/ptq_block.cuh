@@ -8,6 +8,8 @@
 #include <stdint.h>
 #include <type_traits>
 
+#include "ptx_griddep.cuh"
+
 namespace ptq {
 
 constexpr float kLog2e = 1.4426950408889634f;

@@ -25,6 +25,25 @@ inline ptq_status_t launched()
     return PTQ_OK;
 }
 
+// Launch of a call's second or third kernel: it may begin while the one before it drains, and waits for its end (griddep_wait) before it
+// touches memory.  The first kernel of a call is launched the ordinary way.
+template <typename... KArgs, typename... Args>
+ptq_status_t launch_next(void (*kern)(KArgs...), dim3 grid, int threads, size_t smem, cudaStream_t stream, Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(static_cast<unsigned>(threads), 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    PTQ_CUDA(cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...));
+    return launched();
+}
+
 inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
 // Calls fn with the flag as a constant.

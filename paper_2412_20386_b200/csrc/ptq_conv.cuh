@@ -157,6 +157,7 @@ __global__ void __launch_bounds__(256, 2) ptq_conv_backward_kernel(const ConvPar
 {
     constexpr int kE = kConvE;
     __shared__ float s_sum[8][32 * kE];
+    griddep_launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int piece = blockIdx.x * 32 + lane;
     const int c = piece * kE, cn = max(min(kE, p.channels - c), 0);
@@ -275,6 +276,7 @@ __global__ void __launch_bounds__(256, 2) ptq_conv_backward_kernel(const ConvPar
 __global__ void __launch_bounds__(1024) ptq_conv_finish_kernel(const float *part, int rows, int cols, int taps, float *dweight, float *dbias)
 {
     __shared__ float s[32][33];
+    griddep_wait();
     const int col = blockIdx.x * 32 + (threadIdx.x & 31), j = blockIdx.y;
     if (j == taps && !dbias) return;
     const float v = sum_rows(part + static_cast<long long>(j) * cols + col, rows, static_cast<long long>(taps + 1) * cols, col < cols, s);

@@ -101,6 +101,7 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) ptq_norm_kernel(const Norm
     constexpr int kParts = sizeof(T) / 2, kResidualParts = sizeof(R) / 2;
     __shared__ __align__(16) float s_sum[2][kStages][2 * kRB * (kWide ? kNormMaxWarps : 8)];
     extern __shared__ __align__(16) uint4 norm_rows[];
+    if (kBackward) griddep_launch_dependents();
     const int threads = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = threads >> 5;
     const int c = threadIdx.x * 8, left = p.cols - c, cn = max(min(8, left), 0);
     const bool has_dr = kBackward && p.dresidual_out;
@@ -312,6 +313,7 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) ptq_norm_kernel(const Norm
 __global__ void __launch_bounds__(1024) ptq_norm_finish_kernel(const float *part, int rows, int cols, float *dweight, float *dbias, float *dscale)
 {
     __shared__ float s[32][33];
+    griddep_wait();
     const int col = blockIdx.x * 32 + (threadIdx.x & 31);
     float *out = blockIdx.y == 0 ? dweight : blockIdx.y == 1 ? dbias : dscale;
     if (!out) return;

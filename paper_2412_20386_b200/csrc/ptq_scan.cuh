@@ -151,6 +151,8 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_kernel(const Scan
     constexpr int kBC = (kRows * kNP + 32 * kPer - 1) / (32 * kPer);       // accesses of a lane to each
     __shared__ __align__(16) float2 s_pairs[kScanWarps][kRows * kPitch];                   // (dt, dt u), later (o, -)
     __shared__ __align__(16) float s_states[kScanWarps][kKinds * kRows * kNP];           // [B, C][step][state]
+    griddep_wait();
+    if (kMode != kScanForward) griddep_launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long unit = blockIdx.x * static_cast<long long>(kScanWarps) + warp;
     const int chunks = kMode == kScanForward ? p.chunks : p.chunks - 1;
@@ -421,6 +423,8 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
         float2 sum_D[4][32], sum_bias[4][32];             // of the lane's channels, over its rows
     };
     extern __shared__ __align__(16) unsigned char scan_smem[];
+    griddep_wait();
+    griddep_launch_dependents();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     Warp &w = reinterpret_cast<Warp *>(scan_smem)[warp];
     float *const s_sum = reinterpret_cast<float *>(scan_smem + kScanWarps * sizeof(Warp));      // [2][kScanWarps][kRows][2][kNP]: dB, dC
@@ -796,6 +800,7 @@ template <typename T>
 __global__ void __launch_bounds__(kScanFinishThreads) ptq_scan_finish_kernel(const ScanParams p, float *dA, float *dD, float *dbias, int blocks_A, int blocks_D)
 {
     __shared__ float s[32][33];
+    griddep_wait();
     const long long rows = static_cast<long long>(p.batch) * p.chunks;
     int block = blockIdx.x;
     if (block < blocks_A + 2 * blocks_D) {

@@ -92,6 +92,8 @@ ptq_status_t ScanLaunch<T>::forward(int mode, const ptq::ScanParams &p, const Sc
             constexpr int kThreads = ptq::kScanWarps * 32;
             constexpr bool kWhole = decltype(whole)::value;
             const unsigned grid = static_cast<unsigned>(ceil_div(cut.warps, ptq::kScanWarps));
+            if (mode == ptq::kScanForward && p.chunks > 1)
+                return launch_next(ptq::ptq_scan_kernel<T, F::channels, F::states, F::lanes, ptq::kScanForward, kWhole>, grid, kThreads, 0, stream, p);
             if (mode == ptq::kScanForward)
                 ptq::ptq_scan_kernel<T, F::channels, F::states, F::lanes, ptq::kScanForward, kWhole><<<grid, kThreads, 0, stream>>>(p);
             else if (mode == ptq::kScanSum)
@@ -111,6 +113,7 @@ ptq_status_t ScanLaunch<T>::backward(const ptq::ScanParams &p, const ScanCut &cu
             constexpr auto kKern = ptq::ptq_scan_backward_kernel<T, F::channels, F::states, F::lanes, decltype(whole)::value>;
             constexpr size_t kBytes = ptq::scan_backward_smem(F::channels, F::states, F::lanes, sizeof(T));
             PTQ_TRY(ensure_smem<kKern>(static_cast<int>(kBytes)));
+            if (p.chunks > 1) return launch_next(kKern, static_cast<unsigned>(cut.ctas), ptq::kScanWarps * 32, kBytes, stream, p);
             kKern<<<static_cast<unsigned>(cut.ctas), ptq::kScanWarps * 32, kBytes, stream>>>(p);
             return launched();
         });
@@ -123,8 +126,8 @@ ptq_status_t ScanLaunch<T>::finish(const ptq::ScanParams &p, float *dA, float *d
     const int blocks_D = static_cast<int>(ceil_div(p.channels, 32));
     const long long sets = p.part_BC ? ceil_div(static_cast<long long>(p.batch) * p.length, ptq::kScanFinishThreads / (2 * p.states)) * p.groups : 0;
     const int blocks_BC = static_cast<int>(std::min<long long>(sets, 2 * kSms));
-    ptq::ptq_scan_finish_kernel<T><<<blocks_A + 2 * blocks_D + blocks_BC, ptq::kScanFinishThreads, 0, stream>>>(p, dA, dD, dbias, blocks_A, blocks_D);
-    return launched();
+    return launch_next(ptq::ptq_scan_finish_kernel<T>, static_cast<unsigned>(blocks_A + 2 * blocks_D + blocks_BC), ptq::kScanFinishThreads, 0, stream, p,
+                       dA, dD, dbias, blocks_A, blocks_D);
 }
 template <typename T>
 ptq_status_t ScanLaunch<T>::step(const ptq::ScanParams &p, bool whole_rows, cudaStream_t stream)
