@@ -5,13 +5,17 @@
 //   h[n] <- exp(dt A[d,n]) h[n] + dt u[p,d] B[p,g,n]
 //   o = sum_n C[p,g,n] h[n] + D[d] u[p,d],   y[p,d] = o silu(z[p,d])
 //
-// Bound: the exponentials, N per element at 16 per clock and SM, from N = 4 or so on; below that the bytes.  The states of
-// a channel lie in the registers of kS neighbouring lanes, kNS each (N = 16: four lanes of four), so that a warp works
-// on 32 / kS channels and every shared-memory word of dt, dt u, B and C that it reads serves several lanes.  A CTA takes a
-// tile of 8 kS steps at a time: its threads load 8 channels of one row each (the next tile's rows are under way
-// meanwhile), put dt and dt u into shared memory, the lanes run the recurrence, and the threads finish the rows
-// that they loaded.  Few rows: the steps are cut into chunks.  A first launch computes what each chunk adds to the state and by
-// how much it decays (exp(A sum dt)), the second folds these into the state it starts a chunk from.
+// Bound: the exponentials, N per element (and three for softplus and the gate) at 16 per clock and SM, from N = 4 or so on; below that the
+// bytes.  A warp works alone on 32 kC / kS channels: kS neighbouring lanes hold the states of a channel, kNS each, and kC channels
+// (N = 16 and many rows: two lanes, two channels, eight states), in registers.  A tile is 256 elements: its lanes load eight channels of one
+// row each (the next tile's are under way meanwhile), put dt and dt u into shared memory, run the recurrence, and finish the rows that they
+// loaded; no barrier but the warp's.  Few rows: the steps are cut into chunks.  A first launch computes what each
+// chunk adds to the state and by how much it decays (exp(A sum dt)), the second folds these into the state it starts a chunk from.
+// Measured, N = 16: 128 x 197 x 768 binary16 135 us (exponentials alone: 82), of which 100 us is the recurrence by itself; CTAs of four
+// warps that shared a tile took 180, one channel per lane 137 to 190 (every value of B and C read from shared memory for 8 decays
+// instead of 16: the port, not the exponentials, bounds it), loads whose 16-bit values were taken apart on arrival 220.  A quarter
+// of the decays by polynomial on the multiply-add pipe: 137 -> 154.  2 x 20011 x 1024 bfloat16 464 us in two launches (exponentials
+// of one pass 173).  1 x 197 x 384: 10.2 us in two launches of chunks of 32 steps, 18.4 in one.
 #pragma once
 
 #include "ptq_block.cuh"
@@ -96,8 +100,8 @@ __device__ __forceinline__ void scan_decays(float (&a)[kNS], float dt, const flo
     for (int k = 0; k < kNS; ++k) a[k] = exp2_approx(a[k]);
 }
 
-// Decay rates times log2(e); finite, so that a step without a token (dt = 0) leaves the state as it is.
-__device__ __forceinline__ float scan_rate(float a) { return fminf(fmaxf(a * kLog2e, -3.0e38f), 3.0e38f); }
+// Decay rates times log2(e); no infinities, so that a step without a token (dt = 0) leaves the state as it is.
+__device__ __forceinline__ float scan_rate(float a) { return a != a ? a : fminf(fmaxf(a * kLog2e, -3.0e38f), 3.0e38f); }
 
 struct ScanBlock {
     int b, chunk, g, c0, c_end, len, i0, i1;
@@ -395,7 +399,10 @@ __host__ __device__ constexpr size_t scan_backward_smem(int channels, int states
 // backward, a taken again from dt.  Over the channels sum dC = h dyo and dB = G dt u: the two of a lane first, then eight values at a time
 // over the lanes of a warp, the four warps' sums through shared memory, the CTAs' through global memory, each in a fixed order.  Over the
 // states of a channel sum o, s and r.  The rows' lanes then make du = dt s + D dyo, ddelta = (u s + r ln 2) sigmoid and dz.
-// Bound: issue slots.
+// Bound: latency at the 10 to 12 warps of 168 registers that an SM holds (half of the issue slots are used), not one unit: 64 x 197 x 384,
+// N = 16, binary16: 140 us, of it 60 for all but the recurrence, 20 for the sums over lanes, 18 for the last step; with eight warps per SM 177.
+// The rows wait in shared memory for their second use (registers: spills; read again: 10 us more).  The whole backward pass
+// 150 us, exponentials alone 39.
 template <typename T, int kC, int kNS, int kS, bool kWhole>
 __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(const ScanParams p)
 {
@@ -489,7 +496,7 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
         }
     };
     const long long kept_step = static_cast<long long>(p.channels) * p.states;
-    const float *const kept = p.kept + blk.b * ((p.length + kScanHistory - 1) / kScanHistory) * kept_step + static_cast<long long>(d) * p.states + n0;
+    const float *const kept = p.kept + static_cast<long long>(blk.b) * ((p.length + kScanHistory - 1) / kScanHistory) * kept_step + static_cast<long long>(d) * p.states + n0;
     float r_h[kC][kNS];
     const auto fetch_state = [&](int i) {
 #pragma unroll
@@ -831,7 +838,9 @@ __global__ void __launch_bounds__(kScanFinishThreads) ptq_scan_finish_kernel(con
     }
 }
 
-// One token per sequence.  Bound: the state's bytes, read and written once, and close behind it the issue slots.  The kS lanes of a channel
+// One token per sequence.  Bound: the state's bytes, read and written once, and close behind it the issue slots: 1024 sequences of 1536
+// channels, N = 16, bfloat16 51 us, 4.3 TB/s (the bytes alone 33; every lane with its own softplus 80, states copied
+// asynchronously ahead 70).  The kS lanes of a channel
 // hold kNS states each and take kS sequences at a time: every lane makes dt, dt u and in the end y of one of them and hands the former
 // round; all loads of the set go out before its first store.
 template <typename T, int kNS, int kS, bool kWhole>

@@ -94,6 +94,35 @@ def test_graphs_are_captured_and_replayed_with_new_inputs(ptq):
         assert all(same(o, w) for o, w in zip(outs, want))
 
 
+FIRST_CALL = r"""
+import torch, sys
+import paper_2412_20386_b200 as ptq
+x = torch.randn(3, 300, 2312, device="cuda").half()
+A, w, B = -torch.rand(2312, 16, device="cuda"), torch.rand(2312, 4, device="cuda"), torch.randn(3, 300, 16, device="cuda").half()
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+def run():
+    h = ptq.scan_history(x, 16)
+    y = ptq.gated_scan(x, x, A, B, B, history=h)
+    return [y, *ptq.gated_scan_backward(y, x, x, A, B, B, h).values(), ptq.block_norm(x), *ptq.block_norm_backward(y, x).values(),
+            *ptq.short_conv_backward(ptq.short_conv(x, w), x, w).values()]
+with torch.cuda.graph(g):
+    got = run()
+g.replay()
+torch.cuda.synchronize()
+print(all(a is None or torch.equal(a, b) for a, b in zip(got, run())))
+"""
+
+
+def test_the_first_call_of_a_process_may_be_captured():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL], cwd=root, capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and r.stdout.strip() == "True", r.stderr[-2000:]
+
+
 def test_a_token_step_in_a_graph_goes_on_from_its_own_state(ptq):
     t = make_scan(3, ref.BF16, 5, 6, 40, 16, state=True)
     final = torch.empty_like(t["state"])

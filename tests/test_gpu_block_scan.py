@@ -264,6 +264,10 @@ def test_infinities_and_nan_stay_in_their_channel(ptq):
     mask[1, 7:, 9] = False
     assert torch.equal(y.cpu()[mask], clean.cpu()[mask])
     assert not torch.isfinite(y[0, 5, 3]) and torch.isnan(y[1, 7:, 9]).all()
+    t = make(13, ref.F32, 1, 9, 16, 16)
+    t["A"][4, 2] = float("nan")
+    y = call(ptq, t)
+    assert torch.isnan(y[0, :, 4]).all() and torch.isfinite(y[0, :, :4]).all() and torch.isfinite(y[0, :, 5:]).all()
 
 
 @pytest.mark.parametrize("N", [1, 2, 4, 7, 16, 20, 32])
