@@ -404,21 +404,22 @@ __device__ __forceinline__ int first_sum(int lane)
 }
 
 // Column sums of the partial results of other CTAs, in the order of the rows: the sum of part[r * pitch] for r < rows.  Called by all of
-// a CTA of 32 x 32 threads, one column per lane (`on`: it has one), every 32nd row per warp; the result is the first warp's.
-__device__ __forceinline__ float sum_rows(const float *part, long long rows, long long pitch, bool on, float (&s)[32][33])
+// a CTA of kWarps warps, one column per lane (`on`: it has one), every kWarps-th row per warp; the result is the first warp's.
+template <int kWarps>
+__device__ __forceinline__ float sum_rows(const float *part, long long rows, long long pitch, bool on, float (&s)[kWarps][33])
 {
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
     float v = 0.0f;
     if (on) {
 #pragma unroll 8
-        for (long long r = y; r < rows; r += 32) v += part[r * pitch];
+        for (long long r = y; r < rows; r += kWarps) v += part[r * pitch];
     }
     s[y][x] = v;
     __syncthreads();
     v = 0.0f;
     if (y == 0) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v += s[i][x];
+        for (int i = 0; i < kWarps; ++i) v += s[i][x];
     }
     return v;
 }

@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(1024) ptq_conv_finish_kernel(const float *part
     griddep_wait();
     const int col = blockIdx.x * 32 + (threadIdx.x & 31), j = blockIdx.y;
     if (j == taps && !dbias) return;
-    const float v = sum_rows(part + static_cast<long long>(j) * cols + col, rows, static_cast<long long>(taps + 1) * cols, col < cols, s);
+    const float v = sum_rows<32>(part + static_cast<long long>(j) * cols + col, rows, static_cast<long long>(taps + 1) * cols, col < cols, s);
     if (threadIdx.x >= 32 || col >= cols) return;
     if (j < taps)
         dweight[static_cast<long long>(col) * taps + j] = v;

@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(1024) ptq_norm_finish_kernel(const float *part
     const int col = blockIdx.x * 32 + (threadIdx.x & 31);
     float *out = blockIdx.y == 0 ? dweight : blockIdx.y == 1 ? dbias : dscale;
     if (!out) return;
-    const float v = sum_rows(part + static_cast<long long>(blockIdx.y) * cols + col, rows, 3ll * cols, col < cols, s);
+    const float v = sum_rows<32>(part + static_cast<long long>(blockIdx.y) * cols + col, rows, 3ll * cols, col < cols, s);
     if (threadIdx.x < 32 && col < cols) out[col] = v;
 }
 

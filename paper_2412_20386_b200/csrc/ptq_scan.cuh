@@ -802,11 +802,11 @@ __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(c
 }
 
 // The shares of the CTAs of the backward pass: dA, dD and ddelta_bias over the sequences and chunks, dB and dC over the CTAs of a group.
-constexpr int kScanFinishThreads = 1024;    // the threads behind the last whole token have nothing to do
+constexpr int kScanFinishThreads = 256;     // the threads behind the last whole token have nothing to do
 template <typename T>
 __global__ void __launch_bounds__(kScanFinishThreads) ptq_scan_finish_kernel(const ScanParams p, float *dA, float *dD, float *dbias, int blocks_A, int blocks_D)
 {
-    __shared__ float s[32][33];
+    __shared__ float s[kScanFinishThreads / 32][33];
     griddep_wait();
     const long long rows = static_cast<long long>(p.batch) * p.chunks;
     int block = blockIdx.x;
@@ -816,7 +816,7 @@ __global__ void __launch_bounds__(kScanFinishThreads) ptq_scan_finish_kernel(con
         if (!out) return;
         const long long cols = is_A ? static_cast<long long>(p.channels) * p.states : p.channels;
         const long long col = (is_A ? block : (block - blocks_A) % blocks_D) * 32ll + (threadIdx.x & 31);
-        const float v = sum_rows((is_A ? p.part_A : is_D ? p.part_D : p.part_bias) + col, rows, cols, col < cols, s);
+        const float v = sum_rows<kScanFinishThreads / 32>((is_A ? p.part_A : is_D ? p.part_D : p.part_bias) + col, rows, cols, col < cols, s);
         if (threadIdx.x < 32 && col < cols) out[col] = v;
         return;
     }

@@ -125,7 +125,7 @@ ptq_status_t ScanLaunch<T>::finish(const ptq::ScanParams &p, float *dA, float *d
     const int blocks_A = static_cast<int>(ceil_div(static_cast<long long>(p.channels) * p.states, 32));
     const int blocks_D = static_cast<int>(ceil_div(p.channels, 32));
     const long long sets = p.part_BC ? ceil_div(static_cast<long long>(p.batch) * p.length, ptq::kScanFinishThreads / (2 * p.states)) * p.groups : 0;
-    const int blocks_BC = static_cast<int>(std::min<long long>(sets, 2 * kSms));
+    const int blocks_BC = static_cast<int>(std::min<long long>(sets, 8 * kSms));
     return launch_next(ptq::ptq_scan_finish_kernel<T>, static_cast<unsigned>(blocks_A + 2 * blocks_D + blocks_BC), ptq::kScanFinishThreads, 0, stream, p,
                        dA, dD, dbias, blocks_A, blocks_D);
 }
