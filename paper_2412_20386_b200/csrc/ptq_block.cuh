@@ -201,25 +201,41 @@ __device__ __forceinline__ void store_piece(T *p, const float (&f)[kE], int n, i
     store_piece<kWhole, T, kE>(p, r, n, unit);
 }
 
+// Copies kBytes to shared memory without waiting for them; zeros, and nothing is read, unless `on`.
+template <int kBytes>
+__device__ __forceinline__ void copy_async(uint32_t to, const void *from, bool on)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(kBytes), "r"(on ? kBytes : 0) : "memory");
+}
+
 // A piece on its way to shared memory, its 16-byte parts at to[0], to[apart], ... (one thread's of a row of threads, so that no two of them
-// meet a bank): asynchronous where accesses of 16 bytes are allowed.  The thread that asked for it may read it after staged().
+// meet a bank).  The thread that asked for it may read it after staged().  General rows are copied in units of 8 or 4 bytes; what is
+// aligned to 2 bytes only is loaded and stored.
 template <bool kWhole, typename T, int kE>
 __device__ __forceinline__ void stage_piece(uint4 *to, const T *p, int n, int apart = 32, int unit = 1)
 {
     static_assert(kE * sizeof(T) % 16 == 0, "whole parts");
     constexpr int kParts = kE * static_cast<int>(sizeof(T)) / 16, kElems = 16 / static_cast<int>(sizeof(T));
+    const uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(to));
     if constexpr (kWhole) {
-        const uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(to));
 #pragma unroll
         for (int i = 0; i < kParts; ++i) {
             const int bytes = n >= (i + 1) * kElems ? 16 : 0;      // the rest of the 16 is filled with zeros, nothing is read for none
             if constexpr (kParts == 1)
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + 16 * apart * i), "l"(p + i * kElems), "r"(bytes) : "memory");
             else                                           // half a sector: the other part finds it in the first-level cache
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(at + 16 * apart * i), "l"(p + i * kElems), "r"(bytes) : "memory");
+                copy_async<16>(at + 16 * apart * i, p + i * kElems, bytes > 0);
         }
+    } else if (sizeof(T) == 4 || unit == 2) {
+        constexpr int kStep = 4 / static_cast<int>(sizeof(T));
+#pragma unroll
+        for (int e = 0; e < kE; e += kStep) copy_async<4>(at + 16 * apart * (e / kElems) + e % kElems * static_cast<int>(sizeof(T)), p + e, n >= e + kStep);
+    } else if (unit >= 4) {
+        constexpr int kStep = 8 / static_cast<int>(sizeof(T));
+#pragma unroll
+        for (int e = 0; e < kE; e += kStep) copy_async<8>(at + 16 * apart * (e / kElems) + e % kElems * static_cast<int>(sizeof(T)), p + e, n >= e + kStep);
     } else {
-        const Piece<T, kE> r = load_piece<false, T, kE>(p, n, unit);
+        const Piece<T, kE> r = load_piece<false, T, kE>(p, n);
 #pragma unroll
         for (int i = 0; i < kParts; ++i) to[apart * i] = make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]);
     }
