@@ -10,7 +10,7 @@
  * Activations are token-major, [batch, token, channel], of one type per call, with the channels of a token next to
  * each other and any pitch between tokens and between sequences (in elements, not negative): the halves of in_proj's
  * output and the columns of x_proj's are passed as they lie.  Pointers are aligned to their type; rows whose
- * pointers and pitches are multiples of 16 bytes are moved 16 bytes at a time.  Parameters, states of the
+ * pointers and pitches are multiples of 16 bytes are moved 16 bytes at a time.  The pitches of an input that is NULL are ignored.  Parameters, states of the
  * recurrence and gradients of parameters are binary32.  Arithmetic is binary32 throughout; a result is
  * rounded to its type once.  Outputs are dense unless their pitch is an argument, and overlap no input but
  * where a function says so.  Sums have a fixed order: the same call gives the same bits.

@@ -114,12 +114,13 @@ ptq_status_t scan_check(const ptq_scan_t *s)
                     s->groups);
     if (s->channels % s->groups) return fail(PTQ_ERR_SHAPE, "%d channels do not make %d groups", s->channels, s->groups);
     if (s->flags & ~(PTQ_SCAN_SOFTPLUS | PTQ_SEQ_REVERSE)) return fail(PTQ_ERR_VALUE, "unknown flags %u", s->flags);
-    if (!not_negative({s->u_pitch[0], s->u_pitch[1], s->delta_pitch[0], s->delta_pitch[1], s->z_pitch[0], s->z_pitch[1], s->B_pitch[0], s->B_pitch[1],
-                       s->B_pitch[2], s->C_pitch[0], s->C_pitch[1], s->C_pitch[2]}))
+    if (!not_negative({s->u_pitch[0], s->u_pitch[1], s->delta_pitch[0], s->delta_pitch[1], s->z ? s->z_pitch[0] : 0, s->z ? s->z_pitch[1] : 0,
+                       s->B_pitch[0], s->B_pitch[1], s->B_pitch[2], s->C_pitch[0], s->C_pitch[1], s->C_pitch[2]}))
         return fail(PTQ_ERR_SHAPE, "a pitch is negative");
     if (!aligned({s->u, s->delta, s->z, s->B, s->C}, elem_bytes(s->dtype)) || !aligned({s->A, s->D, s->delta_bias, s->state, s->lengths}, 4))
         return fail(PTQ_ERR_ALIGN, "an input is not aligned to its type");
-    if (const ScanPlan plan = scan_plan(*s); std::max(plan.warps, plan.ctas) * plan.chunks > kMaxGrid) return fail(PTQ_ERR_SHAPE, "the batch is too large for one launch");
+    if (const ScanPlan plan = scan_plan(*s); std::max(plan.warps, plan.ctas) * plan.chunks > kMaxGrid)
+        return fail(PTQ_ERR_SHAPE, "the batch is too large for one launch");
     return PTQ_OK;
 }
 
@@ -135,8 +136,8 @@ ptq::ScanParams scan_params(const ptq_scan_t &s, const ScanPlan &plan)
     p.u_l = s.u_pitch[1];
     p.delta_b = s.delta_pitch[0];
     p.delta_l = s.delta_pitch[1];
-    p.z_b = s.z_pitch[0];
-    p.z_l = s.z_pitch[1];
+    p.z_b = s.z ? s.z_pitch[0] : 0;
+    p.z_l = s.z ? s.z_pitch[1] : 0;
     p.B_b = s.B_pitch[0];
     p.B_l = s.B_pitch[1];
     p.B_g = s.B_pitch[2];
@@ -230,7 +231,7 @@ ptq_status_t norm_check(const ptq_norm_t *n)
         return fail(PTQ_ERR_SHAPE, "rows %lld, cols %d out of range", static_cast<long long>(n->rows), n->cols);
     if (n->flags & ~(PTQ_NORM_LAYER | PTQ_NORM_GATE_OUT)) return fail(PTQ_ERR_VALUE, "unknown flags %u", n->flags);
     if (!(n->eps >= 0.0f) || std::isinf(n->eps)) return fail(PTQ_ERR_VALUE, "eps must be finite and not negative");
-    if (!not_negative({n->x_pitch, n->residual_pitch, n->gate_pitch})) return fail(PTQ_ERR_SHAPE, "a pitch is negative");
+    if (!not_negative({n->x_pitch, n->residual ? n->residual_pitch : 0, n->gate ? n->gate_pitch : 0})) return fail(PTQ_ERR_SHAPE, "a pitch is negative");
     if (!aligned({n->x, n->gate}, elem_bytes(n->dtype)) || !aligned({n->residual}, elem_bytes(n->residual_dtype)) ||
         !aligned({n->weight, n->bias, n->scale}, 4))
         return fail(PTQ_ERR_ALIGN, "an input is not aligned to its type");

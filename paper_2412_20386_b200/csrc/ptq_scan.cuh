@@ -5,17 +5,18 @@
 //   h[n] <- exp(dt A[d,n]) h[n] + dt u[p,d] B[p,g,n]
 //   o = sum_n C[p,g,n] h[n] + D[d] u[p,d],   y[p,d] = o silu(z[p,d])
 //
-// Bound: the exponentials, N per element (and three for softplus and the gate) at 16 per clock and SM, from N = 4 or so on; below that the
-// bytes.  A warp works alone on 32 kC / kS channels: kS neighbouring lanes hold the states of a channel, kNS each, and kC channels
+// Bound: the port on which exponentials and shared-memory reads return to the registers (16 powers of two of a warp 71 cycles with three warps
+// per scheduler, with four 16-byte reads beside them 135), from N = 4 or so on; below that issue slots and bytes.  A warp works alone on 32 kC / kS channels: kS neighbouring lanes hold the states of a channel, kNS each, and kC channels
 // (N = 16 and many rows: two lanes, two channels, eight states), in registers.  A tile is 256 elements: its lanes load eight channels of one
 // row each (the next tile's are under way meanwhile), put dt and dt u into shared memory, run the recurrence, and finish the rows that they
 // loaded; no barrier but the warp's.  Few rows: the steps are cut into chunks.  A first launch computes what each
 // chunk adds to the state and by how much it decays (exp(A sum dt)), the second folds these into the state it starts a chunk from.
-// Measured, N = 16: 128 x 197 x 768 binary16 135 us (exponentials alone: 82), of which 100 us is the recurrence by itself; CTAs of four
+// Measured, N = 16: 128 x 197 x 768 binary16 135 us (the N + 3 exponentials per element
+// alone: 45), of which 100 us is the recurrence by itself; CTAs of four
 // warps that shared a tile took 180, one channel per lane 137 to 190 (every value of B and C read from shared memory for 8 decays
-// instead of 16: the port, not the exponentials, bounds it), loads whose 16-bit values were taken apart on arrival 220.  A quarter
+// instead of 16), loads whose 16-bit values were taken apart on arrival 220.  A quarter
 // of the decays by polynomial on the multiply-add pipe: 137 -> 154.  2 x 20011 x 1024 bfloat16 464 us in two launches (exponentials
-// of one pass 173).  1 x 197 x 384: 10.2 us in two launches of chunks of 32 steps, 18.4 in one.
+// of one pass 95).  1 x 197 x 384: 10.2 us in two launches of chunks of 32 steps, 18.4 in one.
 #pragma once
 
 #include "ptq_block.cuh"
@@ -53,7 +54,7 @@ struct ScanParams {
     float *part_BC;                             // [groups * group_blocks][batch][length][2 states], null: straight to dB, dC
 };
 
-// The same of two values: t = e^-|x| and log(1 + e^x) = max(x, 0) + log(1 + t).  The argument of the power of two is carried to about 2^-46
+// Of two values: t = e^-|x| and log(1 + e^x) = max(x, 0) + log(1 + t).  The argument of the power of two is carried to about 2^-46
 // (its rounding alone would cost four units in the last place at |x| = 7); |x| is cut at 126, where t is zero.  log(1 + t) / t is a
 // polynomial fitted to 5e-9 on [0, 1]: accurate relative to the result, small ones too, with half the instructions of expf and log1pf.
 __device__ __forceinline__ void exp_minus_abs_pair(float &t0, float &t1, float x0, float x1)
@@ -402,7 +403,7 @@ __host__ __device__ constexpr size_t scan_backward_smem(int channels, int states
 // Bound: latency at the 10 to 12 warps of 168 registers that an SM holds (half of the issue slots are used), not one unit: 64 x 197 x 384,
 // N = 16, binary16: 140 us, of it 60 for all but the recurrence, 20 for the sums over lanes, 18 for the last step; with eight warps per SM 177.
 // The rows wait in shared memory for their second use (registers: spills; read again: 10 us more).  The whole backward pass
-// 150 us, exponentials alone 39.
+// 150 us, exponentials alone 22.
 template <typename T, int kC, int kNS, int kS, bool kWhole>
 __global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(const ScanParams p)
 {

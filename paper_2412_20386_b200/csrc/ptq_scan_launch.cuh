@@ -9,8 +9,9 @@
 namespace ptq_host {
 
 // Lanes per channel, channels of a lane and states of each.  Forward, a lane has two channels: the values of B and C that it reads from
-// shared memory serve both, and reading them for one channel each (18 cycles of the port per step and 256 decays, 72 for the four
-// schedulers, whose decays take 64) bound the kernel.  Where that leaves few warps, a channel has more lanes.
+// shared memory serve both (128 x 197 x 768, N = 16: 135 us; one channel of eight states 145, of four 183; four channels 148, too few warps).
+// Where two lanes a channel leave few warps, a channel has four, with two channels a lane or with one (64 x 197 x 384: 46 and 60 us;
+// 1 x 197 x 384 in one pass: 18 with one channel a lane).
 struct ScanSplit {
     int lanes, channels, states;
     int width() const { return 32 / lanes * channels; }

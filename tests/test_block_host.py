@@ -96,6 +96,9 @@ def test_scan_refusals(lib):
     for kw in (dict(u=P + 1), dict(A=P + 2), dict(state=P + 2), dict(lengths=P + 1), dict(z=P + 1)):
         assert forward(lib, scan(**kw)) == ALIGN, kw
     assert forward(lib, scan(), y=P + 1) == ALIGN and forward(lib, scan(), final=P + 2) == ALIGN
+    if not torch.cuda.is_available():                        # the pitches of what is not given do not count: as far as the device
+        assert forward(lib, scan(z_pitch=(-1, -1))) in (ARCH, CUDA)
+        assert lib.ptq_norm_forward(ctypes.byref(norm(gate_pitch=-1, residual_pitch=-1)), vp(P), None, None) in (ARCH, CUDA)
     need = lib.ptq_scan_workspace_bytes(ctypes.byref(scan(length=4000)), 0)
     assert need > 0
     assert forward(lib, scan(length=4000), ws=None) == NULL
