@@ -64,18 +64,20 @@ ptq_status_t with_type(int dtype, Fn fn)
 }
 
 // ---------------------------------------------------------------------------------------------------- scan
-// How a call is cut.  The forward pass and the backward pass cut the sequences alike, so that one rule sizes both workspaces.
+// How a call is cut.
 struct ScanPlan {
     ScanSplit split;                  // of the forward pass
     int group_warps, group_blocks, chunk_len, chunks;
     long long warps, ctas;            // of one chunk
     ScanCut cut(int n, bool whole) const { return {split, warps * n, ctas * n, whole}; }
 };
-// Chunks of a multiple of 32 steps.  The time goes as the steps of a chunk and as the sets of warps that the GPU holds at once (12 to
-// an SM).  More than one chunk: everything but the output is gone over twice, there is another launch
+// Chunks of a multiple of 32 steps.  The time goes as the steps of a chunk and as the sets of warps that the GPU holds at once: 12 to an
+// SM, 16 where a lane has two states at most and, in the backward pass, rows of 16-bit values (binary32 rows fill the shared memory: 32 x 784
+// x 384 with one state, 16 assumed: fp16 training 187 -> 167 us, fp32 192 -> 224).  More than one chunk: everything but the output is gone over twice, there is another launch
 // (about 60 steps), and the last chunk folds the others' sums.
-ScanPlan scan_plan(const ptq_scan_t &s)
+ScanPlan scan_plan(const ptq_scan_t &s, bool backward)
 {
+    const double resident = (s.states <= 2 && (!backward || s.dtype != PTQ_F32) ? 16.0 : 12.0) * kSms;
     const int per_group = s.channels / s.groups;
     const long long sequences = static_cast<long long>(s.batch) * s.groups;
     ScanPlan p;
@@ -86,7 +88,7 @@ ScanPlan scan_plan(const ptq_scan_t &s)
     double least = -1.0;
     for (long long n = 1; n <= ceil_div(s.length, 32) && n <= 512; n = n < 16 ? n + 1 : n + n / 8) {
         const double len = 32.0 * static_cast<double>(ceil_div(ceil_div(s.length, n), 32));
-        const double load = std::max(1.0, std::ceil(filled * static_cast<double>(warps) * n / (12.0 * kSms) - 0.02));
+        const double load = std::max(1.0, std::ceil(filled * static_cast<double>(warps) * n / resident - 0.02));
         const double cost = n == 1 ? s.length * load : 1.8 * len * load + 60.0 + 2.0 * n;
         if (least < 0.0 || cost < least) {
             least = cost;
@@ -119,8 +121,11 @@ ptq_status_t scan_check(const ptq_scan_t *s)
         return fail(PTQ_ERR_SHAPE, "a pitch is negative");
     if (!aligned({s->u, s->delta, s->z, s->B, s->C}, elem_bytes(s->dtype)) || !aligned({s->A, s->D, s->delta_bias, s->state, s->lengths}, 4))
         return fail(PTQ_ERR_ALIGN, "an input is not aligned to its type");
-    if (const ScanPlan plan = scan_plan(*s); std::max(plan.warps, plan.ctas) * plan.chunks > kMaxGrid)
-        return fail(PTQ_ERR_SHAPE, "the batch is too large for one launch");
+    return PTQ_OK;
+}
+ptq_status_t scan_check(const ScanPlan &plan)
+{
+    if (std::max(plan.warps, plan.ctas) * plan.chunks > kMaxGrid) return fail(PTQ_ERR_SHAPE, "the batch is too large for one launch");
     return PTQ_OK;
 }
 
@@ -391,7 +396,7 @@ size_t ptq_scan_workspace_bytes(const ptq_scan_t *s, int backward)
     if (!s || s->batch < 1 || s->length < 1 || s->length > PTQ_MAX_LENGTH || s->channels < 1 || s->channels > PTQ_MAX_CHANNELS || s->states < 1 ||
         s->states > PTQ_MAX_STATES || s->groups < 1 || s->channels % s->groups)
         return 0;
-    return scan_space(*s, scan_plan(*s), backward != 0).bytes;
+    return scan_space(*s, scan_plan(*s, backward != 0), backward != 0).bytes;
 }
 
 ptq_status_t ptq_scan_forward(const ptq_scan_t *s, void *y, float *final_state, float *history, void *workspace, size_t workspace_bytes, void *stream)
@@ -399,7 +404,8 @@ ptq_status_t ptq_scan_forward(const ptq_scan_t *s, void *y, float *final_state, 
     PTQ_TRY(scan_check(s));
     if (!y) return fail(PTQ_ERR_NULL, "y is NULL");
     if (!aligned({y}, elem_bytes(s->dtype)) || !aligned({final_state, history}, 4)) return fail(PTQ_ERR_ALIGN, "an output is not aligned to its type");
-    const ScanPlan plan = scan_plan(*s);
+    const ScanPlan plan = scan_plan(*s, false);
+    PTQ_TRY(scan_check(plan));
     const ScanSpace space = scan_space(*s, plan, false);
     PTQ_TRY(check_space(workspace, workspace_bytes, space.bytes));
     PTQ_TRY(check_arch());
@@ -432,7 +438,8 @@ ptq_status_t ptq_scan_backward(const ptq_scan_t *s, const float *history, const 
     if (!aligned({dy, g->du, g->ddelta, g->dz, g->dB, g->dC}, elem_bytes(s->dtype)) ||
         !aligned({history, dfinal, g->dA, g->dD, g->ddelta_bias, g->dstate}, 4))
         return fail(PTQ_ERR_ALIGN, "an argument is not aligned to its type");
-    const ScanPlan plan = scan_plan(*s);
+    const ScanPlan plan = scan_plan(*s, true);
+    PTQ_TRY(scan_check(plan));
     const ScanSpace space = scan_space(*s, plan, true);
     PTQ_TRY(check_space(workspace, workspace_bytes, space.bytes));
     PTQ_TRY(check_arch());

@@ -145,7 +145,7 @@ __device__ __forceinline__ void scan_fold(float (&h)[kNS], const float (&rate)[k
 enum { kScanForward = 0, kScanSum = 1, kScanGradSum = 2 };
 
 template <typename T, int kC, int kNS, int kS, int kMode, bool kWhole>
-__global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_kernel(const ScanParams p)
+__global__ void __launch_bounds__(kScanWarps * 32, kC * kNS <= 2 ? 4 : 3) ptq_scan_kernel(const ScanParams p)
 {
     constexpr int kWidth = 32 / kS * kC, kPitch = kWidth + 2;      // channels of the warp; the pad keeps the rows' lanes off each other's banks
     constexpr int kRows = 256 / kWidth, kNP = kNS * kS;            // steps of a tile, states padded
@@ -405,7 +405,7 @@ __host__ __device__ constexpr size_t scan_backward_smem(int channels, int states
 // The rows wait in shared memory for their second use (registers: spills; read again: 10 us more).  The whole backward pass
 // 150 us, exponentials alone 22.
 template <typename T, int kC, int kNS, int kS, bool kWhole>
-__global__ void __launch_bounds__(kScanWarps * 32, 3) ptq_scan_backward_kernel(const ScanParams p)
+__global__ void __launch_bounds__(kScanWarps * 32, kC * kNS <= 2 && sizeof(T) == 2 ? 4 : 3) ptq_scan_backward_kernel(const ScanParams p)
 {
     constexpr int kWidth = 32 / kS * kC, kPitch = kWidth + 2;      // channels of a warp
     constexpr int kRows = 256 / kWidth, kNP = kNS * kS;            // steps of a tile, states padded
