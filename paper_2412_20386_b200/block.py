@@ -11,9 +11,11 @@ Activations are float16, bfloat16 or float32 tensors ``[batch, length, channels]
 be any distance apart (slices of a projection's output); parameters and recurrent states are float32.  Gradients are explicit
 calls: ``gated_scan_backward``, ``block_norm_backward`` and ``short_conv_backward`` take what the forward call took and return one
 gradient per tensor that was given, dense and in its shape (for an expanded tensor one value per token: the caller sums), in a dict
-by argument name.  They do not record anything for ``torch.autograd``.
+by argument name; ``dy`` and the gradients of further outputs are contiguous.  They do not record anything for ``torch.autograd``.
 
-``stream=None`` is the current stream of the tensors' device.  Outputs that are not passed are allocated by the call.
+``stream=None`` is the current stream of the tensors' device.  Outputs that are not passed are allocated by the call, on its stream;
+buffers that the caller passes (``scan_history`` among them, allocated on the current stream) must not be in use on another one.
+Outputs overlap no input unless a function says so.
 ``lengths`` (int32 ``[batch]`` on the device) makes a batch padded: rows behind a sequence's end are not read; a passed
 output is left as it is there, a new one holds zeros, and gradients are zeros.
 """
@@ -23,6 +25,7 @@ from . import binding
 
 FLAG_SEQ_REVERSE, FLAG_SCAN_SOFTPLUS, FLAG_CONV_SILU, FLAG_NORM_LAYER, FLAG_NORM_GATE_OUT = 2, 1, 1, 1, 2
 SCAN_HISTORY = 8                  # PTQ_SCAN_HISTORY: steps between two states that the backward pass starts from
+
 
 def _native():
     return binding._native_block or binding._load_native_block()
