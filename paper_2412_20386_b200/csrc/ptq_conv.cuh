@@ -93,7 +93,9 @@ __device__ __forceinline__ void conv_shift(float (&x)[kW][kE])
 }
 
 constexpr int kConvE = 4;             // channels of a thread: with eight, weights and window leave too few warps
-constexpr int kConvAhead = 2;         // rows that are loaded together, one set under way while the other is worked on
+// Rows that are loaded together, one set under way while the other is worked on.  With four the call above takes 56 us, with eight 66, of
+// which two take 50: the warps that the registers cost weigh more.
+constexpr int kConvAhead = 2;
 
 template <typename T, int kW, bool kWhole>
 __global__ void __launch_bounds__(256) ptq_conv_kernel(const ConvParams p)
