@@ -268,21 +268,26 @@ bool norm_whole(const ptq_norm_t &n)
     return aligned({n.x, n.residual, n.gate, n.weight, n.bias, n.scale}, 16) && multiples({n.x_pitch, n.gate ? n.gate_pitch : 0, n.cols}, unit) &&
            (!n.residual || n.residual_pitch % residual_unit == 0);
 }
-// Threads of a CTA, rows that it takes at a time, sets of rows and bytes of shared memory, CTAs.
+// Threads of a CTA, rows that it takes at a time, sets of rows, their layout and bytes in shared memory, CTAs.  The number of CTAs goes by the
+// description alone, since the workspace does: it takes a call with a residual to have a dresidual_out, and one without to have none.
 struct NormPlan {
     int threads, rows, stages, bytes, ctas;
+    ptq::NormStage stage;
 };
-NormPlan norm_plan(const ptq_norm_t &n, bool backward)
+NormPlan norm_plan(const ptq_norm_t &n, bool backward, bool has_dresidual)
 {
     NormPlan p;
     p.threads = static_cast<int>(ceil_div(n.cols, 256)) * 32;
     p.rows = p.threads > 256 || n.rows <= 8 * kSms ? 1 : backward ? 2 : 4;
-    const ptq::NormStage stage(n.residual, n.gate, backward, backward && n.residual, elem_bytes(n.dtype) / 2, elem_bytes(n.residual_dtype) / 2, p.rows,
-                               p.threads);
-    p.stages = 2 * 16 * stage.size <= 200 * 1024 ? 2 : 1;
-    p.bytes = p.stages * 16 * stage.size;
+    const auto lay_out = [&](bool dresidual) {
+        p.stage = ptq::norm_stage(n.residual, n.gate, backward, dresidual, elem_bytes(n.dtype) / 2, elem_bytes(n.residual_dtype) / 2, p.rows, p.threads);
+        p.stages = 2 * 16 * p.stage.size <= 200 * 1024 ? 2 : 1;
+        p.bytes = p.stages * 16 * p.stage.size;
+    };
+    lay_out(backward && n.residual);
     const int resident = std::max(1, std::min((backward ? 640 : 1024) / p.threads, 220 * 1024 / (p.bytes + 8 * 1024)));
     p.ctas = static_cast<int>(std::min<long long>(ceil_div(n.rows, p.rows), std::min(resident, 24) * kSms));
+    lay_out(backward && has_dresidual);
     return p;
 }
 template <bool kBackward>
@@ -482,15 +487,16 @@ ptq_status_t ptq_norm_forward(const ptq_norm_t *n, void *y, void *residual_out, 
     ptq::NormParams p = norm_params(*n);
     p.y = y;
     p.residual_out = residual_out;
-    const NormPlan plan = norm_plan(*n, false);
+    const NormPlan plan = norm_plan(*n, false, false);
     p.stages = plan.stages;
+    p.at = plan.stage;
     return launch_norm<false>(*n, plan, p, norm_whole(*n) && aligned({y, residual_out}, 16), static_cast<cudaStream_t>(stream));
 }
 
 size_t ptq_norm_workspace_bytes(const ptq_norm_t *n)
 {
     if (!n || n->rows < 1 || n->cols < 1 || n->cols > PTQ_MAX_NORM_COLS) return 0;
-    return padded(static_cast<size_t>(norm_plan(*n, true).ctas) * 3 * n->cols * 4);
+    return padded(static_cast<size_t>(norm_plan(*n, true, n->residual).ctas) * 3 * n->cols * 4);
 }
 
 ptq_status_t ptq_norm_backward(const ptq_norm_t *n, const void *dy, const void *dresidual_out, const ptq_norm_grads_t *g, void *workspace,
@@ -511,9 +517,10 @@ ptq_status_t ptq_norm_backward(const ptq_norm_t *n, const void *dy, const void *
     p.dresidual = g->dresidual;
     p.dgate = g->dgate;
     p.part = static_cast<float *>(workspace);
-    const NormPlan plan = norm_plan(*n, true);
+    const NormPlan plan = norm_plan(*n, true, dresidual_out);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     p.stages = plan.stages;
+    p.at = plan.stage;
     PTQ_TRY(launch_norm<true>(*n, plan, p, norm_whole(*n) && aligned({dy, dresidual_out, g->dx, g->dresidual, g->dgate}, 16), st));
     if (!g->dweight && !g->dbias && !g->dscale) return PTQ_OK;
     return launch_next(ptq::ptq_norm_finish_kernel, dim3(static_cast<unsigned>(ceil_div(n->cols, 32)), 3), 1024, 0, st, p.part, plan.ctas, n->cols, g->dweight,

@@ -18,6 +18,24 @@ namespace ptq {
 constexpr int kNormMaxWarps = 32;     // 8192 columns
 enum { kGateNone = 0, kGateIn = 1, kGateOut = 2 };
 
+// Where a thread's pieces of the rows lie in shared memory, in units of 16 bytes: kRB rows of each tensor that the call has.  The host makes
+// it, sizes the launch's shared memory by it and hands it over, so that the two cannot differ.
+struct NormStage {
+    int x, residual, gate, dy, dresidual, size;
+};
+inline NormStage norm_stage(bool has_residual, bool has_gate, bool has_dy, bool has_dresidual, int parts, int residual_parts, int rows, int threads)
+{
+    const int unit = rows * threads;
+    NormStage at;
+    at.x = 0;
+    at.residual = at.x + unit * parts;
+    at.gate = at.residual + (has_residual ? unit * residual_parts : 0);
+    at.dy = at.gate + (has_gate ? unit * parts : 0);
+    at.dresidual = at.dy + (has_dy ? unit * parts : 0);
+    at.size = at.dresidual + (has_dresidual ? unit * residual_parts : 0);
+    return at;
+}
+
 struct NormParams {
     const void *x, *residual, *gate;            // residual and gate may be null
     long long x_l, residual_l, gate_l;          // pitches in elements
@@ -27,6 +45,7 @@ struct NormParams {
     float eps, inv_cols;
     bool layer;
     int stages;                                 // sets of rows in shared memory
+    NormStage at;                               // of one set
     void *y, *residual_out;                     // dense
     // backward
     const void *dy, *dresidual_out;             // dense; dresidual_out may be null
@@ -78,21 +97,6 @@ __device__ __forceinline__ void store_columns(V *at, const float (&f)[8], int le
     }
 }
 
-// Where a thread's pieces of the rows lie in shared memory, in units of 16 bytes: kRB rows of each tensor that the call has.
-struct NormStage {
-    int x, residual, gate, dy, dresidual, size;
-    __host__ __device__ NormStage(bool has_residual, bool has_gate, bool has_dy, bool has_dresidual, int parts, int residual_parts, int rows, int threads)
-    {
-        const int unit = rows * threads;
-        x = 0;
-        residual = x + unit * parts;
-        gate = residual + (has_residual ? unit * residual_parts : 0);
-        dy = gate + (has_gate ? unit * parts : 0);
-        dresidual = dy + (has_dy ? unit * parts : 0);
-        size = dresidual + (has_dresidual ? unit * residual_parts : 0);
-    }
-};
-
 // kWide: rows of more than 2048 columns, up to 32 warps of 64 registers: the parameters are taken from the cache for every row.
 // The rows come through shared memory, one set of kRB under way while the other is worked on (p.stages = 2; 1 where a row is too wide
 // for that): held in registers, the loads of two sets would leave too few warps to keep the memory busy.
@@ -107,7 +111,7 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) ptq_norm_kernel(const Norm
     const int threads = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = threads >> 5;
     const int c = threadIdx.x * 8, left = p.cols - c, cn = max(min(8, left), 0);
     const bool has_dr = kBackward && p.dresidual_out;
-    const NormStage at(p.residual, p.gate, kBackward, has_dr, kParts, kResidualParts, kRB, threads);
+    const NormStage &at = p.at;
     float weight[8], bias[8], scale[8];
     const auto parameters = [&] {
         floats_of(weight, load_piece<kWhole, float, 8>(p.weight + c, p.weight ? cn : 0));
