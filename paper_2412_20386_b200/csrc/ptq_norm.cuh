@@ -221,6 +221,7 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) ptq_norm_kernel(const Norm
 #pragma unroll
         for (int i = 0; i < kRB; ++i) {
             rstd[i] = rsqrtf(fmaf(rstd[i], p.inv_cols, p.eps));
+            if (kBackward && i > 0 && m0 + i >= p.rows) rstd[i] = 0.0f;             // no row: zeros, whose 1 / rms is infinite without eps
             mul_each<8>(r[i], rstd[i], r[i]);                                        // n from here on
         }
         if constexpr (!kBackward) {
