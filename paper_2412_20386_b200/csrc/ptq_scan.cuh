@@ -122,6 +122,11 @@ struct ScanBlock {
     }
 };
 
+// The square root of a chunk's decay 2^(rate s).  Multiplied in twice it takes a state over a chunk whose decay itself leaves binary32: states that
+// grow (rates above zero, negative dt) by 2^138 in 32 steps of e^3, from nothing or from little.  It is kept finite and above zero, so that nothing
+// times any growth is nothing and an infinite state stays one, as step by step.
+__device__ __forceinline__ float chunk_decay_root(float rate, float s) { return exp2_approx(fminf(fmaxf(0.5f * (rate * s), -126.0f), 127.0f)); }
+
 // The state that enters a chunk, from what the chunks between it and `first` add: slot j holds the sum of chunk j alone (that of the
 // one next to the sequence's end holds the true state), sums[j] its dt.
 template <bool kWhole, int kNS>
@@ -136,7 +141,10 @@ __device__ __forceinline__ void scan_fold(float (&h)[kNS], const float (&rate)[k
         load_floats<kWhole, kNS>(v, p.slots + (j * step + row) * p.states + n0, nn);
         const float s = p.sums[j * step + row];
 #pragma unroll
-        for (int k = 0; k < kNS; ++k) h[k] = fmaf(exp2_approx(rate[k] * s), h[k], v[k]);
+        for (int k = 0; k < kNS; ++k) {
+            const float half = chunk_decay_root(rate[k], s);
+            h[k] = fmaf(half, half * h[k], v[k]);
+        }
     }
 }
 

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import block_ref as ref
+from parity_util import launches
 from test_gpu_block_norm import make as make_norm
 from test_gpu_block_norm_stream import check as check_norm
 
@@ -26,3 +27,47 @@ def test_norm_without_eps_and_an_incomplete_last_set_of_rows(ptq, kind, gate_at)
     for M, D in ((1185, 72), (1187, 264), (1187, 35)):
         check_norm(ptq, make_norm(M, ref.BF16, M, D, None, True, True), kind, gate_at, ref.BF16, eps=0.0)
     check_norm(ptq, make_norm(1, ref.F32, 1185, 40, None), kind, gate_at, None, eps=0.0)
+
+
+def growing(L, D, N):
+    """Rates above zero without softplus: dt is delta."""
+    gen = torch.Generator().manual_seed(L)
+    r = lambda *s: torch.rand(*s, generator=gen) * 0.5 + 0.5
+    t = {"u": r(1, L, D), "delta": torch.full((1, L, D), 3.0), "A": torch.ones(D, N), "B": r(1, L, N), "C": r(1, L, N)}
+    return {k: v.cuda() for k, v in t.items()}
+
+
+def test_states_that_grow_beyond_binary32_within_a_chunk_but_start_from_nothing(ptq):
+    """32 steps of e^3 are 2^138, more than binary32 holds; nothing comes in that they would multiply, in either direction, and the last eight
+    steps give e^21.  Bound: all terms are positive; a step's decay is off by 2^-22 + 3 (2^-21 + 2^-24), at most 2^-19, over eight steps."""
+    t = growing(200, 8, 16)
+    t["u"][:, :192] = 0.0
+    args = [t[k] for k in ("u", "delta", "A", "B", "C")]
+    final, history = torch.empty(1, 8, 16, device="cuda"), ptq.scan_history(t["u"], 16)
+    assert launches(ptq, lambda: ptq.gated_scan(*args, softplus=False)) == 2             # cut into chunks
+    y = ptq.gated_scan(*args, softplus=False, final_state=final, history=history)
+    x64 = ref.leaves(t)
+    y64, f64 = ref.scan(*(x64[k] for k in ("u", "delta", "A", "B", "C")), softplus=False)
+    ref.close(y, y64, y64.abs(), 2.0 ** -16, "y")
+    ref.close(final, f64, f64.abs(), 2.0 ** -16, "final state")
+    dy = torch.rand(1, 200, 8, device="cuda") + 0.5
+    dy[:, 8:] = 0.0                                         # the gradient of the state grows from here to the front
+    want = ref.gradients((y64, f64), (dy, None), x64)
+    got = ptq.gated_scan_backward(dy, *args, history, softplus=False)
+    for k in ("u", "delta", "A", "B", "C"):
+        ref.close(got[k], want[k], want[k].abs(), 2.0 ** -16, "gradient of " + k)
+
+
+def test_a_small_state_that_grows_by_more_than_binary32_holds(ptq):
+    """1e-20 times e^96 in one chunk of 32 steps.  Bound: 32 steps of 2^-19."""
+    t = growing(200, 8, 16)
+    t["delta"].zero_()
+    t["delta"][:, 0], t["delta"][:, 32:64] = 1.0, 3.0
+    t["u"].zero_()
+    t["u"][:, 0] = 1e-20
+    args = [t[k] for k in ("u", "delta", "A", "B", "C")]
+    final = torch.empty(1, 8, 16, device="cuda")
+    y = ptq.gated_scan(*args, softplus=False, final_state=final)
+    y64, f64 = ref.scan(*(v.double().cpu() for v in args), softplus=False)
+    ref.close(y, y64, y64.abs(), 2.0 ** -14, "y")
+    ref.close(final, f64, f64.abs(), 2.0 ** -14, "final state")
