@@ -124,7 +124,7 @@ typedef struct {
     void *dx;                         /* [rows, cols] */
     void *dgate;                      /* [rows, cols]; NULL exactly where gate is */
     void *dresidual;                  /* [rows, cols]  * */
-    float *dweight, *dbias, *dscale;  /* [cols]  * */
+    float *dweight, *dbias, *dscale;  /* [cols]  *; of an input that is NULL: the gradient at 1, 0 and 1 */
 } ptq_norm_grads_t;
 
 /* n as for the forward pass (residual unchanged); dy, dresidual_out device, dense [rows, cols], the latter or NULL (zeros);

@@ -516,6 +516,7 @@ ptq_status_t ptq_norm_backward(const ptq_norm_t *n, const void *dy, const void *
     p.dx = g->dx;
     p.dresidual = g->dresidual;
     p.dgate = g->dgate;
+    p.sum_scale = g->dscale != nullptr;
     p.part = static_cast<float *>(workspace);
     const NormPlan plan = norm_plan(*n, true, dresidual_out);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -50,6 +50,7 @@ struct NormParams {
     // backward
     const void *dy, *dresidual_out;             // dense; dresidual_out may be null
     void *dx, *dresidual, *dgate;               // dense; the last two may be null
+    bool sum_scale;                             // dscale is wanted
     float *part;                                // [gridDim.x][3][cols]: dweight, dbias, dscale
 };
 
@@ -299,7 +300,7 @@ __global__ void __launch_bounds__(kWide ? 1024 : 256) ptq_norm_kernel(const Norm
                     }
                     store_piece<kWhole, T, 8>(static_cast<T *>(p.dgate) + row, dg, cn);
                 }
-                if (p.scale) fma_each<8>(sum_s, dr, v, sum_s);
+                if (p.sum_scale) fma_each<8>(sum_s, dr, v, sum_s);
                 store_columns<kWhole, T>(static_cast<T *>(p.dx) + row, dx, left, from + at.x + i * kParts * threads, threads, lane);
             }
         }

@@ -1,4 +1,5 @@
 """Calls of the operators between a block's linears at the edges of what their documents allow, against 64 bits."""
+import ctypes
 import itertools
 
 import pytest
@@ -6,6 +7,7 @@ import torch
 
 import block_ref as ref
 from parity_util import launches
+from test_block_host import Norm
 from test_gpu_block_norm import make as make_norm
 from test_gpu_block_norm_stream import check as check_norm
 
@@ -71,3 +73,25 @@ def test_a_small_state_that_grows_by_more_than_binary32_holds(ptq):
     y64, f64 = ref.scan(*(v.double().cpu() for v in args), softplus=False)
     ref.close(y, y64, y64.abs(), 2.0 ** -14, "y")
     ref.close(final, f64, f64.abs(), 2.0 ** -14, "final state")
+
+
+def test_the_gradient_of_a_scale_that_is_not_given(ptq):
+    """C ABI: like the weight, a scale that is NULL is 1 and has a gradient if one is asked for."""
+    from paper_2412_20386_b200 import binding
+    lib = binding.load_library()
+    lib.ptq_norm_workspace_bytes.restype = ctypes.c_size_t
+    rows, cols = 37, 72
+    x, gate, dy = (torch.randn(rows, cols, device="cuda") for _ in range(3))
+    one, dx, dgate = torch.ones(cols, device="cuda"), torch.empty_like(x), torch.empty_like(x)
+    got = []
+    for scale in (one, None):
+        n = Norm(dtype=2, residual_dtype=2, rows=rows, cols=cols, eps=1e-5, x=x.data_ptr(), x_pitch=cols, gate=gate.data_ptr(), gate_pitch=cols,
+                 scale=None if scale is None else scale.data_ptr())
+        space = torch.empty(lib.ptq_norm_workspace_bytes(ctypes.byref(n)), dtype=torch.uint8, device="cuda")
+        sums = torch.full((3, cols), 7.0, device="cuda")
+        grads = (ctypes.c_void_p * 6)(dx.data_ptr(), dgate.data_ptr(), None, *(s.data_ptr() for s in sums))
+        st = lib.ptq_norm_backward(ctypes.byref(n), ctypes.c_void_p(dy.data_ptr()), None, grads, ctypes.c_void_p(space.data_ptr()),
+                                   ctypes.c_size_t(space.numel()), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+        assert st == 0
+        got.append(sums)
+    assert torch.equal(*got) and (got[0][2].abs() > 0).any()
