@@ -94,15 +94,16 @@ def block_norm(x, weight=None, bias=None, residual=None, scale=None, gate=None, 
 
         v = x silu(gate) (gate_at "in"), or x;  r = residual + scale v;  y = norm(r) weight + bias, times silu(gate) (gate_at "out")
 
-    with the root-mean-square norm or (``kind="layer"``) the layer norm.  The residual may be float32 beside any x.  Returns y, or (y, r)
-    where ``residual`` or ``residual_out`` is given; ``residual_out`` may be ``residual`` itself."""
+    with the root-mean-square norm or (``kind="layer"``) the layer norm.  The residual may be float32 beside any x, and
+    so may a ``residual_out`` without one.  Returns y, or (y, r) where ``residual`` or ``residual_out`` is given; ``residual_out`` may be ``residual``
+    itself."""
     out, r = _call(_native().norm, stream, x, x, weight, bias, residual, scale, gate, _norm_flags(kind, gate_at), eps, y, residual_out)
     return out if r is None else (out, r)
 
 
 def block_norm_backward(dy, x, weight=None, bias=None, residual=None, scale=None, gate=None, kind: str = "rms", gate_at: str = "in", eps: float = 1e-5,
                         dresidual_out=None, stream=None):
-    """``ptq_norm_backward``: gradients of ``block_norm`` for dy and dresidual_out (the gradient of r)."""
+    """``ptq_norm_backward``: gradients of ``block_norm`` for dy and dresidual_out (the gradient of r, in r's type)."""
     g = _call(_native().norm_backward, stream, x, x, weight, bias, residual, scale, gate, _norm_flags(kind, gate_at), eps, dy, dresidual_out)
     return dict(zip(("x", "weight", "bias", "residual", "scale", "gate"), g))
 

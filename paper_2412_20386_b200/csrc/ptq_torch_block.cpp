@@ -377,13 +377,22 @@ NormCall read_norm(Args &a)
     return c;
 }
 
+// Without a residual the stream that begins here has the type of r, or of its gradient, as the caller holds it: x's or binary32.
+void begin_stream(NormCall &c, const at::Tensor *r)
+{
+    if (c.n.residual || !r || r->scalar_type() != at::kFloat) return;
+    c.residual_type = at::kFloat;
+    c.n.residual_dtype = PTQ_F32;
+}
+
 // norm(<norm>, y, residual_out) -> (y, residual_out or None) or status
 PyObject *py_norm(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     return guarded([&]() -> PyObject * {
         Args a(args, n, 10);
-        const NormCall c = read_norm(a);
+        NormCall c = read_norm(a);
         const at::Tensor *y_given = a.optional("y"), *r_given = a.optional("residual_out");
+        begin_stream(c, r_given);
         const c10::cuda::CUDAGuard on(a.device());
         const at::Tensor y = output(y_given, "y", c.shape, c.type, a.device(), false);
         at::Tensor r;
@@ -403,9 +412,10 @@ PyObject *py_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     return guarded([&]() -> PyObject * {
         Args a(args, n, 10);
-        const NormCall c = read_norm(a);
+        NormCall c = read_norm(a);
         const at::Tensor &dy = a.tensor("dy");
         const at::Tensor *dr_out = a.optional("dresidual_out");
+        begin_stream(c, dr_out);
         check_dense(dy, "dy", c.type, c.shape);
         if (dr_out) check_dense(*dr_out, "dresidual_out", c.residual_type, c.shape);
         const c10::Device dev = a.device();

@@ -95,3 +95,24 @@ def test_the_gradient_of_a_scale_that_is_not_given(ptq):
         assert st == 0
         got.append(sums)
     assert torch.equal(*got) and (got[0][2].abs() > 0).any()
+
+
+def test_a_binary32_stream_that_begins_beside_16_bit_activations(ptq):
+    """The first block of a network: its x begins a residual stream of binary32, whose gradient comes back as binary32."""
+    for dtype, D in ((ref.BF16, 72), (ref.F16, 35)):
+        t = make_norm(D, dtype, 40, D, None, True, True)
+        out = torch.empty(40, D, device="cuda")
+        y, r = ptq.block_norm(t["x"], t["weight"], t["bias"], scale=t["scale"], gate=t["gate"], residual_out=out)
+        _, r64 = ref.norm(t["x"].double().cpu(), scale=t["scale"].double().cpu(), gate=t["gate"].double().cpu())
+        assert r is out
+        ref.close(r, r64, r64.abs(), 2.0 ** -19, "r")
+        assert torch.equal(y, ptq.block_norm(t["x"], t["weight"], t["bias"], scale=t["scale"], gate=t["gate"]))
+        for kind, gate_at in itertools.product(["rms", "layer"], ["in", "out"]):
+            check_norm(ptq, t, kind, gate_at, ref.F32)
+    wide = make_norm(9, ref.BF16, 1300, 2056, None, True)
+    check_norm(ptq, wide, "layer", "in", ref.F32)
+    for bad in (torch.empty(40, 35, device="cuda", dtype=torch.bfloat16), torch.empty(40, 35, device="cuda", dtype=torch.float64)):
+        with pytest.raises(ValueError):
+            ptq.block_norm(t["x"], residual_out=bad)
+        with pytest.raises(ValueError):
+            ptq.block_norm_backward(t["x"].contiguous(), t["x"], dresidual_out=bad)
