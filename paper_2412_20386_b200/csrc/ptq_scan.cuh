@@ -851,9 +851,10 @@ __global__ void __launch_bounds__(kScanFinishThreads) ptq_scan_finish_kernel(con
 // channels, N = 16, bfloat16 51 us, 4.3 TB/s (the bytes alone 33; every lane with its own softplus 80, states copied
 // asynchronously ahead 70).  The kS lanes of a channel
 // hold kNS states each and take kS sequences at a time: every lane makes dt, dt u and in the end y of one of them and hands the former
-// round; all loads of the set go out before its first store.
+// round; all loads of the set go out before its first store.  Eight sequences at a time (N > 16) take more registers than four CTAs leave: 1024 sequences
+// of 1536 channels, N = 32, binary32 with two CTAs per SM 107 us, four 176 (spills); bfloat16 99 with either.
 template <typename T, int kNS, int kS, bool kWhole>
-__global__ void __launch_bounds__(256, 4) ptq_scan_step_kernel(const ScanParams p)
+__global__ void __launch_bounds__(256, kS > 4 ? 2 : 4) ptq_scan_step_kernel(const ScanParams p)
 {
     const int lane = threadIdx.x & 31, own = lane % kS, base = lane - own;
     const int per_cta = 256 / kS;
@@ -876,12 +877,13 @@ __global__ void __launch_bounds__(256, 4) ptq_scan_step_kernel(const ScanParams 
     T *at_y = static_cast<T *>(p.y) + (b0 + own) * p.channels + d;
     for (; b0 < p.batch; b0 += jump) {
         const bool token = on && b0 + own < p.batch && (!p.lengths || p.lengths[b0 + own] > 0);
+        const unsigned tokens = __ballot_sync(0xffffffffu, token) >> base;           // of the set's sequences: of one without, only the state is read
         float h[kS][kNS];
         Piece<T, kNS> B[kS], C[kS];
 #pragma unroll
         for (int i = 0; i < kS; ++i) {
-            const int n = b0 + i < p.batch ? nn : 0;
-            load_floats<kWhole, kNS>(h[i], p.state + at_state + i * state_step, p.state ? n : 0);
+            load_floats<kWhole, kNS>(h[i], p.state + at_state + i * state_step, p.state && b0 + i < p.batch ? nn : 0);
+            const int n = tokens >> i & 1 ? nn : 0;
             B[i] = load_piece<kWhole, T, kNS>(at_B + i * p.B_b, n);
             C[i] = load_piece<kWhole, T, kNS>(at_C + i * p.C_b, n);
         }
@@ -893,14 +895,14 @@ __global__ void __launch_bounds__(256, 4) ptq_scan_step_kernel(const ScanParams 
 #pragma unroll
         for (int i = 0; i < kS; ++i) {
             const float dt_i = __shfl_sync(0xffffffffu, dt, base + i), in = __shfl_sync(0xffffffffu, dt * u, base + i);
-            const bool token_i = __shfl_sync(0xffffffffu, token, base + i);
+            const bool token_i = tokens >> i & 1;
             float a[kNS], f[kNS];
             scan_decays<kNS>(a, dt_i, rate);
             floats_of(f, B[i]);
             mul_each<kNS>(f, in, f);
             fma_each<kNS>(a, a, h[i], f);
 #pragma unroll
-            for (int k = 0; k < kNS; ++k) h[i][k] = token_i ? a[k] : h[i][k];       // what is read for no token may be anything
+            for (int k = 0; k < kNS; ++k) h[i][k] = token_i ? a[k] : h[i][k];       // as it was, infinities too
             floats_of(f, C[i]);
             o[i] = dot_each<kNS>(h[i], f);
             if (p.final_state) store_floats<kWhole, kNS>(p.final_state + at_state + i * state_step, h[i], b0 + i < p.batch ? nn : 0);

@@ -10,6 +10,7 @@ from parity_util import launches
 from test_block_host import Norm
 from test_gpu_block_norm import make as make_norm
 from test_gpu_block_norm_stream import check as check_norm
+from test_gpu_block_scan import check as check_scan, make as make_scan
 
 pytestmark = pytest.mark.gpu
 
@@ -116,3 +117,10 @@ def test_a_binary32_stream_that_begins_beside_16_bit_activations(ptq):
             ptq.block_norm(t["x"], residual_out=bad)
         with pytest.raises(ValueError):
             ptq.block_norm_backward(t["x"].contiguous(), t["x"], dresidual_out=bad)
+
+
+def test_single_tokens_of_empty_sequences(ptq):
+    """What belongs to a sequence of no tokens is not read: it may be anything."""
+    for N, B in ((16, 9), (2, 3), (32, 20)):
+        t = make_scan(N, ref.BF16, B, 1, 40, N, state=True, lengths=[b % 2 for b in range(B)])
+        check_scan(ptq, t, train=False)
