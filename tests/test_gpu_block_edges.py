@@ -124,3 +124,10 @@ def test_single_tokens_of_empty_sequences(ptq):
     for N, B in ((16, 9), (2, 3), (32, 20)):
         t = make_scan(N, ref.BF16, B, 1, 40, N, state=True, lengths=[b % 2 for b in range(B)])
         check_scan(ptq, t, train=False)
+
+
+def test_padded_reversed_groups_in_many_chunks(ptq):
+    t = make_scan(77, ref.F32, 3, 1100, 12, 16, G=2, state=True, lengths=[1100, 555, 3])
+    check_scan(ptq, t, reverse=True)
+    t = make_scan(78, ref.BF16, 2, 900, 18, 8, G=3, odd=True, lengths=[33, 890])
+    check_scan(ptq, t, reverse=True, dfinal=False)
