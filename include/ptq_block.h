@@ -10,15 +10,18 @@
  * Activations are token-major, [batch, token, channel], of one type per call, with the channels of a token next to
  * each other and any pitch between tokens and between sequences (in elements, not negative): the halves of in_proj's
  * output and the columns of x_proj's are passed as they lie.  Pointers are aligned to their type; rows whose
- * pointers and pitches are multiples of 16 bytes are moved 16 bytes at a time.  The pitches of an input that is NULL are ignored.  Parameters, states of the
- * recurrence and gradients of parameters are binary32.  Arithmetic is binary32 throughout; a result is
- * rounded to its type once.  Outputs are dense unless their pitch is an argument, and overlap no input but
+ * pointers and pitches are multiples of 16 bytes are moved 16 bytes at a time.  The pitches of an input that is NULL
+ * are ignored.  Parameters, states of the recurrence and gradients of parameters are binary32.  Arithmetic is binary32
+ * throughout; a result is rounded to its type once.  Outputs are dense unless their pitch is an argument, and overlap no input but
  * where a function says so.  Sums have a fixed order: the same call gives the same bits.
  *
  * Sequences are processed from the first token to the last or, with PTQ_SEQ_REVERSE, from the last to the first.
  * `lengths` (device, [batch] int32, or NULL) gives the number of tokens of each sequence of a padded batch; values are
  * clamped to 0 .. length.  What lies behind a sequence's end is not read; outputs there are left as they are, gradients are
  * set to zero.
+ *
+ * An infinity or NaN in a token reaches what the formulas make of it and, in the backward passes, all gradients of the parameters
+ * of its channel (in B or C: of the group's channels).
  */
 #ifndef PTQ_BLOCK_H_
 #define PTQ_BLOCK_H_
@@ -48,7 +51,9 @@ typedef enum { PTQ_F16 = 0, PTQ_BF16 = 1, PTQ_F32 = 2 } ptq_dtype_t;
  *     e = delta[p,d] + delta_bias[d];  dt = log(1 + exp(e)), or e
  *     h[d,n] <- exp(dt A[d,n]) h[d,n] + dt u[p,d] B[p,g,n]
  *     o[p,d] = sum_n h[d,n] C[p,g,n] + D[d] u[p,d];   y[p,d] = o[p,d] z[p,d] / (1 + exp(-z[p,d])), or o[p,d]
- * A is negative in a trained model; any finite value and -inf (no memory) are computed.
+ * The decay is the exact solution over a step, the input's factor the first-order dt B, as Mamba blocks are trained (not the
+ * (exp(dt A) - 1) / A B of an input that is held over the step).  A is negative in a trained model; any finite value is computed, and -inf
+ * (no memory where dt > 1e-36; a step with dt = 0 keeps the state with any A).
  */
 typedef struct {
     int dtype;                        /* ptq_dtype_t of u, delta, z, B, C, y and their gradients */

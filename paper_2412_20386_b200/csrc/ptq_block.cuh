@@ -16,16 +16,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 template <typename T>
-__device__ __forceinline__ float to_f32(T v)
-{
-    if constexpr (sizeof(T) == 4)
-        return v;
-    else if constexpr (std::is_same_v<T, __half>)
-        return __half2float(v);
-    else
-        return __bfloat162float(v);
-}
-template <typename T>
 __device__ __forceinline__ T from_f32(float v)
 {
     if constexpr (sizeof(T) == 4)
@@ -386,7 +376,7 @@ __device__ __forceinline__ float dot_each(const float (&a)[kN], const float (&b)
 
 // Sums over the lanes whose numbers differ in the bits kLow, 2 kLow, ..., kHigh of V values per lane: every level that
 // still has two values or more sends one half and keeps the other, so that V values over P lanes take about V (1 - 1/P)
-// shuffles instead of V log2 P.  Returns how many values are left per lane; they are those from index_of on.
+// shuffles instead of V log2 P.  V / P values, or one, are left in a lane, at the front of v: those from first_sum on.
 template <int kV, int kLow, int kHigh>
 __device__ __forceinline__ void lane_sums(float (&v)[kV], int lane)
 {

@@ -4,7 +4,7 @@
 //
 // where the W-1 steps in front of the first one are the caller's state (zeros without one).  Bound: the bytes.  A thread
 // holds four channels and walks over a segment of steps with the last W - 1 rows in registers, its loads kConvAhead rows ahead.
-// Measured, 64 x 197 x 768 binary16, W = 4: forward 15 us (2.6 TB/s), backward 30 us (2 TB/s): both wait for loads, of which a thread has
+// Measured, 64 x 197 x 768 binary16, W = 4: forward 16 us (2.4 TB/s), backward 30 us (2 TB/s): both wait for loads, of which a thread has
 // few in flight; eight channels a thread took 40 and 56, the bytes alone 6 and 9.
 #pragma once
 

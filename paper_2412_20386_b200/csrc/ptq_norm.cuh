@@ -7,8 +7,8 @@
 // parameters (and, backward, whose sums of dweight, dbias and dscale) stay in its registers, a CTA of ceil(D / 256) warps the
 // whole row; it goes over the rows kRB at a time, so that one barrier serves the sums of kRB rows.  Mean and variance are
 // two passes over the registers.  The norm is taken of the unrounded r, in both directions, so y does not depend on the type of r.
-// Measured, 50432 x 768 bfloat16 with a binary32 residual stream: forward 75 us (6.2 TB/s), backward 125 us (5.6 TB/s); backward with
-// the rows in registers 370, binary32 rows in half sectors 160.  16-bit rows alone are bound by issue slots: 50432 x 768 bfloat16 forward 40 us.
+// Measured, 50432 x 768 bfloat16 with a binary32 residual stream: forward 82 us (5.7 TB/s), backward 115 us (6.1 TB/s) and 8 for the column sums;
+// backward with the rows in registers 370, binary32 rows in half sectors 160.  16-bit rows alone are bound by issue slots: 50432 x 768 bfloat16 forward 40 us.
 #pragma once
 
 #include "ptq_block.cuh"

@@ -15,7 +15,7 @@
 // alone: 45), of which 100 us is the recurrence by itself; CTAs of four
 // warps that shared a tile took 180, one channel per lane 137 to 190 (every value of B and C read from shared memory for 8 decays
 // instead of 16), loads whose 16-bit values were taken apart on arrival 220.  A quarter
-// of the decays by polynomial on the multiply-add pipe: 137 -> 154.  2 x 20011 x 1024 bfloat16 464 us in two launches (exponentials
+// of the decays by polynomial on the multiply-add pipe: 137 -> 154.  2 x 20011 x 1024 bfloat16 466 us in two launches (exponentials
 // of one pass 95).  1 x 197 x 384: 10.2 us in two launches of chunks of 32 steps, 18.4 in one.
 #pragma once
 
@@ -56,7 +56,8 @@ struct ScanParams {
 
 // Of two values: t = e^-|x| and log(1 + e^x) = max(x, 0) + log(1 + t).  The argument of the power of two is carried to about 2^-46
 // (its rounding alone would cost four units in the last place at |x| = 7); |x| is cut at 126, where t is zero.  log(1 + t) / t is a
-// polynomial fitted to 5e-9 on [0, 1]: accurate relative to the result, small ones too, with half the instructions of expf and log1pf.
+// polynomial fitted on [0, 1]; with the coefficients as written, log(1 + t) is high by up to 2.3e-8, 3.4e-8 relative (half a unit in the last place),
+// small results too, with half the instructions of expf and log1pf.
 __device__ __forceinline__ void exp_minus_abs_pair(float &t0, float &t1, float x0, float x1)
 {
     const float m0 = -fminf(fabsf(x0), 126.0f), m1 = -fminf(fabsf(x1), 126.0f);
@@ -408,10 +409,12 @@ __host__ __device__ constexpr size_t scan_backward_smem(int channels, int states
 // backward, a taken again from dt.  Over the channels sum dC = h dyo and dB = G dt u: the two of a lane first, then eight values at a time
 // over the lanes of a warp, the four warps' sums through shared memory, the CTAs' through global memory, each in a fixed order.  Over the
 // states of a channel sum o, s and r.  The rows' lanes then make du = dt s + D dyo, ddelta = (u s + r ln 2) sigmoid and dz.
-// Bound: latency at the 10 to 12 warps of 168 registers that an SM holds (half of the issue slots are used), not one unit: 64 x 197 x 384,
-// N = 16, binary16: 140 us, of it 60 for all but the recurrence, 20 for the sums over lanes, 18 for the last step; with eight warps per SM 177.
+// Bound: latency at the 10 to 12 warps that an SM holds (45 % of the issue slots are used), not one unit: 64 x 197 x 384,
+// N = 16, binary16: 140 to 147 us, of it 60 for all but the recurrence, 20 for the sums over lanes, 18 for the last step; with eight warps per SM 177.
+// Three CTAs are as many as 168 registers allow, and as many as 72,704 bytes of shared memory do; with more states or binary32 rows the
+// shared memory allows fewer: two CTAs at N = 9 .. 16 in binary32, one from N = 17 on.
 // The rows wait in shared memory for their second use (registers: spills; read again: 10 us more).  The whole backward pass
-// 150 us, exponentials alone 22.
+// 155 us, exponentials alone 22.
 template <typename T, int kC, int kNS, int kS, bool kWhole>
 __global__ void __launch_bounds__(kScanWarps * 32, kC * kNS <= 2 && sizeof(T) == 2 ? 4 : 3) ptq_scan_backward_kernel(const ScanParams p)
 {
@@ -848,7 +851,7 @@ __global__ void __launch_bounds__(kScanFinishThreads) ptq_scan_finish_kernel(con
 }
 
 // One token per sequence.  Bound: the state's bytes, read and written once, and close behind it the issue slots: 1024 sequences of 1536
-// channels, N = 16, bfloat16 51 us, 4.3 TB/s (the bytes alone 33; every lane with its own softplus 80, states copied
+// channels, N = 16, bfloat16 50 us, 4.3 TB/s (the bytes alone 33; every lane with its own softplus 80, states copied
 // asynchronously ahead 70).  The kS lanes of a channel
 // hold kNS states each and take kS sequences at a time: every lane makes dt, dt u and in the end y of one of them and hands the former
 // round; all loads of the set go out before its first store.  Eight sequences at a time (N > 16) take more registers than four CTAs leave: 1024 sequences
