@@ -1,5 +1,9 @@
-// What the host files of the operators of include/ptq_block.h share.
+// What the host files of the operators of include/ptq_block.h, ptq_heads.h and ptq_fp8.h share.
 #pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
 
 #include <initializer_list>
 #include <type_traits>
@@ -51,6 +55,65 @@ template <class Fn>
 ptq_status_t with_flag(bool flag, Fn fn)
 {
     return flag ? fn(std::true_type()) : fn(std::false_type());
+}
+
+inline ptq_status_t check_arch()
+{
+    constexpr int kMaxDevices = 64;
+    static std::atomic<int> known[kMaxDevices] = {};      // 0: not asked yet, 1: sm_100, 2: another one
+    int dev = -1;
+    PTQ_CUDA(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= kMaxDevices) return fail(PTQ_ERR_CUDA, "device index %d out of range", dev);
+    int k = known[dev].load(std::memory_order_relaxed);
+    if (k == 0) {
+        int major = 0, minor = 0;
+        PTQ_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev));
+        PTQ_CUDA(cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev));
+        k = major == 10 && minor == 0 ? 1 : 2;
+        known[dev].store(k, std::memory_order_relaxed);
+    }
+    return k == 1 ? PTQ_OK : fail(PTQ_ERR_ARCH, "device %d is not compute capability 10.0", dev);
+}
+
+inline int elem_bytes(int dtype) { return dtype == PTQ_F32 ? 4 : 2; }
+inline bool dtype_ok(int dtype) { return dtype == PTQ_F16 || dtype == PTQ_BF16 || dtype == PTQ_F32; }
+
+// Every pointer that is given on a multiple of `bytes`.
+inline bool aligned(std::initializer_list<const void *> ps, int bytes)
+{
+    for (const void *p : ps)
+        if (reinterpret_cast<uintptr_t>(p) % bytes) return false;
+    return true;
+}
+inline bool multiples(std::initializer_list<int64_t> pitches, int unit)
+{
+    for (int64_t v : pitches)
+        if (v % unit) return false;
+    return true;
+}
+inline bool not_negative(std::initializer_list<int64_t> pitches)
+{
+    for (int64_t v : pitches)
+        if (v < 0) return false;
+    return true;
+}
+inline size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+template <class Fn>
+ptq_status_t with_type(int dtype, Fn fn)
+{
+    if (dtype == PTQ_F16) return fn(__half());
+    if (dtype == PTQ_BF16) return fn(__nv_bfloat16());
+    return fn(0.0f);
+}
+
+inline ptq_status_t check_space(const void *workspace, size_t have, size_t need)
+{
+    if (need == 0) return PTQ_OK;
+    if (!workspace) return fail(PTQ_ERR_NULL, "workspace is NULL");
+    if (!aligned({workspace}, 16)) return fail(PTQ_ERR_ALIGN, "workspace is not 16-byte aligned");
+    if (have < need) return fail(PTQ_ERR_SHAPE, "workspace has %zu bytes, %zu are needed", have, need);
+    return PTQ_OK;
 }
 
 }  // namespace ptq_host

@@ -1,0 +1,604 @@
+// Linears in e4m3 with a scale for each block of 128 values (include/ptq_fp8.h): quantize kernels and the product on the
+// tensor cores.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include "ptx_sm100.cuh"
+
+namespace ptq {
+
+constexpr int kFp8Block = 128;                 // values that share a scale; one k-block of the product
+constexpr float kFp8Max = 448.0f;
+constexpr float kFp8Least = 0x1p-100f;         // a block's largest magnitude counts as this at least: both quotients stay finite
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// max(a, |b|) that keeps a NaN of either side.
+__device__ __forceinline__ float max_abs_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    return r;
+}
+
+// Eight values of a row from column c on (zeros from `cols` on): one or two 16-byte loads where whole, else one by one.
+template <typename T>
+__device__ __forceinline__ void load8(const T *row, int c, int cols, bool whole, float (&v)[8])
+{
+    if (whole && c + 8 <= cols) {
+        if constexpr (sizeof(T) == 4) {
+            const float4 a = __ldg(reinterpret_cast<const float4 *>(row + c)), b = __ldg(reinterpret_cast<const float4 *>(row + c) + 1);
+            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        } else {
+            const uint4 a = __ldg(reinterpret_cast<const uint4 *>(row + c));
+            const T *t = reinterpret_cast<const T *>(&a);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = to_f32(t[i]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? to_f32(row[c + i]) : 0.0f;
+    }
+}
+
+// The largest magnitude of the 128 values that 16 neighbouring lanes hold, not below kFp8Least; a NaN stays one.
+__device__ __forceinline__ float block_top(const float (&v)[8])
+{
+    float top = kFp8Least;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max_abs_nan(top, v[i]);
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) top = max_abs_nan(top, __shfl_xor_sync(0xffffffffu, top, d));
+    return top;
+}
+__device__ __forceinline__ uint2 codes8(const float (&v)[8], float inverse)
+{
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * h] * inverse, v[4 * h + 1] * inverse), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * h + 2] * inverse, v[4 * h + 3] * inverse), __NV_SATFINITE, __NV_E4M3);
+        w[h] = lo | hi << 16;
+    }
+    return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ void store_codes8(uint8_t *row, int c, int cols, uint2 w)
+{
+    if (c + 8 <= cols) {
+        *reinterpret_cast<uint2 *>(row + c) = w;
+    } else {
+        for (int i = 0; i < 8 && c + i < cols; ++i) row[c + i] = static_cast<uint8_t>((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------- quantize
+// Bound by memory: 16-bit values are read, codes and a scale for each 128 of them written, once each.  Half a warp holds a block
+// (16 bytes of 16-bit values a lane), four of a row at a time, so that four loads a lane are in flight; the 16 half-warps of a
+// CTA take 16 neighbouring rows, whose scales lie next to each other in the layout that the product reads.
+struct Fp8QuantizeParams {
+    const void *x;
+    int64_t x_pitch, codes_pitch, scale_row, scale_block;
+    int64_t rows;
+    int cols, blocks, span;           // blocks of a row; how many of them a CTA goes over
+    uint8_t *codes;
+    float *scales;
+};
+constexpr int kFp8QuantizeRows = 16;
+template <typename T, bool kWhole>
+__global__ void __launch_bounds__(256) ptq_fp8_quantize_kernel(const Fp8QuantizeParams p)
+{
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * kFp8QuantizeRows + (threadIdx.x >> 4);
+    const int l = threadIdx.x & 15;
+    const bool on = row < p.rows;                       // the others go along: the shuffles are the warp's
+    const T *x = static_cast<const T *>(p.x) + (on ? row : 0) * p.x_pitch;
+    const int first = blockIdx.y * p.span, last = min(p.blocks, first + p.span);
+    griddep_launch_dependents();
+    for (int b0 = first; b0 < last; b0 += 4) {
+        float v[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load8(x, (b0 + i) * kFp8Block + 8 * l, on && b0 + i < last ? p.cols : 0, kWhole, v[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float top = block_top(v[i]);
+            const uint2 w = codes8(v[i], kFp8Max / top);
+            if (!on || b0 + i >= last) continue;
+            store_codes8(p.codes + row * p.codes_pitch, (b0 + i) * kFp8Block + 8 * l, p.cols, w);
+            if (l == 0) p.scales[row * p.scale_row + (b0 + i) * p.scale_block] = top / kFp8Max;
+        }
+    }
+}
+
+// Weights: one CTA goes over a block of 128 x 128 twice (it stays in L1).  Done once per layer.
+template <typename T>
+__global__ void __launch_bounds__(256) ptq_fp8_quantize_weight_kernel(const Fp8QuantizeParams p)
+{
+    __shared__ float tops[8];
+    const int l = threadIdx.x & 15, h = threadIdx.x >> 4, c = blockIdx.x * kFp8Block + 8 * l;
+    const int64_t row0 = static_cast<int64_t>(blockIdx.y) * kFp8Block;
+    float v[8], top = kFp8Least;
+    for (int r = h; r < kFp8Block; r += 16) {
+        const int64_t row = row0 + r;
+        load8(static_cast<const T *>(p.x) + (row < p.rows ? row : 0) * p.x_pitch, c, row < p.rows ? p.cols : 0, false, v);
+        top = max_abs_nan(top, block_top(v));
+    }
+    top = max_abs_nan(top, __shfl_xor_sync(0xffffffffu, top, 16));
+    if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
+    __syncthreads();
+    for (int i = 0; i < 8; ++i) top = max_abs_nan(top, tops[i]);
+    for (int r = h; r < kFp8Block; r += 16) {
+        const int64_t row = row0 + r;
+        if (row >= p.rows) break;
+        load8(static_cast<const T *>(p.x) + row * p.x_pitch, c, p.cols, false, v);
+        store_codes8(p.codes + row * p.codes_pitch, c, p.cols, codes8(v, kFp8Max / top));
+    }
+    if (threadIdx.x == 0) p.scales[static_cast<int64_t>(blockIdx.y) * p.blocks + blockIdx.x] = top / kFp8Max;
+}
+
+// ---------------------------------------------------------------------------------------------------- product
+// One k-block of 128 is one chain of four tcgen05.mma (kind::f8f6f4, binary32 accumulators in TMEM) into one of two
+// accumulator buffers; the epilogue warps read the buffer, multiply it by the block's scales and add it to sums that they
+// keep in registers, while the tensor pipe fills the other one.  The scales cannot go into the operands (they are not powers
+// of two) nor be put off to the end (they change with every k-block).
+//
+// Warp 0 issues the TMA loads, warp 1 the MMAs, warps 2 .. 9 read: 32 TMEM lanes each, the two sets of four half of the
+// columns each.  A tile is 128 (TMEM lanes, operand P) x BN (TMEM columns, operand Q):
+//   many rows   P = activations, Q = weights.  Persistent CTAs.  With BN = 256 a k-block takes the tensor pipe about 512 cycles,
+//               and the eight warps 2 x 128 columns of TMEM loads and packed multiply-adds per scheduler: less than that.
+//   few rows    P = weights, Q = the tokens (BN = 16, 32 or 64): no lane is wasted on rows that are not there.
+// Where there are fewer tiles than SMs the k-blocks of a tile are split over a cluster of up to eight CTAs, which add their
+// parts through distributed shared memory in the order of the parts.
+struct Fp8Params {
+    const float *a_scales, *w_scales, *bias;
+    int64_t scale_row, scale_block;   // of a_scales
+    void *y;
+    int64_t y_pitch;
+    const void *x;                    // fused: the activations before they are quantized
+    int64_t x_pitch;
+    int rows, cols, outputs, blocks;  // blocks: k-blocks
+    int p_tiles, q_tiles, split;
+    int stages;
+    bool whole, x_whole;              // rows of y, of x can be moved 16 bytes at a time
+    unsigned *status;
+};
+
+constexpr int kFp8Threads = 320;
+constexpr int kFp8MaxStages = 8;
+constexpr int kFp8PTile = 128 * kFp8Block;                 // bytes of one k-block of operand P
+constexpr int kFp8Staging = 4096;                          // bytes of an epilogue warp's staging: 32 rows of 128 bytes
+constexpr int kFp8MaxFused = 64;                           // k-blocks x tokens / 16 that a fused CTA may hold (2 KB each)
+
+__device__ __forceinline__ void mma_f8_kblock(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc)
+{
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p, q, e;\n\t"
+        "elect.sync _|e, 0xffffffff;\n\t"
+        ".reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+        "setp.ne.b32 p, 0, 0;\n\t"
+        "setp.eq.b32 q, 0, 0;\n\t"
+        "add.u64 a1, %1, 2;\n\t"
+        "add.u64 a2, %1, 4;\n\t"
+        "add.u64 a3, %1, 6;\n\t"
+        "add.u64 b1, %2, 2;\n\t"
+        "add.u64 b2, %2, 4;\n\t"
+        "add.u64 b3, %2, 6;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a1, b1, %3, q;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a2, b2, %3, q;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a3, b3, %3, q;\n\t"
+        "}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc)
+        : "memory");
+}
+// Instruction descriptor of kind::f8f6f4 with e4m3 operands, both K-major, and binary32 accumulators: D format [4,6) = 1,
+// A and B formats [7,10), [10,13) = 0, N>>3 at [17,23), M>>4 at [24,29).
+__host__ __device__ constexpr uint32_t make_idesc_e4m3(int M, int N)
+{
+    return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+// 32 lanes x N columns (8, 16 or 32).
+template <int N>
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&v)[N])
+{
+    if constexpr (N == 32) {
+        tmem_ld_32x32(taddr, v);
+    } else if constexpr (N == 16) {
+        asm volatile(
+            "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+            : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+              "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+            : "r"(taddr)
+            : "memory");
+    } else {
+        static_assert(N == 8, "8, 16 or 32 columns");
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                     : "r"(taddr)
+                     : "memory");
+    }
+}
+
+// (a0, a1) += (f0 b0, f1 b1), two binary32 multiply-adds in one instruction.
+__device__ __forceinline__ void fma2(float &a0, float &a1, float f0, float f1, uint32_t b0, uint32_t b1)
+{
+    asm("{\n\t"
+        ".reg .b64 a, f, b;\n\t"
+        "mov.b64 a, {%0, %1};\n\t"
+        "mov.b64 f, {%2, %3};\n\t"
+        "mov.b64 b, {%4, %5};\n\t"
+        "fma.rn.f32x2 a, f, b, a;\n\t"
+        "mov.b64 {%0, %1}, a;\n\t"
+        "}"
+        : "+f"(a0), "+f"(a1)
+        : "f"(f0), "f"(f1), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ float ld_cluster_f32(uint32_t local_addr, uint32_t rank)
+{
+    float v;
+    asm volatile(
+        "{\n\t"
+        ".reg .b32 ra;\n\t"
+        "mapa.shared::cluster.u32 ra, %1, %2;\n\t"
+        "ld.shared::cluster.f32 %0, [ra];\n\t"
+        "}"
+        : "=f"(v)
+        : "r"(local_addr), "r"(rank)
+        : "memory");
+    return v;
+}
+
+// Shared memory: stages of (P tile, Q tile) or, fused, stages of P tiles and all Q tiles of the CTA; staging of the epilogue
+// warps (persistent kernels only); fused: scales [k-block][BN]; barriers.
+struct Fp8Layout {
+    int stage, q, staging, scales, bars, bytes;
+};
+template <int BN, bool kSwap, bool kOneTile, bool kFused>
+__host__ __device__ constexpr Fp8Layout fp8_layout(int stages, int blocks)
+{
+    Fp8Layout l = {};
+    l.stage = kFp8PTile + (kFused ? 0 : BN * kFp8Block);
+    l.q = stages * l.stage;
+    l.staging = l.q + (kFused ? blocks * BN * kFp8Block : 0);
+    l.scales = l.staging + (kOneTile ? 0 : 8 * kFp8Staging);
+    l.bars = l.scales + (kFused ? blocks * BN * 4 : 0);
+    l.bytes = l.bars + 8 * (2 * kFp8MaxStages + 5) + 16;
+    // the parts of a split tile lie over the stages, with 4 floats between the rows
+    const int parts = kOneTile ? 4 * (kSwap ? BN * (128 + 4) : 128 * (BN + 4)) : 0;
+    if (kOneTile && l.bars < parts) {
+        l.bars = parts;
+        l.bytes = l.bars + 8 * (2 * kFp8MaxStages + 5) + 16;
+    }
+    return l;
+}
+
+// kOneTile: one tile, or one part of one, per CTA; else persistent.  kFused: operand Q is quantized here from x.
+template <typename Y, int BN, bool kSwap, bool kOneTile, bool kFused>
+__global__ void __launch_bounds__(kFp8Threads, 1)
+ptq_fp8_matmul_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CUtensorMap tmQ, const Fp8Params p)
+{
+    static_assert(!kFused || (kSwap && kOneTile), "tokens are quantized in the kernel for few rows");
+    static_assert(!kSwap || kOneTile, "few rows make few tiles");
+    constexpr int kCols = BN / 2;                          // columns of an epilogue warp
+    constexpr int kLd = kCols < 32 ? kCols : 32;           // columns of one TMEM load
+    constexpr uint32_t kTmem = 2 * BN;
+    constexpr uint32_t kIdesc = make_idesc_e4m3(128, BN);
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    const uint32_t base = smem_u32(smem_raw);
+    if ((base & 1023u) != 0u) {                            // never expected; the same in all CTAs of a cluster
+        if (threadIdx.x == 0) atomicOr(p.status, PTQ_DEV_SMEM_ALIGN);
+        return;
+    }
+    const int rank = kOneTile ? static_cast<int>(blockIdx.x) % p.split : 0;
+    const int first_tile = kOneTile ? static_cast<int>(blockIdx.x) / p.split : static_cast<int>(blockIdx.x);
+    const int tiles = p.p_tiles * p.q_tiles;
+    // the k-blocks of this CTA
+    const int kb0 = kOneTile ? static_cast<int>(static_cast<int64_t>(p.blocks) * rank / p.split) : 0;
+    const int kb1 = kOneTile ? static_cast<int>(static_cast<int64_t>(p.blocks) * (rank + 1) / p.split) : p.blocks;
+    const Fp8Layout at = fp8_layout<BN, kSwap, kOneTile, kFused>(p.stages, (p.blocks + p.split - 1) / p.split);
+    const uint32_t nstages = static_cast<uint32_t>(p.stages);
+    const uint32_t bar_base = base + at.bars;
+    auto full_bar = [&](uint32_t s) { return bar_base + 8u * s; };
+    auto empty_bar = [&](uint32_t s) { return bar_base + 8u * (kFp8MaxStages + s); };
+    auto tfull_bar = [&](uint32_t b) { return bar_base + 8u * (2 * kFp8MaxStages + b); };
+    auto tempty_bar = [&](uint32_t b) { return bar_base + 8u * (2 * kFp8MaxStages + 2 + b); };
+    const uint32_t q_bar = bar_base + 8u * (2 * kFp8MaxStages + 4);
+    volatile uint32_t *tmem_holder = reinterpret_cast<volatile uint32_t *>(smem_raw + at.bars + 8 * (2 * kFp8MaxStages + 5));
+    volatile uint32_t *abort_flag = tmem_holder + 1;
+    const int warp = uniform_warp(), lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (uint32_t s = 0; s < nstages; ++s) {
+            mbar_init(full_bar(s), 1);
+            mbar_init(empty_bar(s), 1);
+        }
+        for (uint32_t b = 0; b < 2; ++b) {
+            mbar_init(tfull_bar(b), 1);
+            mbar_init(tempty_bar(b), 8);
+        }
+        mbar_init(q_bar, 8);
+        *abort_flag = 0u;
+        fence_mbar_init();
+        prefetch_tensormap(&tmP);
+        if (!kFused) prefetch_tensormap(&tmQ);
+    }
+    if (warp == 1) {
+        tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_holder)), kTmem);
+        tmem_relinquish_alloc_permit();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_holder, 0);
+
+    // Twelve P tiles, then the next Q tile: the CTAs that run together share the operands of about 12 x 12 tiles.
+    auto tile_at = [&](int tile, int &pt, int &qt) {
+        const int group = tile / (12 * p.q_tiles), r = tile - group * 12 * p.q_tiles;
+        const int in_group = min(12, p.p_tiles - group * 12);
+        pt = group * 12 + r % in_group;
+        qt = r / in_group;
+    };
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ TMA producer
+        uint32_t stage = 0, phase = 0, issued = 0;
+        bool ok = true;
+        const uint32_t tx = static_cast<uint32_t>(at.stage);           // boxes count whole, also beyond the ends
+        griddep_wait();
+        for (int tile = first_tile; tile < tiles && ok; tile += kOneTile ? tiles : static_cast<int>(gridDim.x)) {
+            int pt, qt;
+            tile_at(tile, pt, qt);
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (!mbar_wait_warp(empty_bar(stage), phase ^ 1u, abort_flag, p.status)) {
+                    ok = false;
+                    break;
+                }
+                const uint32_t dst = base + stage * static_cast<uint32_t>(at.stage);
+                mbar_arrive_expect_tx_warp(full_bar(stage), tx);
+                tma_load_2d_warp(dst, &tmP, kb * kFp8Block, pt * 128, full_bar(stage));
+                if (!kFused) tma_load_2d_warp(dst + kFp8PTile, &tmQ, kb * kFp8Block, qt * BN, full_bar(stage));
+                ++issued;
+                if (++stage == nstages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+            }
+        }
+        if (!ok) {
+            // Error path only: the loads in flight land before the CTA gives up its shared memory (bounded).
+            for (uint32_t s = 0; s < nstages; ++s) {
+                const uint32_t uses = (issued + nstages - 1u - s) / nstages;
+                if (uses == 0u) continue;
+                for (int i = 0; i < 200000 && !mbar_try_wait(full_bar(s), (uses - 1u) & 1u); ++i) {
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer
+        uint32_t stage = 0, phase = 0, buf = 0, bphase = 0;
+        bool ok = !kFused || mbar_wait_warp(q_bar, 0u, abort_flag, p.status);
+        for (int tile = first_tile; tile < tiles && ok; tile += kOneTile ? tiles : static_cast<int>(gridDim.x)) {
+            for (int kb = kb0; kb < kb1; ++kb) {
+                ok = mbar_wait_warp(tempty_bar(buf), bphase ^ 1u, abort_flag, p.status) &&
+                     mbar_wait_warp(full_bar(stage), phase, abort_flag, p.status);
+                if (!ok) break;
+                tc_fence_after_sync();
+                const uint32_t addr = base + stage * static_cast<uint32_t>(at.stage);
+                const uint32_t q_addr = kFused ? base + at.q + static_cast<uint32_t>(kb - kb0) * BN * kFp8Block : addr + kFp8PTile;
+                mma_f8_kblock(tmem_base + buf * BN, make_smem_desc_sw128(addr), make_smem_desc_sw128(q_addr), kIdesc);
+                mma_commit(empty_bar(stage));
+                mma_commit(tfull_bar(buf));
+                if (++stage == nstages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+                buf ^= 1u;
+                if (buf == 0u) bphase ^= 1u;
+            }
+        }
+    } else {
+        // ------------------------------------------------------------------ epilogue warps
+        griddep_wait();
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t tmem_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + half * kCols;
+        float *scales_s = reinterpret_cast<float *>(smem_raw + at.scales);
+        if constexpr (kFused) {
+            // 16 half-warps quantize the tokens of this tile, k-block by k-block, into the layout that the MMAs read
+            // (rows of 128 bytes, 16-byte units exchanged by the row's place among eight)
+            int pt, qt;
+            tile_at(first_tile, pt, qt);
+            const int l = threadIdx.x & 15, hw = (static_cast<int>(threadIdx.x) - 64) >> 4;
+            const Y *x = static_cast<const Y *>(p.x);
+            const int items = (kb1 - kb0) * BN;            // BN is a multiple of 16: all half-warps go through the same number
+            for (int i0 = 0; i0 < items; i0 += 64) {
+                float v[4][8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int item = i0 + 16 * i + hw, r = item % BN, kb = item / BN, m = qt * BN + r;
+                    const bool on = item < items && m < p.rows;
+                    load8(x + (on ? m : 0) * p.x_pitch, (kb0 + kb) * kFp8Block + 8 * l, on ? p.cols : 0, p.x_whole, v[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int item = i0 + 16 * i + hw, r = item % BN, kb = item / BN;
+                    const float top = block_top(v[i]);
+                    const uint2 w = codes8(v[i], kFp8Max / top);
+                    if (item < items) {
+                        const int off = kb * BN * kFp8Block + r * 128 + (((l >> 1) ^ (r & 7)) << 4) + (l & 1) * 8;
+                        *reinterpret_cast<uint2 *>(smem_raw + at.q + off) = w;
+                        if (l == 0) scales_s[kb * BN + r] = top / kFp8Max;
+                    }
+                }
+            }
+            fence_proxy_async_smem();
+            asm volatile("bar.sync 1, 256;" ::: "memory");             // the scales are read by all epilogue warps
+            if (lane == 0) mbar_arrive(q_bar);
+        }
+        uint32_t buf = 0, bphase = 0;
+        for (int tile = first_tile; tile < tiles; tile += kOneTile ? tiles : static_cast<int>(gridDim.x)) {
+            int pt, qt;
+            tile_at(tile, pt, qt);
+            const int p_row = pt * 128 + quarter * 32 + lane;          // this thread's row of operand P
+            const int q_col = qt * BN + half * kCols;                  // its first row of operand Q
+            const int64_t scale_at = static_cast<int64_t>(min(kSwap ? q_col : p_row, p.rows - 1)) * p.scale_row;
+            const int w_block = (kSwap ? pt : q_col / kFp8Block);
+            // beyond the last output there is no scale; the sums there are not stored
+            const float *w_scales = p.w_scales + static_cast<int64_t>(min(w_block, (p.outputs - 1) / kFp8Block)) * p.blocks;
+            float acc[kCols];
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) acc[c] = 0.0f;
+            bool got = true;
+            float sw = __ldg(w_scales + kb0), sa = kSwap ? 0.0f : p.a_scales[scale_at + kb0 * p.scale_block];
+            for (int kb = kb0; kb < kb1; ++kb) {
+                const float row_factor = sw * sa;
+                const float sw_now = sw;
+                float col_factor[kSwap ? kCols : 1];
+                if constexpr (kSwap) {
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) {
+                        if constexpr (kFused)
+                            col_factor[c] = scales_s[(kb - kb0) * BN + half * kCols + c];
+                        else
+                            col_factor[c] = p.a_scales[static_cast<int64_t>(min(q_col + c, p.rows - 1)) * p.scale_row + kb * p.scale_block];
+                    }
+                }
+                if (kb + 1 < kb1) {
+                    sw = __ldg(w_scales + kb + 1);
+                    if (!kSwap) sa = p.a_scales[scale_at + (kb + 1) * p.scale_block];
+                }
+                if (!mbar_wait_warp(tfull_bar(buf), bphase, abort_flag, p.status)) {
+                    got = false;
+                    break;
+                }
+                tc_fence_after_sync();
+#pragma unroll
+                for (int c0 = 0; c0 < kCols; c0 += kLd) {
+                    uint32_t v[kLd];
+                    tmem_ld_cols<kLd>(tmem_row + buf * BN + c0, v);
+                    tmem_ld_wait();
+                    if (c0 + kLd == kCols) {                           // all read: the MMAs may have the buffer
+                        tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(tempty_bar(buf));
+                    }
+#pragma unroll
+                    for (int c = 0; c < kLd; c += 2) {
+                        if constexpr (kSwap)
+                            fma2(acc[c0 + c], acc[c0 + c + 1], col_factor[c0 + c] * sw_now, col_factor[c0 + c + 1] * sw_now, v[c], v[c + 1]);
+                        else
+                            fma2(acc[c0 + c], acc[c0 + c + 1], row_factor, row_factor, v[c], v[c + 1]);
+                    }
+                }
+                buf ^= 1u;
+                if (buf == 0u) bphase ^= 1u;
+            }
+            if constexpr (kOneTile) {
+                // this CTA's part, over the stages: all its loads have landed and all its MMAs are done
+                float *part = reinterpret_cast<float *>(smem_raw);
+                if (!got) break;
+                asm volatile("bar.sync 1, 256;" ::: "memory");         // every warp has seen the last MMA's end
+                if constexpr (kSwap) {
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) part[(half * kCols + c) * (128 + 4) + quarter * 32 + lane] = acc[c];
+                } else {
+                    float4 *row = reinterpret_cast<float4 *>(part + (quarter * 32 + lane) * (BN + 4) + half * kCols);
+#pragma unroll
+                    for (int c = 0; c < kCols; c += 4) row[c / 4] = make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]);
+                }
+            } else {
+                if (!got) break;
+                // through this warp's staging, 128 bytes of each of its 32 rows at a time, so that whole sectors are written
+                constexpr int kStep = 128 / sizeof(Y), kUnit = 16 / sizeof(Y);
+                uint8_t *stage = smem_raw + at.staging + (warp - 2) * kFp8Staging;
+                Y *y = static_cast<Y *>(p.y);
+                const int row0 = pt * 128 + quarter * 32;
+#pragma unroll
+                for (int c0 = 0; c0 < kCols; c0 += kStep) {
+                    if (q_col + c0 >= p.outputs || row0 >= p.rows) continue;               // the same for the whole warp
+                    __syncwarp();
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        __align__(16) Y out[kUnit];
+#pragma unroll
+                        for (int i = 0; i < kUnit; ++i) {
+                            const int c = c0 + u * kUnit + i;
+                            float v = acc[c];
+                            if (p.bias && q_col + c < p.outputs) v += __ldg(p.bias + q_col + c);
+                            out[i] = from_f32<Y>(v);
+                        }
+                        *reinterpret_cast<uint4 *>(stage + lane * 128 + ((u ^ (lane & 7)) << 4)) = *reinterpret_cast<const uint4 *>(out);
+                    }
+                    __syncwarp();
+                    const int u = lane & 7;
+#pragma unroll
+                    for (int r0 = 0; r0 < 32; r0 += 4) {
+                        const int r = r0 + (lane >> 3), n = q_col + c0 + u * kUnit;
+                        if (row0 + r >= p.rows) continue;
+                        const uint4 v = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((u ^ (r & 7)) << 4));
+                        Y *to = y + static_cast<int64_t>(row0 + r) * p.y_pitch + n;
+                        if (p.whole && n + kUnit <= p.outputs) {
+                            *reinterpret_cast<uint4 *>(to) = v;
+                        } else {
+                            for (int i = 0; i < kUnit && n + i < p.outputs; ++i) to[i] = reinterpret_cast<const Y *>(&v)[i];
+                        }
+                    }
+                }
+            }
+        }
+    }
+
+    if constexpr (kOneTile) {
+        // A part that gave up leaves what lies there: its error is in the status word, and nobody waits for it in vain.
+        if (p.split > 1)
+            cluster_sync_all();
+        else
+            __syncthreads();
+        int pt, qt;
+        tile_at(first_tile, pt, qt);
+        constexpr int kMajor = kSwap ? BN : 128, kMinor = kSwap ? 128 : BN, kPitch = kMinor + 4;
+        const int major0 = kMajor * rank / p.split, major1 = kMajor * (rank + 1) / p.split;
+        const int m0 = kSwap ? qt * BN : pt * 128, n0 = kSwap ? pt * 128 : qt * BN;
+        Y *y = static_cast<Y *>(p.y);
+        for (int i = major0 * kMinor + static_cast<int>(threadIdx.x); i < major1 * kMinor; i += kFp8Threads) {
+            const int r = i / kMinor, c = i % kMinor, m = m0 + r, n = n0 + c;
+            if (m >= p.rows) break;
+            if (n >= p.outputs) continue;
+            float v = 0.0f;
+            const uint32_t from = base + 4u * static_cast<uint32_t>(r * kPitch + c);
+            if (p.split > 1) {
+                float part[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) part[q] = q < p.split ? ld_cluster_f32(from, q) : 0.0f;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v += part[q];
+            } else {
+                v = *reinterpret_cast<const float *>(smem_raw + (from - base));
+            }
+            if (p.bias) v += __ldg(p.bias + n);
+            y[static_cast<int64_t>(m) * p.y_pitch + n] = from_f32<Y>(v);
+        }
+        if (p.split > 1) cluster_sync_all();               // nobody leaves while its part is read
+    }
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after_sync();
+        tmem_dealloc(tmem_base, kTmem);
+    }
+}
+
+}  // namespace ptq

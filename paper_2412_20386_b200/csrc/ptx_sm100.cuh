@@ -133,35 +133,6 @@ __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, vo
 // Number of this warp, known to the compiler to be the same for all of its lanes.
 __device__ __forceinline__ int uniform_warp() { return __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) >> 5, 0); }
 
-// Self-test of the bounded wait, for the failure-detection tests: one CTA of 64 threads and one mbarrier
-// that nothing ever arrives on (no copy, no MMA and no other thread refers to it, so giving up leaves
-// nothing in flight).  Thread 0 waits with the short limit `limit_ns` and must give up: it raises the
-// CTA's abort flag and sets PTQ_DEV_TIMEOUT in `status`.  Thread 32 waits on the same barrier with the
-// ordinary long limit and must leave through the abort flag.  out[0], out[1]: what the two waits returned
-// (0 = gave up); out[2]: nanoseconds thread 32 spent waiting.
-__global__ void __launch_bounds__(64) ptq_wait_selftest_kernel(unsigned *status, unsigned long long limit_ns,
-                                                               unsigned *out)
-{
-    __shared__ __align__(8) unsigned long long bar;
-    __shared__ uint32_t abort_word;
-    const uint32_t bar_addr = smem_u32(&bar);
-    if (threadIdx.x == 0) {
-        mbar_init(bar_addr, 1);
-        abort_word = 0u;
-        fence_mbar_init();
-    }
-    __syncthreads();
-    volatile uint32_t *abort_flag = &abort_word;
-    if (threadIdx.x == 0) {
-        out[0] = mbar_wait(bar_addr, 0u, abort_flag, status, limit_ns) ? 1u : 0u;
-    } else if (threadIdx.x == 32) {
-        const unsigned long long t0 = global_timer_ns();
-        out[1] = mbar_wait(bar_addr, 0u, abort_flag, status) ? 1u : 0u;
-        out[2] = static_cast<unsigned>(global_timer_ns() - t0);
-    }
-    __syncthreads();
-}
-
 // ---------------------------------------------------------------- proxies / fences
 __device__ __forceinline__ void fence_proxy_async_smem()
 {
