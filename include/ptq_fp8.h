@@ -58,7 +58,7 @@ ptq_status_t ptq_fp8_matmul(const ptq_fp8_weight_t *w, int64_t rows, const void 
 
 /* Both: quantizes the input and multiplies; y has the input's type.  workspace device, 16-byte aligned, at least
  * ptq_fp8_linear_workspace_bytes(rows, cols, outputs) bytes (0 for few rows: then it may be NULL).  Gives the bits that the
- * two calls give where the sums are cut alike: with up to 64 rows they may be cut otherwise. */
+ * two calls give where the sums are cut alike: with up to 16 rows they may be cut otherwise. */
 size_t ptq_fp8_linear_workspace_bytes(int64_t rows, int cols, int outputs);
 ptq_status_t ptq_fp8_linear(const ptq_fp8_weight_t *w, const ptq_fp8_input_t *in, void *y, int64_t y_pitch, void *workspace,
                             size_t workspace_bytes, void *stream);

@@ -63,6 +63,9 @@ ptq_status_t output_check(const void *y, int dtype, int64_t pitch, int outputs)
     return PTQ_OK;
 }
 
+// Whether the rows of x can be read 16 bytes at a time.
+bool input_whole(const ptq_fp8_input_t &in) { return aligned({in.x}, 16) && in.x_pitch % (16 / elem_bytes(in.dtype)) == 0 && in.cols % 8 == 0; }
+
 ptq_status_t quantize(const ptq_fp8_input_t &in, void *codes, int64_t codes_pitch, float *scales, int64_t scale_row, int64_t scale_block, cudaStream_t stream)
 {
     ptq::Fp8QuantizeParams p = {};
@@ -76,14 +79,19 @@ ptq_status_t quantize(const ptq_fp8_input_t &in, void *codes, int64_t codes_pitc
     p.scales = scales;
     p.scale_row = scale_row;
     p.scale_block = scale_block;
-    // rows first; where they do not fill the GPU, a CTA takes four blocks of a row instead of all
-    const int64_t groups = ceil_div(in.rows, ptq::kFp8QuantizeRows);
-    p.span = groups >= 8 * kSms ? p.blocks : 4;
-    const dim3 grid(static_cast<unsigned>(groups), static_cast<unsigned>(ceil_div(p.blocks, p.span)));
-    const bool whole = aligned({in.x}, 16) && in.x_pitch % (16 / elem_bytes(in.dtype)) == 0;
+    // three blocks at a time where that leaves fewer idle (six of 768 channels)
+    const int set = ceil_div(p.blocks, 3) * 3 < ceil_div(p.blocks, 4) * 4 ? 3 : 4;
+    p.sets = ptq::make_fastdiv(static_cast<unsigned>(ceil_div(p.blocks, set)));
+    const long long ctas = ceil_div(in.rows, ptq::kFp8QuantizeRows) * p.sets.d;
+    if (ctas > kMaxGrid) return fail(PTQ_ERR_SHAPE, "the input is too large for one launch");
     return with_type(in.dtype, [&](auto t) {
-        return with_flag(whole, [&](auto w) {
-            ptq::ptq_fp8_quantize_kernel<decltype(t), decltype(w)::value><<<grid, 256, 0, stream>>>(p);
+        using T = decltype(t);
+        return with_flag(input_whole(in), [&](auto whole) {
+            constexpr bool kWhole = decltype(whole)::value;
+            if (set == 3)
+                ptq::ptq_fp8_quantize_kernel<T, 3, kWhole><<<static_cast<unsigned>(ctas), 256, 0, stream>>>(p);
+            else
+                ptq::ptq_fp8_quantize_kernel<T, 4, kWhole><<<static_cast<unsigned>(ctas), 256, 0, stream>>>(p);
             return launched();
         });
     });
@@ -91,48 +99,53 @@ ptq_status_t quantize(const ptq_fp8_input_t &in, void *codes, int64_t codes_pitc
 
 // Which kernel, and how a product is cut.  bn: columns of a tile; one: a tile or a part of one per CTA.
 struct Fp8Plan {
-    int bn, split, stages;
-    bool swap, one, fused;
+    int bn, split;
+    bool swap, one;
 };
 constexpr int kFp8Smem = 232448;
-// The cost of a cut, in cycles: a k-block takes what its operands take from L2 (about 64 bytes a cycle and SM; for BN = 256 the tensor pipe is as
-// slow), a tile its start and its stores, a split the cluster's barriers and the sums.
-Fp8Plan product_plan(int64_t rows, int blocks, int outputs, bool fused)
+// The cost of a cut, in microseconds, fitted to 9 cuts each of 16 products (1 .. 50432 rows): a k-block of a tile, bound by its loads; a tile's
+// start and stores; a split tile's barriers and sums.  Rows of y that begin anywhere cost a tile of many rows more (its lanes hold rows).
+// The two forms with 16 and with 256 columns, say: 1 x 4096 -> 4096 6.6 and 17 us, 2048 x 2048 -> 2048 over 100 and 12.2.
+Fp8Plan product_plan(int64_t rows, int blocks, int outputs, bool fused, bool whole)
 {
     Fp8Plan best = {};
     double least = -1.0;
     const auto consider = [&](int bn, bool swap, bool one, int split) {
         const long long tiles = swap ? ceil_div(outputs, 128) * ceil_div(rows, bn) : ceil_div(rows, 128) * ceil_div(outputs, bn);
-        const double step = 2.2 * (128 + bn);
+        const double step = bn == 256 ? 0.53 : bn == 128 ? 0.34 : bn == 64 ? 0.30 : bn == 32 ? 0.27 : 0.25;
+        const double ragged = swap || whole ? 0.0 : bn / 50.0;
         double cost;
-        if (one) {
-            const double waves = static_cast<double>(ceil_div(tiles * split, kSms));
-            cost = waves * (static_cast<double>(ceil_div(blocks, split)) * step + 3500.0 + 12.0 * bn / split + (split > 1 ? 1200.0 : 0.0));
-        } else {
-            cost = static_cast<double>(ceil_div(tiles, kSms)) * (blocks * step + 4.0 * bn) + 3500.0;
-        }
+        if (one)
+            cost = 3.8 + static_cast<double>(ceil_div(tiles * split, kSms)) *
+                             (static_cast<double>(ceil_div(blocks, split)) * step + ragged / split + bn / 128.0 * (1.0 + 0.6 * split) + (split > 1 ? 0.6 : 0.0));
+        else
+            cost = 2.3 + static_cast<double>(ceil_div(tiles, kSms)) * (blocks * step + ragged + bn / 128.0);
         if (least < 0.0 || cost < least) {
             least = cost;
-            best = {bn, split, 0, swap, one, fused};
+            best = {bn, split, swap, one};
         }
     };
     for (int split = 1; split <= 8 && split <= blocks; split *= 2) {
+        const int part = static_cast<int>(ceil_div(blocks, split));
+        if (fused) {
+            if (part <= ptq::kFp8MaxFused) consider(ptq::kFp8FusedRows, true, true, split);
+            continue;
+        }
         for (int bn : {16, 32, 64})
-            if (rows <= 4096 && (!fused || ceil_div(blocks, split) * bn / 16 <= ptq::kFp8MaxFused)) consider(bn, true, true, split);
-        if (!fused)
-            for (int bn : {64, 128}) consider(bn, false, true, split);
+            if (rows <= 4096 && part * bn <= ptq::kFp8MaxScales) consider(bn, true, true, split);
+        for (int bn : {64, 128}) consider(bn, false, true, split);
     }
     if (!fused)
         for (int bn : {128, 256}) consider(bn, false, false, 1);
     return best;
 }
 // Few rows are quantized by the CTAs that multiply them, each for itself: one launch instead of two.
-bool linear_fused(int64_t rows, int blocks) { return rows <= 64 && blocks <= 8 * ptq::kFp8MaxFused; }
+bool linear_fused(int64_t rows, int blocks) { return rows <= ptq::kFp8FusedRows && blocks <= 8 * ptq::kFp8MaxFused; }
 
-template <typename Y, int BN, bool kSwap, bool kOneTile, bool kFused>
+template <typename Y, int BN, bool kSwap, bool kOneTile, bool kFused, bool kWhole>
 ptq_status_t launch_product(const Fp8Plan &plan, const ptq::Fp8Params &params, const CUtensorMap &tmP, const CUtensorMap &tmQ, bool next, cudaStream_t stream)
 {
-    constexpr auto kKern = ptq::ptq_fp8_matmul_kernel<Y, BN, kSwap, kOneTile, kFused>;
+    constexpr auto kKern = ptq::ptq_fp8_matmul_kernel<Y, BN, kSwap, kOneTile, kFused, kWhole>;
     PTQ_TRY(ensure_smem<kKern>(kFp8Smem));
     ptq::Fp8Params p = params;
     const int part = static_cast<int>(ceil_div(p.blocks, plan.split));
@@ -164,37 +177,37 @@ ptq_status_t launch_product(const Fp8Plan &plan, const ptq::Fp8Params &params, c
     return launched();
 }
 
-// The product; `fused`: of p.x, else of the codes at `a`.
-ptq_status_t product(const ptq_fp8_weight_t &w, ptq::Fp8Params p, const void *a, int64_t a_pitch, int y_dtype, bool fused, bool next, cudaStream_t stream)
+// The product of the codes at `a` or, where there are none, of p.x (x_whole: input_whole).
+ptq_status_t product(const ptq_fp8_weight_t &w, ptq::Fp8Params p, const void *a, int64_t a_pitch, int y_dtype, bool x_whole, bool next, cudaStream_t stream)
 {
-    const Fp8Plan plan = product_plan(p.rows, p.blocks, p.outputs, fused);
+    const bool fused = a == nullptr;
+    p.whole = aligned({p.y}, 16) && p.y_pitch % (16 / elem_bytes(y_dtype)) == 0;
+    const Fp8Plan plan = product_plan(p.rows, p.blocks, p.outputs, fused, p.whole);
     p.split = plan.split;
     p.p_tiles = static_cast<int>(ceil_div(plan.swap ? p.outputs : p.rows, 128));
     p.q_tiles = static_cast<int>(ceil_div(plan.swap ? p.rows : p.outputs, plan.bn));
     // the group of tiles that run together is counted in 32 bits
     if (static_cast<long long>(p.p_tiles + 12) * p.q_tiles * plan.split > 0x7fffffffll) return fail(PTQ_ERR_SHAPE, "the product is too large for one launch");
-    p.whole = aligned({p.y}, 16) && p.y_pitch % (16 / elem_bytes(y_dtype)) == 0;
     PTQ_TRY(status_word(&p.status));
     CUtensorMap tmW, tmA = {};
     PTQ_TRY(make_map_2d(&tmW, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, w.codes, p.cols, p.outputs, w.codes_pitch, ptq::kFp8Block, plan.swap ? 128 : plan.bn));
     if (!fused) PTQ_TRY(make_map_2d(&tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a, p.cols, p.rows, a_pitch, ptq::kFp8Block, plan.swap ? plan.bn : 128));
     return with_type(y_dtype, [&](auto t) -> ptq_status_t {
         using Y = decltype(t);
+        if (fused)
+            return with_flag(x_whole, [&](auto whole) {
+                return launch_product<Y, ptq::kFp8FusedRows, true, true, true, decltype(whole)::value>(plan, p, tmW, tmW, next, stream);
+            });
         if (plan.swap) {
-            const auto few = [&](auto n) -> ptq_status_t {
-                constexpr int kBN = decltype(n)::value;
-                return fused ? launch_product<Y, kBN, true, true, true>(plan, p, tmW, tmW, next, stream)
-                             : launch_product<Y, kBN, true, true, false>(plan, p, tmW, tmA, next, stream);
-            };
-            if (plan.bn == 16) return few(std::integral_constant<int, 16>());
-            if (plan.bn == 32) return few(std::integral_constant<int, 32>());
-            return few(std::integral_constant<int, 64>());
+            if (plan.bn == 16) return launch_product<Y, 16, true, true, false, false>(plan, p, tmW, tmA, next, stream);
+            if (plan.bn == 32) return launch_product<Y, 32, true, true, false, false>(plan, p, tmW, tmA, next, stream);
+            return launch_product<Y, 64, true, true, false, false>(plan, p, tmW, tmA, next, stream);
         }
         if (plan.one)
-            return plan.bn == 64 ? launch_product<Y, 64, false, true, false>(plan, p, tmA, tmW, next, stream)
-                                 : launch_product<Y, 128, false, true, false>(plan, p, tmA, tmW, next, stream);
-        return plan.bn == 128 ? launch_product<Y, 128, false, false, false>(plan, p, tmA, tmW, next, stream)
-                              : launch_product<Y, 256, false, false, false>(plan, p, tmA, tmW, next, stream);
+            return plan.bn == 64 ? launch_product<Y, 64, false, true, false, false>(plan, p, tmA, tmW, next, stream)
+                                 : launch_product<Y, 128, false, true, false, false>(plan, p, tmA, tmW, next, stream);
+        return plan.bn == 128 ? launch_product<Y, 128, false, false, false, false>(plan, p, tmA, tmW, next, stream)
+                              : launch_product<Y, 256, false, false, false, false>(plan, p, tmA, tmW, next, stream);
     });
 }
 
@@ -289,8 +302,7 @@ ptq_status_t ptq_fp8_linear(const ptq_fp8_weight_t *w, const ptq_fp8_input_t *in
     if (need == 0) {
         p.x = in->x;
         p.x_pitch = in->x_pitch;
-        p.x_whole = aligned({in->x}, 16) && in->x_pitch % (16 / elem_bytes(in->dtype)) == 0;
-        return product(*w, p, nullptr, 0, in->dtype, true, false, st);
+        return product(*w, p, nullptr, 0, in->dtype, input_whole(*in), false, st);
     }
     const int64_t pitch = ceil_div(in->cols, 16) * 16;
     float *scales = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + padded(static_cast<size_t>(in->rows) * pitch));

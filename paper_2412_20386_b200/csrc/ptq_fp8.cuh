@@ -6,6 +6,8 @@
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
+#include <type_traits>
+
 #include "ptx_sm100.cuh"
 
 namespace ptq {
@@ -26,6 +28,21 @@ __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2hal
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <>
+__device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi)
+{
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+template <>
+__device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
 // max(a, |b|) that keeps a NaN of either side.
 __device__ __forceinline__ float max_abs_nan(float a, float b)
 {
@@ -34,16 +51,23 @@ __device__ __forceinline__ float max_abs_nan(float a, float b)
     return r;
 }
 
-// Eight values of a row from column c on (zeros from `cols` on): one or two 16-byte loads where whole, else one by one.
-template <typename T>
-__device__ __forceinline__ void load8(const T *row, int c, int cols, bool whole, float (&v)[8])
+// Eight values of a row from column c on, zeros from `cols` on.  kWhole: 16 bytes at a time; rows begin on multiples of 16 bytes and
+// cols is a multiple of 8.
+template <bool kWhole, typename T>
+__device__ __forceinline__ void load8(const T *row, int c, int cols, float (&v)[8])
 {
-    if (whole && c + 8 <= cols) {
+    if constexpr (kWhole) {
+        const bool on = c < cols;
         if constexpr (sizeof(T) == 4) {
-            const float4 a = __ldg(reinterpret_cast<const float4 *>(row + c)), b = __ldg(reinterpret_cast<const float4 *>(row + c) + 1);
+            float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
+            if (on) {
+                a = __ldg(reinterpret_cast<const float4 *>(row + c));
+                b = __ldg(reinterpret_cast<const float4 *>(row + c) + 1);
+            }
             v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
         } else {
-            const uint4 a = __ldg(reinterpret_cast<const uint4 *>(row + c));
+            uint4 a = make_uint4(0u, 0u, 0u, 0u);
+            if (on) a = __ldg(reinterpret_cast<const uint4 *>(row + c));
             const T *t = reinterpret_cast<const T *>(&a);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = to_f32(t[i]);
@@ -86,38 +110,37 @@ __device__ __forceinline__ void store_codes8(uint8_t *row, int c, int cols, uint
 
 // ---------------------------------------------------------------------------------------------------- quantize
 // Bound by memory: 16-bit values are read, codes and a scale for each 128 of them written, once each.  Half a warp holds a block
-// (16 bytes of 16-bit values a lane), four of a row at a time, so that four loads a lane are in flight; the 16 half-warps of a
-// CTA take 16 neighbouring rows, whose scales lie next to each other in the layout that the product reads.
+// (16 bytes of 16-bit values a lane), kSet neighbouring ones of a row at a time, so that as many loads a lane are in flight; the 16
+// half-warps of a CTA take 16 neighbouring rows, whose scales lie next to each other in the layout that the product reads.
 struct Fp8QuantizeParams {
     const void *x;
     int64_t x_pitch, codes_pitch, scale_row, scale_block;
     int64_t rows;
-    int cols, blocks, span;           // blocks of a row; how many of them a CTA goes over
+    int cols, blocks;                 // blocks of a row
+    FastDiv sets;                     // sets of kSet blocks of a row
     uint8_t *codes;
     float *scales;
 };
 constexpr int kFp8QuantizeRows = 16;
-template <typename T, bool kWhole>
-__global__ void __launch_bounds__(256) ptq_fp8_quantize_kernel(const Fp8QuantizeParams p)
+template <typename T, int kSet, bool kWhole>
+__global__ void __launch_bounds__(256, 6) ptq_fp8_quantize_kernel(const Fp8QuantizeParams p)
 {
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * kFp8QuantizeRows + (threadIdx.x >> 4);
-    const int l = threadIdx.x & 15;
+    const unsigned group = fd_div(blockIdx.x, p.sets);
+    const int64_t row = static_cast<int64_t>(group) * kFp8QuantizeRows + (threadIdx.x >> 4);
+    const int b0 = static_cast<int>(blockIdx.x - group * p.sets.d) * kSet, l = threadIdx.x & 15;
     const bool on = row < p.rows;                       // the others go along: the shuffles are the warp's
     const T *x = static_cast<const T *>(p.x) + (on ? row : 0) * p.x_pitch;
-    const int first = blockIdx.y * p.span, last = min(p.blocks, first + p.span);
     griddep_launch_dependents();
-    for (int b0 = first; b0 < last; b0 += 4) {
-        float v[4][8];
+    float v[kSet][8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) load8(x, (b0 + i) * kFp8Block + 8 * l, on && b0 + i < last ? p.cols : 0, kWhole, v[i]);
+    for (int i = 0; i < kSet; ++i) load8<kWhole>(x, (b0 + i) * kFp8Block + 8 * l, on ? p.cols : 0, v[i]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float top = block_top(v[i]);
-            const uint2 w = codes8(v[i], kFp8Max / top);
-            if (!on || b0 + i >= last) continue;
-            store_codes8(p.codes + row * p.codes_pitch, (b0 + i) * kFp8Block + 8 * l, p.cols, w);
-            if (l == 0) p.scales[row * p.scale_row + (b0 + i) * p.scale_block] = top / kFp8Max;
-        }
+    for (int i = 0; i < kSet; ++i) {
+        const float top = block_top(v[i]);
+        const uint2 w = codes8(v[i], kFp8Max / top);
+        if (!on || b0 + i >= p.blocks) continue;
+        store_codes8(p.codes + row * p.codes_pitch, (b0 + i) * kFp8Block + 8 * l, p.cols, w);
+        if (l == 0) p.scales[row * p.scale_row + (b0 + i) * p.scale_block] = top / kFp8Max;
     }
 }
 
@@ -131,7 +154,7 @@ __global__ void __launch_bounds__(256) ptq_fp8_quantize_weight_kernel(const Fp8Q
     float v[8], top = kFp8Least;
     for (int r = h; r < kFp8Block; r += 16) {
         const int64_t row = row0 + r;
-        load8(static_cast<const T *>(p.x) + (row < p.rows ? row : 0) * p.x_pitch, c, row < p.rows ? p.cols : 0, false, v);
+        load8<false>(static_cast<const T *>(p.x) + (row < p.rows ? row : 0) * p.x_pitch, c, row < p.rows ? p.cols : 0, v);
         top = max_abs_nan(top, block_top(v));
     }
     top = max_abs_nan(top, __shfl_xor_sync(0xffffffffu, top, 16));
@@ -141,7 +164,7 @@ __global__ void __launch_bounds__(256) ptq_fp8_quantize_weight_kernel(const Fp8Q
     for (int r = h; r < kFp8Block; r += 16) {
         const int64_t row = row0 + r;
         if (row >= p.rows) break;
-        load8(static_cast<const T *>(p.x) + row * p.x_pitch, c, p.cols, false, v);
+        load8<false>(static_cast<const T *>(p.x) + row * p.x_pitch, c, p.cols, v);
         store_codes8(p.codes + row * p.codes_pitch, c, p.cols, codes8(v, kFp8Max / top));
     }
     if (threadIdx.x == 0) p.scales[static_cast<int64_t>(blockIdx.y) * p.blocks + blockIdx.x] = top / kFp8Max;
@@ -153,10 +176,9 @@ __global__ void __launch_bounds__(256) ptq_fp8_quantize_weight_kernel(const Fp8Q
 // keep in registers, while the tensor pipe fills the other one.  The scales cannot go into the operands (they are not powers
 // of two) nor be put off to the end (they change with every k-block).
 //
-// Warp 0 issues the TMA loads, warp 1 the MMAs, warps 2 .. 9 read: 32 TMEM lanes each, the two sets of four half of the
+// Warp 0 issues the TMA loads, warp 1 the MMAs, warps 4 .. 11 read: 32 TMEM lanes each, the two teams of four half of the
 // columns each.  A tile is 128 (TMEM lanes, operand P) x BN (TMEM columns, operand Q):
-//   many rows   P = activations, Q = weights.  Persistent CTAs.  With BN = 256 a k-block takes the tensor pipe about 512 cycles,
-//               and the eight warps 2 x 128 columns of TMEM loads and packed multiply-adds per scheduler: less than that.
+//   many rows   P = activations, Q = weights.  Persistent CTAs.
 //   few rows    P = weights, Q = the tokens (BN = 16, 32 or 64): no lane is wasted on rows that are not there.
 // Where there are fewer tiles than SMs the k-blocks of a tile are split over a cluster of up to eight CTAs, which add their
 // parts through distributed shared memory in the order of the parts.
@@ -170,16 +192,19 @@ struct Fp8Params {
     int rows, cols, outputs, blocks;  // blocks: k-blocks
     int p_tiles, q_tiles, split;
     int stages;
-    bool whole, x_whole;              // rows of y, of x can be moved 16 bytes at a time
+    bool whole;                       // rows of y can be moved 16 bytes at a time
     unsigned *status;
 };
 
-constexpr int kFp8Threads = 320;
+constexpr int kFp8Threads = 384;                           // warps 0 TMA, 1 MMA, 4 .. 11 read
 constexpr int kFp8MaxStages = 8;
 constexpr int kFp8PTile = 128 * kFp8Block;                 // bytes of one k-block of operand P
 constexpr int kFp8Staging = 4096;                          // bytes of an epilogue warp's staging: 32 rows of 128 bytes
-constexpr int kFp8MaxFused = 64;                           // k-blocks x tokens / 16 that a fused CTA may hold (2 KB each)
+constexpr int kFp8FusedRows = 16;                          // tokens that the CTAs quantize themselves, at most
+constexpr int kFp8MaxFused = 64;                           // k-blocks of them that a CTA may hold (2 KB each)
+constexpr int kFp8MaxScales = 8192;                        // scales of tokens (k-blocks x BN) that a CTA may hold
 
+// The four MMAs of a k-block into a fresh accumulator; called by a whole warp, one lane issues.
 __device__ __forceinline__ void mma_f8_kblock(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc)
 {
     asm volatile(
@@ -232,38 +257,43 @@ __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&v)[N])
     }
 }
 
-// (a0, a1) += (f0 b0, f1 b1), two binary32 multiply-adds in one instruction.
-__device__ __forceinline__ void fma2(float &a0, float &a1, float f0, float f1, uint32_t b0, uint32_t b1)
+// Waits for this thread's TMEM loads; the values are named so that nothing reads them before.
+template <int N>
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&v)[N])
 {
-    asm("{\n\t"
-        ".reg .b64 a, f, b;\n\t"
-        "mov.b64 a, {%0, %1};\n\t"
-        "mov.b64 f, {%2, %3};\n\t"
-        "mov.b64 b, {%4, %5};\n\t"
-        "fma.rn.f32x2 a, f, b, a;\n\t"
-        "mov.b64 {%0, %1}, a;\n\t"
-        "}"
-        : "+f"(a0), "+f"(a1)
-        : "f"(f0), "f"(f1), "r"(b0), "r"(b1));
+    tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+r"(v[i]));
 }
 
-__device__ __forceinline__ float ld_cluster_f32(uint32_t local_addr, uint32_t rank)
+// Floats of the shared memory of the CTA `rank` of the cluster, at the address that they have here.
+__device__ __forceinline__ void ld_cluster(uint32_t local_addr, uint32_t rank, float (&v)[1])
 {
-    float v;
     asm volatile(
         "{\n\t"
         ".reg .b32 ra;\n\t"
         "mapa.shared::cluster.u32 ra, %1, %2;\n\t"
         "ld.shared::cluster.f32 %0, [ra];\n\t"
         "}"
-        : "=f"(v)
+        : "=f"(v[0])
         : "r"(local_addr), "r"(rank)
         : "memory");
-    return v;
+}
+__device__ __forceinline__ void ld_cluster(uint32_t local_addr, uint32_t rank, float (&v)[4])
+{
+    asm volatile(
+        "{\n\t"
+        ".reg .b32 ra;\n\t"
+        "mapa.shared::cluster.u32 ra, %4, %5;\n\t"
+        "ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [ra];\n\t"
+        "}"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3])
+        : "r"(local_addr), "r"(rank)
+        : "memory");
 }
 
 // Shared memory: stages of (P tile, Q tile) or, fused, stages of P tiles and all Q tiles of the CTA; staging of the epilogue
-// warps (persistent kernels only); fused: scales [k-block][BN]; barriers.
+// warps (persistent kernels only); few rows: scales [k-block][BN]; barriers.
 struct Fp8Layout {
     int stage, q, staging, scales, bars, bytes;
 };
@@ -275,7 +305,7 @@ __host__ __device__ constexpr Fp8Layout fp8_layout(int stages, int blocks)
     l.q = stages * l.stage;
     l.staging = l.q + (kFused ? blocks * BN * kFp8Block : 0);
     l.scales = l.staging + (kOneTile ? 0 : 8 * kFp8Staging);
-    l.bars = l.scales + (kFused ? blocks * BN * 4 : 0);
+    l.bars = l.scales + (kSwap ? blocks * BN * 4 : 0);
     l.bytes = l.bars + 8 * (2 * kFp8MaxStages + 5) + 16;
     // the parts of a split tile lie over the stages, with 4 floats between the rows
     const int parts = kOneTile ? 4 * (kSwap ? BN * (128 + 4) : 128 * (BN + 4)) : 0;
@@ -286,8 +316,9 @@ __host__ __device__ constexpr Fp8Layout fp8_layout(int stages, int blocks)
     return l;
 }
 
-// kOneTile: one tile, or one part of one, per CTA; else persistent.  kFused: operand Q is quantized here from x.
-template <typename Y, int BN, bool kSwap, bool kOneTile, bool kFused>
+// kOneTile: one tile, or one part of one, per CTA; else persistent.  kFused: operand Q is quantized here from x; kWhole: 16 bytes at a
+// time.
+template <typename Y, int BN, bool kSwap, bool kOneTile, bool kFused, bool kWhole>
 __global__ void __launch_bounds__(kFp8Threads, 1)
 ptq_fp8_matmul_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CUtensorMap tmQ, const Fp8Params p)
 {
@@ -297,6 +328,9 @@ ptq_fp8_matmul_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_cons
     constexpr int kLd = kCols < 32 ? kCols : 32;           // columns of one TMEM load
     constexpr uint32_t kTmem = 2 * BN;
     constexpr uint32_t kIdesc = make_idesc_e4m3(128, BN);
+    // The sums of 128 columns and a TMEM load want more registers than 384 threads can have alike: 168 each at the launch,
+    // then 4 x 32 x 40 + 8 x 32 x 232 = 64512, as many.
+    constexpr bool kMoreRegs = kCols == 128;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const uint32_t base = smem_u32(smem_raw);
     if ((base & 1023u) != 0u) {                            // never expected; the same in all CTAs of a cluster
@@ -304,7 +338,8 @@ ptq_fp8_matmul_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_cons
         return;
     }
     const int rank = kOneTile ? static_cast<int>(blockIdx.x) % p.split : 0;
-    const int first_tile = kOneTile ? static_cast<int>(blockIdx.x) / p.split : static_cast<int>(blockIdx.x);
+    const int first_tile = static_cast<int>(blockIdx.x) / (kOneTile ? p.split : 1);
+    const int stride = static_cast<int>(gridDim.x) / (kOneTile ? p.split : 1);         // one tile: all of them
     const int tiles = p.p_tiles * p.q_tiles;
     // the k-blocks of this CTA
     const int kb0 = kOneTile ? static_cast<int>(static_cast<int64_t>(p.blocks) * rank / p.split) : 0;
@@ -353,88 +388,94 @@ ptq_fp8_matmul_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_cons
         qt = r / in_group;
     };
 
-    if (warp == 0) {
-        // ------------------------------------------------------------------ TMA producer
-        uint32_t stage = 0, phase = 0, issued = 0;
-        bool ok = true;
-        const uint32_t tx = static_cast<uint32_t>(at.stage);           // boxes count whole, also beyond the ends
-        griddep_wait();
-        for (int tile = first_tile; tile < tiles && ok; tile += kOneTile ? tiles : static_cast<int>(gridDim.x)) {
-            int pt, qt;
-            tile_at(tile, pt, qt);
-            for (int kb = kb0; kb < kb1; ++kb) {
-                if (!mbar_wait_warp(empty_bar(stage), phase ^ 1u, abort_flag, p.status)) {
-                    ok = false;
-                    break;
-                }
-                const uint32_t dst = base + stage * static_cast<uint32_t>(at.stage);
-                mbar_arrive_expect_tx_warp(full_bar(stage), tx);
-                tma_load_2d_warp(dst, &tmP, kb * kFp8Block, pt * 128, full_bar(stage));
-                if (!kFused) tma_load_2d_warp(dst + kFp8PTile, &tmQ, kb * kFp8Block, qt * BN, full_bar(stage));
-                ++issued;
-                if (++stage == nstages) {
-                    stage = 0;
-                    phase ^= 1u;
-                }
-            }
-        }
-        if (!ok) {
-            // Error path only: the loads in flight land before the CTA gives up its shared memory (bounded).
-            for (uint32_t s = 0; s < nstages; ++s) {
-                const uint32_t uses = (issued + nstages - 1u - s) / nstages;
-                if (uses == 0u) continue;
-                for (int i = 0; i < 200000 && !mbar_try_wait(full_bar(s), (uses - 1u) & 1u); ++i) {
+    if (warp < 4) {
+        if constexpr (kMoreRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (warp == 0) {
+            // -------------------------------------------------------------- TMA producer
+            uint32_t stage = 0, phase = 0, issued = 0;
+            bool ok = true;
+            const uint32_t tx = static_cast<uint32_t>(at.stage);       // boxes count whole, also beyond the ends
+            griddep_wait();
+            for (int tile = first_tile; tile < tiles && ok; tile += stride) {
+                int pt, qt;
+                tile_at(tile, pt, qt);
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (!mbar_wait_warp(empty_bar(stage), phase ^ 1u, abort_flag, p.status)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t dst = base + stage * static_cast<uint32_t>(at.stage);
+                    mbar_arrive_expect_tx_warp(full_bar(stage), tx);
+                    tma_load_2d_warp(dst, &tmP, kb * kFp8Block, pt * 128, full_bar(stage));
+                    if (!kFused) tma_load_2d_warp(dst + kFp8PTile, &tmQ, kb * kFp8Block, qt * BN, full_bar(stage));
+                    ++issued;
+                    if (++stage == nstages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
                 }
             }
-        }
-    } else if (warp == 1) {
-        // ------------------------------------------------------------------ MMA issuer
-        uint32_t stage = 0, phase = 0, buf = 0, bphase = 0;
-        bool ok = !kFused || mbar_wait_warp(q_bar, 0u, abort_flag, p.status);
-        for (int tile = first_tile; tile < tiles && ok; tile += kOneTile ? tiles : static_cast<int>(gridDim.x)) {
-            for (int kb = kb0; kb < kb1; ++kb) {
-                ok = mbar_wait_warp(tempty_bar(buf), bphase ^ 1u, abort_flag, p.status) &&
-                     mbar_wait_warp(full_bar(stage), phase, abort_flag, p.status);
-                if (!ok) break;
-                tc_fence_after_sync();
-                const uint32_t addr = base + stage * static_cast<uint32_t>(at.stage);
-                const uint32_t q_addr = kFused ? base + at.q + static_cast<uint32_t>(kb - kb0) * BN * kFp8Block : addr + kFp8PTile;
-                mma_f8_kblock(tmem_base + buf * BN, make_smem_desc_sw128(addr), make_smem_desc_sw128(q_addr), kIdesc);
-                mma_commit(empty_bar(stage));
-                mma_commit(tfull_bar(buf));
-                if (++stage == nstages) {
-                    stage = 0;
-                    phase ^= 1u;
+            if (!ok) {
+                // Error path only: the loads in flight land before the CTA gives up its shared memory (bounded).
+                for (uint32_t s = 0; s < nstages; ++s) {
+                    const uint32_t uses = (issued + nstages - 1u - s) / nstages;
+                    if (uses == 0u) continue;
+                    for (int i = 0; i < 200000 && !mbar_try_wait(full_bar(s), (uses - 1u) & 1u); ++i) {
+                    }
                 }
-                buf ^= 1u;
-                if (buf == 0u) bphase ^= 1u;
+            }
+        } else if (warp == 1) {
+            // -------------------------------------------------------------- MMA issuer
+            uint32_t stage = 0, phase = 0, buf = 0, bphase = 0;
+            bool ok = !kFused || mbar_wait_warp(q_bar, 0u, abort_flag, p.status);
+            for (int tile = first_tile; tile < tiles && ok; tile += stride) {
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    ok = mbar_wait_warp(tempty_bar(buf), bphase ^ 1u, abort_flag, p.status) &&
+                         mbar_wait_warp(full_bar(stage), phase, abort_flag, p.status);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    const uint32_t addr = base + stage * static_cast<uint32_t>(at.stage);
+                    const uint32_t q_addr = kFused ? base + at.q + static_cast<uint32_t>(kb - kb0) * BN * kFp8Block : addr + kFp8PTile;
+                    mma_f8_kblock(tmem_base + buf * BN, make_smem_desc_sw128(addr), make_smem_desc_sw128(q_addr), kIdesc);
+                    mma_commit(empty_bar(stage));
+                    mma_commit(tfull_bar(buf));
+                    if (++stage == nstages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                    buf ^= 1u;
+                    if (buf == 0u) bphase ^= 1u;
+                }
             }
         }
     } else {
         // ------------------------------------------------------------------ epilogue warps
+        if constexpr (kMoreRegs) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
         griddep_wait();
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
         const uint32_t tmem_row = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + half * kCols;
         float *scales_s = reinterpret_cast<float *>(smem_raw + at.scales);
+        const int et = static_cast<int>(threadIdx.x) - 128;            // 0 .. 255 among the epilogue threads
         if constexpr (kFused) {
-            // 16 half-warps quantize the tokens of this tile, k-block by k-block, into the layout that the MMAs read
-            // (rows of 128 bytes, 16-byte units exchanged by the row's place among eight)
-            int pt, qt;
-            tile_at(first_tile, pt, qt);
-            const int l = threadIdx.x & 15, hw = (static_cast<int>(threadIdx.x) - 64) >> 4;
+            // 16 half-warps quantize the tokens of this tile, four blocks at a time each, into the layout that the MMAs read
+            // (rows of 128 bytes, 16-byte units exchanged by the row's place among eight); rows that are not there are zeros
+            const int l = et & 15, tokens = p.rows, items = (kb1 - kb0) * tokens;          // tokens <= BN: one Q tile
             const Y *x = static_cast<const Y *>(p.x);
-            const int items = (kb1 - kb0) * BN;            // BN is a multiple of 16: all half-warps go through the same number
+            for (int i = et; i < (kb1 - kb0) * BN * (kFp8Block / 16); i += 256)
+                *reinterpret_cast<uint4 *>(smem_raw + at.q + 16 * i) = make_uint4(0u, 0u, 0u, 0u);
+            for (int i = et; i < (kb1 - kb0) * BN; i += 256) scales_s[i] = 0.0f;
+            asm volatile("bar.sync 1, 256;" ::: "memory");
             for (int i0 = 0; i0 < items; i0 += 64) {
                 float v[4][8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int item = i0 + 16 * i + hw, r = item % BN, kb = item / BN, m = qt * BN + r;
-                    const bool on = item < items && m < p.rows;
-                    load8(x + (on ? m : 0) * p.x_pitch, (kb0 + kb) * kFp8Block + 8 * l, on ? p.cols : 0, p.x_whole, v[i]);
+                    const int item = i0 + 16 * i + (et >> 4), kb = item / tokens, r = item - kb * tokens;
+                    const bool on = item < items;
+                    load8<kWhole>(x + (on ? r : 0) * p.x_pitch, (kb0 + kb) * kFp8Block + 8 * l, on ? p.cols : 0, v[i]);
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int item = i0 + 16 * i + hw, r = item % BN, kb = item / BN;
+                    const int item = i0 + 16 * i + (et >> 4), kb = item / tokens, r = item - kb * tokens;
                     const float top = block_top(v[i]);
                     const uint2 w = codes8(v[i], kFp8Max / top);
                     if (item < items) {
@@ -447,14 +488,22 @@ ptq_fp8_matmul_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_cons
             fence_proxy_async_smem();
             asm volatile("bar.sync 1, 256;" ::: "memory");             // the scales are read by all epilogue warps
             if (lane == 0) mbar_arrive(q_bar);
+        } else if constexpr (kSwap) {
+            int pt, qt;
+            tile_at(first_tile, pt, qt);
+            for (int i = et; i < (kb1 - kb0) * BN; i += 256) {
+                const int kb = i / BN, m = qt * BN + i % BN;
+                scales_s[i] = m < p.rows ? p.a_scales[m * p.scale_row + (kb0 + kb) * p.scale_block] : 0.0f;
+            }
+            asm volatile("bar.sync 1, 256;" ::: "memory");
         }
         uint32_t buf = 0, bphase = 0;
-        for (int tile = first_tile; tile < tiles; tile += kOneTile ? tiles : static_cast<int>(gridDim.x)) {
+        for (int tile = first_tile; tile < tiles; tile += stride) {
             int pt, qt;
             tile_at(tile, pt, qt);
-            const int p_row = pt * 128 + quarter * 32 + lane;          // this thread's row of operand P
+            const int p_row0 = pt * 128 + quarter * 32;            // this warp's rows of operand P; a thread has one
             const int q_col = qt * BN + half * kCols;                  // its first row of operand Q
-            const int64_t scale_at = static_cast<int64_t>(min(kSwap ? q_col : p_row, p.rows - 1)) * p.scale_row;
+            const float *a_scales = kSwap ? nullptr : p.a_scales + static_cast<int64_t>(min(p_row0 + lane, p.rows - 1)) * p.scale_row;
             const int w_block = (kSwap ? pt : q_col / kFp8Block);
             // beyond the last output there is no scale; the sums there are not stored
             const float *w_scales = p.w_scales + static_cast<int64_t>(min(w_block, (p.outputs - 1) / kFp8Block)) * p.blocks;
@@ -462,24 +511,17 @@ ptq_fp8_matmul_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_cons
 #pragma unroll
             for (int c = 0; c < kCols; ++c) acc[c] = 0.0f;
             bool got = true;
-            float sw = __ldg(w_scales + kb0), sa = kSwap ? 0.0f : p.a_scales[scale_at + kb0 * p.scale_block];
-            for (int kb = kb0; kb < kb1; ++kb) {
-                const float row_factor = sw * sa;
-                const float sw_now = sw;
-                float col_factor[kSwap ? kCols : 1];
-                if constexpr (kSwap) {
+            // Scales on their way: the next k-block's of the weights, the next three's of the activations, which come from L2.
+            float sw = __ldg(w_scales + kb0), sa[3];
 #pragma unroll
-                    for (int c = 0; c < kCols; ++c) {
-                        if constexpr (kFused)
-                            col_factor[c] = scales_s[(kb - kb0) * BN + half * kCols + c];
-                        else
-                            col_factor[c] = p.a_scales[static_cast<int64_t>(min(q_col + c, p.rows - 1)) * p.scale_row + kb * p.scale_block];
-                    }
-                }
-                if (kb + 1 < kb1) {
-                    sw = __ldg(w_scales + kb + 1);
-                    if (!kSwap) sa = p.a_scales[scale_at + (kb + 1) * p.scale_block];
-                }
+            for (int i = 0; i < 3; ++i) sa[i] = !kSwap && kb0 + i < kb1 ? a_scales[(kb0 + i) * p.scale_block] : 0.0f;
+            for (int kb = kb0; kb < kb1; ++kb) {
+                const float factor = kSwap ? sw : sw * sa[0];
+                sa[0] = sa[1];
+                sa[1] = sa[2];
+                if (!kSwap && kb + 3 < kb1) sa[2] = a_scales[(kb + 3) * p.scale_block];
+                if (kb + 1 < kb1) sw = __ldg(w_scales + kb + 1);
+                const float *col_scales = scales_s + (kb - kb0) * BN + half * kCols;
                 if (!mbar_wait_warp(tfull_bar(buf), bphase, abort_flag, p.status)) {
                     got = false;
                     break;
@@ -489,19 +531,15 @@ ptq_fp8_matmul_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_cons
                 for (int c0 = 0; c0 < kCols; c0 += kLd) {
                     uint32_t v[kLd];
                     tmem_ld_cols<kLd>(tmem_row + buf * BN + c0, v);
-                    tmem_ld_wait();
+                    tmem_ld_wait_for(v);
                     if (c0 + kLd == kCols) {                           // all read: the MMAs may have the buffer
                         tc_fence_before_sync();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(tempty_bar(buf));
                     }
 #pragma unroll
-                    for (int c = 0; c < kLd; c += 2) {
-                        if constexpr (kSwap)
-                            fma2(acc[c0 + c], acc[c0 + c + 1], col_factor[c0 + c] * sw_now, col_factor[c0 + c + 1] * sw_now, v[c], v[c + 1]);
-                        else
-                            fma2(acc[c0 + c], acc[c0 + c + 1], row_factor, row_factor, v[c], v[c + 1]);
-                    }
+                    for (int c = 0; c < kLd; ++c)
+                        acc[c0 + c] = fmaf(kSwap ? factor * col_scales[c0 + c] : factor, __uint_as_float(v[c]), acc[c0 + c]);
                 }
                 buf ^= 1u;
                 if (buf == 0u) bphase ^= 1u;
@@ -523,37 +561,53 @@ ptq_fp8_matmul_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_cons
                 if (!got) break;
                 // through this warp's staging, 128 bytes of each of its 32 rows at a time, so that whole sectors are written
                 constexpr int kStep = 128 / sizeof(Y), kUnit = 16 / sizeof(Y);
-                uint8_t *stage = smem_raw + at.staging + (warp - 2) * kFp8Staging;
+                uint8_t *stage = smem_raw + at.staging + (warp - 4) * kFp8Staging;
                 Y *y = static_cast<Y *>(p.y);
-                const int row0 = pt * 128 + quarter * 32;
+                const int row0 = p_row0;
+                if (p.bias) {
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) acc[c] += __ldg(p.bias + min(q_col + c, p.outputs - 1));
+                }
 #pragma unroll
                 for (int c0 = 0; c0 < kCols; c0 += kStep) {
                     if (q_col + c0 >= p.outputs || row0 >= p.rows) continue;               // the same for the whole warp
                     __syncwarp();
 #pragma unroll
                     for (int u = 0; u < 8; ++u) {
-                        __align__(16) Y out[kUnit];
-#pragma unroll
-                        for (int i = 0; i < kUnit; ++i) {
-                            const int c = c0 + u * kUnit + i;
-                            float v = acc[c];
-                            if (p.bias && q_col + c < p.outputs) v += __ldg(p.bias + q_col + c);
-                            out[i] = from_f32<Y>(v);
+                        uint4 out;
+                        if constexpr (sizeof(Y) == 4) {
+                            const float *f = acc + c0 + 4 * u;
+                            out = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+                        } else {
+                            const float *f = acc + c0 + 8 * u;
+                            out = make_uint4(pack2<Y>(f[0], f[1]), pack2<Y>(f[2], f[3]), pack2<Y>(f[4], f[5]), pack2<Y>(f[6], f[7]));
                         }
-                        *reinterpret_cast<uint4 *>(stage + lane * 128 + ((u ^ (lane & 7)) << 4)) = *reinterpret_cast<const uint4 *>(out);
+                        *reinterpret_cast<uint4 *>(stage + lane * 128 + ((u ^ (lane & 7)) << 4)) = out;
                     }
                     __syncwarp();
-                    const int u = lane & 7;
+                    if (p.whole) {
+                        const int u = lane & 7, n = q_col + c0 + u * kUnit;
 #pragma unroll
-                    for (int r0 = 0; r0 < 32; r0 += 4) {
-                        const int r = r0 + (lane >> 3), n = q_col + c0 + u * kUnit;
-                        if (row0 + r >= p.rows) continue;
-                        const uint4 v = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((u ^ (r & 7)) << 4));
-                        Y *to = y + static_cast<int64_t>(row0 + r) * p.y_pitch + n;
-                        if (p.whole && n + kUnit <= p.outputs) {
-                            *reinterpret_cast<uint4 *>(to) = v;
-                        } else {
-                            for (int i = 0; i < kUnit && n + i < p.outputs; ++i) to[i] = reinterpret_cast<const Y *>(&v)[i];
+                        for (int r0 = 0; r0 < 32; r0 += 4) {
+                            const int r = r0 + (lane >> 3);
+                            if (row0 + r >= p.rows) continue;
+                            const uint4 v = *reinterpret_cast<const uint4 *>(stage + r * 128 + ((u ^ (r & 7)) << 4));
+                            Y *to = y + static_cast<int64_t>(row0 + r) * p.y_pitch + n;
+                            if (n + kUnit <= p.outputs) {
+                                *reinterpret_cast<uint4 *>(to) = v;
+                            } else {
+                                for (int i = 0; i < kUnit && n + i < p.outputs; ++i) to[i] = reinterpret_cast<const Y *>(&v)[i];
+                            }
+                        }
+                    } else {                                           // row by row, neighbouring lanes neighbouring columns
+                        for (int r = 0; r < 32 && row0 + r < p.rows; ++r) {
+#pragma unroll
+                            for (int c = lane; c < kStep; c += 32) {
+                                const int n = q_col + c0 + c;
+                                if (n < p.outputs)
+                                    y[static_cast<int64_t>(row0 + r) * p.y_pitch + n] =
+                                        reinterpret_cast<const Y *>(stage + r * 128 + (((c / kUnit) ^ (r & 7)) << 4))[c % kUnit];
+                            }
                         }
                     }
                 }
@@ -573,24 +627,54 @@ ptq_fp8_matmul_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_cons
         const int major0 = kMajor * rank / p.split, major1 = kMajor * (rank + 1) / p.split;
         const int m0 = kSwap ? qt * BN : pt * 128, n0 = kSwap ? pt * 128 : qt * BN;
         Y *y = static_cast<Y *>(p.y);
-        for (int i = major0 * kMinor + static_cast<int>(threadIdx.x); i < major1 * kMinor; i += kFp8Threads) {
-            const int r = i / kMinor, c = i % kMinor, m = m0 + r, n = n0 + c;
-            if (m >= p.rows) break;
-            if (n >= p.outputs) continue;
-            float v = 0.0f;
-            const uint32_t from = base + 4u * static_cast<uint32_t>(r * kPitch + c);
-            if (p.split > 1) {
-                float part[8];
+        // four columns at a time, or one where rows of y begin anywhere
+        const auto sum = [&](auto wide) {
+            constexpr int kWide = decltype(wide)::value;
+            for (int i = major0 * (kMinor / kWide) + static_cast<int>(threadIdx.x); i < major1 * (kMinor / kWide); i += kFp8Threads) {
+                const int r = i / (kMinor / kWide), c = i % (kMinor / kWide) * kWide, m = m0 + r, n = n0 + c;
+                if (m >= p.rows) break;
+                if (n >= p.outputs) continue;
+                float v[kWide] = {};
+                const uint32_t from = base + 4u * static_cast<uint32_t>(r * kPitch + c);
+                if (p.split > 1) {
+                    float part[8][kWide];
 #pragma unroll
-                for (int q = 0; q < 8; ++q) part[q] = q < p.split ? ld_cluster_f32(from, q) : 0.0f;
+                    for (int q = 0; q < 8; ++q) {
 #pragma unroll
-                for (int q = 0; q < 8; ++q) v += part[q];
-            } else {
-                v = *reinterpret_cast<const float *>(smem_raw + (from - base));
+                        for (int j = 0; j < kWide; ++j) part[q][j] = 0.0f;
+                        if (q < p.split) ld_cluster(from, q, part[q]);
+                    }
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+#pragma unroll
+                        for (int j = 0; j < kWide; ++j) v[j] += part[q][j];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kWide; ++j) v[j] = reinterpret_cast<const float *>(smem_raw + (from - base))[j];
+                }
+                if (p.bias) {
+#pragma unroll
+                    for (int j = 0; j < kWide; ++j) v[j] += __ldg(p.bias + min(n + j, p.outputs - 1));
+                }
+                Y *to = y + static_cast<int64_t>(m) * p.y_pitch + n;
+                if constexpr (kWide == 4) {
+                    if (n + 4 <= p.outputs) {
+                        if constexpr (sizeof(Y) == 4)
+                            *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
+                        else
+                            *reinterpret_cast<uint2 *>(to) = make_uint2(pack2<Y>(v[0], v[1]), pack2<Y>(v[2], v[3]));
+                        continue;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kWide; ++j)
+                    if (n + j < p.outputs) to[j] = from_f32<Y>(v[j]);
             }
-            if (p.bias) v += __ldg(p.bias + n);
-            y[static_cast<int64_t>(m) * p.y_pitch + n] = from_f32<Y>(v);
-        }
+        };
+        if (p.whole)
+            sum(std::integral_constant<int, 4>());
+        else
+            sum(std::integral_constant<int, 1>());
         if (p.split > 1) cluster_sync_all();               // nobody leaves while its part is read
     }
     __syncthreads();

@@ -67,7 +67,7 @@ def fp8_matmul(a, a_scales, w, w_scales, bias=None, dtype=None, y=None, stream=N
 
 
 def fp8_linear(x, w, w_scales, bias=None, y=None, stream=None):
-    """``ptq_fp8_linear``: ``fp8_quantize`` and ``fp8_matmul`` in one call, y ``[..., N]`` of x's type; up to 64 rows in one kernel."""
+    """``ptq_fp8_linear``: ``fp8_quantize`` and ``fp8_matmul`` in one call, y ``[..., N]`` of x's type; up to 16 rows in one kernel."""
     return _call(_native().fp8_linear, stream, x, x, w, w_scales, bias, y)
 
 
