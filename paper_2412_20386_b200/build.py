@@ -20,13 +20,15 @@ from concurrent.futures import ThreadPoolExecutor
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _CSRC = os.path.join(_HERE, "csrc")
 _SO = os.path.join(_HERE, "libptq_linear.so")
-_SOURCES = ["ptq_api.cu", "ptq_block.cu", "ptq_scan_f16.cu", "ptq_scan_bf16.cu", "ptq_scan_f32.cu", "ptq_fp8.cu"]
+_SOURCES = ["ptq_api.cu", "ptq_block.cu", "ptq_scan_f16.cu", "ptq_scan_bf16.cu", "ptq_scan_f32.cu", "ptq_heads.cu", "ptq_heads_f16.cu",
+            "ptq_heads_bf16.cu", "ptq_heads_f32.cu", "ptq_fp8.cu"]
 _DEPS = ["ptq_api.cu", "ptq_gemm.cuh", "ptq_fused.cuh", "ptq_small.cuh", "ptq_short_k.cuh", "ptq_quantize.cuh", "ptq_quantize_dynamic.cuh",
          "ptq_calibrate.cuh", "ptq_probe.cuh", "ptx_sm100.cuh", "ptx_griddep.cuh", "ptq_host.h",
          "ptq_block.cu", "ptq_scan_f16.cu", "ptq_scan_bf16.cu", "ptq_scan_f32.cu", "ptq_block_host.h", "ptq_scan_launch.cuh",
          "ptq_block.cuh", "ptq_scan.cuh", "ptq_norm.cuh", "ptq_conv.cuh",
-         "ptq_fp8.cu", "ptq_fp8.cuh", "ptq_tensor_map.h",
-         *(os.path.join("..", "..", "include", h) for h in ("ptq_linear.h", "ptq_block.h", "ptq_fp8.h"))]
+         "ptq_heads.cu", "ptq_heads_f16.cu", "ptq_heads_bf16.cu", "ptq_heads_f32.cu", "ptq_heads_launch.cuh", "ptq_heads.cuh", "ptq_heads_backward.cuh",
+         "ptq_heads_finish.cuh", "ptq_fp8.cu", "ptq_fp8.cuh", "ptq_tensor_map.h",
+         *(os.path.join("..", "..", "include", h) for h in ("ptq_linear.h", "ptq_block.h", "ptq_heads.h", "ptq_fp8.h"))]
 
 
 def nvcc_path() -> str:
@@ -38,8 +40,8 @@ def nvcc_path() -> str:
 
 _EXT = os.path.join(_HERE, "_ptq_torch.so")
 _EXT_STAMP = os.path.join(_HERE, "_build", "_ptq_torch.versions")     # what the extension was compiled against
-_EXT_SOURCES = ["ptq_torch.cpp", "ptq_torch_block.cpp", "ptq_torch_fp8.cpp"]
-_EXT_DEPS = _EXT_SOURCES + ["ptq_torch.h", "ptq_torch_tensors.h", *(os.path.join("..", "..", "include", h) for h in ("ptq_linear.h", "ptq_block.h", "ptq_fp8.h"))]
+_EXT_SOURCES = ["ptq_torch.cpp", "ptq_torch_block.cpp", "ptq_torch_heads.cpp", "ptq_torch_fp8.cpp"]
+_EXT_DEPS = _EXT_SOURCES + ["ptq_torch.h", "ptq_torch_tensors.h", *(os.path.join("..", "..", "include", h) for h in ("ptq_linear.h", "ptq_block.h", "ptq_heads.h", "ptq_fp8.h"))]
 
 
 def up_to_date(target: str = _SO, deps=_DEPS) -> bool:

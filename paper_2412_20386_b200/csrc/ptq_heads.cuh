@@ -1,0 +1,887 @@
+// Linear attention with a decay for each head (include/ptq_heads.h): what its kernels share, and the forward pass.
+//
+// A chunk of 64 steps is taken as matrix products.  With L_i the sum of dt A over the chunk's steps up to i, w_j the factor of
+// an input (dt or 1) and S the state in front of the chunk:
+//     y_i = sum_{j <= i} e^{L_i - L_j} w_j (C_i . B_j) u_j  +  e^{L_i} S C_i  (+ D u_i)
+//     S  <- e^{L_64} S + sum_j e^{L_64 - L_j} w_j u_j B_j^T
+// A CTA walks over the chunks of a sequence for 64 columns of a head; four warps have 16 steps of each chunk (scores and outputs)
+// and 16 columns of the state, which stays in registers in binary32 from chunk to chunk.
+//
+// The products are mma.sync on 16-bit operands: per chunk they are 64 x 64 x (16 .. 128), the scores go from one product's
+// accumulators through exponentials into the next one's operand and the state's update needs its operand in two halves (the
+// state is binary32), which all happens in the registers of a warp without a barrier; tcgen05 would move each of these
+// matrices through TMEM and shared memory with a hand-over between warps each time.  binary32 activations: the same with tf32
+// operands in two parts, three products for one.
+//
+// e^{L_i - L_j} is formed without a quotient of large numbers: the sums L are binary64, a warp's 16 steps refer to the sum in front
+// of them, so that each factor of an earlier step is one exponential per column of scores and one per row, and only the 16 x 16
+// block on the diagonal needs one per element.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "ptx_griddep.cuh"
+
+namespace ptq {
+
+constexpr int kHeadSteps = 64;        // of a chunk
+constexpr int kHeadCols = 64;         // columns of a head that a CTA has
+constexpr unsigned kHeadsSoftplus = 1u, kHeadsReverse = 2u, kHeadsUnscaled = 4u;
+constexpr double kLog2e = 1.4426950408889634074;
+
+struct HeadParams {
+    const void *u, *delta, *B, *C, *dy;
+    int64_t u_b, u_l, u_h, delta_b, delta_l, delta_h, B_b, B_l, B_g, C_b, C_l, C_g;
+    const float *A, *D, *delta_bias, *state;
+    const int32_t *lengths;
+    void *y;
+    float *final_state, *history;
+    float *slots, *logs;              // of the segments: states [batch, heads, segments, cols, states], log2 of their decays [batch, heads, segments]
+    int batch, length, heads, cols, states, groups, group_heads;
+    int col_tiles, segments, segment_chunks, chunks;
+    int unit, out_unit;               // bytes that rows of the inputs, of y can be moved at a time
+    unsigned flags;
+    // backward pass
+    const float *kept, *dfinal;
+    void *du;
+    float *part_B, *part_C;           // [col_tiles, heads, batch, length, states]
+    float2 *part_dt;                  // [col_tiles, heads, batch, length]: gradients of the log decay and of w
+    float *part_D;                    // [col_tiles, segments, batch, heads]
+};
+
+// ---------------------------------------------------------------------------------------------------- fragments
+// Operands of one 16 x 8 x 16 product as the lanes of a warp hold them (g = lane / 4, t = lane % 4): of the 16 x 16 operand rows g and
+// g + 8, columns 2t, 2t + 1, 2t + 8, 2t + 9; of the 16 x 8 one the same rows of its column g.  binary32: two products of 8.
+template <typename T>
+struct HeadA { uint32_t r[4]; };
+template <>
+struct HeadA<float> { float v[8]; };
+template <typename T>
+struct HeadB { uint32_t r[2]; };
+template <>
+struct HeadB<float> { float v[4]; };
+
+constexpr int kHeadPad = 8;           // elements between the rows of a tile in shared memory, against bank conflicts
+
+__device__ __forceinline__ uint32_t head_smem(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], const void *p)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(head_smem(p)) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], const void *p)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(head_smem(p)) : "memory");
+}
+
+// The 16 x 16 operand at rows m0, columns k0 of a tile [m][k].
+template <typename T>
+__device__ __forceinline__ HeadA<T> load_a(const T *tile, int pitch, int m0, int k0, int lane)
+{
+    HeadA<T> a;
+    if constexpr (sizeof(T) == 2) {
+        ldsm4(a.r, tile + (m0 + (lane & 15)) * pitch + k0 + (lane >> 4) * 8);
+    } else {
+        const T *p = tile + (m0 + (lane >> 2)) * pitch + k0 + 2 * (lane & 3);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 v = *reinterpret_cast<const float2 *>(p + (i & 1) * 8 * pitch + (i >> 1) * 8);
+            a.v[2 * i] = v.x;
+            a.v[2 * i + 1] = v.y;
+        }
+    }
+    return a;
+}
+// The same from a tile [k][m].
+template <typename T>
+__device__ __forceinline__ HeadA<T> load_a_t(const T *tile, int pitch, int m0, int k0, int lane)
+{
+    HeadA<T> a;
+    if constexpr (sizeof(T) == 2) {
+        ldsm4t(a.r, tile + (k0 + (lane >> 4) * 8 + (lane & 7)) * pitch + m0 + ((lane >> 3) & 1) * 8);
+    } else {
+        const T *p = tile + (k0 + 2 * (lane & 3)) * pitch + m0 + (lane >> 2);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a.v[i] = p[((i & 1) + (i >> 2) * 8) * pitch + ((i >> 1) & 1) * 8];
+    }
+    return a;
+}
+// Two 16 x 8 operands, columns n0 .. n0 + 15, rows k0 .. k0 + 15, of a tile [n][k].
+template <typename T>
+__device__ __forceinline__ void load_b(HeadB<T> (&b)[2], const T *tile, int pitch, int n0, int k0, int lane)
+{
+    if constexpr (sizeof(T) == 2) {
+        uint32_t r[4];
+        ldsm4(r, tile + (n0 + (lane >> 4) * 8 + (lane & 7)) * pitch + k0 + ((lane >> 3) & 1) * 8);
+        b[0].r[0] = r[0], b[0].r[1] = r[1], b[1].r[0] = r[2], b[1].r[1] = r[3];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const T *p = tile + (n0 + 8 * j + (lane >> 2)) * pitch + k0 + 2 * (lane & 3);
+            const float2 lo = *reinterpret_cast<const float2 *>(p), hi = *reinterpret_cast<const float2 *>(p + 8);
+            b[j].v[0] = lo.x, b[j].v[1] = lo.y, b[j].v[2] = hi.x, b[j].v[3] = hi.y;
+        }
+    }
+}
+// The same from a tile [k][n].
+template <typename T>
+__device__ __forceinline__ void load_b_t(HeadB<T> (&b)[2], const T *tile, int pitch, int n0, int k0, int lane)
+{
+    if constexpr (sizeof(T) == 2) {
+        uint32_t r[4];
+        ldsm4t(r, tile + (k0 + ((lane >> 3) & 1) * 8 + (lane & 7)) * pitch + n0 + (lane >> 4) * 8);
+        b[0].r[0] = r[0], b[0].r[1] = r[1], b[1].r[0] = r[2], b[1].r[1] = r[3];
+    } else {
+        const T *p = tile + (k0 + 2 * (lane & 3)) * pitch + n0 + (lane >> 2);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) b[j].v[i] = p[((i & 1) + (i >> 1) * 8) * pitch + 8 * j];
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t head_pack(float lo, float hi)
+{
+    if constexpr (std::is_same<T, __half>::value) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    } else {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+}
+template <typename T>
+__device__ __forceinline__ float2 head_unpack(uint32_t v)
+{
+    if constexpr (std::is_same<T, __half>::value)
+        return __half22float2(*reinterpret_cast<const __half2 *>(&v));
+    else
+        return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&v));
+}
+__device__ __forceinline__ float head_f32(float v) { return v; }
+__device__ __forceinline__ float head_f32(__half v) { return __half2float(v); }
+__device__ __forceinline__ float head_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T>
+__device__ __forceinline__ T head_round(float v)
+{
+    if constexpr (std::is_same<T, __half>::value)
+        return __float2half_rn(v);
+    else if constexpr (std::is_same<T, __nv_bfloat16>::value)
+        return __float2bfloat16_rn(v);
+    else
+        return v;
+}
+// Two neighbouring elements.
+template <typename T>
+__device__ __forceinline__ float2 head_pair(const T *p)
+{
+    if constexpr (sizeof(T) == 2)
+        return head_unpack<T>(*reinterpret_cast<const uint32_t *>(p));
+    else
+        return *reinterpret_cast<const float2 *>(p);
+}
+template <typename T>
+__device__ __forceinline__ void head_store_pair(T *p, float x, float y)
+{
+    if constexpr (sizeof(T) == 2)
+        *reinterpret_cast<uint32_t *>(p) = head_pack<T>(x, y);
+    else
+        *reinterpret_cast<float2 *>(p) = make_float2(x, y);
+}
+
+// Operand from the accumulators of two 8-column tiles, times `scale`.
+template <typename T>
+__device__ __forceinline__ HeadA<T> acc_to_a(const float (&lo)[4], const float (&hi)[4], float scale)
+{
+    HeadA<T> a;
+    if constexpr (sizeof(T) == 2) {
+        a.r[0] = head_pack<T>(lo[0] * scale, lo[1] * scale);
+        a.r[1] = head_pack<T>(lo[2] * scale, lo[3] * scale);
+        a.r[2] = head_pack<T>(hi[0] * scale, hi[1] * scale);
+        a.r[3] = head_pack<T>(hi[2] * scale, hi[3] * scale);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            a.v[i] = lo[i];
+            a.v[4 + i] = hi[i];
+        }
+    }
+    return a;
+}
+
+__device__ __forceinline__ uint32_t to_tf32(float v)
+{
+    uint32_t r;
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ void mma_tf32(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// d += a b.  binary32: both operands as two tf32 parts (22 bits), the product of the two lower parts left out (2^-22 of the terms).
+template <typename T>
+__device__ __forceinline__ void head_mma(float (&d)[4], const HeadA<T> &a, const HeadB<T> &b)
+{
+    if constexpr (std::is_same<T, __half>::value) {
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a.r[0]), "r"(a.r[1]), "r"(a.r[2]), "r"(a.r[3]), "r"(b.r[0]), "r"(b.r[1]));
+    } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a.r[0]), "r"(a.r[1]), "r"(a.r[2]), "r"(a.r[3]), "r"(b.r[0]), "r"(b.r[1]));
+    } else {
+        uint32_t ah[8], al[8], bh[4], bl[4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            ah[i] = to_tf32(a.v[i]);
+            al[i] = to_tf32(a.v[i] - __uint_as_float(ah[i]));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            bh[i] = to_tf32(b.v[i]);
+            bl[i] = to_tf32(b.v[i] - __uint_as_float(bh[i]));
+        }
+        // the order of the inner index is the same on both sides: element 2t in place t, 2t + 1 in place t + 4
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            mma_tf32(d, al[4 * k], al[4 * k + 2], al[4 * k + 1], al[4 * k + 3], bh[2 * k], bh[2 * k + 1]);
+            mma_tf32(d, ah[4 * k], ah[4 * k + 2], ah[4 * k + 1], ah[4 * k + 3], bl[2 * k], bl[2 * k + 1]);
+            mma_tf32(d, ah[4 * k], ah[4 * k + 2], ah[4 * k + 1], ah[4 * k + 3], bh[2 * k], bh[2 * k + 1]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------- powers of two for binary16
+// An operand that is formed here may leave binary16's range; its rows are scaled by a power of two that brings their largest
+// magnitude to about 2^13.  (bfloat16 has binary32's range.)
+template <typename T>
+constexpr bool kScaled = std::is_same<T, __half>::value;
+
+__device__ __forceinline__ float finite_abs(float v)
+{
+    const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
+    return b < 0x7f800000u ? __uint_as_float(b) : 0.0f;
+}
+__device__ __forceinline__ float warp_max(float v)
+{
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+}
+// The power of two, within 2^-60 .. 2^60, and its inverse.
+struct HeadScale {
+    float up, down;
+};
+__device__ __forceinline__ HeadScale scale_for(float top)
+{
+    int e = 13 + 127 - static_cast<int>(__float_as_uint(top) >> 23);           // top = 2^(its exponent - 127) (1 ..)
+    e = top == 0.0f ? 0 : max(-60, min(60, e));
+    return {__uint_as_float(static_cast<uint32_t>(127 + e) << 23), __uint_as_float(static_cast<uint32_t>(127 - e) << 23)};
+}
+
+// ---------------------------------------------------------------------------------------------------- loads
+__device__ __forceinline__ void cp_async(uint32_t dst, const void *src, int bytes, bool on)
+{
+    const int n = on ? bytes : 0;                        // what is not copied is filled with zeros
+    if (bytes == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+    else if (bytes == 8)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// 64 rows of kWidth elements into a tile: row r from src + r * step, zeros from `rows` and from column `cols` on.  Moved in units that
+// divide the rows; 2-byte ones go through registers.
+template <int kWidth, int kThreads, typename T>
+__device__ __forceinline__ void load_rows(T *tile, const T *src, int64_t step, int rows, int cols, int unit)
+{
+    constexpr int kPitch = kWidth + kHeadPad;
+    const auto go = [&](auto bytes) {
+        constexpr int kBytes = decltype(bytes)::value, kElems = kBytes / static_cast<int>(sizeof(T)), kRow = kWidth / kElems;
+        for (int i = threadIdx.x; i < kHeadSteps * kRow; i += kThreads) {
+            const int r = i / kRow, c = i % kRow * kElems;
+            const bool on = r < rows && c < cols;
+            cp_async(head_smem(tile + r * kPitch + c), on ? src + r * step + c : src, kBytes, on);
+        }
+    };
+    if (unit == 16) {
+        go(std::integral_constant<int, 16>());
+    } else if (unit == 8) {
+        go(std::integral_constant<int, 8>());
+    } else if (unit == 4) {
+        go(std::integral_constant<int, 4>());
+    } else if constexpr (sizeof(T) == 2) {
+        for (int i = threadIdx.x; i < kHeadSteps * kWidth; i += kThreads) {
+            const int r = i / kWidth, c = i % kWidth;
+            tile[r * kPitch + c] = r < rows && c < cols ? src[r * step + c] : head_round<T>(0.0f);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------- steps of a chunk
+// A lane has steps `lane` and `lane + 32` of a chunk.
+struct HeadSteps {
+    float dt[2], w[2];
+    double sum[2];                    // log2 of the decays up to and with the step
+};
+__device__ __forceinline__ float head_softplus(float e) { return e > 20.0f ? e : log1pf(expf(e)); }
+__device__ __forceinline__ float head_dt(const HeadParams &p, float delta, float bias)
+{
+    if (!p.delta) return 1.0f;
+    const float e = delta + bias;
+    return p.flags & kHeadsSoftplus ? head_softplus(e) : e;
+}
+// delta of the two steps of a lane; n: steps of the sequence
+template <typename T>
+__device__ __forceinline__ void load_delta(const HeadParams &p, int64_t at, int first, int n, int lane, float (&v)[2])
+{
+    const T *d = static_cast<const T *>(p.delta);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int i = first + lane + 32 * k;
+        v[k] = d && i < n ? head_f32(d[at + (p.flags & kHeadsReverse ? n - 1 - i : i) * p.delta_l]) : 0.0f;
+    }
+}
+// A2 = A log2 e.  Below 2^-4000 a step's decay counts as that (zero in binary32 either way), so that -inf does no harm in differences.
+__device__ __forceinline__ HeadSteps head_steps(const HeadParams &p, const float (&delta)[2], float bias, double A2, int first, int n, int lane)
+{
+    HeadSteps s;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const bool on = first + lane + 32 * k < n;
+        s.dt[k] = on ? head_dt(p, delta[k], bias) : 0.0f;
+        s.w[k] = !on ? 0.0f : p.flags & kHeadsUnscaled ? 1.0f : s.dt[k];
+        double a = s.dt[k] == 0.0f ? 0.0 : static_cast<double>(s.dt[k]) * A2;
+        if (a < -4000.0) a = -4000.0;
+        s.sum[k] = a;
+    }
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const double x = __shfl_up_sync(0xffffffffu, s.sum[0], d), y = __shfl_up_sync(0xffffffffu, s.sum[1], d);
+        if (lane >= d) {
+            s.sum[0] += x;
+            s.sum[1] += y;
+        }
+    }
+    s.sum[1] += __shfl_sync(0xffffffffu, s.sum[0], 31);
+    return s;
+}
+__device__ __forceinline__ double sum_at(const HeadSteps &s, int step)
+{
+    return __shfl_sync(0xffffffffu, step < 32 ? s.sum[0] : s.sum[1], step & 31);
+}
+__device__ __forceinline__ float pow2(double x) { return exp2f(static_cast<float>(x)); }
+
+// What a CTA works on.
+struct HeadPlace {
+    int b, h, g, tile, seg, n;        // n: steps of the sequence
+    int cols;                         // of this tile
+};
+__device__ __forceinline__ HeadPlace head_place(const HeadParams &p, int segments)
+{
+    HeadPlace a;
+    int i = static_cast<int>(blockIdx.x);
+    a.seg = i % segments;
+    i /= segments;
+    a.tile = i % p.col_tiles;
+    i /= p.col_tiles;
+    a.h = i % p.heads;
+    a.b = i / p.heads;
+    a.g = a.h / p.group_heads;
+    a.n = p.lengths ? max(0, min(p.length, __ldg(p.lengths + a.b))) : p.length;
+    a.cols = min(kHeadCols, p.cols - a.tile * kHeadCols);
+    return a;
+}
+
+// state[p][n] <- decay state + sum_j f_j x_j[p] z_j[n] over a chunk, for 16 columns p0 ..; x and z are tiles [step][..].  The factors make
+// x an operand of more than 16 bits: it goes in as two.
+template <int NP, typename T>
+__device__ __forceinline__ void state_update(float (&S)[NP / 8][4], const T *x, const T *z, const float *f, float decay, int p0, int lane)
+{
+    constexpr int kXP = kHeadCols + kHeadPad, kZP = NP + kHeadPad;
+    const int t = lane & 3;
+    HeadA<T> a[kHeadSteps / 16];
+#pragma unroll
+    for (int k = 0; k < kHeadSteps / 16; ++k) a[k] = load_a_t(x, kXP, p0, 16 * k, lane);
+    HeadScale sc = {1.0f, 1.0f};
+    if constexpr (kScaled<T>) {
+        float top = 0.0f, ftop = fmaxf(finite_abs(f[lane]), finite_abs(f[lane + 32]));
+#pragma unroll
+        for (int k = 0; k < kHeadSteps / 16; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 v = head_unpack<T>(a[k].r[i]);
+                top = fmaxf(top, fmaxf(finite_abs(v.x), finite_abs(v.y)));
+            }
+        sc = scale_for(warp_max(top) * warp_max(ftop));
+    }
+    const float before = decay * sc.up;
+#pragma unroll
+    for (int n = 0; n < NP / 8; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) S[n][i] *= before;
+#pragma unroll
+    for (int k = 0; k < kHeadSteps / 16; ++k) {
+        const float2 f0 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t), f1 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t + 8);
+        HeadA<T> hi, lo;
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 v = head_unpack<T>(a[k].r[i]), q = i < 2 ? f0 : f1;
+                const float vx = v.x * (q.x * sc.up), vy = v.y * (q.y * sc.up);
+                hi.r[i] = head_pack<T>(vx, vy);
+                const float2 r = head_unpack<T>(hi.r[i]);
+                lo.r[i] = head_pack<T>(vx - r.x, vy - r.y);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) hi.v[i] = a[k].v[i] * (i < 4 ? (i & 1 ? f0.y : f0.x) : (i & 1 ? f1.y : f1.x));
+        }
+#pragma unroll
+        for (int n = 0; n < NP / 16; ++n) {
+            HeadB<T> b[2];
+            load_b_t(b, z, kZP, 16 * n, 16 * k, lane);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if constexpr (sizeof(T) == 2) head_mma(S[2 * n + j], lo, b[j]);
+                head_mma(S[2 * n + j], hi, b[j]);
+            }
+        }
+    }
+    if constexpr (kScaled<T>) {
+#pragma unroll
+        for (int n = 0; n < NP / 8; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) S[n][i] *= sc.down;
+    }
+}
+
+// A warp's 16 columns of a state in memory [cols][states]: rows p0 + g and p0 + g + 8, columns 8 n + 2 t of it.
+template <int NP, class Fn>
+__device__ __forceinline__ void for_state(int p0, int cols, int states, int lane, Fn fn)
+{
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < NP / 8; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int p = p0 + g + (i >> 1) * 8, c = 8 * n + 2 * t + (i & 1);
+            fn(n, i, p < cols && c < states, static_cast<int64_t>(p) * states + c);
+        }
+}
+template <int NP>
+__device__ __forceinline__ void read_state(float (&S)[NP / 8][4], const float *from, int p0, int cols, int states, int lane)
+{
+    if (states % 2 == 0 && (reinterpret_cast<uintptr_t>(from) & 7) == 0) {
+        const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int n = 0; n < NP / 8; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int p = p0 + g + 8 * i, c = 8 * n + 2 * t;
+                float2 v = make_float2(0.0f, 0.0f);
+                if (from && p < cols && c < states) v = *reinterpret_cast<const float2 *>(from + static_cast<int64_t>(p) * states + c);
+                S[n][2 * i] = v.x;
+                S[n][2 * i + 1] = v.y;
+            }
+    } else {
+        for_state<NP>(p0, cols, states, lane, [&](int n, int i, bool on, int64_t at) { S[n][i] = on && from ? from[at] : 0.0f; });
+    }
+}
+template <int NP>
+__device__ __forceinline__ void write_state(const float (&S)[NP / 8][4], float *to, int p0, int cols, int states, int lane)
+{
+    if (states % 2 == 0 && (reinterpret_cast<uintptr_t>(to) & 7) == 0) {
+        const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int n = 0; n < NP / 8; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int p = p0 + g + 8 * i, c = 8 * n + 2 * t;
+                if (p < cols && c < states) *reinterpret_cast<float2 *>(to + static_cast<int64_t>(p) * states + c) = make_float2(S[n][2 * i], S[n][2 * i + 1]);
+            }
+    } else {
+        for_state<NP>(p0, cols, states, lane, [&](int n, int i, bool on, int64_t at) {
+            if (on) to[at] = S[n][i];
+        });
+    }
+}
+
+// A warp's 16 x 64 results from its staging (rows of kHeadCols + 8 elements) to rows of a tensor; token(r): the row's place, or -1.
+template <typename T, class Fn>
+__device__ __forceinline__ void store_rows(const T *stage, T *to, int64_t row_pitch, int cols, int unit, int lane, Fn token)
+{
+    constexpr int kPitch = kHeadCols + kHeadPad;
+    if (unit == 16) {
+        constexpr int kElems = 16 / static_cast<int>(sizeof(T)), kRow = kHeadCols / kElems;
+        for (int i = lane; i < 16 * kRow; i += 32) {
+            const int r = i / kRow, c = i % kRow * kElems;
+            const int64_t at = token(r);
+            if (at >= 0 && c < cols) *reinterpret_cast<uint4 *>(to + at * row_pitch + c) = *reinterpret_cast<const uint4 *>(stage + r * kPitch + c);
+        }
+    } else {
+        for (int r = 0; r < 16; ++r) {
+            const int64_t at = token(r);
+            if (at < 0) continue;
+            for (int c = lane; c < cols; c += 32) to[at * row_pitch + c] = stage[r * kPitch + c];
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------- forward pass
+enum HeadMode {
+    kHeadForward,                     // outputs and final states
+    kHeadSum,                         // what a segment adds to the state, and its decay
+    kHeadGradSum,                     // what a segment's outputs add to the gradient of the state in front of it, and its decay
+};
+
+// Shared memory of the forward kernel, in bytes: two stages of tiles (C, B, u; sums: one of B and C, and u or dy), the state as an
+// operand, staging of the outputs, factors of the steps for each warp, powers of two of the state's columns.
+template <typename T, int NP, int kMode>
+struct HeadSmem {
+    static constexpr int kWide = kHeadSteps * (NP + kHeadPad) * static_cast<int>(sizeof(T));
+    static constexpr int kNarrow = kHeadSteps * (kHeadCols + kHeadPad) * static_cast<int>(sizeof(T));
+    static constexpr int kStage = (kMode == kHeadForward ? 2 : 1) * kWide + kNarrow;
+    static constexpr int kStages = 2 * kStage + (kMode == kHeadForward ? kWide + kNarrow : 0) <= 200 * 1024 ? 2 : 1;
+    // a warp's rows of C are its own: its outputs go over them where they fit
+    static constexpr bool kOverC = NP >= kHeadCols;
+    static constexpr int kState = kStages * kStage;
+    static constexpr int kStaging = kState + (kMode == kHeadForward ? kWide : 0);
+    static constexpr int kFactors = kStaging + (kMode == kHeadForward && !kOverC ? kNarrow : 0);
+    static constexpr int kPowers = kFactors + 4 * 4 * kHeadSteps * 4;
+    static constexpr int kBytes = kPowers + 16;
+};
+
+template <typename T, int NP, int kMode>
+__global__ void __launch_bounds__(128) ptq_heads_kernel(const HeadParams p)
+{
+    using M = HeadSmem<T, NP, kMode>;
+    constexpr int kWP = NP + kHeadPad, kXP = kHeadCols + kHeadPad;
+    constexpr bool kOut = kMode == kHeadForward, kGrad = kMode == kHeadGradSum;
+    extern __shared__ __align__(128) unsigned char smem[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    if (kOut && p.segments > 1) griddep_wait();
+    const HeadPlace a = head_place(p, kOut ? p.segments : p.segments - 1);
+    const int seg = kGrad ? a.seg + 1 : a.seg;            // sums: of all segments but the last, of gradients: but the first
+    const int chunks = (a.n + kHeadSteps - 1) / kHeadSteps;
+    const int chunk0 = min(chunks, seg * p.segment_chunks), chunk1 = min(chunks, chunk0 + p.segment_chunks);
+    const bool reverse = p.flags & kHeadsReverse;
+    const int p0 = 16 * warp;                             // this warp's columns of the state, and its steps of a chunk
+    const auto tile_u = [&](int s) { return reinterpret_cast<T *>(smem + (M::kStages == 2 ? s * M::kStage : 0)); };
+    const auto tile_B = [&](int s) { return reinterpret_cast<T *>(smem + (M::kStages == 2 ? s * M::kStage : 0) + M::kNarrow); };
+    const auto tile_C = [&](int s) { return reinterpret_cast<T *>(smem + (M::kStages == 2 ? s * M::kStage : 0) + M::kNarrow + M::kWide); };
+    T *state_s = reinterpret_cast<T *>(smem + M::kState);
+    float *factors = reinterpret_cast<float *>(smem + M::kFactors) + warp * 4 * kHeadSteps;
+    float *vF = factors, *vC = factors + kHeadSteps, *vW = factors + 2 * kHeadSteps, *vR = factors + 3 * kHeadSteps;
+    float *powers = reinterpret_cast<float *>(smem + M::kPowers);
+
+    const T *u = static_cast<const T *>(kGrad ? p.dy : p.u) +
+                 (kGrad ? (static_cast<int64_t>(a.b) * p.length * p.heads + a.h) * p.cols : a.b * p.u_b + a.h * p.u_h) + a.tile * kHeadCols;
+    const int64_t u_l = kGrad ? static_cast<int64_t>(p.heads) * p.cols : p.u_l;
+    const T *B = static_cast<const T *>(kGrad ? p.C : p.B) + (kGrad ? a.b * p.C_b + a.g * p.C_g : a.b * p.B_b + a.g * p.B_g);
+    const int64_t B_l = kGrad ? p.C_l : p.B_l;
+    const T *C = static_cast<const T *>(p.C) + a.b * p.C_b + a.g * p.C_g;
+    const int64_t delta_at = a.b * p.delta_b + a.h * p.delta_h;
+    const float bias = p.delta_bias ? __ldg(p.delta_bias + a.h) : 0.0f, skip = p.D ? __ldg(p.D + a.h) : 0.0f;
+    const double A2 = static_cast<double>(__ldg(p.A + a.h)) * kLog2e;
+
+    const auto token = [&](int step) { return reverse ? a.n - 1 - step : step; };
+    const auto load = [&](int chunk, int s) {
+        const int first = chunk * kHeadSteps, rows = a.n - first;
+        const int64_t sign = reverse ? -1 : 1, at = token(first);
+        load_rows<kHeadCols, 128>(tile_u(s), u + at * u_l, sign * u_l, rows, a.cols, p.unit);
+        load_rows<NP, 128>(tile_B(s), B + at * B_l, sign * B_l, rows, p.states, p.unit);
+        if (kOut) load_rows<NP, 128>(tile_C(s), C + at * p.C_l, sign * p.C_l, rows, p.states, p.unit);
+        cp_async_commit();
+    };
+
+    const int64_t head_at = (static_cast<int64_t>(a.b) * p.heads + a.h);
+    const int64_t state_size = static_cast<int64_t>(p.cols) * p.states, tile_at = static_cast<int64_t>(a.tile) * kHeadCols * p.states;
+    float S[NP / 8][4];
+    {
+        const float *from = nullptr;
+        // with segments the first one's start is a copy: the last one may be writing final_state over it
+        if (kOut && p.segments > 1 && (seg > 0 || p.state))
+            from = p.slots + (head_at * p.segments + (seg > 0 ? seg : p.segments) - 1) * state_size + tile_at;
+        else if (kOut && p.state)
+            from = p.state + head_at * state_size + tile_at;
+        read_state<NP>(S, from, p0, a.cols, p.states, lane);
+    }
+    double log_decay = 0.0;
+    const int count = chunk1 - chunk0;
+    const auto chunk_of = [&](int i) { return kGrad ? chunk1 - 1 - i : chunk0 + i; };
+    float delta[2] = {};
+    if (count > 0) {
+        load(chunk_of(0), 0);
+        load_delta<T>(p, delta_at, chunk_of(0) * kHeadSteps, a.n, lane, delta);
+    }
+    for (int i = 0; i < count; ++i) {
+        const int chunk = chunk_of(i), first = chunk * kHeadSteps, s = i & 1;
+        const bool busy = p0 < a.cols;                    // this warp has columns of the state
+        HeadScale state_scale = {1.0f, 1.0f};
+        if (kOut) {
+            if (p.history && busy)
+                write_state<NP>(S, p.history + ((static_cast<int64_t>(a.b) * p.chunks + chunk) * p.heads + a.h) * state_size + tile_at, p0, a.cols, p.states, lane);
+            if (i > 0) __syncthreads();                   // everyone is done with the state in front of the last chunk
+            if constexpr (kScaled<T>) {
+                float top = 0.0f;
+#pragma unroll
+                for (int n = 0; n < NP / 8; ++n)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) top = fmaxf(top, finite_abs(S[n][k]));
+                state_scale = scale_for(warp_max(top));
+                if (lane == 0) powers[warp] = state_scale.down;
+            }
+#pragma unroll
+            for (int n = 0; n < NP / 8; ++n) {
+                head_store_pair(state_s + (p0 + g) * kWP + 8 * n + 2 * t, S[n][0] * state_scale.up, S[n][1] * state_scale.up);
+                head_store_pair(state_s + (p0 + g + 8) * kWP + 8 * n + 2 * t, S[n][2] * state_scale.up, S[n][3] * state_scale.up);
+            }
+        }
+        const HeadSteps st = head_steps(p, delta, bias, A2, first, a.n, lane);
+        cp_async_wait<0>();
+        __syncthreads();                                  // the tiles, and the state as an operand
+        if (M::kStages == 2 && i + 1 < count) load(chunk_of(i + 1), s ^ 1);
+        if (i + 1 < count) load_delta<T>(p, delta_at, chunk_of(i + 1) * kHeadSteps, a.n, lane, delta);
+
+        // factors of the steps
+        const double all = sum_at(st, 63), ref = warp ? sum_at(st, 16 * warp - 1) : 0.0;
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int j = lane + 32 * k;
+            vF[j] = kGrad ? pow2(st.sum[k]) : pow2(all - st.sum[k]) * st.w[k];
+            if (kOut) {
+                vC[j] = j < 16 * warp ? pow2(ref - st.sum[k]) * st.w[k] : static_cast<float>(st.sum[k] - ref);
+                vW[j] = st.w[k];
+                vR[j] = pow2(st.sum[k]);
+            }
+        }
+        __syncwarp();
+        const float decay = pow2(all);
+        log_decay += all;
+
+        if constexpr (kOut) {
+            // scores of this warp's 16 steps with all up to them, and what the state gives
+            float m[8][4] = {}, y[8][4] = {};
+#pragma unroll
+            for (int k = 0; k < NP / 16; ++k) {
+                const HeadA<T> c = load_a(tile_C(s), kWP, p0, 16 * k, lane);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j <= warp) {
+                        HeadB<T> b[2];
+                        load_b(b, tile_B(s), kWP, 16 * j, 16 * k, lane);
+                        head_mma(m[2 * j], c, b[0]);
+                        head_mma(m[2 * j + 1], c, b[1]);
+                    }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (16 * j < a.cols) {
+                        HeadB<T> b[2];
+                        load_b(b, state_s, kWP, 16 * j, 16 * k, lane);
+                        head_mma(y[2 * j], c, b[0]);
+                        head_mma(y[2 * j + 1], c, b[1]);
+                    }
+            }
+            const float l0 = vC[p0 + g], l1 = vC[p0 + g + 8], r0 = exp2f(l0), r1 = exp2f(l1);
+            float top = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j / 2 <= warp) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int col = 8 * j + 2 * t + (k & 1);
+                        if (j / 2 < warp) {
+                            m[j][k] *= (k < 2 ? r0 : r1) * vC[col];
+                        } else {
+                            const bool on = col <= p0 + g + (k < 2 ? 0 : 8);
+                            m[j][k] = on ? m[j][k] * (exp2f((k < 2 ? l0 : l1) - vC[col]) * vW[col]) : 0.0f;
+                        }
+                        if constexpr (kScaled<T>) top = fmaxf(top, finite_abs(m[j][k]));
+                    }
+                }
+            HeadScale sc = {1.0f, 1.0f};
+            if constexpr (kScaled<T>) sc = scale_for(warp_max(top));
+            const float R0 = vR[p0 + g] * sc.up, R1 = vR[p0 + g + 8] * sc.up;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float down = kScaled<T> ? powers[j / 2] : 1.0f;
+                y[j][0] *= R0 * down;
+                y[j][1] *= R0 * down;
+                y[j][2] *= R1 * down;
+                y[j][3] *= R1 * down;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j <= warp) {
+                    const HeadA<T> w = acc_to_a<T>(m[2 * j], m[2 * j + 1], sc.up);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (16 * q < a.cols) {
+                            HeadB<T> b[2];
+                            load_b_t(b, tile_u(s), kXP, 16 * q, 16 * j, lane);
+                            head_mma(y[2 * q], w, b[0]);
+                            head_mma(y[2 * q + 1], w, b[1]);
+                        }
+                }
+            // Columns of later steps have the factor zero; where u is not finite there, zero times it is not zero.
+            float odd = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) odd = fmaf(y[j][k], 0.0f, odd);
+            const bool again = __any_sync(0xffffffffu, odd != 0.0f);
+            T *stage = M::kOverC ? tile_C(s) + p0 * kWP : reinterpret_cast<T *>(smem + M::kStaging) + p0 * kXP;
+            __syncwarp();
+            if (!again) {
+                // over this warp's rows of C, which nobody else reads
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int r = g + 8 * k, c = 8 * j + 2 * t;
+                        const float2 v = head_pair(tile_u(s) + (p0 + r) * kXP + c);
+                        head_store_pair(stage + r * kXP + c, fmaf(skip, p.D ? v.x : 0.0f, y[j][2 * k] * sc.down), fmaf(skip, p.D ? v.y : 0.0f, y[j][2 * k + 1] * sc.down));
+                    }
+            } else {
+                // Step by step from shared memory: only what is there enters.  A lane has two columns.  Row r of the staging ends in front
+                // of row r + 1 of C: in this order nothing is staged over what is still read.
+                for (int r = 0; r < 16; ++r) {
+                    const int row = p0 + r;
+                    const double to = sum_at(st, row);
+                    float out[2] = {};
+                    const T *c = tile_C(s) + row * kWP;
+                    for (int q = 0; q < 2; ++q) {
+                        const int col = lane + 32 * q;
+                        float v = 0.0f;
+                        for (int n = 0; n < p.states; ++n) v = fmaf(head_f32(c[n]), head_f32(state_s[col * kWP + n]), v);
+                        out[q] = (i > 0 || seg > 0 || p.state) ? v * vR[row] * (kScaled<T> ? powers[col / 16] : 1.0f) : 0.0f;
+                    }
+                    for (int j = 0; j <= row; ++j) {
+                        float score = 0.0f;
+                        for (int n = lane; n < p.states; n += 32) score = fmaf(head_f32(c[n]), head_f32(tile_B(s)[j * kWP + n]), score);
+#pragma unroll
+                        for (int d = 16; d > 0; d >>= 1) score += __shfl_xor_sync(0xffffffffu, score, d);
+                        score *= pow2(to - sum_at(st, j)) * vW[j];
+                        for (int q = 0; q < 2; ++q) out[q] = fmaf(score, head_f32(tile_u(s)[j * kXP + lane + 32 * q]), out[q]);
+                    }
+                    __syncwarp();
+                    for (int q = 0; q < 2; ++q) {
+                        if (p.D) out[q] = fmaf(skip, head_f32(tile_u(s)[row * kXP + lane + 32 * q]), out[q]);
+                        stage[r * kXP + lane + 32 * q] = head_round<T>(out[q]);
+                    }
+                    __syncwarp();
+                }
+            }
+            __syncwarp();
+            T *y_at = static_cast<T *>(p.y) + (static_cast<int64_t>(a.b) * p.length * p.heads + a.h) * p.cols + a.tile * kHeadCols;
+            store_rows(stage, y_at, static_cast<int64_t>(p.heads) * p.cols, a.cols, p.out_unit, lane, [&](int r) -> int64_t {
+                const int step = first + p0 + r;
+                return step < a.n ? token(step) : -1;
+            });
+        }
+        if (busy) state_update<NP>(S, tile_u(s), tile_B(s), vF, decay, p0, lane);
+        if (M::kStages == 1 && i + 1 < count) {
+            __syncthreads();
+            load(chunk_of(i + 1), 0);
+        }
+    }
+    if constexpr (kOut) {
+        // final states: by the segment that holds the last step, or the first one of an empty sequence
+        if (p.final_state && seg == (chunks > 0 ? (chunks - 1) / p.segment_chunks : 0))
+            write_state<NP>(S, p.final_state + head_at * state_size + tile_at, p0, a.cols, p.states, lane);
+    } else {
+        write_state<NP>(S, p.slots + (head_at * p.segments + seg) * state_size + tile_at, p0, a.cols, p.states, lane);
+        if (threadIdx.x == 0 && a.tile == 0) p.logs[head_at * p.segments + seg] = static_cast<float>(log_decay);
+        griddep_launch_dependents();
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------- single tokens
+// One step of many sequences: bound by reading and writing the binary32 states once.  kLanes lanes have a row of a state (4 values
+// each), a CTA 16 rows of one head (4 rows of 128 states in flight per warp); everything is binary32.
+template <typename T, int kLanes, bool kWhole>
+__global__ void __launch_bounds__(128) ptq_heads_step_kernel(const HeadParams p)
+{
+    constexpr int kAt = 128 / kLanes, kRows = 16 / kAt < 1 ? 1 : 16 / kAt;             // rows at a time, times
+    const int tiles = (p.cols + kAt * kRows - 1) / (kAt * kRows);
+    int i = static_cast<int>(blockIdx.x);
+    const int col0 = i % tiles * (kAt * kRows) + threadIdx.x / kLanes;
+    i /= tiles;
+    const int h = i % p.heads, b = i / p.heads, g = h / p.group_heads, n0 = threadIdx.x % kLanes * 4;
+    const bool on = !p.lengths || __ldg(p.lengths + b) > 0;
+    const int64_t head = static_cast<int64_t>(b) * p.heads + h, base = head * p.cols * p.states;
+    const float *from = p.state ? p.state + base : nullptr;
+    float v[kRows][4];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const int c = col0 + r * kAt;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[r][k] = 0.0f;
+        if (!from || c >= p.cols) continue;
+        const float *row = from + static_cast<int64_t>(c) * p.states + n0;
+        if constexpr (kWhole) {
+            if (n0 < p.states) {
+                const float4 x = *reinterpret_cast<const float4 *>(row);
+                v[r][0] = x.x, v[r][1] = x.y, v[r][2] = x.z, v[r][3] = x.w;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (n0 + k < p.states) v[r][k] = row[k];
+        }
+    }
+    const float delta = p.delta && on ? head_f32(static_cast<const T *>(p.delta)[b * p.delta_b + h * p.delta_h]) : 0.0f;
+    const float dt = on ? head_dt(p, delta, p.delta_bias ? __ldg(p.delta_bias + h) : 0.0f) : 0.0f;
+    const float decay = dt == 0.0f ? 1.0f : expf(dt * __ldg(p.A + h)), w = !on ? 0.0f : p.flags & kHeadsUnscaled ? 1.0f : dt;
+    const T *Bp = static_cast<const T *>(p.B) + b * p.B_b + g * p.B_g + n0, *Cp = static_cast<const T *>(p.C) + b * p.C_b + g * p.C_g + n0;
+    float B[4], C[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const bool in = on && n0 + k < p.states;
+        B[k] = in ? head_f32(Bp[k]) : 0.0f;
+        C[k] = in ? head_f32(Cp[k]) : 0.0f;
+    }
+    const T *u = static_cast<const T *>(p.u) + b * p.u_b + h * p.u_h;
+    const float skip = p.D ? __ldg(p.D + h) : 0.0f;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const int c = col0 + r * kAt;
+        const float x = on && c < p.cols ? head_f32(u[c]) : 0.0f, wx = w * x;
+        float y = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (on) v[r][k] = from ? fmaf(decay, v[r][k], wx * B[k]) : wx * B[k];
+            y = n0 + k < p.states ? fmaf(v[r][k], C[k], y) : y;
+        }
+#pragma unroll
+        for (int d = kLanes / 2; d > 0; d >>= 1) y += __shfl_xor_sync(0xffffffffu, y, d);
+        if (c >= p.cols) continue;
+        if (p.final_state) {
+            float *row = p.final_state + base + static_cast<int64_t>(c) * p.states + n0;
+            if constexpr (kWhole) {
+                if (n0 < p.states) *reinterpret_cast<float4 *>(row) = make_float4(v[r][0], v[r][1], v[r][2], v[r][3]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (n0 + k < p.states) row[k] = v[r][k];
+            }
+        }
+        if (on && n0 == 0) static_cast<T *>(p.y)[head * p.cols + c] = head_round<T>(p.D ? fmaf(skip, x, y) : y);
+    }
+}
+
+}  // namespace ptq

@@ -1,0 +1,512 @@
+// Backward pass of linear attention with a decay for each head (include/ptq_heads.h).
+//
+// With S the state in front of a chunk, G the gradient of the state behind it, M_ij = e^{L_i - L_j} for j <= i (else 0), P_ij = C_i . B_j
+// and R_ij = dy_i . u_j:
+//     dC_i = sum_j M_ij R_ij w_j B_j  +  e^{L_i} S^T dy_i                =: .. + dC'_i
+//     dB_j = w_j ( sum_i M_ij R_ij C_i  +  e^{L_64 - L_j} G^T u_j )      =: w_j ( .. + dB'_j )
+//     du_j = w_j ( sum_i M_ij P_ij dy_i  +  e^{L_64 - L_j} G B_j )  (+ D dy_j)
+//     G   <- e^{L_64} G + sum_i e^{L_i} dy_i C_i^T
+//     dw_j = sum_i K_ij + B_j . dB'_j,   K = M P R (per element)
+//     dL_i = sum_j K_ij w_j + C_i . dC'_i - w_i dw_i, and dL_64 further e^{L_64} <G, S> + sum_j w_j B_j . dB'_j
+// A step's log decay is in all L from it on: its gradient is the sum of those.  Eight warps walk over the chunks from the last to the
+// first: four have 16 steps each as rows i (dC, and 16 columns of G in registers, binary32), four as rows j (dB, du); P and R are
+// computed both ways, which costs less than an exchange.  S comes from the forward pass's history.  Where S, G and the factors of G's
+// update decide states and gradients of parameters they are operands of two 16-bit parts.
+#pragma once
+
+#include "ptq_heads.cuh"
+
+namespace ptq {
+
+template <typename T, int NP>
+struct HeadBackSmem {
+    static constexpr int kWide = kHeadSteps * (NP + kHeadPad) * static_cast<int>(sizeof(T));
+    static constexpr int kNarrow = kHeadSteps * (kHeadCols + kHeadPad) * static_cast<int>(sizeof(T));
+    static constexpr int kStage = 2 * kWide + 2 * kNarrow;
+    static constexpr int kParts = sizeof(T) == 2 ? 2 : 1;                  // of S and G as operands
+    static constexpr int kStages = 2 * kStage + 2 * kParts * kWide <= 200 * 1024 ? 2 : 1;
+    static constexpr int kS = kStages * kStage;
+    static constexpr int kG = kS + kParts * kWide;
+    static constexpr int kFactors = kG + kParts * kWide;                   // floats: w, e^{L}, e^{L_64 - L}, row sums, dw, B . dB', 8 warps' own
+    static constexpr int kSmall = kFactors + (6 + 8) * kHeadSteps * 4;     // floats: largest magnitudes [8], <G, S> [4], dD [4]
+    static constexpr int kBytes = kSmall + 16 * 4;
+};
+
+// A warp's 16 rows of a state as an operand in one or two parts.
+template <int NP, typename T>
+__device__ __forceinline__ void store_parts(T *hi, const float (&S)[NP / 8][4], float up, int p0, int lane)
+{
+    constexpr int kWP = NP + kHeadPad;
+    const int g = lane >> 2, t = lane & 3;
+    T *lo = hi + kHeadSteps * kWP;
+#pragma unroll
+    for (int n = 0; n < NP / 8; ++n)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int at = (p0 + g + 8 * k) * kWP + 8 * n + 2 * t;
+            const float x = S[n][2 * k] * up, y = S[n][2 * k + 1] * up;
+            head_store_pair(hi + at, x, y);
+            if constexpr (sizeof(T) == 2) {
+                const float2 r = head_unpack<T>(head_pack<T>(x, y));
+                head_store_pair(lo + at, x - r.x, y - r.y);
+            }
+        }
+}
+// d[n] += a (rows) times 16 rows k0 .. of a state operand [p][n] in its parts.
+template <int NP, typename T>
+__device__ __forceinline__ void mma_parts(float (&d)[NP / 8][4], const HeadA<T> &a, const T *hi, int k0, int lane)
+{
+    constexpr int kWP = NP + kHeadPad;
+#pragma unroll
+    for (int n = 0; n < NP / 16; ++n) {
+        HeadB<T> b[2];
+        if constexpr (sizeof(T) == 2) {
+            load_b_t(b, hi + kHeadSteps * kWP, kWP, 16 * n, k0, lane);
+            head_mma(d[2 * n], a, b[0]);
+            head_mma(d[2 * n + 1], a, b[1]);
+        }
+        load_b_t(b, hi, kWP, 16 * n, k0, lane);
+        head_mma(d[2 * n], a, b[0]);
+        head_mma(d[2 * n + 1], a, b[1]);
+    }
+}
+// Rows of accumulators times rows of a tile, summed over the columns: what the rows p0 + g and p0 + g + 8 give, in all lanes of a quad.
+template <int NP, typename T>
+__device__ __forceinline__ float2 row_dots(const float (&d)[NP / 8][4], const T *tile, int p0, int lane)
+{
+    constexpr int kWP = NP + kHeadPad;
+    const int g = lane >> 2, t = lane & 3;
+    float2 v = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int n = 0; n < NP / 8; ++n) {
+        const float2 x = head_pair(tile + (p0 + g) * kWP + 8 * n + 2 * t), y = head_pair(tile + (p0 + g + 8) * kWP + 8 * n + 2 * t);
+        v.x = fmaf(d[n][0], x.x, fmaf(d[n][1], x.y, v.x));
+        v.y = fmaf(d[n][2], y.x, fmaf(d[n][3], y.y, v.y));
+    }
+#pragma unroll
+    for (int s = 1; s < 4; s <<= 1) {
+        v.x += __shfl_xor_sync(0xffffffffu, v.x, s);
+        v.y += __shfl_xor_sync(0xffffffffu, v.y, s);
+    }
+    return v;
+}
+template <int N>
+__device__ __forceinline__ void scale_rows(float (&d)[N][4], float s0, float s1)
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        d[n][0] *= s0;
+        d[n][1] *= s0;
+        d[n][2] *= s1;
+        d[n][3] *= s1;
+    }
+}
+template <typename T, int N>
+__device__ __forceinline__ HeadScale scale_of(const float (&d)[N][4])
+{
+    HeadScale sc = {1.0f, 1.0f};
+    if constexpr (kScaled<T>) {
+        float top = 0.0f;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top = fmaxf(top, finite_abs(d[n][k]));
+        sc = scale_for(warp_max(top));
+    }
+    return sc;
+}
+// Two rows of binary32 parts, 8 n + 2 t columns of each.
+template <int NP>
+__device__ __forceinline__ void write_part(const float (&d)[NP / 8][4], float *row0, float *row1, int states, int lane)
+{
+    const int t = lane & 3;
+    const bool pairs = states % 2 == 0;
+#pragma unroll
+    for (int n = 0; n < NP / 8; ++n)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float *row = k ? row1 : row0;
+            const int c = 8 * n + 2 * t;
+            if (!row || c >= states) continue;
+            if (pairs) {
+                *reinterpret_cast<float2 *>(row + c) = make_float2(d[n][2 * k], d[n][2 * k + 1]);
+            } else {
+                row[c] = d[n][2 * k];
+                if (c + 1 < states) row[c + 1] = d[n][2 * k + 1];
+            }
+        }
+}
+
+template <typename T, int NP>
+__global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParams p)
+{
+    using M = HeadBackSmem<T, NP>;
+    constexpr int kWP = NP + kHeadPad, kXP = kHeadCols + kHeadPad;
+    extern __shared__ __align__(128) unsigned char smem[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, r = warp & 3, p0 = 16 * r;
+    const bool rows_i = warp < 4;
+    if (p.segments > 1) griddep_wait();
+    const HeadPlace a = head_place(p, p.segments);
+    const int chunks = (a.n + kHeadSteps - 1) / kHeadSteps;
+    const int chunk0 = min(chunks, a.seg * p.segment_chunks), chunk1 = min(chunks, chunk0 + p.segment_chunks);
+    const bool reverse = p.flags & kHeadsReverse;
+    const auto stage = [&](int s) { return smem + (M::kStages == 2 ? s * M::kStage : 0); };
+    const auto tile_u = [&](int s) { return reinterpret_cast<T *>(stage(s)); };
+    const auto tile_dy = [&](int s) { return reinterpret_cast<T *>(stage(s) + M::kNarrow); };
+    const auto tile_B = [&](int s) { return reinterpret_cast<T *>(stage(s) + 2 * M::kNarrow); };
+    const auto tile_C = [&](int s) { return reinterpret_cast<T *>(stage(s) + 2 * M::kNarrow + M::kWide); };
+    T *S_op = reinterpret_cast<T *>(smem + M::kS), *G_op = reinterpret_cast<T *>(smem + M::kG);
+    float *vW = reinterpret_cast<float *>(smem + M::kFactors), *vR = vW + kHeadSteps, *vE = vW + 2 * kHeadSteps;
+    float *row_sum = vW + 3 * kHeadSteps, *dw = vW + 4 * kHeadSteps, *dot_B = vW + 5 * kHeadSteps, *vC = vW + (6 + warp) * kHeadSteps;
+    float *tops = reinterpret_cast<float *>(smem + M::kSmall), *through = tops + 8, *skip_sum = tops + 12;
+
+    const int64_t dy_l = static_cast<int64_t>(p.heads) * p.cols;
+    const int64_t dense = (static_cast<int64_t>(a.b) * p.length * p.heads + a.h) * p.cols + a.tile * kHeadCols;
+    const T *u = static_cast<const T *>(p.u) + a.b * p.u_b + a.h * p.u_h + a.tile * kHeadCols;
+    const T *dy = static_cast<const T *>(p.dy) + dense;
+    const T *B = static_cast<const T *>(p.B) + a.b * p.B_b + a.g * p.B_g, *C = static_cast<const T *>(p.C) + a.b * p.C_b + a.g * p.C_g;
+    T *du = static_cast<T *>(p.du) + dense;
+    const int64_t delta_at = a.b * p.delta_b + a.h * p.delta_h;
+    const float bias = p.delta_bias ? __ldg(p.delta_bias + a.h) : 0.0f, skip = p.D ? __ldg(p.D + a.h) : 0.0f;
+    const double A2 = static_cast<double>(__ldg(p.A + a.h)) * kLog2e;
+    const int64_t part_row = ((static_cast<int64_t>(a.tile) * p.heads + a.h) * p.batch + a.b) * p.length;
+    const int64_t head_at = static_cast<int64_t>(a.b) * p.heads + a.h, state_size = static_cast<int64_t>(p.cols) * p.states;
+    const int64_t tile_at = static_cast<int64_t>(a.tile) * kHeadCols * p.states;
+
+    // rows of du behind the sequence's end
+    {
+        const int64_t from = static_cast<int64_t>(a.seg) * p.segment_chunks * kHeadSteps, to = from + static_cast<int64_t>(p.segment_chunks) * kHeadSteps;
+        const int first = static_cast<int>(max(from, static_cast<int64_t>(a.n))), last = static_cast<int>(min(to, static_cast<int64_t>(p.length)));
+        for (int step = first + warp; step < last; step += 8)
+            for (int c = lane; c < a.cols; c += 32) du[step * dy_l + c] = head_round<T>(0.0f);
+    }
+
+    const auto token = [&](int step) { return reverse ? a.n - 1 - step : step; };
+    const auto load = [&](int chunk, int s) {
+        const int first = chunk * kHeadSteps, rows = a.n - first;
+        const int64_t sign = reverse ? -1 : 1, at = token(first);
+        load_rows<kHeadCols, 256>(tile_u(s), u + at * p.u_l, sign * p.u_l, rows, a.cols, p.unit);
+        load_rows<kHeadCols, 256>(tile_dy(s), dy + at * dy_l, sign * dy_l, rows, a.cols, p.unit);
+        load_rows<NP, 256>(tile_B(s), B + at * p.B_l, sign * p.B_l, rows, p.states, p.unit);
+        load_rows<NP, 256>(tile_C(s), C + at * p.C_l, sign * p.C_l, rows, p.states, p.unit);
+        cp_async_commit();
+    };
+    const auto kept = [&](int chunk) {
+        return p.kept + ((static_cast<int64_t>(a.b) * p.chunks + chunk) * p.heads + a.h) * state_size + tile_at;
+    };
+
+    // warps of rows i: G; of rows j: S of the chunk that comes
+    float H[NP / 8][4];
+    float skip_grad = 0.0f;
+    if (rows_i) {
+        const float *from = nullptr;
+        if (a.seg < p.segments - 1)
+            from = p.slots + (head_at * p.segments + a.seg + 1) * state_size + tile_at;
+        else if (p.dfinal)
+            from = p.dfinal + head_at * state_size + tile_at;
+        read_state<NP>(H, from, p0, a.cols, p.states, lane);
+    }
+    float delta[2] = {};
+    if (chunk1 > chunk0) {
+        load(chunk1 - 1, 0);
+        load_delta<T>(p, delta_at, (chunk1 - 1) * kHeadSteps, a.n, lane, delta);
+        if (!rows_i) read_state<NP>(H, kept(chunk1 - 1), p0, a.cols, p.states, lane);
+    }
+    for (int chunk = chunk1 - 1, s = 0; chunk >= chunk0; --chunk, s ^= 1) {
+        const int first = chunk * kHeadSteps;
+        HeadScale scS = {1.0f, 1.0f}, scG = {1.0f, 1.0f};
+        if constexpr (kScaled<T>) {                       // one power of two for all columns: they are summed over
+            float top = 0.0f;
+#pragma unroll
+            for (int n = 0; n < NP / 8; ++n)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) top = fmaxf(top, finite_abs(H[n][k]));
+            top = warp_max(top);
+            if (lane == 0) tops[warp] = top;
+            __syncthreads();
+            scG = scale_for(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+            scS = scale_for(fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
+        }
+        store_parts<NP>(rows_i ? G_op : S_op, H, rows_i ? scG.up : scS.up, p0, lane);
+        const HeadSteps st = head_steps(p, delta, bias, A2, first, a.n, lane);
+        const double all = sum_at(st, 63), ref = rows_i ? (r ? sum_at(st, 16 * r - 1) : 0.0) : sum_at(st, 16 * r + 15);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int j = lane + 32 * k;
+            if (warp == 0) {
+                vW[j] = st.w[k];
+                vR[j] = pow2(st.sum[k]);
+                vE[j] = pow2(all - st.sum[k]);
+            }
+            // own steps: the sum; others: their factor (rows i: of earlier steps, rows j: of later ones)
+            const bool other = rows_i ? j < p0 : j >= p0 + 16;
+            vC[j] = other ? pow2(rows_i ? ref - st.sum[k] : st.sum[k] - ref) : static_cast<float>(st.sum[k] - ref);
+        }
+        const float decay = pow2(all);
+        cp_async_wait<0>();
+        __syncthreads();
+        if (M::kStages == 2 && chunk > chunk0) load(chunk - 1, s ^ 1);
+        if (chunk > chunk0) {
+            load_delta<T>(p, delta_at, first - kHeadSteps, a.n, lane, delta);
+            if (!rows_i) read_state<NP>(H, kept(chunk - 1), p0, a.cols, p.states, lane);
+        }
+        const int step0 = first + p0 + g, step1 = step0 + 8;
+        const float l0 = vC[p0 + g], l1 = vC[p0 + g + 8];
+        if (rows_i) {
+            const float r0 = exp2f(l0), r1 = exp2f(l1);
+            float m[8][4] = {}, k0 = 0.0f, k1 = 0.0f;     // M R w; row sums of K w
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j <= r) {
+                    float P[2][4] = {};
+#pragma unroll
+                    for (int k = 0; k < NP / 16; ++k) {
+                        const HeadA<T> c = load_a(tile_C(s), kWP, p0, 16 * k, lane);
+                        HeadB<T> b[2];
+                        load_b(b, tile_B(s), kWP, 16 * j, 16 * k, lane);
+                        head_mma(P[0], c, b[0]);
+                        head_mma(P[1], c, b[1]);
+                    }
+#pragma unroll
+                    for (int k = 0; k < kHeadCols / 16; ++k)
+                        if (16 * k < a.cols) {
+                            const HeadA<T> y = load_a(tile_dy(s), kXP, p0, 16 * k, lane);
+                            HeadB<T> b[2];
+                            load_b(b, tile_u(s), kXP, 16 * j, 16 * k, lane);
+                            head_mma(m[2 * j], y, b[0]);
+                            head_mma(m[2 * j + 1], y, b[1]);
+                        }
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int col = 16 * j + 8 * q + 2 * t + (k & 1), row = p0 + g + (k < 2 ? 0 : 8);
+                            float &v = m[2 * j + q][k];
+                            if (col == row) skip_grad += v;
+                            if (j < r)
+                                v *= (k < 2 ? r0 : r1) * vC[col] * vW[col];
+                            else
+                                v = col <= row ? v * (exp2f((k < 2 ? l0 : l1) - vC[col]) * vW[col]) : 0.0f;
+                            if (k < 2)
+                                k0 = fmaf(v, j < r || col <= row ? P[q][k] : 0.0f, k0);
+                            else
+                                k1 = fmaf(v, j < r || col <= row ? P[q][k] : 0.0f, k1);
+                        }
+                }
+            float d[NP / 8][4] = {};
+#pragma unroll
+            for (int k = 0; k < kHeadCols / 16; ++k)
+                if (16 * k < a.cols) mma_parts<NP>(d, load_a(tile_dy(s), kXP, p0, 16 * k, lane), S_op, 16 * k, lane);
+            scale_rows(d, vR[p0 + g] * scS.down, vR[p0 + g + 8] * scS.down);
+            const float2 x = row_dots<NP>(d, tile_C(s), p0, lane);
+#pragma unroll
+            for (int q = 1; q < 4; q <<= 1) {
+                k0 += __shfl_xor_sync(0xffffffffu, k0, q);
+                k1 += __shfl_xor_sync(0xffffffffu, k1, q);
+            }
+            if (t == 0) {
+                row_sum[p0 + g] = k0 + x.x;
+                row_sum[p0 + g + 8] = k1 + x.y;
+            }
+            const HeadScale sc = scale_of<T>(m);
+            if constexpr (kScaled<T>) scale_rows(d, sc.up, sc.up);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j <= r) {
+                    const HeadA<T> w = acc_to_a<T>(m[2 * j], m[2 * j + 1], sc.up);
+#pragma unroll
+                    for (int n = 0; n < NP / 16; ++n) {
+                        HeadB<T> b[2];
+                        load_b_t(b, tile_B(s), kWP, 16 * n, 16 * j, lane);
+                        head_mma(d[2 * n], w, b[0]);
+                        head_mma(d[2 * n + 1], w, b[1]);
+                    }
+                }
+            if constexpr (kScaled<T>) scale_rows(d, sc.down, sc.down);
+            write_part<NP>(d, step0 < a.n ? p.part_C + (part_row + token(step0)) * p.states : nullptr,
+                           step1 < a.n ? p.part_C + (part_row + token(step1)) * p.states : nullptr, p.states, lane);
+            // <G, S> of this warp's columns, and G in front of the chunk
+            float z = 0.0f;
+#pragma unroll
+            for (int n = 0; n < NP / 8; ++n)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int at = (p0 + g + 8 * k) * kWP + 8 * n + 2 * t;
+                    float2 v = head_pair(S_op + at);
+                    if constexpr (sizeof(T) == 2) {
+                        const float2 lo = head_pair(S_op + kHeadSteps * kWP + at);
+                        v.x += lo.x;
+                        v.y += lo.y;
+                    }
+                    z = fmaf(H[n][2 * k], v.x, fmaf(H[n][2 * k + 1], v.y, z));
+                }
+            z *= scS.down;
+#pragma unroll
+            for (int q = 16; q > 0; q >>= 1) z += __shfl_xor_sync(0xffffffffu, z, q);
+            if (lane == 0) through[r] = z * decay;
+            if (p0 < a.cols) state_update<NP>(H, tile_dy(s), tile_C(s), vR, decay, p0, lane);
+        } else {
+            const float r0 = exp2f(-l0), r1 = exp2f(-l1);
+            float mp[8][4] = {}, mr[8][4] = {}, k0 = 0.0f, k1 = 0.0f;          // M P and M R, transposed; column sums of K
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i >= r) {
+#pragma unroll
+                    for (int k = 0; k < NP / 16; ++k) {
+                        const HeadA<T> c = load_a(tile_B(s), kWP, p0, 16 * k, lane);
+                        HeadB<T> b[2];
+                        load_b(b, tile_C(s), kWP, 16 * i, 16 * k, lane);
+                        head_mma(mp[2 * i], c, b[0]);
+                        head_mma(mp[2 * i + 1], c, b[1]);
+                    }
+#pragma unroll
+                    for (int k = 0; k < kHeadCols / 16; ++k)
+                        if (16 * k < a.cols) {
+                            const HeadA<T> x = load_a(tile_u(s), kXP, p0, 16 * k, lane);
+                            HeadB<T> b[2];
+                            load_b(b, tile_dy(s), kXP, 16 * i, 16 * k, lane);
+                            head_mma(mr[2 * i], x, b[0]);
+                            head_mma(mr[2 * i + 1], x, b[1]);
+                        }
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int col = 16 * i + 8 * q + 2 * t + (k & 1), row = p0 + g + (k < 2 ? 0 : 8);
+                            const bool on = i > r || col >= row;
+                            const float f = i > r ? (k < 2 ? r0 : r1) * vC[col] : exp2f(vC[col] - (k < 2 ? l0 : l1));
+                            float &vp = mp[2 * i + q][k], &vr = mr[2 * i + q][k];
+                            vr = on ? vr * f : 0.0f;
+                            const float e = on ? vr * vp : 0.0f;
+                            vp = on ? vp * f : 0.0f;
+                            if (k < 2)
+                                k0 += e;
+                            else
+                                k1 += e;
+                        }
+                }
+            const float w0 = vW[p0 + g], w1 = vW[p0 + g + 8], e0 = vE[p0 + g], e1 = vE[p0 + g + 8];
+            {
+                float d[8][4] = {};
+#pragma unroll
+                for (int k = 0; k < NP / 16; ++k) {
+                    const HeadA<T> c = load_a(tile_B(s), kWP, p0, 16 * k, lane);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (16 * q < a.cols) {
+                            HeadB<T> b[2];
+                            load_b(b, G_op, kWP, 16 * q, 16 * k, lane);
+                            head_mma(d[2 * q], c, b[0]);
+                            head_mma(d[2 * q + 1], c, b[1]);
+                        }
+                }
+                const HeadScale sc = scale_of<T>(mp);
+                scale_rows(d, e0 * scG.down * sc.up, e1 * scG.down * sc.up);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i >= r) {
+                        const HeadA<T> w = acc_to_a<T>(mp[2 * i], mp[2 * i + 1], sc.up);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            if (16 * q < a.cols) {
+                                HeadB<T> b[2];
+                                load_b_t(b, tile_dy(s), kXP, 16 * q, 16 * i, lane);
+                                head_mma(d[2 * q], w, b[0]);
+                                head_mma(d[2 * q + 1], w, b[1]);
+                            }
+                    }
+                scale_rows(d, w0 * sc.down, w1 * sc.down);
+#pragma unroll
+                for (int n = 0; n < 8; ++n)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int c = 8 * n + 2 * t, step = k ? step1 : step0;
+                        if (step >= a.n || c >= a.cols) continue;
+                        const float2 y = head_pair(tile_dy(s) + (p0 + g + 8 * k) * kXP + c);
+                        const float v0 = p.D ? fmaf(skip, y.x, d[n][2 * k]) : d[n][2 * k], v1 = p.D ? fmaf(skip, y.y, d[n][2 * k + 1]) : d[n][2 * k + 1];
+                        T *to = du + token(step) * dy_l + c;
+                        if (p.out_unit >= 2 * static_cast<int>(sizeof(T))) {
+                            head_store_pair(to, v0, v1);
+                        } else {
+                            to[0] = head_round<T>(v0);
+                            if (c + 1 < a.cols) to[1] = head_round<T>(v1);
+                        }
+                    }
+            }
+            float d[NP / 8][4] = {};
+#pragma unroll
+            for (int k = 0; k < kHeadCols / 16; ++k)
+                if (16 * k < a.cols) mma_parts<NP>(d, load_a(tile_u(s), kXP, p0, 16 * k, lane), G_op, 16 * k, lane);
+            scale_rows(d, e0 * scG.down, e1 * scG.down);
+            const float2 x = row_dots<NP>(d, tile_B(s), p0, lane);
+#pragma unroll
+            for (int q = 1; q < 4; q <<= 1) {
+                k0 += __shfl_xor_sync(0xffffffffu, k0, q);
+                k1 += __shfl_xor_sync(0xffffffffu, k1, q);
+            }
+            if (t == 0) {
+                dw[p0 + g] = k0 + x.x;
+                dw[p0 + g + 8] = k1 + x.y;
+                dot_B[p0 + g] = x.x;
+                dot_B[p0 + g + 8] = x.y;
+            }
+            const HeadScale sc = scale_of<T>(mr);
+            if constexpr (kScaled<T>) scale_rows(d, sc.up, sc.up);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i >= r) {
+                    const HeadA<T> w = acc_to_a<T>(mr[2 * i], mr[2 * i + 1], sc.up);
+#pragma unroll
+                    for (int n = 0; n < NP / 16; ++n) {
+                        HeadB<T> b[2];
+                        load_b_t(b, tile_C(s), kWP, 16 * n, 16 * i, lane);
+                        head_mma(d[2 * n], w, b[0]);
+                        head_mma(d[2 * n + 1], w, b[1]);
+                    }
+                }
+            scale_rows(d, w0 * sc.down, w1 * sc.down);
+            write_part<NP>(d, step0 < a.n ? p.part_B + (part_row + token(step0)) * p.states : nullptr,
+                           step1 < a.n ? p.part_B + (part_row + token(step1)) * p.states : nullptr, p.states, lane);
+        }
+        __syncthreads();                                  // the sums; S and G as operands, and the tiles, have been read
+        if (M::kStages == 1 && chunk > chunk0) load(chunk - 1, 0);
+        if (warp == 0) {
+            double v[2], y = 0.0;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int j = lane + 32 * k;
+                v[k] = static_cast<double>(row_sum[j]) - static_cast<double>(st.w[k]) * dw[j];
+                y += static_cast<double>(st.w[k]) * dot_B[j];
+            }
+#pragma unroll
+            for (int q = 16; q > 0; q >>= 1) y += __shfl_xor_sync(0xffffffffu, y, q);
+            y += static_cast<double>(through[0]) + through[1] + through[2] + through[3];
+#pragma unroll
+            for (int q = 1; q < 32; q <<= 1) {
+                const double e = __shfl_down_sync(0xffffffffu, v[0], q), f = __shfl_down_sync(0xffffffffu, v[1], q);
+                if (lane + q < 32) {
+                    v[0] += e;
+                    v[1] += f;
+                }
+            }
+            v[0] += __shfl_sync(0xffffffffu, v[1], 0);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int step = first + lane + 32 * k;
+                if (step < a.n) p.part_dt[part_row + token(step)] = make_float2(static_cast<float>(v[k] + y), dw[lane + 32 * k]);
+            }
+        }
+    }
+    if (rows_i) {
+        if (a.seg == 0 && p.final_state) write_state<NP>(H, p.final_state + head_at * state_size + tile_at, p0, a.cols, p.states, lane);
+#pragma unroll
+        for (int q = 16; q > 0; q >>= 1) skip_grad += __shfl_xor_sync(0xffffffffu, skip_grad, q);
+        if (lane == 0) skip_sum[r] = skip_grad;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0)
+        p.part_D[((static_cast<int64_t>(a.tile) * p.segments + a.seg) * p.batch + a.b) * p.heads + a.h] = skip_sum[0] + skip_sum[1] + skip_sum[2] + skip_sum[3];
+    griddep_launch_dependents();
+}
+
+}  // namespace ptq

@@ -277,7 +277,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ptq_torch", nullptr, -1, methods,
 PyMODINIT_FUNC PyInit__ptq_torch(void)
 {
     PyObject *m = PyModule_Create(&module);
-    if (m && (ptq_add_block_methods(m) != 0 || ptq_add_fp8_methods(m) != 0)) {
+    if (m && (ptq_add_block_methods(m) != 0 || ptq_add_heads_methods(m) != 0 || ptq_add_fp8_methods(m) != 0)) {
         Py_DECREF(m);
         return nullptr;
     }

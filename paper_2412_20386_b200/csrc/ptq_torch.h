@@ -7,4 +7,5 @@
 #define PTQ_METHOD(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL, nullptr}
 
 int ptq_add_block_methods(PyObject *module);      // the operators of include/ptq_block.h; 0 on success
+int ptq_add_heads_methods(PyObject *module);      // those of include/ptq_heads.h
 int ptq_add_fp8_methods(PyObject *module);        // those of include/ptq_fp8.h
