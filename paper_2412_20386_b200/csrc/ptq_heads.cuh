@@ -225,7 +225,8 @@ __device__ __forceinline__ void mma_tf32(float (&d)[4], uint32_t a0, uint32_t a1
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// d += a b.  binary32: both operands as two tf32 parts (22 bits), the product of the two lower parts left out (2^-22 of the terms).
+// d += a b.  binary32: both operands as two tf32 parts (22 bits), the product of the two lower parts left out (2^-22 of the terms);
+// the tensor cores' sums are cut off rather than rounded, so these 16 terms are summed on their own and added to the others rounded.
 template <typename T>
 __device__ __forceinline__ void head_mma(float (&d)[4], const HeadA<T> &a, const HeadB<T> &b)
 {
@@ -250,12 +251,32 @@ __device__ __forceinline__ void head_mma(float (&d)[4], const HeadA<T> &a, const
             bl[i] = to_tf32(b.v[i] - __uint_as_float(bh[i]));
         }
         // the order of the inner index is the same on both sides: element 2t in place t, 2t + 1 in place t + 4
+        float e[4] = {};
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            mma_tf32(d, al[4 * k], al[4 * k + 2], al[4 * k + 1], al[4 * k + 3], bh[2 * k], bh[2 * k + 1]);
-            mma_tf32(d, ah[4 * k], ah[4 * k + 2], ah[4 * k + 1], ah[4 * k + 3], bl[2 * k], bl[2 * k + 1]);
-            mma_tf32(d, ah[4 * k], ah[4 * k + 2], ah[4 * k + 1], ah[4 * k + 3], bh[2 * k], bh[2 * k + 1]);
+            mma_tf32(e, al[4 * k], al[4 * k + 2], al[4 * k + 1], al[4 * k + 3], bh[2 * k], bh[2 * k + 1]);
+            mma_tf32(e, ah[4 * k], ah[4 * k + 2], ah[4 * k + 1], ah[4 * k + 3], bl[2 * k], bl[2 * k + 1]);
         }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) mma_tf32(e, ah[4 * k], ah[4 * k + 2], ah[4 * k + 1], ah[4 * k + 3], bh[2 * k], bh[2 * k + 1]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] += e[i];
+    }
+}
+
+// Operands of more bits than the activations' type has: two binary16 or three bfloat16 values that add up to one of 22 or 24 bits
+// (binary32: head_mma splits).
+template <typename T>
+constexpr int kHeadParts = std::is_same<T, __half>::value ? 2 : std::is_same<T, __nv_bfloat16>::value ? 3 : 1;
+template <typename T>
+__device__ __forceinline__ void head_split(float x, float y, uint32_t (&r)[kHeadParts<T>])
+{
+#pragma unroll
+    for (int q = 0; q < kHeadParts<T>; ++q) {
+        r[q] = head_pack<T>(x, y);
+        const float2 v = head_unpack<T>(r[q]);
+        x -= v.x;
+        y -= v.y;
     }
 }
 
@@ -406,7 +427,7 @@ __device__ __forceinline__ HeadPlace head_place(const HeadParams &p, int segment
 }
 
 // state[p][n] <- decay state + sum_j f_j x_j[p] z_j[n] over a chunk, for 16 columns p0 ..; x and z are tiles [step][..].  The factors make
-// x an operand of more than 16 bits: it goes in as two.
+// x an operand of more than 16 bits: it goes in in parts.
 template <int NP, typename T>
 __device__ __forceinline__ void state_update(float (&S)[NP / 8][4], const T *x, const T *z, const float *f, float decay, int p0, int lane)
 {
@@ -427,44 +448,41 @@ __device__ __forceinline__ void state_update(float (&S)[NP / 8][4], const T *x, 
             }
         sc = scale_for(warp_max(top) * warp_max(ftop));
     }
-    const float before = decay * sc.up;
-#pragma unroll
-    for (int n = 0; n < NP / 8; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) S[n][i] *= before;
+    // the chunk's sums on their own, joined with the state in binary32: the tensor cores' sums are cut off, not rounded
+    HeadA<T> part[kHeadSteps / 16][kHeadParts<T>];
 #pragma unroll
     for (int k = 0; k < kHeadSteps / 16; ++k) {
         const float2 f0 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t), f1 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t + 8);
-        HeadA<T> hi, lo;
         if constexpr (sizeof(T) == 2) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float2 v = head_unpack<T>(a[k].r[i]), q = i < 2 ? f0 : f1;
-                const float vx = v.x * (q.x * sc.up), vy = v.y * (q.y * sc.up);
-                hi.r[i] = head_pack<T>(vx, vy);
-                const float2 r = head_unpack<T>(hi.r[i]);
-                lo.r[i] = head_pack<T>(vx - r.x, vy - r.y);
+                uint32_t r[kHeadParts<T>];
+                head_split<T>(v.x * (q.x * sc.up), v.y * (q.y * sc.up), r);
+#pragma unroll
+                for (int j = 0; j < kHeadParts<T>; ++j) part[k][j].r[i] = r[j];
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) hi.v[i] = a[k].v[i] * (i < 4 ? (i & 1 ? f0.y : f0.x) : (i & 1 ? f1.y : f1.x));
+            for (int i = 0; i < 8; ++i) part[k][0].v[i] = a[k].v[i] * (i < 4 ? (i & 1 ? f0.y : f0.x) : (i & 1 ? f1.y : f1.x));
         }
+    }
 #pragma unroll
-        for (int n = 0; n < NP / 16; ++n) {
+    for (int n = 0; n < NP / 16; ++n) {
+        float sum[2][4] = {};
+#pragma unroll
+        for (int k = 0; k < kHeadSteps / 16; ++k) {
             HeadB<T> b[2];
             load_b_t(b, z, kZP, 16 * n, 16 * k, lane);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if constexpr (sizeof(T) == 2) head_mma(S[2 * n + j], lo, b[j]);
-                head_mma(S[2 * n + j], hi, b[j]);
-            }
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int q = kHeadParts<T> - 1; q >= 0; --q) head_mma(sum[j], part[k][q], b[j]);
         }
-    }
-    if constexpr (kScaled<T>) {
 #pragma unroll
-        for (int n = 0; n < NP / 8; ++n)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) S[n][i] *= sc.down;
+            for (int i = 0; i < 4; ++i) S[2 * n + j][i] = fmaf(decay, S[2 * n + j][i], sum[j][i] * sc.down);
     }
 }
 

@@ -7,11 +7,12 @@
 //     du_j = w_j ( sum_i M_ij P_ij dy_i  +  e^{L_64 - L_j} G B_j )  (+ D dy_j)
 //     G   <- e^{L_64} G + sum_i e^{L_i} dy_i C_i^T
 //     dw_j = sum_i K_ij + B_j . dB'_j,   K = M P R (per element)
-//     dL_i = sum_j K_ij w_j + C_i . dC'_i - w_i dw_i, and dL_64 further e^{L_64} <G, S> + sum_j w_j B_j . dB'_j
-// A step's log decay is in all L from it on: its gradient is the sum of those.  Eight warps walk over the chunks from the last to the
+//     d(log decay)_t = sum_{j < t <= i} K_ij w_j + sum_{i >= t} C_i . dC'_i + sum_{j < t} w_j B_j . dB'_j + e^{L_64} <G, S>
+// The last line sums what passes step t.  (Gradients of the L_i, summed from t on, are the same; but in them each pair of steps on one
+// side of t comes twice with opposite signs, and what the roundings leave of them is more than the result of a step near an end.)  Eight warps walk over the chunks from the last to the
 // first: four have 16 steps each as rows i (dC, and 16 columns of G in registers, binary32), four as rows j (dB, du); P and R are
 // computed both ways, which costs less than an exchange.  S comes from the forward pass's history.  Where S, G and the factors of G's
-// update decide states and gradients of parameters they are operands of two 16-bit parts.
+// update decide states and gradients of parameters they are operands of several 16-bit parts.
 #pragma once
 
 #include "ptq_heads.cuh"
@@ -23,52 +24,51 @@ struct HeadBackSmem {
     static constexpr int kWide = kHeadSteps * (NP + kHeadPad) * static_cast<int>(sizeof(T));
     static constexpr int kNarrow = kHeadSteps * (kHeadCols + kHeadPad) * static_cast<int>(sizeof(T));
     static constexpr int kStage = 2 * kWide + 2 * kNarrow;
-    static constexpr int kParts = sizeof(T) == 2 ? 2 : 1;                  // of S and G as operands
-    static constexpr int kStages = 2 * kStage + 2 * kParts * kWide <= 200 * 1024 ? 2 : 1;
+    static constexpr int kParts = kHeadParts<T>;                           // of S and G as operands
+    static constexpr int kStages = 2 * kStage + 2 * kParts * kWide <= 220 * 1024 ? 2 : 1;
     static constexpr int kS = kStages * kStage;
     static constexpr int kG = kS + kParts * kWide;
-    static constexpr int kFactors = kG + kParts * kWide;                   // floats: w, e^{L}, e^{L_64 - L}, row sums, dw, B . dB', 8 warps' own
-    static constexpr int kSmall = kFactors + (6 + 8) * kHeadSteps * 4;     // floats: largest magnitudes [8], <G, S> [4], dD [4]
+    static constexpr int kFactors = kG + kParts * kWide;                   // floats: w, e^{L}, e^{L_64 - L}, C . dC', dw, B . dB', 8 warps' own, 4 warps' K
+    static constexpr int kSmall = kFactors + (6 + 8 + 4) * kHeadSteps * 4;     // floats: largest magnitudes [8], <G, S> [4], dD [4]
     static constexpr int kBytes = kSmall + 16 * 4;
 };
 
-// A warp's 16 rows of a state as an operand in one or two parts.
+// A warp's 16 rows of a state as an operand in its parts, one tile each.
 template <int NP, typename T>
-__device__ __forceinline__ void store_parts(T *hi, const float (&S)[NP / 8][4], float up, int p0, int lane)
+__device__ __forceinline__ void store_parts(T *to, const float (&S)[NP / 8][4], float up, int p0, int lane)
 {
     constexpr int kWP = NP + kHeadPad;
     const int g = lane >> 2, t = lane & 3;
-    T *lo = hi + kHeadSteps * kWP;
 #pragma unroll
     for (int n = 0; n < NP / 8; ++n)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const int at = (p0 + g + 8 * k) * kWP + 8 * n + 2 * t;
+            T *at = to + (p0 + g + 8 * k) * kWP + 8 * n + 2 * t;
             const float x = S[n][2 * k] * up, y = S[n][2 * k + 1] * up;
-            head_store_pair(hi + at, x, y);
             if constexpr (sizeof(T) == 2) {
-                const float2 r = head_unpack<T>(head_pack<T>(x, y));
-                head_store_pair(lo + at, x - r.x, y - r.y);
+                uint32_t r[kHeadParts<T>];
+                head_split<T>(x, y, r);
+#pragma unroll
+                for (int q = 0; q < kHeadParts<T>; ++q) *reinterpret_cast<uint32_t *>(at + q * kHeadSteps * kWP) = r[q];
+            } else {
+                *reinterpret_cast<float2 *>(at) = make_float2(x, y);
             }
         }
 }
 // d[n] += a (rows) times 16 rows k0 .. of a state operand [p][n] in its parts.
 template <int NP, typename T>
-__device__ __forceinline__ void mma_parts(float (&d)[NP / 8][4], const HeadA<T> &a, const T *hi, int k0, int lane)
+__device__ __forceinline__ void mma_parts(float (&d)[NP / 8][4], const HeadA<T> &a, const T *state, int k0, int lane)
 {
     constexpr int kWP = NP + kHeadPad;
 #pragma unroll
-    for (int n = 0; n < NP / 16; ++n) {
-        HeadB<T> b[2];
-        if constexpr (sizeof(T) == 2) {
-            load_b_t(b, hi + kHeadSteps * kWP, kWP, 16 * n, k0, lane);
+    for (int n = 0; n < NP / 16; ++n)
+#pragma unroll
+        for (int q = kHeadParts<T> - 1; q >= 0; --q) {
+            HeadB<T> b[2];
+            load_b_t(b, state + q * kHeadSteps * kWP, kWP, 16 * n, k0, lane);
             head_mma(d[2 * n], a, b[0]);
             head_mma(d[2 * n + 1], a, b[1]);
         }
-        load_b_t(b, hi, kWP, 16 * n, k0, lane);
-        head_mma(d[2 * n], a, b[0]);
-        head_mma(d[2 * n + 1], a, b[1]);
-    }
 }
 // Rows of accumulators times rows of a tile, summed over the columns: what the rows p0 + g and p0 + g + 8 give, in all lanes of a quad.
 template <int NP, typename T>
@@ -157,7 +157,8 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
     const auto tile_C = [&](int s) { return reinterpret_cast<T *>(stage(s) + 2 * M::kNarrow + M::kWide); };
     T *S_op = reinterpret_cast<T *>(smem + M::kS), *G_op = reinterpret_cast<T *>(smem + M::kG);
     float *vW = reinterpret_cast<float *>(smem + M::kFactors), *vR = vW + kHeadSteps, *vE = vW + 2 * kHeadSteps;
-    float *row_sum = vW + 3 * kHeadSteps, *dw = vW + 4 * kHeadSteps, *dot_B = vW + 5 * kHeadSteps, *vC = vW + (6 + warp) * kHeadSteps;
+    float *dot_C = vW + 3 * kHeadSteps, *dw = vW + 4 * kHeadSteps, *dot_B = vW + 5 * kHeadSteps, *vC = vW + (6 + warp) * kHeadSteps;
+    float *pairs = vW + 14 * kHeadSteps;                  // [4]: what a warp's rows of K w pass over each step
     float *tops = reinterpret_cast<float *>(smem + M::kSmall), *through = tops + 8, *skip_sum = tops + 12;
 
     const int64_t dy_l = static_cast<int64_t>(p.heads) * p.cols;
@@ -254,7 +255,7 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
         const float l0 = vC[p0 + g], l1 = vC[p0 + g + 8];
         if (rows_i) {
             const float r0 = exp2f(l0), r1 = exp2f(l1);
-            float m[8][4] = {}, k0 = 0.0f, k1 = 0.0f;     // M R w; row sums of K w
+            float m[8][4] = {}, run[2] = {};              // M R w; K w of a row summed up to a column
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 if (j <= r) {
@@ -287,11 +288,34 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
                                 v *= (k < 2 ? r0 : r1) * vC[col] * vW[col];
                             else
                                 v = col <= row ? v * (exp2f((k < 2 ? l0 : l1) - vC[col]) * vW[col]) : 0.0f;
-                            if (k < 2)
-                                k0 = fmaf(v, j < r || col <= row ? P[q][k] : 0.0f, k0);
-                            else
-                                k1 = fmaf(v, j < r || col <= row ? P[q][k] : 0.0f, k1);
+                            P[q][k] = j < r || col <= row ? v * P[q][k] : 0.0f;
                         }
+                    // what passes over step `col`: of each row i >= col its sum up to, not with, col
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        float pass[2] = {};
+                        const int col = 16 * j + 8 * q + 2 * t;
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const int row = p0 + g + 8 * k;
+                            float v = P[q][2 * k] + P[q][2 * k + 1];
+#pragma unroll
+                            for (int z = 1; z < 4; z <<= 1) {
+                                const float w = __shfl_up_sync(0xffffffffu, v, z, 4);
+                                if (t >= z) v += w;
+                            }
+                            const float before = __shfl_up_sync(0xffffffffu, v, 1, 4), at = run[k] + (t ? before : 0.0f);
+                            if (col <= row) pass[0] += at;
+                            if (col + 1 <= row) pass[1] += at + P[q][2 * k];
+                            run[k] += __shfl_sync(0xffffffffu, v, 3, 4);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                            for (int z = 4; z < 32; z <<= 1) pass[k] += __shfl_xor_sync(0xffffffffu, pass[k], z);
+                            if (g == 0) pairs[r * kHeadSteps + col + k] = pass[k];
+                        }
+                    }
                 }
             float d[NP / 8][4] = {};
 #pragma unroll
@@ -299,14 +323,9 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
                 if (16 * k < a.cols) mma_parts<NP>(d, load_a(tile_dy(s), kXP, p0, 16 * k, lane), S_op, 16 * k, lane);
             scale_rows(d, vR[p0 + g] * scS.down, vR[p0 + g + 8] * scS.down);
             const float2 x = row_dots<NP>(d, tile_C(s), p0, lane);
-#pragma unroll
-            for (int q = 1; q < 4; q <<= 1) {
-                k0 += __shfl_xor_sync(0xffffffffu, k0, q);
-                k1 += __shfl_xor_sync(0xffffffffu, k1, q);
-            }
             if (t == 0) {
-                row_sum[p0 + g] = k0 + x.x;
-                row_sum[p0 + g + 8] = k1 + x.y;
+                dot_C[p0 + g] = x.x;
+                dot_C[p0 + g + 8] = x.y;
             }
             const HeadScale sc = scale_of<T>(m);
             if constexpr (kScaled<T>) scale_rows(d, sc.up, sc.up);
@@ -332,11 +351,12 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int at = (p0 + g + 8 * k) * kWP + 8 * n + 2 * t;
-                    float2 v = head_pair(S_op + at);
-                    if constexpr (sizeof(T) == 2) {
-                        const float2 lo = head_pair(S_op + kHeadSteps * kWP + at);
-                        v.x += lo.x;
-                        v.y += lo.y;
+                    float2 v = make_float2(0.0f, 0.0f);
+#pragma unroll
+                    for (int q = kHeadParts<T> - 1; q >= 0; --q) {
+                        const float2 x = head_pair(S_op + q * kHeadSteps * kWP + at);
+                        v.x += x.x;
+                        v.y += x.y;
                     }
                     z = fmaf(H[n][2 * k], v.x, fmaf(H[n][2 * k + 1], v.y, z));
                 }
@@ -471,29 +491,41 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
         __syncthreads();                                  // the sums; S and G as operands, and the tiles, have been read
         if (M::kStages == 1 && chunk > chunk0) load(chunk - 1, 0);
         if (warp == 0) {
-            double v[2], y = 0.0;
+            // from the last step on C . dC', up to the step w B . dB', the pairs over it and <G, S>
+            double v[2], y[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const int j = lane + 32 * k;
-                v[k] = static_cast<double>(row_sum[j]) - static_cast<double>(st.w[k]) * dw[j];
-                y += static_cast<double>(st.w[k]) * dot_B[j];
+                v[k] = dot_C[lane + 32 * k];
+                y[k] = static_cast<double>(st.w[k]) * dot_B[lane + 32 * k];
             }
-#pragma unroll
-            for (int q = 16; q > 0; q >>= 1) y += __shfl_xor_sync(0xffffffffu, y, q);
-            y += static_cast<double>(through[0]) + through[1] + through[2] + through[3];
+            const double y0 = y[0], y1 = y[1];
 #pragma unroll
             for (int q = 1; q < 32; q <<= 1) {
                 const double e = __shfl_down_sync(0xffffffffu, v[0], q), f = __shfl_down_sync(0xffffffffu, v[1], q);
+                const double c = __shfl_up_sync(0xffffffffu, y[0], q), d = __shfl_up_sync(0xffffffffu, y[1], q);
                 if (lane + q < 32) {
                     v[0] += e;
                     v[1] += f;
                 }
+                if (lane >= q) {
+                    y[0] += c;
+                    y[1] += d;
+                }
             }
             v[0] += __shfl_sync(0xffffffffu, v[1], 0);
+            y[1] += __shfl_sync(0xffffffffu, y[0], 31);
+            y[0] -= y0;
+            y[1] -= y1;
+            const double z = static_cast<double>(through[0]) + through[1] + through[2] + through[3];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                v[k] += y[k] + z;
+                for (int q = (lane + 32 * k) / 16; q < 4; ++q) v[k] += pairs[q * kHeadSteps + lane + 32 * k];
+            }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const int step = first + lane + 32 * k;
-                if (step < a.n) p.part_dt[part_row + token(step)] = make_float2(static_cast<float>(v[k] + y), dw[lane + 32 * k]);
+                if (step < a.n) p.part_dt[part_row + token(step)] = make_float2(static_cast<float>(v[k]), dw[lane + 32 * k]);
             }
         }
     }
