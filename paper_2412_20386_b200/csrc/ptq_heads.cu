@@ -195,7 +195,7 @@ ptq_status_t ptq_heads_forward(const ptq_heads_t *s, void *y, float *final_state
     p.y = y;
     p.final_state = final_state;
     p.history = history;
-    p.out_unit = aligned({y}, 16) && s->cols * e % 16 == 0 ? 16 : e;
+    p.out_unit = aligned({y}, 16) && s->cols * e % 16 == 0 ? 16 : aligned({y}, 2 * e) && s->cols % 2 == 0 ? 2 * e : e;
     unsigned char *w = static_cast<unsigned char *>(workspace);
     p.slots = reinterpret_cast<float *>(w + space.slots);
     p.logs = reinterpret_cast<float *>(w + space.logs);

@@ -4,8 +4,9 @@
 // an input (dt or 1) and S the state in front of the chunk:
 //     y_i = sum_{j <= i} e^{L_i - L_j} w_j (C_i . B_j) u_j  +  e^{L_i} S C_i  (+ D u_i)
 //     S  <- e^{L_64} S + sum_j e^{L_64 - L_j} w_j u_j B_j^T
-// A CTA walks over the chunks of a sequence for 64 columns of a head; four warps have 16 steps of each chunk (scores and outputs)
-// and 16 columns of the state, which stays in registers in binary32 from chunk to chunk.
+// A CTA walks over the chunks of a sequence for 64 columns of a head.  Eight warps: two have 16 steps of each chunk, 32 columns of
+// the outputs each (the scores of the steps both), and 16 columns of the state, half of its states each, which stay in registers in
+// binary32 from chunk to chunk.
 //
 // The products are mma.sync on 16-bit operands: per chunk they are 64 x 64 x (16 .. 128), the scores go from one product's
 // accumulators through exponentials into the next one's operand and the state's update needs its operand in two halves (the
@@ -297,6 +298,27 @@ __device__ __forceinline__ float warp_max(float v)
     for (int d = 16; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
     return v;
 }
+// The largest magnitude of a warp's values; if that is infinite, of the finite ones (the others are lost whatever their scale).
+template <int N>
+__device__ __forceinline__ float warp_top(const float (&d)[N][4])
+{
+    float top = 0.0f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        top = fmaxf(top, fmaxf(fabsf(d[n][0]), fabsf(d[n][1])));
+        top = fmaxf(top, fmaxf(fabsf(d[n][2]), fabsf(d[n][3])));
+    }
+    top = warp_max(top);
+    if (__float_as_uint(top) >= 0x7f800000u) {
+        top = 0.0f;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top = fmaxf(top, finite_abs(d[n][k]));
+        top = warp_max(top);
+    }
+    return top;
+}
 // The power of two, within 2^-60 .. 2^60, and its inverse.
 struct HeadScale {
     float up, down;
@@ -330,11 +352,18 @@ __device__ __forceinline__ void load_rows(T *tile, const T *src, int64_t step, i
 {
     constexpr int kPitch = kWidth + kHeadPad;
     const auto go = [&](auto bytes) {
-        constexpr int kBytes = decltype(bytes)::value, kElems = kBytes / static_cast<int>(sizeof(T)), kRow = kWidth / kElems;
-        for (int i = threadIdx.x; i < kHeadSteps * kRow; i += kThreads) {
-            const int r = i / kRow, c = i % kRow * kElems;
-            const bool on = r < rows && c < cols;
-            cp_async(head_smem(tile + r * kPitch + c), on ? src + r * step + c : src, kBytes, on);
+        constexpr int kBytes = decltype(bytes)::value, kElems = kBytes / static_cast<int>(sizeof(T)), kRow = kWidth / kElems, kAt = kThreads / kRow;
+        static_assert(kThreads % kRow == 0 && kHeadSteps % kAt == 0, "a thread has one place of all its rows");
+        const int r0 = threadIdx.x / kRow, c = threadIdx.x % kRow * kElems;
+        const T *from = src + r0 * step + c;
+        uint32_t to = head_smem(tile + r0 * kPitch + c);
+        int left = c < cols ? rows - r0 : 0;
+#pragma unroll
+        for (int i = 0; i < kHeadSteps / kAt; ++i) {
+            cp_async(to, left > 0 ? from : src, kBytes, left > 0);
+            from += kAt * step;
+            to += kAt * kPitch * static_cast<int>(sizeof(T));
+            left -= kAt;
         }
     };
     if (unit == 16) {
@@ -352,7 +381,7 @@ __device__ __forceinline__ void load_rows(T *tile, const T *src, int64_t step, i
 }
 
 // ---------------------------------------------------------------------------------------------------- steps of a chunk
-// A lane has steps `lane` and `lane + 32` of a chunk.
+// A lane has steps 2 lane and 2 lane + 1 of a chunk.
 struct HeadSteps {
     float dt[2], w[2];
     double sum[2];                    // log2 of the decays up to and with the step
@@ -371,7 +400,7 @@ __device__ __forceinline__ void load_delta(const HeadParams &p, int64_t at, int 
     const T *d = static_cast<const T *>(p.delta);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const int i = first + lane + 32 * k;
+        const int i = first + 2 * lane + k;
         v[k] = d && i < n ? head_f32(d[at + (p.flags & kHeadsReverse ? n - 1 - i : i) * p.delta_l]) : 0.0f;
     }
 }
@@ -381,29 +410,37 @@ __device__ __forceinline__ HeadSteps head_steps(const HeadParams &p, const float
     HeadSteps s;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        const bool on = first + lane + 32 * k < n;
+        const bool on = first + 2 * lane + k < n;
         s.dt[k] = on ? head_dt(p, delta[k], bias) : 0.0f;
         s.w[k] = !on ? 0.0f : p.flags & kHeadsUnscaled ? 1.0f : s.dt[k];
         double a = s.dt[k] == 0.0f ? 0.0 : static_cast<double>(s.dt[k]) * A2;
         if (a < -4000.0) a = -4000.0;
         s.sum[k] = a;
     }
+    s.sum[1] += s.sum[0];
+    double all = s.sum[1];
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const double x = __shfl_up_sync(0xffffffffu, s.sum[0], d), y = __shfl_up_sync(0xffffffffu, s.sum[1], d);
-        if (lane >= d) {
-            s.sum[0] += x;
-            s.sum[1] += y;
-        }
+        const double x = __shfl_up_sync(0xffffffffu, all, d);
+        if (lane >= d) all += x;
     }
-    s.sum[1] += __shfl_sync(0xffffffffu, s.sum[0], 31);
+    // not by differences: what comes behind a NaN must not reach what is in front of it
+    const double before = __shfl_up_sync(0xffffffffu, all, 1);
+    if (lane) {
+        s.sum[0] += before;
+        s.sum[1] = all;
+    }
     return s;
 }
-__device__ __forceinline__ double sum_at(const HeadSteps &s, int step)
+__device__ __forceinline__ double sum_at(const HeadSteps &s, int step) { return __shfl_sync(0xffffffffu, s.sum[step & 1], step >> 1); }
+// ex2.approx: 2 units in the last place; results below 2^-126 become zero.
+__device__ __forceinline__ float fast_exp2(float x)
 {
-    return __shfl_sync(0xffffffffu, step < 32 ? s.sum[0] : s.sum[1], step & 31);
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
-__device__ __forceinline__ float pow2(double x) { return exp2f(static_cast<float>(x)); }
+__device__ __forceinline__ float pow2(double x) { return fast_exp2(static_cast<float>(x)); }
 
 // What a CTA works on.
 struct HeadPlace {
@@ -426,10 +463,10 @@ __device__ __forceinline__ HeadPlace head_place(const HeadParams &p, int segment
     return a;
 }
 
-// state[p][n] <- decay state + sum_j f_j x_j[p] z_j[n] over a chunk, for 16 columns p0 ..; x and z are tiles [step][..].  The factors make
-// x an operand of more than 16 bits: it goes in in parts.
-template <int NP, typename T>
-__device__ __forceinline__ void state_update(float (&S)[NP / 8][4], const T *x, const T *z, const float *f, float decay, int p0, int lane)
+// state[p][n] <- decay state + sum_j f_j x_j[p] z_j[n] over a chunk, for 16 columns p0 .. and 8 kN states n0 ..; x and z are tiles
+// [step][..].  The factors make x an operand of more than 16 bits: it goes in in parts.
+template <int NP, int kN, typename T>
+__device__ __forceinline__ void state_update(float (&S)[kN][4], const T *x, const T *z, const float *f, float decay, int p0, int n0, int lane)
 {
     constexpr int kXP = kHeadCols + kHeadPad, kZP = NP + kHeadPad;
     const int t = lane & 3;
@@ -438,15 +475,14 @@ __device__ __forceinline__ void state_update(float (&S)[NP / 8][4], const T *x, 
     for (int k = 0; k < kHeadSteps / 16; ++k) a[k] = load_a_t(x, kXP, p0, 16 * k, lane);
     HeadScale sc = {1.0f, 1.0f};
     if constexpr (kScaled<T>) {
-        float top = 0.0f, ftop = fmaxf(finite_abs(f[lane]), finite_abs(f[lane + 32]));
+        __half2 most = __float2half2_rn(0.0f);
 #pragma unroll
         for (int k = 0; k < kHeadSteps / 16; ++k)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 v = head_unpack<T>(a[k].r[i]);
-                top = fmaxf(top, fmaxf(finite_abs(v.x), finite_abs(v.y)));
-            }
-        sc = scale_for(warp_max(top) * warp_max(ftop));
+            for (int i = 0; i < 4; ++i) most = __hmax2(most, __habs2(*reinterpret_cast<const __half2 *>(&a[k].r[i])));
+        const float2 v = __half22float2(most), q = *reinterpret_cast<const float2 *>(f + 2 * lane);
+        const float top = fminf(fmaxf(v.x, v.y), 65504.0f);            // an infinity: as large as a finite value can be
+        sc = scale_for(warp_max(top) * warp_max(fmaxf(finite_abs(q.x), finite_abs(q.y))));
     }
     // the chunk's sums on their own, joined with the state in binary32: the tensor cores' sums are cut off, not rounded
     HeadA<T> part[kHeadSteps / 16][kHeadParts<T>];
@@ -468,12 +504,12 @@ __device__ __forceinline__ void state_update(float (&S)[NP / 8][4], const T *x, 
         }
     }
 #pragma unroll
-    for (int n = 0; n < NP / 16; ++n) {
+    for (int n = 0; n < kN / 2; ++n) {
         float sum[2][4] = {};
 #pragma unroll
         for (int k = 0; k < kHeadSteps / 16; ++k) {
             HeadB<T> b[2];
-            load_b_t(b, z, kZP, 16 * n, 16 * k, lane);
+            load_b_t(b, z, kZP, n0 + 16 * n, 16 * k, lane);
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -486,75 +522,54 @@ __device__ __forceinline__ void state_update(float (&S)[NP / 8][4], const T *x, 
     }
 }
 
-// A warp's 16 columns of a state in memory [cols][states]: rows p0 + g and p0 + g + 8, columns 8 n + 2 t of it.
-template <int NP, class Fn>
-__device__ __forceinline__ void for_state(int p0, int cols, int states, int lane, Fn fn)
+// A warp's part of a state in memory [cols][states]: rows p0 + g and p0 + g + 8, columns n0 + 8 n + 2 t of it.
+template <int kN, class Fn>
+__device__ __forceinline__ void for_state(int p0, int n0, int cols, int states, int lane, Fn fn)
 {
     const int g = lane >> 2, t = lane & 3;
 #pragma unroll
-    for (int n = 0; n < NP / 8; ++n)
+    for (int n = 0; n < kN; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int p = p0 + g + (i >> 1) * 8, c = 8 * n + 2 * t + (i & 1);
+            const int p = p0 + g + (i >> 1) * 8, c = n0 + 8 * n + 2 * t + (i & 1);
             fn(n, i, p < cols && c < states, static_cast<int64_t>(p) * states + c);
         }
 }
-template <int NP>
-__device__ __forceinline__ void read_state(float (&S)[NP / 8][4], const float *from, int p0, int cols, int states, int lane)
+template <int kN>
+__device__ __forceinline__ void read_state(float (&S)[kN][4], const float *from, int p0, int n0, int cols, int states, int lane)
 {
     if (states % 2 == 0 && (reinterpret_cast<uintptr_t>(from) & 7) == 0) {
         const int g = lane >> 2, t = lane & 3;
 #pragma unroll
-        for (int n = 0; n < NP / 8; ++n)
+        for (int n = 0; n < kN; ++n)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int p = p0 + g + 8 * i, c = 8 * n + 2 * t;
+                const int p = p0 + g + 8 * i, c = n0 + 8 * n + 2 * t;
                 float2 v = make_float2(0.0f, 0.0f);
                 if (from && p < cols && c < states) v = *reinterpret_cast<const float2 *>(from + static_cast<int64_t>(p) * states + c);
                 S[n][2 * i] = v.x;
                 S[n][2 * i + 1] = v.y;
             }
     } else {
-        for_state<NP>(p0, cols, states, lane, [&](int n, int i, bool on, int64_t at) { S[n][i] = on && from ? from[at] : 0.0f; });
+        for_state<kN>(p0, n0, cols, states, lane, [&](int n, int i, bool on, int64_t at) { S[n][i] = on && from ? from[at] : 0.0f; });
     }
 }
-template <int NP>
-__device__ __forceinline__ void write_state(const float (&S)[NP / 8][4], float *to, int p0, int cols, int states, int lane)
+template <int kN>
+__device__ __forceinline__ void write_state(const float (&S)[kN][4], float *to, int p0, int n0, int cols, int states, int lane)
 {
     if (states % 2 == 0 && (reinterpret_cast<uintptr_t>(to) & 7) == 0) {
         const int g = lane >> 2, t = lane & 3;
 #pragma unroll
-        for (int n = 0; n < NP / 8; ++n)
+        for (int n = 0; n < kN; ++n)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int p = p0 + g + 8 * i, c = 8 * n + 2 * t;
+                const int p = p0 + g + 8 * i, c = n0 + 8 * n + 2 * t;
                 if (p < cols && c < states) *reinterpret_cast<float2 *>(to + static_cast<int64_t>(p) * states + c) = make_float2(S[n][2 * i], S[n][2 * i + 1]);
             }
     } else {
-        for_state<NP>(p0, cols, states, lane, [&](int n, int i, bool on, int64_t at) {
+        for_state<kN>(p0, n0, cols, states, lane, [&](int n, int i, bool on, int64_t at) {
             if (on) to[at] = S[n][i];
         });
-    }
-}
-
-// A warp's 16 x 64 results from its staging (rows of kHeadCols + 8 elements) to rows of a tensor; token(r): the row's place, or -1.
-template <typename T, class Fn>
-__device__ __forceinline__ void store_rows(const T *stage, T *to, int64_t row_pitch, int cols, int unit, int lane, Fn token)
-{
-    constexpr int kPitch = kHeadCols + kHeadPad;
-    if (unit == 16) {
-        constexpr int kElems = 16 / static_cast<int>(sizeof(T)), kRow = kHeadCols / kElems;
-        for (int i = lane; i < 16 * kRow; i += 32) {
-            const int r = i / kRow, c = i % kRow * kElems;
-            const int64_t at = token(r);
-            if (at >= 0 && c < cols) *reinterpret_cast<uint4 *>(to + at * row_pitch + c) = *reinterpret_cast<const uint4 *>(stage + r * kPitch + c);
-        }
-    } else {
-        for (int r = 0; r < 16; ++r) {
-            const int64_t at = token(r);
-            if (at < 0) continue;
-            for (int c = lane; c < cols; c += 32) to[at * row_pitch + c] = stage[r * kPitch + c];
-        }
     }
 }
 
@@ -565,45 +580,90 @@ enum HeadMode {
     kHeadGradSum,                     // what a segment's outputs add to the gradient of the state in front of it, and its decay
 };
 
-// Shared memory of the forward kernel, in bytes: two stages of tiles (C, B, u; sums: one of B and C, and u or dy), the state as an
-// operand, staging of the outputs, factors of the steps for each warp, powers of two of the state's columns.
+// Factors of a chunk's steps, which one warp forms for all, a chunk ahead.  The sums refer to the step in front of each 16 steps r.
+struct HeadFactors {
+    float state[kHeadSteps];          // of an input in the state behind the chunk (gradients: of an output in the one in front)
+    float w[kHeadSteps];
+    float into[kHeadSteps];           // e^{L}
+    float pair[4][kHeadSteps];        // for the 16 steps r: of the steps in front of them e^{L_ref - L_j} w_j, of themselves log2 e^{L_j - L_ref}
+    float decay, log_decay;           // of the chunk, log2 of it
+    float pad[2];
+};
+template <int kMode>
+__device__ __forceinline__ void write_factors(HeadFactors &f, const HeadSteps &st, int lane)
+{
+    const double all = __shfl_sync(0xffffffffu, st.sum[1], 31);
+    float2 *to = reinterpret_cast<float2 *>(&f) + lane;
+    constexpr int kRow = kHeadSteps / 2;
+    if constexpr (kMode == kHeadGradSum)
+        to[0] = make_float2(pow2(st.sum[0]), pow2(st.sum[1]));
+    else
+        to[0] = make_float2(pow2(all - st.sum[0]) * st.w[0], pow2(all - st.sum[1]) * st.w[1]);
+    if constexpr (kMode == kHeadForward) {
+        to[kRow] = make_float2(st.w[0], st.w[1]);
+        to[2 * kRow] = make_float2(pow2(st.sum[0]), pow2(st.sum[1]));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const double ref = r ? __shfl_sync(0xffffffffu, st.sum[1], 8 * r - 1) : 0.0;
+            to[(3 + r) * kRow] = lane < 8 * r ? make_float2(pow2(ref - st.sum[0]) * st.w[0], pow2(ref - st.sum[1]) * st.w[1])
+                                              : make_float2(static_cast<float>(st.sum[0] - ref), static_cast<float>(st.sum[1] - ref));
+        }
+    }
+    if (lane == 0) {
+        f.decay = pow2(all);
+        f.log_decay = static_cast<float>(all);
+    }
+}
+
+// Shared memory of the forward kernel, in bytes: two stages of tiles (u, B, C; sums: u or dy, and one of B and C), the state as an
+// operand, factors of two chunks, largest magnitudes of the state's parts.
 template <typename T, int NP, int kMode>
 struct HeadSmem {
     static constexpr int kWide = kHeadSteps * (NP + kHeadPad) * static_cast<int>(sizeof(T));
     static constexpr int kNarrow = kHeadSteps * (kHeadCols + kHeadPad) * static_cast<int>(sizeof(T));
     static constexpr int kStage = (kMode == kHeadForward ? 2 : 1) * kWide + kNarrow;
-    static constexpr int kStages = 2 * kStage + (kMode == kHeadForward ? kWide + kNarrow : 0) <= 200 * 1024 ? 2 : 1;
-    // a warp's rows of C are its own: its outputs go over them where they fit
-    static constexpr bool kOverC = NP >= kHeadCols;
+    static constexpr int kStages = 2 * kStage + (kMode == kHeadForward ? kWide : 0) <= 200 * 1024 ? 2 : 1;
     static constexpr int kState = kStages * kStage;
-    static constexpr int kStaging = kState + (kMode == kHeadForward ? kWide : 0);
-    static constexpr int kFactors = kStaging + (kMode == kHeadForward && !kOverC ? kNarrow : 0);
-    static constexpr int kPowers = kFactors + 4 * 4 * kHeadSteps * 4;
-    static constexpr int kBytes = kPowers + 16;
+    static constexpr int kFactors = kState + (kMode == kHeadForward ? kWide : 0);
+    static constexpr int kTops = kFactors + 2 * static_cast<int>(sizeof(HeadFactors));
+    static constexpr int kBytes = kTops + 2 * 8 * 4;
 };
 
+// The four lanes of a quad hold two columns each of four 8-column tiles, packed: lane t gets all eight columns of tile t.
+__device__ __forceinline__ void quad_transpose(uint32_t (&r)[4], int t)
+{
+#pragma unroll
+    for (int d = 1; d < 4; d <<= 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (!(i & d)) {
+                const uint32_t send = t & d ? r[i] : r[i + d], got = __shfl_xor_sync(0xffffffffu, send, d);
+                (t & d ? r[i] : r[i + d]) = got;
+            }
+}
+
 template <typename T, int NP, int kMode>
-__global__ void __launch_bounds__(128) ptq_heads_kernel(const HeadParams p)
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(const HeadParams p)
 {
     using M = HeadSmem<T, NP, kMode>;
-    constexpr int kWP = NP + kHeadPad, kXP = kHeadCols + kHeadPad;
+    constexpr int kWP = NP + kHeadPad, kXP = kHeadCols + kHeadPad, kN = NP / 16;         // 8-column tiles of this warp's half of the states
     constexpr bool kOut = kMode == kHeadForward, kGrad = kMode == kHeadGradSum;
     extern __shared__ __align__(128) unsigned char smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    // 16 steps r, and 16 columns of the state; the two warps of a scheduler have few and many scores
+    const int r = warp < 4 ? warp : 7 - warp, half = warp >> 2, p0 = 16 * r, q0 = 32 * half, n0 = half * (NP / 2);
     if (kOut && p.segments > 1) griddep_wait();
     const HeadPlace a = head_place(p, kOut ? p.segments : p.segments - 1);
     const int seg = kGrad ? a.seg + 1 : a.seg;            // sums: of all segments but the last, of gradients: but the first
     const int chunks = (a.n + kHeadSteps - 1) / kHeadSteps;
     const int chunk0 = min(chunks, seg * p.segment_chunks), chunk1 = min(chunks, chunk0 + p.segment_chunks);
     const bool reverse = p.flags & kHeadsReverse;
-    const int p0 = 16 * warp;                             // this warp's columns of the state, and its steps of a chunk
     const auto tile_u = [&](int s) { return reinterpret_cast<T *>(smem + (M::kStages == 2 ? s * M::kStage : 0)); };
     const auto tile_B = [&](int s) { return reinterpret_cast<T *>(smem + (M::kStages == 2 ? s * M::kStage : 0) + M::kNarrow); };
     const auto tile_C = [&](int s) { return reinterpret_cast<T *>(smem + (M::kStages == 2 ? s * M::kStage : 0) + M::kNarrow + M::kWide); };
     T *state_s = reinterpret_cast<T *>(smem + M::kState);
-    float *factors = reinterpret_cast<float *>(smem + M::kFactors) + warp * 4 * kHeadSteps;
-    float *vF = factors, *vC = factors + kHeadSteps, *vW = factors + 2 * kHeadSteps, *vR = factors + 3 * kHeadSteps;
-    float *powers = reinterpret_cast<float *>(smem + M::kPowers);
+    HeadFactors *factors = reinterpret_cast<HeadFactors *>(smem + M::kFactors);
+    float *all_tops = reinterpret_cast<float *>(smem + M::kTops);      // of two chunks: a warp may be one ahead
 
     const T *u = static_cast<const T *>(kGrad ? p.dy : p.u) +
                  (kGrad ? (static_cast<int64_t>(a.b) * p.length * p.heads + a.h) * p.cols : a.b * p.u_b + a.h * p.u_h) + a.tile * kHeadCols;
@@ -614,20 +674,34 @@ __global__ void __launch_bounds__(128) ptq_heads_kernel(const HeadParams p)
     const int64_t delta_at = a.b * p.delta_b + a.h * p.delta_h;
     const float bias = p.delta_bias ? __ldg(p.delta_bias + a.h) : 0.0f, skip = p.D ? __ldg(p.D + a.h) : 0.0f;
     const double A2 = static_cast<double>(__ldg(p.A + a.h)) * kLog2e;
+    const int64_t y_l = static_cast<int64_t>(p.heads) * p.cols;
+    T *y_at = static_cast<T *>(p.y) + (static_cast<int64_t>(a.b) * p.length * p.heads + a.h) * p.cols + a.tile * kHeadCols;
 
     const auto token = [&](int step) { return reverse ? a.n - 1 - step : step; };
     const auto load = [&](int chunk, int s) {
         const int first = chunk * kHeadSteps, rows = a.n - first;
         const int64_t sign = reverse ? -1 : 1, at = token(first);
-        load_rows<kHeadCols, 128>(tile_u(s), u + at * u_l, sign * u_l, rows, a.cols, p.unit);
-        load_rows<NP, 128>(tile_B(s), B + at * B_l, sign * B_l, rows, p.states, p.unit);
-        if (kOut) load_rows<NP, 128>(tile_C(s), C + at * p.C_l, sign * p.C_l, rows, p.states, p.unit);
+        load_rows<kHeadCols, 256>(tile_u(s), u + at * u_l, sign * u_l, rows, a.cols, p.unit);
+        load_rows<NP, 256>(tile_B(s), B + at * B_l, sign * B_l, rows, p.states, p.unit);
+        if (kOut) load_rows<NP, 256>(tile_C(s), C + at * p.C_l, sign * p.C_l, rows, p.states, p.unit);
         cp_async_commit();
     };
 
     const int64_t head_at = (static_cast<int64_t>(a.b) * p.heads + a.h);
     const int64_t state_size = static_cast<int64_t>(p.cols) * p.states, tile_at = static_cast<int64_t>(a.tile) * kHeadCols * p.states;
-    float S[NP / 8][4];
+    const int count = chunk1 - chunk0;
+    const auto chunk_of = [&](int i) { return kGrad ? chunk1 - 1 - i : chunk0 + i; };
+    // Warp i % 8 forms the factors of chunk i + 1 while chunk i is worked on; it has read delta a chunk before that.
+    float delta[2] = {};
+    if (count > 0) {
+        load(chunk_of(0), 0);
+        if (warp == 0) {
+            load_delta<T>(p, delta_at, chunk_of(0) * kHeadSteps, a.n, lane, delta);
+            write_factors<kMode>(factors[0], head_steps(p, delta, bias, A2, chunk_of(0) * kHeadSteps, a.n, lane), lane);
+            if (count > 1) load_delta<T>(p, delta_at, chunk_of(1) * kHeadSteps, a.n, lane, delta);
+        }
+    }
+    float S[kN][4];
     {
         const float *from = nullptr;
         // with segments the first one's start is a copy: the last one may be writing final_state over it
@@ -635,108 +709,89 @@ __global__ void __launch_bounds__(128) ptq_heads_kernel(const HeadParams p)
             from = p.slots + (head_at * p.segments + (seg > 0 ? seg : p.segments) - 1) * state_size + tile_at;
         else if (kOut && p.state)
             from = p.state + head_at * state_size + tile_at;
-        read_state<NP>(S, from, p0, a.cols, p.states, lane);
+        read_state<kN>(S, from, p0, n0, a.cols, p.states, lane);
     }
+    const bool started = kOut && (seg > 0 || p.state);    // else the state in front of the first chunk is zero
     double log_decay = 0.0;
-    const int count = chunk1 - chunk0;
-    const auto chunk_of = [&](int i) { return kGrad ? chunk1 - 1 - i : chunk0 + i; };
-    float delta[2] = {};
-    if (count > 0) {
-        load(chunk_of(0), 0);
-        load_delta<T>(p, delta_at, chunk_of(0) * kHeadSteps, a.n, lane, delta);
-    }
     for (int i = 0; i < count; ++i) {
         const int chunk = chunk_of(i), first = chunk * kHeadSteps, s = i & 1;
         const bool busy = p0 < a.cols;                    // this warp has columns of the state
-        HeadScale state_scale = {1.0f, 1.0f};
+        float *tops = all_tops + 8 * s;
         if (kOut) {
             if (p.history && busy)
-                write_state<NP>(S, p.history + ((static_cast<int64_t>(a.b) * p.chunks + chunk) * p.heads + a.h) * state_size + tile_at, p0, a.cols, p.states, lane);
-            if (i > 0) __syncthreads();                   // everyone is done with the state in front of the last chunk
+                write_state<kN>(S, p.history + ((static_cast<int64_t>(a.b) * p.chunks + chunk) * p.heads + a.h) * state_size + tile_at, p0, n0, a.cols, p.states, lane);
+            float up = 1.0f;
             if constexpr (kScaled<T>) {
-                float top = 0.0f;
-#pragma unroll
-                for (int n = 0; n < NP / 8; ++n)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) top = fmaxf(top, finite_abs(S[n][k]));
-                state_scale = scale_for(warp_max(top));
-                if (lane == 0) powers[warp] = state_scale.down;
+                const float top = warp_top<kN>(S);
+                if (lane == 0) tops[2 * r + half] = top;
             }
+            if (kScaled<T> || i > 0) __syncthreads();     // everyone is done with the state in front of the last chunk
+            if constexpr (kScaled<T>) up = scale_for(fmaxf(tops[2 * r], tops[2 * r + 1])).up;
 #pragma unroll
-            for (int n = 0; n < NP / 8; ++n) {
-                head_store_pair(state_s + (p0 + g) * kWP + 8 * n + 2 * t, S[n][0] * state_scale.up, S[n][1] * state_scale.up);
-                head_store_pair(state_s + (p0 + g + 8) * kWP + 8 * n + 2 * t, S[n][2] * state_scale.up, S[n][3] * state_scale.up);
+            for (int n = 0; n < kN; ++n) {
+                head_store_pair(state_s + (p0 + g) * kWP + n0 + 8 * n + 2 * t, S[n][0] * up, S[n][1] * up);
+                head_store_pair(state_s + (p0 + g + 8) * kWP + n0 + 8 * n + 2 * t, S[n][2] * up, S[n][3] * up);
             }
         }
-        const HeadSteps st = head_steps(p, delta, bias, A2, first, a.n, lane);
         cp_async_wait<0>();
-        __syncthreads();                                  // the tiles, and the state as an operand
+        __syncthreads();                                  // the tiles, their steps' factors, and the state as an operand
         if (M::kStages == 2 && i + 1 < count) load(chunk_of(i + 1), s ^ 1);
-        if (i + 1 < count) load_delta<T>(p, delta_at, chunk_of(i + 1) * kHeadSteps, a.n, lane, delta);
-
-        // factors of the steps
-        const double all = sum_at(st, 63), ref = warp ? sum_at(st, 16 * warp - 1) : 0.0;
-        __syncwarp();
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int j = lane + 32 * k;
-            vF[j] = kGrad ? pow2(st.sum[k]) : pow2(all - st.sum[k]) * st.w[k];
-            if (kOut) {
-                vC[j] = j < 16 * warp ? pow2(ref - st.sum[k]) * st.w[k] : static_cast<float>(st.sum[k] - ref);
-                vW[j] = st.w[k];
-                vR[j] = pow2(st.sum[k]);
-            }
-        }
-        __syncwarp();
-        const float decay = pow2(all);
-        log_decay += all;
+        if (warp == ((i + 1) & 7) && i + 2 < count) load_delta<T>(p, delta_at, chunk_of(i + 2) * kHeadSteps, a.n, lane, delta);
+        const HeadFactors &f = factors[s];
+        const float decay = f.decay;
+        log_decay += f.log_decay;
 
         if constexpr (kOut) {
-            // scores of this warp's 16 steps with all up to them, and what the state gives
-            float m[8][4] = {}, y[8][4] = {};
+            // scores of these 16 steps with all up to them, and what the state gives
+            float m[8][4] = {}, y[4][4] = {};
 #pragma unroll
             for (int k = 0; k < NP / 16; ++k) {
                 const HeadA<T> c = load_a(tile_C(s), kWP, p0, 16 * k, lane);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (j <= warp) {
+                    if (j <= r) {
                         HeadB<T> b[2];
                         load_b(b, tile_B(s), kWP, 16 * j, 16 * k, lane);
                         head_mma(m[2 * j], c, b[0]);
                         head_mma(m[2 * j + 1], c, b[1]);
                     }
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (16 * j < a.cols) {
+                for (int j = 0; j < 2; ++j)
+                    if (q0 + 16 * j < a.cols) {
                         HeadB<T> b[2];
-                        load_b(b, state_s, kWP, 16 * j, 16 * k, lane);
+                        load_b(b, state_s, kWP, q0 + 16 * j, 16 * k, lane);
                         head_mma(y[2 * j], c, b[0]);
                         head_mma(y[2 * j + 1], c, b[1]);
                     }
             }
-            const float l0 = vC[p0 + g], l1 = vC[p0 + g + 8], r0 = exp2f(l0), r1 = exp2f(l1);
-            float top = 0.0f;
+            const float *pair = f.pair[r];
+            const float l0 = pair[p0 + g], l1 = pair[p0 + g + 8], r0 = fast_exp2(l0), r1 = fast_exp2(l1);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (j / 2 <= warp) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int col = 8 * j + 2 * t + (k & 1);
-                        if (j / 2 < warp) {
-                            m[j][k] *= (k < 2 ? r0 : r1) * vC[col];
-                        } else {
-                            const bool on = col <= p0 + g + (k < 2 ? 0 : 8);
-                            m[j][k] = on ? m[j][k] * (exp2f((k < 2 ? l0 : l1) - vC[col]) * vW[col]) : 0.0f;
-                        }
-                        if constexpr (kScaled<T>) top = fmaxf(top, finite_abs(m[j][k]));
+                if (j / 2 <= r) {
+                    const int col = 8 * j + 2 * t;
+                    const float2 v = *reinterpret_cast<const float2 *>(pair + col);
+                    if (j / 2 < r) {
+                        m[j][0] *= r0 * v.x;
+                        m[j][1] *= r0 * v.y;
+                        m[j][2] *= r1 * v.x;
+                        m[j][3] *= r1 * v.y;
+                    } else {
+                        const float2 w = *reinterpret_cast<const float2 *>(f.w + col);
+                        const int row = p0 + g;
+                        m[j][0] = col <= row ? m[j][0] * (fast_exp2(l0 - v.x) * w.x) : 0.0f;
+                        m[j][1] = col + 1 <= row ? m[j][1] * (fast_exp2(l0 - v.y) * w.y) : 0.0f;
+                        m[j][2] = col <= row + 8 ? m[j][2] * (fast_exp2(l1 - v.x) * w.x) : 0.0f;
+                        m[j][3] = col + 1 <= row + 8 ? m[j][3] * (fast_exp2(l1 - v.y) * w.y) : 0.0f;
                     }
                 }
             HeadScale sc = {1.0f, 1.0f};
-            if constexpr (kScaled<T>) sc = scale_for(warp_max(top));
-            const float R0 = vR[p0 + g] * sc.up, R1 = vR[p0 + g + 8] * sc.up;
+            if constexpr (kScaled<T>) sc = scale_for(warp_top<8>(m));
+            const float R0 = f.into[p0 + g] * sc.up, R1 = f.into[p0 + g + 8] * sc.up;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float down = kScaled<T> ? powers[j / 2] : 1.0f;
+            for (int j = 0; j < 4; ++j) {
+                const int from = 2 * (2 * half + j / 2);   // the 16 columns of the state that these belong to
+                const float down = kScaled<T> ? scale_for(fmaxf(tops[from], tops[from + 1])).down : 1.0f;
                 y[j][0] *= R0 * down;
                 y[j][1] *= R0 * down;
                 y[j][2] *= R1 * down;
@@ -744,13 +799,13 @@ __global__ void __launch_bounds__(128) ptq_heads_kernel(const HeadParams p)
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (j <= warp) {
+                if (j <= r) {
                     const HeadA<T> w = acc_to_a<T>(m[2 * j], m[2 * j + 1], sc.up);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (16 * q < a.cols) {
+                    for (int q = 0; q < 2; ++q)
+                        if (q0 + 16 * q < a.cols) {
                             HeadB<T> b[2];
-                            load_b_t(b, tile_u(s), kXP, 16 * q, 16 * j, lane);
+                            load_b_t(b, tile_u(s), kXP, q0 + 16 * q, 16 * j, lane);
                             head_mma(y[2 * q], w, b[0]);
                             head_mma(y[2 * q + 1], w, b[1]);
                         }
@@ -758,60 +813,69 @@ __global__ void __launch_bounds__(128) ptq_heads_kernel(const HeadParams p)
             // Columns of later steps have the factor zero; where u is not finite there, zero times it is not zero.
             float odd = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) odd = fmaf(y[j][k], 0.0f, odd);
-            const bool again = __any_sync(0xffffffffu, odd != 0.0f);
-            T *stage = M::kOverC ? tile_C(s) + p0 * kWP : reinterpret_cast<T *>(smem + M::kStaging) + p0 * kXP;
-            __syncwarp();
-            if (!again) {
-                // over this warp's rows of C, which nobody else reads
+            const int step0 = first + p0 + g, step1 = step0 + 8;
+            if (!__any_sync(0xffffffffu, odd != 0.0f)) {
+                uint32_t out[2][4];
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
+                for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        const int r = g + 8 * k, c = 8 * j + 2 * t;
-                        const float2 v = head_pair(tile_u(s) + (p0 + r) * kXP + c);
-                        head_store_pair(stage + r * kXP + c, fmaf(skip, p.D ? v.x : 0.0f, y[j][2 * k] * sc.down), fmaf(skip, p.D ? v.y : 0.0f, y[j][2 * k + 1] * sc.down));
+                        const int c = q0 + 8 * j + 2 * t, step = k ? step1 : step0;
+                        float v0 = y[j][2 * k] * sc.down, v1 = y[j][2 * k + 1] * sc.down;
+                        if (p.D) {
+                            const float2 x = head_pair(tile_u(s) + (p0 + g + 8 * k) * kXP + c);
+                            v0 = fmaf(skip, x.x, v0);
+                            v1 = fmaf(skip, x.y, v1);
+                        }
+                        if constexpr (sizeof(T) == 2) out[k][j] = head_pack<T>(v0, v1);
+                        if (sizeof(T) == 4 || p.out_unit < 16) {
+                            if (step >= a.n || c >= a.cols) continue;
+                            T *to = y_at + token(step) * y_l + c;
+                            if (p.out_unit >= 2 * static_cast<int>(sizeof(T))) {
+                                head_store_pair(to, v0, v1);
+                            } else {
+                                to[0] = head_round<T>(v0);
+                                if (c + 1 < a.cols) to[1] = head_round<T>(v1);
+                            }
+                        }
                     }
+                if (sizeof(T) == 2 && p.out_unit == 16) {  // 16 bytes of a row a lane
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        quad_transpose(out[k], t);
+                        const int c = q0 + 8 * t, step = k ? step1 : step0;
+                        if (step < a.n && c < a.cols)
+                            *reinterpret_cast<uint4 *>(y_at + token(step) * y_l + c) = make_uint4(out[k][0], out[k][1], out[k][2], out[k][3]);
+                    }
+                }
             } else {
-                // Step by step from shared memory: only what is there enters.  A lane has two columns.  Row r of the staging ends in front
-                // of row r + 1 of C: in this order nothing is staged over what is still read.
-                for (int r = 0; r < 16; ++r) {
-                    const int row = p0 + r;
-                    const double to = sum_at(st, row);
-                    float out[2] = {};
+                // Step by step from shared memory: only what is there enters.  A lane has a column.
+                const int col = q0 + lane;
+                const float down = kScaled<T> ? scale_for(fmaxf(tops[col / 16 * 2], tops[col / 16 * 2 + 1])).down : 1.0f;
+                for (int row = p0; row < p0 + 16; ++row) {
                     const T *c = tile_C(s) + row * kWP;
-                    for (int q = 0; q < 2; ++q) {
-                        const int col = lane + 32 * q;
-                        float v = 0.0f;
-                        for (int n = 0; n < p.states; ++n) v = fmaf(head_f32(c[n]), head_f32(state_s[col * kWP + n]), v);
-                        out[q] = (i > 0 || seg > 0 || p.state) ? v * vR[row] * (kScaled<T> ? powers[col / 16] : 1.0f) : 0.0f;
-                    }
+                    float v = 0.0f;
+                    for (int n = 0; n < p.states; ++n) v = fmaf(head_f32(c[n]), head_f32(state_s[col * kWP + n]), v);
+                    v = i > 0 || started ? v * f.into[row] * down : 0.0f;
                     for (int j = 0; j <= row; ++j) {
                         float score = 0.0f;
                         for (int n = lane; n < p.states; n += 32) score = fmaf(head_f32(c[n]), head_f32(tile_B(s)[j * kWP + n]), score);
 #pragma unroll
                         for (int d = 16; d > 0; d >>= 1) score += __shfl_xor_sync(0xffffffffu, score, d);
-                        score *= pow2(to - sum_at(st, j)) * vW[j];
-                        for (int q = 0; q < 2; ++q) out[q] = fmaf(score, head_f32(tile_u(s)[j * kXP + lane + 32 * q]), out[q]);
+                        score *= j < p0 ? fast_exp2(pair[row]) * pair[j] : fast_exp2(pair[row] - pair[j]) * f.w[j];
+                        v = fmaf(score, head_f32(tile_u(s)[j * kXP + col]), v);
                     }
-                    __syncwarp();
-                    for (int q = 0; q < 2; ++q) {
-                        if (p.D) out[q] = fmaf(skip, head_f32(tile_u(s)[row * kXP + lane + 32 * q]), out[q]);
-                        stage[r * kXP + lane + 32 * q] = head_round<T>(out[q]);
-                    }
-                    __syncwarp();
+                    if (p.D) v = fmaf(skip, head_f32(tile_u(s)[row * kXP + col]), v);
+                    if (first + row < a.n && col < a.cols) y_at[token(first + row) * y_l + col] = head_round<T>(v);
                 }
             }
-            __syncwarp();
-            T *y_at = static_cast<T *>(p.y) + (static_cast<int64_t>(a.b) * p.length * p.heads + a.h) * p.cols + a.tile * kHeadCols;
-            store_rows(stage, y_at, static_cast<int64_t>(p.heads) * p.cols, a.cols, p.out_unit, lane, [&](int r) -> int64_t {
-                const int step = first + p0 + r;
-                return step < a.n ? token(step) : -1;
-            });
         }
-        if (busy) state_update<NP>(S, tile_u(s), tile_B(s), vF, decay, p0, lane);
+        if (busy) state_update<NP, kN>(S, tile_u(s), tile_B(s), f.state, decay, p0, n0, lane);
+        if (warp == (i & 7) && i + 1 < count)
+            write_factors<kMode>(factors[s ^ 1], head_steps(p, delta, bias, A2, chunk_of(i + 1) * kHeadSteps, a.n, lane), lane);
         if (M::kStages == 1 && i + 1 < count) {
             __syncthreads();
             load(chunk_of(i + 1), 0);
@@ -820,9 +884,9 @@ __global__ void __launch_bounds__(128) ptq_heads_kernel(const HeadParams p)
     if constexpr (kOut) {
         // final states: by the segment that holds the last step, or the first one of an empty sequence
         if (p.final_state && seg == (chunks > 0 ? (chunks - 1) / p.segment_chunks : 0))
-            write_state<NP>(S, p.final_state + head_at * state_size + tile_at, p0, a.cols, p.states, lane);
+            write_state<kN>(S, p.final_state + head_at * state_size + tile_at, p0, n0, a.cols, p.states, lane);
     } else {
-        write_state<NP>(S, p.slots + (head_at * p.segments + seg) * state_size + tile_at, p0, a.cols, p.states, lane);
+        write_state<kN>(S, p.slots + (head_at * p.segments + seg) * state_size + tile_at, p0, n0, a.cols, p.states, lane);
         if (threadIdx.x == 0 && a.tile == 0) p.logs[head_at * p.segments + seg] = static_cast<float>(log_decay);
         griddep_launch_dependents();
     }

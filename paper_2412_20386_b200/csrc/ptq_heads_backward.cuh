@@ -205,13 +205,13 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
             from = p.slots + (head_at * p.segments + a.seg + 1) * state_size + tile_at;
         else if (p.dfinal)
             from = p.dfinal + head_at * state_size + tile_at;
-        read_state<NP>(H, from, p0, a.cols, p.states, lane);
+        read_state<NP / 8>(H, from, p0, 0, a.cols, p.states, lane);
     }
     float delta[2] = {};
     if (chunk1 > chunk0) {
         load(chunk1 - 1, 0);
         load_delta<T>(p, delta_at, (chunk1 - 1) * kHeadSteps, a.n, lane, delta);
-        if (!rows_i) read_state<NP>(H, kept(chunk1 - 1), p0, a.cols, p.states, lane);
+        if (!rows_i) read_state<NP / 8>(H, kept(chunk1 - 1), p0, 0, a.cols, p.states, lane);
     }
     for (int chunk = chunk1 - 1, s = 0; chunk >= chunk0; --chunk, s ^= 1) {
         const int first = chunk * kHeadSteps;
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
         const double all = sum_at(st, 63), ref = rows_i ? (r ? sum_at(st, 16 * r - 1) : 0.0) : sum_at(st, 16 * r + 15);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const int j = lane + 32 * k;
+            const int j = 2 * lane + k;
             if (warp == 0) {
                 vW[j] = st.w[k];
                 vR[j] = pow2(st.sum[k]);
@@ -249,12 +249,12 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
         if (M::kStages == 2 && chunk > chunk0) load(chunk - 1, s ^ 1);
         if (chunk > chunk0) {
             load_delta<T>(p, delta_at, first - kHeadSteps, a.n, lane, delta);
-            if (!rows_i) read_state<NP>(H, kept(chunk - 1), p0, a.cols, p.states, lane);
+            if (!rows_i) read_state<NP / 8>(H, kept(chunk - 1), p0, 0, a.cols, p.states, lane);
         }
         const int step0 = first + p0 + g, step1 = step0 + 8;
         const float l0 = vC[p0 + g], l1 = vC[p0 + g + 8];
         if (rows_i) {
-            const float r0 = exp2f(l0), r1 = exp2f(l1);
+            const float r0 = fast_exp2(l0), r1 = fast_exp2(l1);
             float m[8][4] = {}, run[2] = {};              // M R w; K w of a row summed up to a column
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
                             if (j < r)
                                 v *= (k < 2 ? r0 : r1) * vC[col] * vW[col];
                             else
-                                v = col <= row ? v * (exp2f((k < 2 ? l0 : l1) - vC[col]) * vW[col]) : 0.0f;
+                                v = col <= row ? v * (fast_exp2((k < 2 ? l0 : l1) - vC[col]) * vW[col]) : 0.0f;
                             P[q][k] = j < r || col <= row ? v * P[q][k] : 0.0f;
                         }
                     // what passes over step `col`: of each row i >= col its sum up to, not with, col
@@ -364,9 +364,9 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
 #pragma unroll
             for (int q = 16; q > 0; q >>= 1) z += __shfl_xor_sync(0xffffffffu, z, q);
             if (lane == 0) through[r] = z * decay;
-            if (p0 < a.cols) state_update<NP>(H, tile_dy(s), tile_C(s), vR, decay, p0, lane);
+            if (p0 < a.cols) state_update<NP, NP / 8>(H, tile_dy(s), tile_C(s), vR, decay, p0, 0, lane);
         } else {
-            const float r0 = exp2f(-l0), r1 = exp2f(-l1);
+            const float r0 = fast_exp2(-l0), r1 = fast_exp2(-l1);
             float mp[8][4] = {}, mr[8][4] = {}, k0 = 0.0f, k1 = 0.0f;          // M P and M R, transposed; column sums of K
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
                         for (int k = 0; k < 4; ++k) {
                             const int col = 16 * i + 8 * q + 2 * t + (k & 1), row = p0 + g + (k < 2 ? 0 : 8);
                             const bool on = i > r || col >= row;
-                            const float f = i > r ? (k < 2 ? r0 : r1) * vC[col] : exp2f(vC[col] - (k < 2 ? l0 : l1));
+                            const float f = i > r ? (k < 2 ? r0 : r1) * vC[col] : fast_exp2(vC[col] - (k < 2 ? l0 : l1));
                             float &vp = mp[2 * i + q][k], &vr = mr[2 * i + q][k];
                             vr = on ? vr * f : 0.0f;
                             const float e = on ? vr * vp : 0.0f;
@@ -495,42 +495,37 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
             double v[2], y[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                v[k] = dot_C[lane + 32 * k];
-                y[k] = static_cast<double>(st.w[k]) * dot_B[lane + 32 * k];
+                v[k] = dot_C[2 * lane + k];
+                y[k] = static_cast<double>(st.w[k]) * dot_B[2 * lane + k];
             }
-            const double y0 = y[0], y1 = y[1];
+            double after = v[0] + v[1], before = y[0] + y[1];
 #pragma unroll
             for (int q = 1; q < 32; q <<= 1) {
-                const double e = __shfl_down_sync(0xffffffffu, v[0], q), f = __shfl_down_sync(0xffffffffu, v[1], q);
-                const double c = __shfl_up_sync(0xffffffffu, y[0], q), d = __shfl_up_sync(0xffffffffu, y[1], q);
-                if (lane + q < 32) {
-                    v[0] += e;
-                    v[1] += f;
-                }
-                if (lane >= q) {
-                    y[0] += c;
-                    y[1] += d;
-                }
+                const double e = __shfl_down_sync(0xffffffffu, after, q), c = __shfl_up_sync(0xffffffffu, before, q);
+                if (lane + q < 32) after += e;
+                if (lane >= q) before += c;
             }
-            v[0] += __shfl_sync(0xffffffffu, v[1], 0);
-            y[1] += __shfl_sync(0xffffffffu, y[0], 31);
-            y[0] -= y0;
-            y[1] -= y1;
+            after = __shfl_down_sync(0xffffffffu, after, 1);
+            before = __shfl_up_sync(0xffffffffu, before, 1);
+            if (lane < 31) v[1] += after;
+            v[0] += v[1];
+            y[1] = (lane ? before : 0.0) + y[0];
+            y[0] = lane ? before : 0.0;
             const double z = static_cast<double>(through[0]) + through[1] + through[2] + through[3];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 v[k] += y[k] + z;
-                for (int q = (lane + 32 * k) / 16; q < 4; ++q) v[k] += pairs[q * kHeadSteps + lane + 32 * k];
+                for (int q = (2 * lane + k) / 16; q < 4; ++q) v[k] += pairs[q * kHeadSteps + 2 * lane + k];
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const int step = first + lane + 32 * k;
-                if (step < a.n) p.part_dt[part_row + token(step)] = make_float2(static_cast<float>(v[k]), dw[lane + 32 * k]);
+                const int step = first + 2 * lane + k;
+                if (step < a.n) p.part_dt[part_row + token(step)] = make_float2(static_cast<float>(v[k]), dw[2 * lane + k]);
             }
         }
     }
     if (rows_i) {
-        if (a.seg == 0 && p.final_state) write_state<NP>(H, p.final_state + head_at * state_size + tile_at, p0, a.cols, p.states, lane);
+        if (a.seg == 0 && p.final_state) write_state<NP / 8>(H, p.final_state + head_at * state_size + tile_at, p0, 0, a.cols, p.states, lane);
 #pragma unroll
         for (int q = 16; q > 0; q >>= 1) skip_grad += __shfl_xor_sync(0xffffffffu, skip_grad, q);
         if (lane == 0) skip_sum[r] = skip_grad;

@@ -36,8 +36,8 @@ ptq_status_t HeadsLaunch<T>::chunks(int mode, const ptq::HeadParams &p, bool nex
             PTQ_TRY(ensure_smem<kKern>(kBytes));
             const long long ctas = static_cast<long long>(p.batch) * p.heads * p.col_tiles * (kMode == ptq::kHeadForward ? p.segments : p.segments - 1);
             const dim3 grid(static_cast<unsigned>(ctas));
-            if (next) return launch_next(kKern, grid, 128, kBytes, stream, p);
-            kKern<<<grid, 128, kBytes, stream>>>(p);
+            if (next) return launch_next(kKern, grid, 256, kBytes, stream, p);
+            kKern<<<grid, 256, kBytes, stream>>>(p);
             return launched();
         };
         if (mode == ptq::kHeadForward) return go(std::integral_constant<int, ptq::kHeadForward>());
