@@ -68,6 +68,9 @@ struct HeadB<float> { float v[4]; };
 
 constexpr int kHeadPad = 8;           // elements between the rows of a tile in shared memory, against bank conflicts
 
+// Number of this warp, known to the compiler to be the same for all of its lanes.
+__device__ __forceinline__ int head_warp() { return __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x) >> 5, 0); }
+
 __device__ __forceinline__ uint32_t head_smem(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], const void *p)
 {
@@ -319,14 +322,13 @@ __device__ __forceinline__ float warp_top(const float (&d)[N][4])
     }
     return top;
 }
-// The power of two, within 2^-60 .. 2^60, and its inverse.
+// The power of two, within 2^-most .. 2^most, that brings `top` into 2^to .. 2^(to + 1), and its inverse.
 struct HeadScale {
     float up, down;
 };
-__device__ __forceinline__ HeadScale scale_for(float top)
+__device__ __forceinline__ HeadScale scale_for(float top, int to = 13, int most = 60)
 {
-    int e = 13 + 127 - static_cast<int>(__float_as_uint(top) >> 23);           // top = 2^(its exponent - 127) (1 ..)
-    e = top == 0.0f ? 0 : max(-60, min(60, e));
+    const int e = top == 0.0f ? 0 : max(-most, min(most, to + 127 - static_cast<int>(__float_as_uint(top) >> 23)));
     return {__uint_as_float(static_cast<uint32_t>(127 + e) << 23), __uint_as_float(static_cast<uint32_t>(127 - e) << 23)};
 }
 
@@ -473,7 +475,8 @@ __device__ __forceinline__ void state_update(float (&S)[kN][4], const T *x, cons
     HeadA<T> a[kHeadSteps / 16];
 #pragma unroll
     for (int k = 0; k < kHeadSteps / 16; ++k) a[k] = load_a_t(x, kXP, p0, 16 * k, lane);
-    HeadScale sc = {1.0f, 1.0f};
+    // binary16: u is brought to at most 2, the factors to at most 2^13
+    HeadScale scu = {1.0f, 1.0f}, scf = {1.0f, 1.0f};
     if constexpr (kScaled<T>) {
         __half2 most = __float2half2_rn(0.0f);
 #pragma unroll
@@ -481,20 +484,41 @@ __device__ __forceinline__ void state_update(float (&S)[kN][4], const T *x, cons
 #pragma unroll
             for (int i = 0; i < 4; ++i) most = __hmax2(most, __habs2(*reinterpret_cast<const __half2 *>(&a[k].r[i])));
         const float2 v = __half22float2(most), q = *reinterpret_cast<const float2 *>(f + 2 * lane);
-        const float top = fminf(fmaxf(v.x, v.y), 65504.0f);            // an infinity: as large as a finite value can be
-        sc = scale_for(warp_max(top) * warp_max(fmaxf(finite_abs(q.x), finite_abs(q.y))));
+        // of u 2^-15 .. 2^15, which binary16 holds; an infinity counts as the largest finite value
+        scu = scale_for(warp_max(fminf(fmaxf(v.x, v.y), 65504.0f)), 0, 15);
+        scf = scale_for(warp_max(fmaxf(finite_abs(q.x), finite_abs(q.y))));
     }
     // the chunk's sums on their own, joined with the state in binary32: the tensor cores' sums are cut off, not rounded
     HeadA<T> part[kHeadSteps / 16][kHeadParts<T>];
 #pragma unroll
     for (int k = 0; k < kHeadSteps / 16; ++k) {
         const float2 f0 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t), f1 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t + 8);
-        if constexpr (sizeof(T) == 2) {
+        if constexpr (std::is_same<T, __half>::value) {
+            // u f as two binary16 values in binary16 arithmetic: f in two parts, the product with the upper one and what its
+            // rounding left (a fused multiply-add leaves it whole), plus that with the lower one
+            uint32_t fh[2], fl[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                uint32_t r[2];
+                head_split<T>((q ? f1.x : f0.x) * scf.up, (q ? f1.y : f0.y) * scf.up, r);
+                fh[q] = r[0];
+                fl[q] = r[1];
+            }
+            const __half2 up = __float2half2_rn(scu.up);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&a[k].r[i]), up);
+                const __half2 h = *reinterpret_cast<const __half2 *>(&fh[i >> 1]), l = *reinterpret_cast<const __half2 *>(&fl[i >> 1]);
+                const __half2 hi = __hmul2_rn(v, h), lo = __hfma2(v, l, __hfma2(v, h, __hneg2(hi)));
+                part[k][0].r[i] = *reinterpret_cast<const uint32_t *>(&hi);
+                part[k][1].r[i] = *reinterpret_cast<const uint32_t *>(&lo);
+            }
+        } else if constexpr (sizeof(T) == 2) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float2 v = head_unpack<T>(a[k].r[i]), q = i < 2 ? f0 : f1;
                 uint32_t r[kHeadParts<T>];
-                head_split<T>(v.x * (q.x * sc.up), v.y * (q.y * sc.up), r);
+                head_split<T>(v.x * q.x, v.y * q.y, r);
 #pragma unroll
                 for (int j = 0; j < kHeadParts<T>; ++j) part[k][j].r[i] = r[j];
             }
@@ -503,6 +527,7 @@ __device__ __forceinline__ void state_update(float (&S)[kN][4], const T *x, cons
             for (int i = 0; i < 8; ++i) part[k][0].v[i] = a[k].v[i] * (i < 4 ? (i & 1 ? f0.y : f0.x) : (i & 1 ? f1.y : f1.x));
         }
     }
+    const float down = scu.down * scf.down;
 #pragma unroll
     for (int n = 0; n < kN / 2; ++n) {
         float sum[2][4] = {};
@@ -518,7 +543,7 @@ __device__ __forceinline__ void state_update(float (&S)[kN][4], const T *x, cons
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) S[2 * n + j][i] = fmaf(decay, S[2 * n + j][i], sum[j][i] * sc.down);
+            for (int i = 0; i < 4; ++i) S[2 * n + j][i] = fmaf(decay, S[2 * n + j][i], kScaled<T> ? sum[j][i] * down : sum[j][i]);
     }
 }
 
@@ -649,7 +674,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
     constexpr int kWP = NP + kHeadPad, kXP = kHeadCols + kHeadPad, kN = NP / 16;         // 8-column tiles of this warp's half of the states
     constexpr bool kOut = kMode == kHeadForward, kGrad = kMode == kHeadGradSum;
     extern __shared__ __align__(128) unsigned char smem[];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int warp = head_warp(), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     // 16 steps r, and 16 columns of the state; the two warps of a scheduler have few and many scores
     const int r = warp < 4 ? warp : 7 - warp, half = warp >> 2, p0 = 16 * r, q0 = 32 * half, n0 = half * (NP / 2);
     if (kOut && p.segments > 1) griddep_wait();
@@ -742,74 +767,90 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
         log_decay += f.log_decay;
 
         if constexpr (kOut) {
-            // scores of these 16 steps with all up to them, and what the state gives
-            float m[8][4] = {}, y[4][4] = {};
+            // what the state gives these 16 steps
+            float y[4][4] = {};
 #pragma unroll
             for (int k = 0; k < NP / 16; ++k) {
                 const HeadA<T> c = load_a(tile_C(s), kWP, p0, 16 * k, lane);
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j <= r) {
-                        HeadB<T> b[2];
-                        load_b(b, tile_B(s), kWP, 16 * j, 16 * k, lane);
-                        head_mma(m[2 * j], c, b[0]);
-                        head_mma(m[2 * j + 1], c, b[1]);
-                    }
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    if (q0 + 16 * j < a.cols) {
-                        HeadB<T> b[2];
-                        load_b(b, state_s, kWP, q0 + 16 * j, 16 * k, lane);
-                        head_mma(y[2 * j], c, b[0]);
-                        head_mma(y[2 * j + 1], c, b[1]);
-                    }
+                for (int j = 0; j < 2; ++j) {
+                    HeadB<T> b[2];
+                    load_b(b, state_s, kWP, q0 + 16 * j, 16 * k, lane);
+                    head_mma(y[2 * j], c, b[0]);
+                    head_mma(y[2 * j + 1], c, b[1]);
+                }
             }
             const float *pair = f.pair[r];
-            const float l0 = pair[p0 + g], l1 = pair[p0 + g + 8], r0 = fast_exp2(l0), r1 = fast_exp2(l1);
+            const float l0 = pair[p0 + g], l1 = pair[p0 + g + 8];
+            {
+                const float R0 = f.into[p0 + g], R1 = f.into[p0 + g + 8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j / 2 <= r) {
-                    const int col = 8 * j + 2 * t;
+                for (int j = 0; j < 2; ++j) {
+                    const int from = 2 * (2 * half + j);   // the 16 columns of the state that these belong to
+                    const float down = kScaled<T> ? scale_for(fmaxf(tops[from], tops[from + 1])).down : 1.0f;
+#pragma unroll
+                    for (int n = 2 * j; n < 2 * j + 2; ++n) {
+                        y[n][0] *= R0 * down;
+                        y[n][1] *= R0 * down;
+                        y[n][2] *= R1 * down;
+                        y[n][3] *= R1 * down;
+                    }
+                }
+            }
+            // and what the steps up to them give, 16 at a time, the ones on the diagonal last
+            HeadScale sc = {1.0f, 1.0f};
+            const auto add = [&](int j, bool diagonal) {
+                float m[2][4] = {};
+#pragma unroll
+                for (int k = 0; k < NP / 16; ++k) {
+                    HeadB<T> b[2];
+                    load_b(b, tile_B(s), kWP, 16 * j, 16 * k, lane);
+                    const HeadA<T> c = load_a(tile_C(s), kWP, p0, 16 * k, lane);
+                    head_mma(m[0], c, b[0]);
+                    head_mma(m[1], c, b[1]);
+                }
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    const int col = 16 * j + 8 * n + 2 * t;
                     const float2 v = *reinterpret_cast<const float2 *>(pair + col);
-                    if (j / 2 < r) {
-                        m[j][0] *= r0 * v.x;
-                        m[j][1] *= r0 * v.y;
-                        m[j][2] *= r1 * v.x;
-                        m[j][3] *= r1 * v.y;
+                    if (!diagonal) {
+                        const float r0 = fast_exp2(l0), r1 = fast_exp2(l1);
+                        m[n][0] *= r0 * v.x;
+                        m[n][1] *= r0 * v.y;
+                        m[n][2] *= r1 * v.x;
+                        m[n][3] *= r1 * v.y;
                     } else {
                         const float2 w = *reinterpret_cast<const float2 *>(f.w + col);
                         const int row = p0 + g;
-                        m[j][0] = col <= row ? m[j][0] * (fast_exp2(l0 - v.x) * w.x) : 0.0f;
-                        m[j][1] = col + 1 <= row ? m[j][1] * (fast_exp2(l0 - v.y) * w.y) : 0.0f;
-                        m[j][2] = col <= row + 8 ? m[j][2] * (fast_exp2(l1 - v.x) * w.x) : 0.0f;
-                        m[j][3] = col + 1 <= row + 8 ? m[j][3] * (fast_exp2(l1 - v.y) * w.y) : 0.0f;
+                        m[n][0] = col <= row ? m[n][0] * (fast_exp2(l0 - v.x) * w.x) : 0.0f;
+                        m[n][1] = col + 1 <= row ? m[n][1] * (fast_exp2(l0 - v.y) * w.y) : 0.0f;
+                        m[n][2] = col <= row + 8 ? m[n][2] * (fast_exp2(l1 - v.x) * w.x) : 0.0f;
+                        m[n][3] = col + 1 <= row + 8 ? m[n][3] * (fast_exp2(l1 - v.y) * w.y) : 0.0f;
                     }
                 }
-            HeadScale sc = {1.0f, 1.0f};
-            if constexpr (kScaled<T>) sc = scale_for(warp_top<8>(m));
-            const float R0 = f.into[p0 + g] * sc.up, R1 = f.into[p0 + g + 8] * sc.up;
+                if constexpr (kScaled<T>) {                // y is in the units of the smallest power of two so far
+                    const HeadScale now = scale_for(warp_top<2>(m));
+                    if (j == 0 || now.up < sc.up) {
+                        const float by = j == 0 ? now.up : now.up * sc.down;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int from = 2 * (2 * half + j / 2);   // the 16 columns of the state that these belong to
-                const float down = kScaled<T> ? scale_for(fmaxf(tops[from], tops[from + 1])).down : 1.0f;
-                y[j][0] *= R0 * down;
-                y[j][1] *= R0 * down;
-                y[j][2] *= R1 * down;
-                y[j][3] *= R1 * down;
-            }
+                        for (int n = 0; n < 4; ++n)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j <= r) {
-                    const HeadA<T> w = acc_to_a<T>(m[2 * j], m[2 * j + 1], sc.up);
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-                        if (q0 + 16 * q < a.cols) {
-                            HeadB<T> b[2];
-                            load_b_t(b, tile_u(s), kXP, q0 + 16 * q, 16 * j, lane);
-                            head_mma(y[2 * q], w, b[0]);
-                            head_mma(y[2 * q + 1], w, b[1]);
-                        }
+                            for (int k = 0; k < 4; ++k) y[n][k] *= by;
+                        sc = now;
+                    }
                 }
+                const HeadA<T> w = acc_to_a<T>(m[0], m[1], sc.up);
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    HeadB<T> b[2];
+                    load_b_t(b, tile_u(s), kXP, q0 + 16 * q, 16 * j, lane);
+                    head_mma(y[2 * q], w, b[0]);
+                    head_mma(y[2 * q + 1], w, b[1]);
+                }
+            };
+#pragma unroll 1
+            for (int j = 0; j < r; ++j) add(j, false);
+            add(r, true);
             // Columns of later steps have the factor zero; where u is not finite there, zero times it is not zero.
             float odd = 0.0f;
 #pragma unroll

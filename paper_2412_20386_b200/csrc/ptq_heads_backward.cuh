@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
     using M = HeadBackSmem<T, NP>;
     constexpr int kWP = NP + kHeadPad, kXP = kHeadCols + kHeadPad;
     extern __shared__ __align__(128) unsigned char smem[];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, r = warp & 3, p0 = 16 * r;
+    const int warp = head_warp(), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, r = warp & 3, p0 = 16 * r;
     const bool rows_i = warp < 4;
     if (p.segments > 1) griddep_wait();
     const HeadPlace a = head_place(p, p.segments);
