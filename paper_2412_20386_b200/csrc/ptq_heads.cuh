@@ -4,9 +4,8 @@
 // an input (dt or 1) and S the state in front of the chunk:
 //     y_i = sum_{j <= i} e^{L_i - L_j} w_j (C_i . B_j) u_j  +  e^{L_i} S C_i  (+ D u_i)
 //     S  <- e^{L_64} S + sum_j e^{L_64 - L_j} w_j u_j B_j^T
-// A CTA walks over the chunks of a sequence for 64 columns of a head.  Eight warps: two have 16 steps of each chunk, 32 columns of
-// the outputs each (the scores of the steps both), and 16 columns of the state, half of its states each, which stay in registers in
-// binary32 from chunk to chunk.
+// A CTA walks over the chunks of a sequence for 64 columns of a head.  Eight warps: four have 16 steps of each chunk (scores and
+// outputs), four 16 columns of the state, which stay in registers in binary32 from chunk to chunk.
 //
 // The products are mma.sync on 16-bit operands: per chunk they are 64 x 64 x (16 .. 128), the scores go from one product's
 // accumulators through exponentials into the next one's operand and the state's update needs its operand in two halves (the
@@ -229,19 +228,19 @@ __device__ __forceinline__ void mma_tf32(float (&d)[4], uint32_t a0, uint32_t a1
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// d += a b.  binary32: both operands as two tf32 parts (22 bits), the product of the two lower parts left out (2^-22 of the terms);
+// d = a b + c.  binary32: both operands as two tf32 parts (22 bits), the product of the two lower parts left out (2^-22 of the terms);
 // the tensor cores' sums are cut off rather than rounded, so these 16 terms are summed on their own and added to the others rounded.
 template <typename T>
-__device__ __forceinline__ void head_mma(float (&d)[4], const HeadA<T> &a, const HeadB<T> &b)
+__device__ __forceinline__ void head_mma(float (&d)[4], const HeadA<T> &a, const HeadB<T> &b, float c0, float c1, float c2, float c3)
 {
     if constexpr (std::is_same<T, __half>::value) {
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a.r[0]), "r"(a.r[1]), "r"(a.r[2]), "r"(a.r[3]), "r"(b.r[0]), "r"(b.r[1]));
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+            : "r"(a.r[0]), "r"(a.r[1]), "r"(a.r[2]), "r"(a.r[3]), "r"(b.r[0]), "r"(b.r[1]), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
     } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a.r[0]), "r"(a.r[1]), "r"(a.r[2]), "r"(a.r[3]), "r"(b.r[0]), "r"(b.r[1]));
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+            : "r"(a.r[0]), "r"(a.r[1]), "r"(a.r[2]), "r"(a.r[3]), "r"(b.r[0]), "r"(b.r[1]), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
     } else {
         uint32_t ah[8], al[8], bh[4], bl[4];
 #pragma unroll
@@ -263,9 +262,20 @@ __device__ __forceinline__ void head_mma(float (&d)[4], const HeadA<T> &a, const
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) mma_tf32(e, ah[4 * k], ah[4 * k + 2], ah[4 * k + 1], ah[4 * k + 3], bh[2 * k], bh[2 * k + 1]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) d[i] += e[i];
+        d[0] = c0 + e[0];
+        d[1] = c1 + e[1];
+        d[2] = c2 + e[2];
+        d[3] = c3 + e[3];
     }
+}
+// d += a b; with `fresh` d = a b.
+template <typename T>
+__device__ __forceinline__ void head_mma(float (&d)[4], const HeadA<T> &a, const HeadB<T> &b, bool fresh = false)
+{
+    if (fresh)
+        head_mma(d, a, b, 0.0f, 0.0f, 0.0f, 0.0f);
+    else
+        head_mma(d, a, b, d[0], d[1], d[2], d[3]);
 }
 
 // Operands of more bits than the activations' type has: two binary16 or three bfloat16 values that add up to one of 22 or 24 bits
@@ -322,14 +332,20 @@ __device__ __forceinline__ float warp_top(const float (&d)[N][4])
     }
     return top;
 }
-// The power of two, within 2^-most .. 2^most, that brings `top` into 2^to .. 2^(to + 1), and its inverse.
+// The power of two, within 2^-60 .. 2^60, that brings `top` into 2^13 .. 2^14, and its inverse; 1 where `top` is 2^-4 .. 2^15: what
+// binary16 cannot hold is less than 2^-21 of it then, and what need not be scaled is not.
 struct HeadScale {
     float up, down;
 };
-__device__ __forceinline__ HeadScale scale_for(float top, int to = 13, int most = 60)
+__device__ __forceinline__ HeadScale exact_scale(float top, int to, int most)          // into 2^to .. 2^(to + 1), within 2^-most .. 2^most
 {
     const int e = top == 0.0f ? 0 : max(-most, min(most, to + 127 - static_cast<int>(__float_as_uint(top) >> 23)));
     return {__uint_as_float(static_cast<uint32_t>(127 + e) << 23), __uint_as_float(static_cast<uint32_t>(127 - e) << 23)};
+}
+__device__ __forceinline__ HeadScale scale_for(float top)
+{
+    if (top >= 0.0625f && top < 32768.0f) return {1.0f, 1.0f};
+    return exact_scale(top, 13, 60);
 }
 
 // ---------------------------------------------------------------------------------------------------- loads
@@ -485,13 +501,19 @@ __device__ __forceinline__ void state_update(float (&S)[kN][4], const T *x, cons
             for (int i = 0; i < 4; ++i) most = __hmax2(most, __habs2(*reinterpret_cast<const __half2 *>(&a[k].r[i])));
         const float2 v = __half22float2(most), q = *reinterpret_cast<const float2 *>(f + 2 * lane);
         // of u 2^-15 .. 2^15, which binary16 holds; an infinity counts as the largest finite value
-        scu = scale_for(warp_max(fminf(fmaxf(v.x, v.y), 65504.0f)), 0, 15);
-        scf = scale_for(warp_max(fmaxf(finite_abs(q.x), finite_abs(q.y))));
+        scu = exact_scale(warp_max(fminf(fmaxf(v.x, v.y), 65504.0f)), 0, 15);
+        scf = exact_scale(warp_max(fmaxf(finite_abs(q.x), finite_abs(q.y))), 13, 60);
     }
     // the chunk's sums on their own, joined with the state in binary32: the tensor cores' sums are cut off, not rounded
-    HeadA<T> part[kHeadSteps / 16][kHeadParts<T>];
+    // (three parts of 64 steps are too many registers: 32 steps at a time)
+    constexpr int kSet = kHeadParts<T> > 2 ? 2 : 4;
+    const float down = scu.down * scf.down;
 #pragma unroll
-    for (int k = 0; k < kHeadSteps / 16; ++k) {
+    for (int k0 = 0; k0 < kHeadSteps / 16; k0 += kSet) {
+    HeadA<T> part[kSet][kHeadParts<T>];
+#pragma unroll
+    for (int ks = 0; ks < kSet; ++ks) {
+        const int k = k0 + ks;
         const float2 f0 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t), f1 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t + 8);
         if constexpr (std::is_same<T, __half>::value) {
             // u f as two binary16 values in binary16 arithmetic: f in two parts, the product with the upper one and what its
@@ -510,8 +532,8 @@ __device__ __forceinline__ void state_update(float (&S)[kN][4], const T *x, cons
                 const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&a[k].r[i]), up);
                 const __half2 h = *reinterpret_cast<const __half2 *>(&fh[i >> 1]), l = *reinterpret_cast<const __half2 *>(&fl[i >> 1]);
                 const __half2 hi = __hmul2_rn(v, h), lo = __hfma2(v, l, __hfma2(v, h, __hneg2(hi)));
-                part[k][0].r[i] = *reinterpret_cast<const uint32_t *>(&hi);
-                part[k][1].r[i] = *reinterpret_cast<const uint32_t *>(&lo);
+                part[ks][0].r[i] = *reinterpret_cast<const uint32_t *>(&hi);
+                part[ks][1].r[i] = *reinterpret_cast<const uint32_t *>(&lo);
             }
         } else if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -520,30 +542,33 @@ __device__ __forceinline__ void state_update(float (&S)[kN][4], const T *x, cons
                 uint32_t r[kHeadParts<T>];
                 head_split<T>(v.x * q.x, v.y * q.y, r);
 #pragma unroll
-                for (int j = 0; j < kHeadParts<T>; ++j) part[k][j].r[i] = r[j];
+                for (int j = 0; j < kHeadParts<T>; ++j) part[ks][j].r[i] = r[j];
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) part[k][0].v[i] = a[k].v[i] * (i < 4 ? (i & 1 ? f0.y : f0.x) : (i & 1 ? f1.y : f1.x));
+            for (int i = 0; i < 8; ++i) part[ks][0].v[i] = a[k].v[i] * (i < 4 ? (i & 1 ? f0.y : f0.x) : (i & 1 ? f1.y : f1.x));
         }
     }
-    const float down = scu.down * scf.down;
 #pragma unroll
     for (int n = 0; n < kN / 2; ++n) {
-        float sum[2][4] = {};
+        float sum[2][4];
 #pragma unroll
-        for (int k = 0; k < kHeadSteps / 16; ++k) {
+        for (int ks = 0; ks < kSet; ++ks) {
             HeadB<T> b[2];
-            load_b_t(b, z, kZP, n0 + 16 * n, 16 * k, lane);
+            load_b_t(b, z, kZP, n0 + 16 * n, 16 * (k0 + ks), lane);
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int q = kHeadParts<T> - 1; q >= 0; --q) head_mma(sum[j], part[k][q], b[j]);
+                for (int q = kHeadParts<T> - 1; q >= 0; --q) head_mma(sum[j], part[ks][q], b[j], ks == 0 && q == kHeadParts<T> - 1);
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) S[2 * n + j][i] = fmaf(decay, S[2 * n + j][i], kScaled<T> ? sum[j][i] * down : sum[j][i]);
+            for (int i = 0; i < 4; ++i) {
+                const float v = kScaled<T> ? sum[j][i] * down : sum[j][i];
+                S[2 * n + j][i] = k0 == 0 ? fmaf(decay, S[2 * n + j][i], v) : S[2 * n + j][i] + v;
+            }
+    }
     }
 }
 
@@ -641,7 +666,7 @@ __device__ __forceinline__ void write_factors(HeadFactors &f, const HeadSteps &s
 }
 
 // Shared memory of the forward kernel, in bytes: two stages of tiles (u, B, C; sums: u or dy, and one of B and C), the state as an
-// operand, factors of two chunks, largest magnitudes of the state's parts.
+// operand, factors of two chunks, powers of two of its columns.
 template <typename T, int NP, int kMode>
 struct HeadSmem {
     static constexpr int kWide = kHeadSteps * (NP + kHeadPad) * static_cast<int>(sizeof(T));
@@ -650,9 +675,35 @@ struct HeadSmem {
     static constexpr int kStages = 2 * kStage + (kMode == kHeadForward ? kWide : 0) <= 200 * 1024 ? 2 : 1;
     static constexpr int kState = kStages * kStage;
     static constexpr int kFactors = kState + (kMode == kHeadForward ? kWide : 0);
-    static constexpr int kTops = kFactors + 2 * static_cast<int>(sizeof(HeadFactors));
-    static constexpr int kBytes = kTops + 2 * 8 * 4;
+    static constexpr int kPowers = kFactors + 2 * static_cast<int>(sizeof(HeadFactors));
+    static constexpr int kBytes = kPowers + 4 * 4;
 };
+
+// Whether an operand holds an infinity or NaN (zero times it is not zero).
+template <typename T, int N>
+__device__ __forceinline__ bool not_finite(const HeadB<T> (&v)[N][2])
+{
+    if constexpr (std::is_same<T, __half>::value) {
+        const __half2 zero = __float2half2_rn(0.0f);
+        __half2 sum = zero;
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) sum = __hfma2(*reinterpret_cast<const __half2 *>(&v[i / 4][i / 2 % 2].r[i % 2]), zero, sum);
+        const float2 f = __half22float2(sum);
+        return f.x + f.y != 0.0f;
+    } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        const __nv_bfloat162 zero = __float2bfloat162_rn(0.0f);
+        __nv_bfloat162 sum = zero;
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) sum = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&v[i / 4][i / 2 % 2].r[i % 2]), zero, sum);
+        const float2 f = __bfloat1622float2(sum);
+        return f.x + f.y != 0.0f;
+    } else {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8 * N; ++i) sum = fmaf(v[i / 8][i / 4 % 2].v[i % 4], 0.0f, sum);
+        return sum != 0.0f;
+    }
+}
 
 // The four lanes of a quad hold two columns each of four 8-column tiles, packed: lane t gets all eight columns of tile t.
 __device__ __forceinline__ void quad_transpose(uint32_t (&r)[4], int t)
@@ -671,12 +722,15 @@ template <typename T, int NP, int kMode>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(const HeadParams p)
 {
     using M = HeadSmem<T, NP, kMode>;
-    constexpr int kWP = NP + kHeadPad, kXP = kHeadCols + kHeadPad, kN = NP / 16;         // 8-column tiles of this warp's half of the states
+    constexpr int kWP = NP + kHeadPad, kXP = kHeadCols + kHeadPad;
+    constexpr int kN = NP / (kMode == kHeadForward ? 8 : 16);                            // 8-column tiles of a warp's states
     constexpr bool kOut = kMode == kHeadForward, kGrad = kMode == kHeadGradSum;
     extern __shared__ __align__(128) unsigned char smem[];
     const int warp = head_warp(), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    // 16 steps r, and 16 columns of the state; the two warps of a scheduler have few and many scores
-    const int r = warp < 4 ? warp : 7 - warp, half = warp >> 2, p0 = 16 * r, q0 = 32 * half, n0 = half * (NP / 2);
+    // Outputs: warps 0 .. 3 have 16 steps each, 4 .. 7 16 columns of the state.  (The last steps have four times the first ones' scores: in the
+    // CTAs that share an SM, some 148 apart, on different schedulers.)  Sums: two warps 16 columns, half of the states each.
+    const bool outputs = kOut && warp < 4;
+    const int r = outputs && (blockIdx.x / 148) & 1 ? 3 - warp : warp & 3, p0 = 16 * r, n0 = kOut ? 0 : (warp >> 2) * (NP / 2);
     if (kOut && p.segments > 1) griddep_wait();
     const HeadPlace a = head_place(p, kOut ? p.segments : p.segments - 1);
     const int seg = kGrad ? a.seg + 1 : a.seg;            // sums: of all segments but the last, of gradients: but the first
@@ -688,7 +742,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
     const auto tile_C = [&](int s) { return reinterpret_cast<T *>(smem + (M::kStages == 2 ? s * M::kStage : 0) + M::kNarrow + M::kWide); };
     T *state_s = reinterpret_cast<T *>(smem + M::kState);
     HeadFactors *factors = reinterpret_cast<HeadFactors *>(smem + M::kFactors);
-    float *all_tops = reinterpret_cast<float *>(smem + M::kTops);      // of two chunks: a warp may be one ahead
+    float *powers = reinterpret_cast<float *>(smem + M::kPowers);
 
     const T *u = static_cast<const T *>(kGrad ? p.dy : p.u) +
                  (kGrad ? (static_cast<int64_t>(a.b) * p.length * p.heads + a.h) * p.cols : a.b * p.u_b + a.h * p.u_h) + a.tile * kHeadCols;
@@ -716,11 +770,11 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
     const int64_t state_size = static_cast<int64_t>(p.cols) * p.states, tile_at = static_cast<int64_t>(a.tile) * kHeadCols * p.states;
     const int count = chunk1 - chunk0;
     const auto chunk_of = [&](int i) { return kGrad ? chunk1 - 1 - i : chunk0 + i; };
-    // Warp i % 8 forms the factors of chunk i + 1 while chunk i is worked on; it has read delta a chunk before that.
+    // One of warps 4 .. 7 forms the factors of chunk i + 1 while chunk i is worked on; it has read delta a chunk before that.
     float delta[2] = {};
     if (count > 0) {
         load(chunk_of(0), 0);
-        if (warp == 0) {
+        if (warp == 4) {
             load_delta<T>(p, delta_at, chunk_of(0) * kHeadSteps, a.n, lane, delta);
             write_factors<kMode>(factors[0], head_steps(p, delta, bias, A2, chunk_of(0) * kHeadSteps, a.n, lane), lane);
             if (count > 1) load_delta<T>(p, delta_at, chunk_of(1) * kHeadSteps, a.n, lane, delta);
@@ -734,80 +788,81 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
             from = p.slots + (head_at * p.segments + (seg > 0 ? seg : p.segments) - 1) * state_size + tile_at;
         else if (kOut && p.state)
             from = p.state + head_at * state_size + tile_at;
-        read_state<kN>(S, from, p0, n0, a.cols, p.states, lane);
+        if (!outputs) read_state<kN>(S, from, p0, n0, a.cols, p.states, lane);
     }
     const bool started = kOut && (seg > 0 || p.state);    // else the state in front of the first chunk is zero
     double log_decay = 0.0;
-    for (int i = 0; i < count; ++i) {
-        const int chunk = chunk_of(i), first = chunk * kHeadSteps, s = i & 1;
-        const bool busy = p0 < a.cols;                    // this warp has columns of the state
-        float *tops = all_tops + 8 * s;
-        if (kOut) {
-            if (p.history && busy)
-                write_state<kN>(S, p.history + ((static_cast<int64_t>(a.b) * p.chunks + chunk) * p.heads + a.h) * state_size + tile_at, p0, n0, a.cols, p.states, lane);
-            float up = 1.0f;
-            if constexpr (kScaled<T>) {
-                const float top = warp_top<kN>(S);
-                if (lane == 0) tops[2 * r + half] = top;
-            }
-            if (kScaled<T> || i > 0) __syncthreads();     // everyone is done with the state in front of the last chunk
-            if constexpr (kScaled<T>) up = scale_for(fmaxf(tops[2 * r], tops[2 * r + 1])).up;
+    const bool busy = !outputs && p0 < a.cols;            // this warp has columns of the state
+    // the state as an operand: its columns brought into binary16's range
+    const auto publish = [&](int chunk) {
+        if (p.history && busy)
+            write_state<kN>(S, p.history + ((static_cast<int64_t>(a.b) * p.chunks + chunk) * p.heads + a.h) * state_size + tile_at, p0, n0, a.cols, p.states, lane);
+        HeadScale sc = {1.0f, 1.0f};
+        if constexpr (kScaled<T>) {
+            sc = scale_for(warp_top<kN>(S));
+            if (lane == 0) powers[r] = sc.down;
+        }
+        const auto store = [&](float by) {
 #pragma unroll
             for (int n = 0; n < kN; ++n) {
-                head_store_pair(state_s + (p0 + g) * kWP + n0 + 8 * n + 2 * t, S[n][0] * up, S[n][1] * up);
-                head_store_pair(state_s + (p0 + g + 8) * kWP + n0 + 8 * n + 2 * t, S[n][2] * up, S[n][3] * up);
+                head_store_pair(state_s + (p0 + g) * kWP + 8 * n + 2 * t, S[n][0] * by, S[n][1] * by);
+                head_store_pair(state_s + (p0 + g + 8) * kWP + 8 * n + 2 * t, S[n][2] * by, S[n][3] * by);
             }
-        }
+        };
+        if (sc.up == 1.0f)
+            store(1.0f);
+        else
+            store(sc.up);
+    };
+    if (kOut && !outputs && count > 0) publish(chunk0);
+    for (int i = 0; i < count; ++i) {
+        const int chunk = chunk_of(i), first = chunk * kHeadSteps, s = i & 1;
         cp_async_wait<0>();
-        __syncthreads();                                  // the tiles, their steps' factors, and the state as an operand
+        __syncthreads();                                  // the tiles, their steps' factors, and the state as an operand; the last chunk is done
         if (M::kStages == 2 && i + 1 < count) load(chunk_of(i + 1), s ^ 1);
-        if (warp == ((i + 1) & 7) && i + 2 < count) load_delta<T>(p, delta_at, chunk_of(i + 2) * kHeadSteps, a.n, lane, delta);
+        if (warp == 4 + ((i + 1) & 3) && i + 2 < count) load_delta<T>(p, delta_at, chunk_of(i + 2) * kHeadSteps, a.n, lane, delta);
         const HeadFactors &f = factors[s];
         const float decay = f.decay;
         log_decay += f.log_decay;
 
-        if constexpr (kOut) {
-            // what the state gives these 16 steps
-            float y[4][4] = {};
-#pragma unroll
-            for (int k = 0; k < NP / 16; ++k) {
-                const HeadA<T> c = load_a(tile_C(s), kWP, p0, 16 * k, lane);
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    HeadB<T> b[2];
-                    load_b(b, state_s, kWP, q0 + 16 * j, 16 * k, lane);
-                    head_mma(y[2 * j], c, b[0]);
-                    head_mma(y[2 * j + 1], c, b[1]);
-                }
-            }
+        if (outputs) {
             const float *pair = f.pair[r];
             const float l0 = pair[p0 + g], l1 = pair[p0 + g + 8];
-            {
-                const float R0 = f.into[p0 + g], R1 = f.into[p0 + g + 8];
+            float y[8][4] = {};
+            if (i > 0 || started) {                        // what the state gives these 16 steps
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int from = 2 * (2 * half + j);   // the 16 columns of the state that these belong to
-                    const float down = kScaled<T> ? scale_for(fmaxf(tops[from], tops[from + 1])).down : 1.0f;
+                for (int k = 0; k < NP / 16; ++k) {
+                    const HeadA<T> c = load_a(tile_C(s), kWP, p0, 16 * k, lane);
 #pragma unroll
-                    for (int n = 2 * j; n < 2 * j + 2; ++n) {
-                        y[n][0] *= R0 * down;
-                        y[n][1] *= R0 * down;
-                        y[n][2] *= R1 * down;
-                        y[n][3] *= R1 * down;
+                    for (int j = 0; j < 4; ++j) {
+                        HeadB<T> b[2];
+                        load_b(b, state_s, kWP, 16 * j, 16 * k, lane);
+                        head_mma(y[2 * j], c, b[0], k == 0);
+                        head_mma(y[2 * j + 1], c, b[1], k == 0);
                     }
                 }
+                const float R0 = f.into[p0 + g], R1 = f.into[p0 + g + 8];
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {
+                    const float down = kScaled<T> ? powers[n / 2] : 1.0f;
+                    y[n][0] *= R0 * down;
+                    y[n][1] *= R0 * down;
+                    y[n][2] *= R1 * down;
+                    y[n][3] *= R1 * down;
+                }
             }
+            asm volatile("bar.arrive 1, 256;" ::: "memory");           // the state and its powers have been read
             // and what the steps up to them give, 16 at a time, the ones on the diagonal last
             HeadScale sc = {1.0f, 1.0f};
             const auto add = [&](int j, bool diagonal) {
-                float m[2][4] = {};
+                float m[2][4];
 #pragma unroll
                 for (int k = 0; k < NP / 16; ++k) {
                     HeadB<T> b[2];
                     load_b(b, tile_B(s), kWP, 16 * j, 16 * k, lane);
                     const HeadA<T> c = load_a(tile_C(s), kWP, p0, 16 * k, lane);
-                    head_mma(m[0], c, b[0]);
-                    head_mma(m[1], c, b[1]);
+                    head_mma(m[0], c, b[0], k == 0);
+                    head_mma(m[1], c, b[1], k == 0);
                 }
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
@@ -830,92 +885,104 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
                 }
                 if constexpr (kScaled<T>) {                // y is in the units of the smallest power of two so far
                     const HeadScale now = scale_for(warp_top<2>(m));
-                    if (j == 0 || now.up < sc.up) {
-                        const float by = j == 0 ? now.up : now.up * sc.down;
+                    if (j == 0 ? now.up != 1.0f : now.up < sc.up) {
+                        const float by = now.up * sc.down;
 #pragma unroll
-                        for (int n = 0; n < 4; ++n)
+                        for (int n = 0; n < 8; ++n)
 #pragma unroll
                             for (int k = 0; k < 4; ++k) y[n][k] *= by;
                         sc = now;
                     }
                 }
-                const HeadA<T> w = acc_to_a<T>(m[0], m[1], sc.up);
+                if (kScaled<T> && sc.up != 1.0f) {
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    HeadB<T> b[2];
-                    load_b_t(b, tile_u(s), kXP, q0 + 16 * q, 16 * j, lane);
-                    head_mma(y[2 * q], w, b[0]);
-                    head_mma(y[2 * q + 1], w, b[1]);
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) m[n][k] *= sc.up;
+                }
+                HeadB<T> v[4][2];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) load_b_t(v[q], tile_u(s), kXP, 16 * q, 16 * j, lane);
+                // On the diagonal columns of later steps have the factor zero; where u is not finite there, zero times it is not zero.
+                if (diagonal && __any_sync(0xffffffffu, not_finite<T>(v))) {
+#pragma unroll 1
+                    for (int c = 0; c < 16; ++c) {
+                        const int from = (lane & 28) + (c & 7) / 2;
+                        const float e0 = c < 8 ? (c & 1 ? m[0][1] : m[0][0]) : (c & 1 ? m[1][1] : m[1][0]);
+                        const float e1 = c < 8 ? (c & 1 ? m[0][3] : m[0][2]) : (c & 1 ? m[1][3] : m[1][2]);
+                        const float w0 = __shfl_sync(0xffffffffu, e0, from), w1 = __shfl_sync(0xffffffffu, e1, from);
+#pragma unroll
+                        for (int n = 0; n < 8; ++n) {
+                            const float2 x = head_pair(tile_u(s) + (16 * j + c) * kXP + 8 * n + 2 * t);
+                            if (c <= g) {
+                                y[n][0] = fmaf(w0, x.x, y[n][0]);
+                                y[n][1] = fmaf(w0, x.y, y[n][1]);
+                            }
+                            if (c <= g + 8) {
+                                y[n][2] = fmaf(w1, x.x, y[n][2]);
+                                y[n][3] = fmaf(w1, x.y, y[n][3]);
+                            }
+                        }
+                    }
+                    return;
+                }
+                const HeadA<T> w = acc_to_a<T>(m[0], m[1], 1.0f);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    head_mma(y[2 * q], w, v[q][0]);
+                    head_mma(y[2 * q + 1], w, v[q][1]);
                 }
             };
 #pragma unroll 1
             for (int j = 0; j < r; ++j) add(j, false);
             add(r, true);
-            // Columns of later steps have the factor zero; where u is not finite there, zero times it is not zero.
-            float odd = 0.0f;
+            if (kScaled<T> && sc.down != 1.0f) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+                for (int n = 0; n < 8; ++n)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) odd = fmaf(y[j][k], 0.0f, odd);
+                    for (int k = 0; k < 4; ++k) y[n][k] *= sc.down;
+            }
             const int step0 = first + p0 + g, step1 = step0 + 8;
-            if (!__any_sync(0xffffffffu, odd != 0.0f)) {
-                uint32_t out[2][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+            for (int h = 0; h < 2; ++h)                            // 32 columns at a time
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const int c = q0 + 8 * j + 2 * t, step = k ? step1 : step0;
-                        float v0 = y[j][2 * k] * sc.down, v1 = y[j][2 * k + 1] * sc.down;
+                for (int k = 0; k < 2; ++k) {
+                    const int step = k ? step1 : step0;
+                    T *row = y_at + token(step) * y_l;
+                    uint32_t out[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int c = 32 * h + 8 * j + 2 * t;
+                        float v0 = y[4 * h + j][2 * k], v1 = y[4 * h + j][2 * k + 1];
                         if (p.D) {
                             const float2 x = head_pair(tile_u(s) + (p0 + g + 8 * k) * kXP + c);
                             v0 = fmaf(skip, x.x, v0);
                             v1 = fmaf(skip, x.y, v1);
                         }
-                        if constexpr (sizeof(T) == 2) out[k][j] = head_pack<T>(v0, v1);
+                        if constexpr (sizeof(T) == 2) out[j] = head_pack<T>(v0, v1);
                         if (sizeof(T) == 4 || p.out_unit < 16) {
                             if (step >= a.n || c >= a.cols) continue;
-                            T *to = y_at + token(step) * y_l + c;
                             if (p.out_unit >= 2 * static_cast<int>(sizeof(T))) {
-                                head_store_pair(to, v0, v1);
+                                head_store_pair(row + c, v0, v1);
                             } else {
-                                to[0] = head_round<T>(v0);
-                                if (c + 1 < a.cols) to[1] = head_round<T>(v1);
+                                row[c] = head_round<T>(v0);
+                                if (c + 1 < a.cols) row[c + 1] = head_round<T>(v1);
                             }
                         }
                     }
-                if (sizeof(T) == 2 && p.out_unit == 16) {  // 16 bytes of a row a lane
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        quad_transpose(out[k], t);
-                        const int c = q0 + 8 * t, step = k ? step1 : step0;
-                        if (step < a.n && c < a.cols)
-                            *reinterpret_cast<uint4 *>(y_at + token(step) * y_l + c) = make_uint4(out[k][0], out[k][1], out[k][2], out[k][3]);
+                    if (sizeof(T) == 2 && p.out_unit == 16) {      // 16 bytes of a row a lane
+                        quad_transpose(out, t);
+                        const int c = 32 * h + 8 * t;
+                        if (step < a.n && c < a.cols) *reinterpret_cast<uint4 *>(row + c) = make_uint4(out[0], out[1], out[2], out[3]);
                     }
                 }
-            } else {
-                // Step by step from shared memory: only what is there enters.  A lane has a column.
-                const int col = q0 + lane;
-                const float down = kScaled<T> ? scale_for(fmaxf(tops[col / 16 * 2], tops[col / 16 * 2 + 1])).down : 1.0f;
-                for (int row = p0; row < p0 + 16; ++row) {
-                    const T *c = tile_C(s) + row * kWP;
-                    float v = 0.0f;
-                    for (int n = 0; n < p.states; ++n) v = fmaf(head_f32(c[n]), head_f32(state_s[col * kWP + n]), v);
-                    v = i > 0 || started ? v * f.into[row] * down : 0.0f;
-                    for (int j = 0; j <= row; ++j) {
-                        float score = 0.0f;
-                        for (int n = lane; n < p.states; n += 32) score = fmaf(head_f32(c[n]), head_f32(tile_B(s)[j * kWP + n]), score);
-#pragma unroll
-                        for (int d = 16; d > 0; d >>= 1) score += __shfl_xor_sync(0xffffffffu, score, d);
-                        score *= j < p0 ? fast_exp2(pair[row]) * pair[j] : fast_exp2(pair[row] - pair[j]) * f.w[j];
-                        v = fmaf(score, head_f32(tile_u(s)[j * kXP + col]), v);
-                    }
-                    if (p.D) v = fmaf(skip, head_f32(tile_u(s)[row * kXP + col]), v);
-                    if (first + row < a.n && col < a.cols) y_at[token(first + row) * y_l + col] = head_round<T>(v);
-                }
-            }
         }
         if (busy) state_update<NP, kN>(S, tile_u(s), tile_B(s), f.state, decay, p0, n0, lane);
-        if (warp == (i & 7) && i + 1 < count)
+        if (kOut && !outputs) {
+            asm volatile("bar.sync 1, 256;" ::: "memory");             // the outputs' warps have read the state
+            if (i + 1 < count) publish(chunk + 1);
+        }
+        if (warp == 4 + (i & 3) && i + 1 < count)
             write_factors<kMode>(factors[s ^ 1], head_steps(p, delta, bias, A2, chunk_of(i + 1) * kHeadSteps, a.n, lane), lane);
         if (M::kStages == 1 && i + 1 < count) {
             __syncthreads();
@@ -924,7 +991,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
     }
     if constexpr (kOut) {
         // final states: by the segment that holds the last step, or the first one of an empty sequence
-        if (p.final_state && seg == (chunks > 0 ? (chunks - 1) / p.segment_chunks : 0))
+        if (!outputs && p.final_state && seg == (chunks > 0 ? (chunks - 1) / p.segment_chunks : 0))
             write_state<kN>(S, p.final_state + head_at * state_size + tile_at, p0, n0, a.cols, p.states, lane);
     } else {
         write_state<kN>(S, p.slots + (head_at * p.segments + seg) * state_size + tile_at, p0, n0, a.cols, p.states, lane);
@@ -935,11 +1002,11 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
 
 // ---------------------------------------------------------------------------------------------------- single tokens
 // One step of many sequences: bound by reading and writing the binary32 states once.  kLanes lanes have a row of a state (4 values
-// each), a CTA 16 rows of one head (4 rows of 128 states in flight per warp); everything is binary32.
+// each), a CTA 32 rows of one head (8 rows of 128 states in flight per warp); everything is binary32.
 template <typename T, int kLanes, bool kWhole>
 __global__ void __launch_bounds__(128) ptq_heads_step_kernel(const HeadParams p)
 {
-    constexpr int kAt = 128 / kLanes, kRows = 16 / kAt < 1 ? 1 : 16 / kAt;             // rows at a time, times
+    constexpr int kAt = 128 / kLanes, kRows = kLanes / 4;                               // rows at a time, times
     const int tiles = (p.cols + kAt * kRows - 1) / (kAt * kRows);
     int i = static_cast<int>(blockIdx.x);
     const int col0 = i % tiles * (kAt * kRows) + threadIdx.x / kLanes;

@@ -52,7 +52,7 @@ ptq_status_t HeadsLaunch<T>::step(const ptq::HeadParams &p, bool whole, cudaStre
     return with_states(p.states, [&](auto n) {
         return with_flag(whole, [&](auto w) {
             constexpr int kLanes = decltype(n)::value / 4;
-            constexpr int kRows = 128 / kLanes * (kLanes == 32 ? 4 : kLanes == 16 ? 2 : 1);      // rows of a CTA
+            constexpr int kRows = 32;                // rows of a CTA
             const long long ctas = static_cast<long long>(p.batch) * p.heads * ceil_div(p.cols, kRows);
             if (ctas > kMaxGrid) return fail(PTQ_ERR_SHAPE, "the batch is too large for one launch");
             ptq::ptq_heads_step_kernel<T, kLanes, decltype(w)::value><<<static_cast<unsigned>(ctas), 128, 0, stream>>>(p);
