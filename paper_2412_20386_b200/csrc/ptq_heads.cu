@@ -195,18 +195,19 @@ ptq_status_t ptq_heads_forward(const ptq_heads_t *s, void *y, float *final_state
     p.y = y;
     p.final_state = final_state;
     p.history = history;
-    p.out_unit = aligned({y}, 16) && s->cols * e % 16 == 0 ? 16 : aligned({y}, 2 * e) && s->cols % 2 == 0 ? 2 * e : e;
+    p.out_unit = aligned({y}, 2 * e) && s->cols % 2 == 0 ? 2 * e : e;
     unsigned char *w = static_cast<unsigned char *>(workspace);
     p.slots = reinterpret_cast<float *>(w + space.slots);
     p.logs = reinterpret_cast<float *>(w + space.logs);
+    const bool whole = p.unit == 16 && aligned({y}, 16) && aligned({s->state, final_state, history}, 8);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return with_launch(s->dtype, [&](auto launch) -> ptq_status_t {
         if (s->length == 1 && !history) return launch.step(p, s->states % 4 == 0 && aligned({s->state, final_state}, 16), st);
         if (plan.segments > 1) {
-            PTQ_TRY(launch.chunks(ptq::kHeadSum, p, false, st));
+            PTQ_TRY(launch.chunks(ptq::kHeadSum, p, whole, false, st));
             PTQ_TRY(fold(p, s->state, 0, st));
         }
-        return launch.chunks(ptq::kHeadForward, p, plan.segments > 1, st);
+        return launch.chunks(ptq::kHeadForward, p, whole, plan.segments > 1, st);
     });
 }
 
@@ -242,15 +243,16 @@ ptq_status_t ptq_heads_backward(const ptq_heads_t *s, const float *history, cons
     p.du = g->du;
     p.final_state = g->dstate;
     p.out_unit = aligned({g->du}, 2 * e) && s->cols % 2 == 0 ? 2 * e : e;
+    const bool whole = p.unit == 16 && aligned({g->du}, 2 * e) && aligned({history, dfinal, g->dstate}, 8);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return with_type(s->dtype, [&](auto t) -> ptq_status_t {
         using T = decltype(t);
         using Launch = HeadsLaunch<T>;
         if (plan.segments > 1) {
-            PTQ_TRY(Launch::chunks(ptq::kHeadGradSum, p, false, st));
+            PTQ_TRY(Launch::chunks(ptq::kHeadGradSum, p, whole, false, st));
             PTQ_TRY(fold(p, dfinal, 1, st));
         }
-        PTQ_TRY(Launch::backward(p, plan.segments > 1, st));
+        PTQ_TRY(Launch::backward(p, whole, plan.segments > 1, st));
         PTQ_TRY(launch_next(ptq::ptq_heads_finish_kernel<T>, dim3(static_cast<unsigned>(sums), 2), 256, 0, st, p, static_cast<T *>(g->dB), static_cast<T *>(g->dC)));
         PTQ_TRY(launch_next(ptq::ptq_heads_finish_delta_kernel<T>, dim3(static_cast<unsigned>(s->batch * s->heads)), 128, 0, st, p, static_cast<T *>(g->ddelta), shares));
         return launch_next(ptq::ptq_heads_finish_sums_kernel, dim3(static_cast<unsigned>(s->heads)), 128, 0, st, p, shares, g->dA, g->ddelta_bias, g->dD);

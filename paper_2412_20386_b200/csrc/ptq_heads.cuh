@@ -305,12 +305,8 @@ __device__ __forceinline__ float finite_abs(float v)
     const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
     return b < 0x7f800000u ? __uint_as_float(b) : 0.0f;
 }
-__device__ __forceinline__ float warp_max(float v)
-{
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
-    return v;
-}
+// The largest of a warp's values, none of them negative: their bits are in the same order.
+__device__ __forceinline__ float warp_max(float v) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v))); }
 // The largest magnitude of a warp's values; if that is infinite, of the finite ones (the others are lost whatever their scale).
 template <int N>
 __device__ __forceinline__ float warp_top(const float (&d)[N][4])
@@ -363,9 +359,10 @@ __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commi
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// 64 rows of kWidth elements into a tile: row r from src + r * step, zeros from `rows` and from column `cols` on.  Moved in units that
-// divide the rows; 2-byte ones go through registers.
-template <int kWidth, int kThreads, typename T>
+// 64 rows of kWidth elements into a tile: row r from src + r * step, zeros from `rows` and from column `cols` on.  kWhole: 16 bytes at a
+// time; else in units of 8, 4 or (through registers) 2 bytes that divide the rows.  (Two kernels: what the general one needs
+// would crowd the instruction cache of the other.)
+template <int kWidth, int kThreads, bool kWhole, typename T>
 __device__ __forceinline__ void load_rows(T *tile, const T *src, int64_t step, int rows, int cols, int unit)
 {
     constexpr int kPitch = kWidth + kHeadPad;
@@ -384,9 +381,9 @@ __device__ __forceinline__ void load_rows(T *tile, const T *src, int64_t step, i
             left -= kAt;
         }
     };
-    if (unit == 16) {
+    if constexpr (kWhole) {
         go(std::integral_constant<int, 16>());
-    } else if (unit == 8) {
+    } else if (unit >= 8) {
         go(std::integral_constant<int, 8>());
     } else if (unit == 4) {
         go(std::integral_constant<int, 4>());
@@ -505,8 +502,8 @@ __device__ __forceinline__ void state_update(float (&S)[kN][4], const T *x, cons
         scf = exact_scale(warp_max(fmaxf(finite_abs(q.x), finite_abs(q.y))), 13, 60);
     }
     // the chunk's sums on their own, joined with the state in binary32: the tensor cores' sums are cut off, not rounded
-    // (three parts of 64 steps are too many registers: 32 steps at a time)
-    constexpr int kSet = kHeadParts<T> > 2 ? 2 : 4;
+    // (beside all states of 16 columns three parts of 64 steps are too many registers: 32 steps at a time)
+    constexpr int kSet = kHeadParts<T> > 2 && kN > 8 ? 2 : 4;
     const float down = scu.down * scf.down;
 #pragma unroll
     for (int k0 = 0; k0 < kHeadSteps / 16; k0 += kSet) {
@@ -585,10 +582,11 @@ __device__ __forceinline__ void for_state(int p0, int n0, int cols, int states, 
             fn(n, i, p < cols && c < states, static_cast<int64_t>(p) * states + c);
         }
 }
-template <int kN>
+// kWhole: two values at a time.
+template <bool kWhole, int kN>
 __device__ __forceinline__ void read_state(float (&S)[kN][4], const float *from, int p0, int n0, int cols, int states, int lane)
 {
-    if (states % 2 == 0 && (reinterpret_cast<uintptr_t>(from) & 7) == 0) {
+    if constexpr (kWhole) {
         const int g = lane >> 2, t = lane & 3;
 #pragma unroll
         for (int n = 0; n < kN; ++n)
@@ -604,10 +602,10 @@ __device__ __forceinline__ void read_state(float (&S)[kN][4], const float *from,
         for_state<kN>(p0, n0, cols, states, lane, [&](int n, int i, bool on, int64_t at) { S[n][i] = on && from ? from[at] : 0.0f; });
     }
 }
-template <int kN>
+template <bool kWhole, int kN>
 __device__ __forceinline__ void write_state(const float (&S)[kN][4], float *to, int p0, int n0, int cols, int states, int lane)
 {
-    if (states % 2 == 0 && (reinterpret_cast<uintptr_t>(to) & 7) == 0) {
+    if constexpr (kWhole) {
         const int g = lane >> 2, t = lane & 3;
 #pragma unroll
         for (int n = 0; n < kN; ++n)
@@ -666,15 +664,17 @@ __device__ __forceinline__ void write_factors(HeadFactors &f, const HeadSteps &s
 }
 
 // Shared memory of the forward kernel, in bytes: two stages of tiles (u, B, C; sums: u or dy, and one of B and C), the state as an
-// operand, factors of two chunks, powers of two of its columns.
+// operand, staging, factors of two chunks, powers of two of the state's columns.
 template <typename T, int NP, int kMode>
 struct HeadSmem {
     static constexpr int kWide = kHeadSteps * (NP + kHeadPad) * static_cast<int>(sizeof(T));
     static constexpr int kNarrow = kHeadSteps * (kHeadCols + kHeadPad) * static_cast<int>(sizeof(T));
     static constexpr int kStage = (kMode == kHeadForward ? 2 : 1) * kWide + kNarrow;
     static constexpr int kStages = 2 * kStage + (kMode == kHeadForward ? kWide : 0) <= 200 * 1024 ? 2 : 1;
+    static constexpr bool kOverC = NP >= kHeadCols;                        // staging of the outputs: rows as wide as theirs
     static constexpr int kState = kStages * kStage;
-    static constexpr int kFactors = kState + (kMode == kHeadForward ? kWide : 0);
+    static constexpr int kStaging = kState + (kMode == kHeadForward ? kWide : 0);
+    static constexpr int kFactors = kStaging + (kMode == kHeadForward && sizeof(T) == 2 && !kOverC ? kNarrow : 0);
     static constexpr int kPowers = kFactors + 2 * static_cast<int>(sizeof(HeadFactors));
     static constexpr int kBytes = kPowers + 4 * 4;
 };
@@ -705,20 +705,7 @@ __device__ __forceinline__ bool not_finite(const HeadB<T> (&v)[N][2])
     }
 }
 
-// The four lanes of a quad hold two columns each of four 8-column tiles, packed: lane t gets all eight columns of tile t.
-__device__ __forceinline__ void quad_transpose(uint32_t (&r)[4], int t)
-{
-#pragma unroll
-    for (int d = 1; d < 4; d <<= 1)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (!(i & d)) {
-                const uint32_t send = t & d ? r[i] : r[i + d], got = __shfl_xor_sync(0xffffffffu, send, d);
-                (t & d ? r[i] : r[i + d]) = got;
-            }
-}
-
-template <typename T, int NP, int kMode>
+template <typename T, int NP, int kMode, bool kWhole>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(const HeadParams p)
 {
     using M = HeadSmem<T, NP, kMode>;
@@ -760,9 +747,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
     const auto load = [&](int chunk, int s) {
         const int first = chunk * kHeadSteps, rows = a.n - first;
         const int64_t sign = reverse ? -1 : 1, at = token(first);
-        load_rows<kHeadCols, 256>(tile_u(s), u + at * u_l, sign * u_l, rows, a.cols, p.unit);
-        load_rows<NP, 256>(tile_B(s), B + at * B_l, sign * B_l, rows, p.states, p.unit);
-        if (kOut) load_rows<NP, 256>(tile_C(s), C + at * p.C_l, sign * p.C_l, rows, p.states, p.unit);
+        load_rows<kHeadCols, 256, kWhole>(tile_u(s), u + at * u_l, sign * u_l, rows, a.cols, p.unit);
+        load_rows<NP, 256, kWhole>(tile_B(s), B + at * B_l, sign * B_l, rows, p.states, p.unit);
+        if (kOut) load_rows<NP, 256, kWhole>(tile_C(s), C + at * p.C_l, sign * p.C_l, rows, p.states, p.unit);
         cp_async_commit();
     };
 
@@ -770,16 +757,6 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
     const int64_t state_size = static_cast<int64_t>(p.cols) * p.states, tile_at = static_cast<int64_t>(a.tile) * kHeadCols * p.states;
     const int count = chunk1 - chunk0;
     const auto chunk_of = [&](int i) { return kGrad ? chunk1 - 1 - i : chunk0 + i; };
-    // One of warps 4 .. 7 forms the factors of chunk i + 1 while chunk i is worked on; it has read delta a chunk before that.
-    float delta[2] = {};
-    if (count > 0) {
-        load(chunk_of(0), 0);
-        if (warp == 4) {
-            load_delta<T>(p, delta_at, chunk_of(0) * kHeadSteps, a.n, lane, delta);
-            write_factors<kMode>(factors[0], head_steps(p, delta, bias, A2, chunk_of(0) * kHeadSteps, a.n, lane), lane);
-            if (count > 1) load_delta<T>(p, delta_at, chunk_of(1) * kHeadSteps, a.n, lane, delta);
-        }
-    }
     float S[kN][4];
     {
         const float *from = nullptr;
@@ -788,7 +765,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
             from = p.slots + (head_at * p.segments + (seg > 0 ? seg : p.segments) - 1) * state_size + tile_at;
         else if (kOut && p.state)
             from = p.state + head_at * state_size + tile_at;
-        if (!outputs) read_state<kN>(S, from, p0, n0, a.cols, p.states, lane);
+        if (!outputs) read_state<kWhole>(S, from, p0, n0, a.cols, p.states, lane);
     }
     const bool started = kOut && (seg > 0 || p.state);    // else the state in front of the first chunk is zero
     double log_decay = 0.0;
@@ -796,7 +773,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
     // the state as an operand: its columns brought into binary16's range
     const auto publish = [&](int chunk) {
         if (p.history && busy)
-            write_state<kN>(S, p.history + ((static_cast<int64_t>(a.b) * p.chunks + chunk) * p.heads + a.h) * state_size + tile_at, p0, n0, a.cols, p.states, lane);
+            write_state<kWhole>(S, p.history + ((static_cast<int64_t>(a.b) * p.chunks + chunk) * p.heads + a.h) * state_size + tile_at, p0, n0, a.cols, p.states, lane);
         HeadScale sc = {1.0f, 1.0f};
         if constexpr (kScaled<T>) {
             sc = scale_for(warp_top<kN>(S));
@@ -814,31 +791,33 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
         else
             store(sc.up);
     };
-    if (kOut && !outputs && count > 0) publish(chunk0);
-    for (int i = 0; i < count; ++i) {
+    // Tiles come a chunk ahead.  Of warps 4 .. 7 the one with the number of the chunk forms the factors of its steps a chunk ahead; it has read
+    // delta a chunk before that.
+    float delta[2] = {};
+    if (warp == 4 && count > 0) load_delta<T>(p, delta_at, chunk_of(0) * kHeadSteps, a.n, lane, delta);
+    for (int i = -1; i < count; ++i) {
         const int chunk = chunk_of(i), first = chunk * kHeadSteps, s = i & 1;
-        cp_async_wait<0>();
-        __syncthreads();                                  // the tiles, their steps' factors, and the state as an operand; the last chunk is done
-        if (M::kStages == 2 && i + 1 < count) load(chunk_of(i + 1), s ^ 1);
-        if (warp == 4 + ((i + 1) & 3) && i + 2 < count) load_delta<T>(p, delta_at, chunk_of(i + 2) * kHeadSteps, a.n, lane, delta);
+        const bool next = i + 1 < count;
+        if (i >= 0) {
+            cp_async_wait<0>();
+            __syncthreads();                              // the tiles, their steps' factors, and the state as an operand; the last chunk is done
+        }
+        if (M::kStages == 2 && next) load(chunk_of(i + 1), s ^ 1);
         const HeadFactors &f = factors[s];
-        const float decay = f.decay;
-        log_decay += f.log_decay;
-
-        if (outputs) {
+        if (outputs && i >= 0) {
             const float *pair = f.pair[r];
-            const float l0 = pair[p0 + g], l1 = pair[p0 + g + 8];
+            const float l0 = pair[p0 + g], l1 = pair[p0 + g + 8], r0 = fast_exp2(l0), r1 = fast_exp2(l1);
             float y[8][4] = {};
             if (i > 0 || started) {                        // what the state gives these 16 steps
-#pragma unroll
+#pragma unroll 2
                 for (int k = 0; k < NP / 16; ++k) {
                     const HeadA<T> c = load_a(tile_C(s), kWP, p0, 16 * k, lane);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         HeadB<T> b[2];
                         load_b(b, state_s, kWP, 16 * j, 16 * k, lane);
-                        head_mma(y[2 * j], c, b[0], k == 0);
-                        head_mma(y[2 * j + 1], c, b[1], k == 0);
+                        head_mma(y[2 * j], c, b[0]);
+                        head_mma(y[2 * j + 1], c, b[1]);
                     }
                 }
                 const float R0 = f.into[p0 + g], R1 = f.into[p0 + g + 8];
@@ -854,34 +833,45 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
             asm volatile("bar.arrive 1, 256;" ::: "memory");           // the state and its powers have been read
             // and what the steps up to them give, 16 at a time, the ones on the diagonal last
             HeadScale sc = {1.0f, 1.0f};
-            const auto add = [&](int j, bool diagonal) {
-                float m[2][4];
+#pragma unroll 1
+            for (int j = 0; j <= r; ++j) {
+                const bool diagonal = j == r;
+                float m[2][4], odd[2][4];                  // two chains of products each
 #pragma unroll
-                for (int k = 0; k < NP / 16; ++k) {
-                    HeadB<T> b[2];
+                for (int k = 0; k < NP / 16; k += 2) {
+                    HeadB<T> b[2], e[2];
                     load_b(b, tile_B(s), kWP, 16 * j, 16 * k, lane);
                     const HeadA<T> c = load_a(tile_C(s), kWP, p0, 16 * k, lane);
-                    head_mma(m[0], c, b[0], k == 0);
-                    head_mma(m[1], c, b[1], k == 0);
+                    load_b(e, tile_B(s), kWP, 16 * j, 16 * k + 16, lane);
+                    const HeadA<T> d = load_a(tile_C(s), kWP, p0, 16 * k + 16, lane);
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        head_mma(m[n], c, b[n], k == 0);
+                        head_mma(odd[n], d, e[n], k == 0);
+                    }
                 }
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
                     const int col = 16 * j + 8 * n + 2 * t;
                     const float2 v = *reinterpret_cast<const float2 *>(pair + col);
+                    float f00, f01, f10, f11;              // factors of the rows p0 + g and p0 + g + 8
                     if (!diagonal) {
-                        const float r0 = fast_exp2(l0), r1 = fast_exp2(l1);
-                        m[n][0] *= r0 * v.x;
-                        m[n][1] *= r0 * v.y;
-                        m[n][2] *= r1 * v.x;
-                        m[n][3] *= r1 * v.y;
+                        f00 = r0 * v.x;
+                        f01 = r0 * v.y;
+                        f10 = r1 * v.x;
+                        f11 = r1 * v.y;
                     } else {
                         const float2 w = *reinterpret_cast<const float2 *>(f.w + col);
-                        const int row = p0 + g;
-                        m[n][0] = col <= row ? m[n][0] * (fast_exp2(l0 - v.x) * w.x) : 0.0f;
-                        m[n][1] = col + 1 <= row ? m[n][1] * (fast_exp2(l0 - v.y) * w.y) : 0.0f;
-                        m[n][2] = col <= row + 8 ? m[n][2] * (fast_exp2(l1 - v.x) * w.x) : 0.0f;
-                        m[n][3] = col + 1 <= row + 8 ? m[n][3] * (fast_exp2(l1 - v.y) * w.y) : 0.0f;
+                        f00 = fast_exp2(l0 - v.x) * w.x;
+                        f01 = fast_exp2(l0 - v.y) * w.y;
+                        f10 = fast_exp2(l1 - v.x) * w.x;
+                        f11 = fast_exp2(l1 - v.y) * w.y;
                     }
+                    const int row = diagonal ? p0 + g : kHeadSteps;                    // in front of the diagonal all count
+                    m[n][0] = col <= row ? (m[n][0] + odd[n][0]) * f00 : 0.0f;
+                    m[n][1] = col + 1 <= row ? (m[n][1] + odd[n][1]) * f01 : 0.0f;
+                    m[n][2] = col <= row + 8 ? (m[n][2] + odd[n][2]) * f10 : 0.0f;
+                    m[n][3] = col + 1 <= row + 8 ? (m[n][3] + odd[n][3]) * f11 : 0.0f;
                 }
                 if constexpr (kScaled<T>) {                // y is in the units of the smallest power of two so far
                     const HeadScale now = scale_for(warp_top<2>(m));
@@ -924,18 +914,15 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
                             }
                         }
                     }
-                    return;
-                }
-                const HeadA<T> w = acc_to_a<T>(m[0], m[1], 1.0f);
+                } else {
+                    const HeadA<T> w = acc_to_a<T>(m[0], m[1], 1.0f);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    head_mma(y[2 * q], w, v[q][0]);
-                    head_mma(y[2 * q + 1], w, v[q][1]);
+                    for (int q = 0; q < 4; ++q) {
+                        head_mma(y[2 * q], w, v[q][0]);
+                        head_mma(y[2 * q + 1], w, v[q][1]);
+                    }
                 }
-            };
-#pragma unroll 1
-            for (int j = 0; j < r; ++j) add(j, false);
-            add(r, true);
+            }
             if (kScaled<T> && sc.down != 1.0f) {
 #pragma unroll
                 for (int n = 0; n < 8; ++n)
@@ -943,48 +930,52 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
                     for (int k = 0; k < 4; ++k) y[n][k] *= sc.down;
             }
             const int step0 = first + p0 + g, step1 = step0 + 8;
+            // through shared memory (16-bit values: over this warp's rows of C, which nobody else reads) to whole 16-byte stores
+            T *stage = M::kOverC ? tile_C(s) + p0 * kWP : reinterpret_cast<T *>(smem + M::kStaging) + p0 * kXP;
+            if (M::kOverC) __syncwarp();
 #pragma unroll
-            for (int h = 0; h < 2; ++h)                            // 32 columns at a time
+            for (int n = 0; n < 8; ++n)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const int step = k ? step1 : step0;
-                    T *row = y_at + token(step) * y_l;
-                    uint32_t out[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int c = 32 * h + 8 * j + 2 * t;
-                        float v0 = y[4 * h + j][2 * k], v1 = y[4 * h + j][2 * k + 1];
-                        if (p.D) {
-                            const float2 x = head_pair(tile_u(s) + (p0 + g + 8 * k) * kXP + c);
-                            v0 = fmaf(skip, x.x, v0);
-                            v1 = fmaf(skip, x.y, v1);
-                        }
-                        if constexpr (sizeof(T) == 2) out[j] = head_pack<T>(v0, v1);
-                        if (sizeof(T) == 4 || p.out_unit < 16) {
-                            if (step >= a.n || c >= a.cols) continue;
-                            if (p.out_unit >= 2 * static_cast<int>(sizeof(T))) {
-                                head_store_pair(row + c, v0, v1);
-                            } else {
-                                row[c] = head_round<T>(v0);
-                                if (c + 1 < a.cols) row[c + 1] = head_round<T>(v1);
-                            }
-                        }
+                    const int c = 8 * n + 2 * t, step = k ? step1 : step0;
+                    float v0 = y[n][2 * k], v1 = y[n][2 * k + 1];
+                    if (p.D) {
+                        const float2 x = head_pair(tile_u(s) + (p0 + g + 8 * k) * kXP + c);
+                        v0 = fmaf(skip, x.x, v0);
+                        v1 = fmaf(skip, x.y, v1);
                     }
-                    if (sizeof(T) == 2 && p.out_unit == 16) {      // 16 bytes of a row a lane
-                        quad_transpose(out, t);
-                        const int c = 32 * h + 8 * t;
-                        if (step < a.n && c < a.cols) *reinterpret_cast<uint4 *>(row + c) = make_uint4(out[0], out[1], out[2], out[3]);
+                    if (sizeof(T) == 2 && kWhole) {
+                        head_store_pair(stage + (g + 8 * k) * kXP + c, v0, v1);
+                    } else if (step < a.n && c < a.cols) {
+                        T *to = y_at + token(step) * y_l + c;
+                        if (kWhole || p.out_unit >= 2 * static_cast<int>(sizeof(T))) {
+                            head_store_pair(to, v0, v1);
+                        } else {
+                            to[0] = head_round<T>(v0);
+                            if (c + 1 < a.cols) to[1] = head_round<T>(v1);
+                        }
                     }
                 }
+            if (sizeof(T) == 2 && kWhole) {
+                __syncwarp();
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int row = 4 * q + (lane >> 3), c = 8 * (lane & 7), step = first + p0 + row;
+                    if (step < a.n && c < a.cols)
+                        *reinterpret_cast<uint4 *>(y_at + token(step) * y_l + c) = *reinterpret_cast<const uint4 *>(stage + row * kXP + c);
+                }
+            }
         }
-        if (busy) state_update<NP, kN>(S, tile_u(s), tile_B(s), f.state, decay, p0, n0, lane);
-        if (kOut && !outputs) {
-            asm volatile("bar.sync 1, 256;" ::: "memory");             // the outputs' warps have read the state
-            if (i + 1 < count) publish(chunk + 1);
+        if (i >= 0) {
+            log_decay += f.log_decay;
+            if (busy) state_update<NP, kN>(S, tile_u(s), tile_B(s), f.state, f.decay, p0, n0, lane);
+            if (kOut && !outputs) asm volatile("bar.sync 1, 256;" ::: "memory");           // the outputs' warps have read the state
         }
-        if (warp == 4 + (i & 3) && i + 1 < count)
+        if (kOut && !outputs && next) publish(chunk_of(i + 1));
+        if (warp == 4 + ((i + 1) & 3) && next)
             write_factors<kMode>(factors[s ^ 1], head_steps(p, delta, bias, A2, chunk_of(i + 1) * kHeadSteps, a.n, lane), lane);
-        if (M::kStages == 1 && i + 1 < count) {
+        if (warp == 4 + ((i + 2) & 3) && i + 2 < count) load_delta<T>(p, delta_at, chunk_of(i + 2) * kHeadSteps, a.n, lane, delta);
+        if (M::kStages == 1 && next) {
             __syncthreads();
             load(chunk_of(i + 1), 0);
         }
@@ -992,9 +983,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
     if constexpr (kOut) {
         // final states: by the segment that holds the last step, or the first one of an empty sequence
         if (!outputs && p.final_state && seg == (chunks > 0 ? (chunks - 1) / p.segment_chunks : 0))
-            write_state<kN>(S, p.final_state + head_at * state_size + tile_at, p0, n0, a.cols, p.states, lane);
+            write_state<kWhole>(S, p.final_state + head_at * state_size + tile_at, p0, n0, a.cols, p.states, lane);
     } else {
-        write_state<kN>(S, p.slots + (head_at * p.segments + seg) * state_size + tile_at, p0, n0, a.cols, p.states, lane);
+        write_state<kWhole>(S, p.slots + (head_at * p.segments + seg) * state_size + tile_at, p0, n0, a.cols, p.states, lane);
         if (threadIdx.x == 0 && a.tile == 0) p.logs[head_at * p.segments + seg] = static_cast<float>(log_decay);
         griddep_launch_dependents();
     }

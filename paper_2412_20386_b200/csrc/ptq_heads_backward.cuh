@@ -116,11 +116,10 @@ __device__ __forceinline__ HeadScale scale_of(const float (&d)[N][4])
     return sc;
 }
 // Two rows of binary32 parts, 8 n + 2 t columns of each.
-template <int NP>
+template <int NP, bool kPairs>
 __device__ __forceinline__ void write_part(const float (&d)[NP / 8][4], float *row0, float *row1, int states, int lane)
 {
     const int t = lane & 3;
-    const bool pairs = states % 2 == 0;
 #pragma unroll
     for (int n = 0; n < NP / 8; ++n)
 #pragma unroll
@@ -128,7 +127,7 @@ __device__ __forceinline__ void write_part(const float (&d)[NP / 8][4], float *r
             float *row = k ? row1 : row0;
             const int c = 8 * n + 2 * t;
             if (!row || c >= states) continue;
-            if (pairs) {
+            if constexpr (kPairs) {
                 *reinterpret_cast<float2 *>(row + c) = make_float2(d[n][2 * k], d[n][2 * k + 1]);
             } else {
                 row[c] = d[n][2 * k];
@@ -137,7 +136,7 @@ __device__ __forceinline__ void write_part(const float (&d)[NP / 8][4], float *r
         }
 }
 
-template <typename T, int NP>
+template <typename T, int NP, bool kWhole>
 __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParams p)
 {
     using M = HeadBackSmem<T, NP>;
@@ -186,10 +185,10 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
     const auto load = [&](int chunk, int s) {
         const int first = chunk * kHeadSteps, rows = a.n - first;
         const int64_t sign = reverse ? -1 : 1, at = token(first);
-        load_rows<kHeadCols, 256>(tile_u(s), u + at * p.u_l, sign * p.u_l, rows, a.cols, p.unit);
-        load_rows<kHeadCols, 256>(tile_dy(s), dy + at * dy_l, sign * dy_l, rows, a.cols, p.unit);
-        load_rows<NP, 256>(tile_B(s), B + at * p.B_l, sign * p.B_l, rows, p.states, p.unit);
-        load_rows<NP, 256>(tile_C(s), C + at * p.C_l, sign * p.C_l, rows, p.states, p.unit);
+        load_rows<kHeadCols, 256, kWhole>(tile_u(s), u + at * p.u_l, sign * p.u_l, rows, a.cols, p.unit);
+        load_rows<kHeadCols, 256, kWhole>(tile_dy(s), dy + at * dy_l, sign * dy_l, rows, a.cols, p.unit);
+        load_rows<NP, 256, kWhole>(tile_B(s), B + at * p.B_l, sign * p.B_l, rows, p.states, p.unit);
+        load_rows<NP, 256, kWhole>(tile_C(s), C + at * p.C_l, sign * p.C_l, rows, p.states, p.unit);
         cp_async_commit();
     };
     const auto kept = [&](int chunk) {
@@ -205,13 +204,13 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
             from = p.slots + (head_at * p.segments + a.seg + 1) * state_size + tile_at;
         else if (p.dfinal)
             from = p.dfinal + head_at * state_size + tile_at;
-        read_state<NP / 8>(H, from, p0, 0, a.cols, p.states, lane);
+        read_state<kWhole>(H, from, p0, 0, a.cols, p.states, lane);
     }
     float delta[2] = {};
     if (chunk1 > chunk0) {
         load(chunk1 - 1, 0);
         load_delta<T>(p, delta_at, (chunk1 - 1) * kHeadSteps, a.n, lane, delta);
-        if (!rows_i) read_state<NP / 8>(H, kept(chunk1 - 1), p0, 0, a.cols, p.states, lane);
+        if (!rows_i) read_state<kWhole>(H, kept(chunk1 - 1), p0, 0, a.cols, p.states, lane);
     }
     for (int chunk = chunk1 - 1, s = 0; chunk >= chunk0; --chunk, s ^= 1) {
         const int first = chunk * kHeadSteps;
@@ -249,7 +248,7 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
         if (M::kStages == 2 && chunk > chunk0) load(chunk - 1, s ^ 1);
         if (chunk > chunk0) {
             load_delta<T>(p, delta_at, first - kHeadSteps, a.n, lane, delta);
-            if (!rows_i) read_state<NP / 8>(H, kept(chunk - 1), p0, 0, a.cols, p.states, lane);
+            if (!rows_i) read_state<kWhole>(H, kept(chunk - 1), p0, 0, a.cols, p.states, lane);
         }
         const int step0 = first + p0 + g, step1 = step0 + 8;
         const float l0 = vC[p0 + g], l1 = vC[p0 + g + 8];
@@ -342,7 +341,7 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
                     }
                 }
             if constexpr (kScaled<T>) scale_rows(d, sc.down, sc.down);
-            write_part<NP>(d, step0 < a.n ? p.part_C + (part_row + token(step0)) * p.states : nullptr,
+            write_part<NP, kWhole>(d, step0 < a.n ? p.part_C + (part_row + token(step0)) * p.states : nullptr,
                            step1 < a.n ? p.part_C + (part_row + token(step1)) * p.states : nullptr, p.states, lane);
             // <G, S> of this warp's columns, and G in front of the chunk
             float z = 0.0f;
@@ -445,7 +444,7 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
                         const float2 y = head_pair(tile_dy(s) + (p0 + g + 8 * k) * kXP + c);
                         const float v0 = p.D ? fmaf(skip, y.x, d[n][2 * k]) : d[n][2 * k], v1 = p.D ? fmaf(skip, y.y, d[n][2 * k + 1]) : d[n][2 * k + 1];
                         T *to = du + token(step) * dy_l + c;
-                        if (p.out_unit >= 2 * static_cast<int>(sizeof(T))) {
+                        if (kWhole || p.out_unit >= 2 * static_cast<int>(sizeof(T))) {
                             head_store_pair(to, v0, v1);
                         } else {
                             to[0] = head_round<T>(v0);
@@ -485,7 +484,7 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
                     }
                 }
             scale_rows(d, w0 * sc.down, w1 * sc.down);
-            write_part<NP>(d, step0 < a.n ? p.part_B + (part_row + token(step0)) * p.states : nullptr,
+            write_part<NP, kWhole>(d, step0 < a.n ? p.part_B + (part_row + token(step0)) * p.states : nullptr,
                            step1 < a.n ? p.part_B + (part_row + token(step1)) * p.states : nullptr, p.states, lane);
         }
         __syncthreads();                                  // the sums; S and G as operands, and the tiles, have been read
@@ -525,7 +524,7 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
         }
     }
     if (rows_i) {
-        if (a.seg == 0 && p.final_state) write_state<NP / 8>(H, p.final_state + head_at * state_size + tile_at, p0, 0, a.cols, p.states, lane);
+        if (a.seg == 0 && p.final_state) write_state<kWhole>(H, p.final_state + head_at * state_size + tile_at, p0, 0, a.cols, p.states, lane);
 #pragma unroll
         for (int q = 16; q > 0; q >>= 1) skip_grad += __shfl_xor_sync(0xffffffffu, skip_grad, q);
         if (lane == 0) skip_sum[r] = skip_grad;
