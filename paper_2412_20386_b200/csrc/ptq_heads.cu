@@ -254,7 +254,7 @@ ptq_status_t ptq_heads_backward(const ptq_heads_t *s, const float *history, cons
         }
         PTQ_TRY(Launch::backward(p, whole, plan.segments > 1, st));
         PTQ_TRY(launch_next(ptq::ptq_heads_finish_kernel<T>, dim3(static_cast<unsigned>(sums), 2), 256, 0, st, p, static_cast<T *>(g->dB), static_cast<T *>(g->dC)));
-        PTQ_TRY(launch_next(ptq::ptq_heads_finish_delta_kernel<T>, dim3(static_cast<unsigned>(s->batch * s->heads)), 128, 0, st, p, static_cast<T *>(g->ddelta), shares));
+        PTQ_TRY(launch_next(ptq::ptq_heads_finish_delta_kernel<T>, dim3(static_cast<unsigned>(s->batch * s->heads)), 512, 0, st, p, static_cast<T *>(g->ddelta), shares));
         return launch_next(ptq::ptq_heads_finish_sums_kernel, dim3(static_cast<unsigned>(s->heads)), 128, 0, st, p, shares, g->dA, g->ddelta_bias, g->dD);
     });
 }

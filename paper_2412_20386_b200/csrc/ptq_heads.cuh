@@ -1016,7 +1016,7 @@ __global__ void __launch_bounds__(128) ptq_heads_step_kernel(const HeadParams p)
         const float *row = from + static_cast<int64_t>(c) * p.states + n0;
         if constexpr (kWhole) {
             if (n0 < p.states) {
-                const float4 x = *reinterpret_cast<const float4 *>(row);
+                const float4 x = __ldcs(reinterpret_cast<const float4 *>(row));
                 v[r][0] = x.x, v[r][1] = x.y, v[r][2] = x.z, v[r][3] = x.w;
             }
         } else {
@@ -1054,7 +1054,7 @@ __global__ void __launch_bounds__(128) ptq_heads_step_kernel(const HeadParams p)
         if (p.final_state) {
             float *row = p.final_state + base + static_cast<int64_t>(c) * p.states + n0;
             if constexpr (kWhole) {
-                if (n0 < p.states) *reinterpret_cast<float4 *>(row) = make_float4(v[r][0], v[r][1], v[r][2], v[r][3]);
+                if (n0 < p.states) __stcs(reinterpret_cast<float4 *>(row), make_float4(v[r][0], v[r][1], v[r][2], v[r][3]));
             } else {
 #pragma unroll
                 for (int k = 0; k < 4; ++k)

@@ -19,17 +19,49 @@
 
 namespace ptq {
 
+// Factors of a chunk's steps, which one warp forms for all, a chunk ahead.  `pair[r]` refers to the steps' 16 steps r: of steps in front of
+// them e^{L_ref - L_j} (ref: the step in front of the 16), of themselves log2 e^{L_j - L_ref}, of steps behind them e^{L_i - L_last} (last: the
+// last of the 16).
+struct HeadBackFactors {
+    float w[kHeadSteps], into[kHeadSteps];                // e^{L}
+    float pair[4][kHeadSteps];
+    float rest[4];                                        // log2 e^{L_64 - L_ref}
+    float decay, pad[3];                                  // e^{L_64}
+};
+__device__ __forceinline__ void write_back_factors(HeadBackFactors &f, const HeadSteps &st, int lane)
+{
+    const double all = __shfl_sync(0xffffffffu, st.sum[1], 31);
+    reinterpret_cast<float2 *>(f.w)[lane] = make_float2(st.w[0], st.w[1]);
+    reinterpret_cast<float2 *>(f.into)[lane] = make_float2(pow2(st.sum[0]), pow2(st.sum[1]));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const double ref = r ? __shfl_sync(0xffffffffu, st.sum[1], 8 * r - 1) : 0.0, last = __shfl_sync(0xffffffffu, st.sum[1], 8 * r + 7);
+        float v[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            v[k] = lane < 8 * r ? pow2(ref - st.sum[k]) : lane < 8 * r + 8 ? static_cast<float>(st.sum[k] - ref) : pow2(st.sum[k] - last);
+        reinterpret_cast<float2 *>(f.pair[r])[lane] = make_float2(v[0], v[1]);
+        if (lane == r) f.rest[r] = static_cast<float>(all - ref);
+    }
+    if (lane == 0) f.decay = pow2(all);
+}
+
 template <typename T, int NP>
 struct HeadBackSmem {
     static constexpr int kWide = kHeadSteps * (NP + kHeadPad) * static_cast<int>(sizeof(T));
     static constexpr int kNarrow = kHeadSteps * (kHeadCols + kHeadPad) * static_cast<int>(sizeof(T));
     static constexpr int kStage = 2 * kWide + 2 * kNarrow;
     static constexpr int kParts = kHeadParts<T>;                           // of S and G as operands
-    static constexpr int kStages = 2 * kStage + 2 * kParts * kWide <= 220 * 1024 ? 2 : 1;
+    static constexpr int kSums = 7 * kHeadSteps * 4;                       // floats: C . dC', dw, B . dB', 4 warps' K
+    static constexpr int kOther = 2 * kParts * kWide + 2 * static_cast<int>(sizeof(HeadBackFactors)) + kSums + 16 * 4;
+    // two CTAs to an SM where that is possible, else two stages
+    static constexpr int kCtas = sizeof(T) == 2 && NP <= 64 ? 2 : 1;
+    static constexpr int kStages = 2 * kStage + kOther <= (kCtas == 2 ? 113 : 227) * 1024 ? 2 : 1;
     static constexpr int kS = kStages * kStage;
     static constexpr int kG = kS + kParts * kWide;
-    static constexpr int kFactors = kG + kParts * kWide;                   // floats: w, e^{L}, e^{L_64 - L}, C . dC', dw, B . dB', 8 warps' own, 4 warps' K
-    static constexpr int kSmall = kFactors + (6 + 8 + 4) * kHeadSteps * 4;     // floats: largest magnitudes [8], <G, S> [4], dD [4]
+    static constexpr int kFactors = kG + kParts * kWide;
+    static constexpr int kSum = kFactors + 2 * static_cast<int>(sizeof(HeadBackFactors));
+    static constexpr int kSmall = kSum + kSums;                            // floats: largest magnitudes [8], <G, S> [4], dD [4]
     static constexpr int kBytes = kSmall + 16 * 4;
 };
 
@@ -101,20 +133,6 @@ __device__ __forceinline__ void scale_rows(float (&d)[N][4], float s0, float s1)
         d[n][3] *= s1;
     }
 }
-template <typename T, int N>
-__device__ __forceinline__ HeadScale scale_of(const float (&d)[N][4])
-{
-    HeadScale sc = {1.0f, 1.0f};
-    if constexpr (kScaled<T>) {
-        float top = 0.0f;
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) top = fmaxf(top, finite_abs(d[n][k]));
-        sc = scale_for(warp_max(top));
-    }
-    return sc;
-}
 // Two rows of binary32 parts, 8 n + 2 t columns of each.
 template <int NP, bool kPairs>
 __device__ __forceinline__ void write_part(const float (&d)[NP / 8][4], float *row0, float *row1, int states, int lane)
@@ -136,8 +154,48 @@ __device__ __forceinline__ void write_part(const float (&d)[NP / 8][4], float *r
         }
 }
 
+// Sixteen more steps of M R or M P as an operand: brings `sums`, which it is multiplied into, and `m` to a common power of two.
+template <typename T, int N>
+__device__ __forceinline__ void join_scale(float (&m)[2][4], float (&sums)[N][4], HeadScale &sc, bool first)
+{
+    if constexpr (kScaled<T>) {
+        const HeadScale now = scale_for(warp_top<2>(m));
+        if (first ? now.up != 1.0f : now.up < sc.up) {
+            const float by = now.up * sc.down;
+            scale_rows(sums, by, by);
+            sc = now;
+        }
+        if (sc.up != 1.0f) scale_rows(m, sc.up, sc.up);
+    }
+}
+// 16 x 16 scores: rows p0 .. of the one tile with rows q0 .. of the other, over kK columns.
+template <int kK, typename T>
+__device__ __forceinline__ void scores(float (&d)[2][4], const T *rows, const T *cols, int p0, int q0, int lane)
+{
+#pragma unroll
+    for (int k = 0; k < kK / 16; ++k) {
+        HeadB<T> b[2];
+        load_b(b, cols, kK + kHeadPad, q0, 16 * k, lane);
+        const HeadA<T> a = load_a(rows, kK + kHeadPad, p0, 16 * k, lane);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) head_mma(d[n], a, b[n], k == 0);
+    }
+}
+// d[n] += a times the 16 rows k0 .. of a tile [k][n].
+template <int NP, typename T>
+__device__ __forceinline__ void mma_rows(float (&d)[NP / 8][4], const HeadA<T> &a, const T *tile, int k0, int lane)
+{
+#pragma unroll
+    for (int n = 0; n < NP / 16; ++n) {
+        HeadB<T> b[2];
+        load_b_t(b, tile, NP + kHeadPad, 16 * n, k0, lane);
+        head_mma(d[2 * n], a, b[0]);
+        head_mma(d[2 * n + 1], a, b[1]);
+    }
+}
+
 template <typename T, int NP, bool kWhole>
-__global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParams p)
+__global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_backward_kernel(const HeadParams p)
 {
     using M = HeadBackSmem<T, NP>;
     constexpr int kWP = NP + kHeadPad, kXP = kHeadCols + kHeadPad;
@@ -147,7 +205,7 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
     if (p.segments > 1) griddep_wait();
     const HeadPlace a = head_place(p, p.segments);
     const int chunks = (a.n + kHeadSteps - 1) / kHeadSteps;
-    const int chunk0 = min(chunks, a.seg * p.segment_chunks), chunk1 = min(chunks, chunk0 + p.segment_chunks);
+    const int chunk0 = min(chunks, a.seg * p.segment_chunks), chunk1 = min(chunks, chunk0 + p.segment_chunks), count = chunk1 - chunk0;
     const bool reverse = p.flags & kHeadsReverse;
     const auto stage = [&](int s) { return smem + (M::kStages == 2 ? s * M::kStage : 0); };
     const auto tile_u = [&](int s) { return reinterpret_cast<T *>(stage(s)); };
@@ -155,9 +213,9 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
     const auto tile_B = [&](int s) { return reinterpret_cast<T *>(stage(s) + 2 * M::kNarrow); };
     const auto tile_C = [&](int s) { return reinterpret_cast<T *>(stage(s) + 2 * M::kNarrow + M::kWide); };
     T *S_op = reinterpret_cast<T *>(smem + M::kS), *G_op = reinterpret_cast<T *>(smem + M::kG);
-    float *vW = reinterpret_cast<float *>(smem + M::kFactors), *vR = vW + kHeadSteps, *vE = vW + 2 * kHeadSteps;
-    float *dot_C = vW + 3 * kHeadSteps, *dw = vW + 4 * kHeadSteps, *dot_B = vW + 5 * kHeadSteps, *vC = vW + (6 + warp) * kHeadSteps;
-    float *pairs = vW + 14 * kHeadSteps;                  // [4]: what a warp's rows of K w pass over each step
+    HeadBackFactors *factors = reinterpret_cast<HeadBackFactors *>(smem + M::kFactors);
+    float *dot_C = reinterpret_cast<float *>(smem + M::kSum), *dw = dot_C + kHeadSteps, *dot_B = dot_C + 2 * kHeadSteps;
+    float *pairs = dot_C + 3 * kHeadSteps;                // [4]: what a warp's rows of K w pass over each step
     float *tops = reinterpret_cast<float *>(smem + M::kSmall), *through = tops + 8, *skip_sum = tops + 12;
 
     const int64_t dy_l = static_cast<int64_t>(p.heads) * p.cols;
@@ -191,11 +249,9 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
         load_rows<NP, 256, kWhole>(tile_C(s), C + at * p.C_l, sign * p.C_l, rows, p.states, p.unit);
         cp_async_commit();
     };
-    const auto kept = [&](int chunk) {
-        return p.kept + ((static_cast<int64_t>(a.b) * p.chunks + chunk) * p.heads + a.h) * state_size + tile_at;
-    };
+    const auto chunk_of = [&](int i) { return chunk1 - 1 - i; };
 
-    // warps of rows i: G; of rows j: S of the chunk that comes
+    // warps of rows i: G; of rows j, between chunks: S of the one that comes
     float H[NP / 8][4];
     float skip_grad = 0.0f;
     if (rows_i) {
@@ -206,143 +262,91 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
             from = p.dfinal + head_at * state_size + tile_at;
         read_state<kWhole>(H, from, p0, 0, a.cols, p.states, lane);
     }
-    float delta[2] = {};
-    if (chunk1 > chunk0) {
-        load(chunk1 - 1, 0);
-        load_delta<T>(p, delta_at, (chunk1 - 1) * kHeadSteps, a.n, lane, delta);
-        if (!rows_i) read_state<kWhole>(H, kept(chunk1 - 1), p0, 0, a.cols, p.states, lane);
-    }
-    for (int chunk = chunk1 - 1, s = 0; chunk >= chunk0; --chunk, s ^= 1) {
-        const int first = chunk * kHeadSteps;
+    float delta[2] = {};                                  // of the next chunk, in warp 0, which forms the factors
+    if (warp == 0 && count > 0) load_delta<T>(p, delta_at, chunk_of(0) * kHeadSteps, a.n, lane, delta);
+    for (int i = -1; i < count; ++i) {
+        const int chunk = chunk_of(i), first = chunk * kHeadSteps, s = i & 1;
+        const bool next = i + 1 < count;
+        const HeadBackFactors &f = factors[s];
         HeadScale scS = {1.0f, 1.0f}, scG = {1.0f, 1.0f};
-        if constexpr (kScaled<T>) {                       // one power of two for all columns: they are summed over
-            float top = 0.0f;
-#pragma unroll
-            for (int n = 0; n < NP / 8; ++n)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) top = fmaxf(top, finite_abs(H[n][k]));
-            top = warp_max(top);
-            if (lane == 0) tops[warp] = top;
-            __syncthreads();
-            scG = scale_for(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
-            scS = scale_for(fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
-        }
-        store_parts<NP>(rows_i ? G_op : S_op, H, rows_i ? scG.up : scS.up, p0, lane);
-        const HeadSteps st = head_steps(p, delta, bias, A2, first, a.n, lane);
-        const double all = sum_at(st, 63), ref = rows_i ? (r ? sum_at(st, 16 * r - 1) : 0.0) : sum_at(st, 16 * r + 15);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int j = 2 * lane + k;
-            if (warp == 0) {
-                vW[j] = st.w[k];
-                vR[j] = pow2(st.sum[k]);
-                vE[j] = pow2(all - st.sum[k]);
+        if (i >= 0) {
+            if constexpr (kScaled<T>) {                   // one power of two for all columns: they are summed over
+                const float top = warp_top<NP / 8>(H);
+                if (lane == 0) tops[warp] = top;
+                __syncthreads();
+                scG = scale_for(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+                scS = scale_for(fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
             }
-            // own steps: the sum; others: their factor (rows i: of earlier steps, rows j: of later ones)
-            const bool other = rows_i ? j < p0 : j >= p0 + 16;
-            vC[j] = other ? pow2(rows_i ? ref - st.sum[k] : st.sum[k] - ref) : static_cast<float>(st.sum[k] - ref);
+            store_parts<NP>(rows_i ? G_op : S_op, H, rows_i ? scG.up : scS.up, p0, lane);
+            cp_async_wait<0>();
+            __syncthreads();
         }
-        const float decay = pow2(all);
-        cp_async_wait<0>();
-        __syncthreads();
-        if (M::kStages == 2 && chunk > chunk0) load(chunk - 1, s ^ 1);
-        if (chunk > chunk0) {
-            load_delta<T>(p, delta_at, first - kHeadSteps, a.n, lane, delta);
-            if (!rows_i) read_state<kWhole>(H, kept(chunk - 1), p0, 0, a.cols, p.states, lane);
-        }
+        if (M::kStages == 2 && next) load(chunk_of(i + 1), s ^ 1);
         const int step0 = first + p0 + g, step1 = step0 + 8;
-        const float l0 = vC[p0 + g], l1 = vC[p0 + g + 8];
-        if (rows_i) {
-            const float r0 = fast_exp2(l0), r1 = fast_exp2(l1);
-            float m[8][4] = {}, run[2] = {};              // M R w; K w of a row summed up to a column
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j <= r) {
-                    float P[2][4] = {};
-#pragma unroll
-                    for (int k = 0; k < NP / 16; ++k) {
-                        const HeadA<T> c = load_a(tile_C(s), kWP, p0, 16 * k, lane);
-                        HeadB<T> b[2];
-                        load_b(b, tile_B(s), kWP, 16 * j, 16 * k, lane);
-                        head_mma(P[0], c, b[0]);
-                        head_mma(P[1], c, b[1]);
-                    }
-#pragma unroll
-                    for (int k = 0; k < kHeadCols / 16; ++k)
-                        if (16 * k < a.cols) {
-                            const HeadA<T> y = load_a(tile_dy(s), kXP, p0, 16 * k, lane);
-                            HeadB<T> b[2];
-                            load_b(b, tile_u(s), kXP, 16 * j, 16 * k, lane);
-                            head_mma(m[2 * j], y, b[0]);
-                            head_mma(m[2 * j + 1], y, b[1]);
-                        }
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int col = 16 * j + 8 * q + 2 * t + (k & 1), row = p0 + g + (k < 2 ? 0 : 8);
-                            float &v = m[2 * j + q][k];
-                            if (col == row) skip_grad += v;
-                            if (j < r)
-                                v *= (k < 2 ? r0 : r1) * vC[col] * vW[col];
-                            else
-                                v = col <= row ? v * (fast_exp2((k < 2 ? l0 : l1) - vC[col]) * vW[col]) : 0.0f;
-                            P[q][k] = j < r || col <= row ? v * P[q][k] : 0.0f;
-                        }
-                    // what passes over step `col`: of each row i >= col its sum up to, not with, col
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        float pass[2] = {};
-                        const int col = 16 * j + 8 * q + 2 * t;
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const int row = p0 + g + 8 * k;
-                            float v = P[q][2 * k] + P[q][2 * k + 1];
-#pragma unroll
-                            for (int z = 1; z < 4; z <<= 1) {
-                                const float w = __shfl_up_sync(0xffffffffu, v, z, 4);
-                                if (t >= z) v += w;
-                            }
-                            const float before = __shfl_up_sync(0xffffffffu, v, 1, 4), at = run[k] + (t ? before : 0.0f);
-                            if (col <= row) pass[0] += at;
-                            if (col + 1 <= row) pass[1] += at + P[q][2 * k];
-                            run[k] += __shfl_sync(0xffffffffu, v, 3, 4);
-                        }
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-#pragma unroll
-                            for (int z = 4; z < 32; z <<= 1) pass[k] += __shfl_xor_sync(0xffffffffu, pass[k], z);
-                            if (g == 0) pairs[r * kHeadSteps + col + k] = pass[k];
-                        }
-                    }
-                }
+        if (i >= 0 && rows_i) {
+            const float *pair = f.pair[r];
+            const float l0 = pair[p0 + g], l1 = pair[p0 + g + 8], r0 = fast_exp2(l0), r1 = fast_exp2(l1);
+            // what the state gives dC
             float d[NP / 8][4] = {};
-#pragma unroll
-            for (int k = 0; k < kHeadCols / 16; ++k)
-                if (16 * k < a.cols) mma_parts<NP>(d, load_a(tile_dy(s), kXP, p0, 16 * k, lane), S_op, 16 * k, lane);
-            scale_rows(d, vR[p0 + g] * scS.down, vR[p0 + g + 8] * scS.down);
+#pragma unroll 2
+            for (int k = 0; k < kHeadCols / 16; ++k) mma_parts<NP>(d, load_a(tile_dy(s), kXP, p0, 16 * k, lane), S_op, 16 * k, lane);
+            scale_rows(d, f.into[p0 + g] * scS.down, f.into[p0 + g + 8] * scS.down);
             const float2 x = row_dots<NP>(d, tile_C(s), p0, lane);
             if (t == 0) {
                 dot_C[p0 + g] = x.x;
                 dot_C[p0 + g + 8] = x.y;
             }
-            const HeadScale sc = scale_of<T>(m);
-            if constexpr (kScaled<T>) scale_rows(d, sc.up, sc.up);
+            // what the steps up to these give it, 16 at a time
+            HeadScale sc = {1.0f, 1.0f};
+            float run[2] = {};                            // K w of a row summed up to a column
+#pragma unroll 1
+            for (int j = 0; j <= r; ++j) {
+                const bool diagonal = j == r;
+                float m[2][4], P[2][4];                   // R, then M R w; P, then K w
+                scores<kHeadCols>(m, tile_dy(s), tile_u(s), p0, 16 * j, lane);
+                scores<NP>(P, tile_C(s), tile_B(s), p0, 16 * j, lane);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j <= r) {
-                    const HeadA<T> w = acc_to_a<T>(m[2 * j], m[2 * j + 1], sc.up);
+                for (int q = 0; q < 2; ++q) {
+                    const int col = 16 * j + 8 * q + 2 * t;
+                    const float2 v = *reinterpret_cast<const float2 *>(pair + col), w = *reinterpret_cast<const float2 *>(f.w + col);
 #pragma unroll
-                    for (int n = 0; n < NP / 16; ++n) {
-                        HeadB<T> b[2];
-                        load_b_t(b, tile_B(s), kWP, 16 * n, 16 * j, lane);
-                        head_mma(d[2 * n], w, b[0]);
-                        head_mma(d[2 * n + 1], w, b[1]);
+                    for (int k = 0; k < 4; ++k) {
+                        const int at = col + (k & 1), row = p0 + g + (k < 2 ? 0 : 8);
+                        const float vk = k & 1 ? v.y : v.x, wk = k & 1 ? w.y : w.x;
+                        if (at == row) skip_grad += m[q][k];
+                        const float by = (diagonal ? fast_exp2((k < 2 ? l0 : l1) - vk) : (k < 2 ? r0 : r1) * vk) * wk;
+                        const bool on = !diagonal || at <= row;
+                        m[q][k] = on ? m[q][k] * by : 0.0f;
+                        P[q][k] = on ? m[q][k] * P[q][k] : 0.0f;
                     }
+                    // what passes over step `col`: of each row i >= col its sum up to, not with, col
+                    float pass[2] = {};
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int row = p0 + g + 8 * k;
+                        float v = P[q][2 * k] + P[q][2 * k + 1];
+#pragma unroll
+                        for (int z = 1; z < 4; z <<= 1) {
+                            const float w = __shfl_up_sync(0xffffffffu, v, z, 4);
+                            if (t >= z) v += w;
+                        }
+                        const float before = __shfl_up_sync(0xffffffffu, v, 1, 4), at = run[k] + (t ? before : 0.0f);
+                        if (col <= row) pass[0] += at;
+                        if (col + 1 <= row) pass[1] += at + P[q][2 * k];
+                        run[k] += __shfl_sync(0xffffffffu, v, 3, 4);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int z = 4; z < 32; z <<= 1) pass[k] += __shfl_xor_sync(0xffffffffu, pass[k], z);
+                    if (g == 0) *reinterpret_cast<float2 *>(pairs + r * kHeadSteps + col) = make_float2(pass[0], pass[1]);
                 }
-            if constexpr (kScaled<T>) scale_rows(d, sc.down, sc.down);
+                join_scale<T>(m, d, sc, j == 0);
+                mma_rows<NP>(d, acc_to_a<T>(m[0], m[1], 1.0f), tile_B(s), 16 * j, lane);
+            }
+            if (kScaled<T> && sc.down != 1.0f) scale_rows(d, sc.down, sc.down);
             write_part<NP, kWhole>(d, step0 < a.n ? p.part_C + (part_row + token(step0)) * p.states : nullptr,
-                           step1 < a.n ? p.part_C + (part_row + token(step1)) * p.states : nullptr, p.states, lane);
+                                   step1 < a.n ? p.part_C + (part_row + token(step1)) * p.states : nullptr, p.states, lane);
             // <G, S> of this warp's columns, and G in front of the chunk
             float z = 0.0f;
 #pragma unroll
@@ -362,140 +366,118 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
             z *= scS.down;
 #pragma unroll
             for (int q = 16; q > 0; q >>= 1) z += __shfl_xor_sync(0xffffffffu, z, q);
-            if (lane == 0) through[r] = z * decay;
-            if (p0 < a.cols) state_update<NP, NP / 8>(H, tile_dy(s), tile_C(s), vR, decay, p0, 0, lane);
-        } else {
-            const float r0 = fast_exp2(-l0), r1 = fast_exp2(-l1);
-            float mp[8][4] = {}, mr[8][4] = {}, k0 = 0.0f, k1 = 0.0f;          // M P and M R, transposed; column sums of K
+            if (lane == 0) through[r] = z * f.decay;
+            if (p0 < a.cols) state_update<NP, NP / 8>(H, tile_dy(s), tile_C(s), f.into, f.decay, p0, 0, lane);
+        } else if (i >= 0) {
+            const float *pair = f.pair[r];
+            const float l0 = pair[p0 + g], l1 = pair[p0 + g + 8], last = pair[p0 + 15], rest = f.rest[r];
+            const float r0 = fast_exp2(last - l0), r1 = fast_exp2(last - l1), e0 = fast_exp2(rest - l0) * scG.down, e1 = fast_exp2(rest - l1) * scG.down;
+            const float w0 = f.w[p0 + g], w1 = f.w[p0 + g + 8];
+            // what the state behind the chunk gives du and dB
+            float x[8][4] = {}, d[NP / 8][4] = {};
+#pragma unroll 2
+            for (int k = 0; k < NP / 16; ++k) {
+                const HeadA<T> c = load_a(tile_B(s), kWP, p0, 16 * k, lane);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i >= r) {
-#pragma unroll
-                    for (int k = 0; k < NP / 16; ++k) {
-                        const HeadA<T> c = load_a(tile_B(s), kWP, p0, 16 * k, lane);
-                        HeadB<T> b[2];
-                        load_b(b, tile_C(s), kWP, 16 * i, 16 * k, lane);
-                        head_mma(mp[2 * i], c, b[0]);
-                        head_mma(mp[2 * i + 1], c, b[1]);
-                    }
-#pragma unroll
-                    for (int k = 0; k < kHeadCols / 16; ++k)
-                        if (16 * k < a.cols) {
-                            const HeadA<T> x = load_a(tile_u(s), kXP, p0, 16 * k, lane);
-                            HeadB<T> b[2];
-                            load_b(b, tile_dy(s), kXP, 16 * i, 16 * k, lane);
-                            head_mma(mr[2 * i], x, b[0]);
-                            head_mma(mr[2 * i + 1], x, b[1]);
-                        }
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int col = 16 * i + 8 * q + 2 * t + (k & 1), row = p0 + g + (k < 2 ? 0 : 8);
-                            const bool on = i > r || col >= row;
-                            const float f = i > r ? (k < 2 ? r0 : r1) * vC[col] : fast_exp2(vC[col] - (k < 2 ? l0 : l1));
-                            float &vp = mp[2 * i + q][k], &vr = mr[2 * i + q][k];
-                            vr = on ? vr * f : 0.0f;
-                            const float e = on ? vr * vp : 0.0f;
-                            vp = on ? vp * f : 0.0f;
-                            if (k < 2)
-                                k0 += e;
-                            else
-                                k1 += e;
-                        }
+                for (int q = 0; q < 4; ++q) {
+                    HeadB<T> b[2];
+                    load_b(b, G_op, kWP, 16 * q, 16 * k, lane);
+                    head_mma(x[2 * q], c, b[0]);
+                    head_mma(x[2 * q + 1], c, b[1]);
                 }
-            const float w0 = vW[p0 + g], w1 = vW[p0 + g + 8], e0 = vE[p0 + g], e1 = vE[p0 + g + 8];
-            {
-                float d[8][4] = {};
-#pragma unroll
-                for (int k = 0; k < NP / 16; ++k) {
-                    const HeadA<T> c = load_a(tile_B(s), kWP, p0, 16 * k, lane);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (16 * q < a.cols) {
-                            HeadB<T> b[2];
-                            load_b(b, G_op, kWP, 16 * q, 16 * k, lane);
-                            head_mma(d[2 * q], c, b[0]);
-                            head_mma(d[2 * q + 1], c, b[1]);
-                        }
-                }
-                const HeadScale sc = scale_of<T>(mp);
-                scale_rows(d, e0 * scG.down * sc.up, e1 * scG.down * sc.up);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i >= r) {
-                        const HeadA<T> w = acc_to_a<T>(mp[2 * i], mp[2 * i + 1], sc.up);
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-                            if (16 * q < a.cols) {
-                                HeadB<T> b[2];
-                                load_b_t(b, tile_dy(s), kXP, 16 * q, 16 * i, lane);
-                                head_mma(d[2 * q], w, b[0]);
-                                head_mma(d[2 * q + 1], w, b[1]);
-                            }
-                    }
-                scale_rows(d, w0 * sc.down, w1 * sc.down);
-#pragma unroll
-                for (int n = 0; n < 8; ++n)
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const int c = 8 * n + 2 * t, step = k ? step1 : step0;
-                        if (step >= a.n || c >= a.cols) continue;
-                        const float2 y = head_pair(tile_dy(s) + (p0 + g + 8 * k) * kXP + c);
-                        const float v0 = p.D ? fmaf(skip, y.x, d[n][2 * k]) : d[n][2 * k], v1 = p.D ? fmaf(skip, y.y, d[n][2 * k + 1]) : d[n][2 * k + 1];
-                        T *to = du + token(step) * dy_l + c;
-                        if (kWhole || p.out_unit >= 2 * static_cast<int>(sizeof(T))) {
-                            head_store_pair(to, v0, v1);
-                        } else {
-                            to[0] = head_round<T>(v0);
-                            if (c + 1 < a.cols) to[1] = head_round<T>(v1);
-                        }
-                    }
             }
-            float d[NP / 8][4] = {};
+            scale_rows(x, e0, e1);
+#pragma unroll 2
+            for (int k = 0; k < kHeadCols / 16; ++k) mma_parts<NP>(d, load_a(tile_u(s), kXP, p0, 16 * k, lane), G_op, 16 * k, lane);
+            scale_rows(d, e0, e1);
+            const float2 b = row_dots<NP>(d, tile_B(s), p0, lane);
+            // and what these steps and the ones behind them do, 16 at a time
+            HeadScale scx = {1.0f, 1.0f}, scd = {1.0f, 1.0f};
+            float k0 = 0.0f, k1 = 0.0f;                   // column sums of K
+#pragma unroll 1
+            for (int j = r; j < 4; ++j) {
+                const bool diagonal = j == r;
+                float mp[2][4], mr[2][4];                 // M P and M R, transposed
+                scores<NP>(mp, tile_B(s), tile_C(s), p0, 16 * j, lane);
+                scores<kHeadCols>(mr, tile_u(s), tile_dy(s), p0, 16 * j, lane);
 #pragma unroll
-            for (int k = 0; k < kHeadCols / 16; ++k)
-                if (16 * k < a.cols) mma_parts<NP>(d, load_a(tile_u(s), kXP, p0, 16 * k, lane), G_op, 16 * k, lane);
-            scale_rows(d, e0 * scG.down, e1 * scG.down);
-            const float2 x = row_dots<NP>(d, tile_B(s), p0, lane);
+                for (int q = 0; q < 2; ++q) {
+                    const int col = 16 * j + 8 * q + 2 * t;
+                    const float2 v = *reinterpret_cast<const float2 *>(pair + col);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int at = col + (k & 1), row = p0 + g + (k < 2 ? 0 : 8);
+                        const float vk = k & 1 ? v.y : v.x;
+                        const float by = diagonal ? fast_exp2(vk - (k < 2 ? l0 : l1)) : (k < 2 ? r0 : r1) * vk;
+                        const bool on = !diagonal || at >= row;
+                        mr[q][k] = on ? mr[q][k] * by : 0.0f;
+                        const float e = on ? mr[q][k] * mp[q][k] : 0.0f;
+                        mp[q][k] = on ? mp[q][k] * by : 0.0f;
+                        if (k < 2)
+                            k0 += e;
+                        else
+                            k1 += e;
+                    }
+                }
+                join_scale<T>(mp, x, scx, diagonal);
+                mma_rows<kHeadCols>(x, acc_to_a<T>(mp[0], mp[1], 1.0f), tile_dy(s), 16 * j, lane);
+                join_scale<T>(mr, d, scd, diagonal);
+                mma_rows<NP>(d, acc_to_a<T>(mr[0], mr[1], 1.0f), tile_C(s), 16 * j, lane);
+            }
 #pragma unroll
             for (int q = 1; q < 4; q <<= 1) {
                 k0 += __shfl_xor_sync(0xffffffffu, k0, q);
                 k1 += __shfl_xor_sync(0xffffffffu, k1, q);
             }
             if (t == 0) {
-                dw[p0 + g] = k0 + x.x;
-                dw[p0 + g + 8] = k1 + x.y;
-                dot_B[p0 + g] = x.x;
-                dot_B[p0 + g + 8] = x.y;
+                dw[p0 + g] = k0 + b.x;
+                dw[p0 + g + 8] = k1 + b.y;
+                dot_B[p0 + g] = b.x;
+                dot_B[p0 + g + 8] = b.y;
             }
-            const HeadScale sc = scale_of<T>(mr);
-            if constexpr (kScaled<T>) scale_rows(d, sc.up, sc.up);
+            scale_rows(x, w0 * scx.down, w1 * scx.down);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i >= r) {
-                    const HeadA<T> w = acc_to_a<T>(mr[2 * i], mr[2 * i + 1], sc.up);
+            for (int n = 0; n < 8; ++n)
 #pragma unroll
-                    for (int n = 0; n < NP / 16; ++n) {
-                        HeadB<T> b[2];
-                        load_b_t(b, tile_C(s), kWP, 16 * n, 16 * i, lane);
-                        head_mma(d[2 * n], w, b[0]);
-                        head_mma(d[2 * n + 1], w, b[1]);
+                for (int k = 0; k < 2; ++k) {
+                    const int c = 8 * n + 2 * t, step = k ? step1 : step0;
+                    if (step >= a.n || c >= a.cols) continue;
+                    float v0 = x[n][2 * k], v1 = x[n][2 * k + 1];
+                    if (p.D) {
+                        const float2 y = head_pair(tile_dy(s) + (p0 + g + 8 * k) * kXP + c);
+                        v0 = fmaf(skip, y.x, v0);
+                        v1 = fmaf(skip, y.y, v1);
+                    }
+                    T *to = du + token(step) * dy_l + c;
+                    if (kWhole || p.out_unit >= 2 * static_cast<int>(sizeof(T))) {
+                        head_store_pair(to, v0, v1);
+                    } else {
+                        to[0] = head_round<T>(v0);
+                        if (c + 1 < a.cols) to[1] = head_round<T>(v1);
                     }
                 }
-            scale_rows(d, w0 * sc.down, w1 * sc.down);
+            scale_rows(d, w0 * scd.down, w1 * scd.down);
             write_part<NP, kWhole>(d, step0 < a.n ? p.part_B + (part_row + token(step0)) * p.states : nullptr,
-                           step1 < a.n ? p.part_B + (part_row + token(step1)) * p.states : nullptr, p.states, lane);
+                                   step1 < a.n ? p.part_B + (part_row + token(step1)) * p.states : nullptr, p.states, lane);
+        }
+        if (next) {
+            if (!rows_i)
+                read_state<kWhole>(H, p.kept + ((static_cast<int64_t>(a.b) * p.chunks + chunk_of(i + 1)) * p.heads + a.h) * state_size + tile_at, p0, 0, a.cols,
+                                   p.states, lane);
+            if (warp == 0) {
+                write_back_factors(factors[s ^ 1], head_steps(p, delta, bias, A2, chunk_of(i + 1) * kHeadSteps, a.n, lane), lane);
+                if (i + 2 < count) load_delta<T>(p, delta_at, chunk_of(i + 2) * kHeadSteps, a.n, lane, delta);
+            }
         }
         __syncthreads();                                  // the sums; S and G as operands, and the tiles, have been read
-        if (M::kStages == 1 && chunk > chunk0) load(chunk - 1, 0);
-        if (warp == 0) {
+        if (M::kStages == 1 && next) load(chunk_of(i + 1), 0);
+        if (i >= 0 && warp == 7) {
             // from the last step on C . dC', up to the step w B . dB', the pairs over it and <G, S>
             double v[2], y[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 v[k] = dot_C[2 * lane + k];
-                y[k] = static_cast<double>(st.w[k]) * dot_B[2 * lane + k];
+                y[k] = static_cast<double>(f.w[2 * lane + k]) * dot_B[2 * lane + k];
             }
             double after = v[0] + v[1], before = y[0] + y[1];
 #pragma unroll
@@ -513,13 +495,10 @@ __global__ void __launch_bounds__(256) ptq_heads_backward_kernel(const HeadParam
             const double z = static_cast<double>(through[0]) + through[1] + through[2] + through[3];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
+                const int j = 2 * lane + k;
                 v[k] += y[k] + z;
-                for (int q = (2 * lane + k) / 16; q < 4; ++q) v[k] += pairs[q * kHeadSteps + 2 * lane + k];
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int step = first + 2 * lane + k;
-                if (step < a.n) p.part_dt[part_row + token(step)] = make_float2(static_cast<float>(v[k]), dw[2 * lane + k]);
+                for (int q = j / 16; q < 4; ++q) v[k] += pairs[q * kHeadSteps + j];
+                if (first + j < a.n) p.part_dt[part_row + token(first + j)] = make_float2(static_cast<float>(v[k]), dw[j]);
             }
         }
     }

@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(256) ptq_heads_finish_kernel(const HeadParams 
 
 // ddelta of one head of one sequence, and that sequence's shares of dA and ddelta_bias.
 template <typename T>
-__global__ void __launch_bounds__(128) ptq_heads_finish_delta_kernel(const HeadParams p, T *ddelta, float2 *shares)
+__global__ void __launch_bounds__(512) ptq_heads_finish_delta_kernel(const HeadParams p, T *ddelta, float2 *shares)
 {
     griddep_wait();
     const int h = static_cast<int>(blockIdx.x) % p.heads, b = static_cast<int>(blockIdx.x) / p.heads;
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(128) ptq_heads_finish_delta_kernel(const HeadP
     const int64_t rows = static_cast<int64_t>(p.batch) * p.length;
     const T *delta = static_cast<const T *>(p.delta);
     double sum_A = 0.0, sum_bias = 0.0;
-    for (int t = threadIdx.x; t < p.length; t += 128) {
+    for (int t = threadIdx.x; t < p.length; t += 512) {
         const int64_t row = static_cast<int64_t>(b) * p.length + t;
         float de = 0.0f;
         if (t < n) {
@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(128) ptq_heads_finish_delta_kernel(const HeadP
         }
         if (ddelta) ddelta[row * p.heads + h] = head_round<T>(de);
     }
-    __shared__ double warps[2][4];
+    __shared__ double warps[2][16];
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) {
         sum_A += __shfl_xor_sync(0xffffffffu, sum_A, d);
@@ -89,9 +89,14 @@ __global__ void __launch_bounds__(128) ptq_heads_finish_delta_kernel(const HeadP
         warps[1][threadIdx.x >> 5] = sum_bias;
     }
     __syncthreads();
-    if (threadIdx.x == 0)
-        shares[static_cast<int64_t>(b) * p.heads + h] = make_float2(static_cast<float>(warps[0][0] + warps[0][1] + warps[0][2] + warps[0][3]),
-                                                                    static_cast<float>(warps[1][0] + warps[1][1] + warps[1][2] + warps[1][3]));
+    if (threadIdx.x == 0) {
+        double v[2] = {};
+        for (int k = 0; k < 16; ++k) {
+            v[0] += warps[0][k];
+            v[1] += warps[1][k];
+        }
+        shares[static_cast<int64_t>(b) * p.heads + h] = make_float2(static_cast<float>(v[0]), static_cast<float>(v[1]));
+    }
 }
 
 // dA, ddelta_bias and dD of one head: the sequences' shares in their order.
