@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
             const float l0 = pair[p0 + g], l1 = pair[p0 + g + 8], r0 = fast_exp2(l0), r1 = fast_exp2(l1);
             // what the state gives dC
             float d[NP / 8][4] = {};
-#pragma unroll 2
+#pragma unroll 1
             for (int k = 0; k < kHeadCols / 16; ++k) mma_parts<NP>(d, load_a(tile_dy(s), kXP, p0, 16 * k, lane), S_op, 16 * k, lane);
             scale_rows(d, f.into[p0 + g] * scS.down, f.into[p0 + g + 8] * scS.down);
             const float2 x = row_dots<NP>(d, tile_C(s), p0, lane);
@@ -375,7 +375,7 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
             const float w0 = f.w[p0 + g], w1 = f.w[p0 + g + 8];
             // what the state behind the chunk gives du and dB
             float x[8][4] = {}, d[NP / 8][4] = {};
-#pragma unroll 2
+#pragma unroll 1
             for (int k = 0; k < NP / 16; ++k) {
                 const HeadA<T> c = load_a(tile_B(s), kWP, p0, 16 * k, lane);
 #pragma unroll
@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
                 }
             }
             scale_rows(x, e0, e1);
-#pragma unroll 2
+#pragma unroll 1
             for (int k = 0; k < kHeadCols / 16; ++k) mma_parts<NP>(d, load_a(tile_u(s), kXP, p0, 16 * k, lane), G_op, 16 * k, lane);
             scale_rows(d, e0, e1);
             const float2 b = row_dots<NP>(d, tile_B(s), p0, lane);
