@@ -41,8 +41,9 @@ extern "C" {
  *
  * Accuracy: steps are taken 64 at a time as matrix products.  16-bit operands enter the tensor cores as they are, sums are
  * binary32; products of two operands and the state are rounded to the activations' type where they become operands themselves
- * for y and the gradients of activations, and split into two such values where they go into states and gradients of
- * parameters.  binary32 operands are split in two throughout.
+ * for y and the gradients of activations, and split into two or three such values where they go into states and gradients of
+ * parameters.  (binary16: the state and products of operands are rounded relative to the largest of 16 columns or steps and scaled
+ * by powers of two, so that they neither overflow nor vanish.)  binary32 operands are split in two throughout.
  *
  * An infinity or NaN in a token reaches what the formulas make of it (an infinity perhaps as NaN in the state), in the forward
  * pass no earlier token, in the backward pass all gradients of the 64 steps around it, the earlier ones' and the parameters'.

@@ -488,7 +488,7 @@ __device__ __forceinline__ void state_update(float (&S)[kN][4], const T *x, cons
     HeadA<T> a[kHeadSteps / 16];
 #pragma unroll
     for (int k = 0; k < kHeadSteps / 16; ++k) a[k] = load_a_t(x, kXP, p0, 16 * k, lane);
-    // binary16: u is brought to at most 2, the factors to at most 2^13
+    // binary16: u is brought to less than 2^15 (what is 2^-29 of its largest magnitude is still held whole), the factors to less than 1
     HeadScale scu = {1.0f, 1.0f}, scf = {1.0f, 1.0f};
     if constexpr (kScaled<T>) {
         __half2 most = __float2half2_rn(0.0f);
@@ -497,9 +497,9 @@ __device__ __forceinline__ void state_update(float (&S)[kN][4], const T *x, cons
 #pragma unroll
             for (int i = 0; i < 4; ++i) most = __hmax2(most, __habs2(*reinterpret_cast<const __half2 *>(&a[k].r[i])));
         const float2 v = __half22float2(most), q = *reinterpret_cast<const float2 *>(f + 2 * lane);
-        // of u 2^-15 .. 2^15, which binary16 holds; an infinity counts as the largest finite value
-        scu = exact_scale(warp_max(fminf(fmaxf(v.x, v.y), 65504.0f)), 0, 15);
-        scf = exact_scale(warp_max(fmaxf(finite_abs(q.x), finite_abs(q.y))), 13, 60);
+        // a power of two that binary16 holds; an infinity counts as the largest finite value
+        scu = exact_scale(warp_max(fminf(fmaxf(v.x, v.y), 65504.0f)), 14, 15);
+        scf = exact_scale(warp_max(fmaxf(finite_abs(q.x), finite_abs(q.y))), -1, 60);
     }
     // the chunk's sums on their own, joined with the state in binary32: the tensor cores' sums are cut off, not rounded
     // (beside all states of 16 columns three parts of 64 steps are too many registers: 32 steps at a time)
@@ -705,6 +705,27 @@ __device__ __forceinline__ bool not_finite(const HeadB<T> (&v)[N][2])
     }
 }
 
+// Zeros in the place of such values.
+template <typename T, int N>
+__device__ __forceinline__ void only_finite(HeadB<T> (&v)[N][2])
+{
+#pragma unroll
+    for (int i = 0; i < 4 * N; ++i) {
+        if constexpr (sizeof(T) == 2) {
+            constexpr uint32_t kExp = std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
+            uint32_t &x = v[i / 4][i / 2 % 2].r[i % 2];
+            if ((x & kExp) == kExp) x &= 0xffff0000u;
+            if ((x >> 16 & kExp) == kExp) x &= 0x0000ffffu;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                float &x = v[i / 4][i / 2 % 2].v[2 * (i % 2) + k];
+                x = isfinite(x) ? x : 0.0f;
+            }
+        }
+    }
+}
+
 template <typename T, int NP, int kMode, bool kWhole>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(const HeadParams p)
 {
@@ -893,8 +914,17 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
                 HeadB<T> v[4][2];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) load_b_t(v[q], tile_u(s), kXP, 16 * q, 16 * j, lane);
-                // On the diagonal columns of later steps have the factor zero; where u is not finite there, zero times it is not zero.
-                if (diagonal && __any_sync(0xffffffffu, not_finite<T>(v))) {
+                // On the diagonal columns of later steps have the factor zero; where u is not finite there, zero times it is not zero: it stays out
+                // of the product and goes where it belongs by itself, so that the other rows and columns are the same as without it.
+                const bool odd_u = diagonal && __any_sync(0xffffffffu, not_finite<T>(v));
+                if (odd_u) only_finite<T>(v);
+                const HeadA<T> w = acc_to_a<T>(m[0], m[1], 1.0f);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    head_mma(y[2 * q], w, v[q][0]);
+                    head_mma(y[2 * q + 1], w, v[q][1]);
+                }
+                if (odd_u) {
 #pragma unroll 1
                     for (int c = 0; c < 16; ++c) {
                         const int from = (lane & 28) + (c & 7) / 2;
@@ -904,22 +934,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
 #pragma unroll
                         for (int n = 0; n < 8; ++n) {
                             const float2 x = head_pair(tile_u(s) + (16 * j + c) * kXP + 8 * n + 2 * t);
-                            if (c <= g) {
-                                y[n][0] = fmaf(w0, x.x, y[n][0]);
-                                y[n][1] = fmaf(w0, x.y, y[n][1]);
-                            }
-                            if (c <= g + 8) {
-                                y[n][2] = fmaf(w1, x.x, y[n][2]);
-                                y[n][3] = fmaf(w1, x.y, y[n][3]);
-                            }
+                            const bool on0 = !isfinite(x.x), on1 = !isfinite(x.y);
+                            if (c <= g && on0) y[n][0] = fmaf(w0, x.x, y[n][0]);
+                            if (c <= g && on1) y[n][1] = fmaf(w0, x.y, y[n][1]);
+                            if (c <= g + 8 && on0) y[n][2] = fmaf(w1, x.x, y[n][2]);
+                            if (c <= g + 8 && on1) y[n][3] = fmaf(w1, x.y, y[n][3]);
                         }
-                    }
-                } else {
-                    const HeadA<T> w = acc_to_a<T>(m[0], m[1], 1.0f);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        head_mma(y[2 * q], w, v[q][0]);
-                        head_mma(y[2 * q + 1], w, v[q][1]);
                     }
                 }
             }

@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(512) ptq_heads_finish_delta_kernel(const HeadP
             }
             const float raw = delta ? head_f32(delta[b * p.delta_b + t * p.delta_l + h * p.delta_h]) : 0.0f, dt = head_dt(p, raw, bias);
             if (dt != 0.0f) sum_A += static_cast<double>(dt) * v.x;          // a step with dt = 0 keeps the state with any A
-            de = (dt != 0.0f || isfinite(A) ? A * v.x : 0.0f) + (p.flags & kHeadsUnscaled ? 0.0f : v.y);
+            de = (v.x != 0.0f ? A * v.x : 0.0f) + (p.flags & kHeadsUnscaled ? 0.0f : v.y);
             if (p.flags & kHeadsSoftplus) de *= 1.0f / (1.0f + expf(-(raw + bias)));
             sum_bias += de;
         }
