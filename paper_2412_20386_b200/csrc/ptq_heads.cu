@@ -199,6 +199,7 @@ ptq_status_t ptq_heads_forward(const ptq_heads_t *s, void *y, float *final_state
     unsigned char *w = static_cast<unsigned char *>(workspace);
     p.slots = reinterpret_cast<float *>(w + space.slots);
     p.logs = reinterpret_cast<float *>(w + space.logs);
+    p.share = s->dtype == PTQ_F16 || static_cast<long long>(s->batch) * s->heads * p.col_tiles * p.segments <= kSms;
     const bool whole = p.unit == 16 && aligned({y}, 16) && aligned({s->state, final_state, history}, 8);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return with_launch(s->dtype, [&](auto launch) -> ptq_status_t {

@@ -44,6 +44,7 @@ struct HeadParams {
     int batch, length, heads, cols, states, groups, group_heads;
     int col_tiles, segments, segment_chunks, chunks;
     int unit, out_unit;               // bytes that rows of the inputs, of y can be moved at a time
+    bool share;                       // forward: the states' warps take some of the outputs' products
     unsigned flags;
     // backward pass
     const float *kept, *dfinal;
@@ -676,7 +677,10 @@ struct HeadSmem {
     static constexpr int kStaging = kState + (kMode == kHeadForward ? kWide : 0);
     static constexpr int kFactors = kStaging + (kMode == kHeadForward && sizeof(T) == 2 && !kOverC ? kNarrow : 0);
     static constexpr int kPowers = kFactors + 2 * static_cast<int>(sizeof(HeadFactors));
-    static constexpr int kBytes = kPowers + 4 * 4;
+    // what the states' warps add to outputs, 16 x 64 binary32 sums each: over the state's operand where that is large enough
+    static constexpr bool kOverState = kWide >= 4 * 4096;
+    static constexpr int kHelp = kOverState ? kState : kPowers + 4 * 4;
+    static constexpr int kBytes = kPowers + 4 * 4 + (kMode == kHeadForward && !kOverState ? 4 * 4096 : 0);
 };
 
 // Whether an operand holds an infinity or NaN (zero times it is not zero).
@@ -751,6 +755,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
     T *state_s = reinterpret_cast<T *>(smem + M::kState);
     HeadFactors *factors = reinterpret_cast<HeadFactors *>(smem + M::kFactors);
     float *powers = reinterpret_cast<float *>(smem + M::kPowers);
+    float4 *help = reinterpret_cast<float4 *>(smem + M::kHelp);
 
     const T *u = static_cast<const T *>(kGrad ? p.dy : p.u) +
                  (kGrad ? (static_cast<int64_t>(a.b) * p.length * p.heads + a.h) * p.cols : a.b * p.u_b + a.h * p.u_h) + a.tile * kHeadCols;
@@ -853,9 +858,10 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
             }
             asm volatile("bar.arrive 1, 256;" ::: "memory");           // the state and its powers have been read
             // and what the steps up to them give, 16 at a time, the ones on the diagonal last
+            const int j0 = p.share ? (r + 1) / 2 : 0;      // the ones before: by the states' warps
             HeadScale sc = {1.0f, 1.0f};
 #pragma unroll 1
-            for (int j = 0; j <= r; ++j) {
+            for (int j = j0; j <= r; ++j) {
                 const bool diagonal = j == r;
                 float m[2][4], odd[2][4];                  // two chains of products each
 #pragma unroll
@@ -896,7 +902,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
                 }
                 if constexpr (kScaled<T>) {                // y is in the units of the smallest power of two so far
                     const HeadScale now = scale_for(warp_top<2>(m));
-                    if (j == 0 ? now.up != 1.0f : now.up < sc.up) {
+                    if (j == j0 ? now.up != 1.0f : now.up < sc.up) {
                         const float by = now.up * sc.down;
 #pragma unroll
                         for (int n = 0; n < 8; ++n)
@@ -949,6 +955,22 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
 #pragma unroll
                     for (int k = 0; k < 4; ++k) y[n][k] *= sc.down;
             }
+            if (p.share) {
+                asm volatile("bar.sync 2, 256;" ::: "memory");         // the others' sums are there
+                const auto add = [&](int from) {
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) {
+                        const float4 v = help[from * 256 + n * 32 + lane];
+                        y[n][0] += v.x;
+                        y[n][1] += v.y;
+                        y[n][2] += v.z;
+                        y[n][3] += v.w;
+                    }
+                };
+                if (r > 0) add(r == 3 ? 0 : 4 - r);
+                if (r == 3) add(1);
+                if (M::kOverState) asm volatile("bar.arrive 3, 256;" ::: "memory");
+            }
             const int step0 = first + p0 + g, step1 = step0 + 8;
             // through shared memory (16-bit values: over this warp's rows of C, which nobody else reads) to whole 16-byte stores
             T *stage = M::kOverC ? tile_C(s) + p0 * kWP : reinterpret_cast<T *>(smem + M::kStaging) + p0 * kXP;
@@ -986,10 +1008,53 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
                 }
             }
         }
+        if (kOut && !outputs && i >= 0 && p.share) {
+            // The last steps have four sets of 16 steps up to them, the first ones one: the states' warps take one each, of the steps
+            // 48 .. 63 the first two, of 32 .. 47 and of 16 .. 31 the first.  A chunk is shorter for it (1 image 16.4 -> 14.4 us; 128 x 197 x 12 heads,
+            // binary16, 144.7 -> 141.6), but with operands in three parts and two CTAs to an SM the states' warps are the slower ones
+            // (bfloat16, 2 x 20011 x 16 heads: 349 -> 368 us): not there.
+            const int hr = r == 0 ? 3 : 4 - r, hj = r == 1 ? 1 : 0;
+            const float *pair = f.pair[hr];
+            float m[2][4];
+#pragma unroll
+            for (int k = 0; k < NP / 16; ++k) {
+                HeadB<T> b[2];
+                load_b(b, tile_B(s), kWP, 16 * hj, 16 * k, lane);
+                const HeadA<T> c = load_a(tile_C(s), kWP, 16 * hr, 16 * k, lane);
+                head_mma(m[0], c, b[0], k == 0);
+                head_mma(m[1], c, b[1], k == 0);
+            }
+            const float r0 = fast_exp2(pair[16 * hr + g]), r1 = fast_exp2(pair[16 * hr + g + 8]);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const float2 v = *reinterpret_cast<const float2 *>(pair + 16 * hj + 8 * n + 2 * t);
+                m[n][0] *= r0 * v.x;
+                m[n][1] *= r0 * v.y;
+                m[n][2] *= r1 * v.x;
+                m[n][3] *= r1 * v.y;
+            }
+            HeadScale sc = {1.0f, 1.0f};
+            if constexpr (kScaled<T>) sc = scale_for(warp_top<2>(m));
+            const HeadA<T> w = acc_to_a<T>(m[0], m[1], sc.up);
+            if (M::kOverState) asm volatile("bar.sync 1, 256;" ::: "memory");              // the outputs' warps have read the state
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                HeadB<T> b[2];
+                load_b_t(b, tile_u(s), kXP, 16 * q, 16 * hj, lane);
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    float x[4];
+                    head_mma(x, w, b[n], true);
+                    help[r * 256 + (2 * q + n) * 32 + lane] = make_float4(x[0] * sc.down, x[1] * sc.down, x[2] * sc.down, x[3] * sc.down);
+                }
+            }
+            asm volatile("bar.arrive 2, 256;" ::: "memory");
+        }
         if (i >= 0) {
             log_decay += f.log_decay;
             if (busy) state_update<NP, kN>(S, tile_u(s), tile_B(s), f.state, f.decay, p0, n0, lane);
-            if (kOut && !outputs) asm volatile("bar.sync 1, 256;" ::: "memory");           // the outputs' warps have read the state
+            // the outputs' warps have read the state, or what lies over it
+            if (kOut && !outputs) asm volatile("bar.sync %0, 256;" ::"r"(M::kOverState && p.share ? 3 : 1) : "memory");
         }
         if (kOut && !outputs && next) publish(chunk_of(i + 1));
         if (warp == 4 + ((i + 1) & 3) && next)
