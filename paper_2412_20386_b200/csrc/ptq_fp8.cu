@@ -79,8 +79,10 @@ ptq_status_t quantize(const ptq_fp8_input_t &in, void *codes, int64_t codes_pitc
     p.scales = scales;
     p.scale_row = scale_row;
     p.scale_block = scale_block;
-    // three blocks at a time where that leaves fewer idle (six of 768 channels)
-    const int set = ceil_div(p.blocks, 3) * 3 < ceil_div(p.blocks, 4) * 4 ? 3 : 4;
+    // six, four or three blocks at a time, whichever leaves the fewest idle
+    int set = 6;
+    for (int n : {4, 3})
+        if (ceil_div(p.blocks, n) * n < ceil_div(p.blocks, set) * set) set = n;
     p.sets = ptq::make_fastdiv(static_cast<unsigned>(ceil_div(p.blocks, set)));
     const long long ctas = ceil_div(in.rows, ptq::kFp8QuantizeRows) * p.sets.d;
     if (ctas > kMaxGrid) return fail(PTQ_ERR_SHAPE, "the input is too large for one launch");
@@ -88,7 +90,9 @@ ptq_status_t quantize(const ptq_fp8_input_t &in, void *codes, int64_t codes_pitc
         using T = decltype(t);
         return with_flag(input_whole(in), [&](auto whole) {
             constexpr bool kWhole = decltype(whole)::value;
-            if (set == 3)
+            if (set == 6)
+                ptq::ptq_fp8_quantize_kernel<T, 6, kWhole><<<static_cast<unsigned>(ctas), 256, 0, stream>>>(p);
+            else if (set == 3)
                 ptq::ptq_fp8_quantize_kernel<T, 3, kWhole><<<static_cast<unsigned>(ctas), 256, 0, stream>>>(p);
             else
                 ptq::ptq_fp8_quantize_kernel<T, 4, kWhole><<<static_cast<unsigned>(ctas), 256, 0, stream>>>(p);

@@ -51,42 +51,63 @@ __device__ __forceinline__ float max_abs_nan(float a, float b)
     return r;
 }
 
-// Eight values of a row from column c on, zeros from `cols` on.  kWhole: 16 bytes at a time; rows begin on multiples of 16 bytes and
-// cols is a multiple of 8.
+// Eight values of a row from column c on, zeros from `cols` on, as they are stored.  kWhole: 16 bytes at a time; rows begin on multiples of
+// 16 bytes and cols is a multiple of 8.
+template <typename T>
+struct Eight {
+    uint4 q[sizeof(T) / 2];
+};
 template <bool kWhole, typename T>
-__device__ __forceinline__ void load8(const T *row, int c, int cols, float (&v)[8])
+__device__ __forceinline__ Eight<T> load8(const T *row, int c, int cols)
 {
-    if constexpr (kWhole) {
-        const bool on = c < cols;
-        if constexpr (sizeof(T) == 4) {
-            float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
-            if (on) {
-                a = __ldg(reinterpret_cast<const float4 *>(row + c));
-                b = __ldg(reinterpret_cast<const float4 *>(row + c) + 1);
-            }
-            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-        } else {
-            uint4 a = make_uint4(0u, 0u, 0u, 0u);
-            if (on) a = __ldg(reinterpret_cast<const uint4 *>(row + c));
-            const T *t = reinterpret_cast<const T *>(&a);
+    Eight<T> v;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = to_f32(t[i]);
+    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) v.q[i] = make_uint4(0u, 0u, 0u, 0u);
+    if constexpr (kWhole) {
+        if (c < cols) {
+#pragma unroll
+            for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) v.q[i] = __ldcs(reinterpret_cast<const uint4 *>(row + c) + i);
         }
     } else {
+        T *t = reinterpret_cast<T *>(&v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? to_f32(row[c + i]) : 0.0f;
+        for (int i = 0; i < 8; ++i)
+            if (c + i < cols) t[i] = row[c + i];
     }
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void unpack8(const Eight<T> &e, float (&v)[8])
+{
+    const T *t = reinterpret_cast<const T *>(&e);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = to_f32(t[i]);
 }
 
 // The largest magnitude of the 128 values that 16 neighbouring lanes hold, not below kFp8Least; a NaN stays one.
-__device__ __forceinline__ float block_top(const float (&v)[8])
+template <typename T>
+__device__ __forceinline__ float block_top(const Eight<T> &e)
 {
     float top = kFp8Least;
+    if constexpr (sizeof(T) == 2) {                       // two at a time, in the type itself
+        using T2 = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
+        const T2 *t = reinterpret_cast<const T2 *>(&e);
+        const T2 m = __hmax2_nan(__hmax2_nan(__habs2(t[0]), __habs2(t[1])), __hmax2_nan(__habs2(t[2]), __habs2(t[3])));
+        top = max_abs_nan(max_abs_nan(top, to_f32(m.x)), to_f32(m.y));
+    } else {
+        const float *t = reinterpret_cast<const float *>(&e);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max_abs_nan(top, v[i]);
+        for (int i = 0; i < 8; ++i) top = max_abs_nan(top, t[i]);
+    }
 #pragma unroll
     for (int d = 8; d > 0; d >>= 1) top = max_abs_nan(top, __shfl_xor_sync(0xffffffffu, top, d));
     return top;
+}
+// 448 / top in all 16 lanes and top / 448 in the second one (elsewhere it is not that): one division for both.
+__device__ __forceinline__ void block_scales(float top, int l, float &inverse, float &scale)
+{
+    scale = (l == 1 ? top : kFp8Max) / (l == 1 ? kFp8Max : top);
+    inverse = __shfl_sync(0xffffffffu, scale, 0, 16);
 }
 __device__ __forceinline__ uint2 codes8(const float (&v)[8], float inverse)
 {
@@ -123,7 +144,7 @@ struct Fp8QuantizeParams {
 };
 constexpr int kFp8QuantizeRows = 16;
 template <typename T, int kSet, bool kWhole>
-__global__ void __launch_bounds__(256, 6) ptq_fp8_quantize_kernel(const Fp8QuantizeParams p)
+__global__ void __launch_bounds__(256) ptq_fp8_quantize_kernel(const Fp8QuantizeParams p)
 {
     const unsigned group = fd_div(blockIdx.x, p.sets);
     const int64_t row = static_cast<int64_t>(group) * kFp8QuantizeRows + (threadIdx.x >> 4);
@@ -131,16 +152,18 @@ __global__ void __launch_bounds__(256, 6) ptq_fp8_quantize_kernel(const Fp8Quant
     const bool on = row < p.rows;                       // the others go along: the shuffles are the warp's
     const T *x = static_cast<const T *>(p.x) + (on ? row : 0) * p.x_pitch;
     griddep_launch_dependents();
-    float v[kSet][8];
+    Eight<T> e[kSet];
 #pragma unroll
-    for (int i = 0; i < kSet; ++i) load8<kWhole>(x, (b0 + i) * kFp8Block + 8 * l, on ? p.cols : 0, v[i]);
+    for (int i = 0; i < kSet; ++i) e[i] = load8<kWhole>(x, (b0 + i) * kFp8Block + 8 * l, on ? p.cols : 0);
 #pragma unroll
     for (int i = 0; i < kSet; ++i) {
-        const float top = block_top(v[i]);
-        const uint2 w = codes8(v[i], kFp8Max / top);
+        float inverse, scale, v[8];
+        block_scales(block_top(e[i]), l, inverse, scale);
+        unpack8(e[i], v);
+        const uint2 w = codes8(v, inverse);
         if (!on || b0 + i >= p.blocks) continue;
         store_codes8(p.codes + row * p.codes_pitch, (b0 + i) * kFp8Block + 8 * l, p.cols, w);
-        if (l == 0) p.scales[row * p.scale_row + (b0 + i) * p.scale_block] = top / kFp8Max;
+        if (l == 1) p.scales[row * p.scale_row + (b0 + i) * p.scale_block] = scale;
     }
 }
 
@@ -154,8 +177,7 @@ __global__ void __launch_bounds__(256) ptq_fp8_quantize_weight_kernel(const Fp8Q
     float v[8], top = kFp8Least;
     for (int r = h; r < kFp8Block; r += 16) {
         const int64_t row = row0 + r;
-        load8<false>(static_cast<const T *>(p.x) + (row < p.rows ? row : 0) * p.x_pitch, c, row < p.rows ? p.cols : 0, v);
-        top = max_abs_nan(top, block_top(v));
+        top = max_abs_nan(top, block_top(load8<false>(static_cast<const T *>(p.x) + (row < p.rows ? row : 0) * p.x_pitch, c, row < p.rows ? p.cols : 0)));
     }
     top = max_abs_nan(top, __shfl_xor_sync(0xffffffffu, top, 16));
     if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
@@ -164,7 +186,7 @@ __global__ void __launch_bounds__(256) ptq_fp8_quantize_weight_kernel(const Fp8Q
     for (int r = h; r < kFp8Block; r += 16) {
         const int64_t row = row0 + r;
         if (row >= p.rows) break;
-        load8<false>(static_cast<const T *>(p.x) + row * p.x_pitch, c, p.cols, v);
+        unpack8(load8<false>(static_cast<const T *>(p.x) + row * p.x_pitch, c, p.cols), v);
         store_codes8(p.codes + row * p.codes_pitch, c, p.cols, codes8(v, kFp8Max / top));
     }
     if (threadIdx.x == 0) p.scales[static_cast<int64_t>(blockIdx.y) * p.blocks + blockIdx.x] = top / kFp8Max;
@@ -466,22 +488,24 @@ ptq_fp8_matmul_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_cons
             for (int i = et; i < (kb1 - kb0) * BN; i += 256) scales_s[i] = 0.0f;
             asm volatile("bar.sync 1, 256;" ::: "memory");
             for (int i0 = 0; i0 < items; i0 += 64) {
-                float v[4][8];
+                Eight<Y> e[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int item = i0 + 16 * i + (et >> 4), kb = item / tokens, r = item - kb * tokens;
                     const bool on = item < items;
-                    load8<kWhole>(x + (on ? r : 0) * p.x_pitch, (kb0 + kb) * kFp8Block + 8 * l, on ? p.cols : 0, v[i]);
+                    e[i] = load8<kWhole>(x + (on ? r : 0) * p.x_pitch, (kb0 + kb) * kFp8Block + 8 * l, on ? p.cols : 0);
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int item = i0 + 16 * i + (et >> 4), kb = item / tokens, r = item - kb * tokens;
-                    const float top = block_top(v[i]);
-                    const uint2 w = codes8(v[i], kFp8Max / top);
+                    float inverse, scale, v[8];
+                    block_scales(block_top(e[i]), l, inverse, scale);
+                    unpack8(e[i], v);
+                    const uint2 w = codes8(v, inverse);
                     if (item < items) {
                         const int off = kb * BN * kFp8Block + r * 128 + (((l >> 1) ^ (r & 7)) << 4) + (l & 1) * 8;
                         *reinterpret_cast<uint2 *>(smem_raw + at.q + off) = w;
-                        if (l == 0) scales_s[kb * BN + r] = top / kFp8Max;
+                        if (l == 1) scales_s[kb * BN + r] = scale;
                     }
                 }
             }
