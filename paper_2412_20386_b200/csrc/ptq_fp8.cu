@@ -79,23 +79,21 @@ ptq_status_t quantize(const ptq_fp8_input_t &in, void *codes, int64_t codes_pitc
     p.scales = scales;
     p.scale_row = scale_row;
     p.scale_block = scale_block;
-    // six, four or three blocks at a time, whichever leaves the fewest idle
-    int set = 6;
-    for (int n : {4, 3})
-        if (ceil_div(p.blocks, n) * n < ceil_div(p.blocks, set) * set) set = n;
+    // three blocks at a time where that leaves fewer idle (six of 768 channels)
+    const int set = ceil_div(p.blocks, 3) * 3 < ceil_div(p.blocks, 4) * 4 ? 3 : 4;
     p.sets = ptq::make_fastdiv(static_cast<unsigned>(ceil_div(p.blocks, set)));
-    const long long ctas = ceil_div(in.rows, ptq::kFp8QuantizeRows) * p.sets.d;
-    if (ctas > kMaxGrid) return fail(PTQ_ERR_SHAPE, "the input is too large for one launch");
+    const long long items = ceil_div(in.rows, ptq::kFp8QuantizeRows) * p.sets.d;
+    if (items > kMaxGrid - 16 * kSms) return fail(PTQ_ERR_SHAPE, "the input is too large for one launch");
+    p.items = static_cast<unsigned>(items);
+    const unsigned ctas = static_cast<unsigned>(std::min<long long>(items, 5 * kSms));
     return with_type(in.dtype, [&](auto t) {
         using T = decltype(t);
         return with_flag(input_whole(in), [&](auto whole) {
             constexpr bool kWhole = decltype(whole)::value;
-            if (set == 6)
-                ptq::ptq_fp8_quantize_kernel<T, 6, kWhole><<<static_cast<unsigned>(ctas), 256, 0, stream>>>(p);
-            else if (set == 3)
-                ptq::ptq_fp8_quantize_kernel<T, 3, kWhole><<<static_cast<unsigned>(ctas), 256, 0, stream>>>(p);
+            if (set == 3)
+                ptq::ptq_fp8_quantize_kernel<T, 3, kWhole><<<ctas, 256, 0, stream>>>(p);
             else
-                ptq::ptq_fp8_quantize_kernel<T, 4, kWhole><<<static_cast<unsigned>(ctas), 256, 0, stream>>>(p);
+                ptq::ptq_fp8_quantize_kernel<T, 4, kWhole><<<ctas, 256, 0, stream>>>(p);
             return launched();
         });
     });

@@ -103,11 +103,15 @@ __device__ __forceinline__ float block_top(const Eight<T> &e)
     for (int d = 8; d > 0; d >>= 1) top = max_abs_nan(top, __shfl_xor_sync(0xffffffffu, top, d));
     return top;
 }
-// 448 / top in all 16 lanes and top / 448 in the second one (elsewhere it is not that): one division for both.
-__device__ __forceinline__ void block_scales(float top, int l, float &inverse, float &scale)
+// Of N blocks that 16 neighbouring lanes hold, one division for all: lane i gets 448 / top[i], lane 8 + i top[i] / 448.
+template <int N>
+__device__ __forceinline__ float block_scales(const float (&top)[N], int l)
 {
-    scale = (l == 1 ? top : kFp8Max) / (l == 1 ? kFp8Max : top);
-    inverse = __shfl_sync(0xffffffffu, scale, 0, 16);
+    static_assert(N <= 8, "two divisions of each block in 16 lanes");
+    float t = top[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) t = (l & 7) == i ? top[i] : t;
+    return (l < 8 ? kFp8Max : t) / (l < 8 ? t : kFp8Max);
 }
 __device__ __forceinline__ uint2 codes8(const float (&v)[8], float inverse)
 {
@@ -120,9 +124,10 @@ __device__ __forceinline__ uint2 codes8(const float (&v)[8], float inverse)
     }
     return make_uint2(w[0], w[1]);
 }
+template <bool kWhole>
 __device__ __forceinline__ void store_codes8(uint8_t *row, int c, int cols, uint2 w)
 {
-    if (c + 8 <= cols) {
+    if (kWhole ? c < cols : c + 8 <= cols) {
         *reinterpret_cast<uint2 *>(row + c) = w;
     } else {
         for (int i = 0; i < 8 && c + i < cols; ++i) row[c + i] = static_cast<uint8_t>((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
@@ -131,14 +136,16 @@ __device__ __forceinline__ void store_codes8(uint8_t *row, int c, int cols, uint
 
 // ---------------------------------------------------------------------------------------------------- quantize
 // Bound by memory: 16-bit values are read, codes and a scale for each 128 of them written, once each.  Half a warp holds a block
-// (16 bytes of 16-bit values a lane), kSet neighbouring ones of a row at a time, so that as many loads a lane are in flight; the 16
-// half-warps of a CTA take 16 neighbouring rows, whose scales lie next to each other in the layout that the product reads.
+// (16 bytes of 16-bit values a lane), kSet neighbouring ones of a row at a time; the 16 half-warps of a CTA take 16 neighbouring rows,
+// whose scales lie next to each other in the layout that the product reads.  CTAs go over the rows with the loads of the next
+// set under way while one is worked on.
 struct Fp8QuantizeParams {
     const void *x;
     int64_t x_pitch, codes_pitch, scale_row, scale_block;
     int64_t rows;
     int cols, blocks;                 // blocks of a row
     FastDiv sets;                     // sets of kSet blocks of a row
+    unsigned items;                   // sets of 16 rows
     uint8_t *codes;
     float *scales;
 };
@@ -146,24 +153,41 @@ constexpr int kFp8QuantizeRows = 16;
 template <typename T, int kSet, bool kWhole>
 __global__ void __launch_bounds__(256) ptq_fp8_quantize_kernel(const Fp8QuantizeParams p)
 {
-    const unsigned group = fd_div(blockIdx.x, p.sets);
-    const int64_t row = static_cast<int64_t>(group) * kFp8QuantizeRows + (threadIdx.x >> 4);
-    const int b0 = static_cast<int>(blockIdx.x - group * p.sets.d) * kSet, l = threadIdx.x & 15;
-    const bool on = row < p.rows;                       // the others go along: the shuffles are the warp's
-    const T *x = static_cast<const T *>(p.x) + (on ? row : 0) * p.x_pitch;
+    const int h = threadIdx.x >> 4, l = threadIdx.x & 15;
     griddep_launch_dependents();
-    Eight<T> e[kSet];
+    int64_t row, next_row;
+    int b0, next_b0;
+    Eight<T> e[kSet], next[kSet];
+    const auto load = [&](unsigned item) {
+        const unsigned group = fd_div(item, p.sets);
+        next_row = static_cast<int64_t>(group) * kFp8QuantizeRows + h;
+        next_b0 = static_cast<int>(item - group * p.sets.d) * kSet;
+        const bool on = item < p.items && next_row < p.rows;
+        const T *x = static_cast<const T *>(p.x) + (on ? next_row : 0) * p.x_pitch;
 #pragma unroll
-    for (int i = 0; i < kSet; ++i) e[i] = load8<kWhole>(x, (b0 + i) * kFp8Block + 8 * l, on ? p.cols : 0);
+        for (int i = 0; i < kSet; ++i) next[i] = load8<kWhole>(x, (next_b0 + i) * kFp8Block + 8 * l, on ? p.cols : 0);
+    };
+    load(blockIdx.x);
+    for (unsigned item = blockIdx.x; item < p.items; item += gridDim.x) {
+        row = next_row;
+        b0 = next_b0;
 #pragma unroll
-    for (int i = 0; i < kSet; ++i) {
-        float inverse, scale, v[8];
-        block_scales(block_top(e[i]), l, inverse, scale);
-        unpack8(e[i], v);
-        const uint2 w = codes8(v, inverse);
-        if (!on || b0 + i >= p.blocks) continue;
-        store_codes8(p.codes + row * p.codes_pitch, (b0 + i) * kFp8Block + 8 * l, p.cols, w);
-        if (l == 1) p.scales[row * p.scale_row + (b0 + i) * p.scale_block] = scale;
+        for (int i = 0; i < kSet; ++i) e[i] = next[i];
+        load(item + gridDim.x);
+        const bool on = row < p.rows;                   // the others go along: the shuffles are the warp's
+        float top[kSet];
+#pragma unroll
+        for (int i = 0; i < kSet; ++i) top[i] = block_top(e[i]);
+        const float q = block_scales(top, l);
+        uint8_t *codes = p.codes + row * p.codes_pitch;
+#pragma unroll
+        for (int i = 0; i < kSet; ++i) {
+            float v[8];
+            unpack8(e[i], v);
+            const uint2 w = codes8(v, __shfl_sync(0xffffffffu, q, i, 16));
+            store_codes8<kWhole>(codes, (b0 + i) * kFp8Block + 8 * l, on ? p.cols : 0, w);
+        }
+        if (on && l >= 8 && l < 8 + kSet && b0 + l - 8 < p.blocks) p.scales[row * p.scale_row + (b0 + l - 8) * p.scale_block] = q;
     }
 }
 
@@ -187,7 +211,7 @@ __global__ void __launch_bounds__(256) ptq_fp8_quantize_weight_kernel(const Fp8Q
         const int64_t row = row0 + r;
         if (row >= p.rows) break;
         unpack8(load8<false>(static_cast<const T *>(p.x) + row * p.x_pitch, c, p.cols), v);
-        store_codes8(p.codes + row * p.codes_pitch, c, p.cols, codes8(v, kFp8Max / top));
+        store_codes8<false>(p.codes + row * p.codes_pitch, c, p.cols, codes8(v, kFp8Max / top));
     }
     if (threadIdx.x == 0) p.scales[static_cast<int64_t>(blockIdx.y) * p.blocks + blockIdx.x] = top / kFp8Max;
 }
@@ -495,17 +519,20 @@ ptq_fp8_matmul_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_cons
                     const bool on = item < items;
                     e[i] = load8<kWhole>(x + (on ? r : 0) * p.x_pitch, (kb0 + kb) * kFp8Block + 8 * l, on ? p.cols : 0);
                 }
+                float top[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top[i] = block_top(e[i]);
+                const float q = block_scales(top, l);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int item = i0 + 16 * i + (et >> 4), kb = item / tokens, r = item - kb * tokens;
-                    float inverse, scale, v[8];
-                    block_scales(block_top(e[i]), l, inverse, scale);
+                    float v[8];
                     unpack8(e[i], v);
-                    const uint2 w = codes8(v, inverse);
+                    const uint2 w = codes8(v, __shfl_sync(0xffffffffu, q, i, 16));
                     if (item < items) {
                         const int off = kb * BN * kFp8Block + r * 128 + (((l >> 1) ^ (r & 7)) << 4) + (l & 1) * 8;
                         *reinterpret_cast<uint2 *>(smem_raw + at.q + off) = w;
-                        if (l == 1) scales_s[kb * BN + r] = scale;
+                        if (l == 8 + i) scales_s[kb * BN + r] = q;
                     }
                 }
             }
