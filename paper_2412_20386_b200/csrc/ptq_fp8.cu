@@ -79,13 +79,13 @@ ptq_status_t quantize(const ptq_fp8_input_t &in, void *codes, int64_t codes_pitc
     p.scales = scales;
     p.scale_row = scale_row;
     p.scale_block = scale_block;
-    // three blocks at a time where that leaves fewer idle (six of 768 channels)
-    const int set = ceil_div(p.blocks, 3) * 3 < ceil_div(p.blocks, 4) * 4 ? 3 : 4;
+    // three blocks at a time where that leaves no more of them idle (768 and 1536 channels), else four (4096)
+    const int set = ceil_div(p.blocks, 3) * 3 <= ceil_div(p.blocks, 4) * 4 ? 3 : 4;
     p.sets = ptq::make_fastdiv(static_cast<unsigned>(ceil_div(p.blocks, set)));
     const long long items = ceil_div(in.rows, ptq::kFp8QuantizeRows) * p.sets.d;
     if (items > kMaxGrid - 16 * kSms) return fail(PTQ_ERR_SHAPE, "the input is too large for one launch");
     p.items = static_cast<unsigned>(items);
-    const unsigned ctas = static_cast<unsigned>(std::min<long long>(items, 5 * kSms));
+    const unsigned ctas = static_cast<unsigned>(std::min<long long>(items, (set == 3 ? 5 : 4) * kSms));   // as many as an SM holds
     return with_type(in.dtype, [&](auto t) {
         using T = decltype(t);
         return with_flag(input_whole(in), [&](auto whole) {

@@ -25,28 +25,38 @@ __global__ void __launch_bounds__(256) ptq_heads_fold_kernel(float *slots, const
     griddep_launch_dependents();
 }
 
-// dB (blockIdx.y 0) and dC (1): the heads of a group and their column tiles summed in their order, rounded.  Bound by reading the
-// binary32 parts once.
-template <typename T>
+// dB (blockIdx.y 0) and dC (1): the heads of a group and their column tiles summed in their order, rounded; kN neighbouring states a
+// thread (four where `states` and the outputs' alignment allow it).  Bound by reading the binary32 parts once.
+template <typename T, int kN>
 __global__ void __launch_bounds__(256) ptq_heads_finish_kernel(const HeadParams p, T *dB, T *dC)
 {
     griddep_wait();
     const float *part = blockIdx.y ? p.part_C : p.part_B;
     T *to = blockIdx.y ? dC : dB;
+    const int sets = p.states / kN;
     const int64_t rows = static_cast<int64_t>(p.batch) * p.length, i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= rows * p.groups * p.states) return;
-    const int64_t row = i / (p.groups * p.states);
-    const int in = static_cast<int>(i - row * p.groups * p.states), g = in / p.states, n = in - g * p.states;
+    if (i >= rows * p.groups * sets) return;
+    const int64_t row = i / (p.groups * sets);
+    const int in = static_cast<int>(i - row * p.groups * sets), g = in / sets, n = (in - g * sets) * kN;
     const int b = static_cast<int>(row / p.length), t = static_cast<int>(row - static_cast<int64_t>(b) * p.length);
-    float v = 0.0f;
+    struct alignas(kN * 4) Parts { float v[kN]; };
+    struct alignas(kN * sizeof(T)) Out { T v[kN]; };
+    Parts sum = {};
     if (!p.lengths || t < __ldg(p.lengths + b)) {
         for (int tile = 0; tile < p.col_tiles; ++tile) {
             const float *at = part + ((static_cast<int64_t>(tile) * p.heads + g * p.group_heads) * rows + row) * p.states + n;
-#pragma unroll 4
-            for (int h = 0; h < p.group_heads; ++h) v += at[h * rows * p.states];
+#pragma unroll 8
+            for (int h = 0; h < p.group_heads; ++h) {
+                const Parts x = *reinterpret_cast<const Parts *>(at + h * rows * p.states);
+#pragma unroll
+                for (int k = 0; k < kN; ++k) sum.v[k] += x.v[k];
+            }
         }
     }
-    to[i] = head_round<T>(v);
+    Out out;
+#pragma unroll
+    for (int k = 0; k < kN; ++k) out.v[k] = head_round<T>(sum.v[k]);
+    *reinterpret_cast<Out *>(to + kN * i) = out;
 }
 
 // ddelta of one head of one sequence, and that sequence's shares of dA and ddelta_bias.
