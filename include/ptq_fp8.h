@@ -38,7 +38,7 @@ typedef struct {
 } ptq_fp8_input_t;
 
 /* codes device [rows, cols], codes_pitch bytes between rows; scales device: that of block b of row m at
- * scales[m * scales_pitch[0] + b * scales_pitch[1]].  Outputs overlap no input. */
+ * scales[m * scales_pitch[0] + b * scales_pitch[1]], each in a place of its own.  Outputs overlap no input. */
 ptq_status_t ptq_fp8_quantize(const ptq_fp8_input_t *in, void *codes, int64_t codes_pitch, float *scales, const int64_t scales_pitch[2],
                               void *stream);
 /* The same for weights (rows: outputs, at most PTQ_FP8_MAX_OUTPUTS); scales dense [ceil(rows/128), ceil(cols/128)]. */

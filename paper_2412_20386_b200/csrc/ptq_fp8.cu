@@ -238,6 +238,7 @@ ptq_status_t ptq_fp8_quantize(const ptq_fp8_input_t *in, void *codes, int64_t co
     if (!scales || !scales_pitch) return fail(PTQ_ERR_NULL, "the scales or their pitches are NULL");
     if (!aligned({scales}, 4)) return fail(PTQ_ERR_ALIGN, "the scales are not aligned to their type");
     if (!not_negative({scales_pitch[0], scales_pitch[1]})) return fail(PTQ_ERR_SHAPE, "a pitch is negative");
+    if ((in->rows > 1 && scales_pitch[0] == 0) || (blocks_of(in->cols) > 1 && scales_pitch[1] == 0)) return fail(PTQ_ERR_SHAPE, "scales overlap");
     PTQ_TRY(check_arch());
     return quantize(*in, codes, codes_pitch, scales, scales_pitch[0], scales_pitch[1], static_cast<cudaStream_t>(stream));
 }

@@ -144,6 +144,13 @@ def test_fp8_refusals(lib):
     assert linear(x=inp(cols=96, rows=100)) == SHAPE and linear(y=None) == NULL and linear(pitch=1) == SHAPE
 
 
+def test_fp8_scales_that_are_written_do_not_overlap(lib):
+    q = lambda x, pitches: lib.ptq_fp8_quantize(ctypes.byref(x), vp(P), i64(x.cols + 15 & ~15), vp(P), (i64 * 2)(*pitches), None)
+    assert q(inp(rows=3, cols=100), (0, 1)) == SHAPE and q(inp(rows=1, cols=300), (1, 0)) == SHAPE
+    if not torch.cuda.is_available():                        # a single row, a single block: any pitch will do
+        assert q(inp(rows=1, cols=300), (0, 1)) in (ARCH, CUDA) and q(inp(rows=3, cols=100), (1, 0)) in (ARCH, CUDA)
+
+
 def test_without_a_device_a_good_call_fails_with_an_error_code(lib):
     if torch.cuda.is_available():
         pytest.skip("a CUDA device is present")
