@@ -794,6 +794,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
         if (!outputs) read_state<kWhole>(S, from, p0, n0, a.cols, p.states, lane);
     }
     const bool started = kOut && (seg > 0 || p.state);    // else the state in front of the first chunk is zero
+    // this segment holds the last step (or is the first one of an empty sequence): its state is the final one
+    const bool ends = kOut && p.final_state && seg == (chunks > 0 ? (chunks - 1) / p.segment_chunks : 0);
     double log_decay = 0.0;
     const bool busy = !outputs && p0 < a.cols;            // this warp has columns of the state
     // the state as an operand: its columns brought into binary16's range
@@ -830,11 +832,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
         }
         if (M::kStages == 2 && next) load(chunk_of(i + 1), s ^ 1);
         const HeadFactors &f = factors[s];
+        const int sixteens = (min(a.n - first, kHeadSteps) + 15) / 16;                  // sets of 16 steps that are there
         if (outputs && i >= 0) {
             const float *pair = f.pair[r];
             const float l0 = pair[p0 + g], l1 = pair[p0 + g + 8], r0 = fast_exp2(l0), r1 = fast_exp2(l1);
             float y[8][4] = {};
-            if (i > 0 || started) {                        // what the state gives these 16 steps
+            if ((i > 0 || started) && r < sixteens) {      // what the state gives these 16 steps
 #pragma unroll 2
                 for (int k = 0; k < NP / 16; ++k) {
                     const HeadA<T> c = load_a(tile_C(s), kWP, p0, 16 * k, lane);
@@ -861,7 +864,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
             const int j0 = p.share ? (r + 1) / 2 : 0;      // the ones before: by the states' warps
             HeadScale sc = {1.0f, 1.0f};
 #pragma unroll 1
-            for (int j = j0; j <= r; ++j) {
+            for (int j = j0; j <= r && r < sixteens; ++j) {
                 const bool diagonal = j == r;
                 float m[2][4], odd[2][4];                  // two chains of products each
 #pragma unroll
@@ -1014,6 +1017,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
             // binary16, 144.7 -> 141.6), but with operands in three parts and two CTAs to an SM the states' warps are the slower ones
             // (bfloat16, 2 x 20011 x 16 heads: 349 -> 368 us): not there.
             const int hr = r == 0 ? 3 : 4 - r, hj = r == 1 ? 1 : 0;
+            if (hr < sixteens) {
             const float *pair = f.pair[hr];
             float m[2][4];
 #pragma unroll
@@ -1048,11 +1052,14 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
                     help[r * 256 + (2 * q + n) * 32 + lane] = make_float4(x[0] * sc.down, x[1] * sc.down, x[2] * sc.down, x[3] * sc.down);
                 }
             }
+            } else if (M::kOverState) {
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+            }
             asm volatile("bar.arrive 2, 256;" ::: "memory");
         }
         if (i >= 0) {
             log_decay += f.log_decay;
-            if (busy) state_update<NP, kN>(S, tile_u(s), tile_B(s), f.state, f.decay, p0, n0, lane);
+            if (busy && (!kOut || next || ends)) state_update<NP, kN>(S, tile_u(s), tile_B(s), f.state, f.decay, p0, n0, lane);
             // the outputs' warps have read the state, or what lies over it
             if (kOut && !outputs) asm volatile("bar.sync %0, 256;" ::"r"(M::kOverState && p.share ? 3 : 1) : "memory");
         }
@@ -1066,8 +1073,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
         }
     }
     if constexpr (kOut) {
-        // final states: by the segment that holds the last step, or the first one of an empty sequence
-        if (!outputs && p.final_state && seg == (chunks > 0 ? (chunks - 1) / p.segment_chunks : 0))
+        if (!outputs && ends)
             write_state<kWhole>(S, p.final_state + head_at * state_size + tile_at, p0, n0, a.cols, p.states, lane);
     } else {
         write_state<kWhole>(S, p.slots + (head_at * p.segments + seg) * state_size + tile_at, p0, n0, a.cols, p.states, lane);

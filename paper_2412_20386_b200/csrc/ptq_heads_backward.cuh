@@ -262,6 +262,7 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
             from = p.dfinal + head_at * state_size + tile_at;
         read_state<kWhole>(H, from, p0, 0, a.cols, p.states, lane);
     }
+    const bool starts = a.seg == 0 && p.final_state;      // G in front of this segment is wanted
     float delta[2] = {};                                  // of the next chunk, in warp 0, which forms the factors
     if (warp == 0 && count > 0) load_delta<T>(p, delta_at, chunk_of(0) * kHeadSteps, a.n, lane, delta);
     for (int i = -1; i < count; ++i) {
@@ -283,7 +284,9 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
         }
         if (M::kStages == 2 && next) load(chunk_of(i + 1), s ^ 1);
         const int step0 = first + p0 + g, step1 = step0 + 8;
+        const int sixteens = (min(a.n - first, kHeadSteps) + 15) / 16;                  // sets of 16 steps that are there
         if (i >= 0 && rows_i) {
+            if (r < sixteens) {
             const float *pair = f.pair[r];
             const float l0 = pair[p0 + g], l1 = pair[p0 + g + 8], r0 = fast_exp2(l0), r1 = fast_exp2(l1);
             // what the state gives dC
@@ -347,6 +350,10 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
             if (kScaled<T> && sc.down != 1.0f) scale_rows(d, sc.down, sc.down);
             write_part<NP, kWhole>(d, step0 < a.n ? p.part_C + (part_row + token(step0)) * p.states : nullptr,
                                    step1 < a.n ? p.part_C + (part_row + token(step1)) * p.states : nullptr, p.states, lane);
+            } else {
+                if (lane < 16) dot_C[p0 + lane] = 0.0f;
+                reinterpret_cast<float2 *>(pairs + r * kHeadSteps)[lane] = make_float2(0.0f, 0.0f);
+            }
             // <G, S> of this warp's columns, and G in front of the chunk
             float z = 0.0f;
 #pragma unroll
@@ -367,7 +374,9 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
 #pragma unroll
             for (int q = 16; q > 0; q >>= 1) z += __shfl_xor_sync(0xffffffffu, z, q);
             if (lane == 0) through[r] = z * f.decay;
-            if (p0 < a.cols) state_update<NP, NP / 8>(H, tile_dy(s), tile_C(s), f.into, f.decay, p0, 0, lane);
+            if (p0 < a.cols && (next || starts)) state_update<NP, NP / 8>(H, tile_dy(s), tile_C(s), f.into, f.decay, p0, 0, lane);
+        } else if (i >= 0 && r >= sixteens) {
+            if (lane < 16) dw[p0 + lane] = dot_B[p0 + lane] = 0.0f;
         } else if (i >= 0) {
             const float *pair = f.pair[r];
             const float l0 = pair[p0 + g], l1 = pair[p0 + g + 8], last = pair[p0 + 15], rest = f.rest[r];
@@ -395,7 +404,7 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
             HeadScale scx = {1.0f, 1.0f}, scd = {1.0f, 1.0f};
             float k0 = 0.0f, k1 = 0.0f;                   // column sums of K
 #pragma unroll 1
-            for (int j = r; j < 4; ++j) {
+            for (int j = r; j < sixteens; ++j) {
                 const bool diagonal = j == r;
                 float mp[2][4], mr[2][4];                 // M P and M R, transposed
                 scores<NP>(mp, tile_B(s), tile_C(s), p0, 16 * j, lane);
@@ -503,7 +512,7 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
         }
     }
     if (rows_i) {
-        if (a.seg == 0 && p.final_state) write_state<kWhole>(H, p.final_state + head_at * state_size + tile_at, p0, 0, a.cols, p.states, lane);
+        if (starts) write_state<kWhole>(H, p.final_state + head_at * state_size + tile_at, p0, 0, a.cols, p.states, lane);
 #pragma unroll
         for (int q = 16; q > 0; q >>= 1) skip_grad += __shfl_xor_sync(0xffffffffu, skip_grad, q);
         if (lane == 0) skip_sum[r] = skip_grad;
