@@ -403,8 +403,10 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
             // and what these steps and the ones behind them do, 16 at a time
             HeadScale scx = {1.0f, 1.0f}, scd = {1.0f, 1.0f};
             float k0 = 0.0f, k1 = 0.0f;                   // column sums of K
+            // (binary32: a bound that the compiler knows is worth more than the steps that are not there, 141 instead of 157 us of 8 x 784 x 6 heads)
+            const int sets = sizeof(T) == 2 ? sixteens : kHeadSteps / 16;
 #pragma unroll 1
-            for (int j = r; j < sixteens; ++j) {
+            for (int j = r; j < sets; ++j) {
                 const bool diagonal = j == r;
                 float mp[2][4], mr[2][4];                 // M P and M R, transposed
                 scores<NP>(mp, tile_B(s), tile_C(s), p0, 16 * j, lane);
