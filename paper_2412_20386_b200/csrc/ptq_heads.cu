@@ -228,7 +228,8 @@ ptq_status_t ptq_heads_backward(const ptq_heads_t *s, const float *history, cons
     PTQ_TRY(check_space(workspace, workspace_bytes, space.bytes));
     const bool fours = s->states % 4 == 0 && aligned({g->dB, g->dC}, 4 * e);
     const int64_t sums = ceil_div(static_cast<int64_t>(s->batch) * s->length * s->groups * (s->states / (fours ? 4 : 1)), 256);
-    if (sums > kMaxGrid) return fail(PTQ_ERR_SHAPE, "the batch is too large for one launch");
+    const int64_t ctas = std::max(sums, static_cast<int64_t>(s->batch) * s->heads);
+    if (ctas > kMaxGrid) return fail(PTQ_ERR_SHAPE, "the batch is too large for one launch");
     PTQ_TRY(check_arch());
     ptq::HeadParams p = heads_params(*s, plan, dy);
     unsigned char *w = static_cast<unsigned char *>(workspace);
@@ -255,9 +256,8 @@ ptq_status_t ptq_heads_backward(const ptq_heads_t *s, const float *history, cons
             PTQ_TRY(fold(p, dfinal, 1, st));
         }
         PTQ_TRY(Launch::backward(p, whole, plan.segments > 1, st));
-        PTQ_TRY(launch_next(fours ? ptq::ptq_heads_finish_kernel<T, 4> : ptq::ptq_heads_finish_kernel<T, 1>, dim3(static_cast<unsigned>(sums), 2), 256, 0, st, p,
-                            static_cast<T *>(g->dB), static_cast<T *>(g->dC)));
-        PTQ_TRY(launch_next(ptq::ptq_heads_finish_delta_kernel<T>, dim3(static_cast<unsigned>(s->batch * s->heads)), 512, 0, st, p, static_cast<T *>(g->ddelta), shares));
+        PTQ_TRY(launch_next(fours ? ptq::ptq_heads_finish_kernel<T, 4> : ptq::ptq_heads_finish_kernel<T, 1>, dim3(static_cast<unsigned>(ctas), 3), 256, 0, st, p,
+                            static_cast<T *>(g->dB), static_cast<T *>(g->dC), static_cast<T *>(g->ddelta), shares));
         return launch_next(ptq::ptq_heads_finish_sums_kernel, dim3(static_cast<unsigned>(s->heads)), 128, 0, st, p, shares, g->dA, g->ddelta_bias, g->dD);
     });
 }
