@@ -47,7 +47,8 @@ struct HeadsPlan {
 HeadsPlan heads_plan(const ptq_heads_t &s, bool backward)
 {
     const long long base = static_cast<long long>(s.batch) * s.heads * col_tiles(s), chunks = chunks_of(s);
-    const double resident = backward || (s.dtype == PTQ_F32 && s.states > 64) ? kSms : 2 * kSms, unit = backward ? 4.0 : 1.5, sums = backward ? 1.0 : 0.75;
+    const bool two = s.dtype != PTQ_F32 && (!backward || s.states <= 64);
+    const double resident = two ? 2 * kSms : kSms, unit = backward ? 4.0 : 1.5, sums = backward ? 1.0 : 0.75;
     // a padded batch holds about half the steps
     const double filled = s.lengths ? 0.5 : 1.0;
     long long best = 1;
