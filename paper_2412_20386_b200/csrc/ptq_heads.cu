@@ -38,9 +38,12 @@ ptq_status_t heads_check(const ptq_heads_t *s)
 int col_tiles(const ptq_heads_t &s) { return static_cast<int>(ceil_div(s.cols, ptq::kHeadCols)); }
 int chunks_of(const ptq_heads_t &s) { return static_cast<int>(ceil_div(s.length, ptq::kHeadSteps)); }
 
-// Sequences are cut into segments where there are too few heads to fill the GPU: states of all segments but the last are summed first, which
-// takes about half of the outputs' time, and joined (another 6 us); a chunk takes about 1.5 us, in the backward pass 4.  An SM has two
-// CTAs of the forward kernel, one of the backward kernel.
+// Sequences are cut into segments where there are too few heads to fill the GPU: the states of all segments but the last are summed first
+// and joined.  A chunk of the forward pass costs 1.5 here, of the sums half of that, of the backward pass 8 (its sums 1), the join 6 and
+// some per segment (in about two microseconds).  An SM has one CTA where activations are binary32 and of the backward pass with
+// more than 64 states, else two; the last of several rounds is taken to be half full.  2 x 20011 x 16 heads (bfloat16, 128 states) in 4, 9
+// and 18 segments: 554, 357, 373 us; training 8 x 784 x 6 heads (binary32, 16 states), the backward pass in 1, 3 and 13: 280, 212, 190;
+// 1 x 197 x 6 heads (binary16, 64 states) in 1 and 4: 14.4 and 18.3.
 struct HeadsPlan {
     int segments, segment_chunks;
 };
@@ -48,14 +51,14 @@ HeadsPlan heads_plan(const ptq_heads_t &s, bool backward)
 {
     const long long base = static_cast<long long>(s.batch) * s.heads * col_tiles(s), chunks = chunks_of(s);
     const bool two = s.dtype != PTQ_F32 && (!backward || s.states <= 64);
-    const double resident = two ? 2 * kSms : kSms, unit = backward ? 4.0 : 1.5, sums = backward ? 1.0 : 0.75;
+    const double resident = two ? 2 * kSms : kSms, unit = backward ? 8.0 : 1.5, sums = backward ? 1.0 : 0.75;
     // a padded batch holds about half the steps
     const double filled = s.lengths ? 0.5 : 1.0;
     long long best = 1;
     double least = -1.0;
     for (long long n = 1; n <= chunks && n <= 256 && base * n <= 16 * kSms; ++n) {
         const long long per = ceil_div(chunks, n);
-        const double waves = std::max(1.0, std::ceil(filled * static_cast<double>(base * n) / resident - 0.02));
+        const double full = filled * static_cast<double>(base * n) / resident, waves = std::max(1.0, 0.5 * (full + std::ceil(full - 0.02)));
         const double cost = waves * per * unit + (n > 1 ? waves * per * sums + 6.0 + 0.1 * n : 0.0);
         if (least < 0.0 || cost < least) {
             least = cost;
