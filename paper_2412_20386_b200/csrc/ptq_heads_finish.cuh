@@ -75,7 +75,7 @@ __device__ __forceinline__ void finish_delta(const HeadParams &p, int b, int h, 
 
 // blockIdx.y 0: ddelta; dB (1) and dC (2): the heads of a group and their column tiles summed in their order, rounded; kN neighbouring
 // states a thread (four where `states` and the outputs' alignment allow it).  Bound by reading the binary32 parts once: 77 MB of a
-// training batch of 64 x 197 x 12 heads, 64 states, in 20 us, ddelta beside it (8 us as a launch of its own).
+// training batch of 64 x 197 x 12 heads, 64 states, in 20 us, 23 with ddelta beside it (9 us as a launch of its own).
 template <typename T, int kN>
 __global__ void __launch_bounds__(256) ptq_heads_finish_kernel(const HeadParams p, T *dB, T *dC, T *ddelta, float2 *shares)
 {
