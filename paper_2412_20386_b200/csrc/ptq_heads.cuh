@@ -515,65 +515,65 @@ __device__ __forceinline__ void state_update(float (&S)[kN][4], const T *x, cons
     const float down = scu.down * scf.down;
 #pragma unroll
     for (int k0 = 0; k0 < kHeadSteps / 16; k0 += kSet) {
-    HeadA<T> part[kSet][kHeadParts<T>];
-#pragma unroll
-    for (int ks = 0; ks < kSet; ++ks) {
-        const int k = k0 + ks;
-        const float2 f0 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t), f1 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t + 8);
-        if constexpr (std::is_same<T, __half>::value) {
-            // u f as two binary16 values in binary16 arithmetic: f in two parts, the product with the upper one and what its
-            // rounding left (a fused multiply-add leaves it whole), plus that with the lower one
-            uint32_t fh[2], fl[2];
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                uint32_t r[2];
-                head_split<T>((q ? f1.x : f0.x) * scf.up, (q ? f1.y : f0.y) * scf.up, r);
-                fh[q] = r[0];
-                fl[q] = r[1];
-            }
-            const __half2 up = __float2half2_rn(scu.up);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&a[k].r[i]), up);
-                const __half2 h = *reinterpret_cast<const __half2 *>(&fh[i >> 1]), l = *reinterpret_cast<const __half2 *>(&fl[i >> 1]);
-                const __half2 hi = __hmul2_rn(v, h), lo = __hfma2(v, l, __hfma2(v, h, __hneg2(hi)));
-                part[ks][0].r[i] = *reinterpret_cast<const uint32_t *>(&hi);
-                part[ks][1].r[i] = *reinterpret_cast<const uint32_t *>(&lo);
-            }
-        } else if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 v = head_unpack<T>(a[k].r[i]), q = i < 2 ? f0 : f1;
-                uint32_t r[kHeadParts<T>];
-                head_split<T>(v.x * q.x, v.y * q.y, r);
-#pragma unroll
-                for (int j = 0; j < kHeadParts<T>; ++j) part[ks][j].r[i] = r[j];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) part[ks][0].v[i] = a[k].v[i] * (i < 4 ? (i & 1 ? f0.y : f0.x) : (i & 1 ? f1.y : f1.x));
-        }
-    }
-#pragma unroll
-    for (int n = 0; n < kN / 2; ++n) {
-        float sum[2][4];
+        HeadA<T> part[kSet][kHeadParts<T>];
 #pragma unroll
         for (int ks = 0; ks < kSet; ++ks) {
-            HeadB<T> b[2];
-            load_b_t(b, z, kZP, n0 + 16 * n, 16 * (k0 + ks), lane);
+            const int k = k0 + ks;
+            const float2 f0 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t), f1 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t + 8);
+            if constexpr (std::is_same<T, __half>::value) {
+                // u f as two binary16 values in binary16 arithmetic: f in two parts, the product with the upper one and what its
+                // rounding left (a fused multiply-add leaves it whole), plus that with the lower one
+                uint32_t fh[2], fl[2];
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    uint32_t r[2];
+                    head_split<T>((q ? f1.x : f0.x) * scf.up, (q ? f1.y : f0.y) * scf.up, r);
+                    fh[q] = r[0];
+                    fl[q] = r[1];
+                }
+                const __half2 up = __float2half2_rn(scu.up);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&a[k].r[i]), up);
+                    const __half2 h = *reinterpret_cast<const __half2 *>(&fh[i >> 1]), l = *reinterpret_cast<const __half2 *>(&fl[i >> 1]);
+                    const __half2 hi = __hmul2_rn(v, h), lo = __hfma2(v, l, __hfma2(v, h, __hneg2(hi)));
+                    part[ks][0].r[i] = *reinterpret_cast<const uint32_t *>(&hi);
+                    part[ks][1].r[i] = *reinterpret_cast<const uint32_t *>(&lo);
+                }
+            } else if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 v = head_unpack<T>(a[k].r[i]), q = i < 2 ? f0 : f1;
+                    uint32_t r[kHeadParts<T>];
+                    head_split<T>(v.x * q.x, v.y * q.y, r);
+#pragma unroll
+                    for (int j = 0; j < kHeadParts<T>; ++j) part[ks][j].r[i] = r[j];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) part[ks][0].v[i] = a[k].v[i] * (i < 4 ? (i & 1 ? f0.y : f0.x) : (i & 1 ? f1.y : f1.x));
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < kN / 2; ++n) {
+            float sum[2][4];
+#pragma unroll
+            for (int ks = 0; ks < kSet; ++ks) {
+                HeadB<T> b[2];
+                load_b_t(b, z, kZP, n0 + 16 * n, 16 * (k0 + ks), lane);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int q = kHeadParts<T> - 1; q >= 0; --q) head_mma(sum[j], part[ks][q], b[j], ks == 0 && q == kHeadParts<T> - 1);
+            }
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int q = kHeadParts<T> - 1; q >= 0; --q) head_mma(sum[j], part[ks][q], b[j], ks == 0 && q == kHeadParts<T> - 1);
+                for (int i = 0; i < 4; ++i) {
+                    const float v = kScaled<T> ? sum[j][i] * down : sum[j][i];
+                    S[2 * n + j][i] = k0 == 0 ? fmaf(decay, S[2 * n + j][i], v) : S[2 * n + j][i] + v;
+                }
         }
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float v = kScaled<T> ? sum[j][i] * down : sum[j][i];
-                S[2 * n + j][i] = k0 == 0 ? fmaf(decay, S[2 * n + j][i], v) : S[2 * n + j][i] + v;
-            }
-    }
     }
 }
 
@@ -1025,40 +1025,40 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
             // (bfloat16, 2 x 20011 x 16 heads: 349 -> 368 us): not there.
             const int hr = r == 0 ? 3 : 4 - r, hj = r == 1 ? 1 : 0;
             if (hr < sixteens) {
-            const float *pair = f.pair[hr];
-            float m[2][4];
+                const float *pair = f.pair[hr];
+                float m[2][4];
 #pragma unroll
-            for (int k = 0; k < NP / 16; ++k) {
-                HeadB<T> b[2];
-                load_b(b, tile_B(s), kWP, 16 * hj, 16 * k, lane);
-                const HeadA<T> c = load_a(tile_C(s), kWP, 16 * hr, 16 * k, lane);
-                head_mma(m[0], c, b[0], k == 0);
-                head_mma(m[1], c, b[1], k == 0);
-            }
-            const float r0 = fast_exp2(pair[16 * hr + g]), r1 = fast_exp2(pair[16 * hr + g + 8]);
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const float2 v = *reinterpret_cast<const float2 *>(pair + 16 * hj + 8 * n + 2 * t);
-                m[n][0] *= r0 * v.x;
-                m[n][1] *= r0 * v.y;
-                m[n][2] *= r1 * v.x;
-                m[n][3] *= r1 * v.y;
-            }
-            HeadScale sc = {1.0f, 1.0f};
-            if constexpr (kScaled<T>) sc = scale_for(warp_top<2>(m));
-            const HeadA<T> w = acc_to_a<T>(m[0], m[1], sc.up);
-            if (M::kOverState) asm volatile("bar.sync 1, 256;" ::: "memory");              // the outputs' warps have read the state
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                HeadB<T> b[2];
-                load_b_t(b, tile_u(s), kXP, 16 * q, 16 * hj, lane);
+                for (int k = 0; k < NP / 16; ++k) {
+                    HeadB<T> b[2];
+                    load_b(b, tile_B(s), kWP, 16 * hj, 16 * k, lane);
+                    const HeadA<T> c = load_a(tile_C(s), kWP, 16 * hr, 16 * k, lane);
+                    head_mma(m[0], c, b[0], k == 0);
+                    head_mma(m[1], c, b[1], k == 0);
+                }
+                const float r0 = fast_exp2(pair[16 * hr + g]), r1 = fast_exp2(pair[16 * hr + g + 8]);
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
-                    float x[4];
-                    head_mma(x, w, b[n], true);
-                    help[r * 256 + (2 * q + n) * 32 + lane] = make_float4(x[0] * sc.down, x[1] * sc.down, x[2] * sc.down, x[3] * sc.down);
+                    const float2 v = *reinterpret_cast<const float2 *>(pair + 16 * hj + 8 * n + 2 * t);
+                    m[n][0] *= r0 * v.x;
+                    m[n][1] *= r0 * v.y;
+                    m[n][2] *= r1 * v.x;
+                    m[n][3] *= r1 * v.y;
                 }
-            }
+                HeadScale sc = {1.0f, 1.0f};
+                if constexpr (kScaled<T>) sc = scale_for(warp_top<2>(m));
+                const HeadA<T> w = acc_to_a<T>(m[0], m[1], sc.up);
+                if (M::kOverState) asm volatile("bar.sync 1, 256;" ::: "memory");              // the outputs' warps have read the state
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    HeadB<T> b[2];
+                    load_b_t(b, tile_u(s), kXP, 16 * q, 16 * hj, lane);
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        float x[4];
+                        head_mma(x, w, b[n], true);
+                        help[r * 256 + (2 * q + n) * 32 + lane] = make_float4(x[0] * sc.down, x[1] * sc.down, x[2] * sc.down, x[3] * sc.down);
+                    }
+                }
             } else if (M::kOverState) {
                 asm volatile("bar.sync 1, 256;" ::: "memory");
             }
