@@ -5,6 +5,14 @@
 
 namespace ptq {
 
+// 2^l v + w for any l: growth over a segment may leave binary32's range where what it multiplies (nothing, or a small state) does not.
+__device__ __forceinline__ float fold_add(float l, float v, float w)
+{
+    if (l < 126.0f) return fmaf(exp2f(l), v, w);
+    const float whole = rintf(l);
+    return scalbnf(v * exp2f(l - whole), static_cast<int>(whole)) + w;
+}
+
 // Joins the segments, one element of a state per thread: slot s becomes the state behind segment s (gradients: that in front of
 // it); forward, the last slot a copy of the start.
 __global__ void __launch_bounds__(256) ptq_heads_fold_kernel(float *slots, const float *logs, const float *start, int64_t heads, int segments, int64_t size, int grad)
@@ -18,7 +26,7 @@ __global__ void __launch_bounds__(256) ptq_heads_fold_kernel(float *slots, const
         for (int k = 0; k < segments - 1; ++k) {
             const int s = grad ? segments - 1 - k : k;
             float *slot = slots + (head * segments + s) * size + e;
-            v = k == 0 && !start ? *slot : fmaf(exp2f(logs[head * segments + s]), v, *slot);
+            v = k == 0 && !start ? *slot : fold_add(logs[head * segments + s], v, *slot);
             *slot = v;
         }
     }
