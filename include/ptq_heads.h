@@ -36,8 +36,8 @@ extern "C" {
  *     e = delta[t,h] + delta_bias[h];  dt = log(1 + exp(e)), or e, or 1 where delta is NULL
  *     S[h,p,n] <- exp(dt A[h]) S[h,p,n] + dt u[t,h,p] B[t,g,n]
  *     y[t,h,p] = sum_n S[h,p,n] C[t,g,n] + D[h] u[t,h,p]
- * Decays are at most 1 in a trained model (A <= 0, dt >= 0); growth is computed as long as it stays in binary32's range over
- * 64 steps.  A may be -inf.
+ * Decays are at most 1 in a trained model (A <= 0, dt >= 0); growth is computed as long as it, and dt u B times it, stay in binary32's
+ * range over 64 steps.  A decay below 2^-126 over up to 64 steps counts as zero.  A may be -inf.
  *
  * Accuracy: steps are taken 64 at a time as matrix products.  16-bit operands enter the tensor cores as they are, sums are
  * binary32; products of two operands and the state are rounded to the activations' type where they become operands themselves

@@ -336,21 +336,25 @@ __device__ __forceinline__ float warp_top(const float (&d)[N][4])
     }
     return top;
 }
-// The power of two, within 2^-60 .. 2^60, that brings `top` into 2^13 .. 2^14, and its inverse; 1 where `top` is 2^-4 .. 2^15: what
-// binary16 cannot hold is less than 2^-21 of it then, and what need not be scaled is not.
 struct HeadScale {
     float up, down;
 };
-__device__ __forceinline__ HeadScale exact_scale(float top, int to, int most)          // into 2^to .. 2^(to + 1), within 2^-most .. 2^most
+// The power of two, within 2^-126 .. 2^most, that brings `top` into 2^to .. 2^(to + 1), and its inverse.
+__device__ __forceinline__ HeadScale exact_scale(float top, int to, int most)
 {
-    const int e = top == 0.0f ? 0 : max(-most, min(most, to + 127 - static_cast<int>(__float_as_uint(top) >> 23)));
+    const int e = top == 0.0f ? 0 : max(-126, min(most, to + 127 - static_cast<int>(__float_as_uint(top) >> 23)));
     return {__uint_as_float(static_cast<uint32_t>(127 + e) << 23), __uint_as_float(static_cast<uint32_t>(127 - e) << 23)};
 }
+// Into 2^13 .. 2^14; 1 where `top` is 2^-4 .. 2^15: what binary16 cannot hold is less than 2^-21 of it then, and what need not be scaled is
+// not.  `most`: 126 for states, which a growing chunk makes large from however small; 60 for operands whose products join sums that
+// are scaled with them (smaller ones vanish beside what binary16 holds in the result).
+template <int kMost>
 __device__ __forceinline__ HeadScale scale_for(float top)
 {
     if (top >= 0.0625f && top < 32768.0f) return {1.0f, 1.0f};
-    return exact_scale(top, 13, 60);
+    return exact_scale(top, 13, kMost);
 }
+constexpr int kScaleSums = 60, kScaleState = 126;
 
 // ---------------------------------------------------------------------------------------------------- loads
 __device__ __forceinline__ void cp_async(uint32_t dst, const void *src, int bytes, bool on)
@@ -505,9 +509,11 @@ __device__ __forceinline__ void state_update(float (&S)[kN][4], const T *x, cons
 #pragma unroll
             for (int i = 0; i < 4; ++i) most = __hmax2(most, __habs2(*reinterpret_cast<const __half2 *>(&a[k].r[i])));
         const float2 v = __half22float2(most), q = *reinterpret_cast<const float2 *>(f + 2 * lane);
-        // a power of two that binary16 holds; an infinity counts as the largest finite value
-        scu = exact_scale(warp_max(fminf(fmaxf(v.x, v.y), 65504.0f)), 14, 15);
-        scf = exact_scale(warp_max(fmaxf(finite_abs(q.x), finite_abs(q.y))), -1, 60);
+        const float top = warp_max(fmaxf(finite_abs(q.x), finite_abs(q.y)));
+        scf = exact_scale(top, -1, 126);
+        // a power of two that binary16 holds; an infinity counts as the largest finite value (factors of growth that 2^-126 leaves above 1: to
+        // less than 4 then, and u to 2^13)
+        scu = exact_scale(warp_max(fminf(fmaxf(v.x, v.y), 65504.0f)), top < 0x1p126f ? 14 : 12, 15);
     }
     // the chunk's sums on their own, joined with the state in binary32: the tensor cores' sums are cut off, not rounded
     // (beside all states of 16 columns three parts of 64 steps are too many registers: 32 steps at a time)
@@ -811,7 +817,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
             write_state<kWhole>(S, p.history + ((static_cast<int64_t>(a.b) * p.chunks + chunk) * p.heads + a.h) * state_size + tile_at, p0, n0, a.cols, p.states, lane);
         HeadScale sc = {1.0f, 1.0f};
         if constexpr (kScaled<T>) {
-            sc = scale_for(warp_top<kN>(S));
+            sc = scale_for<kScaleState>(warp_top<kN>(S));
             if (lane == 0) powers[r] = sc.down;
         }
         const auto store = [&](float by) {
@@ -911,7 +917,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
                     m[n][3] = col + 1 <= row + 8 ? (m[n][3] + odd[n][3]) * f11 : 0.0f;
                 }
                 if constexpr (kScaled<T>) {                // y is in the units of the smallest power of two so far
-                    const HeadScale now = scale_for(warp_top<2>(m));
+                    const HeadScale now = scale_for<kScaleSums>(warp_top<2>(m));
                     if (j == j0 ? now.up != 1.0f : now.up < sc.up) {
                         const float by = now.up * sc.down;
 #pragma unroll
@@ -1045,7 +1051,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
                     m[n][3] *= r1 * v.y;
                 }
                 HeadScale sc = {1.0f, 1.0f};
-                if constexpr (kScaled<T>) sc = scale_for(warp_top<2>(m));
+                if constexpr (kScaled<T>) sc = scale_for<kScaleSums>(warp_top<2>(m));
                 const HeadA<T> w = acc_to_a<T>(m[0], m[1], sc.up);
                 if (M::kOverState) asm volatile("bar.sync 1, 256;" ::: "memory");              // the outputs' warps have read the state
 #pragma unroll

@@ -165,7 +165,7 @@ template <typename T, int N>
 __device__ __forceinline__ void join_scale(float (&m)[2][4], float (&sums)[N][4], HeadScale &sc, bool first)
 {
     if constexpr (kScaled<T>) {
-        const HeadScale now = scale_for(warp_top<2>(m));
+        const HeadScale now = scale_for<kScaleSums>(warp_top<2>(m));
         if (first ? now.up != 1.0f : now.up < sc.up) {
             const float by = now.up * sc.down;
             scale_rows(sums, by, by);
@@ -281,8 +281,8 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
                 const float top = warp_top<NP / 8>(H);
                 if (lane == 0) tops[warp] = top;
                 __syncthreads();
-                scG = scale_for(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
-                scS = scale_for(fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
+                scG = scale_for<kScaleState>(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+                scS = scale_for<kScaleState>(fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
             }
             store_parts<NP>(rows_i ? G_op : S_op, H, rows_i ? scG.up : scS.up, p0, lane);
             cp_async_wait<0>();

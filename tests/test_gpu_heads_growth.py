@@ -77,3 +77,49 @@ def test_gradients_grow_over_a_segment(ptq, dtype, end):
     for k, v in g.items():
         if v is not None:
             close(v, value[k], scale[k], ref.factor(k, v.dtype, limit(L)), "d" + k)
+
+
+@pytest.mark.parametrize("H", [2, 160], ids=["few heads", "many heads"])
+def test_binary16_operands_of_growth(ptq, H):
+    """Factors of up to 2^83 within 64 steps, of inputs that are zero and of ones that are as small as binary16 has them, and states that are as large."""
+    L = 256
+    t = make(F16, L, H, 8, 32)
+    t["delta"][:, 64:128] = -0.90625
+    t["delta"][:, 128:192] = 1.0
+    t["u"][:, 64:192] = 0
+    t["u"][:, 66, ::2] = 2.0 ** -24                          # grows to 2^57, and shrinks to 2^-35
+    t["u"][:, :64] = 0
+    t["C"][:, 64:192:2] = 0                                  # y of the others would be more than binary16 holds:
+    value, scale, _ = ref.solve(t, **KW)
+    final = torch.empty(1, H, 8, 32, device="cuda")
+    y = forward(ptq, t, final_state=final)
+    held = value["y"].abs() < 65504
+    assert held[:, ::2].all() and held[:, :, 1::2].all() and not held.all()
+    assert torch.isfinite(y.cpu()[held]).all()
+    close(torch.where(held.cuda(), y, 0), torch.where(held, value["y"], 0.0), torch.where(held, scale["y"], 1.0), ref.factor("y", F16, limit(L)), "y")
+    close(final, value["final"], scale["final"], limit(L), "final state")
+    # the gradients of a loss on the tokens in front of the growth and behind it
+    gen = torch.Generator().manual_seed(2)
+    dy = torch.randn(1, L, H, 8, generator=gen).half()
+    dy[:, 64:192] = 0
+    value, scale, _ = ref.solve(t, dy=dy, **KW)
+    history = ptq.head_scan_history(t["u"], 32)
+    forward(ptq, t, history=history)
+    g = ptq.head_scan_backward(dy.cuda(), t["u"], t["delta"], t["A"], t["B"], t["C"], history, D=t["D"], **KW)
+    for k, v in g.items():
+        if v is not None:
+            assert value[k].abs().max() < 65504
+            close(v, value[k], scale[k], ref.factor(k, v.dtype, limit(L)), "d" + k)
+
+
+def test_binary16_growth_over_a_segment(ptq):
+    """test_growth_over_a_segment in binary16, which cannot hold what grows: nothing does."""
+    L = 3000
+    t = make(F16, L, 2, 16, 16)
+    t["u"][:, :256] = 0
+    t["delta"][:, 128:256] = -0.90625
+    value, scale, _ = ref.solve(t, **KW)
+    final = torch.empty(1, 2, 16, 16, device="cuda")
+    y = forward(ptq, t, final_state=final)
+    close(y, value["y"], scale["y"], ref.factor("y", F16, limit(L)), "y")
+    close(final, value["final"], scale["final"], limit(L), "final state")
