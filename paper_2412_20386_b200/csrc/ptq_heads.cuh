@@ -916,9 +916,10 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
                     m[n][2] = col <= row + 8 ? (m[n][2] + odd[n][2]) * f10 : 0.0f;
                     m[n][3] = col + 1 <= row + 8 ? (m[n][3] + odd[n][3]) * f11 : 0.0f;
                 }
-                if constexpr (kScaled<T>) {                // y is in the units of the smallest power of two so far
-                    const HeadScale now = scale_for<kScaleSums>(warp_top<2>(m));
-                    if (j == j0 ? now.up != 1.0f : now.up < sc.up) {
+                if constexpr (kScaled<T>) {                // y goes along to the units of these scores, unless they are all zero
+                    const float top = warp_top<2>(m);
+                    const HeadScale now = top == 0.0f ? sc : scale_for<kScaleSums>(top);
+                    if (now.up != sc.up) {
                         const float by = now.up * sc.down;
 #pragma unroll
                         for (int n = 0; n < 8; ++n)

@@ -160,13 +160,15 @@ __device__ __forceinline__ void write_part(const float (&d)[NP / 8][4], float *r
         }
 }
 
-// Sixteen more steps of M R or M P as an operand: brings `sums`, which it is multiplied into, and `m` to a common power of two.
+// Sixteen more steps of M R or M P as an operand: brings `m`, unless it is zero, into binary16's range and `sums`, which it is multiplied into,
+// to the same power of two.
 template <typename T, int N>
-__device__ __forceinline__ void join_scale(float (&m)[2][4], float (&sums)[N][4], HeadScale &sc, bool first)
+__device__ __forceinline__ void join_scale(float (&m)[2][4], float (&sums)[N][4], HeadScale &sc)
 {
     if constexpr (kScaled<T>) {
-        const HeadScale now = scale_for<kScaleSums>(warp_top<2>(m));
-        if (first ? now.up != 1.0f : now.up < sc.up) {
+        const float top = warp_top<2>(m);
+        const HeadScale now = top == 0.0f ? sc : scale_for<kScaleSums>(top);
+        if (now.up != sc.up) {
             const float by = now.up * sc.down;
             scale_rows(sums, by, by);
             sc = now;
@@ -350,7 +352,7 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
                         for (int z = 4; z < 32; z <<= 1) pass[k] += __shfl_xor_sync(0xffffffffu, pass[k], z);
                     if (g == 0) *reinterpret_cast<float2 *>(pairs + r * kHeadSteps + col) = make_float2(pass[0], pass[1]);
                 }
-                join_scale<T>(m, d, sc, j == 0);
+                join_scale<T>(m, d, sc);
                 mma_rows<NP>(d, acc_to_a<T>(m[0], m[1], 1.0f), tile_B(s), 16 * j, lane);
             }
             if (kScaled<T> && sc.down != 1.0f) scale_rows(d, sc.down, sc.down);
@@ -436,9 +438,9 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
                             k1 += e;
                     }
                 }
-                join_scale<T>(mp, x, scx, diagonal);
+                join_scale<T>(mp, x, scx);
                 mma_rows<kHeadCols>(x, acc_to_a<T>(mp[0], mp[1], 1.0f), tile_dy(s), 16 * j, lane);
-                join_scale<T>(mr, d, scd, diagonal);
+                join_scale<T>(mr, d, scd);
                 mma_rows<NP>(d, acc_to_a<T>(mr[0], mr[1], 1.0f), tile_C(s), 16 * j, lane);
             }
 #pragma unroll
