@@ -15,7 +15,10 @@
 //
 // e^{L_i - L_j} is formed without a quotient of large numbers: the sums L are binary64, a warp's 16 steps refer to the sum in front
 // of them, so that each factor of an earlier step is one exponential per column of scores and one per row, and only the 16 x 16
-// block on the diagonal needs one per element.
+// block on the diagonal needs one per element.  For that block the sums themselves are kept: behind steps that leave nothing of the state
+// they are large and their differences are not.  A step counts as 2^-256 at most, so the sums are below 16 x 256; in binary32 their rounding is
+// 2^-16.5 of a factor behind one such step, 2^-12.5 behind fifteen.  That is below half a step of the 16-bit types; binary32 activations
+// have what the rounding leaves beside it (in all types: 2 % of the batch's time).
 //
 // What bounds it: the latency of dependent instructions.  128 x 197 x 12 heads of 64 columns, 128 states, binary16: 133 us, 0.7 TB/s of the
 // bytes that count and 94 TFLOP/s; issue slots 42 % busy, the tensor pipe 33 %, stalls fixed latency 2.1, barriers 2.0, shared
@@ -431,7 +434,8 @@ __device__ __forceinline__ void load_delta(const HeadParams &p, int64_t at, int 
         v[k] = d && i < n ? head_f32(d[at + (p.flags & kHeadsReverse ? n - 1 - i : i) * p.delta_l]) : 0.0f;
     }
 }
-// A2 = A log2 e.  Below 2^-4000 a step's decay counts as that (zero in binary32 either way), so that -inf does no harm in differences.
+// A2 = A log2 e.  Below 2^-256 a step's decay counts as that: nothing in binary32, whatever growth up to 2^127 is beside it, and -inf does no
+// harm in differences.
 __device__ __forceinline__ HeadSteps head_steps(const HeadParams &p, const float (&delta)[2], float bias, double A2, int first, int n, int lane)
 {
     HeadSteps s;
@@ -441,7 +445,7 @@ __device__ __forceinline__ HeadSteps head_steps(const HeadParams &p, const float
         s.dt[k] = on ? head_dt(p, delta[k], bias) : 0.0f;
         s.w[k] = !on ? 0.0f : p.flags & kHeadsUnscaled ? 1.0f : s.dt[k];
         double a = s.dt[k] == 0.0f ? 0.0 : static_cast<double>(s.dt[k]) * A2;
-        if (a < -4000.0) a = -4000.0;
+        if (a < -256.0) a = -256.0;
         s.sum[k] = a;
     }
     s.sum[1] += s.sum[0];
@@ -643,16 +647,34 @@ enum HeadMode {
 };
 
 // Factors of a chunk's steps, which one warp forms for all, a chunk ahead.  The sums refer to the step in front of each 16 steps r.
+template <typename T>
 struct HeadFactors {
     float state[kHeadSteps];          // of an input in the state behind the chunk (gradients: of an output in the one in front)
     float w[kHeadSteps];
     float into[kHeadSteps];           // e^{L}
     float pair[4][kHeadSteps];        // for the 16 steps r: of the steps in front of them e^{L_ref - L_j} w_j, of themselves log2 e^{L_j - L_ref}
+    float low[sizeof(T) == 4 ? kHeadSteps : 2];           // binary32 activations: what is left of that logarithm
     float decay, log_decay;           // of the chunk, log2 of it
     float pad[2];
 };
-template <int kMode>
-__device__ __forceinline__ void write_factors(HeadFactors &f, const HeadSteps &st, int lane)
+// What binary32 leaves of the logarithms of a lane's steps, which refer to the step in front of their 16.
+__device__ __forceinline__ void write_low(float *low, const HeadSteps &st, int lane)
+{
+    const double ref = __shfl_sync(0xffffffffu, st.sum[1], ((lane & 24) - 1) & 31), own = lane < 8 ? 0.0 : ref, x = st.sum[0] - own, y = st.sum[1] - own;
+    reinterpret_cast<float2 *>(low)[lane] = make_float2(static_cast<float>(x - static_cast<float>(x)), static_cast<float>(y - static_cast<float>(y)));
+}
+// d: of the rows row, row + 8 the differences with the columns col, col + 1.
+__device__ __forceinline__ void add_low(float (&d)[4], const float *low, int row, int col)
+{
+    const float2 z = *reinterpret_cast<const float2 *>(low + col);
+    const float z0 = low[row], z1 = low[row + 8];
+    d[0] += z0 - z.x;
+    d[1] += z0 - z.y;
+    d[2] += z1 - z.x;
+    d[3] += z1 - z.y;
+}
+template <int kMode, typename T>
+__device__ __forceinline__ void write_factors(HeadFactors<T> &f, const HeadSteps &st, int lane)
 {
     const double all = __shfl_sync(0xffffffffu, st.sum[1], 31);
     float2 *to = reinterpret_cast<float2 *>(&f) + lane;
@@ -670,10 +692,12 @@ __device__ __forceinline__ void write_factors(HeadFactors &f, const HeadSteps &s
             to[(3 + r) * kRow] = lane < 8 * r ? make_float2(pow2(ref - st.sum[0]) * st.w[0], pow2(ref - st.sum[1]) * st.w[1])
                                               : make_float2(static_cast<float>(st.sum[0] - ref), static_cast<float>(st.sum[1] - ref));
         }
+        if constexpr (sizeof(T) == 4) write_low(f.low, st, lane);
     }
     if (lane == 0) {
         f.decay = pow2(all);
-        f.log_decay = static_cast<float>(all);
+        // nothing of the state in front of the chunk comes through it: no growth behind it in the segment brings that back
+        f.log_decay = f.decay == 0.0f ? -1e30f : static_cast<float>(all);
     }
 }
 
@@ -689,7 +713,7 @@ struct HeadSmem {
     static constexpr int kState = kStages * kStage;
     static constexpr int kStaging = kState + (kMode == kHeadForward ? kWide : 0);
     static constexpr int kFactors = kStaging + (kMode == kHeadForward && sizeof(T) == 2 && !kOverC ? kNarrow : 0);
-    static constexpr int kPowers = kFactors + 2 * static_cast<int>(sizeof(HeadFactors));
+    static constexpr int kPowers = kFactors + 2 * static_cast<int>(sizeof(HeadFactors<T>));
     // what the states' warps add to outputs, 16 x 64 binary32 sums each: over the state's operand where that is large enough
     static constexpr bool kOverState = kWide >= 4 * 4096;
     static constexpr int kHelp = kOverState ? kState : kPowers + 4 * 4;
@@ -766,7 +790,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
     const auto tile_B = [&](int s) { return reinterpret_cast<T *>(smem + (M::kStages == 2 ? s * M::kStage : 0) + M::kNarrow); };
     const auto tile_C = [&](int s) { return reinterpret_cast<T *>(smem + (M::kStages == 2 ? s * M::kStage : 0) + M::kNarrow + M::kWide); };
     T *state_s = reinterpret_cast<T *>(smem + M::kState);
-    HeadFactors *factors = reinterpret_cast<HeadFactors *>(smem + M::kFactors);
+    HeadFactors<T> *factors = reinterpret_cast<HeadFactors<T> *>(smem + M::kFactors);
     float *powers = reinterpret_cast<float *>(smem + M::kPowers);
     float4 *help = reinterpret_cast<float4 *>(smem + M::kHelp);
 
@@ -844,7 +868,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
             __syncthreads();                              // the tiles, their steps' factors, and the state as an operand; the last chunk is done
         }
         if (M::kStages == 2 && next) load(chunk_of(i + 1), s ^ 1);
-        const HeadFactors &f = factors[s];
+        const HeadFactors<T> &f = factors[s];
         const int sixteens = (min(a.n - first, kHeadSteps) + 15) / 16;                  // sets of 16 steps that are there
         if (outputs && i >= 0) {
             const float *pair = f.pair[r];
@@ -905,10 +929,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
                         f11 = r1 * v.y;
                     } else {
                         const float2 w = *reinterpret_cast<const float2 *>(f.w + col);
-                        f00 = fast_exp2(l0 - v.x) * w.x;
-                        f01 = fast_exp2(l0 - v.y) * w.y;
-                        f10 = fast_exp2(l1 - v.x) * w.x;
-                        f11 = fast_exp2(l1 - v.y) * w.y;
+                        float d[4] = {l0 - v.x, l0 - v.y, l1 - v.x, l1 - v.y};
+                        if constexpr (sizeof(T) == 4) add_low(d, f.low, p0 + g, col);
+                        f00 = fast_exp2(d[0]) * w.x;
+                        f01 = fast_exp2(d[1]) * w.y;
+                        f10 = fast_exp2(d[2]) * w.x;
+                        f11 = fast_exp2(d[3]) * w.y;
                     }
                     const int row = diagonal ? p0 + g : kHeadSteps;                    // in front of the diagonal all count
                     m[n][0] = col <= row ? (m[n][0] + odd[n][0]) * f00 : 0.0f;

@@ -28,13 +28,16 @@ namespace ptq {
 // Factors of a chunk's steps, which one warp forms for all, a chunk ahead.  `pair[r]` refers to the steps' 16 steps r: of steps in front of
 // them e^{L_ref - L_j} (ref: the step in front of the 16), of themselves log2 e^{L_j - L_ref}, of steps behind them e^{L_i - L_last} (last: the
 // last of the 16).
+template <typename T>
 struct HeadBackFactors {
     float w[kHeadSteps], into[kHeadSteps];                // e^{L}
     float pair[4][kHeadSteps];
-    float rest[4];                                        // log2 e^{L_64 - L_ref}
-    float decay, pad[3];                                  // e^{L_64}
+    float low[sizeof(T) == 4 ? kHeadSteps : 2];           // binary32 activations: what is left of the logarithms of the steps
+    float rest[4], rest_low[4];                           // log2 e^{L_64 - L_ref}
+    float decay, pad;                                     // e^{L_64}
 };
-__device__ __forceinline__ void write_back_factors(HeadBackFactors &f, const HeadSteps &st, int lane)
+template <typename T>
+__device__ __forceinline__ void write_back_factors(HeadBackFactors<T> &f, const HeadSteps &st, int lane)
 {
     const double all = __shfl_sync(0xffffffffu, st.sum[1], 31);
     reinterpret_cast<float2 *>(f.w)[lane] = make_float2(st.w[0], st.w[1]);
@@ -47,8 +50,13 @@ __device__ __forceinline__ void write_back_factors(HeadBackFactors &f, const Hea
         for (int k = 0; k < 2; ++k)
             v[k] = lane < 8 * r ? pow2(ref - st.sum[k]) : lane < 8 * r + 8 ? static_cast<float>(st.sum[k] - ref) : pow2(st.sum[k] - last);
         reinterpret_cast<float2 *>(f.pair[r])[lane] = make_float2(v[0], v[1]);
-        if (lane == r) f.rest[r] = static_cast<float>(all - ref);
+        if (lane == r) {
+            const double x = all - ref;
+            f.rest[r] = static_cast<float>(x);
+            if constexpr (sizeof(T) == 4) f.rest_low[r] = static_cast<float>(x - static_cast<float>(x));
+        }
     }
+    if constexpr (sizeof(T) == 4) write_low(f.low, st, lane);
     if (lane == 0) f.decay = pow2(all);
 }
 
@@ -59,14 +67,14 @@ struct HeadBackSmem {
     static constexpr int kStage = 2 * kWide + 2 * kNarrow;
     static constexpr int kParts = kHeadParts<T>;                           // of S and G as operands
     static constexpr int kSums = 7 * kHeadSteps * 4;                       // floats: C . dC', dw, B . dB', 4 warps' K
-    static constexpr int kOther = 2 * kParts * kWide + 2 * static_cast<int>(sizeof(HeadBackFactors)) + kSums + 16 * 4;
+    static constexpr int kOther = 2 * kParts * kWide + 2 * static_cast<int>(sizeof(HeadBackFactors<T>)) + kSums + 16 * 4;
     // two CTAs to an SM where that is possible, else two stages
     static constexpr int kCtas = sizeof(T) == 2 && NP <= 64 ? 2 : 1;
     static constexpr int kStages = 2 * kStage + kOther <= (kCtas == 2 ? 113 : 227) * 1024 ? 2 : 1;
     static constexpr int kS = kStages * kStage;
     static constexpr int kG = kS + kParts * kWide;
     static constexpr int kFactors = kG + kParts * kWide;
-    static constexpr int kSum = kFactors + 2 * static_cast<int>(sizeof(HeadBackFactors));
+    static constexpr int kSum = kFactors + 2 * static_cast<int>(sizeof(HeadBackFactors<T>));
     static constexpr int kSmall = kSum + kSums;                            // floats: largest magnitudes [8], <G, S> [4], dD [4]
     static constexpr int kBytes = kSmall + 16 * 4;
 };
@@ -221,7 +229,7 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
     const auto tile_B = [&](int s) { return reinterpret_cast<T *>(stage(s) + 2 * M::kNarrow); };
     const auto tile_C = [&](int s) { return reinterpret_cast<T *>(stage(s) + 2 * M::kNarrow + M::kWide); };
     T *S_op = reinterpret_cast<T *>(smem + M::kS), *G_op = reinterpret_cast<T *>(smem + M::kG);
-    HeadBackFactors *factors = reinterpret_cast<HeadBackFactors *>(smem + M::kFactors);
+    HeadBackFactors<T> *factors = reinterpret_cast<HeadBackFactors<T> *>(smem + M::kFactors);
     float *dot_C = reinterpret_cast<float *>(smem + M::kSum), *dw = dot_C + kHeadSteps, *dot_B = dot_C + 2 * kHeadSteps;
     float *pairs = dot_C + 3 * kHeadSteps;                // [4]: what a warp's rows of K w pass over each step
     float *tops = reinterpret_cast<float *>(smem + M::kSmall), *through = tops + 8, *skip_sum = tops + 12;
@@ -276,7 +284,7 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
     for (int i = -1; i < count; ++i) {
         const int chunk = chunk_of(i), first = chunk * kHeadSteps, s = i & 1;
         const bool next = i + 1 < count;
-        const HeadBackFactors &f = factors[s];
+        const HeadBackFactors<T> &f = factors[s];
         HeadScale scS = {1.0f, 1.0f}, scG = {1.0f, 1.0f};
         if (i >= 0) {
             if constexpr (kScaled<T>) {                   // one power of two for all columns: they are summed over
@@ -320,12 +328,16 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
                 for (int q = 0; q < 2; ++q) {
                     const int col = 16 * j + 8 * q + 2 * t;
                     const float2 v = *reinterpret_cast<const float2 *>(pair + col), w = *reinterpret_cast<const float2 *>(f.w + col);
+                    float between[4] = {l0 - v.x, l0 - v.y, l1 - v.x, l1 - v.y};
+                    if constexpr (sizeof(T) == 4) {
+                        if (diagonal) add_low(between, f.low, p0 + g, col);
+                    }
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int at = col + (k & 1), row = p0 + g + (k < 2 ? 0 : 8);
                         const float vk = k & 1 ? v.y : v.x, wk = k & 1 ? w.y : w.x;
                         if (at == row) skip_grad += m[q][k];
-                        const float by = (diagonal ? fast_exp2((k < 2 ? l0 : l1) - vk) : (k < 2 ? r0 : r1) * vk) * wk;
+                        const float by = (diagonal ? fast_exp2(between[k]) : (k < 2 ? r0 : r1) * vk) * wk;
                         const bool on = !diagonal || at <= row;
                         m[q][k] = on ? m[q][k] * by : 0.0f;
                         P[q][k] = on ? m[q][k] * P[q][k] : 0.0f;
@@ -388,7 +400,15 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
         } else if (i >= 0) {
             const float *pair = f.pair[r];
             const float l0 = pair[p0 + g], l1 = pair[p0 + g + 8], last = pair[p0 + 15], rest = f.rest[r];
-            const float r0 = fast_exp2(last - l0), r1 = fast_exp2(last - l1), e0 = fast_exp2(rest - l0) * scG.down, e1 = fast_exp2(rest - l1) * scG.down;
+            float to_last[2] = {last - l0, last - l1}, to_end[2] = {rest - l0, rest - l1};
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    to_last[k] += f.low[p0 + 15] - f.low[p0 + g + 8 * k];
+                    to_end[k] += f.rest_low[r] - f.low[p0 + g + 8 * k];
+                }
+            }
+            const float r0 = fast_exp2(to_last[0]), r1 = fast_exp2(to_last[1]), e0 = fast_exp2(to_end[0]) * scG.down, e1 = fast_exp2(to_end[1]) * scG.down;
             const float w0 = f.w[p0 + g], w1 = f.w[p0 + g + 8];
             // what the state behind the chunk gives du and dB
             float x[8][4] = {}, d[NP / 8][4] = {};
@@ -423,11 +443,15 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
                 for (int q = 0; q < 2; ++q) {
                     const int col = 16 * j + 8 * q + 2 * t;
                     const float2 v = *reinterpret_cast<const float2 *>(pair + col);
+                    float between[4] = {l0 - v.x, l0 - v.y, l1 - v.x, l1 - v.y};
+                    if constexpr (sizeof(T) == 4) {
+                        if (diagonal) add_low(between, f.low, p0 + g, col);
+                    }
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int at = col + (k & 1), row = p0 + g + (k < 2 ? 0 : 8);
                         const float vk = k & 1 ? v.y : v.x;
-                        const float by = diagonal ? fast_exp2(vk - (k < 2 ? l0 : l1)) : (k < 2 ? r0 : r1) * vk;
+                        const float by = diagonal ? fast_exp2(-between[k]) : (k < 2 ? r0 : r1) * vk;
                         const bool on = !diagonal || at >= row;
                         mr[q][k] = on ? mr[q][k] * by : 0.0f;
                         const float e = on ? mr[q][k] * mp[q][k] : 0.0f;
