@@ -17,7 +17,7 @@
 // of them, so that each factor of an earlier step is one exponential per column of scores and one per row, and only the 16 x 16
 // block on the diagonal needs one per element.  For that block the sums themselves are kept: behind steps that leave nothing of the state
 // they are large and their differences are not.  A step counts as 2^-256 at most, so the sums are below 16 x 256; in binary32 their rounding is
-// 2^-16.5 of a factor behind one such step, 2^-12.5 behind fifteen.  That is below half a step of the 16-bit types; binary32 activations
+// 2^-15.5 of a factor behind one such step, 2^-12.5 behind fifteen.  That is below half a step of the 16-bit types; binary32 activations
 // have what the rounding leaves beside it (in all types: 2 % of the batch's time).
 //
 // What bounds it: the latency of dependent instructions.  128 x 197 x 12 heads of 64 columns, 128 states, binary16: 133 us, 0.7 TB/s of the
