@@ -54,8 +54,10 @@ __device__ __forceinline__ void finish_delta(const HeadParams &p, int b, int h, 
             }
             const float raw = delta ? head_f32(delta[b * p.delta_b + t * p.delta_l + h * p.delta_h]) : 0.0f, dt = head_dt(p, raw, bias);
             if (dt != 0.0f) sum_A += static_cast<double>(dt) * v.x;          // a step with dt = 0 keeps the state with any A
-            de = (v.x != 0.0f ? A * v.x : 0.0f) + (p.flags & kHeadsUnscaled ? 0.0f : v.y);
-            if (p.flags & kHeadsSoftplus) de *= 1.0f / (1.0f + expf(-(raw + bias)));
+            const float slope = p.flags & kHeadsSoftplus ? 1.0f / (1.0f + expf(-(raw + bias))) : 1.0f;
+            // an infinite rate does nothing where no step passes, and where softplus gives the step no length with any delta nearby
+            const bool rate = v.x != 0.0f && !(slope == 0.0f && isinf(A));
+            de = ((rate ? A * v.x : 0.0f) + (p.flags & kHeadsUnscaled ? 0.0f : v.y)) * slope;
             sum_bias += de;
         }
         if (ddelta) ddelta[row * p.heads + h] = head_round<T>(de);

@@ -55,3 +55,25 @@ def test_weak_steps_beside_strong_ones(ptq, dtype, strong, at, reverse):
         close(g[k], value[k], scale[k], ref.factor(k, dtype, Y + more), "d" + k)
     for k in ("delta", "A"):
         close(g[k], value[k], scale[k], GRADS + more, "d" + k)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32], ids=["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("none", [-200.0, -float("inf")], ids=str)
+def test_steps_of_no_length_with_an_infinite_rate(ptq, dtype, none):
+    """A = -inf: a step leaves nothing of the state, unless softplus gives it no length in binary32; then it leaves the state as it is, and delta has no gradient."""
+    at = [0, 5, 6, 40, 41, 42, 43, 44, 45, 46, 47, 48, 63]
+    t = make(dtype, -200.0, at)
+    t["A"] = torch.tensor([-float("inf"), -0.7], device="cuda")
+    t["delta_bias"] = torch.tensor([-1.0, 0.5], device="cuda")
+    gen = torch.Generator().manual_seed(6)
+    dy = torch.randn(1, 64, 2, 16, generator=gen).to(dtype)
+    value, scale, _ = ref.solve({**t, "A": torch.tensor([-1e30, -0.7])}, dy=dy)              # 64 bits: the same decays
+    t["delta"][:, at] = none
+    history = ptq.head_scan_history(t["u"], 16)
+    y = ptq.head_scan(t["u"], t["delta"], t["A"], t["B"], t["C"], delta_bias=t["delta_bias"], history=history)
+    close(y, value["y"], scale["y"], ref.factor("y", dtype, Y), "y")
+    g = ptq.head_scan_backward(dy.cuda(), t["u"], t["delta"], t["A"], t["B"], t["C"], history, delta_bias=t["delta_bias"])
+    for k in ("u", "B", "C"):
+        close(g[k], value[k], scale[k], ref.factor(k, dtype, Y), "d" + k)
+    for k in ("delta", "A", "delta_bias"):
+        close(g[k], value[k], scale[k], GRADS, "d" + k)
