@@ -2,6 +2,7 @@
 #include "../../include/ptq_fp8.h"
 
 #include <algorithm>
+#include <numeric>
 
 #include "ptq_block_host.h"
 #include "ptq_fp8.cuh"
@@ -61,6 +62,14 @@ ptq_status_t output_check(const void *y, int dtype, int64_t pitch, int outputs)
     if (pitch < outputs) return fail(PTQ_ERR_SHAPE, "rows of y overlap");
     if (!aligned({y}, elem_bytes(dtype))) return fail(PTQ_ERR_ALIGN, "y is not aligned to its type");
     return PTQ_OK;
+}
+
+// Whether two of rows x blocks scales have the same place: i rows on are j blocks on, with the least such i and j (not both zero).
+bool scales_overlap(int64_t rows, int64_t blocks, int64_t row, int64_t block)
+{
+    if (row == 0 && block == 0) return rows > 1 || blocks > 1;
+    const int64_t both = std::gcd(row, block);
+    return block / both < rows && row / both < blocks;
 }
 
 // Whether the rows of x can be read 16 bytes at a time.
@@ -238,7 +247,7 @@ ptq_status_t ptq_fp8_quantize(const ptq_fp8_input_t *in, void *codes, int64_t co
     if (!scales || !scales_pitch) return fail(PTQ_ERR_NULL, "the scales or their pitches are NULL");
     if (!aligned({scales}, 4)) return fail(PTQ_ERR_ALIGN, "the scales are not aligned to their type");
     if (!not_negative({scales_pitch[0], scales_pitch[1]})) return fail(PTQ_ERR_SHAPE, "a pitch is negative");
-    if ((in->rows > 1 && scales_pitch[0] == 0) || (blocks_of(in->cols) > 1 && scales_pitch[1] == 0)) return fail(PTQ_ERR_SHAPE, "scales overlap");
+    if (scales_overlap(in->rows, blocks_of(in->cols), scales_pitch[0], scales_pitch[1])) return fail(PTQ_ERR_SHAPE, "scales overlap");
     PTQ_TRY(check_arch());
     return quantize(*in, codes, codes_pitch, scales, scales_pitch[0], scales_pitch[1], static_cast<cudaStream_t>(stream));
 }
