@@ -36,3 +36,17 @@ def test_the_ends_of_the_sizes(ptq, dtype, M, K, N):
         want, scale = a[rows] @ w.t() + b.double(), a[rows].abs() @ w.abs().t() + b.double().abs()
         for got in (y, two):
             close(got[rows], want.cpu(), scale.cpu(), factor, "y")
+
+
+def test_weights_that_are_not_finite_make_their_128_columns_nan(ptq):
+    """In every form of the product."""
+    w = torch.randn(600, 300, device="cuda")
+    x = torch.randn(5000, 300, device="cuda", dtype=BF16)
+    codes, scales = ptq.fp8_quantize_weight(w)
+    for value in (float("nan"), float("inf")):
+        bad = w.clone()
+        bad[130, 257] = value
+        c, s = ptq.fp8_quantize_weight(bad)
+        for M in (1, 16, 17, 60, 300, 5000):
+            want, got = ptq.fp8_linear(x[:M], codes, scales), ptq.fp8_linear(x[:M], c, s)
+            assert torch.isnan(got[:, 128:256]).all() and torch.equal(got[:, :128], want[:, :128]) and torch.equal(got[:, 256:], want[:, 256:])
