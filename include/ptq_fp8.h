@@ -10,7 +10,8 @@
  *     y[m,n] = sum_b a_scale[m,b] w_scale[n / 128, b] sum_{k in block b} a[m,k] w[n,k]  (+ bias[n])
  * The products of a block of 128 are summed on the tensor cores in binary32, the blocks in binary32 in their order (where a
  * sum is split over several CTAs: parts in their order); the same call gives the same bits.  A block that holds an
- * infinity or NaN makes the row of the result NaN.
+ * infinity or NaN makes the row of the result NaN (of weights: its 128 columns).  The two scales are multiplied first: beyond binary32's range that
+ * makes infinities and NaN, below its normal values it is inexact or zero.
  *
  * Codes lie in rows on 16-byte boundaries: base and pitch are multiples of 16.  What lies between cols and the pitch is not read.
  */

@@ -36,8 +36,8 @@ extern "C" {
  *     e = delta[t,h] + delta_bias[h];  dt = log(1 + exp(e)), or e, or 1 where delta is NULL
  *     S[h,p,n] <- exp(dt A[h]) S[h,p,n] + dt u[t,h,p] B[t,g,n]
  *     y[t,h,p] = sum_n S[h,p,n] C[t,g,n] + D[h] u[t,h,p]
- * Decays are at most 1 in a trained model (A <= 0, dt >= 0); growth is computed as long as it, and dt u B times it, stay in binary32's
- * range over 64 steps.  A decay below 2^-126 over up to 64 steps counts as zero.  A may be -inf.
+ * Decays are at most 1 in a trained model (A <= 0, dt >= 0); growth is computed as long as it, and products of operands times it, stay in
+ * binary32's range over 64 steps.  A decay below 2^-126 over up to 64 steps counts as zero.  A may be -inf.
  *
  * Accuracy: steps are taken 64 at a time as matrix products.  16-bit operands enter the tensor cores as they are, sums are
  * binary32; products of two operands and the state are rounded to the activations' type where they become operands themselves
@@ -92,7 +92,8 @@ typedef struct {
  *   history   as the forward pass wrote it
  *   dy        device, [batch, length, heads, cols], dense
  *   dfinal    device, [batch, heads, cols, states], gradient of final_state, or NULL (zeros)
- *   workspace device, 16-byte aligned, at least ptq_heads_workspace_bytes(s, 1) bytes
+ *   workspace device, 16-byte aligned, at least ptq_heads_workspace_bytes(s, 1) bytes (8 for each token, head and state, for each 64 columns of
+ *             a head, and some more)
  */
 ptq_status_t ptq_heads_backward(const ptq_heads_t *s, const float *history, const void *dy, const float *dfinal, const ptq_heads_grads_t *grads,
                                 void *workspace, size_t workspace_bytes, void *stream);

@@ -139,7 +139,8 @@ __device__ __forceinline__ void store_codes8(uint8_t *row, int c, int cols, uint
 // (16 bytes of 16-bit values a lane), kSet neighbouring ones of a row at a time; the 16 half-warps of a CTA take 16 neighbouring rows,
 // whose scales lie next to each other in the layout that the product reads.  CTAs, as many as the SMs hold, go over the rows with the loads
 // of the next set under way while one is worked on; one division makes all scales of a step.  (One set per CTA and a division per block:
-// 26.7 us where this takes 20.6.)  50432 rows of 768 bfloat16 channels: 20.6 us, 5.7 TB/s; of 1536 39.6 us, 5.9 TB/s.
+// 26.7 us where this takes 20.7.)  50432 rows of 768 bfloat16 channels: 20.7 us where the same rows come again, 5.7 TB/s, 22.7 to 23.8 on others each time,
+// 5.0 to 5.2 TB/s; of 1536 channels 41.3 and 43.0 us, 5.7 and 5.5 TB/s.
 struct Fp8QuantizeParams {
     const void *x;
     int64_t x_pitch, codes_pitch, scale_row, scale_block;
@@ -192,7 +193,8 @@ __global__ void __launch_bounds__(256) ptq_fp8_quantize_kernel(const Fp8Quantize
     }
 }
 
-// Weights: one CTA goes over a block of 128 x 128 twice (it stays in L1).  Done once per layer.
+// Weights: one CTA goes over a block of 128 x 128 twice (it stays in L1), element by element.  Done once per layer.  8192 x 4096 in bfloat16: 43 us,
+// 2.3 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(256) ptq_fp8_quantize_weight_kernel(const Fp8QuantizeParams p)
 {
@@ -231,7 +233,7 @@ __global__ void __launch_bounds__(256) ptq_fp8_quantize_weight_kernel(const Fp8Q
 // parts through distributed shared memory in the order of the parts.
 //
 // What bounds it.  8192 x 4096 -> 8192: 241 us alone (2280 TFLOP/s, 68 % of twice the library's bf16 rate; the library's bf16 product of
-// this size takes 332), 279 in a long loop under the power limit: a k-block of a 128 x 256 tile is 128 columns of TMEM reads and as many fused
+// this size takes 332), 285 in a long loop under the power limit: a k-block of a 128 x 256 tile is 128 columns of TMEM reads and as many fused
 // multiply-adds for each of 8 warps, beside operands from L2.  Pairs of CTAs on one tile took twice as long, packed
 // multiply-adds and one accumulator for each team of warps no faster.  1 x 4096 -> 4096: 6.6 us, launch and one chain of loads (2.5 TB/s
 // of weights); 2048 x 2048 -> 2048 12.2 us.

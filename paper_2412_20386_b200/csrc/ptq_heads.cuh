@@ -20,6 +20,10 @@
 // 2^-15.5 of a factor behind one such step, 2^-12.5 behind fifteen.  That is below half a step of the 16-bit types; binary32 activations
 // have what the rounding leaves beside it (in all types: 2 % of the batch's time).
 //
+// 16-bit activations: scores times decays, and the state where C is multiplied by it, are rounded to the type as operands; each is off by half a step
+// of itself, as y is of y.  Against 64 bits y is off by 2.5e-4 of its size in binary16 and 2.1e-3 in bfloat16, where y rounded alone is by 2.1e-4 and
+// 1.7e-3; the results of a training step by 2.9e-4 and 2.3e-3.  Operands in two parts would be half as many products again.
+//
 // What bounds it: the latency of dependent instructions.  128 x 197 x 12 heads of 64 columns, 128 states, binary16: 133 us, 0.7 TB/s of the
 // bytes that count and 94 TFLOP/s; issue slots 42 % busy, the tensor pipe 33 %, stalls fixed latency 2.1, barriers 2.0, shared
 // memory 1.5 per instruction.  The states and sums of a CTA fill half of an SM's registers, so two CTAs are all there are.  One warp for 16
@@ -1015,7 +1019,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
                 if (M::kOverState) asm volatile("bar.arrive 3, 256;" ::: "memory");
             }
             const int step0 = first + p0 + g, step1 = step0 + 8;
-            // through shared memory (16-bit values: over this warp's rows of C, which nobody else reads) to whole 16-byte stores
+            // through shared memory (16-bit values: over this warp's rows of C) to whole 16-byte stores.  Of the states' warps, which read these rows
+            // where they share the work, barrier 2 has come after that; they read no others' rows of C otherwise.
             T *stage = M::kOverC ? tile_C(s) + p0 * kWP : reinterpret_cast<T *>(smem + M::kStaging) + p0 * kXP;
             if (M::kOverC) __syncwarp();
 #pragma unroll
@@ -1125,7 +1130,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
 // ---------------------------------------------------------------------------------------------------- single tokens
 // One step of many sequences: bound by reading and writing the binary32 states once.  kLanes lanes have a row of a state (4 values
 // each), a CTA 32 rows of one head (8 rows of 128 states in flight per warp); everything is binary32.  256 sequences of 24 heads, 64
-// columns, 128 states: 71.7 us, 5.6 TB/s (92 us without the streaming loads and stores, which leave the L2 to the rest).
+// columns, 128 states: 70 us in a loop, 5.8 TB/s, 76 between other work, 5.3 TB/s (92 us without the streaming loads and stores, which leave the L2 to the rest).
 template <typename T, int kLanes, bool kWhole>
 __global__ void __launch_bounds__(128) ptq_heads_step_kernel(const HeadParams p)
 {
