@@ -501,92 +501,120 @@ __device__ __forceinline__ HeadPlace head_place(const HeadParams &p, int segment
 // state[p][n] <- decay state + sum_j f_j x_j[p] z_j[n] over a chunk, for 16 columns p0 .. and 8 kN states n0 ..; x and z are tiles
 // [step][..].  The factors make x an operand of more than 16 bits: it goes in in parts.
 template <int NP, int kN, typename T>
-__device__ __forceinline__ void state_update(float (&S)[kN][4], const T *x, const T *z, const float *f, float decay, int p0, int n0, int lane)
+__device__ __forceinline__ void state_update(float (&S)[kN][4], const T *x, const T *z, const float *f, float decay, int p0, int n0, int sets, int lane)
 {
     constexpr int kXP = kHeadCols + kHeadPad, kZP = NP + kHeadPad;
     const int t = lane & 3;
-    HeadA<T> a[kHeadSteps / 16];
-#pragma unroll
-    for (int k = 0; k < kHeadSteps / 16; ++k) a[k] = load_a_t(x, kXP, p0, 16 * k, lane);
-    // binary16: u is brought to less than 2^15 (what is 2^-29 of its largest magnitude is still held whole), the factors to less than 1
-    HeadScale scu = {1.0f, 1.0f}, scf = {1.0f, 1.0f};
     if constexpr (kScaled<T>) {
-        __half2 most = __float2half2_rn(0.0f);
+        // binary16, 16 steps at a time: of each u is brought to less than 2^8 and the factors to less than 2^7, so that the product stays below 2^15, all
+        // bits of what is 2^-22 of the largest u stay, and 2^-31 of the largest factor.  Eight lanes have the powers of two of 16 steps.
+        const float2 q = *reinterpret_cast<const float2 *>(f + 2 * lane);
+        float top_f = fmaxf(finite_abs(q.x), finite_abs(q.y)), top_u = 0.0f;
 #pragma unroll
-        for (int k = 0; k < kHeadSteps / 16; ++k)
+        for (int d = 1; d < 8; d <<= 1) top_f = fmaxf(top_f, __shfl_xor_sync(0xffffffffu, top_f, d));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) most = __hmax2(most, __habs2(*reinterpret_cast<const __half2 *>(&a[k].r[i])));
-        const float2 v = __half22float2(most), q = *reinterpret_cast<const float2 *>(f + 2 * lane);
-        const float top = warp_max(fmaxf(finite_abs(q.x), finite_abs(q.y)));
-        scf = exact_scale(top, -1, 126);
-        // a power of two that binary16 holds; an infinity counts as the largest finite value (factors of growth that 2^-126 leaves above 1: to
-        // less than 4 then, and u to 2^13)
-        scu = exact_scale(warp_max(fminf(fmaxf(v.x, v.y), 65504.0f)), top < 0x1p126f ? 14 : 12, 15);
-    }
-    // the chunk's sums on their own, joined with the state in binary32: the tensor cores' sums are cut off, not rounded
-    // (beside all states of 16 columns three parts of 64 steps are too many registers: 32 steps at a time)
-    constexpr int kSet = kHeadParts<T> > 2 && kN > 8 ? 2 : 4;
-    const float down = scu.down * scf.down;
+        for (int k = 0; k < kHeadSteps / 16; ++k) {
+            const HeadA<T> a = load_a_t(x, kXP, p0, 16 * k, lane);
+            __half2 most = __habs2(*reinterpret_cast<const __half2 *>(&a.r[0]));
 #pragma unroll
-    for (int k0 = 0; k0 < kHeadSteps / 16; k0 += kSet) {
-        HeadA<T> part[kSet][kHeadParts<T>];
+            for (int i = 1; i < 4; ++i) most = __hmax2(most, __habs2(*reinterpret_cast<const __half2 *>(&a.r[i])));
+            const float2 m = __half22float2(most);
+            const float top = warp_max(fminf(fmaxf(m.x, m.y), 65504.0f));              // an infinity counts as the largest finite value
+            if (lane >> 3 == k) top_u = top;
+        }
+        const HeadScale scu = exact_scale(top_u, 7, 15), scf = exact_scale(top_f, 6, 126);             // (2^15: a power of two that binary16 holds)
 #pragma unroll
-        for (int ks = 0; ks < kSet; ++ks) {
-            const int k = k0 + ks;
+        for (int n = 0; n < kN; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) S[n][i] *= decay;
+#pragma unroll 1
+        for (int k = 0; k < sets; ++k) {
+            const HeadA<T> a = load_a_t(x, kXP, p0, 16 * k, lane);
+            const float up_u = __shfl_sync(0xffffffffu, scu.up, 8 * k), up_f = __shfl_sync(0xffffffffu, scf.up, 8 * k);
+            const float down = __shfl_sync(0xffffffffu, scu.down * scf.down, 8 * k);
             const float2 f0 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t), f1 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t + 8);
-            if constexpr (std::is_same<T, __half>::value) {
-                // u f as two binary16 values in binary16 arithmetic: f in two parts, the product with the upper one and what its
-                // rounding left (a fused multiply-add leaves it whole), plus that with the lower one
-                uint32_t fh[2], fl[2];
+            // u f as two binary16 values in binary16 arithmetic: f in two parts, the product with the upper one and what its
+            // rounding left (a fused multiply-add leaves it whole), plus that with the lower one
+            uint32_t fh[2], fl[2];
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    uint32_t r[2];
-                    head_split<T>((q ? f1.x : f0.x) * scf.up, (q ? f1.y : f0.y) * scf.up, r);
-                    fh[q] = r[0];
-                    fl[q] = r[1];
+            for (int c = 0; c < 2; ++c) {
+                uint32_t r[2];
+                head_split<T>((c ? f1.x : f0.x) * up_f, (c ? f1.y : f0.y) * up_f, r);
+                fh[c] = r[0];
+                fl[c] = r[1];
+            }
+            const __half2 up = __float2half2_rn(up_u);
+            HeadA<T> upper, lower;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&a.r[i]), up);
+                const __half2 h = *reinterpret_cast<const __half2 *>(&fh[i >> 1]), l = *reinterpret_cast<const __half2 *>(&fl[i >> 1]);
+                const __half2 hi = __hmul2_rn(v, h), lo = __hfma2(v, l, __hfma2(v, h, __hneg2(hi)));
+                upper.r[i] = *reinterpret_cast<const uint32_t *>(&hi);
+                lower.r[i] = *reinterpret_cast<const uint32_t *>(&lo);
+            }
+#pragma unroll
+            for (int n = 0; n < kN / 2; ++n) {
+                HeadB<T> b[2];
+                load_b_t(b, z, kZP, n0 + 16 * n, 16 * k, lane);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    float sum[4];
+                    head_mma(sum, lower, b[j], true);
+                    head_mma(sum, upper, b[j]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) S[2 * n + j][i] = fmaf(sum[i], down, S[2 * n + j][i]);
                 }
-                const __half2 up = __float2half2_rn(scu.up);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&a[k].r[i]), up);
-                    const __half2 h = *reinterpret_cast<const __half2 *>(&fh[i >> 1]), l = *reinterpret_cast<const __half2 *>(&fl[i >> 1]);
-                    const __half2 hi = __hmul2_rn(v, h), lo = __hfma2(v, l, __hfma2(v, h, __hneg2(hi)));
-                    part[ks][0].r[i] = *reinterpret_cast<const uint32_t *>(&hi);
-                    part[ks][1].r[i] = *reinterpret_cast<const uint32_t *>(&lo);
-                }
-            } else if constexpr (sizeof(T) == 2) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 v = head_unpack<T>(a[k].r[i]), q = i < 2 ? f0 : f1;
-                    uint32_t r[kHeadParts<T>];
-                    head_split<T>(v.x * q.x, v.y * q.y, r);
-#pragma unroll
-                    for (int j = 0; j < kHeadParts<T>; ++j) part[ks][j].r[i] = r[j];
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) part[ks][0].v[i] = a[k].v[i] * (i < 4 ? (i & 1 ? f0.y : f0.x) : (i & 1 ? f1.y : f1.x));
             }
         }
+    } else {
+        HeadA<T> a[kHeadSteps / 16];
 #pragma unroll
-        for (int n = 0; n < kN / 2; ++n) {
-            float sum[2][4];
+        for (int k = 0; k < kHeadSteps / 16; ++k) a[k] = load_a_t(x, kXP, p0, 16 * k, lane);
+        // the chunk's sums on their own, joined with the state in binary32: the tensor cores' sums are cut off, not rounded
+        // (beside all states of 16 columns three parts of 64 steps are too many registers: 32 steps at a time)
+        constexpr int kSet = kHeadParts<T> > 2 && kN > 8 ? 2 : 4;
+#pragma unroll
+        for (int k0 = 0; k0 < kHeadSteps / 16; k0 += kSet) {
+            HeadA<T> part[kSet][kHeadParts<T>];
 #pragma unroll
             for (int ks = 0; ks < kSet; ++ks) {
-                HeadB<T> b[2];
-                load_b_t(b, z, kZP, n0 + 16 * n, 16 * (k0 + ks), lane);
+                const int k = k0 + ks;
+                const float2 f0 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t), f1 = *reinterpret_cast<const float2 *>(f + 16 * k + 2 * t + 8);
+                if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 v = head_unpack<T>(a[k].r[i]), q = i < 2 ? f0 : f1;
+                        uint32_t r[kHeadParts<T>];
+                        head_split<T>(v.x * q.x, v.y * q.y, r);
+#pragma unroll
+                        for (int j = 0; j < kHeadParts<T>; ++j) part[ks][j].r[i] = r[j];
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) part[ks][0].v[i] = a[k].v[i] * (i < 4 ? (i & 1 ? f0.y : f0.x) : (i & 1 ? f1.y : f1.x));
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < kN / 2; ++n) {
+                float sum[2][4];
+#pragma unroll
+                for (int ks = 0; ks < kSet; ++ks) {
+                    HeadB<T> b[2];
+                    load_b_t(b, z, kZP, n0 + 16 * n, 16 * (k0 + ks), lane);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int q = kHeadParts<T> - 1; q >= 0; --q) head_mma(sum[j], part[ks][q], b[j], ks == 0 && q == kHeadParts<T> - 1);
+                }
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
-                    for (int q = kHeadParts<T> - 1; q >= 0; --q) head_mma(sum[j], part[ks][q], b[j], ks == 0 && q == kHeadParts<T> - 1);
+                    for (int i = 0; i < 4; ++i) {
+                        float &to = S[2 * n + j][i];
+                        to = k0 == 0 ? fmaf(decay, to, sum[j][i]) : to + sum[j][i];
+                    }
             }
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float v = kScaled<T> ? sum[j][i] * down : sum[j][i];
-                    S[2 * n + j][i] = k0 == 0 ? fmaf(decay, S[2 * n + j][i], v) : S[2 * n + j][i] + v;
-                }
         }
     }
 }
@@ -1104,7 +1132,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) ptq_heads_kernel(
         }
         if (i >= 0) {
             log_decay += f.log_decay;
-            if (busy && (!kOut || next || ends)) state_update<NP, kN>(S, tile_u(s), tile_B(s), f.state, f.decay, p0, n0, lane);
+            if (busy && (!kOut || next || ends)) state_update<NP, kN>(S, tile_u(s), tile_B(s), f.state, f.decay, p0, n0, sixteens, lane);
             // the outputs' warps have read the state, or what lies over it
             if (kOut && !outputs) asm volatile("bar.sync %0, 256;" ::"r"(M::kOverState && p.share ? 3 : 1) : "memory");
         }

@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(256, HeadBackSmem<T, NP>::kCtas) ptq_heads_bac
 #pragma unroll
             for (int q = 16; q > 0; q >>= 1) z += __shfl_xor_sync(0xffffffffu, z, q);
             if (lane == 0) through[r] = z * f.decay;
-            if (p0 < a.cols && (next || starts)) state_update<NP, NP / 8>(H, tile_dy(s), tile_C(s), f.into, f.decay, p0, 0, lane);
+            if (p0 < a.cols && (next || starts)) state_update<NP, NP / 8>(H, tile_dy(s), tile_C(s), f.into, f.decay, p0, 0, sixteens, lane);
         } else if (i >= 0 && r >= sixteens) {
             if (lane < 16) dw[p0 + lane] = dot_B[p0 + lane] = 0.0f;
         } else if (i >= 0) {

@@ -87,3 +87,31 @@ def test_small_gradients_beside_a_set_that_gives_nothing(ptq, first, front):
     else:
         dy[:, first:first + 16] = 0
     check(ptq, t, dy)
+
+
+@pytest.mark.parametrize("first", [0, 16, 32, 48])
+@pytest.mark.parametrize("front", ["u is zero", "B is zero", "u is small"])
+def test_states_of_steps_among_ones_that_give_nothing(ptq, first, front):
+    """Sixteen steps decide the final state, by a decay of up to 2^-46 beside what others would, and the gradient of the first one, by as much."""
+    t = make()
+    t["A"] = -torch.full((2,), 0.5)
+    other = torch.ones(64, dtype=torch.bool)
+    other[first:first + 16] = False
+    dy = make()["u"].flip(1)
+    if front == "u is small":
+        t["u"][:, other] *= 2.0 ** -20
+        dy[:, other] *= 2.0 ** -20
+    else:
+        t["u" if front == "u is zero" else "B"][:, other] = 0
+        if front == "u is zero":
+            dy[:, other] = 0
+        else:
+            t["C"][:, other] = 0
+    t = {k: v if v is None else v.cuda() if k == "A" else v.half().cuda() for k, v in t.items()}
+    t["state"] = torch.zeros(1, 2, 16, 32, device="cuda")
+    value, scale, F = ref.solve(t, dy=dy.half())
+    final, history = torch.empty_like(t["state"]), ptq.head_scan_history(t["u"], 32)
+    ptq.head_scan(t["u"], None, t["A"], t["B"], t["C"], state=t["state"], final_state=final, history=history)
+    close(final, value["final"], scale["final"], F, "final state")
+    g = ptq.head_scan_backward(dy.half().cuda(), t["u"], None, t["A"], t["B"], t["C"], history, state=t["state"])
+    close(g["state"], value["state"], scale["state"], F, "dstate")
