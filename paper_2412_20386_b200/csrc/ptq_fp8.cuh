@@ -139,8 +139,8 @@ __device__ __forceinline__ void store_codes8(uint8_t *row, int c, int cols, uint
 // (16 bytes of 16-bit values a lane), kSet neighbouring ones of a row at a time; the 16 half-warps of a CTA take 16 neighbouring rows,
 // whose scales lie next to each other in the layout that the product reads.  CTAs, as many as the SMs hold, go over the rows with the loads
 // of the next set under way while one is worked on; one division makes all scales of a step.  (One set per CTA and a division per block:
-// 26.7 us where this takes 20.7.)  50432 rows of 768 bfloat16 channels: 20.7 us where the same rows come again, 5.7 TB/s, 22.7 to 23.8 on others each time,
-// 5.0 to 5.2 TB/s; of 1536 channels 41.3 and 43.0 us, 5.7 and 5.5 TB/s.
+// 26.7 us where this takes 20.7.)  50432 rows of 768 bfloat16 channels: 20.7 us where the same rows come again, 5.7 TB/s, 22.7 to 24.0 on others each time,
+// 4.9 to 5.2 TB/s; of 1536 channels 41.3 and 43.0 us, 5.7 and 5.5 TB/s.
 struct Fp8QuantizeParams {
     const void *x;
     int64_t x_pitch, codes_pitch, scale_row, scale_block;

@@ -24,8 +24,8 @@
 // of itself, as y is of y.  Against 64 bits y is off by 2.5e-4 of its size in binary16 and 2.1e-3 in bfloat16, where y rounded alone is by 2.1e-4 and
 // 1.7e-3; the results of a training step by 2.9e-4 and 2.3e-3.  Operands in two parts would be half as many products again.
 //
-// What bounds it: the latency of dependent instructions.  128 x 197 x 12 heads of 64 columns, 128 states, binary16: 133 us, 0.7 TB/s of the
-// bytes that count and 94 TFLOP/s; issue slots 42 % busy, the tensor pipe 33 %, stalls fixed latency 2.1, barriers 2.0, shared
+// What bounds it: the latency of dependent instructions.  128 x 197 x 12 heads of 64 columns, 128 states, binary16: 134 us, 0.7 TB/s of the
+// bytes that count and 93 TFLOP/s; issue slots 42 % busy, the tensor pipe 33 %, stalls fixed latency 2.1, barriers 2.0, shared
 // memory 1.5 per instruction.  The states and sums of a CTA fill half of an SM's registers, so two CTAs are all there are.  One warp for 16
 // steps and 16 columns of the state (four warps to a CTA) took 235 us; roles of warps of their own, factors formed a chunk ahead by
 // one warp, 16 earlier steps at a time and separate kernels for aligned rows (instruction cache) made the difference.  The factors on

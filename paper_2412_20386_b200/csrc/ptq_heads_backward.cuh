@@ -16,7 +16,7 @@
 //
 // What bounds it: latency again, at two CTAs to an SM (up to 64 states, 16 bits; else one), and fetching instructions: issue slots 33 %
 // busy, the tensor pipe 20 %, stalls barriers 2.7, no instruction 2.5, fixed latency 1.7, shared memory 1.5 per instruction.  64 x 197 x 12
-// heads of 64 columns, 64 states, binary16: 170 us (all kernels of the step, forward included, 249).  Loops that are not unrolled over sets of 16 steps took it from 386 to 320 us
+// heads of 64 columns, 64 states, binary16: 172 us (all kernels of the step, forward included, 249).  Loops that are not unrolled over sets of 16 steps took it from 386 to 320 us
 // (the step), shared factors and a second CTA to 295.  binary32: 8 x 784 x 6 heads, 16 states, 188 us for the step; splitting operands into tf32
 // parts is most of the instructions.
 #pragma once
